@@ -50,7 +50,8 @@ typedef struct {
 
 typedef enum {
   IM2WIN_F32 = 0,       /* 4-byte elements, IEEE binary32 */
-  IM2WIN_F16 = 1        /* 2-byte elements, IEEE binary16 */
+  IM2WIN_F16 = 1,       /* 2-byte elements, IEEE binary16 */
+  IM2WIN_BF16 = 2       /* 2-byte elements, the upper half of binary32; the operators on token sequences only */
 } im2win_dtype;
 
 typedef enum {
@@ -341,6 +342,67 @@ const char* im2win_nhwc_kernel_name(const im2win_shape* shape, const im2win_epil
 #define IM2WIN_STATIC_SCRATCH_BYTES (4u << 20)
 im2win_status im2win_conv_f32_static(const float* window, const float* filter_oihw, float* y_nchw,
                                      const im2win_shape* shape, void* cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Operators on token sequences (the paper has no counterpart): what a model
+ * whose layers are windows and recurrences over a sequence of tokens computes
+ * between its dense layers when it answers prompts and generates.  Like the
+ * convolution they are forward only, work on buffers the caller owns, and what
+ * a sequence carries from one call to the next (the rows its window still
+ * needs, the matrix of its recurrence) lies in a pool of states of the caller.
+ *
+ * Rows of tokens are packed: sequence b takes rows cu_seqlens[b] up to (not
+ * including) cu_seqlens[b+1] of every tensor, or, without cu_seqlens, the b-th
+ * of `sequences` equal parts.  A sequence may have no rows, or one (the next
+ * token of a generation).  Rows behind the last sequence are neither read nor
+ * written.  cu_seqlens lies in device memory and is not looked at by the host:
+ * it has to begin at 0, never fall, and stay within `tokens`; values that
+ * break this leave the affected results undefined, but nothing outside the
+ * buffers is read or written.
+ *
+ * Sequence b keeps its state in element slots[b] of the pools (without
+ * `slots`: element b).  One whose slot is negative, or not below the number of
+ * states in a pool, is padding: its rows and its state are neither read nor
+ * written, so a call captured for a batch can be replayed for a smaller one.
+ * Two sequences of one call must not name the same slot.  Sequence b starts
+ * from state_in where resume[b] is not 0 (without `resume`: every sequence
+ * does), else, and where state_in is NULL, from zeros.  state_out receives the
+ * state behind the last row (of a sequence without rows: the one it started
+ * from); it may be NULL, and it may be state_in itself.  Elements that no
+ * sequence of the call names stay as they are.
+ */
+typedef struct {
+  const int32_t* cu_seqlens;  /* DEVICE pointer to sequences + 1 row numbers, or NULL     */
+  const int32_t* slots;       /* DEVICE pointer to sequences pool elements, or NULL       */
+  const uint8_t* resume;      /* DEVICE pointer to sequences flags (0 or 1), or NULL      */
+} im2win_sequences;
+
+typedef struct {
+  int32_t tokens;             /* rows of x and y (>= 0)                                   */
+  int32_t sequences;          /* >= 1; divides tokens where there is no cu_seqlens        */
+  int32_t slots;              /* states in each pool; 0 without pools and without slots   */
+  int32_t channels;           /* >= 1                                                     */
+  int32_t taps;               /* 1 to 8                                                   */
+  int32_t silu;               /* 0 or 1                                                   */
+  int64_t x_stride, y_stride; /* elements from a row to the next one (>= channels)        */
+} im2win_conv1d_shape;
+
+/*
+ * Causal depthwise convolution along the tokens, the one-dimensional window
+ * product of the channel-innermost form with a filter for each channel:
+ *     z[t][c] = bias[c] + sum_{i < taps} weight[c][i] * x[t - (taps-1) + i][c],
+ *     y = z, or z / (1 + exp(-z)) (if silu),
+ * where the taps-1 rows before a sequence's first are those of its state (or
+ * zeros) and no row of another sequence is ever met.  x, weight [channels]
+ * [taps], y and the states [slots][taps-1][channels] hold elements of `dtype`
+ * (any of the three); bias holds floats or is NULL.  Sums are fp32, y is
+ * rounded once, states are copied bit for bit.  `seqs` may be NULL.  The
+ * pointers need the alignment of their elements only; rows that start on
+ * 16-byte boundaries and hold whole 16-byte vectors are the fast ones.
+ */
+im2win_status im2win_causal_conv1d(const void* x, const void* weight, const float* bias, void* y,
+                                   const void* state_in, void* state_out, const im2win_sequences* seqs,
+                                   const im2win_conv1d_shape* shape, im2win_dtype dtype, void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -17,6 +17,7 @@ from . import build as _build
 
 F32 = 0
 F16 = 1
+BF16 = 2      # the operators on token sequences only
 
 STATUS_NAMES = {
     0: "IM2WIN_OK", 1: "IM2WIN_ERR_INVALID_ARG", 2: "IM2WIN_ERR_NULL_POINTER", 3: "IM2WIN_ERR_MISALIGNED",
@@ -28,7 +29,7 @@ EXPORTS = (
     "im2win_check_status", "im2win_layer_workspace_size", "im2win_layer_forward_host",
     "im2win_conv_f32_static", "im2win_pack_filter", "im2win_conv_packed", "im2win_conv_kernel_name", "im2win_nhwc_kernel_name",
     "im2win_nhwc_workspace_size", "im2win_transform_nhwc", "im2win_conv_f16_nhwc", "im2win_pack_filter_nhwc",
-    "im2win_conv_packed_nhwc",
+    "im2win_conv_packed_nhwc", "im2win_causal_conv1d",
 )
 
 STATIC_SCRATCH_BYTES = 4 << 20
@@ -47,6 +48,17 @@ class Epilogue(ctypes.Structure):
 
     _fields_ = [("bias", ctypes.c_void_p), ("relu", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
                 ("out_layout", ctypes.c_int32)]
+
+
+class Sequences(ctypes.Structure):
+    """im2win_sequences: device pointers to row numbers, pool elements and flags, each NULL or one a sequence."""
+
+    _fields_ = [("cu_seqlens", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("resume", ctypes.c_void_p)]
+
+
+class Conv1dShape(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("tokens", "sequences", "slots", "channels", "taps", "silu")] + \
+               [(k, ctypes.c_int64) for k in ("x_stride", "y_stride")]
 
 
 class Im2winError(RuntimeError):
@@ -88,6 +100,7 @@ def lib() -> ctypes.CDLL:
     L.im2win_conv_f16_nhwc.argtypes = [vp, vp, vp, P(Epilogue), vp, sz, P(Shape), vp]
     L.im2win_pack_filter_nhwc.argtypes = [vp, vp, sz, P(Shape), vp]
     L.im2win_conv_packed_nhwc.argtypes = [vp, vp, P(Epilogue), vp, sz, P(Shape), vp]
+    L.im2win_causal_conv1d.argtypes = [vp, vp, vp, vp, vp, vp, P(Sequences), P(Conv1dShape), ctypes.c_int, vp]
     for name in EXPORTS[1:]:
         getattr(L, name).restype = ctypes.c_int
     L.im2win_conv_kernel_name.restype = ctypes.c_char_p
@@ -356,6 +369,125 @@ def alloc_nhwc_buffers(shape, out_dtype: torch.dtype = torch.float32, out_layout
     yshape = (s.N, s.Co, ho, wo) if out_layout == NCHW else (s.N, ho, wo, s.Co)
     y = torch.empty(yshape, dtype=out_dtype, device=device)
     return window, scratch, y
+
+
+# ------------------------------------------------------- operators on token sequences
+# Rows of tokens are given packed, as [tokens, ...] with `cu_seqlens`, or as [sequences, tokens of each, ...]; [tokens, ...] without
+# `cu_seqlens` is one token of each of `tokens` sequences (the next token of a generation).  See include/im2win.h.
+_SEQUENCE_DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+
+
+def _sequence_dtype(dtype: torch.dtype) -> int:
+    code = _SEQUENCE_DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return code
+
+
+def _on_current_device(*tensors) -> None:
+    """The kernels are launched on the current device: tensors of another one, or of the host, are refused."""
+    device = None
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if at != device:
+                if at < 0:
+                    raise ValueError("tensors have to be on a CUDA device")
+                if device is not None or at != _device():
+                    raise ValueError("tensors have to be on the current device (see torch.cuda.device)")
+                device = at
+
+
+def _row_stride(t: torch.Tensor, inner: int, name: str) -> int:
+    """Elements from a row of t to the next one: its last `inner` (1 or 2) dimensions are a row, dense; those before them count rows."""
+    shape, stride = t.shape, t.stride()
+    width = shape[-1]
+    if stride[-1] != 1 and width != 1:
+        raise ValueError(f"{name}: the elements of a row have to lie one behind the other")
+    if inner == 2:
+        if shape[-2] != 1 and stride[-2] != width:
+            raise ValueError(f"{name}: the heads of a row have to lie one behind the other")
+        width *= shape[-2]
+    n = len(shape) - inner
+    if n == 2:
+        if shape[0] > 1 and shape[1] > 1:
+            if stride[0] != shape[1] * stride[1]:
+                raise ValueError(f"{name}: the sequences have to lie one behind the other")
+            return stride[1]
+        return stride[1] if shape[1] > 1 else stride[0] if shape[0] > 1 else width
+    return stride[0] if shape[0] > 1 else width
+
+
+def _take_sequences(rows, cu_seqlens, slots, resume, state, state_out):
+    """(tokens, sequences, states in a pool, pointer to im2win_sequences or None) for tensors with the leading dimensions `rows`."""
+    pool = 0
+    if cu_seqlens is not None:
+        if len(rows) != 1:
+            raise ValueError("with cu_seqlens the tokens are the one leading dimension")
+        if cu_seqlens.dtype != torch.int32 or cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2 or not cu_seqlens.is_contiguous():
+            raise ValueError("cu_seqlens: sequences + 1 int32 values")
+        tokens, sequences = rows[0], cu_seqlens.numel() - 1
+    else:
+        sequences = rows[0]
+        tokens = sequences if len(rows) == 1 else sequences * rows[1]
+        if sequences < 1:
+            raise ValueError("there has to be a sequence")
+    if tokens >= 1 << 31:
+        raise ValueError("fewer than 2^31 tokens")
+    for p in (state, state_out):
+        if p is not None:
+            if not p.is_contiguous():
+                raise ValueError("state and state_out have to be contiguous")
+            if p.shape[0] < 1 or (pool and p.shape[0] != pool):
+                raise ValueError("state and state_out have to hold as many states")
+            pool = p.shape[0]
+    if slots is not None:
+        if slots.dtype != torch.int32 or slots.dim() != 1 or slots.numel() != sequences or not slots.is_contiguous():
+            raise ValueError("slots: an int32 value for each sequence")
+        pool = pool or 0x7fffffff
+    elif pool and pool < sequences:
+        raise ValueError("the pool has fewer states than there are sequences")
+    if resume is not None and (resume.dtype not in (torch.bool, torch.uint8) or resume.dim() != 1 or resume.numel() != sequences
+                               or not resume.is_contiguous()):
+        raise ValueError("resume: a flag for each sequence")
+    if cu_seqlens is None and slots is None and resume is None:
+        return tokens, sequences, pool, None
+    return tokens, sequences, pool, ctypes.byref(Sequences(_ptr(cu_seqlens), _ptr(slots), _ptr(resume)))
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def im2win_causal_conv1d(x, weight, y, bias=None, silu: bool = False, state=None, state_out=None, cu_seqlens=None, slots=None,
+                         resume=None, stream=None) -> None:
+    """Causal depthwise convolution along the tokens into y: x and y [tokens, channels] or [sequences, tokens, channels], weight
+    [channels, taps], bias float32 [channels], state and state_out [slots, taps - 1, channels] (may be one tensor)."""
+    dtype = x.dtype
+    code = _sequence_dtype(dtype)
+    _on_current_device(x, weight, y, bias, state, state_out, cu_seqlens, slots, resume)
+    shape = x.shape
+    if not 2 <= len(shape) <= 3 or y.shape != shape:
+        raise ValueError("x and y: [tokens, channels] or [sequences, tokens, channels]")
+    channels = shape[-1]
+    if weight.dim() != 2 or weight.shape[0] != channels or not weight.is_contiguous():
+        raise ValueError("weight: [channels, taps], contiguous")
+    taps = weight.shape[1]
+    if weight.dtype != dtype or y.dtype != dtype:
+        raise ValueError("x, weight and y have to be of one dtype")
+    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (channels,) or not bias.is_contiguous()):
+        raise ValueError("bias: [channels] of float32")
+    for p in (state, state_out):
+        if p is not None and (p.dtype != dtype or p.shape[1:] != (taps - 1, channels)):
+            raise ValueError("state and state_out: [slots, taps - 1, channels] of x's dtype")
+    tokens, sequences, pool, seqs = _take_sequences(shape[:-1], cu_seqlens, slots, resume, state, state_out)
+    sizes = Conv1dShape(tokens, sequences, pool, channels, taps, 1 if silu else 0, _row_stride(x, 1, "x"), _row_stride(y, 1, "y"))
+    if taps == 1:                                            # nothing is carried
+        state = state_out = None
+    code = lib().im2win_causal_conv1d(x.data_ptr(), weight.data_ptr(), _ptr(bias), y.data_ptr(), _ptr(state), _ptr(state_out), seqs,
+                                      ctypes.byref(sizes), code, _stream(stream))
+    if code:
+        _check(code, "im2win_causal_conv1d")
 
 
 # ---------------------------------------------------------------- conveniences

@@ -1,0 +1,84 @@
+"""Plain implementations, in 64 bits on the CPU, of the operators on token sequences, and what their tests share."""
+import math
+
+import torch
+
+from gpu_helpers import GUARD
+
+DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def half_step(dtype):
+    """The largest relative error of one rounding to nearest."""
+    return torch.finfo(dtype).eps / 2
+
+
+def rounding(y, dtype):
+    """The largest error of rounding y (float64) once to dtype: relative, or half a subnormal step."""
+    info = torch.finfo(dtype)
+    return y.abs() * half_step(dtype) + info.tiny * info.eps / 2
+
+
+def sequence_list(lengths, slots=None, resume=None):
+    """(first row, length, slot or None for padding, whether it resumes) of each sequence."""
+    at, out = 0, []
+    for b, n in enumerate(lengths):
+        slot = b if slots is None else slots[b]
+        out.append((at, n, slot, True if resume is None else bool(resume[b])))
+        at += n
+    return out
+
+
+def conv1d_64(x, weight, bias, silu, y, state, state_out, sequences, pool):
+    """The definition, row by row; y and state_out: what lay there before.  Also returns the sums of magnitudes that bound fp32 sums."""
+    x, w = x.double(), weight.double()
+    y, bound = y.double().clone(), torch.zeros_like(y, dtype=torch.float64)
+    state_out = None if state_out is None else state_out.double().clone()
+    taps = w.shape[1]
+    for first, n, slot, resumes in sequences:
+        if not 0 <= slot < pool:
+            continue
+        old = state[slot].double() if state is not None and resumes else torch.zeros(taps - 1, x.shape[1], dtype=torch.float64)
+        whole = torch.cat([old, x[first:first + n]])
+        for t in range(n):
+            window = whole[t:t + taps]
+            z = (window * w.T).sum(0)
+            a = (window.abs() * w.T.abs()).sum(0)
+            if bias is not None:
+                z, a = z + bias.double(), a + bias.double().abs()
+            y[first + t] = z / (1 + torch.exp(-z)) if silu else z
+            bound[first + t] = a
+        if state_out is not None and taps > 1:
+            state_out[slot] = whole[n:]
+    return y, state_out, bound
+
+
+class Guarded:
+    """A device tensor with canaries before and behind it (values that no kernel computes), and rows as far apart as wanted."""
+
+    def __init__(self, shape, dtype, pitch=0, fill=-77.0, shift=0):
+        width = math.prod(shape[1:])
+        self.shape, self.fill, self.shift = shape, fill, shift
+        self.pitch = width + pitch
+        self.whole = torch.full((2 * GUARD + shift + shape[0] * self.pitch,), fill, dtype=dtype, device="cuda")
+        inner = [1]
+        for n in reversed(shape[2:]):
+            inner.insert(0, inner[0] * n)
+        self.view = self.whole.as_strided(shape, [self.pitch] + inner if len(shape) > 1 else [1], GUARD + shift)
+
+    def assert_untouched_outside(self):
+        whole = self.whole.clone()
+        whole.as_strided(self.view.shape, self.view.stride(), GUARD + self.shift).fill_(self.fill)
+        assert bool((whole == self.fill).all()), "written outside the tensor"
+
+
+def close(got, want, bound, what):
+    """got within bound of want, element by element; NaN and infinities where want has them."""
+    got, want = got.double().cpu(), want.cpu()
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaNs elsewhere"
+    rest = ~fine & ~torch.isnan(want)
+    assert torch.equal(got[rest], want[rest]), f"{what}: infinities elsewhere"
+    err = (got - want).abs()[fine]
+    over = err > bound.cpu()[fine]
+    assert not bool(over.any()), f"{what}: {int(over.sum())} of {over.numel()} off, the largest error {float(err.max()):.3g}"
