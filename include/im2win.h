@@ -404,6 +404,49 @@ im2win_status im2win_causal_conv1d(const void* x, const void* weight, const floa
                                    const void* state_in, void* state_out, const im2win_sequences* seqs,
                                    const im2win_conv1d_shape* shape, im2win_dtype dtype, void* cuda_stream);
 
+typedef struct {
+  int32_t tokens;             /* rows of q, k, v, log_decay and o (>= 0)                  */
+  int32_t sequences;          /* >= 1; divides tokens where there is no cu_seqlens        */
+  int32_t slots;              /* states in each pool; 0 without pools and without slots   */
+  int32_t max_len;            /* rows of the longest sequence, or 0: unknown              */
+  int32_t heads;              /* heads of v and o                                         */
+  int32_t qk_heads;           /* heads of q and k; divides heads                          */
+  int32_t dk, dv;             /* elements of a q or k row (1 to 256), of a v or o row     */
+  float scale;
+  int64_t q_stride, k_stride, v_stride, o_stride;     /* elements from a row to the next  */
+  int64_t decay_stride;       /* floats from a row of log_decay to the next; 0: one decay
+                                 for each head, the same for every token                  */
+} im2win_attention_shape;
+
+/*
+ * Linear attention with a decay for each head.  Head h of a row t of sequence
+ * b, with q and k of head h / (heads / qk_heads):
+ *     S_t = exp(log_decay[t][h]) * S_{t-1} + k_t^T v_t,      S [dk][dv],
+ *     o_t = scale * q_t S_t.
+ * q and k are [tokens][qk_heads][dk], v and o [tokens][heads][dv], with
+ * elements of `dtype` (any of the three) and the heads of a row one behind the
+ * other; log_decay holds floats (normally <= 0; -infinity empties the state);
+ * the states [slots][heads][dk][dv] are fp32 and 16-byte aligned, and so is
+ * `workspace`.  A max_len below the longest sequence's rows leaves results
+ * undefined, but nothing outside the buffers is read or written.
+ *
+ * The states are fp32 to within a few units of their last place, o is rounded
+ * once from fp32 sums.  Sums are in a fixed order: the same call gives the
+ * same bits.
+ *
+ * `workspace` needs the bytes of im2win_linear_attention_workspace_size; it
+ * starts with a status block as a convolution's scratch does (cleared by the
+ * call; see im2win_check_status).  Nothing in it outlives the call, but calls
+ * that may overlap on the GPU need one each.
+ */
+im2win_status im2win_linear_attention_workspace_size(const im2win_attention_shape* shape, im2win_dtype dtype, size_t* bytes);
+im2win_status im2win_linear_attention(const void* q, const void* k, const void* v, const float* log_decay, void* o,
+                                      const float* state_in, float* state_out, const im2win_sequences* seqs,
+                                      void* workspace, size_t workspace_bytes, const im2win_attention_shape* shape,
+                                      im2win_dtype dtype, void* cuda_stream);
+/* "tokens" (the recurrence as it stands); "none" for an invalid shape.  Host-only, static storage; for reports and tests. */
+const char* im2win_linear_attention_kernel_name(const im2win_attention_shape* shape, im2win_dtype dtype);
+
 #ifdef __cplusplus
 }
 #endif

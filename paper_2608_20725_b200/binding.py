@@ -29,7 +29,8 @@ EXPORTS = (
     "im2win_check_status", "im2win_layer_workspace_size", "im2win_layer_forward_host",
     "im2win_conv_f32_static", "im2win_pack_filter", "im2win_conv_packed", "im2win_conv_kernel_name", "im2win_nhwc_kernel_name",
     "im2win_nhwc_workspace_size", "im2win_transform_nhwc", "im2win_conv_f16_nhwc", "im2win_pack_filter_nhwc",
-    "im2win_conv_packed_nhwc", "im2win_causal_conv1d",
+    "im2win_conv_packed_nhwc", "im2win_causal_conv1d", "im2win_linear_attention",
+    "im2win_linear_attention_workspace_size", "im2win_linear_attention_kernel_name",
 )
 
 STATIC_SCRATCH_BYTES = 4 << 20
@@ -59,6 +60,12 @@ class Sequences(ctypes.Structure):
 class Conv1dShape(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int32) for k in ("tokens", "sequences", "slots", "channels", "taps", "silu")] + \
                [(k, ctypes.c_int64) for k in ("x_stride", "y_stride")]
+
+
+class AttentionShape(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("tokens", "sequences", "slots", "max_len", "heads", "qk_heads", "dk", "dv")] + \
+               [("scale", ctypes.c_float)] + \
+               [(k, ctypes.c_int64) for k in ("q_stride", "k_stride", "v_stride", "o_stride", "decay_stride")]
 
 
 class Im2winError(RuntimeError):
@@ -101,11 +108,15 @@ def lib() -> ctypes.CDLL:
     L.im2win_pack_filter_nhwc.argtypes = [vp, vp, sz, P(Shape), vp]
     L.im2win_conv_packed_nhwc.argtypes = [vp, vp, P(Epilogue), vp, sz, P(Shape), vp]
     L.im2win_causal_conv1d.argtypes = [vp, vp, vp, vp, vp, vp, P(Sequences), P(Conv1dShape), ctypes.c_int, vp]
+    L.im2win_linear_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, P(Sequences), vp, sz, P(AttentionShape), ctypes.c_int, vp]
+    L.im2win_linear_attention_workspace_size.argtypes = [P(AttentionShape), ctypes.c_int, P(sz)]
     for name in EXPORTS[1:]:
         getattr(L, name).restype = ctypes.c_int
     L.im2win_conv_kernel_name.restype = ctypes.c_char_p
     L.im2win_nhwc_kernel_name.argtypes = [P(Shape), P(Epilogue)]
     L.im2win_nhwc_kernel_name.restype = ctypes.c_char_p
+    L.im2win_linear_attention_kernel_name.argtypes = [P(AttentionShape), ctypes.c_int]
+    L.im2win_linear_attention_kernel_name.restype = ctypes.c_char_p
     # the library looks at IM2WIN_DEBUG in its first plan: here, so that both sides see the same
     _debug = bool(os.environ.get("IM2WIN_DEBUG"))
     L.im2win_conv_kernel_name(ctypes.byref(Shape(1, 64, 1, 1, 1, 1, 1, 1, 0)), F32)
@@ -488,6 +499,68 @@ def im2win_causal_conv1d(x, weight, y, bias=None, silu: bool = False, state=None
                                       ctypes.byref(sizes), code, _stream(stream))
     if code:
         _check(code, "im2win_causal_conv1d")
+
+
+def make_attention_shape(tokens, sequences, heads, qk_heads, dk, dv, max_len=0) -> AttentionShape:
+    """The sizes that im2win_linear_attention's workspace depends on."""
+    return AttentionShape(int(tokens), int(sequences), 0, int(max_len), int(heads), int(qk_heads), int(dk), int(dv), 1.0, 0, 0, 0, 0, 0)
+
+
+def im2win_linear_attention_workspace_size(shape: AttentionShape, dtype: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().im2win_linear_attention_workspace_size(ctypes.byref(shape), dtype, ctypes.byref(n)),
+           "im2win_linear_attention_workspace_size")
+    return n.value
+
+
+def im2win_linear_attention_kernel_name(shape: AttentionShape, dtype: int) -> str:
+    """How im2win_linear_attention runs these sizes (for reports and tests)."""
+    return lib().im2win_linear_attention_kernel_name(ctypes.byref(shape), dtype).decode()
+
+
+def alloc_attention_workspace(shape: AttentionShape, dtype: torch.dtype, device="cuda") -> torch.Tensor:
+    """A workspace for im2win_linear_attention, with torch (device memory only)."""
+    return torch.empty(im2win_linear_attention_workspace_size(shape, _sequence_dtype(dtype)), dtype=torch.uint8, device=device)
+
+
+def im2win_linear_attention(q, k, v, log_decay, o, workspace, scale: float = 1.0, state=None, state_out=None, cu_seqlens=None,
+                            slots=None, resume=None, max_len: int = 0, stream=None) -> None:
+    """Linear attention with a decay for each head into o: q and k [tokens, qk_heads, dk] or [sequences, tokens, qk_heads, dk], v and o
+    the same with heads and dv, log_decay float32 [tokens, heads] (or [sequences, tokens, heads]) or [heads], state and state_out float32
+    [slots, heads, dk, dv] (may be one tensor), workspace from alloc_attention_workspace for these sizes and max_len."""
+    dtype = q.dtype
+    code = _sequence_dtype(dtype)
+    _on_current_device(q, k, v, log_decay, o, workspace, state, state_out, cu_seqlens, slots, resume)
+    if k.dtype != dtype or v.dtype != dtype or o.dtype != dtype:
+        raise ValueError("q, k, v and o have to be of one dtype")
+    qs, vs = q.shape, v.shape
+    if not 3 <= len(qs) <= 4 or k.shape != qs or o.shape != vs or vs[:-2] != qs[:-2]:
+        raise ValueError("q and k: [..., tokens, qk_heads, dk], v and o: [..., tokens, heads, dv]")
+    qk_heads, dk = qs[-2:]
+    heads, dv = vs[-2:]
+    gs = log_decay.shape
+    if log_decay.dtype != torch.float32 or (gs != vs[:-1] and gs != (heads,)):
+        raise ValueError("log_decay: [..., tokens, heads] or [heads] of float32")
+    for p in (state, state_out):
+        if p is not None and (p.dtype != torch.float32 or p.shape[1:] != (heads, dk, dv)):
+            raise ValueError("state and state_out: [slots, heads, dk, dv] of float32")
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous, of uint8")
+    tokens, sequences, pool, seqs = _take_sequences(qs[:-2], cu_seqlens, slots, resume, state, state_out)
+    strides = log_decay.stride()
+    if len(gs) == 1 or (tokens > 1 and all(n == 1 or step == 0 for n, step in zip(gs[:-1], strides))):
+        decay_stride = 0                                     # one decay for each head (it may be an expanded view)
+        if heads > 1 and strides[-1] != 1:
+            raise ValueError("log_decay: the heads have to lie one behind the other")
+    else:
+        decay_stride = _row_stride(log_decay, 1, "log_decay")
+    sizes = AttentionShape(tokens, sequences, pool, max_len, heads, qk_heads, dk, dv, scale, _row_stride(q, 2, "q"), _row_stride(k, 2, "k"),
+                           _row_stride(v, 2, "v"), _row_stride(o, 2, "o"), decay_stride)
+    code = lib().im2win_linear_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), o.data_ptr(), _ptr(state),
+                                         _ptr(state_out), seqs, workspace.data_ptr(), workspace.nbytes, ctypes.byref(sizes),
+                                         code, _stream(stream))
+    if code:
+        _check(code, "im2win_linear_attention")
 
 
 # ---------------------------------------------------------------- conveniences

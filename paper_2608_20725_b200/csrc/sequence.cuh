@@ -109,4 +109,20 @@ cudaError_t launch_causal_conv1d(const void* x, const void* weight, const float*
                                  void* state_out, const Sequences& seqs, const im2win_conv1d_shape& shape, im2win_dtype dtype,
                                  cudaStream_t stream);
 
+
+struct AttentionArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const float* decay;
+  void* o;
+  const float* state_in;
+  float* state_out;
+  void* workspace;
+  Sequences seqs;
+  im2win_attention_shape shape;
+  im2win_dtype dtype;
+};
+cudaError_t launch_attention_tokens(const AttentionArgs& a, cudaStream_t stream);
+
 }  // namespace im2win

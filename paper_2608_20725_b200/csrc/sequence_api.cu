@@ -31,6 +31,15 @@ im2win_status from_launch(cudaError_t e) {
   return e == cudaSuccess ? IM2WIN_OK : IM2WIN_ERR_CUDA;
 }
 
+im2win_status check_attention(const im2win_attention_shape* s, im2win_dtype dtype) {
+  if (!s) return IM2WIN_ERR_NULL_POINTER;
+  if (!known_dtype(dtype) || s->tokens < 0 || s->sequences < 1 || s->slots < 0 || s->max_len < 0 || s->heads < 1 ||
+      s->qk_heads < 1 || s->heads % s->qk_heads != 0 || s->dk < 1 || s->dv < 1)
+    return IM2WIN_ERR_INVALID_ARG;
+  if (s->dk > 256 || (int64_t)s->heads * s->dv >= kMost || (int64_t)s->heads * s->dk >= kMost) return IM2WIN_ERR_UNSUPPORTED;
+  return IM2WIN_OK;
+}
+
 }  // namespace
 }  // namespace im2win
 
@@ -56,6 +65,44 @@ im2win_status im2win_causal_conv1d(const void* x, const void* weight, const floa
   if (!aligned_to(bias, 4)) return IM2WIN_ERR_MISALIGNED;
   return from_launch(launch_causal_conv1d(x, weight, bias, y, state_in, state_out, s, *shape, dtype,
                                           static_cast<cudaStream_t>(cuda_stream)));
+}
+
+im2win_status im2win_linear_attention_workspace_size(const im2win_attention_shape* shape, im2win_dtype dtype, size_t* bytes) {
+  const im2win_status st = check_attention(shape, dtype);
+  if (st != IM2WIN_OK) return st;
+  if (bytes) *bytes = 256;
+  return IM2WIN_OK;
+}
+
+const char* im2win_linear_attention_kernel_name(const im2win_attention_shape* shape, im2win_dtype dtype) {
+  return check_attention(shape, dtype) == IM2WIN_OK ? "tokens" : "none";
+}
+
+im2win_status im2win_linear_attention(const void* q, const void* k, const void* v, const float* log_decay, void* o,
+                                      const float* state_in, float* state_out, const im2win_sequences* seqs, void* workspace,
+                                      size_t workspace_bytes, const im2win_attention_shape* shape, im2win_dtype dtype,
+                                      void* cuda_stream) {
+  if (!shape || !workspace) return IM2WIN_ERR_NULL_POINTER;
+  im2win_status st = check_attention(shape, dtype);
+  if (st != IM2WIN_OK) return st;
+  const int64_t qk_row = (int64_t)shape->qk_heads * shape->dk, v_row = (int64_t)shape->heads * shape->dv;
+  if (shape->q_stride < qk_row || shape->k_stride < qk_row || shape->v_stride < v_row || shape->o_stride < v_row ||
+      (shape->decay_stride != 0 && shape->decay_stride < shape->heads))
+    return IM2WIN_ERR_INVALID_ARG;
+  AttentionArgs a = {q, k, v, log_decay, o, state_in, state_out, workspace, {}, *shape, dtype};
+  st = take_sequences(seqs, shape->tokens, shape->sequences, shape->slots, state_in || state_out, &a.seqs);
+  if (st != IM2WIN_OK) return st;
+  if (shape->tokens > 0 && (!q || !k || !v || !log_decay || !o)) return IM2WIN_ERR_NULL_POINTER;
+  const size_t es = element_bytes(dtype);
+  for (const void* at : {q, k, v, (const void*)o})
+    if (!aligned_to(at, es)) return IM2WIN_ERR_MISALIGNED;
+  if (!aligned_to(log_decay, 4) || !aligned_to(state_in, 16) || !aligned_to(state_out, 16) || !aligned_to(workspace, 16))
+    return IM2WIN_ERR_MISALIGNED;
+  size_t need = 0;
+  st = im2win_linear_attention_workspace_size(shape, dtype, &need);
+  if (st != IM2WIN_OK) return st;
+  if (workspace_bytes < need) return IM2WIN_ERR_WORKSPACE_TOO_SMALL;
+  return from_launch(launch_attention_tokens(a, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 }  // extern "C"

@@ -82,3 +82,31 @@ def close(got, want, bound, what):
     err = (got - want).abs()[fine]
     over = err > bound.cpu()[fine]
     assert not bool(over.any()), f"{what}: {int(over.sum())} of {over.numel()} off, the largest error {float(err.max()):.3g}"
+
+
+def linear_64(q, k, v, g, scale, o, state, state_out, sequences, pool, products_off=0.0):
+    """The recurrence, token by token; o and state_out: what lay there before.  Also returns how far results may be off:
+      the state   E <- exp(g) E + 8 * 2^-24 A with A <- exp(g) A + |k|^T |v|: eight roundings of a token's sums (the recurrence makes three)
+      o           |scale| |q| (E + products_off A + (dk + 128) 2^-23 A): the sum over dk (and 128 terms of a chunk more, each cut off instead of
+                  rounded) on top; products_off: the rounding of what enters the 16-bit products (a term's weight, an element of the state)"""
+    q, k, v, g = q.double(), k.double(), v.double(), g.double()
+    h, dk, dv = v.shape[1], q.shape[2], v.shape[2]
+    of = torch.arange(h) // (h // q.shape[1])
+    o, o_off = o.double().clone(), torch.zeros_like(o, dtype=torch.float64)
+    new, new_off = (None, None) if state_out is None else (state_out.double().clone(), torch.zeros_like(state_out, dtype=torch.float64))
+    for first, n, slot, resumes in sequences:
+        if not 0 <= slot < pool:
+            continue
+        S = state[slot].double().clone() if state is not None and resumes else torch.zeros(h, dk, dv, dtype=torch.float64)
+        A, E = S.abs(), torch.zeros_like(S)
+        for t in range(first, first + n):
+            a = torch.exp(g if g.dim() == 1 else g[t])[:, None, None]
+            kk, qq = k[t][of], q[t][of]
+            S = a * S + kk[:, :, None] * v[t][:, None, :]
+            A = a * A + kk.abs()[:, :, None] * v[t].abs()[:, None, :]
+            E = a * E + 8 * 2.0 ** -24 * A
+            o[t] = scale * (qq[:, :, None] * S).sum(1)
+            o_off[t] = abs(scale) * (qq.abs()[:, :, None] * (E + (products_off + (dk + 128) * 2.0 ** -23) * A)).sum(1)
+        if new is not None:
+            new[slot], new_off[slot] = S, E + 2.0 ** -149
+    return o, o_off, new, new_off

@@ -94,3 +94,39 @@ def test_binding_refuses_sequences_that_do_not_fit():
                  ((1,), None, None, None, torch.zeros(0, 2), None)):
         with pytest.raises(ValueError):
             take(*args)
+
+
+def attention(q=A, k=A, v=A, g=A, o=A, state=None, state_out=None, cu=None, slots_at=None, workspace=A, workspace_bytes=1 << 40,
+              dtype=binding.BF16, **sizes):
+    s = dict(tokens=8, sequences=2, slots=0, max_len=0, heads=4, qk_heads=2, dk=64, dv=64, scale=1.0, q_stride=128, k_stride=128,
+             v_stride=256, o_stride=256, decay_stride=4)
+    s.update(sizes)
+    seqs = binding.Sequences(cu, slots_at, None)
+    return binding.lib().im2win_linear_attention(q, k, v, g, o, state, state_out, ctypes.byref(seqs), workspace, workspace_bytes,
+                                                 ctypes.byref(binding.AttentionShape(**s)), dtype, None)
+
+
+@pytest.mark.parametrize("status,call", [
+    (NULL, dict(q=None)), (NULL, dict(k=None)), (NULL, dict(v=None)), (NULL, dict(g=None)), (NULL, dict(o=None)), (NULL, dict(workspace=None)),
+    (INVALID, dict(heads=0)), (INVALID, dict(qk_heads=0)), (INVALID, dict(qk_heads=3)), (INVALID, dict(dk=0)), (INVALID, dict(dv=0)),
+    (INVALID, dict(tokens=-1)), (INVALID, dict(tokens=9)), (INVALID, dict(sequences=0)), (INVALID, dict(max_len=-1)), (INVALID, dict(dtype=3)),
+    (INVALID, dict(q_stride=127)), (INVALID, dict(k_stride=127)), (INVALID, dict(v_stride=255)), (INVALID, dict(o_stride=255)),
+    (INVALID, dict(decay_stride=3)), (INVALID, dict(state=A)), (INVALID, dict(state_out=A, slots=1)), (INVALID, dict(slots_at=A)),
+    (MISALIGNED, dict(q=A + 1)), (MISALIGNED, dict(o=A + 1)), (MISALIGNED, dict(g=A + 2)), (MISALIGNED, dict(state=A + 4, slots=2)),
+    (MISALIGNED, dict(state_out=A + 8, slots=2)), (MISALIGNED, dict(workspace=A + 8)), (MISALIGNED, dict(cu=A + 1)),
+    (SMALL, dict(workspace_bytes=255)),
+    (UNSUPPORTED, dict(dk=257, q_stride=1024, k_stride=1024)), (UNSUPPORTED, dict(dv=2 ** 30, v_stride=2 ** 33, o_stride=2 ** 33)),
+], ids=str)
+def test_attention_refuses(status, call):
+    assert attention(**call) == status
+
+
+def test_attention_kernel_names_and_sizes():
+    shape = binding.make_attention_shape(8, 2, 4, 3, 64, 64)
+    assert binding.im2win_linear_attention_kernel_name(shape, binding.BF16) == "none"
+    with pytest.raises(binding.Im2winError):
+        binding.im2win_linear_attention_workspace_size(shape, binding.BF16)
+    shape = binding.make_attention_shape(8, 8, 4, 2, 64, 64)
+    for code in (binding.F32, binding.F16, binding.BF16):
+        assert binding.im2win_linear_attention_kernel_name(shape, code) == "tokens"
+        assert binding.im2win_linear_attention_workspace_size(shape, code) >= 256
