@@ -447,6 +447,31 @@ im2win_status im2win_linear_attention(const void* q, const void* k, const void* 
 /* "tokens" (the recurrence as it stands); "none" for an invalid shape.  Host-only, static storage; for reports and tests. */
 const char* im2win_linear_attention_kernel_name(const im2win_attention_shape* shape, im2win_dtype dtype);
 
+typedef struct {
+  int32_t M;                  /* rows of x and y: 1 to 16                                 */
+  int32_t N, K;               /* the matrix is [N][K]                                     */
+  int32_t group;              /* elements along K that share a scale: 32, 64 or a multiple of 128 */
+  int64_t x_stride, y_stride; /* elements from a row to the next one (>= K, >= N)         */
+} im2win_int4_shape;
+
+/*
+ * A few rows times a matrix of 4-bit weights (a 1x1 layer on a few positions
+ * whose filter is held in 4 bits):
+ *     y[m][n] = bias[n] + sum_k x[m][k] * scales[n][k / group] * (w[n][k] - z[n][k / group]),
+ * w[n][k] in 0..15: the low (k even) or high (k odd) half of byte k/2 of row n
+ * of `weight` [N][(K+1)/2]; z from `zeros` [N][ceil(K/group)] (bytes, taken
+ * modulo 16), or 8 where `zeros` is NULL.  x [M][K], scales [N][ceil(K/group)]
+ * and y [M][N] hold elements of `dtype` (any of the three); bias holds floats
+ * or is NULL.  (w - z) and its products with x are exact, sums are fp32, a
+ * group's sum is multiplied by its scale in fp32, y is rounded once; the order
+ * of sums is fixed by the shape.  The pointers need the alignment of their
+ * elements only; rows of x and of the matrix that start on 16-byte boundaries
+ * are the fast ones.
+ */
+im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros,
+                                 const float* bias, void* y, const im2win_int4_shape* shape, im2win_dtype dtype,
+                                 void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

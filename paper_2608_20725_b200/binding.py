@@ -30,7 +30,7 @@ EXPORTS = (
     "im2win_conv_f32_static", "im2win_pack_filter", "im2win_conv_packed", "im2win_conv_kernel_name", "im2win_nhwc_kernel_name",
     "im2win_nhwc_workspace_size", "im2win_transform_nhwc", "im2win_conv_f16_nhwc", "im2win_pack_filter_nhwc",
     "im2win_conv_packed_nhwc", "im2win_causal_conv1d", "im2win_linear_attention",
-    "im2win_linear_attention_workspace_size", "im2win_linear_attention_kernel_name",
+    "im2win_linear_attention_workspace_size", "im2win_linear_attention_kernel_name", "im2win_matvec_int4",
 )
 
 STATIC_SCRATCH_BYTES = 4 << 20
@@ -66,6 +66,10 @@ class AttentionShape(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int32) for k in ("tokens", "sequences", "slots", "max_len", "heads", "qk_heads", "dk", "dv")] + \
                [("scale", ctypes.c_float)] + \
                [(k, ctypes.c_int64) for k in ("q_stride", "k_stride", "v_stride", "o_stride", "decay_stride")]
+
+
+class Int4Shape(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("M", "N", "K", "group")] + [(k, ctypes.c_int64) for k in ("x_stride", "y_stride")]
 
 
 class Im2winError(RuntimeError):
@@ -110,6 +114,7 @@ def lib() -> ctypes.CDLL:
     L.im2win_causal_conv1d.argtypes = [vp, vp, vp, vp, vp, vp, P(Sequences), P(Conv1dShape), ctypes.c_int, vp]
     L.im2win_linear_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, P(Sequences), vp, sz, P(AttentionShape), ctypes.c_int, vp]
     L.im2win_linear_attention_workspace_size.argtypes = [P(AttentionShape), ctypes.c_int, P(sz)]
+    L.im2win_matvec_int4.argtypes = [vp, vp, vp, vp, vp, vp, P(Int4Shape), ctypes.c_int, vp]
     for name in EXPORTS[1:]:
         getattr(L, name).restype = ctypes.c_int
     L.im2win_conv_kernel_name.restype = ctypes.c_char_p
@@ -561,6 +566,33 @@ def im2win_linear_attention(q, k, v, log_decay, o, workspace, scale: float = 1.0
                                          code, _stream(stream))
     if code:
         _check(code, "im2win_linear_attention")
+
+
+def im2win_matvec_int4(x, weight, scales, y, group: int, zeros=None, bias=None, stream=None) -> None:
+    """A few rows times a matrix of 4-bit weights into y: x [M, K], weight uint8 [N, (K + 1) // 2], scales [N, ceil(K / group)], zeros
+    uint8 of that shape, bias float32 [N], y [M, N]."""
+    dtype = x.dtype
+    code = _sequence_dtype(dtype)
+    _on_current_device(x, weight, scales, y, zeros, bias)
+    if x.dim() != 2 or y.dim() != 2 or x.shape[0] != y.shape[0] or y.dtype != dtype:
+        raise ValueError("x: [M, K], y: [M, N] of one dtype")
+    (m, k), n = x.shape, y.shape[1]
+    if m < 1 or n < 1 or k < 1 or group < 1:
+        raise ValueError("M, N, K and group have to be positive")
+    if weight.dtype != torch.uint8 or weight.shape != (n, (k + 1) // 2) or not weight.is_contiguous():
+        raise ValueError("weight: [N, (K + 1) // 2] of uint8")
+    groups = (n, -(-k // group))
+    if scales.dtype != dtype or scales.shape != groups or not scales.is_contiguous():
+        raise ValueError("scales: [N, ceil(K / group)] of x's dtype")
+    if zeros is not None and (zeros.dtype != torch.uint8 or zeros.shape != groups or not zeros.is_contiguous()):
+        raise ValueError("zeros: [N, ceil(K / group)] of uint8")
+    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,) or not bias.is_contiguous()):
+        raise ValueError("bias: [N] of float32")
+    sizes = Int4Shape(m, n, k, group, _row_stride(x, 1, "x"), _row_stride(y, 1, "y"))
+    code = lib().im2win_matvec_int4(x.data_ptr(), weight.data_ptr(), scales.data_ptr(), _ptr(zeros), _ptr(bias), y.data_ptr(),
+                                    ctypes.byref(sizes), code, _stream(stream))
+    if code:
+        _check(code, "im2win_matvec_int4")
 
 
 # ---------------------------------------------------------------- conveniences

@@ -124,5 +124,7 @@ struct AttentionArgs {
   im2win_dtype dtype;
 };
 cudaError_t launch_attention_tokens(const AttentionArgs& a, cudaStream_t stream);
+cudaError_t launch_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros, const float* bias,
+                               void* y, const im2win_int4_shape& shape, im2win_dtype dtype, cudaStream_t stream);
 
 }  // namespace im2win

@@ -105,4 +105,21 @@ im2win_status im2win_linear_attention(const void* q, const void* k, const void* 
   return from_launch(launch_attention_tokens(a, static_cast<cudaStream_t>(cuda_stream)));
 }
 
+im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros,
+                                 const float* bias, void* y, const im2win_int4_shape* shape, im2win_dtype dtype,
+                                 void* cuda_stream) {
+  if (!x || !weight || !scales || !y || !shape) return IM2WIN_ERR_NULL_POINTER;
+  if (!known_dtype(dtype) || shape->M < 1 || shape->N < 1 || shape->K < 1 || shape->x_stride < shape->K ||
+      shape->y_stride < shape->N || shape->group < 1)
+    return IM2WIN_ERR_INVALID_ARG;
+  if (shape->M > 16 || (shape->group != 32 && shape->group != 64 && shape->group % 128 != 0) || shape->K > kMost - 4096 ||
+      shape->N > kMost - 4096)
+    return IM2WIN_ERR_UNSUPPORTED;
+  const size_t es = element_bytes(dtype);
+  for (const void* at : {x, scales, (const void*)y})
+    if (!aligned_to(at, es)) return IM2WIN_ERR_MISALIGNED;
+  if (!aligned_to(bias, 4)) return IM2WIN_ERR_MISALIGNED;
+  return from_launch(launch_matvec_int4(x, weight, scales, zeros, bias, y, *shape, dtype, static_cast<cudaStream_t>(cuda_stream)));
+}
+
 }  // extern "C"

@@ -110,3 +110,13 @@ def linear_64(q, k, v, g, scale, o, state, state_out, sequences, pool, products_
         if new is not None:
             new[slot], new_off[slot] = S, E + 2.0 ** -149
     return o, o_off, new, new_off
+
+
+def matvec_64(x, weight, scales, zeros, bias, group):
+    """The definition, and the sum of the magnitudes of its terms."""
+    x, k = x.double(), x.shape[1]
+    w = torch.stack([weight & 15, weight >> 4], 2).flatten(1)[:, :k].double()
+    of = torch.arange(k) // group
+    w = (w - (8.0 if zeros is None else (zeros & 15).double()[:, of])) * scales.double()[:, of]
+    y, a = x @ w.T, x.abs() @ w.abs().T
+    return (y, a) if bias is None else (y + bias.double(), a + bias.double().abs())

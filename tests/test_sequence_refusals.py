@@ -130,3 +130,20 @@ def test_attention_kernel_names_and_sizes():
     for code in (binding.F32, binding.F16, binding.BF16):
         assert binding.im2win_linear_attention_kernel_name(shape, code) == "tokens"
         assert binding.im2win_linear_attention_workspace_size(shape, code) >= 256
+
+
+def matvec(x=A, weight=A, scales=A, zeros=None, bias=None, y=A, dtype=binding.BF16, **sizes):
+    s = dict(M=2, N=64, K=256, group=64, x_stride=256, y_stride=64)
+    s.update(sizes)
+    return binding.lib().im2win_matvec_int4(x, weight, scales, zeros, bias, y, ctypes.byref(binding.Int4Shape(**s)), dtype, None)
+
+
+@pytest.mark.parametrize("status,call", [
+    (NULL, dict(x=None)), (NULL, dict(weight=None)), (NULL, dict(scales=None)), (NULL, dict(y=None)),
+    (INVALID, dict(M=0)), (INVALID, dict(N=0)), (INVALID, dict(K=0)), (INVALID, dict(group=0)), (INVALID, dict(x_stride=255)),
+    (INVALID, dict(y_stride=63)), (INVALID, dict(dtype=3)), (UNSUPPORTED, dict(M=17)), (UNSUPPORTED, dict(group=16)),
+    (UNSUPPORTED, dict(group=96)), (UNSUPPORTED, dict(K=2 ** 31 - 1, x_stride=2 ** 31)), (MISALIGNED, dict(x=A + 1)), (MISALIGNED, dict(y=A + 1)),
+    (MISALIGNED, dict(scales=A + 1)), (MISALIGNED, dict(bias=A + 2)), (MISALIGNED, dict(x=A + 2, dtype=binding.F32)),
+], ids=str)
+def test_matvec_refuses(status, call):
+    assert matvec(**call) == status
