@@ -1,0 +1,769 @@
+// Linear attention with a decay for each head, by chunks of 64 tokens on the tensor cores (im2win_linear_attention).
+//
+// With G_i the sum of log_decay up to and including token i of a chunk, S the state before it and n its tokens:
+//
+//   o_i  = scale ( exp(G_i) q_i S  +  sum_{j <= i} exp(G_i - G_j) (q_i . k_j) v_j )        "inter" and "intra"
+//   S   <- exp(G_n) S + sum_j exp(G_n - G_j) k_j^T v_j                                      "added"
+//
+// A block has one head, a tile of 128 columns of dv and a run of chunks of one sequence.  S stays in its registers, transposed: a
+// thread has a column of dv and half of dk.  All products with S or v are made transposed, so that their 128 rows are dv:
+//
+//   inter^T [dv][64 tokens] = S^T (16 bits, tensor memory) x q        added^T [dv][dk] = v^T x (weighted k)
+//   intra^T [dv][64 tokens] = v^T x P,  P_ij = exp(G_i - G_j) (q_i . k_j)
+//
+// v^T and the weighted k are read as they lie, rows of tokens, as operands whose 64 elements of a row are innermost along M or N
+// (transposed by the descriptor); the 64 x 64 products q . k, of which half are needed, are made by the warps (mma.sync) and stay in
+// registers until they are weighted and masked.
+//
+// What is rounded to 16 bits: P and the copy of S that meets q, once each, as the result o is; their errors and o's own rounding are of
+// one size and independent.  The weighted k are not: the state is carried from call to call in fp32 and has to stay fp32, so they go
+// through the tensor cores as pieces whose sum is the fp32 product to 2^-22 (three of bf16, cut off exactly; two of fp16).  fp16 has no
+// room for large or small numbers: S, P and the weighted k are brought to 2^13 by a power of two for each chunk.
+// log_decay is summed in 64 bits, differences are split into whole and fractional powers of two, so that no cancellation is left
+// behind a strong decay.  A product of a masked 0, or of a piece that is 0 or has the other sign, with an infinity of v is a NaN: where
+// o is not finite the chunk's intra part is made again from its terms j <= i alone, and where what a chunk adds to the state is not,
+// that is made again from the fp32 products.
+//
+// Long sequences are cut into segments of several chunks where there are too few heads and sequences for the GPU: one launch sums up
+// what each segment adds to a zero state, a second one runs over the segments of a sequence and leaves each one's starting state, and
+// the main one then has all segments at once.
+#include <float.h>
+
+#include "common.cuh"
+#include "ptx_sm100.cuh"
+#include "sequence.cuh"
+
+namespace im2win {
+namespace {
+
+using namespace ptx;
+
+constexpr int kChunk = 64;               // tokens
+constexpr int kThreads = 256;
+constexpr int kTile = 128;               // columns of dv of a block: rows of the products
+constexpr uint32_t kPanel = 64 * 128;    // 64 rows of 64 16-bit elements, 128-byte swizzle
+
+struct ChunkParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  const float* decay;
+  void* o;
+  const float* state_in;                 // states of the pool, or of the segments (segmented)
+  float* state_out;
+  float* added;                          // [segments][heads][dk][dv]
+  float2* totals;                        // [segments][heads]: decay of a whole segment, and less one
+  uint32_t* status;
+  Sequences seqs;
+  int64_t q_stride, k_stride, v_stride, o_stride, decay_stride;
+  int32_t heads, share, dk, dv, tiles, L;
+  int32_t segmented;
+  float scale;
+};
+
+template <typename T> struct Kind;
+template <> struct Kind<__nv_bfloat16> {
+  static constexpr int kPieces = 3;
+  static constexpr bool kScaled = false;
+  static constexpr uint32_t kFormats = (1u << 7) | (1u << 10);
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+  }
+  static __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+  static __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+  static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+  // Two numbers as pieces: the upper half, the upper half of the rest, the rest of that (exact: 24 bits).  An infinity is its first
+  // piece, a NaN too.
+  static __device__ __forceinline__ void split(float a, float b, uint32_t (&piece)[3]) {
+    const float a1 = a - __uint_as_float(__float_as_uint(a) & 0xffff0000u), b1 = b - __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+    piece[0] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    const float ra = a1 == a1 ? a1 : 0.0f, rb = b1 == b1 ? b1 : 0.0f;
+    piece[1] = __byte_perm(__float_as_uint(ra), __float_as_uint(rb), 0x7632);
+    const float a2 = ra - __uint_as_float(__float_as_uint(ra) & 0xffff0000u), b2 = rb - __uint_as_float(__float_as_uint(rb) & 0xffff0000u);
+    piece[2] = __byte_perm(__float_as_uint(a2), __float_as_uint(b2), 0x7632);
+  }
+};
+template <> struct Kind<__half> {
+  static constexpr int kPieces = 2;
+  static constexpr bool kScaled = true;
+  static constexpr uint32_t kFormats = 0;
+  static __device__ __forceinline__ uint32_t pack(float a, float b) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+  }
+  static __device__ __forceinline__ float low(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xffffu))); }
+  static __device__ __forceinline__ float high(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
+  static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+  // Two numbers as pieces: rounded, and the rest rounded (22 bits).
+  static __device__ __forceinline__ void split(float a, float b, uint32_t (&piece)[2]) {
+    piece[0] = pack(a, b);
+    const float a1 = a - low(piece[0]), b1 = b - high(piece[0]);
+    piece[1] = pack(a1 == a1 ? a1 : 0.0f, b1 == b1 ? b1 : 0.0f);
+  }
+};
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t ld_shared_u16(uint32_t addr) {
+  unsigned short v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_shared4(uint32_t addr, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+      "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// MMA with A in tensor memory (its elements two a column along K) and B by descriptor.
+__device__ __forceinline__ void umma_f16_ta(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "mov.b64 db, {%2, %3};\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Descriptor halves of an operand whose rows of 64 elements (128 bytes, 128-byte swizzle) run along M or N: panels of 64 of them
+// kPanel bytes apart (leading offset), groups of eight rows, along K, 1024 bytes apart (stride offset).
+__device__ __forceinline__ uint32_t desc_lo_mn(uint32_t saddr) { return ((saddr & 0x3ffffu) >> 4) | ((kPanel >> 4) << 16); }
+constexpr uint32_t kDescHi = kSmemDescHiSw128;
+constexpr uint32_t kAlongM = 1u << 15, kAlongN = 1u << 16;     // of the instruction descriptor: A, B lie that way
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// The decays of one chunk, all relative to its start.
+struct Decays {
+  float whole[kChunk], part[kChunk];     // G_i in powers of two: its floor and the rest
+  float from_start[kChunk];              // exp(G_i)
+  float to_end[kChunk];                  // exp(G_n - G_i)
+  float total, total_less_one;           // exp(G_n)
+};
+
+// One warp: lane l has tokens 2l and 2l+1.  Returns G_n (powers of two).
+__device__ __forceinline__ double chunk_decays(float g0, float g1, Decays& d) {
+  const int lane = threadIdx.x & 31;
+  auto powers = [](float g) -> double {
+    const double p = (double)g * 1.4426950408889634074;
+    return p < -1000.0 ? -1000.0 : p;          // (2^-1000 is 0 in fp32; a NaN stays one)
+  };
+  const double a = powers(g0), b = powers(g1);
+  double sum = a + b;
+#pragma unroll
+  for (int s = 1; s < 32; s *= 2) {
+    const double other = __shfl_up_sync(0xffffffffu, sum, s);
+    if (lane >= s) sum += other;
+  }
+  const double all = __shfl_sync(0xffffffffu, sum, 31);
+  const double G[2] = {sum - b, sum};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const double floor_of = floor(G[i]);
+    d.whole[2 * lane + i] = (float)floor_of;
+    d.part[2 * lane + i] = (float)(G[i] - floor_of);
+    d.from_start[2 * lane + i] = (float)exp2(G[i]);
+    d.to_end[2 * lane + i] = (float)exp2(all - G[i]);
+  }
+  if (lane == 0) {
+    d.total = (float)exp2(all);
+    d.total_less_one = (float)expm1(all * 0.69314718055994530942);
+  }
+  return all;
+}
+
+// A power of two that brings numbers of at most `bits` (of a float) to below 2^14.
+__device__ __forceinline__ float scale_for(uint32_t bits) {
+  const int e = (int)(bits >> 23);
+  if (e == 0) return 1.0f;
+  return __uint_as_float((uint32_t)min(max(127 + 13 - (e - 127), 1), 254) << 23);
+}
+__device__ __forceinline__ uint32_t finite_bits(float x) {
+  const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
+  return b < 0x7f800000u ? b : 0u;
+}
+__device__ __forceinline__ void raise_max(uint32_t* at, uint32_t bits) {
+  const uint32_t m = __reduce_max_sync(0xffffffffu, bits);
+  if ((threadIdx.x & 31) == 0) atomicMax(at, m);
+}
+
+// S <- total S + added
+__device__ __forceinline__ float carry(float s, float total, float less_one, float added) {
+  if (total > 0.5f) {
+    const float part = fabsf(s) <= FLT_MAX ? s : 0.0f;         // (see attention_tokens.cu)
+    return s + fmaf(part, less_one, added);
+  }
+  return fmaf(s, total, added);
+}
+
+template <typename T, int DK, bool OUT>
+struct Layout {
+  static constexpr uint32_t kQK = DK / 64 * kPanel;            // q or k of a chunk
+  static constexpr uint32_t kV = 2 * kPanel;
+  static constexpr uint32_t kStage = (OUT ? 2 : 1) * kQK + kV;
+  static constexpr uint32_t kPiecesAt = 2 * kStage;
+  static constexpr uint32_t kPAt = kPiecesAt + Kind<T>::kPieces * kQK;
+  static constexpr uint32_t kBytes = kPAt + (OUT ? kPanel : 0) + 1024;
+  // columns of tensor memory
+  static constexpr uint32_t kAdded = 0, kInter = DK, kIntra = DK + 64, kS = DK + 128;
+  static constexpr uint32_t kColumns = OUT ? (DK == 128 ? 512 : 256) : DK;
+};
+
+template <typename T, int DK, bool OUT>
+__global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p) {
+  using K = Kind<T>;
+  using L = Layout<T, DK, OUT>;
+  constexpr int kHalf = DK / 2;                                // columns of S of a thread
+  extern __shared__ uint8_t dynamic_smem[];
+  __shared__ Decays decays[2];
+  __shared__ __align__(8) uint64_t done_bar;
+  __shared__ uint32_t tmem_base_at, abort_flag, again, largest[2][3];
+  const uint32_t smem = (smem_u32(dynamic_smem) + 1023u) & ~1023u;
+  const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
+  const uint32_t tile = blockIdx.x % (uint32_t)p.tiles, rest = blockIdx.x / (uint32_t)p.tiles;
+  const int head = (int)(rest % (uint32_t)p.heads);
+  const uint32_t id = rest / (uint32_t)p.heads;
+  const Piece piece = find_piece(p.seqs, id, p.L);
+  const int slot = slot_of(p.seqs, piece.sequence);
+  const bool leads = piece.first == piece.rows.begin;
+  if (slot < 0 || (!leads && piece.first >= piece.rows.end)) return;
+  const int first = (int)piece.first, end = (int)min(piece.first + p.L, (int64_t)piece.rows.end);
+  const bool last = end == piece.rows.end;
+  if (!OUT && last) return;                                    // (nothing starts behind it)
+
+  const int half = warp >> 2, row = (warp & 3) * 32 + lane;    // row: of the transposed products, a column of dv
+  const int col = (int)tile * kTile + row;
+  const bool live = col < p.dv;
+  const int64_t state_size = (int64_t)p.dk * p.dv;
+
+  const uint32_t bar = smem_u32(&done_bar);
+  if (warp == 0) tmem_alloc(smem_u32(&tmem_base_at), L::kColumns);
+  if (tid == 0) {
+    mbar_init(bar, 1);
+    abort_flag = 0;
+    again = 0;
+    for (int i = 0; i < 6; ++i) largest[i / 3][i % 3] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (OUT)
+    for (uint32_t at = tid * 16; at < kPanel; at += kThreads * 16) st_shared16(smem + L::kPAt + at, 0, 0, 0, 0);
+
+  const T* q = static_cast<const T*>(p.q) + (int64_t)(head / p.share) * p.dk;
+  const T* k = static_cast<const T*>(p.k) + (int64_t)(head / p.share) * p.dk;
+  const T* v = static_cast<const T*>(p.v) + (int64_t)head * p.dv + tile * kTile;
+  auto load = [&](int stage, int t0) {
+    const uint32_t base = smem + stage * L::kStage;
+    constexpr int kUnits = DK / 8;
+#pragma unroll
+    for (int u = tid; u < kChunk * kUnits; u += kThreads) {
+      const int r = u / kUnits, c = u % kUnits;
+      const bool there = t0 + r < end && c * 8 < p.dk;
+      const uint32_t at = (c / 8) * kPanel + r * 128 + (((c % 8) ^ (r & 7)) << 4);
+      const int64_t t = there ? t0 + r : 0;
+      const int off = there ? c * 8 : 0;
+      copy16(base + at, k + t * p.k_stride + off, there);
+      if (OUT) copy16(base + L::kQK + L::kV + at, q + t * p.q_stride + off, there);
+    }
+#pragma unroll
+    for (int u = tid; u < kChunk * 16; u += kThreads) {
+      const int r = u / 16, c = u % 16;
+      const bool there = t0 + r < end && (int)tile * kTile + c * 8 < p.dv;
+      const uint32_t at = (c / 8) * kPanel + r * 128 + (((c % 8) ^ (r & 7)) << 4);
+      copy16(base + L::kQK + at, v + (there ? (t0 + r) * p.v_stride + c * 8 : 0), there);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto load_decay = [&](int t0, float& g0, float& g1) {
+    const int t = t0 + 2 * lane;
+    g0 = t < end ? p.decay[(int64_t)t * p.decay_stride + head] : 0.0f;
+    g1 = t + 1 < end ? p.decay[(int64_t)(t + 1) * p.decay_stride + head] : 0.0f;
+  };
+
+  if (first < end) load(0, first);
+  double all_decay = 0.0;
+  if (warp == 7 && first < end) {
+    float g0, g1;
+    load_decay(first, g0, g1);
+    all_decay = chunk_decays(g0, g1, decays[0]);
+  }
+  // the starting state
+  float S[kHalf];
+  {
+    const float* from = nullptr;
+    if (OUT && live) {
+      if (p.segmented)
+        from = p.state_in + ((int64_t)id * p.heads + head) * state_size;
+      else if (p.state_in && resumes(p.seqs, piece.sequence))
+        from = p.state_in + ((int64_t)slot * p.heads + head) * state_size;
+    }
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j) {
+      const int d = half * kHalf + j;
+      S[j] = from && d < p.dk ? from[(int64_t)d * p.dv + col] : 0.0f;
+    }
+  }
+
+  T* o = static_cast<T*>(p.o) + (int64_t)head * p.dv + col;
+  uint32_t tmem = 0, lanes = 0;
+  bool ok = true;
+  const int chunks = (end - first + kChunk - 1) / kChunk;
+  // the intra part of the chunk before, from its terms j <= i alone
+  auto make_again = [&](int c) {
+    if (!OUT) return;
+    const Decays& d = decays[c & 1];
+    const uint32_t vt = smem + (c & 1) * L::kStage + L::kQK + (row >> 6) * kPanel;
+    const int t0 = first + c * kChunk;
+    float is = 1.0f, ip = 1.0f;
+    if (K::kScaled) {
+      is = 1.0f / scale_for(largest[c & 1][2]);
+      ip = 1.0f / scale_for(largest[c & 1][1]);
+    }
+    uint32_t inter[32];
+    tmem_ld32(tmem + lanes + L::kInter + half * 32, inter);
+    for (int i = 0; i < 32; ++i) {
+      const int ti = half * 32 + i;
+      float sum = 0.0f;
+      for (int j = 0; j <= ti; ++j) {
+        const float w = K::low(ld_shared_u16(smem + L::kPAt + ti * 128 + ((((uint32_t)j >> 3) ^ (ti & 7)) << 4) + (j & 7) * 2));
+        const float x = K::low(ld_shared_u16(vt + j * 128 + ((((uint32_t)(row & 63) >> 3) ^ (j & 7)) << 4) + (row & 7) * 2));
+        sum = fmaf(w, x, sum);
+      }
+      float from_state = 0.0f;
+#pragma unroll
+      for (int u = 0; u < 32; ++u)
+        if (u == i) from_state = __uint_as_float(inter[u]);
+      if (live && t0 + ti < end)
+        o[(int64_t)(t0 + ti) * p.o_stride] = from_float<T>(p.scale * fmaf(d.from_start[ti] * is, from_state, sum * ip));
+    }
+  };
+
+  for (int c = 0; c < chunks; ++c) {
+    const int stage = c & 1, t0 = first + c * kChunk;
+    const uint32_t base = smem + stage * L::kStage;
+    const uint32_t kt = base, vt = base + L::kQK, qt = base + L::kQK + L::kV;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    fence_proxy_async_smem();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (c == 0) {
+      tmem = tmem_base_at;
+      lanes = (uint32_t)(warp & 3) << 21;                      // this warp's 32 lanes
+    }
+    if (*(volatile uint32_t*)&abort_flag) { ok = false; break; }
+    if (OUT && *(volatile uint32_t*)&again) {                  // (the same for every thread: raised before the barrier)
+      make_again(c - 1);
+      tc_fence_before();
+      __syncthreads();
+      tc_fence_after();
+      if (tid == 0) again = 0;
+    }
+    if (c + 1 < chunks) load(stage ^ 1, t0 + kChunk);
+    float g0 = 0.0f, g1 = 0.0f;
+    if (warp == 7 && c + 1 < chunks) load_decay(t0 + kChunk, g0, g1);
+    const Decays& d = decays[stage];
+
+    // q . k: 16 x 8 blocks that reach below the diagonal; of the four rows of blocks, the last one's eight go to warps 0 to 2, the
+    // next one's six to 3 and 4, then four to 5 and 6, and two to 7
+    float P[3][4];
+    const int rb = warp < 3 ? 3 : warp < 5 ? 2 : warp < 7 ? 1 : 0;
+    const int nt0 = warp < 3 ? warp * 3 : warp < 5 ? (warp - 3) * 3 : warp < 7 ? (warp - 5) * 2 : 0;
+    const int nts = rb == 3 ? min(3, 8 - nt0) : rb == 2 ? 3 : 2;
+    if (OUT) {
+#pragma unroll
+      for (int n = 0; n < 3; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) P[n][i] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < DK / 16; ks += 2) {                // 32 elements of dk
+        uint32_t a[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = rb * 16 + (lane & 15), cc = (ks + i) * 2 + (lane >> 4);
+          ldmatrix_x4(qt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), a[i]);
+        }
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+          if (n >= nts) break;
+          const int r = (nt0 + n) * 8 + (lane & 7), cc = ks * 2 + (lane >> 3);
+          uint32_t b[4];
+          ldmatrix_x4(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), b);
+          K::mma(P[n], a[0], b[0], b[1]);
+          K::mma(P[n], a[1], b[2], b[3]);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < 3; ++n) {
+        if (n >= nts) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int ti = rb * 16 + (lane >> 2) + 8 * (i >> 1), tj = (nt0 + n) * 8 + 2 * (lane & 3) + (i & 1);
+          const float power = (d.whole[ti] - d.whole[tj]) + (d.part[ti] - d.part[tj]);
+          P[n][i] = tj <= ti ? P[n][i] * exp2_fast(power) : 0.0f;
+        }
+      }
+    }
+    constexpr int kUnits = DK / 8, kMine = kChunk * kUnits / kThreads;
+    uint4 kk[kMine];
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) {
+      const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
+      kk[m] = ld_shared16(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4));
+    }
+    float scale_k = 1.0f, scale_p = 1.0f, scale_s = 1.0f;
+    if (K::kScaled) {
+      uint32_t top = 0, odd = 0;
+#pragma unroll
+      for (int m = 0; m < kMine; ++m)
+        for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) {
+          top = __vmaxu2(top, w & 0x7fff7fffu);
+          odd |= ((w & 0x7fff7fffu) + 0x04000400u) & 0x80008000u;
+        }
+      if (odd) {                                               // infinities or NaNs: the largest of the others
+        top = 0;
+        for (int m = 0; m < kMine; ++m)
+          for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) {
+            if ((w & 0x7c00u) != 0x7c00u) top = __vmaxu2(top, w & 0x7fffu);
+            if ((w & 0x7c000000u) != 0x7c000000u) top = __vmaxu2(top, w & 0x7fff0000u);
+          }
+      }
+      raise_max(&largest[stage][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
+      if (OUT) {
+        uint32_t pm = 0, sm = 0;
+#pragma unroll
+        for (int n = 0; n < 3; ++n)
+          if (n < nts)
+            for (int i = 0; i < 4; ++i) pm = max(pm, finite_bits(P[n][i]));
+        raise_max(&largest[stage][1], pm);
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j) sm = max(sm, finite_bits(S[j]));
+        raise_max(&largest[stage][2], sm);
+      }
+      __syncthreads();
+      scale_k = scale_for(largest[stage][0]);
+      if (OUT) {
+        scale_p = scale_for(largest[stage][1]);
+        scale_s = scale_for(largest[stage][2]);
+      }
+    }
+    if (OUT) {
+#pragma unroll
+      for (int n = 0; n < 3; ++n) {
+        if (n >= nts) break;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int ti = rb * 16 + (lane >> 2) + 8 * i, cc = nt0 + n;
+          st_shared4(smem + L::kPAt + ti * 128 + ((cc ^ (ti & 7)) << 4) + (lane & 3) * 4, K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kHalf; j += 64) {
+        uint32_t r[32];
+        if (kHalf >= 64) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) r[i] = K::pack(S[(j + 2 * i) % kHalf] * scale_s, S[(j + 2 * i + 1) % kHalf] * scale_s);
+          tmem_st32(tmem + lanes + L::kS + half * (kHalf / 2) + j / 2, r);
+        } else {
+          uint32_t h[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) h[i] = K::pack(S[2 * i] * scale_s, S[2 * i + 1] * scale_s);
+          tmem_st16(tmem + lanes + L::kS + half * (kHalf / 2), h);
+        }
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) {
+      const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
+      const float w = d.to_end[r] * scale_k;
+      const uint32_t words[4] = {kk[m].x, kk[m].y, kk[m].z, kk[m].w};
+      uint32_t out[K::kPieces][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t piece_of[K::kPieces];
+        K::split(K::low(words[i]) * w, K::high(words[i]) * w, piece_of);
+#pragma unroll
+        for (int n = 0; n < K::kPieces; ++n) out[n][i] = piece_of[n];
+      }
+      const uint32_t at = (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4);
+#pragma unroll
+      for (int n = 0; n < K::kPieces; ++n) st_shared16(smem + L::kPiecesAt + n * L::kQK + at, out[n][0], out[n][1], out[n][2], out[n][3]);
+    }
+    if (OUT) tmem_st_wait();
+    fence_proxy_async_smem();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0 && elect_one()) {
+      tc_fence_after();
+      constexpr uint32_t kBase = K::kFormats;
+      if (OUT) {
+#pragma unroll
+        for (int ks = 0; ks < DK / 16; ++ks)
+          umma_f16_ta(tmem + L::kInter, tmem + L::kS + ks * 8, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), kDescHi,
+                      kBase | instr_desc_f16(128, 64), ks > 0);
+      }
+#pragma unroll
+      for (int n = K::kPieces - 1; n >= 0; --n)                // the smallest pieces first
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          umma_f16_ab(tmem + L::kAdded, desc_lo_mn(vt + ks * 2048), kDescHi, desc_lo_mn(smem + L::kPiecesAt + n * L::kQK + ks * 2048), kDescHi,
+                      kBase | kAlongM | kAlongN | instr_desc_f16(128, DK), n < K::kPieces - 1 || ks > 0);
+      if (OUT) {
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          umma_f16_ab(tmem + L::kIntra, desc_lo_mn(vt + ks * 2048), kDescHi, smem_desc_lo(smem + L::kPAt + ks * 32), kDescHi,
+                      kBase | kAlongM | instr_desc_f16(128, 64), ks > 0);
+      }
+      umma_commit(bar);
+    }
+    if (K::kScaled && tid == 32)
+      for (int i = 0; i < 3; ++i) largest[stage ^ 1][i] = 0;
+    if (warp == 7 && c + 1 < chunks) all_decay += chunk_decays(g0, g1, decays[stage ^ 1]);
+    mbar_wait(bar, (uint32_t)(c & 1), &abort_flag, p.status);
+    tc_fence_after();
+
+    if (OUT) {
+      const float is = 1.0f / scale_s, ip = 1.0f / scale_p;
+      uint32_t inter[32], intra[32];
+      tmem_ld32_issue(tmem + lanes + L::kInter + half * 32, inter);
+      tmem_ld32_issue(tmem + lanes + L::kIntra + half * 32, intra);
+      tmem_ld_wait_for(inter);
+      tmem_ld_wait_for(intra);
+      bool fine = true;
+      T* at = o + (int64_t)(t0 + half * 32) * p.o_stride;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const float from = d.from_start[half * 32 + i] * is;
+        const float y = p.scale * fmaf(from, __uint_as_float(inter[i]), __uint_as_float(intra[i]) * ip);
+        fine = fine && fabsf(y) <= FLT_MAX;
+        if (live && t0 + half * 32 + i < end) at[(int64_t)i * p.o_stride] = from_float<T>(y);
+      }
+      if (!fine) again = 1;
+    }
+    const float ik = 1.0f / scale_k, total = d.total, less_one = d.total_less_one;
+#pragma unroll
+    for (int j = 0; j < kHalf; j += 32) {
+      uint32_t added[32];
+      tmem_ld32(tmem + lanes + L::kAdded + half * kHalf + j, added);
+      float none = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) none = fmaf(__uint_as_float(added[i]), 0.0f, none);
+      if (none != 0.0f) {                                      // (a NaN: a piece's 0 or other sign may have met an infinity of v)
+        const uint32_t column = vt + (row >> 6) * kPanel;
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i) {
+          const int e = half * kHalf + j + i;
+          float sum = 0.0f;
+#pragma unroll 1
+          for (int t = 0; t < kChunk; ++t) {
+            const float kv = K::low(ld_shared_u16(kt + (e >> 6) * kPanel + t * 128 + ((((uint32_t)(e & 63) >> 3) ^ (t & 7)) << 4) + (e & 7) * 2));
+            const float vv = K::low(ld_shared_u16(column + t * 128 + ((((uint32_t)(row & 63) >> 3) ^ (t & 7)) << 4) + (row & 7) * 2));
+            if (t0 + t < end) sum = fmaf(kv * d.to_end[t], vv, sum);
+          }
+#pragma unroll
+          for (int u = 0; u < 32; ++u)
+            if (u == i) added[u] = __float_as_uint(sum * scale_k);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) S[j + i] = carry(S[j + i], total, less_one, __uint_as_float(added[i]) * ik);
+    }
+  }
+
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (chunks == 0) tmem = tmem_base_at;
+  if (OUT && ok && chunks > 0 && again) make_again(chunks - 1);
+  float* to = nullptr;
+  if (!OUT)
+    to = p.added + ((int64_t)id * p.heads + head) * state_size;
+  else if (p.state_out && last)
+    to = p.state_out + ((int64_t)slot * p.heads + head) * state_size;
+  if (to && live) {
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j) {
+      const int dd = half * kHalf + j;
+      if (dd < p.dk) to[(int64_t)dd * p.dv + col] = S[j];
+    }
+  }
+  if (!OUT && warp == 7 && lane == 0 && tile == 0)
+    p.totals[(int64_t)id * p.heads + head] = make_float2((float)exp2(all_decay), (float)expm1(all_decay * 0.69314718055994530942));
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, L::kColumns);
+}
+
+// The starting state of every segment, in the place of what it adds: a thread has a number of a head's state and runs over the
+// segments of a sequence.
+__global__ void __launch_bounds__(256) segment_states_kernel(const ChunkParams p, const float* pool, int32_t blocks) {
+  const uint32_t rest = blockIdx.x / (uint32_t)blocks;
+  const int head = (int)(rest % (uint32_t)p.heads), b = (int)(rest / (uint32_t)p.heads);
+  const int slot = slot_of(p.seqs, b);
+  const int64_t size = (int64_t)p.dk * p.dv, e = (int64_t)(blockIdx.x % (uint32_t)blocks) * 256 + threadIdx.x;
+  if (slot < 0 || e >= size) return;
+  const SequenceRows rows = rows_of(p.seqs, b);
+  const int32_t len = rows.end - rows.begin, n = len > p.L ? (len + p.L - 1) / p.L : 1;
+  // (as find_piece numbers them)
+  const int64_t id0 = p.seqs.cu ? (int64_t)(rows.begin / p.L) + b : (int64_t)b * n;
+  float s = pool && resumes(p.seqs, b) ? pool[((int64_t)slot * p.heads + head) * size + e] : 0.0f;
+  constexpr int kAhead = 8;
+  for (int i0 = 0; i0 < n; i0 += kAhead) {
+    float added[kAhead];
+    float2 total[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t at = (id0 + i0 + i) * p.heads + head;
+      const bool there = i0 + i + 1 < n;                       // (the last one's sum is not made)
+      added[i] = there ? p.added[at * size + e] : 0.0f;
+      total[i] = there ? p.totals[at] : make_float2(1.0f, 0.0f);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (i0 + i >= n) break;
+      p.added[((id0 + i0 + i) * p.heads + head) * size + e] = s;
+      s = carry(s, total[i].x, total[i].y, added[i]);
+    }
+  }
+}
+
+struct ChunkPlan {
+  bool eligible;
+  int32_t tiles, L;
+  int64_t segments;                      // 0: every sequence is one
+  size_t totals_off, added_off, bytes;
+};
+
+// Segments by an estimate, in chunks' times: rounds of 148 blocks over the chunks of a segment, and where sequences are cut, as many for
+// what the segments but the last add, which takes 0.6 of the time, and the time of two more launches.
+ChunkPlan plan_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool has_cu) {
+  ChunkPlan c = {};
+  const int64_t longest = has_cu ? (s.max_len > 0 ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens) : s.tokens / s.sequences;
+  // Not the shortest prompts: up to 16 tokens the recurrence, which waits for nothing but its loads, is as fast.
+  c.eligible = dtype != IM2WIN_F32 && s.dk <= 128 && s.dk % 8 == 0 && s.dv % 8 == 0 && longest > 16;
+  if (!c.eligible) return c;
+  c.tiles = (s.dv + kTile - 1) / kTile;
+  const int64_t blocks = (int64_t)s.heads * c.tiles;
+  const int64_t chunks = (longest + kChunk - 1) / kChunk;
+  // sequences of the longest one's length that there can be
+  int64_t like = s.tokens / longest;
+  if (like < 1) like = 1;
+  double best = 0;
+  int64_t best_n = 1;
+  for (int64_t n = 1; n <= chunks && n <= 64; ++n) {
+    const int64_t per = (chunks + n - 1) / n;
+    double cost = (double)((like * blocks * n + 147) / 148) * (double)per;
+    if (n > 1) cost += (double)((like * blocks * (n - 1) + 147) / 148) * (double)per * 0.6 + 8.0;
+    if (n == 1 || cost < best) { best = cost; best_n = n; }
+  }
+  c.totals_off = c.added_off = c.bytes = kStatusBytes;
+  c.L = INT32_MAX;
+  if (best_n > 1) {
+    c.L = (int32_t)((chunks + best_n - 1) / best_n * kChunk);
+    c.segments = number_of_pieces(s.tokens, s.sequences, c.L, has_cu);
+    c.added_off = c.totals_off + (size_t)((c.segments * s.heads * (int64_t)sizeof(float2) + 255) / 256 * 256);
+    c.bytes = c.added_off + (size_t)(c.segments * s.heads * (int64_t)s.dk * s.dv * 4);
+  }
+  return c;
+}
+
+template <typename T, int DK, bool OUT>
+cudaError_t launch(const ChunkParams& p, int64_t pieces, cudaStream_t stream) {
+  constexpr uint32_t kBytes = Layout<T, DK, OUT>::kBytes;
+  static bool attr_done[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (!attr_done[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<T, DK, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
+    if (e != cudaSuccess) return e;
+    attr_done[dev] = true;
+  }
+  const int64_t grid = pieces * p.heads * p.tiles;
+  if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
+  chunk_kernel<T, DK, OUT><<<(unsigned)grid, kThreads, kBytes, stream>>>(p);
+  return cudaGetLastError();
+}
+
+template <typename T, int DK>
+cudaError_t launch_all(ChunkParams& p, const ChunkPlan& plan, const AttentionArgs& a, cudaStream_t stream) {
+  if (cudaMemsetAsync(p.status, 0, kStatusBytes, stream) != cudaSuccess) return cudaErrorUnknown;
+  int64_t pieces = number_of_pieces(a.shape.tokens, a.shape.sequences, p.L, a.seqs.cu != nullptr);
+  if (plan.segments) {
+    pieces = plan.segments;
+    cudaError_t e = launch<T, DK, false>(p, pieces, stream);
+    if (e != cudaSuccess) return e;
+    const int32_t blocks = (int32_t)(((int64_t)p.dk * p.dv + 255) / 256);
+    const int64_t grid = (int64_t)blocks * p.heads * a.shape.sequences;
+    if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
+    segment_states_kernel<<<(unsigned)grid, 256, 0, stream>>>(p, a.state_in, blocks);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    p.state_in = p.added;
+    p.segmented = 1;
+  }
+  return launch<T, DK, true>(p, pieces, stream);
+}
+
+}  // namespace
+
+bool attention_by_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool has_cu, size_t* workspace_bytes, bool* segmented) {
+  const ChunkPlan plan = plan_chunks(s, dtype, has_cu);
+  *workspace_bytes = plan.eligible ? plan.bytes : kStatusBytes;
+  *segmented = plan.eligible && plan.segments > 0;
+  return plan.eligible;
+}
+
+cudaError_t launch_attention_chunks(const AttentionArgs& a, cudaStream_t stream) {
+  const im2win_attention_shape& s = a.shape;
+  const ChunkPlan plan = plan_chunks(s, a.dtype, a.seqs.cu != nullptr);
+  uint8_t* ws = static_cast<uint8_t*>(a.workspace);
+  ChunkParams p = {a.q, a.k, a.v, a.decay, a.o, a.state_in, a.state_out, reinterpret_cast<float*>(ws + plan.added_off),
+                   reinterpret_cast<float2*>(ws + plan.totals_off), reinterpret_cast<uint32_t*>(ws), a.seqs, s.q_stride, s.k_stride,
+                   s.v_stride, s.o_stride, s.decay_stride, s.heads, s.heads / s.qk_heads, s.dk, s.dv, plan.tiles, plan.L, 0, s.scale};
+  if (a.dtype == IM2WIN_F16)
+    return s.dk <= 64 ? launch_all<__half, 64>(p, plan, a, stream) : launch_all<__half, 128>(p, plan, a, stream);
+  return s.dk <= 64 ? launch_all<__nv_bfloat16, 64>(p, plan, a, stream) : launch_all<__nv_bfloat16, 128>(p, plan, a, stream);
+}
+
+}  // namespace im2win

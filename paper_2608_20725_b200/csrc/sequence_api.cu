@@ -70,12 +70,20 @@ im2win_status im2win_causal_conv1d(const void* x, const void* weight, const floa
 im2win_status im2win_linear_attention_workspace_size(const im2win_attention_shape* shape, im2win_dtype dtype, size_t* bytes) {
   const im2win_status st = check_attention(shape, dtype);
   if (st != IM2WIN_OK) return st;
-  if (bytes) *bytes = 256;
+  size_t packed = 0, equal = 0;                      // with cu_seqlens and without
+  bool segmented;
+  attention_by_chunks(*shape, dtype, true, &packed, &segmented);
+  if (shape->tokens % shape->sequences == 0) attention_by_chunks(*shape, dtype, false, &equal, &segmented);
+  if (bytes) *bytes = packed > equal ? packed : equal;
   return IM2WIN_OK;
 }
 
 const char* im2win_linear_attention_kernel_name(const im2win_attention_shape* shape, im2win_dtype dtype) {
-  return check_attention(shape, dtype) == IM2WIN_OK ? "tokens" : "none";
+  if (check_attention(shape, dtype) != IM2WIN_OK) return "none";
+  size_t bytes;
+  bool segmented;
+  if (!attention_by_chunks(*shape, dtype, true, &bytes, &segmented)) return "tokens";
+  return segmented ? "chunks+segments" : "chunks";
 }
 
 im2win_status im2win_linear_attention(const void* q, const void* k, const void* v, const float* log_decay, void* o,
@@ -99,10 +107,13 @@ im2win_status im2win_linear_attention(const void* q, const void* k, const void* 
   if (!aligned_to(log_decay, 4) || !aligned_to(state_in, 16) || !aligned_to(state_out, 16) || !aligned_to(workspace, 16))
     return IM2WIN_ERR_MISALIGNED;
   size_t need = 0;
-  st = im2win_linear_attention_workspace_size(shape, dtype, &need);
-  if (st != IM2WIN_OK) return st;
+  bool segmented;
+  const bool chunks = attention_by_chunks(*shape, dtype, a.seqs.cu != nullptr, &need, &segmented);
   if (workspace_bytes < need) return IM2WIN_ERR_WORKSPACE_TOO_SMALL;
-  return from_launch(launch_attention_tokens(a, static_cast<cudaStream_t>(cuda_stream)));
+  const bool rows_aligned = shape->q_stride % 8 == 0 && shape->k_stride % 8 == 0 && shape->v_stride % 8 == 0 && aligned_to(q, 16) &&
+                            aligned_to(k, 16) && aligned_to(v, 16);
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  return from_launch(chunks && rows_aligned ? launch_attention_chunks(a, stream) : launch_attention_tokens(a, stream));
 }
 
 im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros,

@@ -72,10 +72,13 @@ class Guarded:
         assert bool((whole == self.fill).all()), "written outside the tensor"
 
 
-def close(got, want, bound, what):
-    """got within bound of want, element by element; NaN and infinities where want has them."""
+def close(got, want, bound, what, same_infinities=True):
+    """got within bound of want, element by element; NaN and infinities where want has them (without same_infinities: one or the other)."""
     got, want = got.double().cpu(), want.cpu()
     fine = torch.isfinite(want)
+    if not same_infinities:
+        assert torch.equal(torch.isfinite(got), fine), f"{what}: finite elsewhere"
+        got, want = got.where(fine, 0.0), want.where(fine, 0.0)
     assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{what}: NaNs elsewhere"
     rest = ~fine & ~torch.isnan(want)
     assert torch.equal(got[rest], want[rest]), f"{what}: infinities elsewhere"

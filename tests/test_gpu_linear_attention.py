@@ -63,7 +63,9 @@ def run(dtype, lengths, heads, qk_heads, dk, dv, tail=0, slots=None, pool=None, 
     bound_pool = pool if state or slots is None else 1 << 31
     o, off, new, new_off = linear_64(q, k, v, g, scale, o_before, st, new_before, sequence_list(lengths, slots, resume), bound_pool,
                                      0.0 if dtype == "f32" else half_step(tdt))
-    close(og.view, o, off + rounding(o, tdt), "o")
+    # By chunks an infinity of v meets q . k, one number: it comes out as an infinity.  In the recurrence it meets each element of k and then
+    # of q, infinities of both signs, whose sum is a NaN.  Both are right readings of the formula; o is not finite in the same places.
+    close(og.view, o, off + rounding(o, tdt), "o", same_infinities=dtype == "f32")
     for t in (og, ws):
         t.assert_untouched_outside()
     if state:
