@@ -6,7 +6,7 @@
 //   S   <- exp(G_n) S + sum_j exp(G_n - G_j) k_j^T v_j                                      "added"
 //
 // A block has one head, a tile of 128 columns of dv and a run of chunks of one sequence.  S stays in its registers, transposed: a
-// thread has a column of dv and half of dk.  All products with S or v are made transposed, so that their 128 rows are dv:
+// thread has a column of dv and a quarter of dk.  All products with S or v are made transposed, so that their 128 rows are dv:
 //
 //   inter^T [dv][64 tokens] = S^T (16 bits, tensor memory) x q        added^T [dv][dk] = v^T x (weighted k)
 //   intra^T [dv][64 tokens] = v^T x P,  P_ij = exp(G_i - G_j) (q_i . k_j)
@@ -20,14 +20,16 @@
 // through the tensor cores as pieces whose sum is the fp32 product to 2^-22 (three of bf16, cut off exactly; two of fp16).  fp16 has no
 // room for large or small numbers: S, P and the weighted k are brought to 2^13 by a power of two for each chunk.
 // log_decay is summed in 64 bits, differences are split into whole and fractional powers of two, so that no cancellation is left
-// behind a strong decay.  A product of a masked 0, or of a piece that is 0 or has the other sign, with an infinity of v is a NaN: where
-// o is not finite the chunk's intra part is made again from its terms j <= i alone, and where what a chunk adds to the state is not,
-// that is made again from the fp32 products.
+// behind a strong decay.  A product of a masked 0, or of a piece that is 0 or has the other sign, with an infinity of v is a NaN: a
+// chunk whose k or v hold any has its intra part made again from the terms j <= i alone, and what it adds to the state from fp32 products.
 //
 // Long sequences are cut into segments of several chunks where there are too few heads and sequences for the GPU: one launch sums up
 // what each segment adds to a zero state, a second one runs over the segments of a sequence and leaves each one's starting state, and
 // the main one then has all segments at once.
 #include <float.h>
+#include <stdlib.h>
+
+#include <algorithm>
 
 #include "common.cuh"
 #include "ptx_sm100.cuh"
@@ -39,7 +41,9 @@ namespace {
 using namespace ptx;
 
 constexpr int kChunk = 64;               // tokens
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
+constexpr int kQuarters = kThreads / 128; // parts of dk, and of a chunk's tokens, of the threads that have a column of dv
+constexpr int kDecayWarp = 15;
 constexpr int kTile = 128;               // columns of dv of a block: rows of the products
 constexpr uint32_t kPanel = 64 * 128;    // 64 rows of 64 16-bit elements, 128-byte swizzle
 
@@ -52,7 +56,7 @@ struct ChunkParams {
   const float* state_in;                 // states of the pool, or of the segments (segmented)
   float* state_out;
   float* added;                          // [segments][heads][dk][dv]
-  float2* totals;                        // [segments][heads]: decay of a whole segment, and less one
+  float2* totals;                        // [segments][heads]: decay of a whole segment, in two parts
   uint32_t* status;
   Sequences seqs;
   int64_t q_stride, k_stride, v_stride, o_stride, decay_stride;
@@ -66,6 +70,7 @@ template <> struct Kind<__nv_bfloat16> {
   static constexpr int kPieces = 3;
   static constexpr bool kScaled = false;
   static constexpr uint32_t kFormats = (1u << 7) | (1u << 10);
+  static constexpr uint32_t kOddStep = 0x00800080u;          // added to an exponent of all ones reaches the sign
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
@@ -78,14 +83,12 @@ template <> struct Kind<__nv_bfloat16> {
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
-  // Two numbers as pieces: the upper half, the upper half of the rest, the rest of that (exact: 24 bits).  An infinity is its first
-  // piece, a NaN too.
+  // Two numbers as pieces: the upper half, the upper half of the rest, the rest of that (exact: 24 bits).
   static __device__ __forceinline__ void split(float a, float b, uint32_t (&piece)[3]) {
     const float a1 = a - __uint_as_float(__float_as_uint(a) & 0xffff0000u), b1 = b - __uint_as_float(__float_as_uint(b) & 0xffff0000u);
     piece[0] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-    const float ra = a1 == a1 ? a1 : 0.0f, rb = b1 == b1 ? b1 : 0.0f;
-    piece[1] = __byte_perm(__float_as_uint(ra), __float_as_uint(rb), 0x7632);
-    const float a2 = ra - __uint_as_float(__float_as_uint(ra) & 0xffff0000u), b2 = rb - __uint_as_float(__float_as_uint(rb) & 0xffff0000u);
+    piece[1] = __byte_perm(__float_as_uint(a1), __float_as_uint(b1), 0x7632);
+    const float a2 = a1 - __uint_as_float(__float_as_uint(a1) & 0xffff0000u), b2 = b1 - __uint_as_float(__float_as_uint(b1) & 0xffff0000u);
     piece[2] = __byte_perm(__float_as_uint(a2), __float_as_uint(b2), 0x7632);
   }
 };
@@ -93,6 +96,7 @@ template <> struct Kind<__half> {
   static constexpr int kPieces = 2;
   static constexpr bool kScaled = true;
   static constexpr uint32_t kFormats = 0;
+  static constexpr uint32_t kOddStep = 0x04000400u;
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
@@ -109,7 +113,7 @@ template <> struct Kind<__half> {
   static __device__ __forceinline__ void split(float a, float b, uint32_t (&piece)[2]) {
     piece[0] = pack(a, b);
     const float a1 = a - low(piece[0]), b1 = b - high(piece[0]);
-    piece[1] = pack(a1 == a1 ? a1 : 0.0f, b1 == b1 ? b1 : 0.0f);
+    piece[1] = pack(a1, b1);
   }
 };
 
@@ -133,22 +137,17 @@ __device__ __forceinline__ uint32_t ld_shared_u16(uint32_t addr) {
   return v;
 }
 __device__ __forceinline__ void st_shared4(uint32_t addr, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
-      "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // MMA with A in tensor memory (its elements two a column along K) and B by descriptor.
@@ -177,13 +176,25 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // The decays of one chunk, all relative to its start.
 struct Decays {
   float whole[kChunk], part[kChunk];     // G_i in powers of two: its floor and the rest
-  float from_start[kChunk];              // exp(G_i)
+  float from_start[kChunk];              // exp(G_i) scale
   float to_end[kChunk];                  // exp(G_n - G_i)
-  float total, total_less_one;           // exp(G_n)
+  float2 total;                          // exp(G_n) in two parts
 };
 
+// S <- exp(G_n) S + added, exp(G_n) in two parts (see chunk_decays): off by less than a rounding of the sum, also after many chunks of
+// a decay near 1.
+__device__ __forceinline__ float carry(float s, float2 total, float added) { return fmaf(s, total.x, fmaf(s, total.y, added)); }
+
+// exp2(power) as the float below it and the rest, so that an infinity times either has its sign (and no rest where nothing is left).
+__device__ __forceinline__ float2 two_parts(double power) {
+  const double all = exp2(power);
+  const float hi = __double2float_rz(all);
+  const float lo = (float)(all - (double)hi);
+  return make_float2(hi, hi > 0.0f && lo < FLT_MIN ? FLT_MIN : lo);
+}
+
 // One warp: lane l has tokens 2l and 2l+1.  Returns G_n (powers of two).
-__device__ __forceinline__ double chunk_decays(float g0, float g1, Decays& d) {
+__device__ __forceinline__ double chunk_decays(float g0, float g1, float scale, Decays& d) {
   const int lane = threadIdx.x & 31;
   auto powers = [](float g) -> double {
     const double p = (double)g * 1.4426950408889634074;
@@ -203,13 +214,10 @@ __device__ __forceinline__ double chunk_decays(float g0, float g1, Decays& d) {
     const double floor_of = floor(G[i]);
     d.whole[2 * lane + i] = (float)floor_of;
     d.part[2 * lane + i] = (float)(G[i] - floor_of);
-    d.from_start[2 * lane + i] = (float)exp2(G[i]);
+    d.from_start[2 * lane + i] = (float)exp2(G[i]) * scale;
     d.to_end[2 * lane + i] = (float)exp2(all - G[i]);
   }
-  if (lane == 0) {
-    d.total = (float)exp2(all);
-    d.total_less_one = (float)expm1(all * 0.69314718055994530942);
-  }
+  if (lane == 0) d.total = two_parts(all);
   return all;
 }
 
@@ -228,15 +236,6 @@ __device__ __forceinline__ void raise_max(uint32_t* at, uint32_t bits) {
   if ((threadIdx.x & 31) == 0) atomicMax(at, m);
 }
 
-// S <- total S + added
-__device__ __forceinline__ float carry(float s, float total, float less_one, float added) {
-  if (total > 0.5f) {
-    const float part = fabsf(s) <= FLT_MAX ? s : 0.0f;         // (see attention_tokens.cu)
-    return s + fmaf(part, less_one, added);
-  }
-  return fmaf(s, total, added);
-}
-
 template <typename T, int DK, bool OUT>
 struct Layout {
   static constexpr uint32_t kQK = DK / 64 * kPanel;            // q or k of a chunk
@@ -250,15 +249,39 @@ struct Layout {
   static constexpr uint32_t kColumns = OUT ? (DK == 128 ? 512 : 256) : DK;
 };
 
+// N columns of tensor memory, 32 bits each, of this warp's lanes.
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[N]) {
+  static_assert(N == 16 || N == 32, "");
+  if constexpr (N == 32) {
+    tmem_ld32_issue(taddr, r);
+  } else {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+  }
+}
+// The wait for a load into r[] (naming the registers keeps every use of them behind it).
+template <int N>
+__device__ __forceinline__ void tmem_ld_done(uint32_t (&r)[N]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
+
 template <typename T, int DK, bool OUT>
 __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p) {
   using K = Kind<T>;
   using L = Layout<T, DK, OUT>;
-  constexpr int kHalf = DK / 2;                                // columns of S of a thread
+  constexpr int kMine = DK / kQuarters;                        // columns of S of a thread
+  constexpr int kTokens = kChunk / kQuarters;                  // rows of o of a thread
   extern __shared__ uint8_t dynamic_smem[];
   __shared__ Decays decays[2];
   __shared__ __align__(8) uint64_t done_bar;
-  __shared__ uint32_t tmem_base_at, abort_flag, again, largest[2][3];
+  __shared__ uint32_t tmem_base_at, abort_flag, odd_values[2], largest[2][3];
   const uint32_t smem = (smem_u32(dynamic_smem) + 1023u) & ~1023u;
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
   const uint32_t tile = blockIdx.x % (uint32_t)p.tiles, rest = blockIdx.x / (uint32_t)p.tiles;
@@ -272,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
   const bool last = end == piece.rows.end;
   if (!OUT && last) return;                                    // (nothing starts behind it)
 
-  const int half = warp >> 2, row = (warp & 3) * 32 + lane;    // row: of the transposed products, a column of dv
+  const int quarter = warp >> 2, row = (warp & 3) * 32 + lane; // row: of the transposed products, a column of dv
   const int col = (int)tile * kTile + row;
   const bool live = col < p.dv;
   const int64_t state_size = (int64_t)p.dk * p.dv;
@@ -282,12 +305,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
   if (tid == 0) {
     mbar_init(bar, 1);
     abort_flag = 0;
-    again = 0;
     for (int i = 0; i < 6; ++i) largest[i / 3][i % 3] = 0;
+    odd_values[0] = odd_values[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (OUT)
-    for (uint32_t at = tid * 16; at < kPanel; at += kThreads * 16) st_shared16(smem + L::kPAt + at, 0, 0, 0, 0);
+  if (OUT && tid < kPanel / 16) st_shared16(smem + L::kPAt + tid * 16, 0, 0, 0, 0);      // (above the diagonal it stays 0)
 
   const T* q = static_cast<const T*>(p.q) + (int64_t)(head / p.share) * p.dk;
   const T* k = static_cast<const T*>(p.k) + (int64_t)(head / p.share) * p.dk;
@@ -322,13 +344,13 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
 
   if (first < end) load(0, first);
   double all_decay = 0.0;
-  if (warp == 7 && first < end) {
+  if (warp == kDecayWarp && first < end) {
     float g0, g1;
     load_decay(first, g0, g1);
-    all_decay = chunk_decays(g0, g1, decays[0]);
+    all_decay = chunk_decays(g0, g1, p.scale, decays[0]);
   }
   // the starting state
-  float S[kHalf];
+  float S[kMine];
   {
     const float* from = nullptr;
     if (OUT && live) {
@@ -338,46 +360,15 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
         from = p.state_in + ((int64_t)slot * p.heads + head) * state_size;
     }
 #pragma unroll
-    for (int j = 0; j < kHalf; ++j) {
-      const int d = half * kHalf + j;
+    for (int j = 0; j < kMine; ++j) {
+      const int d = quarter * kMine + j;
       S[j] = from && d < p.dk ? from[(int64_t)d * p.dv + col] : 0.0f;
     }
   }
 
   T* o = static_cast<T*>(p.o) + (int64_t)head * p.dv + col;
   uint32_t tmem = 0, lanes = 0;
-  bool ok = true;
   const int chunks = (end - first + kChunk - 1) / kChunk;
-  // the intra part of the chunk before, from its terms j <= i alone
-  auto make_again = [&](int c) {
-    if (!OUT) return;
-    const Decays& d = decays[c & 1];
-    const uint32_t vt = smem + (c & 1) * L::kStage + L::kQK + (row >> 6) * kPanel;
-    const int t0 = first + c * kChunk;
-    float is = 1.0f, ip = 1.0f;
-    if (K::kScaled) {
-      is = 1.0f / scale_for(largest[c & 1][2]);
-      ip = 1.0f / scale_for(largest[c & 1][1]);
-    }
-    uint32_t inter[32];
-    tmem_ld32(tmem + lanes + L::kInter + half * 32, inter);
-    for (int i = 0; i < 32; ++i) {
-      const int ti = half * 32 + i;
-      float sum = 0.0f;
-      for (int j = 0; j <= ti; ++j) {
-        const float w = K::low(ld_shared_u16(smem + L::kPAt + ti * 128 + ((((uint32_t)j >> 3) ^ (ti & 7)) << 4) + (j & 7) * 2));
-        const float x = K::low(ld_shared_u16(vt + j * 128 + ((((uint32_t)(row & 63) >> 3) ^ (j & 7)) << 4) + (row & 7) * 2));
-        sum = fmaf(w, x, sum);
-      }
-      float from_state = 0.0f;
-#pragma unroll
-      for (int u = 0; u < 32; ++u)
-        if (u == i) from_state = __uint_as_float(inter[u]);
-      if (live && t0 + ti < end)
-        o[(int64_t)(t0 + ti) * p.o_stride] = from_float<T>(p.scale * fmaf(d.from_start[ti] * is, from_state, sum * ip));
-    }
-  };
-
   for (int c = 0; c < chunks; ++c) {
     const int stage = c & 1, t0 = first + c * kChunk;
     const uint32_t base = smem + stage * L::kStage;
@@ -391,28 +382,21 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
       tmem = tmem_base_at;
       lanes = (uint32_t)(warp & 3) << 21;                      // this warp's 32 lanes
     }
-    if (*(volatile uint32_t*)&abort_flag) { ok = false; break; }
-    if (OUT && *(volatile uint32_t*)&again) {                  // (the same for every thread: raised before the barrier)
-      make_again(c - 1);
-      tc_fence_before();
-      __syncthreads();
-      tc_fence_after();
-      if (tid == 0) again = 0;
-    }
+    if (*(volatile uint32_t*)&abort_flag) break;
     if (c + 1 < chunks) load(stage ^ 1, t0 + kChunk);
     float g0 = 0.0f, g1 = 0.0f;
-    if (warp == 7 && c + 1 < chunks) load_decay(t0 + kChunk, g0, g1);
+    if (warp == kDecayWarp && c + 1 < chunks) load_decay(t0 + kChunk, g0, g1);
     const Decays& d = decays[stage];
 
-    // q . k: 16 x 8 blocks that reach below the diagonal; of the four rows of blocks, the last one's eight go to warps 0 to 2, the
-    // next one's six to 3 and 4, then four to 5 and 6, and two to 7
-    float P[3][4];
-    const int rb = warp < 3 ? 3 : warp < 5 ? 2 : warp < 7 ? 1 : 0;
-    const int nt0 = warp < 3 ? warp * 3 : warp < 5 ? (warp - 3) * 3 : warp < 7 ? (warp - 5) * 2 : 0;
-    const int nts = rb == 3 ? min(3, 8 - nt0) : rb == 2 ? 3 : 2;
-    if (OUT) {
+    // q . k: the 16 x 8 blocks that reach below the diagonal, two in each of the first ten warps: eight of the last row of blocks,
+    // six of the one before, four, two
+    float P[2][4];
+    const int rb = warp < 4 ? 3 : warp < 7 ? 2 : warp < 9 ? 1 : 0;
+    const int nt0 = 2 * (warp < 4 ? warp : warp < 7 ? warp - 4 : warp < 9 ? warp - 7 : 0);
+    const bool makes_p = OUT && warp < 10;
+    if (makes_p) {
 #pragma unroll
-      for (int n = 0; n < 3; ++n)
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) P[n][i] = 0.0f;
 #pragma unroll
@@ -424,8 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
           ldmatrix_x4(qt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), a[i]);
         }
 #pragma unroll
-        for (int n = 0; n < 3; ++n) {
-          if (n >= nts) break;
+        for (int n = 0; n < 2; ++n) {
           const int r = (nt0 + n) * 8 + (lane & 7), cc = ks * 2 + (lane >> 3);
           uint32_t b[4];
           ldmatrix_x4(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), b);
@@ -434,35 +417,43 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
         }
       }
 #pragma unroll
-      for (int n = 0; n < 3; ++n) {
-        if (n >= nts) break;
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int ti = rb * 16 + (lane >> 2) + 8 * (i >> 1), tj = (nt0 + n) * 8 + 2 * (lane & 3) + (i & 1);
           const float power = (d.whole[ti] - d.whole[tj]) + (d.part[ti] - d.part[tj]);
-          P[n][i] = tj <= ti ? P[n][i] * exp2_fast(power) : 0.0f;
+          P[n][i] = tj <= ti ? P[n][i] * (exp2_fast(power) * p.scale) : 0.0f;
         }
-      }
     }
-    constexpr int kUnits = DK / 8, kMine = kChunk * kUnits / kThreads;
-    uint4 kk[kMine];
+    constexpr int kUnits = DK / 8, kVectors = kChunk * kUnits / kThreads;
+    uint4 kk[kVectors];
+    uint32_t odd = 0;                                          // bits 15 and 31: an infinity or NaN
+    auto look = [&](uint32_t w) { odd |= (w & 0x7fff7fffu) + K::kOddStep; };
 #pragma unroll
-    for (int m = 0; m < kMine; ++m) {
+    for (int m = 0; m < kVectors; ++m) {
       const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
       kk[m] = ld_shared16(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4));
+      look(kk[m].x); look(kk[m].y); look(kk[m].z); look(kk[m].w);
     }
+    const bool odd_k = (odd & 0x80008000u) != 0;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const uint4 vv = ld_shared16(vt + (tid + m * kThreads) * 16);
+      look(vv.x); look(vv.y); look(vv.z); look(vv.w);
+    }
+    if (odd & 0x80008000u) odd_values[stage] = 1;
     float scale_k = 1.0f, scale_p = 1.0f, scale_s = 1.0f;
     if (K::kScaled) {
-      uint32_t top = 0, odd = 0;
+      uint32_t top = 0;
 #pragma unroll
-      for (int m = 0; m < kMine; ++m)
-        for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) {
-          top = __vmaxu2(top, w & 0x7fff7fffu);
-          odd |= ((w & 0x7fff7fffu) + 0x04000400u) & 0x80008000u;
-        }
-      if (odd) {                                               // infinities or NaNs: the largest of the others
+      for (int m = 0; m < kVectors; ++m)
+#pragma unroll
+        for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) top = __vmaxu2(top, w & 0x7fff7fffu);
+      if (odd_k) {                                             // the largest of the others
         top = 0;
-        for (int m = 0; m < kMine; ++m)
+#pragma unroll
+        for (int m = 0; m < kVectors; ++m)
+#pragma unroll
           for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) {
             if ((w & 0x7c00u) != 0x7c00u) top = __vmaxu2(top, w & 0x7fffu);
             if ((w & 0x7c000000u) != 0x7c000000u) top = __vmaxu2(top, w & 0x7fff0000u);
@@ -471,13 +462,15 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
       raise_max(&largest[stage][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
       if (OUT) {
         uint32_t pm = 0, sm = 0;
+        if (makes_p) {
 #pragma unroll
-        for (int n = 0; n < 3; ++n)
-          if (n < nts)
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
             for (int i = 0; i < 4; ++i) pm = max(pm, finite_bits(P[n][i]));
-        raise_max(&largest[stage][1], pm);
+          raise_max(&largest[stage][1], pm);
+        }
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) sm = max(sm, finite_bits(S[j]));
+        for (int j = 0; j < kMine; ++j) sm = max(sm, finite_bits(S[j]));
         raise_max(&largest[stage][2], sm);
       }
       __syncthreads();
@@ -487,33 +480,23 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
         scale_s = scale_for(largest[stage][2]);
       }
     }
-    if (OUT) {
+    if (makes_p) {
 #pragma unroll
-      for (int n = 0; n < 3; ++n) {
-        if (n >= nts) break;
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int ti = rb * 16 + (lane >> 2) + 8 * i, cc = nt0 + n;
           st_shared4(smem + L::kPAt + ti * 128 + ((cc ^ (ti & 7)) << 4) + (lane & 3) * 4, K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
         }
-      }
+    }
+    if (OUT) {
+      uint32_t r[kMine / 2];
 #pragma unroll
-      for (int j = 0; j < kHalf; j += 64) {
-        uint32_t r[32];
-        if (kHalf >= 64) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) r[i] = K::pack(S[(j + 2 * i) % kHalf] * scale_s, S[(j + 2 * i + 1) % kHalf] * scale_s);
-          tmem_st32(tmem + lanes + L::kS + half * (kHalf / 2) + j / 2, r);
-        } else {
-          uint32_t h[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) h[i] = K::pack(S[2 * i] * scale_s, S[2 * i + 1] * scale_s);
-          tmem_st16(tmem + lanes + L::kS + half * (kHalf / 2), h);
-        }
-      }
+      for (int i = 0; i < kMine / 2; ++i) r[i] = K::pack(S[2 * i] * scale_s, S[2 * i + 1] * scale_s);
+      tmem_st(tmem + lanes + L::kS + quarter * (kMine / 2), r);
     }
 #pragma unroll
-    for (int m = 0; m < kMine; ++m) {
+    for (int m = 0; m < kVectors; ++m) {
       const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
       const float w = d.to_end[r] * scale_k;
       const uint32_t words[4] = {kk[m].x, kk[m].y, kk[m].z, kk[m].w};
@@ -541,6 +524,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
         for (int ks = 0; ks < DK / 16; ++ks)
           umma_f16_ta(tmem + L::kInter, tmem + L::kS + ks * 8, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), kDescHi,
                       kBase | instr_desc_f16(128, 64), ks > 0);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          umma_f16_ab(tmem + L::kIntra, desc_lo_mn(vt + ks * 2048), kDescHi, smem_desc_lo(smem + L::kPAt + ks * 32), kDescHi,
+                      kBase | kAlongM | instr_desc_f16(128, 64), ks > 0);
       }
 #pragma unroll
       for (int n = K::kPieces - 1; n >= 0; --n)                // the smallest pieces first
@@ -548,74 +535,72 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
         for (int ks = 0; ks < 4; ++ks)
           umma_f16_ab(tmem + L::kAdded, desc_lo_mn(vt + ks * 2048), kDescHi, desc_lo_mn(smem + L::kPiecesAt + n * L::kQK + ks * 2048), kDescHi,
                       kBase | kAlongM | kAlongN | instr_desc_f16(128, DK), n < K::kPieces - 1 || ks > 0);
-      if (OUT) {
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          umma_f16_ab(tmem + L::kIntra, desc_lo_mn(vt + ks * 2048), kDescHi, smem_desc_lo(smem + L::kPAt + ks * 32), kDescHi,
-                      kBase | kAlongM | instr_desc_f16(128, 64), ks > 0);
-      }
       umma_commit(bar);
     }
-    if (K::kScaled && tid == 32)
-      for (int i = 0; i < 3; ++i) largest[stage ^ 1][i] = 0;
-    if (warp == 7 && c + 1 < chunks) all_decay += chunk_decays(g0, g1, decays[stage ^ 1]);
+    if (tid == 32) {
+      odd_values[stage ^ 1] = 0;
+      if (K::kScaled)
+        for (int i = 0; i < 3; ++i) largest[stage ^ 1][i] = 0;
+    }
+    if (warp == kDecayWarp && c + 1 < chunks) all_decay += chunk_decays(g0, g1, p.scale, decays[stage ^ 1]);
     mbar_wait(bar, (uint32_t)(c & 1), &abort_flag, p.status);
     tc_fence_after();
 
+    // (every thread sees the same: written before the barrier)
+    const bool again = *(volatile uint32_t*)&odd_values[stage] != 0;
+    // element e of row t of a panel pair at `at`
+    auto element = [&](uint32_t at, int t, int e) {
+      return K::low(ld_shared_u16(at + (e >> 6) * kPanel + t * 128 + ((((uint32_t)(e & 63) >> 3) ^ (t & 7)) << 4) + (e & 7) * 2));
+    };
+    uint32_t added[kMine];
+    tmem_ld(tmem + lanes + L::kAdded + quarter * kMine, added);
     if (OUT) {
       const float is = 1.0f / scale_s, ip = 1.0f / scale_p;
-      uint32_t inter[32], intra[32];
-      tmem_ld32_issue(tmem + lanes + L::kInter + half * 32, inter);
-      tmem_ld32_issue(tmem + lanes + L::kIntra + half * 32, intra);
-      tmem_ld_wait_for(inter);
-      tmem_ld_wait_for(intra);
-      bool fine = true;
-      T* at = o + (int64_t)(t0 + half * 32) * p.o_stride;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const float from = d.from_start[half * 32 + i] * is;
-        const float y = p.scale * fmaf(from, __uint_as_float(inter[i]), __uint_as_float(intra[i]) * ip);
-        fine = fine && fabsf(y) <= FLT_MAX;
-        if (live && t0 + half * 32 + i < end) at[(int64_t)i * p.o_stride] = from_float<T>(y);
-      }
-      if (!fine) again = 1;
-    }
-    const float ik = 1.0f / scale_k, total = d.total, less_one = d.total_less_one;
-#pragma unroll
-    for (int j = 0; j < kHalf; j += 32) {
-      uint32_t added[32];
-      tmem_ld32(tmem + lanes + L::kAdded + half * kHalf + j, added);
-      float none = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) none = fmaf(__uint_as_float(added[i]), 0.0f, none);
-      if (none != 0.0f) {                                      // (a NaN: a piece's 0 or other sign may have met an infinity of v)
-        const uint32_t column = vt + (row >> 6) * kPanel;
+      uint32_t inter[kTokens], intra[kTokens];
+      tmem_ld(tmem + lanes + L::kInter + quarter * kTokens, inter);
+      tmem_ld(tmem + lanes + L::kIntra + quarter * kTokens, intra);
+      tmem_ld_done(inter);
+      tmem_ld_done(intra);
+      if (again) {                                             // from the terms j <= i alone
 #pragma unroll 1
-        for (int i = 0; i < 32; ++i) {
-          const int e = half * kHalf + j + i;
+        for (int i = 0; i < kTokens; ++i) {
+          const int ti = quarter * kTokens + i;
           float sum = 0.0f;
 #pragma unroll 1
-          for (int t = 0; t < kChunk; ++t) {
-            const float kv = K::low(ld_shared_u16(kt + (e >> 6) * kPanel + t * 128 + ((((uint32_t)(e & 63) >> 3) ^ (t & 7)) << 4) + (e & 7) * 2));
-            const float vv = K::low(ld_shared_u16(column + t * 128 + ((((uint32_t)(row & 63) >> 3) ^ (t & 7)) << 4) + (row & 7) * 2));
-            if (t0 + t < end) sum = fmaf(kv * d.to_end[t], vv, sum);
-          }
+          for (int j = 0; j <= ti; ++j) sum = fmaf(element(smem + L::kPAt, ti, j), element(vt, j, row), sum);
 #pragma unroll
-          for (int u = 0; u < 32; ++u)
-            if (u == i) added[u] = __float_as_uint(sum * scale_k);
+          for (int u = 0; u < kTokens; ++u)
+            if (u == i) intra[u] = __float_as_uint(sum);
         }
       }
+      T* at = o + (int64_t)(t0 + quarter * kTokens) * p.o_stride;
+      const int n = live ? end - (t0 + quarter * kTokens) : 0;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) S[j + i] = carry(S[j + i], total, less_one, __uint_as_float(added[i]) * ik);
+      for (int i = 0; i < kTokens; ++i) {
+        const float y = fmaf(d.from_start[quarter * kTokens + i] * is, __uint_as_float(inter[i]), __uint_as_float(intra[i]) * ip);
+        if (i < n) at[(int64_t)i * p.o_stride] = from_float<T>(y);
+      }
     }
+    tmem_ld_done(added);
+    if (again) {                                               // from the products in fp32
+#pragma unroll 1
+      for (int i = 0; i < kMine; ++i) {
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int t = 0; t < kChunk && t0 + t < end; ++t)
+          sum = fmaf(element(kt, t, quarter * kMine + i) * d.to_end[t], element(vt, t, row), sum);
+#pragma unroll
+        for (int u = 0; u < kMine; ++u)
+          if (u == i) added[u] = __float_as_uint(sum * scale_k);
+      }
+    }
+    const float ik = 1.0f / scale_k;
+    const float2 total = d.total;
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) S[j] = carry(S[j], total, __uint_as_float(added[j]) * ik);
   }
 
   asm volatile("cp.async.wait_group 0;" ::: "memory");
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  if (chunks == 0) tmem = tmem_base_at;
-  if (OUT && ok && chunks > 0 && again) make_again(chunks - 1);
   float* to = nullptr;
   if (!OUT)
     to = p.added + ((int64_t)id * p.heads + head) * state_size;
@@ -623,16 +608,16 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
     to = p.state_out + ((int64_t)slot * p.heads + head) * state_size;
   if (to && live) {
 #pragma unroll
-    for (int j = 0; j < kHalf; ++j) {
-      const int dd = half * kHalf + j;
-      if (dd < p.dk) to[(int64_t)dd * p.dv + col] = S[j];
+    for (int j = 0; j < kMine; ++j) {
+      const int e = quarter * kMine + j;
+      if (e < p.dk) to[(int64_t)e * p.dv + col] = S[j];
     }
   }
-  if (!OUT && warp == 7 && lane == 0 && tile == 0)
-    p.totals[(int64_t)id * p.heads + head] = make_float2((float)exp2(all_decay), (float)expm1(all_decay * 0.69314718055994530942));
+  if (!OUT && warp == kDecayWarp && lane == 0 && tile == 0) p.totals[(int64_t)id * p.heads + head] = two_parts(all_decay);
   tc_fence_before();
   __syncthreads();
-  if (warp == 0) tmem_dealloc(tmem, L::kColumns);
+  tc_fence_after();
+  if (warp == 0) tmem_dealloc(tmem_base_at, L::kColumns);
 }
 
 // The starting state of every segment, in the place of what it adds: a thread has a number of a head's state and runs over the
@@ -663,7 +648,7 @@ __global__ void __launch_bounds__(256) segment_states_kernel(const ChunkParams p
     for (int i = 0; i < kAhead; ++i) {
       if (i0 + i >= n) break;
       p.added[((id0 + i0 + i) * p.heads + head) * size + e] = s;
-      s = carry(s, total[i].x, total[i].y, added[i]);
+      s = carry(s, total[i], added[i]);
     }
   }
 }
@@ -697,6 +682,7 @@ ChunkPlan plan_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool 
     if (n > 1) cost += (double)((like * blocks * (n - 1) + 147) / 148) * (double)per * 0.6 + 8.0;
     if (n == 1 || cost < best) { best = cost; best_n = n; }
   }
+  if (const char* v = debug_getenv("IM2WIN_SEGMENTS")) best_n = std::min<int64_t>(std::max(atoi(v), 1), chunks);    // testing aid
   c.totals_off = c.added_off = c.bytes = kStatusBytes;
   c.L = INT32_MAX;
   if (best_n > 1) {
