@@ -43,7 +43,9 @@ using namespace ptx;
 constexpr int kChunk = 64;               // tokens
 constexpr int kThreads = 512;
 constexpr int kQuarters = kThreads / 128; // parts of dk, and of a chunk's tokens, of the threads that have a column of dv
-constexpr int kDecayWarp = 15;
+constexpr int kStages = 3;
+// Warps with a job besides their share; those that make no P (see chunk_kernel)
+constexpr int kLoadWarp = 13, kDecayWarp = 14, kMmaWarp = 15;
 constexpr int kTile = 128;               // columns of dv of a block: rows of the products
 constexpr uint32_t kPanel = 64 * 128;    // 64 rows of 64 16-bit elements, 128-byte swizzle
 
@@ -61,8 +63,13 @@ struct ChunkParams {
   Sequences seqs;
   int64_t q_stride, k_stride, v_stride, o_stride, decay_stride;
   int32_t heads, share, dk, dv, tiles, L;
-  int32_t segmented;
+  int32_t segmented, o_by_map;           // o_by_map: rows of o start on 16-byte boundaries
   float scale;
+};
+
+// q, k, v as [tokens][heads][dk or dv] in boxes of 64 tokens of 64 elements of a head, o in boxes of 64 tokens of 128.
+struct alignas(64) ChunkMaps {
+  CUtensorMap q, k, v, o;
 };
 
 template <typename T> struct Kind;
@@ -181,46 +188,6 @@ struct Decays {
   float2 total;                          // exp(G_n) in two parts
 };
 
-// S <- exp(G_n) S + added, exp(G_n) in two parts (see chunk_decays): off by less than a rounding of the sum, also after many chunks of
-// a decay near 1.
-__device__ __forceinline__ float carry(float s, float2 total, float added) { return fmaf(s, total.x, fmaf(s, total.y, added)); }
-
-// exp2(power) as the float below it and the rest, so that an infinity times either has its sign (and no rest where nothing is left).
-__device__ __forceinline__ float2 two_parts(double power) {
-  const double all = exp2(power);
-  const float hi = __double2float_rz(all);
-  const float lo = (float)(all - (double)hi);
-  return make_float2(hi, hi > 0.0f && lo < FLT_MIN ? FLT_MIN : lo);
-}
-
-// One warp: lane l has tokens 2l and 2l+1.  Returns G_n (powers of two).
-__device__ __forceinline__ double chunk_decays(float g0, float g1, float scale, Decays& d) {
-  const int lane = threadIdx.x & 31;
-  auto powers = [](float g) -> double {
-    const double p = (double)g * 1.4426950408889634074;
-    return p < -1000.0 ? -1000.0 : p;          // (2^-1000 is 0 in fp32; a NaN stays one)
-  };
-  const double a = powers(g0), b = powers(g1);
-  double sum = a + b;
-#pragma unroll
-  for (int s = 1; s < 32; s *= 2) {
-    const double other = __shfl_up_sync(0xffffffffu, sum, s);
-    if (lane >= s) sum += other;
-  }
-  const double all = __shfl_sync(0xffffffffu, sum, 31);
-  const double G[2] = {sum - b, sum};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const double floor_of = floor(G[i]);
-    d.whole[2 * lane + i] = (float)floor_of;
-    d.part[2 * lane + i] = (float)(G[i] - floor_of);
-    d.from_start[2 * lane + i] = (float)exp2(G[i]) * scale;
-    d.to_end[2 * lane + i] = (float)exp2(all - G[i]);
-  }
-  if (lane == 0) d.total = two_parts(all);
-  return all;
-}
-
 // A power of two that brings numbers of at most `bits` (of a float) to below 2^14.
 __device__ __forceinline__ float scale_for(uint32_t bits) {
   const int e = (int)(bits >> 23);
@@ -236,17 +203,73 @@ __device__ __forceinline__ void raise_max(uint32_t* at, uint32_t bits) {
   if ((threadIdx.x & 31) == 0) atomicMax(at, m);
 }
 
+// S <- exp(G_n) S + added, exp(G_n) in two parts (see two_parts): off by less than a rounding of the sum, also after many chunks of
+// a decay near 1.
+__device__ __forceinline__ float carry(float s, float2 total, float added) { return fmaf(s, total.x, fmaf(s, total.y, added)); }
+
+// exp2(power) as the float below it and the rest, so that an infinity times either has its sign (and no rest where nothing is left).
+__device__ __forceinline__ float2 two_parts(double power) {
+  const double all = exp2(power);
+  const float hi = __double2float_rz(all);
+  const float lo = (float)(all - (double)hi);
+  return make_float2(hi, hi > 0.0f && lo < FLT_MIN ? FLT_MIN : lo);
+}
+
+// One warp: lane l has tokens 2l and 2l+1.  Returns G_n (powers of two).  Sums are of whole numbers of 2^-44: exact, and without
+// the 64-bit floating-point units, which took 1300 cycles for sums and powers.
+__device__ __forceinline__ double chunk_decays(float g0, float g1, float scale, Decays& d) {
+  constexpr float kNaN = __builtin_nanf("");
+  const int lane = threadIdx.x & 31;
+  auto powers = [](float g) -> int64_t {                       // (beyond 2^+-1000 nothing changes in fp32)
+    return __double2ll_rn((double)fminf(fmaxf(g, -700.0f), 700.0f) * (1.4426950408889634074 * 17592186044416.0));
+  };
+  const int64_t a = powers(g0), b = powers(g1);
+  const uint32_t nan0 = __ballot_sync(0xffffffffu, g0 != g0), nan1 = __ballot_sync(0xffffffffu, g1 != g1);
+  int64_t sum = a + b;
+#pragma unroll
+  for (int s = 1; s < 32; s *= 2) {
+    const int64_t other = __shfl_up_sync(0xffffffffu, sum, s);
+    if (lane >= s) sum += other;
+  }
+  const int64_t all = __shfl_sync(0xffffffffu, sum, 31);
+  auto fraction = [](int64_t x) { return (float)((uint32_t)(x >> 20) & 0xffffffu) * 5.9604644775390625e-8f; };
+  auto power_of_two = [](int64_t x) { return __uint_as_float((uint32_t)(min(max((int)(x >> 44), -127), 128) + 127) << 23); };
+  const int64_t G[2] = {sum - b, sum};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t rest = all - G[i];
+    float whole = (float)(int)(G[i] >> 44), from = exp2f(fraction(G[i])) * power_of_two(G[i]) * scale;
+    float to_end = exp2f(fraction(rest)) * power_of_two(rest);
+    if (nan0 | nan1) {                                         // behind a NaN every sum is one
+      const uint32_t behind0 = (2u << lane) - 1u, behind1 = i ? (2u << lane) - 1u : (1u << lane) - 1u;
+      if ((nan0 & behind0) | (nan1 & behind1)) whole = from = kNaN;
+      to_end = kNaN;
+    }
+    d.whole[2 * lane + i] = whole;
+    d.part[2 * lane + i] = fraction(G[i]);
+    d.from_start[2 * lane + i] = from;
+    d.to_end[2 * lane + i] = to_end;
+  }
+  const double end = nan0 | nan1 ? (double)kNaN : (double)all * (1.0 / 17592186044416.0);
+  const float2 total = two_parts(end);
+  if (lane == 0) d.total = total;
+  return end;
+}
+
+// Shared memory: three stages of q, k and v, the pieces of the weighted k (two sets where o is not made), P, o on its way out.
 template <typename T, int DK, bool OUT>
 struct Layout {
   static constexpr uint32_t kQK = DK / 64 * kPanel;            // q or k of a chunk
   static constexpr uint32_t kV = 2 * kPanel;
   static constexpr uint32_t kStage = (OUT ? 2 : 1) * kQK + kV;
-  static constexpr uint32_t kPiecesAt = 2 * kStage;
-  static constexpr uint32_t kPAt = kPiecesAt + Kind<T>::kPieces * kQK;
-  static constexpr uint32_t kBytes = kPAt + (OUT ? kPanel : 0) + 1024;
+  static constexpr uint32_t kPieces = Kind<T>::kPieces * kQK;
+  static constexpr uint32_t kPiecesAt = kStages * kStage;
+  static constexpr uint32_t kPAt = kPiecesAt + (OUT ? 1 : 2) * kPieces;
+  static constexpr uint32_t kOAt = kPAt + kPanel;
+  static constexpr uint32_t kBytes = (OUT ? kOAt + kChunk * kTile * 2 : kPAt) + 1024;
   // columns of tensor memory
-  static constexpr uint32_t kAdded = 0, kInter = DK, kIntra = DK + 64, kS = DK + 128;
-  static constexpr uint32_t kColumns = OUT ? (DK == 128 ? 512 : 256) : DK;
+  static constexpr uint32_t kAdded = 0, kInter = DK, kIntra = DK + 128, kS = DK + 192;     // (o: two of inter; otherwise two of added)
+  static constexpr uint32_t kColumns = OUT ? 512 : 2 * DK;
 };
 
 // N columns of tensor memory, 32 bits each, of this warp's lanes.
@@ -272,16 +295,23 @@ __device__ __forceinline__ void tmem_ld_done(uint32_t (&r)[N]) {
   for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
 }
 
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y),
+               "r"(z)
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
 template <typename T, int DK, bool OUT>
-__global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p) {
+__global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constant__ ChunkMaps maps, const ChunkParams p) {
   using K = Kind<T>;
   using L = Layout<T, DK, OUT>;
   constexpr int kMine = DK / kQuarters;                        // columns of S of a thread
   constexpr int kTokens = kChunk / kQuarters;                  // rows of o of a thread
   extern __shared__ uint8_t dynamic_smem[];
-  __shared__ Decays decays[2];
-  __shared__ __align__(8) uint64_t done_bar;
-  __shared__ uint32_t tmem_base_at, abort_flag, odd_values[2], largest[2][3];
+  __shared__ Decays decays[3];
+  __shared__ __align__(8) uint64_t bars[kStages + 2];          // stages loaded; state products done (two), intra products done
+  __shared__ uint32_t tmem_base_at, abort_flag, odd_values[3], largest[2][3];
   const uint32_t smem = (smem_u32(dynamic_smem) + 1023u) & ~1023u;
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
   const uint32_t tile = blockIdx.x % (uint32_t)p.tiles, rest = blockIdx.x / (uint32_t)p.tiles;
@@ -299,54 +329,77 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
   const int col = (int)tile * kTile + row;
   const bool live = col < p.dv;
   const int64_t state_size = (int64_t)p.dk * p.dv;
+  const int chunks = (end - first + kChunk - 1) / kChunk, whole = (end - first) / kChunk;
 
-  const uint32_t bar = smem_u32(&done_bar);
+  const uint32_t loaded = smem_u32(bars), done = smem_u32(bars + kStages), intra_done = smem_u32(bars + kStages + 1);
   if (warp == 0) tmem_alloc(smem_u32(&tmem_base_at), L::kColumns);
   if (tid == 0) {
-    mbar_init(bar, 1);
+    for (int i = 0; i < kStages + 2; ++i) mbar_init(smem_u32(bars + i), 1);
     abort_flag = 0;
     for (int i = 0; i < 6; ++i) largest[i / 3][i % 3] = 0;
-    odd_values[0] = odd_values[1] = 0;
+    for (int i = 0; i < 3; ++i) odd_values[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async_smem();
   }
   if (OUT && tid < kPanel / 16) st_shared16(smem + L::kPAt + tid * 16, 0, 0, 0, 0);      // (above the diagonal it stays 0)
 
   const T* q = static_cast<const T*>(p.q) + (int64_t)(head / p.share) * p.dk;
   const T* k = static_cast<const T*>(p.k) + (int64_t)(head / p.share) * p.dk;
   const T* v = static_cast<const T*>(p.v) + (int64_t)head * p.dv + tile * kTile;
-  auto load = [&](int stage, int t0) {
-    const uint32_t base = smem + stage * L::kStage;
+  // A whole chunk: one thread, by TMA (elements beyond a head's read as 0).
+  auto load_whole = [&](int c) {
+    const uint32_t base = smem + (c % kStages) * L::kStage, bar = loaded + (c % kStages) * 8;
+    const int t0 = first + c * kChunk;
+    mbar_arrive_expect_tx(bar, L::kStage);
+#pragma unroll
+    for (int i = 0; i < DK / 64; ++i) {
+      tma_load_3d(base + i * kPanel, &maps.k, i * 64, head / p.share, t0, bar);
+      if (OUT) tma_load_3d(base + L::kQK + L::kV + i * kPanel, &maps.q, i * 64, head / p.share, t0, bar);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) tma_load_3d(base + L::kQK + i * kPanel, &maps.v, (int)tile * kTile + i * 64, head, t0, bar);
+  };
+  // The last chunk of a sequence: all threads; the rows of the next sequence, and those behind the last, as 0.
+  auto load_part = [&](int c) {
+    const uint32_t base = smem + (c % kStages) * L::kStage;
+    const int t0 = first + c * kChunk;
     constexpr int kUnits = DK / 8;
 #pragma unroll
     for (int u = tid; u < kChunk * kUnits; u += kThreads) {
-      const int r = u / kUnits, c = u % kUnits;
-      const bool there = t0 + r < end && c * 8 < p.dk;
-      const uint32_t at = (c / 8) * kPanel + r * 128 + (((c % 8) ^ (r & 7)) << 4);
+      const int r = u / kUnits, cc = u % kUnits;
+      const bool there = t0 + r < end && cc * 8 < p.dk;
+      const uint32_t at = (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4);
       const int64_t t = there ? t0 + r : 0;
-      const int off = there ? c * 8 : 0;
+      const int off = there ? cc * 8 : 0;
       copy16(base + at, k + t * p.k_stride + off, there);
       if (OUT) copy16(base + L::kQK + L::kV + at, q + t * p.q_stride + off, there);
     }
 #pragma unroll
     for (int u = tid; u < kChunk * 16; u += kThreads) {
-      const int r = u / 16, c = u % 16;
-      const bool there = t0 + r < end && (int)tile * kTile + c * 8 < p.dv;
-      const uint32_t at = (c / 8) * kPanel + r * 128 + (((c % 8) ^ (r & 7)) << 4);
-      copy16(base + L::kQK + at, v + (there ? (t0 + r) * p.v_stride + c * 8 : 0), there);
+      const int r = u / 16, cc = u % 16;
+      const bool there = t0 + r < end && (int)tile * kTile + cc * 8 < p.dv;
+      const uint32_t at = (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4);
+      copy16(base + L::kQK + at, v + (there ? (t0 + r) * p.v_stride + cc * 8 : 0), there);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto load_decay = [&](int t0, float& g0, float& g1) {
-    const int t = t0 + 2 * lane;
+  auto load = [&](int c) {                                     // (called by all threads, its stage free)
+    if (c < whole) {
+      if (warp == kLoadWarp && elect_one()) load_whole(c);
+    } else if (c < chunks) {
+      load_part(c);
+    }
+  };
+  auto load_decay = [&](int c, float& g0, float& g1) {
+    const int t = first + c * kChunk + 2 * lane;
     g0 = t < end ? p.decay[(int64_t)t * p.decay_stride + head] : 0.0f;
     g1 = t + 1 < end ? p.decay[(int64_t)(t + 1) * p.decay_stride + head] : 0.0f;
   };
 
-  if (first < end) load(0, first);
   double all_decay = 0.0;
-  if (warp == kDecayWarp && first < end) {
+  if (warp == kDecayWarp && chunks > 0) {
     float g0, g1;
-    load_decay(first, g0, g1);
+    load_decay(0, g0, g1);
     all_decay = chunk_decays(g0, g1, p.scale, decays[0]);
   }
   // the starting state
@@ -365,66 +418,98 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
       S[j] = from && d < p.dk ? from[(int64_t)d * p.dv + col] : 0.0f;
     }
   }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_at, lanes = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes
+  load(0);
+  load(1);
 
   T* o = static_cast<T*>(p.o) + (int64_t)head * p.dv + col;
-  uint32_t tmem = 0, lanes = 0;
-  const int chunks = (end - first + kChunk - 1) / kChunk;
-  for (int c = 0; c < chunks; ++c) {
-    const int stage = c & 1, t0 = first + c * kChunk;
+  // element e of row t of panels at `at`
+  auto element = [&](uint32_t at, int t, int e) {
+    return K::low(ld_shared_u16(at + (e >> 6) * kPanel + t * 128 + ((((uint32_t)(e & 63) >> 3) ^ (t & 7)) << 4) + (e & 7) * 2));
+  };
+  float prev_s = 1.0f, prev_p = 1.0f;                          // the scales of S and P of the chunk whose o comes next
+  // o of chunk c, whose products are done; staged: through shared memory
+  auto finish = [&](int c, bool staged) {
+    const Decays& d = decays[c % 3];
+    const int t0 = first + c * kChunk;
+    const float is = 1.0f / prev_s, ip = 1.0f / prev_p;
+    uint32_t inter[kTokens], intra[kTokens];
+    tmem_ld(tmem + lanes + L::kInter + (c & 1) * 64 + quarter * kTokens, inter);
+    tmem_ld(tmem + lanes + L::kIntra + quarter * kTokens, intra);
+    tmem_ld_done(inter);
+    tmem_ld_done(intra);
+    if (*(volatile uint32_t*)&odd_values[c % 3]) {             // from the terms j <= i alone
+      const uint32_t vt = smem + (c % kStages) * L::kStage + L::kQK;
+#pragma unroll 1
+      for (int i = 0; i < kTokens; ++i) {
+        const int ti = quarter * kTokens + i;
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int j = 0; j <= ti; ++j) sum = fmaf(element(smem + L::kPAt, ti, j), element(vt, j, row), sum);
+#pragma unroll
+        for (int u = 0; u < kTokens; ++u)
+          if (u == i) intra[u] = __float_as_uint(sum);
+      }
+    }
+    T* at = o + (int64_t)(t0 + quarter * kTokens) * p.o_stride;
+    const uint32_t to = smem + L::kOAt + quarter * kTokens * (kTile * 2) + row * 2;
+    const int n = live ? end - (t0 + quarter * kTokens) : 0;
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+      const T y = from_float<T>(fmaf(d.from_start[quarter * kTokens + i] * is, __uint_as_float(inter[i]), __uint_as_float(intra[i]) * ip));
+      if (staged)
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + i * kTile * 2), "h"(*reinterpret_cast<const unsigned short*>(&y)) : "memory");
+      else if (i < n)
+        at[(int64_t)i * p.o_stride] = y;
+    }
+  };
+  // what chunk c added, once its products are done
+  auto add = [&](int c, float scale_k) {
+    const Decays& d = decays[c % 3];
+    uint32_t added[kMine];
+    tmem_ld(tmem + lanes + L::kAdded + (OUT ? 0 : (c & 1) * DK) + quarter * kMine, added);
+    tmem_ld_done(added);
+    if (*(volatile uint32_t*)&odd_values[c % 3]) {             // from the products in fp32
+      const uint32_t base = smem + (c % kStages) * L::kStage;
+      const int n = min(kChunk, end - (first + c * kChunk));
+#pragma unroll 1
+      for (int i = 0; i < kMine; ++i) {
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int t = 0; t < n; ++t) sum = fmaf(element(base, t, quarter * kMine + i) * d.to_end[t], element(base + L::kQK, t, row), sum);
+#pragma unroll
+        for (int u = 0; u < kMine; ++u)
+          if (u == i) added[u] = __float_as_uint(sum * scale_k);
+      }
+    }
+    const float ik = 1.0f / scale_k;
+    const float2 total = d.total;
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) S[j] = carry(S[j], total, __uint_as_float(added[j]) * ik);
+  };
+
+  bool failed = false;
+  float prev_k = 1.0f;
+  int c = 0;
+  for (; c < chunks; ++c) {
+    const int stage = c % kStages;
     const uint32_t base = smem + stage * L::kStage;
     const uint32_t kt = base, vt = base + L::kQK, qt = base + L::kQK + L::kV;
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    fence_proxy_async_smem();
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    if (c == 0) {
-      tmem = tmem_base_at;
-      lanes = (uint32_t)(warp & 3) << 21;                      // this warp's 32 lanes
-    }
-    if (*(volatile uint32_t*)&abort_flag) break;
-    if (c + 1 < chunks) load(stage ^ 1, t0 + kChunk);
+    const Decays& d = decays[c % 3];
     float g0 = 0.0f, g1 = 0.0f;
-    if (warp == kDecayWarp && c + 1 < chunks) load_decay(t0 + kChunk, g0, g1);
-    const Decays& d = decays[stage];
-
-    // q . k: the 16 x 8 blocks that reach below the diagonal, two in each of the first ten warps: eight of the last row of blocks,
-    // six of the one before, four, two
-    float P[2][4];
-    const int rb = warp < 4 ? 3 : warp < 7 ? 2 : warp < 9 ? 1 : 0;
-    const int nt0 = 2 * (warp < 4 ? warp : warp < 7 ? warp - 4 : warp < 9 ? warp - 7 : 0);
-    const bool makes_p = OUT && warp < 10;
-    if (makes_p) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) P[n][i] = 0.0f;
-#pragma unroll
-      for (int ks = 0; ks < DK / 16; ks += 2) {                // 32 elements of dk
-        uint32_t a[2][4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int r = rb * 16 + (lane & 15), cc = (ks + i) * 2 + (lane >> 4);
-          ldmatrix_x4(qt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), a[i]);
-        }
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const int r = (nt0 + n) * 8 + (lane & 7), cc = ks * 2 + (lane >> 3);
-          uint32_t b[4];
-          ldmatrix_x4(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), b);
-          K::mma(P[n], a[0], b[0], b[1]);
-          K::mma(P[n], a[1], b[2], b[3]);
-        }
-      }
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int ti = rb * 16 + (lane >> 2) + 8 * (i >> 1), tj = (nt0 + n) * 8 + 2 * (lane & 3) + (i & 1);
-          const float power = (d.whole[ti] - d.whole[tj]) + (d.part[ti] - d.part[tj]);
-          P[n][i] = tj <= ti ? P[n][i] * (exp2_fast(power) * p.scale) : 0.0f;
-        }
+    if (warp == kDecayWarp && c + 1 < chunks) load_decay(c + 1, g0, g1);
+    if (c < whole) {
+      failed = !mbar_wait(loaded + stage * 8, (uint32_t)(c / kStages) & 1, &abort_flag, p.status) || failed;
+    } else {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      fence_proxy_async_smem();
+      __syncthreads();
     }
+
+    // k weighted and in pieces, the copy of S
     constexpr int kUnits = DK / 8, kVectors = kChunk * kUnits / kThreads;
     uint4 kk[kVectors];
     uint32_t odd = 0;                                          // bits 15 and 31: an infinity or NaN
@@ -441,8 +526,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
       const uint4 vv = ld_shared16(vt + (tid + m * kThreads) * 16);
       look(vv.x); look(vv.y); look(vv.z); look(vv.w);
     }
-    if (odd & 0x80008000u) odd_values[stage] = 1;
-    float scale_k = 1.0f, scale_p = 1.0f, scale_s = 1.0f;
+    if (odd & 0x80008000u) odd_values[c % 3] = 1;
+    float scale_k = 1.0f, scale_s = 1.0f;
     if (K::kScaled) {
       uint32_t top = 0;
 #pragma unroll
@@ -459,35 +544,16 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
             if ((w & 0x7c000000u) != 0x7c000000u) top = __vmaxu2(top, w & 0x7fff0000u);
           }
       }
-      raise_max(&largest[stage][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
+      raise_max(&largest[c & 1][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
       if (OUT) {
-        uint32_t pm = 0, sm = 0;
-        if (makes_p) {
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pm = max(pm, finite_bits(P[n][i]));
-          raise_max(&largest[stage][1], pm);
-        }
+        uint32_t sm = 0;
 #pragma unroll
         for (int j = 0; j < kMine; ++j) sm = max(sm, finite_bits(S[j]));
-        raise_max(&largest[stage][2], sm);
+        raise_max(&largest[c & 1][2], sm);
       }
       __syncthreads();
-      scale_k = scale_for(largest[stage][0]);
-      if (OUT) {
-        scale_p = scale_for(largest[stage][1]);
-        scale_s = scale_for(largest[stage][2]);
-      }
-    }
-    if (makes_p) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int ti = rb * 16 + (lane >> 2) + 8 * i, cc = nt0 + n;
-          st_shared4(smem + L::kPAt + ti * 128 + ((cc ^ (ti & 7)) << 4) + (lane & 3) * 4, K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
-        }
+      scale_k = scale_for(largest[c & 1][0]);
+      if (OUT) scale_s = scale_for(largest[c & 1][2]);
     }
     if (OUT) {
       uint32_t r[kMine / 2];
@@ -495,6 +561,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
       for (int i = 0; i < kMine / 2; ++i) r[i] = K::pack(S[2 * i] * scale_s, S[2 * i + 1] * scale_s);
       tmem_st(tmem + lanes + L::kS + quarter * (kMine / 2), r);
     }
+    const uint32_t pieces = smem + L::kPiecesAt + (OUT ? 0 : (c & 1) * L::kPieces);
 #pragma unroll
     for (int m = 0; m < kVectors; ++m) {
       const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
@@ -510,97 +577,154 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
       }
       const uint32_t at = (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4);
 #pragma unroll
-      for (int n = 0; n < K::kPieces; ++n) st_shared16(smem + L::kPiecesAt + n * L::kQK + at, out[n][0], out[n][1], out[n][2], out[n][3]);
+      for (int n = 0; n < K::kPieces; ++n) st_shared16(pieces + n * L::kQK + at, out[n][0], out[n][1], out[n][2], out[n][3]);
     }
     if (OUT) tmem_st_wait();
+    if (OUT && warp == kLoadWarp) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // (its last store of o has been read)
     fence_proxy_async_smem();
     tc_fence_before();
-    __syncthreads();
-    if (warp == 0 && elect_one()) {
+    failed = __syncthreads_or(failed);
+    if (failed) break;
+
+    if (warp == kMmaWarp && elect_one()) {
       tc_fence_after();
       constexpr uint32_t kBase = K::kFormats;
       if (OUT) {
 #pragma unroll
         for (int ks = 0; ks < DK / 16; ++ks)
-          umma_f16_ta(tmem + L::kInter, tmem + L::kS + ks * 8, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), kDescHi,
+          umma_f16_ta(tmem + L::kInter + (c & 1) * 64, tmem + L::kS + ks * 8, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), kDescHi,
                       kBase | instr_desc_f16(128, 64), ks > 0);
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          umma_f16_ab(tmem + L::kIntra, desc_lo_mn(vt + ks * 2048), kDescHi, smem_desc_lo(smem + L::kPAt + ks * 32), kDescHi,
-                      kBase | kAlongM | instr_desc_f16(128, 64), ks > 0);
       }
 #pragma unroll
       for (int n = K::kPieces - 1; n >= 0; --n)                // the smallest pieces first
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
-          umma_f16_ab(tmem + L::kAdded, desc_lo_mn(vt + ks * 2048), kDescHi, desc_lo_mn(smem + L::kPiecesAt + n * L::kQK + ks * 2048), kDescHi,
-                      kBase | kAlongM | kAlongN | instr_desc_f16(128, DK), n < K::kPieces - 1 || ks > 0);
-      umma_commit(bar);
+          umma_f16_ab(tmem + L::kAdded + (OUT ? 0 : (c & 1) * DK), desc_lo_mn(vt + ks * 2048), kDescHi, desc_lo_mn(pieces + n * L::kQK + ks * 2048),
+                      kDescHi, kBase | kAlongM | kAlongN | instr_desc_f16(128, DK), n < K::kPieces - 1 || ks > 0);
+      umma_commit(done + (OUT ? 0 : (c & 1) * 8));
     }
+    if (warp == kDecayWarp && c + 1 < chunks) all_decay += chunk_decays(g0, g1, p.scale, decays[(c + 1) % 3]);
     if (tid == 32) {
-      odd_values[stage ^ 1] = 0;
+      odd_values[(c + 1) % 3] = 0;
       if (K::kScaled)
-        for (int i = 0; i < 3; ++i) largest[stage ^ 1][i] = 0;
+        for (int i = 0; i < 3; ++i) largest[(c + 1) & 1][i] = 0;
     }
-    if (warp == kDecayWarp && c + 1 < chunks) all_decay += chunk_decays(g0, g1, p.scale, decays[stage ^ 1]);
-    mbar_wait(bar, (uint32_t)(c & 1), &abort_flag, p.status);
-    tc_fence_after();
 
-    // (every thread sees the same: written before the barrier)
-    const bool again = *(volatile uint32_t*)&odd_values[stage] != 0;
-    // element e of row t of a panel pair at `at`
-    auto element = [&](uint32_t at, int t, int e) {
-      return K::low(ld_shared_u16(at + (e >> 6) * kPanel + t * 128 + ((((uint32_t)(e & 63) >> 3) ^ (t & 7)) << 4) + (e & 7) * 2));
-    };
-    uint32_t added[kMine];
-    tmem_ld(tmem + lanes + L::kAdded + quarter * kMine, added);
     if (OUT) {
-      const float is = 1.0f / scale_s, ip = 1.0f / scale_p;
-      uint32_t inter[kTokens], intra[kTokens];
-      tmem_ld(tmem + lanes + L::kInter + quarter * kTokens, inter);
-      tmem_ld(tmem + lanes + L::kIntra + quarter * kTokens, intra);
-      tmem_ld_done(inter);
-      tmem_ld_done(intra);
-      if (again) {                                             // from the terms j <= i alone
-#pragma unroll 1
-        for (int i = 0; i < kTokens; ++i) {
-          const int ti = quarter * kTokens + i;
-          float sum = 0.0f;
-#pragma unroll 1
-          for (int j = 0; j <= ti; ++j) sum = fmaf(element(smem + L::kPAt, ti, j), element(vt, j, row), sum);
+      // o of the chunk before, then P
+      if (c > 0) {
+        failed = !mbar_wait(intra_done, (uint32_t)(c - 1) & 1, &abort_flag, p.status) || failed;
+        tc_fence_after();
+        finish(c - 1, p.o_by_map != 0);
+        if (*(volatile uint32_t*)&odd_values[(c - 1) % 3]) __syncthreads();    // (P has been read)
+      }
+      // q . k: the 16 x 8 blocks that reach below the diagonal, two in each of the first ten warps: eight of the last row of blocks,
+      // six of the one before, four, two
+      float P[2][4];
+      const int rb = warp < 4 ? 3 : warp < 7 ? 2 : warp < 9 ? 1 : 0;
+      const int nt0 = 2 * (warp < 4 ? warp : warp < 7 ? warp - 4 : warp < 9 ? warp - 7 : 0);
+      const bool makes_p = warp < 10;
+      float scale_p = 1.0f;
+      if (makes_p) {
+        float P2[2][4];                                        // (two chains of additions)
 #pragma unroll
-          for (int u = 0; u < kTokens; ++u)
-            if (u == i) intra[u] = __float_as_uint(sum);
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) P[n][i] = P2[n][i] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < DK / 16; ks += 2) {              // 32 elements of dk
+          uint32_t a[2][4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int r = rb * 16 + (lane & 15), cc = (ks + i) * 2 + (lane >> 4);
+            ldmatrix_x4(qt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), a[i]);
+          }
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const int r = (nt0 + n) * 8 + (lane & 7), cc = ks * 2 + (lane >> 3);
+            uint32_t b[4];
+            ldmatrix_x4(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), b);
+            K::mma(P[n], a[0], b[0], b[1]);
+            K::mma(P2[n], a[1], b[2], b[3]);
+          }
         }
-      }
-      T* at = o + (int64_t)(t0 + quarter * kTokens) * p.o_stride;
-      const int n = live ? end - (t0 + quarter * kTokens) : 0;
 #pragma unroll
-      for (int i = 0; i < kTokens; ++i) {
-        const float y = fmaf(d.from_start[quarter * kTokens + i] * is, __uint_as_float(inter[i]), __uint_as_float(intra[i]) * ip);
-        if (i < n) at[(int64_t)i * p.o_stride] = from_float<T>(y);
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int ti = rb * 16 + (lane >> 2) + 8 * (i >> 1), tj = (nt0 + n) * 8 + 2 * (lane & 3) + (i & 1);
+            const float power = (d.whole[ti] - d.whole[tj]) + (d.part[ti] - d.part[tj]);
+            P[n][i] = tj <= ti ? (P[n][i] + P2[n][i]) * (exp2_fast(power) * p.scale) : 0.0f;
+          }
       }
+      if (K::kScaled) {
+        if (makes_p) {
+          uint32_t pm = 0;
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pm = max(pm, finite_bits(P[n][i]));
+          raise_max(&largest[c & 1][1], pm);
+        }
+        __syncthreads();
+        scale_p = scale_for(largest[c & 1][1]);
+      }
+      if (makes_p) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int ti = rb * 16 + (lane >> 2) + 8 * i, cc = nt0 + n;
+            st_shared4(smem + L::kPAt + ti * 128 + ((cc ^ (ti & 7)) << 4) + (lane & 3) * 4, K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
+          }
+      }
+      fence_proxy_async_smem();
+      tc_fence_before();
+      __syncthreads();
+      if (warp == kMmaWarp && elect_one()) {
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          umma_f16_ab(tmem + L::kIntra, desc_lo_mn(vt + ks * 2048), kDescHi, smem_desc_lo(smem + L::kPAt + ks * 32), kDescHi,
+                      K::kFormats | kAlongM | instr_desc_f16(128, 64), ks > 0);
+        umma_commit(intra_done);
+      }
+      if (c > 0 && p.o_by_map && warp == kLoadWarp && elect_one())
+        tma_store_3d(&maps.o, smem + L::kOAt, (int)tile * kTile, head, first + (c - 1) * kChunk);
+      load(c + 2);                                             // (into the stage of the chunk before)
+      failed = !mbar_wait(done, (uint32_t)c & 1, &abort_flag, p.status) || failed;
+      tc_fence_after();
+      add(c, scale_k);
+      prev_s = scale_s;
+      prev_p = scale_p;
+    } else {
+      if (c > 0) {
+        failed = !mbar_wait(done + ((c - 1) & 1) * 8, (uint32_t)((c - 1) >> 1) & 1, &abort_flag, p.status) || failed;
+        tc_fence_after();
+        add(c - 1, prev_k);
+        if (*(volatile uint32_t*)&odd_values[(c - 1) % 3]) __syncthreads();    // (k and v have been read)
+      }
+      load(c + 2);
+      prev_k = scale_k;
     }
-    tmem_ld_done(added);
-    if (again) {                                               // from the products in fp32
-#pragma unroll 1
-      for (int i = 0; i < kMine; ++i) {
-        float sum = 0.0f;
-#pragma unroll 1
-        for (int t = 0; t < kChunk && t0 + t < end; ++t)
-          sum = fmaf(element(kt, t, quarter * kMine + i) * d.to_end[t], element(vt, t, row), sum);
-#pragma unroll
-        for (int u = 0; u < kMine; ++u)
-          if (u == i) added[u] = __float_as_uint(sum * scale_k);
-      }
+  }
+  if (failed) {                                                // (its loads under way end before the block does)
+    for (int i = c; i < c + 2 && i < whole; ++i) mbar_wait(loaded + (i % kStages) * 8, (uint32_t)(i / kStages) & 1, &abort_flag, p.status);
+  } else if (chunks > 0) {
+    const int z = chunks - 1;
+    if (OUT) {
+      mbar_wait(intra_done, (uint32_t)z & 1, &abort_flag, p.status);
+      tc_fence_after();
+      finish(z, false);
+    } else {
+      mbar_wait(done + (z & 1) * 8, (uint32_t)(z >> 1) & 1, &abort_flag, p.status);
+      tc_fence_after();
+      add(z, prev_k);
     }
-    const float ik = 1.0f / scale_k;
-    const float2 total = d.total;
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) S[j] = carry(S[j], total, __uint_as_float(added[j]) * ik);
   }
 
   asm volatile("cp.async.wait_group 0;" ::: "memory");
+  if (OUT && warp == kLoadWarp) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   float* to = nullptr;
   if (!OUT)
     to = p.added + ((int64_t)id * p.heads + head) * state_size;
@@ -613,11 +737,14 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const ChunkParams p)
       if (e < p.dk) to[(int64_t)e * p.dv + col] = S[j];
     }
   }
-  if (!OUT && warp == kDecayWarp && lane == 0 && tile == 0) p.totals[(int64_t)id * p.heads + head] = two_parts(all_decay);
+  if (!OUT && warp == kDecayWarp && tile == 0) {
+    const float2 total = two_parts(all_decay);
+    if (lane == 0) p.totals[(int64_t)id * p.heads + head] = total;
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 0) tmem_dealloc(tmem_base_at, L::kColumns);
+  if (warp == 0) tmem_dealloc(tmem, L::kColumns);
 }
 
 // The starting state of every segment, in the place of what it adds: a thread has a number of a head's state and runs over the
@@ -694,8 +821,31 @@ ChunkPlan plan_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool 
   return c;
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+EncodeTiledFn get_encode_fn() {
+  static EncodeTiledFn fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(f);
+  }();
+  return fn;
+}
+
+bool encode(EncodeTiledFn fn, CUtensorMap* map, im2win_dtype dtype, const void* at, int64_t tokens, int64_t heads, int64_t size, int64_t stride,
+            uint32_t box_elements, CUtensorMapSwizzle swizzle) {
+  const cuuint64_t dims[3] = {(cuuint64_t)size, (cuuint64_t)heads, (cuuint64_t)tokens};
+  const cuuint64_t strides[2] = {(cuuint64_t)size * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {box_elements, 1, kChunk}, one[3] = {1, 1, 1};
+  return fn(map, dtype == IM2WIN_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(at), dims, strides,
+            box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int DK, bool OUT>
-cudaError_t launch(const ChunkParams& p, int64_t pieces, cudaStream_t stream) {
+cudaError_t launch(const ChunkMaps& maps, const ChunkParams& p, int64_t pieces, cudaStream_t stream) {
   constexpr uint32_t kBytes = Layout<T, DK, OUT>::kBytes;
   static bool attr_done[64] = {};
   int dev = 0;
@@ -707,17 +857,17 @@ cudaError_t launch(const ChunkParams& p, int64_t pieces, cudaStream_t stream) {
   }
   const int64_t grid = pieces * p.heads * p.tiles;
   if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
-  chunk_kernel<T, DK, OUT><<<(unsigned)grid, kThreads, kBytes, stream>>>(p);
+  chunk_kernel<T, DK, OUT><<<(unsigned)grid, kThreads, kBytes, stream>>>(maps, p);
   return cudaGetLastError();
 }
 
 template <typename T, int DK>
-cudaError_t launch_all(ChunkParams& p, const ChunkPlan& plan, const AttentionArgs& a, cudaStream_t stream) {
+cudaError_t launch_all(const ChunkMaps& maps, ChunkParams& p, const ChunkPlan& plan, const AttentionArgs& a, cudaStream_t stream) {
   if (cudaMemsetAsync(p.status, 0, kStatusBytes, stream) != cudaSuccess) return cudaErrorUnknown;
   int64_t pieces = number_of_pieces(a.shape.tokens, a.shape.sequences, p.L, a.seqs.cu != nullptr);
   if (plan.segments) {
     pieces = plan.segments;
-    cudaError_t e = launch<T, DK, false>(p, pieces, stream);
+    cudaError_t e = launch<T, DK, false>(maps, p, pieces, stream);
     if (e != cudaSuccess) return e;
     const int32_t blocks = (int32_t)(((int64_t)p.dk * p.dv + 255) / 256);
     const int64_t grid = (int64_t)blocks * p.heads * a.shape.sequences;
@@ -728,7 +878,7 @@ cudaError_t launch_all(ChunkParams& p, const ChunkPlan& plan, const AttentionArg
     p.state_in = p.added;
     p.segmented = 1;
   }
-  return launch<T, DK, true>(p, pieces, stream);
+  return launch<T, DK, true>(maps, p, pieces, stream);
 }
 
 }  // namespace
@@ -746,10 +896,20 @@ cudaError_t launch_attention_chunks(const AttentionArgs& a, cudaStream_t stream)
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   ChunkParams p = {a.q, a.k, a.v, a.decay, a.o, a.state_in, a.state_out, reinterpret_cast<float*>(ws + plan.added_off),
                    reinterpret_cast<float2*>(ws + plan.totals_off), reinterpret_cast<uint32_t*>(ws), a.seqs, s.q_stride, s.k_stride,
-                   s.v_stride, s.o_stride, s.decay_stride, s.heads, s.heads / s.qk_heads, s.dk, s.dv, plan.tiles, plan.L, 0, s.scale};
+                   s.v_stride, s.o_stride, s.decay_stride, s.heads, s.heads / s.qk_heads, s.dk, s.dv, plan.tiles, plan.L, 0, 0, s.scale};
+  const EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return cudaErrorNotSupported;
+  p.o_by_map = s.o_stride % 8 == 0 && aligned_to(a.o, 16);
+  ChunkMaps maps = {};
+  const CUtensorMapSwizzle rows = CU_TENSOR_MAP_SWIZZLE_128B;
+  if (!encode(fn, &maps.q, a.dtype, a.q, s.tokens, s.qk_heads, s.dk, s.q_stride, 64, rows) ||
+      !encode(fn, &maps.k, a.dtype, a.k, s.tokens, s.qk_heads, s.dk, s.k_stride, 64, rows) ||
+      !encode(fn, &maps.v, a.dtype, a.v, s.tokens, s.heads, s.dv, s.v_stride, 64, rows) ||
+      (p.o_by_map && !encode(fn, &maps.o, a.dtype, a.o, s.tokens, s.heads, s.dv, s.o_stride, kTile, CU_TENSOR_MAP_SWIZZLE_NONE)))
+    return cudaErrorInvalidValue;
   if (a.dtype == IM2WIN_F16)
-    return s.dk <= 64 ? launch_all<__half, 64>(p, plan, a, stream) : launch_all<__half, 128>(p, plan, a, stream);
-  return s.dk <= 64 ? launch_all<__nv_bfloat16, 64>(p, plan, a, stream) : launch_all<__nv_bfloat16, 128>(p, plan, a, stream);
+    return s.dk <= 64 ? launch_all<__half, 64>(maps, p, plan, a, stream) : launch_all<__half, 128>(maps, p, plan, a, stream);
+  return s.dk <= 64 ? launch_all<__nv_bfloat16, 64>(maps, p, plan, a, stream) : launch_all<__nv_bfloat16, 128>(maps, p, plan, a, stream);
 }
 
 }  // namespace im2win
