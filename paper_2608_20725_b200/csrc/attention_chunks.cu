@@ -85,11 +85,6 @@ template <> struct Kind<__nv_bfloat16> {
   }
   static __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
   static __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-  static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  }
   // Two numbers as pieces: the upper half, the upper half of the rest, the rest of that (exact: 24 bits).
   static __device__ __forceinline__ void split(float a, float b, uint32_t (&piece)[3]) {
     const float a1 = a - __uint_as_float(__float_as_uint(a) & 0xffff0000u), b1 = b - __uint_as_float(__float_as_uint(b) & 0xffff0000u);
@@ -111,11 +106,6 @@ template <> struct Kind<__half> {
   }
   static __device__ __forceinline__ float low(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xffffu))); }
   static __device__ __forceinline__ float high(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
-  static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  }
   // Two numbers as pieces: rounded, and the rest rounded (22 bits).
   static __device__ __forceinline__ void split(float a, float b, uint32_t (&piece)[2]) {
     piece[0] = pack(a, b);
@@ -126,12 +116,6 @@ template <> struct Kind<__half> {
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
 }
 __device__ __forceinline__ uint4 ld_shared16(uint32_t addr) {
   uint4 v;
@@ -256,19 +240,20 @@ __device__ __forceinline__ double chunk_decays(float g0, float g1, float scale, 
   return end;
 }
 
-// Shared memory: three stages of q, k and v, the pieces of the weighted k (two sets where o is not made), P, o on its way out.
+// Shared memory: three stages of k, v and q, the pieces of the weighted k (two sets where o is not made), P.
 template <typename T, int DK, bool OUT>
 struct Layout {
   static constexpr uint32_t kQK = DK / 64 * kPanel;            // q or k of a chunk
   static constexpr uint32_t kV = 2 * kPanel;
-  static constexpr uint32_t kStage = (OUT ? 2 : 1) * kQK + kV;
+  static constexpr uint32_t kO = kChunk * kTile * 2;           // o of a chunk on its way out, in the place of its q
+  static constexpr uint32_t kLoaded = (OUT ? 2 : 1) * kQK + kV;
+  static constexpr uint32_t kStage = kQK + kV + (OUT ? (kO > kQK ? kO : kQK) : 0);
   static constexpr uint32_t kPieces = Kind<T>::kPieces * kQK;
   static constexpr uint32_t kPiecesAt = kStages * kStage;
   static constexpr uint32_t kPAt = kPiecesAt + (OUT ? 1 : 2) * kPieces;
-  static constexpr uint32_t kOAt = kPAt + kPanel;
-  static constexpr uint32_t kBytes = (OUT ? kOAt + kChunk * kTile * 2 : kPAt) + 1024;
+  static constexpr uint32_t kBytes = kPAt + (OUT ? kPanel : 0) + 1024;
   // columns of tensor memory
-  static constexpr uint32_t kAdded = 0, kInter = DK, kIntra = DK + 128, kS = DK + 192;     // (o: two of inter; otherwise two of added)
+  static constexpr uint32_t kAdded = 0, kInter = DK, kIntra = DK + 64, kQK64 = DK + 128, kS = DK + 192;      // (where o is not made: two of added)
   static constexpr uint32_t kColumns = OUT ? 512 : 2 * DK;
 };
 
@@ -286,6 +271,13 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[N]) {
         : "r"(taddr)
         : "memory");
   }
+}
+// 16 lanes and 16 columns: r[4n + 2h + i] is row lane / 4 + 8h, column 8n + 2 (lane % 4) + i.
+__device__ __forceinline__ void tmem_ld_16x16(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
 }
 // The wait for a load into r[] (naming the registers keeps every use of them behind it).
 template <int N>
@@ -309,9 +301,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   constexpr int kMine = DK / kQuarters;                        // columns of S of a thread
   constexpr int kTokens = kChunk / kQuarters;                  // rows of o of a thread
   extern __shared__ uint8_t dynamic_smem[];
-  __shared__ Decays decays[3];
-  __shared__ __align__(8) uint64_t bars[kStages + 2];          // stages loaded; state products done (two), intra products done
-  __shared__ uint32_t tmem_base_at, abort_flag, odd_values[3], largest[2][3];
+  __shared__ Decays decays[4];
+  __shared__ __align__(8) uint64_t bars[kStages + 3];          // stages loaded; state products done (two), intra, q . k done
+  __shared__ uint32_t tmem_base_at, abort_flag, odd_values[4], largest[4][3];
   const uint32_t smem = (smem_u32(dynamic_smem) + 1023u) & ~1023u;
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
   const uint32_t tile = blockIdx.x % (uint32_t)p.tiles, rest = blockIdx.x / (uint32_t)p.tiles;
@@ -331,13 +323,14 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const int64_t state_size = (int64_t)p.dk * p.dv;
   const int chunks = (end - first + kChunk - 1) / kChunk, whole = (end - first) / kChunk;
 
-  const uint32_t loaded = smem_u32(bars), done = smem_u32(bars + kStages), intra_done = smem_u32(bars + kStages + 1);
+  const uint32_t loaded = smem_u32(bars), done = smem_u32(bars + kStages), intra_done = smem_u32(bars + kStages + 1),
+                 qk_done = smem_u32(bars + kStages + 2);
   if (warp == 0) tmem_alloc(smem_u32(&tmem_base_at), L::kColumns);
   if (tid == 0) {
-    for (int i = 0; i < kStages + 2; ++i) mbar_init(smem_u32(bars + i), 1);
+    for (int i = 0; i < kStages + 3; ++i) mbar_init(smem_u32(bars + i), 1);
     abort_flag = 0;
-    for (int i = 0; i < 6; ++i) largest[i / 3][i % 3] = 0;
-    for (int i = 0; i < 3; ++i) odd_values[i] = 0;
+    for (int i = 0; i < 12; ++i) largest[i / 3][i % 3] = 0;
+    for (int i = 0; i < 4; ++i) odd_values[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async_smem();
   }
@@ -350,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   auto load_whole = [&](int c) {
     const uint32_t base = smem + (c % kStages) * L::kStage, bar = loaded + (c % kStages) * 8;
     const int t0 = first + c * kChunk;
-    mbar_arrive_expect_tx(bar, L::kStage);
+    mbar_arrive_expect_tx(bar, L::kLoaded);
 #pragma unroll
     for (int i = 0; i < DK / 64; ++i) {
       tma_load_3d(base + i * kPanel, &maps.k, i * 64, head / p.share, t0, bar);
@@ -383,13 +376,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto load = [&](int c) {                                     // (called by all threads, its stage free)
-    if (c < whole) {
-      if (warp == kLoadWarp && elect_one()) load_whole(c);
-    } else if (c < chunks) {
-      load_part(c);
-    }
-  };
   auto load_decay = [&](int c, float& g0, float& g1) {
     const int t = first + c * kChunk + 2 * lane;
     g0 = t < end ? p.decay[(int64_t)t * p.decay_stride + head] : 0.0f;
@@ -398,9 +384,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
 
   double all_decay = 0.0;
   if (warp == kDecayWarp && chunks > 0) {
-    float g0, g1;
+    float g0, g1, h0, h1;
     load_decay(0, g0, g1);
+    load_decay(1, h0, h1);
     all_decay = chunk_decays(g0, g1, p.scale, decays[0]);
+    if (chunks > 1) all_decay += chunk_decays(h0, h1, p.scale, decays[1]);
   }
   // the starting state
   float S[kMine];
@@ -422,26 +410,28 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base_at, lanes = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes
-  load(0);
-  load(1);
+  if (warp == kLoadWarp && lane == 0) {
+    if (0 < whole) load_whole(0);
+    if (1 < whole) load_whole(1);
+  }
+  if (whole == 0 && chunks > 0) load_part(0);
 
   T* o = static_cast<T*>(p.o) + (int64_t)head * p.dv + col;
   // element e of row t of panels at `at`
   auto element = [&](uint32_t at, int t, int e) {
     return K::low(ld_shared_u16(at + (e >> 6) * kPanel + t * 128 + ((((uint32_t)(e & 63) >> 3) ^ (t & 7)) << 4) + (e & 7) * 2));
   };
-  float prev_s = 1.0f, prev_p = 1.0f;                          // the scales of S and P of the chunk whose o comes next
   // o of chunk c, whose products are done; staged: through shared memory
-  auto finish = [&](int c, bool staged) {
-    const Decays& d = decays[c % 3];
+  auto finish = [&](int c, float scale_s, float scale_p, bool staged) {
+    const Decays& d = decays[c & 3];
     const int t0 = first + c * kChunk;
-    const float is = 1.0f / prev_s, ip = 1.0f / prev_p;
+    const float is = 1.0f / scale_s, ip = 1.0f / scale_p;
     uint32_t inter[kTokens], intra[kTokens];
-    tmem_ld(tmem + lanes + L::kInter + (c & 1) * 64 + quarter * kTokens, inter);
+    tmem_ld(tmem + lanes + L::kInter + quarter * kTokens, inter);
     tmem_ld(tmem + lanes + L::kIntra + quarter * kTokens, intra);
     tmem_ld_done(inter);
     tmem_ld_done(intra);
-    if (*(volatile uint32_t*)&odd_values[c % 3]) {             // from the terms j <= i alone
+    if (*(volatile uint32_t*)&odd_values[c & 3]) {             // from the terms j <= i alone
       const uint32_t vt = smem + (c % kStages) * L::kStage + L::kQK;
 #pragma unroll 1
       for (int i = 0; i < kTokens; ++i) {
@@ -454,25 +444,31 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
           if (u == i) intra[u] = __float_as_uint(sum);
       }
     }
-    T* at = o + (int64_t)(t0 + quarter * kTokens) * p.o_stride;
-    const uint32_t to = smem + L::kOAt + quarter * kTokens * (kTile * 2) + row * 2;
-    const int n = live ? end - (t0 + quarter * kTokens) : 0;
+    unsigned short y[kTokens];
 #pragma unroll
     for (int i = 0; i < kTokens; ++i) {
-      const T y = from_float<T>(fmaf(d.from_start[quarter * kTokens + i] * is, __uint_as_float(inter[i]), __uint_as_float(intra[i]) * ip));
-      if (staged)
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + i * kTile * 2), "h"(*reinterpret_cast<const unsigned short*>(&y)) : "memory");
-      else if (i < n)
-        at[(int64_t)i * p.o_stride] = y;
+      const T t = from_float<T>(fmaf(d.from_start[quarter * kTokens + i] * is, __uint_as_float(inter[i]), __uint_as_float(intra[i]) * ip));
+      y[i] = *reinterpret_cast<const unsigned short*>(&t);
+    }
+    if (staged) {
+      const uint32_t to = smem + (c % kStages) * L::kStage + L::kQK + L::kV + quarter * kTokens * (kTile * 2) + row * 2;
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i) asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + i * kTile * 2), "h"(y[i]) : "memory");
+    } else {
+      unsigned short* at = reinterpret_cast<unsigned short*>(o) + (int64_t)(t0 + quarter * kTokens) * p.o_stride;
+      const int n = live ? end - (t0 + quarter * kTokens) : 0;
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i)
+        if (i < n) at[(int64_t)i * p.o_stride] = y[i];
     }
   };
   // what chunk c added, once its products are done
   auto add = [&](int c, float scale_k) {
-    const Decays& d = decays[c % 3];
+    const Decays& d = decays[c & 3];
     uint32_t added[kMine];
     tmem_ld(tmem + lanes + L::kAdded + (OUT ? 0 : (c & 1) * DK) + quarter * kMine, added);
     tmem_ld_done(added);
-    if (*(volatile uint32_t*)&odd_values[c % 3]) {             // from the products in fp32
+    if (*(volatile uint32_t*)&odd_values[c & 3]) {             // from the products in fp32
       const uint32_t base = smem + (c % kStages) * L::kStage;
       const int n = min(kChunk, end - (first + c * kChunk));
 #pragma unroll 1
@@ -491,25 +487,43 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     for (int j = 0; j < kMine; ++j) S[j] = carry(S[j], total, __uint_as_float(added[j]) * ik);
   };
 
+  // q . k of chunk c: one thread
+  auto issue_qk = [&](int c) {
+    const uint32_t kt = smem + (c % kStages) * L::kStage, qt = kt + L::kQK + L::kV;
+#pragma unroll
+    for (int ks = 0; ks < DK / 16; ++ks)
+      umma_f16_lohi(tmem + L::kQK64, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), smem_desc_lo(kt + (ks / 4) * kPanel + (ks % 4) * 32),
+                    K::kFormats | instr_desc_f16(64, 64), ks > 0);
+    umma_commit(qk_done);
+  };
+
   bool failed = false;
   float prev_k = 1.0f;
+  if (OUT && whole > 0 && warp == kMmaWarp) {
+    failed = !mbar_wait(loaded, 0, &abort_flag, p.status);
+    if (elect_one()) issue_qk(0);
+  }
   int c = 0;
   for (; c < chunks; ++c) {
     const int stage = c % kStages;
     const uint32_t base = smem + stage * L::kStage;
     const uint32_t kt = base, vt = base + L::kQK, qt = base + L::kQK + L::kV;
-    const Decays& d = decays[c % 3];
+    const Decays& d = decays[c & 3];
     float g0 = 0.0f, g1 = 0.0f;
-    if (warp == kDecayWarp && c + 1 < chunks) load_decay(c + 1, g0, g1);
+    if (warp == kDecayWarp && c + 2 < chunks) load_decay(c + 2, g0, g1);
     if (c < whole) {
       failed = !mbar_wait(loaded + stage * 8, (uint32_t)(c / kStages) & 1, &abort_flag, p.status) || failed;
     } else {
       asm volatile("cp.async.wait_group 0;" ::: "memory");
       fence_proxy_async_smem();
       __syncthreads();
+      if (OUT && warp == kMmaWarp && elect_one()) {
+        tc_fence_after();
+        issue_qk(c);
+      }
     }
 
-    // k weighted and in pieces, the copy of S
+    // k weighted and in pieces, the copy of S, P
     constexpr int kUnits = DK / 8, kVectors = kChunk * kUnits / kThreads;
     uint4 kk[kVectors];
     uint32_t odd = 0;                                          // bits 15 and 31: an infinity or NaN
@@ -526,8 +540,29 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       const uint4 vv = ld_shared16(vt + (tid + m * kThreads) * 16);
       look(vv.x); look(vv.y); look(vv.z); look(vv.w);
     }
-    if (odd & 0x80008000u) odd_values[c % 3] = 1;
-    float scale_k = 1.0f, scale_s = 1.0f;
+    if (odd & 0x80008000u) odd_values[c & 3] = 1;
+    // P: the 16 x 16 blocks that reach below the diagonal, one to a warp: rows 16 rb, columns 16 quarter
+    float P[2][4];
+    const int rb = warp & 3;
+    const bool makes_p = OUT && quarter <= rb;
+    if (OUT) {
+      failed = !mbar_wait(qk_done, (uint32_t)c & 1, &abort_flag, p.status) || failed;
+      tc_fence_after();
+    }
+    if (makes_p) {
+      uint32_t dots[8];
+      tmem_ld_16x16(tmem + lanes + L::kQK64 + quarter * 16, dots);
+      tmem_ld_done(dots);
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int ti = rb * 16 + (lane >> 2) + 8 * (i >> 1), tj = quarter * 16 + n * 8 + 2 * (lane & 3) + (i & 1);
+          const float power = (d.whole[ti] - d.whole[tj]) + (d.part[ti] - d.part[tj]);
+          P[n][i] = tj <= ti ? __uint_as_float(dots[4 * n + i]) * (exp2_fast(power) * p.scale) : 0.0f;
+        }
+    }
+    float scale_k = 1.0f, scale_s = 1.0f, scale_p = 1.0f;
     if (K::kScaled) {
       uint32_t top = 0;
 #pragma unroll
@@ -544,22 +579,42 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
             if ((w & 0x7c000000u) != 0x7c000000u) top = __vmaxu2(top, w & 0x7fff0000u);
           }
       }
-      raise_max(&largest[c & 1][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
+      raise_max(&largest[c & 3][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
       if (OUT) {
         uint32_t sm = 0;
 #pragma unroll
         for (int j = 0; j < kMine; ++j) sm = max(sm, finite_bits(S[j]));
-        raise_max(&largest[c & 1][2], sm);
+        raise_max(&largest[c & 3][2], sm);
+        if (makes_p) {
+          uint32_t pm = 0;
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pm = max(pm, finite_bits(P[n][i]));
+          raise_max(&largest[c & 3][1], pm);
+        }
       }
       __syncthreads();
-      scale_k = scale_for(largest[c & 1][0]);
-      if (OUT) scale_s = scale_for(largest[c & 1][2]);
+      scale_k = scale_for(largest[c & 3][0]);
+      if (OUT) {
+        scale_p = scale_for(largest[c & 3][1]);
+        scale_s = scale_for(largest[c & 3][2]);
+      }
     }
     if (OUT) {
       uint32_t r[kMine / 2];
 #pragma unroll
       for (int i = 0; i < kMine / 2; ++i) r[i] = K::pack(S[2 * i] * scale_s, S[2 * i + 1] * scale_s);
       tmem_st(tmem + lanes + L::kS + quarter * (kMine / 2), r);
+    }
+    if (makes_p) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int ti = rb * 16 + (lane >> 2) + 8 * i, cc = quarter * 2 + n;
+          st_shared4(smem + L::kPAt + ti * 128 + ((cc ^ (ti & 7)) << 4) + (lane & 3) * 4, K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
+        }
     }
     const uint32_t pieces = smem + L::kPiecesAt + (OUT ? 0 : (c & 1) * L::kPieces);
 #pragma unroll
@@ -580,7 +635,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       for (int n = 0; n < K::kPieces; ++n) st_shared16(pieces + n * L::kQK + at, out[n][0], out[n][1], out[n][2], out[n][3]);
     }
     if (OUT) tmem_st_wait();
-    if (OUT && warp == kLoadWarp) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // (its last store of o has been read)
     fence_proxy_async_smem();
     tc_fence_before();
     failed = __syncthreads_or(failed);
@@ -592,7 +646,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       if (OUT) {
 #pragma unroll
         for (int ks = 0; ks < DK / 16; ++ks)
-          umma_f16_ta(tmem + L::kInter + (c & 1) * 64, tmem + L::kS + ks * 8, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), kDescHi,
+          umma_f16_ta(tmem + L::kInter, tmem + L::kS + ks * 8, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), kDescHi,
                       kBase | instr_desc_f16(128, 64), ks > 0);
       }
 #pragma unroll
@@ -602,121 +656,54 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
           umma_f16_ab(tmem + L::kAdded + (OUT ? 0 : (c & 1) * DK), desc_lo_mn(vt + ks * 2048), kDescHi, desc_lo_mn(pieces + n * L::kQK + ks * 2048),
                       kDescHi, kBase | kAlongM | kAlongN | instr_desc_f16(128, DK), n < K::kPieces - 1 || ks > 0);
       umma_commit(done + (OUT ? 0 : (c & 1) * 8));
-    }
-    if (warp == kDecayWarp && c + 1 < chunks) all_decay += chunk_decays(g0, g1, p.scale, decays[(c + 1) % 3]);
-    if (tid == 32) {
-      odd_values[(c + 1) % 3] = 0;
-      if (K::kScaled)
-        for (int i = 0; i < 3; ++i) largest[(c + 1) & 1][i] = 0;
-    }
-
-    if (OUT) {
-      // o of the chunk before, then P
-      if (c > 0) {
-        failed = !mbar_wait(intra_done, (uint32_t)(c - 1) & 1, &abort_flag, p.status) || failed;
-        tc_fence_after();
-        finish(c - 1, p.o_by_map != 0);
-        if (*(volatile uint32_t*)&odd_values[(c - 1) % 3]) __syncthreads();    // (P has been read)
-      }
-      // q . k: the 16 x 8 blocks that reach below the diagonal, two in each of the first ten warps: eight of the last row of blocks,
-      // six of the one before, four, two
-      float P[2][4];
-      const int rb = warp < 4 ? 3 : warp < 7 ? 2 : warp < 9 ? 1 : 0;
-      const int nt0 = 2 * (warp < 4 ? warp : warp < 7 ? warp - 4 : warp < 9 ? warp - 7 : 0);
-      const bool makes_p = warp < 10;
-      float scale_p = 1.0f;
-      if (makes_p) {
-        float P2[2][4];                                        // (two chains of additions)
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) P[n][i] = P2[n][i] = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < DK / 16; ks += 2) {              // 32 elements of dk
-          uint32_t a[2][4];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int r = rb * 16 + (lane & 15), cc = (ks + i) * 2 + (lane >> 4);
-            ldmatrix_x4(qt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), a[i]);
-          }
-#pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const int r = (nt0 + n) * 8 + (lane & 7), cc = ks * 2 + (lane >> 3);
-            uint32_t b[4];
-            ldmatrix_x4(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4), b);
-            K::mma(P[n], a[0], b[0], b[1]);
-            K::mma(P2[n], a[1], b[2], b[3]);
-          }
-        }
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int ti = rb * 16 + (lane >> 2) + 8 * (i >> 1), tj = (nt0 + n) * 8 + 2 * (lane & 3) + (i & 1);
-            const float power = (d.whole[ti] - d.whole[tj]) + (d.part[ti] - d.part[tj]);
-            P[n][i] = tj <= ti ? (P[n][i] + P2[n][i]) * (exp2_fast(power) * p.scale) : 0.0f;
-          }
-      }
-      if (K::kScaled) {
-        if (makes_p) {
-          uint32_t pm = 0;
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pm = max(pm, finite_bits(P[n][i]));
-          raise_max(&largest[c & 1][1], pm);
-        }
-        __syncthreads();
-        scale_p = scale_for(largest[c & 1][1]);
-      }
-      if (makes_p) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int ti = rb * 16 + (lane >> 2) + 8 * i, cc = nt0 + n;
-            st_shared4(smem + L::kPAt + ti * 128 + ((cc ^ (ti & 7)) << 4) + (lane & 3) * 4, K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
-          }
-      }
-      fence_proxy_async_smem();
-      tc_fence_before();
-      __syncthreads();
-      if (warp == kMmaWarp && elect_one()) {
-        tc_fence_after();
+      if (OUT) {
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
           umma_f16_ab(tmem + L::kIntra, desc_lo_mn(vt + ks * 2048), kDescHi, smem_desc_lo(smem + L::kPAt + ks * 32), kDescHi,
-                      K::kFormats | kAlongM | instr_desc_f16(128, 64), ks > 0);
+                      kBase | kAlongM | instr_desc_f16(128, 64), ks > 0);
         umma_commit(intra_done);
+        if (c + 1 < whole && mbar_wait(loaded + ((c + 1) % kStages) * 8, (uint32_t)((c + 1) / kStages) & 1, &abort_flag, p.status)) issue_qk(c + 1);
       }
-      if (c > 0 && p.o_by_map && warp == kLoadWarp && elect_one())
-        tma_store_3d(&maps.o, smem + L::kOAt, (int)tile * kTile, head, first + (c - 1) * kChunk);
-      load(c + 2);                                             // (into the stage of the chunk before)
+    }
+    // (for the chunk two behind this one, in the places of the one two before: a barrier lies on either side)
+    if (warp == kDecayWarp && c + 2 < chunks) all_decay += chunk_decays(g0, g1, p.scale, decays[(c + 2) & 3]);
+    if (tid == 32) {
+      odd_values[(c + 2) & 3] = 0;
+      if (K::kScaled)
+        for (int i = 0; i < 3; ++i) largest[(c + 2) & 3][i] = 0;
+    }
+    if (c + 1 == whole && whole < chunks) load_part(whole);
+
+    if (OUT) {
+      if (c > 0 && p.o_by_map && warp == kLoadWarp && lane == 0)
+        tma_store_3d(&maps.o, smem + ((c - 1) % kStages) * L::kStage + L::kQK + L::kV, (int)tile * kTile, head, first + (c - 1) * kChunk);
       failed = !mbar_wait(done, (uint32_t)c & 1, &abort_flag, p.status) || failed;
       tc_fence_after();
       add(c, scale_k);
-      prev_s = scale_s;
-      prev_p = scale_p;
+      failed = !mbar_wait(intra_done, (uint32_t)c & 1, &abort_flag, p.status) || failed;
+      tc_fence_after();
+      finish(c, scale_s, scale_p, p.o_by_map && c + 1 < chunks);
+      if (*(volatile uint32_t*)&odd_values[c & 3]) __syncthreads();          // (P has been read)
     } else {
       if (c > 0) {
         failed = !mbar_wait(done + ((c - 1) & 1) * 8, (uint32_t)((c - 1) >> 1) & 1, &abort_flag, p.status) || failed;
         tc_fence_after();
         add(c - 1, prev_k);
-        if (*(volatile uint32_t*)&odd_values[(c - 1) % 3]) __syncthreads();    // (k and v have been read)
+        if (*(volatile uint32_t*)&odd_values[(c - 1) & 3]) __syncthreads();  // (its k and v have been read)
       }
-      load(c + 2);
       prev_k = scale_k;
+    }
+    // into the stage of the chunk before, out of which o has gone
+    if (warp == kLoadWarp && lane == 0) {
+      if (OUT) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      if (c + 2 < whole) load_whole(c + 2);
     }
   }
   if (failed) {                                                // (its loads under way end before the block does)
     for (int i = c; i < c + 2 && i < whole; ++i) mbar_wait(loaded + (i % kStages) * 8, (uint32_t)(i / kStages) & 1, &abort_flag, p.status);
   } else if (chunks > 0) {
     const int z = chunks - 1;
-    if (OUT) {
-      mbar_wait(intra_done, (uint32_t)z & 1, &abort_flag, p.status);
-      tc_fence_after();
-      finish(z, false);
-    } else {
+    if (!OUT) {
       mbar_wait(done + (z & 1) * 8, (uint32_t)(z >> 1) & 1, &abort_flag, p.status);
       tc_fence_after();
       add(z, prev_k);
