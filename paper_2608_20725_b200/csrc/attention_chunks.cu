@@ -31,6 +31,7 @@
 
 #include <algorithm>
 
+#define IM2WIN_INLINE_SLOW_WAIT          // (register counts set by warpgroup leave no room for calls)
 #include "common.cuh"
 #include "ptx_sm100.cuh"
 #include "sequence.cuh"
@@ -41,11 +42,15 @@ namespace {
 using namespace ptx;
 
 constexpr int kChunk = 64;               // tokens
-constexpr int kThreads = 512;
+constexpr int kThreads = 512;           // that have a part of S; two more warps
+constexpr int kAllThreads = kThreads + 128;
+// Registers: 640 threads are launched with 96 each; four warpgroups of workers take what the fifth gives back (512 x 104 + 128 x 64).
+// With 96 the workers spill, to the L2 cache: shared memory leaves none of the first level.
+constexpr int kWorkerRegisters = 104, kHelperRegisters = 64;
 constexpr int kQuarters = kThreads / 128; // parts of dk, and of a chunk's tokens, of the threads that have a column of dv
 constexpr int kStages = 3;
-// Warps with a job besides their share; those that make no P (see chunk_kernel)
-constexpr int kLoadWarp = 13, kDecayWarp = 14, kMmaWarp = 15;
+constexpr int kIssueWarp = 16;          // one thread of it starts loads and products
+constexpr int kDecayWarp = 17;          // sends o out, sums up log_decay, two chunks ahead
 constexpr int kTile = 128;               // columns of dv of a block: rows of the products
 constexpr uint32_t kPanel = 64 * 128;    // 64 rows of 64 16-bit elements, 128-byte swizzle
 
@@ -165,7 +170,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // The decays of one chunk, all relative to its start.
-struct Decays {
+struct alignas(16) Decays {
   float whole[kChunk], part[kChunk];     // G_i in powers of two: its floor and the rest
   float from_start[kChunk];              // exp(G_i) scale
   float to_end[kChunk];                  // exp(G_n - G_i)
@@ -240,20 +245,19 @@ __device__ __forceinline__ double chunk_decays(float g0, float g1, float scale, 
   return end;
 }
 
-// Shared memory: three stages of k, v and q, the pieces of the weighted k (two sets where o is not made), P.
+// Shared memory: three stages of k, v and q, the pieces of the weighted k (two sets where o is not made), P, o on its way out.
 template <typename T, int DK, bool OUT>
 struct Layout {
   static constexpr uint32_t kQK = DK / 64 * kPanel;            // q or k of a chunk
   static constexpr uint32_t kV = 2 * kPanel;
-  static constexpr uint32_t kO = kChunk * kTile * 2;           // o of a chunk on its way out, in the place of its q
-  static constexpr uint32_t kLoaded = (OUT ? 2 : 1) * kQK + kV;
-  static constexpr uint32_t kStage = kQK + kV + (OUT ? (kO > kQK ? kO : kQK) : 0);
+  static constexpr uint32_t kStage = (OUT ? 2 : 1) * kQK + kV;
   static constexpr uint32_t kPieces = Kind<T>::kPieces * kQK;
   static constexpr uint32_t kPiecesAt = kStages * kStage;
   static constexpr uint32_t kPAt = kPiecesAt + (OUT ? 1 : 2) * kPieces;
-  static constexpr uint32_t kBytes = kPAt + (OUT ? kPanel : 0) + 1024;
-  // columns of tensor memory
-  static constexpr uint32_t kAdded = 0, kInter = DK, kIntra = DK + 64, kQK64 = DK + 128, kS = DK + 192;      // (where o is not made: two of added)
+  static constexpr uint32_t kOAt = kPAt + kPanel;
+  static constexpr uint32_t kBytes = (OUT ? kOAt + kChunk * kTile * 2 : kPAt) + 1024;
+  // columns of tensor memory: added (two where o is not made), two of inter, two of intra, q . k, the copy of S
+  static constexpr uint32_t kAdded = 0, kInter = DK, kIntra = DK + 128, kDots = DK + 256, kS = DK + 320;
   static constexpr uint32_t kColumns = OUT ? 512 : 2 * DK;
 };
 
@@ -294,15 +298,41 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t sr
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
+// A wait that has mostly come about (a look costs a fifth of the time of a try that may suspend).
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status) {
+  if (mbar_test_wait(bar, parity)) return true;
+  return mbar_wait(bar, parity, abort_flag, status);
+}
+
+// Barriers of the workers and the two helping warps.
+__device__ __forceinline__ void sync_all() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads + 64) : "memory"); }
+__device__ __forceinline__ bool sync_or(bool any) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 q, %1, 0;\n\t"
+      "bar.red.or.pred p, 1, %2, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)any), "n"(kThreads + 64)
+      : "memory");
+  return r != 0;
+}
+
+// The order of work for chunk c, between its barrier and the next chunk's:
+//   issue warp    the loads of chunk c+2; q . k of chunk c+1; inter, added and intra of chunk c
+//   decay warp    the store of o of chunk c-2, the decays of chunk c+2
+//   all others    P of chunk c+1; o of chunk c-1 to shared memory; S with what chunk c added
+// and before the barrier: weighted k in pieces, the copy of S, P of chunk c to where the products read them.
 template <typename T, int DK, bool OUT>
-__global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constant__ ChunkMaps maps, const ChunkParams p) {
+__global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_constant__ ChunkMaps maps, const ChunkParams p) {
   using K = Kind<T>;
   using L = Layout<T, DK, OUT>;
   constexpr int kMine = DK / kQuarters;                        // columns of S of a thread
   constexpr int kTokens = kChunk / kQuarters;                  // rows of o of a thread
   extern __shared__ uint8_t dynamic_smem[];
   __shared__ Decays decays[4];
-  __shared__ __align__(8) uint64_t bars[kStages + 3];          // stages loaded; state products done (two), intra, q . k done
+  __shared__ __align__(8) uint64_t bars[kStages + 4];          // stages loaded; added done (two), intra, q . k done, o stored
   __shared__ uint32_t tmem_base_at, abort_flag, odd_values[4], largest[4][3];
   const uint32_t smem = (smem_u32(dynamic_smem) + 1023u) & ~1023u;
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
@@ -317,17 +347,13 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const bool last = end == piece.rows.end;
   if (!OUT && last) return;                                    // (nothing starts behind it)
 
-  const int quarter = warp >> 2, row = (warp & 3) * 32 + lane; // row: of the transposed products, a column of dv
-  const int col = (int)tile * kTile + row;
-  const bool live = col < p.dv;
-  const int64_t state_size = (int64_t)p.dk * p.dv;
   const int chunks = (end - first + kChunk - 1) / kChunk, whole = (end - first) / kChunk;
 
   const uint32_t loaded = smem_u32(bars), done = smem_u32(bars + kStages), intra_done = smem_u32(bars + kStages + 1),
-                 qk_done = smem_u32(bars + kStages + 2);
+                 dots_done = smem_u32(bars + kStages + 2), stored = smem_u32(bars + kStages + 3);
   if (warp == 0) tmem_alloc(smem_u32(&tmem_base_at), L::kColumns);
   if (tid == 0) {
-    for (int i = 0; i < kStages + 3; ++i) mbar_init(smem_u32(bars + i), 1);
+    for (int i = 0; i < kStages + 4; ++i) mbar_init(smem_u32(bars + i), 1);
     abort_flag = 0;
     for (int i = 0; i < 12; ++i) largest[i / 3][i % 3] = 0;
     for (int i = 0; i < 4; ++i) odd_values[i] = 0;
@@ -335,15 +361,13 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     fence_proxy_async_smem();
   }
   if (OUT && tid < kPanel / 16) st_shared16(smem + L::kPAt + tid * 16, 0, 0, 0, 0);      // (above the diagonal it stays 0)
+  auto wait = [&](uint32_t bar, uint32_t phase) { return wait_for(bar, phase & 1, &abort_flag, p.status); };
 
-  const T* q = static_cast<const T*>(p.q) + (int64_t)(head / p.share) * p.dk;
-  const T* k = static_cast<const T*>(p.k) + (int64_t)(head / p.share) * p.dk;
-  const T* v = static_cast<const T*>(p.v) + (int64_t)head * p.dv + tile * kTile;
   // A whole chunk: one thread, by TMA (elements beyond a head's read as 0).
   auto load_whole = [&](int c) {
     const uint32_t base = smem + (c % kStages) * L::kStage, bar = loaded + (c % kStages) * 8;
     const int t0 = first + c * kChunk;
-    mbar_arrive_expect_tx(bar, L::kLoaded);
+    mbar_arrive_expect_tx(bar, L::kStage);
 #pragma unroll
     for (int i = 0; i < DK / 64; ++i) {
       tma_load_3d(base + i * kPanel, &maps.k, i * 64, head / p.share, t0, bar);
@@ -352,12 +376,15 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
 #pragma unroll
     for (int i = 0; i < 2; ++i) tma_load_3d(base + L::kQK + i * kPanel, &maps.v, (int)tile * kTile + i * 64, head, t0, bar);
   };
-  // The last chunk of a sequence: all threads; the rows of the next sequence, and those behind the last, as 0.
+  // The last chunk of a sequence: the workers; the rows of the next sequence, and those behind the last, as 0.
   auto load_part = [&](int c) {
+    const T* q = static_cast<const T*>(p.q) + (int64_t)(head / p.share) * p.dk;
+    const T* k = static_cast<const T*>(p.k) + (int64_t)(head / p.share) * p.dk;
+    const T* v = static_cast<const T*>(p.v) + (int64_t)head * p.dv + tile * kTile;
     const uint32_t base = smem + (c % kStages) * L::kStage;
     const int t0 = first + c * kChunk;
     constexpr int kUnits = DK / 8;
-#pragma unroll
+#pragma unroll 1
     for (int u = tid; u < kChunk * kUnits; u += kThreads) {
       const int r = u / kUnits, cc = u % kUnits;
       const bool there = t0 + r < end && cc * 8 < p.dk;
@@ -367,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       copy16(base + at, k + t * p.k_stride + off, there);
       if (OUT) copy16(base + L::kQK + L::kV + at, q + t * p.q_stride + off, there);
     }
-#pragma unroll
+#pragma unroll 1
     for (int u = tid; u < kChunk * 16; u += kThreads) {
       const int r = u / 16, cc = u % 16;
       const bool there = t0 + r < end && (int)tile * kTile + cc * 8 < p.dv;
@@ -382,351 +409,448 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     g1 = t + 1 < end ? p.decay[(int64_t)(t + 1) * p.decay_stride + head] : 0.0f;
   };
 
-  double all_decay = 0.0;
-  if (warp == kDecayWarp && chunks > 0) {
-    float g0, g1, h0, h1;
-    load_decay(0, g0, g1);
-    load_decay(1, h0, h1);
-    all_decay = chunk_decays(g0, g1, p.scale, decays[0]);
-    if (chunks > 1) all_decay += chunk_decays(h0, h1, p.scale, decays[1]);
-  }
-  // the starting state
-  float S[kMine];
-  {
-    const float* from = nullptr;
-    if (OUT && live) {
-      if (p.segmented)
-        from = p.state_in + ((int64_t)id * p.heads + head) * state_size;
-      else if (p.state_in && resumes(p.seqs, piece.sequence))
-        from = p.state_in + ((int64_t)slot * p.heads + head) * state_size;
-    }
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const int d = quarter * kMine + j;
-      S[j] = from && d < p.dk ? from[(int64_t)d * p.dv + col] : 0.0f;
-    }
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base_at, lanes = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes
-  if (warp == kLoadWarp && lane == 0) {
-    if (0 < whole) load_whole(0);
-    if (1 < whole) load_whole(1);
-  }
-  if (whole == 0 && chunks > 0) load_part(0);
-
-  T* o = static_cast<T*>(p.o) + (int64_t)head * p.dv + col;
-  // element e of row t of panels at `at`
-  auto element = [&](uint32_t at, int t, int e) {
-    return K::low(ld_shared_u16(at + (e >> 6) * kPanel + t * 128 + ((((uint32_t)(e & 63) >> 3) ^ (t & 7)) << 4) + (e & 7) * 2));
-  };
-  // o of chunk c, whose products are done; staged: through shared memory
-  auto finish = [&](int c, float scale_s, float scale_p, bool staged) {
-    const Decays& d = decays[c & 3];
-    const int t0 = first + c * kChunk;
-    const float is = 1.0f / scale_s, ip = 1.0f / scale_p;
-    uint32_t inter[kTokens], intra[kTokens];
-    tmem_ld(tmem + lanes + L::kInter + quarter * kTokens, inter);
-    tmem_ld(tmem + lanes + L::kIntra + quarter * kTokens, intra);
-    tmem_ld_done(inter);
-    tmem_ld_done(intra);
-    if (*(volatile uint32_t*)&odd_values[c & 3]) {             // from the terms j <= i alone
-      const uint32_t vt = smem + (c % kStages) * L::kStage + L::kQK;
-#pragma unroll 1
-      for (int i = 0; i < kTokens; ++i) {
-        const int ti = quarter * kTokens + i;
-        float sum = 0.0f;
-#pragma unroll 1
-        for (int j = 0; j <= ti; ++j) sum = fmaf(element(smem + L::kPAt, ti, j), element(vt, j, row), sum);
-#pragma unroll
-        for (int u = 0; u < kTokens; ++u)
-          if (u == i) intra[u] = __float_as_uint(sum);
-      }
-    }
-    unsigned short y[kTokens];
-#pragma unroll
-    for (int i = 0; i < kTokens; ++i) {
-      const T t = from_float<T>(fmaf(d.from_start[quarter * kTokens + i] * is, __uint_as_float(inter[i]), __uint_as_float(intra[i]) * ip));
-      y[i] = *reinterpret_cast<const unsigned short*>(&t);
-    }
-    if (staged) {
-      const uint32_t to = smem + (c % kStages) * L::kStage + L::kQK + L::kV + quarter * kTokens * (kTile * 2) + row * 2;
-#pragma unroll
-      for (int i = 0; i < kTokens; ++i) asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + i * kTile * 2), "h"(y[i]) : "memory");
-    } else {
-      unsigned short* at = reinterpret_cast<unsigned short*>(o) + (int64_t)(t0 + quarter * kTokens) * p.o_stride;
-      const int n = live ? end - (t0 + quarter * kTokens) : 0;
-#pragma unroll
-      for (int i = 0; i < kTokens; ++i)
-        if (i < n) at[(int64_t)i * p.o_stride] = y[i];
-    }
-  };
-  // what chunk c added, once its products are done
-  auto add = [&](int c, float scale_k) {
-    const Decays& d = decays[c & 3];
-    uint32_t added[kMine];
-    tmem_ld(tmem + lanes + L::kAdded + (OUT ? 0 : (c & 1) * DK) + quarter * kMine, added);
-    tmem_ld_done(added);
-    if (*(volatile uint32_t*)&odd_values[c & 3]) {             // from the products in fp32
-      const uint32_t base = smem + (c % kStages) * L::kStage;
-      const int n = min(kChunk, end - (first + c * kChunk));
-#pragma unroll 1
-      for (int i = 0; i < kMine; ++i) {
-        float sum = 0.0f;
-#pragma unroll 1
-        for (int t = 0; t < n; ++t) sum = fmaf(element(base, t, quarter * kMine + i) * d.to_end[t], element(base + L::kQK, t, row), sum);
-#pragma unroll
-        for (int u = 0; u < kMine; ++u)
-          if (u == i) added[u] = __float_as_uint(sum * scale_k);
-      }
-    }
-    const float ik = 1.0f / scale_k;
-    const float2 total = d.total;
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) S[j] = carry(S[j], total, __uint_as_float(added[j]) * ik);
-  };
-
   // q . k of chunk c: one thread
-  auto issue_qk = [&](int c) {
+  auto issue_dots = [&](int c) {
     const uint32_t kt = smem + (c % kStages) * L::kStage, qt = kt + L::kQK + L::kV;
 #pragma unroll
     for (int ks = 0; ks < DK / 16; ++ks)
-      umma_f16_lohi(tmem + L::kQK64, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), smem_desc_lo(kt + (ks / 4) * kPanel + (ks % 4) * 32),
+      umma_f16_lohi(tmem + L::kDots, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), smem_desc_lo(kt + (ks / 4) * kPanel + (ks % 4) * 32),
                     K::kFormats | instr_desc_f16(64, 64), ks > 0);
-    umma_commit(qk_done);
+    umma_commit(dots_done);
   };
-
   bool failed = false;
-  float prev_k = 1.0f;
-  if (OUT && whole > 0 && warp == kMmaWarp) {
-    failed = !mbar_wait(loaded, 0, &abort_flag, p.status);
-    if (elect_one()) issue_qk(0);
-  }
-  int c = 0;
-  for (; c < chunks; ++c) {
-    const int stage = c % kStages;
-    const uint32_t base = smem + stage * L::kStage;
-    const uint32_t kt = base, vt = base + L::kQK, qt = base + L::kQK + L::kV;
-    const Decays& d = decays[c & 3];
-    float g0 = 0.0f, g1 = 0.0f;
-    if (warp == kDecayWarp && c + 2 < chunks) load_decay(c + 2, g0, g1);
-    if (c < whole) {
-      failed = !mbar_wait(loaded + stage * 8, (uint32_t)(c / kStages) & 1, &abort_flag, p.status) || failed;
-    } else {
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
-      fence_proxy_async_smem();
-      __syncthreads();
-      if (OUT && warp == kMmaWarp && elect_one()) {
+  if (warp >= kThreads / 32) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHelperRegisters));
+    bool odd_1 = false, odd_2 = false;
+    if (warp == kIssueWarp) {
+      // (Waits by the whole warp, issue by one elected lane: operands of the tensor cores and of TMA are uniform registers, which they stay
+      // in where the compiler sees no other branch.)
+      if (elect_one()) {
+        if (0 < whole) load_whole(0);
+        if (1 < whole) load_whole(1);
+      }
+      __syncwarp();
+      if (OUT && 0 < whole) {
+        failed = !wait(loaded, 0);
+        if (elect_one()) issue_dots(0);
+        __syncwarp();
+      }
+      sync_all();
+      int c = 0;
+      for (; c < chunks; ++c) {
+        const uint32_t kt = smem + (c % kStages) * L::kStage, vt = kt + L::kQK, qt = vt + L::kV;
+        const uint32_t pieces = smem + L::kPiecesAt + (OUT ? 0 : (c & 1) * L::kPieces);
+        if (c == whole) {
+          sync_all();
+          tc_fence_after();
+          if (OUT && elect_one()) issue_dots(c);
+          __syncwarp();
+        }
+        if (K::kScaled) sync_all();
+        failed = sync_or(failed);
+        if (failed) break;
         tc_fence_after();
-        issue_qk(c);
+        const bool odd_0 = *(volatile uint32_t*)&odd_values[c & 3] != 0;
+        if (OUT && c + 1 < whole) {
+          failed = !wait(loaded + ((c + 1) % kStages) * 8, (c + 1) / kStages);
+          if (elect_one()) issue_dots(c + 1);
+          __syncwarp();
+        }
+        if (elect_one()) {
+          if (OUT) {
+#pragma unroll
+            for (int ks = 0; ks < DK / 16; ++ks)
+              umma_f16_ta(tmem + L::kInter + (c & 1) * 64, tmem + L::kS + ks * 8, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), kDescHi,
+                          K::kFormats | instr_desc_f16(128, 64), ks > 0);
+          }
+#pragma unroll
+          for (int n = K::kPieces - 1; n >= 0; --n)            // the smallest pieces first
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              umma_f16_ab(tmem + L::kAdded + (OUT ? 0 : (c & 1) * DK), desc_lo_mn(vt + ks * 2048), kDescHi,
+                          desc_lo_mn(pieces + n * L::kQK + ks * 2048), kDescHi, K::kFormats | kAlongM | kAlongN | instr_desc_f16(128, DK),
+                          n < K::kPieces - 1 || ks > 0);
+          umma_commit(done + (OUT ? 0 : (c & 1) * 8));
+          if (OUT) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              umma_f16_ab(tmem + L::kIntra + (c & 1) * 64, desc_lo_mn(vt + ks * 2048), kDescHi, smem_desc_lo(smem + L::kPAt + ks * 32), kDescHi,
+                          K::kFormats | kAlongM | instr_desc_f16(128, 64), ks > 0);
+            umma_commit(intra_done);
+            if (c + 2 < whole) load_whole(c + 2);              // (the products of the chunk before are done: seen before the barrier)
+          }
+        }
+        __syncwarp();
+        if (!OUT && c > 0) failed = !wait(done + ((c - 1) & 1) * 8, (c - 1) >> 1) || failed;
+        if (OUT ? odd_0 : odd_1) sync_all();                   // (the workers have read P, k and v)
+        if (!OUT && c + 2 < whole && elect_one()) load_whole(c + 2);
+        __syncwarp();
+        odd_1 = odd_0;
+      }
+      if (failed)                                              // (its loads under way end before the block does)
+        for (int i = c; i < c + 2 && i < whole; ++i) wait(loaded + (i % kStages) * 8, i / kStages);
+    } else if (warp == kDecayWarp) {
+      double all_decay = 0.0;
+      float g0 = 0.0f, g1 = 0.0f;
+      if (chunks > 0) {
+        load_decay(0, g0, g1);
+        all_decay = chunk_decays(g0, g1, p.scale, decays[0]);
+        load_decay(1, g0, g1);
+        if (chunks > 1) all_decay += chunk_decays(g0, g1, p.scale, decays[1]);
+      }
+      sync_all();
+      for (int c = 0; c < chunks; ++c) {
+        if (c + 2 < chunks) load_decay(c + 2, g0, g1);
+        if (c == whole) sync_all();
+        if (K::kScaled) sync_all();
+        if (sync_or(false)) break;
+        const bool odd_0 = *(volatile uint32_t*)&odd_values[c & 3] != 0;
+        if (OUT && elect_one()) {
+          if (p.o_by_map && c > 1 && !odd_2) {
+            tma_store_3d(&maps.o, smem + L::kOAt, (int)tile * kTile, head, first + (c - 2) * kChunk);
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          }
+          mbar_arrive(stored);
+        }
+        __syncwarp();
+        // (in the places of the chunk two before, a barrier behind its last use and one before its first)
+        if (c + 2 < chunks) all_decay += chunk_decays(g0, g1, p.scale, decays[(c + 2) & 3]);
+        __syncwarp();
+        if (lane == 0) {
+          odd_values[(c + 2) & 3] = 0;
+          if (K::kScaled)
+            for (int i = 0; i < 3; ++i) largest[(c + 2) & 3][i] = 0;
+        }
+        if (OUT ? odd_0 : odd_1) sync_all();
+        odd_2 = odd_1;
+        odd_1 = odd_0;
+      }
+      if (OUT) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+      if (!OUT && tile == 0) {
+        const float2 total = two_parts(all_decay);
+        if (lane == 0) p.totals[(int64_t)id * p.heads + head] = total;
       }
     }
-
-    // k weighted and in pieces, the copy of S, P
-    constexpr int kUnits = DK / 8, kVectors = kChunk * kUnits / kThreads;
-    uint4 kk[kVectors];
-    uint32_t odd = 0;                                          // bits 15 and 31: an infinity or NaN
-    auto look = [&](uint32_t w) { odd |= (w & 0x7fff7fffu) + K::kOddStep; };
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWorkerRegisters));
+    const int quarter = warp >> 2, row = (warp & 3) * 32 + lane;           // row: of the transposed products, a column of dv
+    const int col = (int)tile * kTile + row;
+    const bool live = col < p.dv;
+    const int64_t state_size = (int64_t)p.dk * p.dv;
+    if (whole == 0 && chunks > 0) load_part(0);
+    // the starting state
+    float S[kMine];
+    {
+      const float* from = nullptr;
+      if (OUT && live) {
+        if (p.segmented)
+          from = p.state_in + ((int64_t)id * p.heads + head) * state_size;
+        else if (p.state_in && resumes(p.seqs, piece.sequence))
+          from = p.state_in + ((int64_t)slot * p.heads + head) * state_size;
+      }
 #pragma unroll
-    for (int m = 0; m < kVectors; ++m) {
-      const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
-      kk[m] = ld_shared16(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4));
-      look(kk[m].x); look(kk[m].y); look(kk[m].z); look(kk[m].w);
+      for (int j = 0; j < kMine; ++j) {
+        const int d = quarter * kMine + j;
+        S[j] = from && d < p.dk ? from[(int64_t)d * p.dv + col] : 0.0f;
+      }
     }
-    const bool odd_k = (odd & 0x80008000u) != 0;
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const uint4 vv = ld_shared16(vt + (tid + m * kThreads) * 16);
-      look(vv.x); look(vv.y); look(vv.z); look(vv.w);
-    }
-    if (odd & 0x80008000u) odd_values[c & 3] = 1;
-    // P: the 16 x 16 blocks that reach below the diagonal, one to a warp: rows 16 rb, columns 16 quarter
-    float P[2][4];
+    // element e of row t of panels at `at`
+    auto element = [&](uint32_t at, int t, int e) {
+      return K::low(ld_shared_u16(at + (e >> 6) * kPanel + t * 128 + ((((uint32_t)(e & 63) >> 3) ^ (t & 7)) << 4) + (e & 7) * 2));
+    };
+    // P of chunk c, whose q . k are done (its 16 x 16 blocks that reach below the diagonal, one to a warp: rows 16 rb, columns 16 quarter)
     const int rb = warp & 3;
     const bool makes_p = OUT && quarter <= rb;
-    if (OUT) {
-      failed = !mbar_wait(qk_done, (uint32_t)c & 1, &abort_flag, p.status) || failed;
-      tc_fence_after();
-    }
-    if (makes_p) {
+    float P[2][4];
+    auto make_p = [&](int c) {
+      const Decays& d = decays[c & 3];
       uint32_t dots[8];
-      tmem_ld_16x16(tmem + lanes + L::kQK64 + quarter * 16, dots);
+      tmem_ld_16x16(tmem + lanes + L::kDots + quarter * 16, dots);
+      const int ti = rb * 16 + (lane >> 2), tj = quarter * 16 + 2 * (lane & 3);
+      const float wi[2] = {d.whole[ti], d.whole[ti + 8]}, pi[2] = {d.part[ti], d.part[ti + 8]};
       tmem_ld_done(dots);
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int n = 0; n < 2; ++n) {
+        const float2 wj = *reinterpret_cast<const float2*>(&d.whole[tj + 8 * n]), pj = *reinterpret_cast<const float2*>(&d.part[tj + 8 * n]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int ti = rb * 16 + (lane >> 2) + 8 * (i >> 1), tj = quarter * 16 + n * 8 + 2 * (lane & 3) + (i & 1);
-          const float power = (d.whole[ti] - d.whole[tj]) + (d.part[ti] - d.part[tj]);
-          P[n][i] = tj <= ti ? __uint_as_float(dots[4 * n + i]) * (exp2_fast(power) * p.scale) : 0.0f;
+          const float power = (wi[i >> 1] - (i & 1 ? wj.y : wj.x)) + (pi[i >> 1] - (i & 1 ? pj.y : pj.x));
+          const float w = __uint_as_float(dots[4 * n + i]) * (exp2_fast(power) * p.scale);
+          P[n][i] = tj + 8 * n + (i & 1) <= ti + 8 * (i >> 1) ? w : 0.0f;
         }
+      }
+      if (K::kScaled) {
+        uint32_t pm = 0;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) pm = max(pm, finite_bits(P[n][i]));
+        raise_max(&largest[c & 3][1], pm);
+      }
+    };
+    // o of chunk c, whose products are done, two rows a register
+    auto make_o = [&](int c, float scale_s, float scale_p, bool odd, uint32_t (&y)[kTokens / 2]) {
+      const Decays& d = decays[c & 3];
+      const float is = 1.0f / scale_s, ip = 1.0f / scale_p;
+      uint32_t inter[kTokens], intra[kTokens];
+      tmem_ld(tmem + lanes + L::kInter + (c & 1) * 64 + quarter * kTokens, inter);
+      tmem_ld(tmem + lanes + L::kIntra + (c & 1) * 64 + quarter * kTokens, intra);
+      tmem_ld_done(inter);
+      tmem_ld_done(intra);
+      if (odd) {                                                 // from the terms j <= i alone
+        const uint32_t vt = smem + (c % kStages) * L::kStage + L::kQK;
+#pragma unroll 1
+        for (int i = 0; i < kTokens; ++i) {
+          const int ti = quarter * kTokens + i;
+          float sum = 0.0f;
+#pragma unroll 1
+          for (int j = 0; j <= ti; ++j) sum = fmaf(element(smem + L::kPAt, ti, j), element(vt, j, row), sum);
+#pragma unroll
+          for (int u = 0; u < kTokens; ++u)
+            if (u == i) intra[u] = __float_as_uint(sum);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kTokens; i += 4) {
+        const float4 from = *reinterpret_cast<const float4*>(&d.from_start[quarter * kTokens + i]);
+        const float f[4] = {from.x, from.y, from.z, from.w};
+#pragma unroll
+        for (int u = 0; u < 4; u += 2)
+          y[(i + u) / 2] = K::pack(fmaf(f[u] * is, __uint_as_float(inter[i + u]), __uint_as_float(intra[i + u]) * ip),
+                                   fmaf(f[u + 1] * is, __uint_as_float(inter[i + u + 1]), __uint_as_float(intra[i + u + 1]) * ip));
+      }
+    };
+    auto store_o = [&](int c, const uint32_t (&y)[kTokens / 2]) {
+      const int t0 = first + c * kChunk + quarter * kTokens;
+      unsigned short* at = static_cast<unsigned short*>(p.o) + (int64_t)head * p.dv + col + (int64_t)t0 * p.o_stride;
+      const int n = live ? end - t0 : 0;
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i)
+        if (i < n) at[(int64_t)i * p.o_stride] = (unsigned short)(y[i / 2] >> (16 * (i & 1)));
+    };
+    auto stage_o = [&](const uint32_t (&y)[kTokens / 2]) {
+      const uint32_t to = smem + L::kOAt + quarter * kTokens * (kTile * 2) + row * 2;
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i)
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + i * kTile * 2), "h"((unsigned short)(y[i / 2] >> (16 * (i & 1)))) : "memory");
+    };
+    // what chunk c added, once its products are done
+    auto add = [&](int c, float scale_k, bool odd) {
+      const Decays& d = decays[c & 3];
+      uint32_t added[kMine];
+      tmem_ld(tmem + lanes + L::kAdded + (OUT ? 0 : (c & 1) * DK) + quarter * kMine, added);
+      const float2 total = d.total;
+      tmem_ld_done(added);
+      if (odd) {                                                 // from the products in fp32
+        const uint32_t base = smem + (c % kStages) * L::kStage;
+        const int n = min(kChunk, end - (first + c * kChunk));
+#pragma unroll 1
+        for (int i = 0; i < kMine; ++i) {
+          float sum = 0.0f;
+#pragma unroll 1
+          for (int t = 0; t < n; ++t) sum = fmaf(element(base, t, quarter * kMine + i) * d.to_end[t], element(base + L::kQK, t, row), sum);
+#pragma unroll
+          for (int u = 0; u < kMine; ++u)
+            if (u == i) added[u] = __float_as_uint(sum * scale_k);
+        }
+      }
+      const float ik = 1.0f / scale_k;
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) S[j] = carry(S[j], total, __uint_as_float(added[j]) * ik);
+    };
+
+    float prev_k = 1.0f, prev_s = 1.0f, prev_p = 1.0f;         // the chunk before's scales,
+    bool odd_1 = false;                                        // whether its k and v hold infinities or NaNs
+    sync_all();                                                // (the first decays)
+    if (OUT && 0 < whole) {
+      failed = !wait(dots_done, 0);
+      tc_fence_after();
+      if (makes_p) make_p(0);
     }
-    float scale_k = 1.0f, scale_s = 1.0f, scale_p = 1.0f;
-    if (K::kScaled) {
-      uint32_t top = 0;
+    for (int c = 0; c < chunks; ++c) {
+      const uint32_t kt = smem + (c % kStages) * L::kStage, vt = kt + L::kQK;
+      const uint32_t pieces = smem + L::kPiecesAt + (OUT ? 0 : (c & 1) * L::kPieces);
+      if (c == whole) {                                        // the last one, in part
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        fence_proxy_async_smem();
+        sync_all();
+        if (OUT) {
+          failed = !wait(dots_done, c) || failed;
+          tc_fence_after();
+          if (makes_p) make_p(c);
+        }
+      } else {
+        failed = !wait(loaded + (c % kStages) * 8, c / kStages) || failed;
+      }
+
+      constexpr int kUnits = DK / 8, kVectors = kChunk * kUnits / kThreads;
+      uint4 kk[kVectors];
+      uint32_t odd = 0;                                        // bits 15 and 31: an infinity or NaN
+      auto look = [&](uint32_t w) { odd |= (w & 0x7fff7fffu) + K::kOddStep; };
 #pragma unroll
-      for (int m = 0; m < kVectors; ++m)
+      for (int m = 0; m < kVectors; ++m) {
+        const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
+        kk[m] = ld_shared16(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4));
+      }
 #pragma unroll
-        for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) top = __vmaxu2(top, w & 0x7fff7fffu);
-      if (odd_k) {                                             // the largest of the others
-        top = 0;
+      for (int m = 0; m < kVectors; ++m) { look(kk[m].x); look(kk[m].y); look(kk[m].z); look(kk[m].w); }
+      const bool odd_k = (odd & 0x80008000u) != 0;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const uint4 vv = ld_shared16(vt + (tid + m * kThreads) * 16);
+        look(vv.x); look(vv.y); look(vv.z); look(vv.w);
+      }
+      if (odd & 0x80008000u) odd_values[c & 3] = 1;
+      float scale_k = 1.0f, scale_s = 1.0f, scale_p = 1.0f;
+      if (K::kScaled) {
+        uint32_t top = 0;
 #pragma unroll
         for (int m = 0; m < kVectors; ++m)
 #pragma unroll
-          for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) {
-            if ((w & 0x7c00u) != 0x7c00u) top = __vmaxu2(top, w & 0x7fffu);
-            if ((w & 0x7c000000u) != 0x7c000000u) top = __vmaxu2(top, w & 0x7fff0000u);
-          }
-      }
-      raise_max(&largest[c & 3][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
-      if (OUT) {
-        uint32_t sm = 0;
+          for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) top = __vmaxu2(top, w & 0x7fff7fffu);
+        if (odd_k) {                                           // the largest of the others
+          top = 0;
 #pragma unroll
-        for (int j = 0; j < kMine; ++j) sm = max(sm, finite_bits(S[j]));
-        raise_max(&largest[c & 3][2], sm);
+          for (int m = 0; m < kVectors; ++m)
+#pragma unroll
+            for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) {
+              if ((w & 0x7c00u) != 0x7c00u) top = __vmaxu2(top, w & 0x7fffu);
+              if ((w & 0x7c000000u) != 0x7c000000u) top = __vmaxu2(top, w & 0x7fff0000u);
+            }
+        }
+        raise_max(&largest[c & 3][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
+        if (OUT) {
+          uint32_t sm = 0;
+#pragma unroll
+          for (int j = 0; j < kMine; ++j) sm = max(sm, finite_bits(S[j]));
+          raise_max(&largest[c & 3][2], sm);
+        }
+        sync_all();
+        scale_k = scale_for(largest[c & 3][0]);
+        if (OUT) {
+          scale_p = scale_for(largest[c & 3][1]);
+          scale_s = scale_for(largest[c & 3][2]);
+        }
+      }
+      if (OUT) {
+        uint32_t r[kMine / 2];
+#pragma unroll
+        for (int i = 0; i < kMine / 2; ++i) r[i] = K::pack(S[2 * i] * scale_s, S[2 * i + 1] * scale_s);
+        tmem_st(tmem + lanes + L::kS + quarter * (kMine / 2), r);
+      }
+      {
+        const Decays& d = decays[c & 3];
+#pragma unroll
+        for (int m = 0; m < kVectors; ++m) {
+          const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
+          const float w = d.to_end[r] * scale_k;
+          const uint32_t words[4] = {kk[m].x, kk[m].y, kk[m].z, kk[m].w};
+          uint32_t out[K::kPieces][4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t piece_of[K::kPieces];
+            K::split(K::low(words[i]) * w, K::high(words[i]) * w, piece_of);
+#pragma unroll
+            for (int n = 0; n < K::kPieces; ++n) out[n][i] = piece_of[n];
+          }
+          const uint32_t at = (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4);
+#pragma unroll
+          for (int n = 0; n < K::kPieces; ++n) st_shared16(pieces + n * L::kQK + at, out[n][0], out[n][1], out[n][2], out[n][3]);
+        }
+      }
+      if (OUT) {
+        if (c > 0) failed = !wait(intra_done, c - 1) || failed;      // (it read P)
         if (makes_p) {
-          uint32_t pm = 0;
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pm = max(pm, finite_bits(P[n][i]));
-          raise_max(&largest[c & 3][1], pm);
+            for (int i = 0; i < 2; ++i) {
+              const int ti = rb * 16 + (lane >> 2) + 8 * i, cc = quarter * 2 + n;
+              st_shared4(smem + L::kPAt + ti * 128 + ((cc ^ (ti & 7)) << 4) + (lane & 3) * 4, K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
+            }
         }
+        tmem_st_wait();
       }
-      __syncthreads();
-      scale_k = scale_for(largest[c & 3][0]);
+      fence_proxy_async_smem();
+      tc_fence_before();
+      failed = sync_or(failed);
+      if (failed) break;
+      tc_fence_after();
+      const bool odd_0 = *(volatile uint32_t*)&odd_values[c & 3] != 0;     // (set before the barrier: every thread sees the same)
+      if (c + 1 == whole && whole < chunks) load_part(whole);
       if (OUT) {
-        scale_p = scale_for(largest[c & 3][1]);
-        scale_s = scale_for(largest[c & 3][2]);
-      }
-    }
-    if (OUT) {
-      uint32_t r[kMine / 2];
-#pragma unroll
-      for (int i = 0; i < kMine / 2; ++i) r[i] = K::pack(S[2 * i] * scale_s, S[2 * i + 1] * scale_s);
-      tmem_st(tmem + lanes + L::kS + quarter * (kMine / 2), r);
-    }
-    if (makes_p) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int ti = rb * 16 + (lane >> 2) + 8 * i, cc = quarter * 2 + n;
-          st_shared4(smem + L::kPAt + ti * 128 + ((cc ^ (ti & 7)) << 4) + (lane & 3) * 4, K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
+        if (c + 1 < whole) {
+          failed = !wait(dots_done, c + 1) || failed;
+          tc_fence_after();
+          if (makes_p) make_p(c + 1);
         }
-    }
-    const uint32_t pieces = smem + L::kPiecesAt + (OUT ? 0 : (c & 1) * L::kPieces);
-#pragma unroll
-    for (int m = 0; m < kVectors; ++m) {
-      const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
-      const float w = d.to_end[r] * scale_k;
-      const uint32_t words[4] = {kk[m].x, kk[m].y, kk[m].z, kk[m].w};
-      uint32_t out[K::kPieces][4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t piece_of[K::kPieces];
-        K::split(K::low(words[i]) * w, K::high(words[i]) * w, piece_of);
-#pragma unroll
-        for (int n = 0; n < K::kPieces; ++n) out[n][i] = piece_of[n];
-      }
-      const uint32_t at = (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4);
-#pragma unroll
-      for (int n = 0; n < K::kPieces; ++n) st_shared16(pieces + n * L::kQK + at, out[n][0], out[n][1], out[n][2], out[n][3]);
-    }
-    if (OUT) tmem_st_wait();
-    fence_proxy_async_smem();
-    tc_fence_before();
-    failed = __syncthreads_or(failed);
-    if (failed) break;
-
-    if (warp == kMmaWarp && elect_one()) {
-      tc_fence_after();
-      constexpr uint32_t kBase = K::kFormats;
-      if (OUT) {
-#pragma unroll
-        for (int ks = 0; ks < DK / 16; ++ks)
-          umma_f16_ta(tmem + L::kInter, tmem + L::kS + ks * 8, smem_desc_lo(qt + (ks / 4) * kPanel + (ks % 4) * 32), kDescHi,
-                      kBase | instr_desc_f16(128, 64), ks > 0);
-      }
-#pragma unroll
-      for (int n = K::kPieces - 1; n >= 0; --n)                // the smallest pieces first
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          umma_f16_ab(tmem + L::kAdded + (OUT ? 0 : (c & 1) * DK), desc_lo_mn(vt + ks * 2048), kDescHi, desc_lo_mn(pieces + n * L::kQK + ks * 2048),
-                      kDescHi, kBase | kAlongM | kAlongN | instr_desc_f16(128, DK), n < K::kPieces - 1 || ks > 0);
-      umma_commit(done + (OUT ? 0 : (c & 1) * 8));
-      if (OUT) {
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-          umma_f16_ab(tmem + L::kIntra, desc_lo_mn(vt + ks * 2048), kDescHi, smem_desc_lo(smem + L::kPAt + ks * 32), kDescHi,
-                      kBase | kAlongM | instr_desc_f16(128, 64), ks > 0);
-        umma_commit(intra_done);
-        if (c + 1 < whole && mbar_wait(loaded + ((c + 1) % kStages) * 8, (uint32_t)((c + 1) / kStages) & 1, &abort_flag, p.status)) issue_qk(c + 1);
-      }
-    }
-    // (for the chunk two behind this one, in the places of the one two before: a barrier lies on either side)
-    if (warp == kDecayWarp && c + 2 < chunks) all_decay += chunk_decays(g0, g1, p.scale, decays[(c + 2) & 3]);
-    if (tid == 32) {
-      odd_values[(c + 2) & 3] = 0;
-      if (K::kScaled)
-        for (int i = 0; i < 3; ++i) largest[(c + 2) & 3][i] = 0;
-    }
-    if (c + 1 == whole && whole < chunks) load_part(whole);
-
-    if (OUT) {
-      if (c > 0 && p.o_by_map && warp == kLoadWarp && lane == 0)
-        tma_store_3d(&maps.o, smem + ((c - 1) % kStages) * L::kStage + L::kQK + L::kV, (int)tile * kTile, head, first + (c - 1) * kChunk);
-      failed = !mbar_wait(done, (uint32_t)c & 1, &abort_flag, p.status) || failed;
-      tc_fence_after();
-      add(c, scale_k);
-      failed = !mbar_wait(intra_done, (uint32_t)c & 1, &abort_flag, p.status) || failed;
-      tc_fence_after();
-      finish(c, scale_s, scale_p, p.o_by_map && c + 1 < chunks);
-      if (*(volatile uint32_t*)&odd_values[c & 3]) __syncthreads();          // (P has been read)
-    } else {
-      if (c > 0) {
-        failed = !mbar_wait(done + ((c - 1) & 1) * 8, (uint32_t)((c - 1) >> 1) & 1, &abort_flag, p.status) || failed;
+        if (c > 0 && !odd_1) {                                 // (an odd chunk's has been stored)
+          uint32_t y[kTokens / 2];
+          make_o(c - 1, prev_s, prev_p, false, y);
+          if (p.o_by_map && c + 1 < chunks) {
+            failed = !wait(stored, c) || failed;
+            stage_o(y);
+          } else {
+            store_o(c - 1, y);
+          }
+        }
+        failed = !wait(done, c) || failed;
         tc_fence_after();
-        add(c - 1, prev_k);
-        if (*(volatile uint32_t*)&odd_values[(c - 1) & 3]) __syncthreads();  // (its k and v have been read)
+        add(c, scale_k, odd_0);
+        if (odd_0) {
+          failed = !wait(intra_done, c) || failed;
+          tc_fence_after();
+          uint32_t y[kTokens / 2];
+          make_o(c, scale_s, scale_p, true, y);
+          store_o(c, y);
+          sync_all();                                          // (P and v have been read)
+        }
+        prev_s = scale_s;
+        prev_p = scale_p;
+      } else {
+        if (c > 0) {
+          failed = !wait(done + ((c - 1) & 1) * 8, (c - 1) >> 1) || failed;
+          tc_fence_after();
+          add(c - 1, prev_k, odd_1);
+        }
+        if (odd_1) sync_all();                                 // (k and v of the chunk before have been read)
+        prev_k = scale_k;
       }
-      prev_k = scale_k;
+      odd_1 = odd_0;
     }
-    // into the stage of the chunk before, out of which o has gone
-    if (warp == kLoadWarp && lane == 0) {
-      if (OUT) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-      if (c + 2 < whole) load_whole(c + 2);
+    if (!failed && chunks > 0) {
+      const int z = chunks - 1;
+      if (OUT) {
+        if (!odd_1) {
+          wait(intra_done, z);
+          tc_fence_after();
+          uint32_t y[kTokens / 2];
+          make_o(z, prev_s, prev_p, false, y);
+          store_o(z, y);
+        }
+      } else {
+        wait(done + (z & 1) * 8, z >> 1);
+        tc_fence_after();
+        add(z, prev_k, odd_1);
+      }
     }
-  }
-  if (failed) {                                                // (its loads under way end before the block does)
-    for (int i = c; i < c + 2 && i < whole; ++i) mbar_wait(loaded + (i % kStages) * 8, (uint32_t)(i / kStages) & 1, &abort_flag, p.status);
-  } else if (chunks > 0) {
-    const int z = chunks - 1;
-    if (!OUT) {
-      mbar_wait(done + (z & 1) * 8, (uint32_t)(z >> 1) & 1, &abort_flag, p.status);
-      tc_fence_after();
-      add(z, prev_k);
-    }
-  }
-
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-  if (OUT && warp == kLoadWarp) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-  float* to = nullptr;
-  if (!OUT)
-    to = p.added + ((int64_t)id * p.heads + head) * state_size;
-  else if (p.state_out && last)
-    to = p.state_out + ((int64_t)slot * p.heads + head) * state_size;
-  if (to && live) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    float* to = nullptr;
+    if (!OUT)
+      to = p.added + ((int64_t)id * p.heads + head) * state_size;
+    else if (p.state_out && last)
+      to = p.state_out + ((int64_t)slot * p.heads + head) * state_size;
+    if (to && live) {
 #pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const int e = quarter * kMine + j;
-      if (e < p.dk) to[(int64_t)e * p.dv + col] = S[j];
+      for (int j = 0; j < kMine; ++j) {
+        const int e = quarter * kMine + j;
+        if (e < p.dk) to[(int64_t)e * p.dv + col] = S[j];
+      }
     }
-  }
-  if (!OUT && warp == kDecayWarp && tile == 0) {
-    const float2 total = two_parts(all_decay);
-    if (lane == 0) p.totals[(int64_t)id * p.heads + head] = total;
   }
   tc_fence_before();
   __syncthreads();
@@ -844,7 +968,7 @@ cudaError_t launch(const ChunkMaps& maps, const ChunkParams& p, int64_t pieces, 
   }
   const int64_t grid = pieces * p.heads * p.tiles;
   if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
-  chunk_kernel<T, DK, OUT><<<(unsigned)grid, kThreads, kBytes, stream>>>(maps, p);
+  chunk_kernel<T, DK, OUT><<<(unsigned)grid, kAllThreads, kBytes, stream>>>(maps, p);
   return cudaGetLastError();
 }
 
