@@ -60,9 +60,9 @@ struct ChunkParams {
   const void* v;
   const float* decay;
   void* o;
-  const float* state_in;                 // states of the pool, or of the segments (segmented)
+  const float* state_in;
   float* state_out;
-  float* added;                          // [segments][heads][dk][dv]
+  float* added;                          // [segments][heads][dk][dv]: what each adds, then (segmented) its starting state
   float2* totals;                        // [segments][heads]: decay of a whole segment, in two parts
   uint32_t* status;
   Sequences seqs;
@@ -82,7 +82,13 @@ template <> struct Kind<__nv_bfloat16> {
   static constexpr int kPieces = 3;
   static constexpr bool kScaled = false;
   static constexpr uint32_t kFormats = (1u << 7) | (1u << 10);
-  static constexpr uint32_t kOddStep = 0x00800080u;          // added to an exponent of all ones reaches the sign
+  // The larger magnitudes, two at once; a NaN is larger than anything.
+  static __device__ __forceinline__ uint32_t largest(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("{\n\t.reg .b32 m;\n\tabs.bf16x2 m, %2;\n\tmax.NaN.bf16x2 %0, %1, m;\n\t}" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ bool odd(uint32_t top) { return ((top & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; }
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
@@ -103,7 +109,12 @@ template <> struct Kind<__half> {
   static constexpr int kPieces = 2;
   static constexpr bool kScaled = true;
   static constexpr uint32_t kFormats = 0;
-  static constexpr uint32_t kOddStep = 0x04000400u;
+  static __device__ __forceinline__ uint32_t largest(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("{\n\t.reg .b32 m;\n\tabs.f16x2 m, %2;\n\tmax.NaN.f16x2 %0, %1, m;\n\t}" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ bool odd(uint32_t top) { return ((top & 0x7fff7fffu) + 0x04000400u) & 0x80008000u; }
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
@@ -172,9 +183,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // The decays of one chunk, all relative to its start.
 struct alignas(16) Decays {
   float whole[kChunk], part[kChunk];     // G_i in powers of two: its floor and the rest
-  float from_start[kChunk];              // exp(G_i) scale
-  float to_end[kChunk];                  // exp(G_n - G_i)
-  float2 total;                          // exp(G_n) in two parts
+  float from_start[kChunk];              // exp(G_i) scale E, E of the state before the chunk
+  float to_end[kChunk];                  // exp(G_n - G_i) / E, E of the state behind it
+  float total, behind;                   // exp(G_n), rounded; E behind the chunk
 };
 
 // A power of two that brings numbers of at most `bits` (of a float) to below 2^14.
@@ -192,8 +203,7 @@ __device__ __forceinline__ void raise_max(uint32_t* at, uint32_t bits) {
   if ((threadIdx.x & 31) == 0) atomicMax(at, m);
 }
 
-// S <- exp(G_n) S + added, exp(G_n) in two parts (see two_parts): off by less than a rounding of the sum, also after many chunks of
-// a decay near 1.
+// S <- exp(G_n) S + added, for the decay of a segment, in two parts.
 __device__ __forceinline__ float carry(float s, float2 total, float added) { return fmaf(s, total.x, fmaf(s, total.y, added)); }
 
 // exp2(power) as the float below it and the rest, so that an infinity times either has its sign (and no rest where nothing is left).
@@ -206,7 +216,9 @@ __device__ __forceinline__ float2 two_parts(double power) {
 
 // One warp: lane l has tokens 2l and 2l+1.  Returns G_n (powers of two).  Sums are of whole numbers of 2^-44: exact, and without
 // the 64-bit floating-point units, which took 1300 cycles for sums and powers.
-__device__ __forceinline__ double chunk_decays(float g0, float g1, float scale, Decays& d) {
+// The states in registers are S / E: a chunk multiplies them by exp(G_n) rounded to a float, and what that is off, the same at every
+// chunk of a constant decay, goes into E, a double, instead: S is off by less than a rounding of its sums after any number of chunks.
+__device__ __forceinline__ double chunk_decays(float g0, float g1, float scale, double& E, Decays& d) {
   constexpr float kNaN = __builtin_nanf("");
   const int lane = threadIdx.x & 31;
   auto powers = [](float g) -> int64_t {                       // (beyond 2^+-1000 nothing changes in fp32)
@@ -224,11 +236,17 @@ __device__ __forceinline__ double chunk_decays(float g0, float g1, float scale, 
   auto fraction = [](int64_t x) { return (float)((uint32_t)(x >> 20) & 0xffffffu) * 5.9604644775390625e-8f; };
   auto power_of_two = [](int64_t x) { return __uint_as_float((uint32_t)(min(max((int)(x >> 44), -127), 128) + 127) << 23); };
   const int64_t G[2] = {sum - b, sum};
+  const double end = nan0 | nan1 ? (double)kNaN : (double)all * (1.0 / 17592186044416.0);
+  const double exact = exp2(end);
+  const float total = (float)exact;
+  const float before = (float)E * scale;
+  if (total > 1e-30f && total < 1e30f) E += E * (double)__fdividef((float)(exact - (double)total), total);
+  const float per = 1.0f / (float)E;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int64_t rest = all - G[i];
-    float whole = (float)(int)(G[i] >> 44), from = exp2f(fraction(G[i])) * power_of_two(G[i]) * scale;
-    float to_end = exp2f(fraction(rest)) * power_of_two(rest);
+    float whole = (float)(int)(G[i] >> 44), from = exp2f(fraction(G[i])) * power_of_two(G[i]) * before;
+    float to_end = exp2f(fraction(rest)) * power_of_two(rest) * per;
     if (nan0 | nan1) {                                         // behind a NaN every sum is one
       const uint32_t behind0 = (2u << lane) - 1u, behind1 = i ? (2u << lane) - 1u : (1u << lane) - 1u;
       if ((nan0 & behind0) | (nan1 & behind1)) whole = from = kNaN;
@@ -239,9 +257,10 @@ __device__ __forceinline__ double chunk_decays(float g0, float g1, float scale, 
     d.from_start[2 * lane + i] = from;
     d.to_end[2 * lane + i] = to_end;
   }
-  const double end = nan0 | nan1 ? (double)kNaN : (double)all * (1.0 / 17592186044416.0);
-  const float2 total = two_parts(end);
-  if (lane == 0) d.total = total;
+  if (lane == 0) {
+    d.total = total;
+    d.behind = (float)E;
+  }
   return end;
 }
 
@@ -494,13 +513,13 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       if (failed)                                              // (its loads under way end before the block does)
         for (int i = c; i < c + 2 && i < whole; ++i) wait(loaded + (i % kStages) * 8, i / kStages);
     } else if (warp == kDecayWarp) {
-      double all_decay = 0.0;
+      double all_decay = 0.0, E = 1.0;
       float g0 = 0.0f, g1 = 0.0f;
       if (chunks > 0) {
         load_decay(0, g0, g1);
-        all_decay = chunk_decays(g0, g1, p.scale, decays[0]);
+        all_decay = chunk_decays(g0, g1, p.scale, E, decays[0]);
         load_decay(1, g0, g1);
-        if (chunks > 1) all_decay += chunk_decays(g0, g1, p.scale, decays[1]);
+        if (chunks > 1) all_decay += chunk_decays(g0, g1, p.scale, E, decays[1]);
       }
       sync_all();
       for (int c = 0; c < chunks; ++c) {
@@ -518,7 +537,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         }
         __syncwarp();
         // (in the places of the chunk two before, a barrier behind its last use and one before its first)
-        if (c + 2 < chunks) all_decay += chunk_decays(g0, g1, p.scale, decays[(c + 2) & 3]);
+        if (c + 2 < chunks) all_decay += chunk_decays(g0, g1, p.scale, E, decays[(c + 2) & 3]);
         __syncwarp();
         if (lane == 0) {
           odd_values[(c + 2) & 3] = 0;
@@ -547,8 +566,8 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
     {
       const float* from = nullptr;
       if (OUT && live) {
-        if (p.segmented)
-          from = p.state_in + ((int64_t)id * p.heads + head) * state_size;
+        if (p.segmented && !(leads && last))                   // (of a sequence that is cut)
+          from = p.added + ((int64_t)id * p.heads + head) * state_size;
         else if (p.state_in && resumes(p.seqs, piece.sequence))
           from = p.state_in + ((int64_t)slot * p.heads + head) * state_size;
       }
@@ -584,12 +603,19 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         }
       }
       if (K::kScaled) {
-        uint32_t pm = 0;
+        float pm = 0.0f;
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) pm = max(pm, finite_bits(P[n][i]));
-        raise_max(&largest[c & 3][1], pm);
+          for (int i = 0; i < 4; ++i) pm = fmaxf(pm, fabsf(P[n][i]));
+        if (pm > FLT_MAX) {
+          pm = 0.0f;
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pm = fmaxf(pm, fabsf(P[n][i]) <= FLT_MAX ? fabsf(P[n][i]) : 0.0f);
+        }
+        raise_max(&largest[c & 3][1], __float_as_uint(pm));
       }
     };
     // o of chunk c, whose products are done, two rows a register
@@ -643,7 +669,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       const Decays& d = decays[c & 3];
       uint32_t added[kMine];
       tmem_ld(tmem + lanes + L::kAdded + (OUT ? 0 : (c & 1) * DK) + quarter * kMine, added);
-      const float2 total = d.total;
+      const float total = d.total;
       tmem_ld_done(added);
       if (odd) {                                                 // from the products in fp32
         const uint32_t base = smem + (c % kStages) * L::kStage;
@@ -660,9 +686,20 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       }
       const float ik = 1.0f / scale_k;
 #pragma unroll
-      for (int j = 0; j < kMine; ++j) S[j] = carry(S[j], total, __uint_as_float(added[j]) * ik);
+      for (int j = 0; j < kMine; ++j) S[j] = fmaf(S[j], total, __uint_as_float(added[j]) * ik);
     };
 
+    // infinities and NaNs among v of chunk c
+    auto look_at_v = [&](int c) {
+      const uint32_t vt = smem + (c % kStages) * L::kStage + L::kQK;
+      uint32_t top = 0;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const uint4 vv = ld_shared16(vt + (tid + m * kThreads) * 16);
+        top = K::largest(K::largest(K::largest(K::largest(top, vv.x), vv.y), vv.z), vv.w);
+      }
+      if (K::odd(top)) odd_values[c & 3] = 1;
+    };
     float prev_k = 1.0f, prev_s = 1.0f, prev_p = 1.0f;         // the chunk before's scales,
     bool odd_1 = false;                                        // whether its k and v hold infinities or NaNs
     sync_all();                                                // (the first decays)
@@ -670,6 +707,8 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       failed = !wait(dots_done, 0);
       tc_fence_after();
       if (makes_p) make_p(0);
+      failed = !wait(loaded, 0) || failed;
+      look_at_v(0);
     }
     for (int c = 0; c < chunks; ++c) {
       const uint32_t kt = smem + (c % kStages) * L::kStage, vt = kt + L::kQK;
@@ -683,35 +722,25 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
           tc_fence_after();
           if (makes_p) make_p(c);
         }
-      } else {
+      } else if (!OUT) {                                       // (otherwise waited for with the chunk before)
         failed = !wait(loaded + (c % kStages) * 8, c / kStages) || failed;
       }
 
       constexpr int kUnits = DK / 8, kVectors = kChunk * kUnits / kThreads;
       uint4 kk[kVectors];
-      uint32_t odd = 0;                                        // bits 15 and 31: an infinity or NaN
-      auto look = [&](uint32_t w) { odd |= (w & 0x7fff7fffu) + K::kOddStep; };
+      if (c == whole || !OUT) look_at_v(c);
 #pragma unroll
       for (int m = 0; m < kVectors; ++m) {
         const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
         kk[m] = ld_shared16(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4));
       }
+      uint32_t top = 0;
 #pragma unroll
-      for (int m = 0; m < kVectors; ++m) { look(kk[m].x); look(kk[m].y); look(kk[m].z); look(kk[m].w); }
-      const bool odd_k = (odd & 0x80008000u) != 0;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const uint4 vv = ld_shared16(vt + (tid + m * kThreads) * 16);
-        look(vv.x); look(vv.y); look(vv.z); look(vv.w);
-      }
-      if (odd & 0x80008000u) odd_values[c & 3] = 1;
+      for (int m = 0; m < kVectors; ++m) top = K::largest(K::largest(K::largest(K::largest(top, kk[m].x), kk[m].y), kk[m].z), kk[m].w);
+      const bool odd_k = K::odd(top);
+      if (odd_k) odd_values[c & 3] = 1;
       float scale_k = 1.0f, scale_s = 1.0f, scale_p = 1.0f;
       if (K::kScaled) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int m = 0; m < kVectors; ++m)
-#pragma unroll
-          for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) top = __vmaxu2(top, w & 0x7fff7fffu);
         if (odd_k) {                                           // the largest of the others
           top = 0;
 #pragma unroll
@@ -724,10 +753,15 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         }
         raise_max(&largest[c & 3][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
         if (OUT) {
-          uint32_t sm = 0;
+          float sm = 0.0f;
 #pragma unroll
-          for (int j = 0; j < kMine; ++j) sm = max(sm, finite_bits(S[j]));
-          raise_max(&largest[c & 3][2], sm);
+          for (int j = 0; j < kMine; ++j) sm = fmaxf(sm, fabsf(S[j]));
+          if (sm > FLT_MAX) {                                  // (an infinity: the largest of the others; NaNs do not count)
+            sm = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) sm = fmaxf(sm, fabsf(S[j]) <= FLT_MAX ? fabsf(S[j]) : 0.0f);
+          }
+          raise_max(&largest[c & 3][2], __float_as_uint(sm));
         }
         sync_all();
         scale_k = scale_for(largest[c & 3][0]);
@@ -783,11 +817,6 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       const bool odd_0 = *(volatile uint32_t*)&odd_values[c & 3] != 0;     // (set before the barrier: every thread sees the same)
       if (c + 1 == whole && whole < chunks) load_part(whole);
       if (OUT) {
-        if (c + 1 < whole) {
-          failed = !wait(dots_done, c + 1) || failed;
-          tc_fence_after();
-          if (makes_p) make_p(c + 1);
-        }
         if (c > 0 && !odd_1) {                                 // (an odd chunk's has been stored)
           uint32_t y[kTokens / 2];
           make_o(c - 1, prev_s, prev_p, false, y);
@@ -797,6 +826,13 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
           } else {
             store_o(c - 1, y);
           }
+        }
+        if (c + 1 < whole) {
+          failed = !wait(dots_done, c + 1) || failed;
+          tc_fence_after();
+          if (makes_p) make_p(c + 1);
+          failed = !wait(loaded + ((c + 1) % kStages) * 8, (c + 1) / kStages) || failed;
+          look_at_v(c + 1);
         }
         failed = !wait(done, c) || failed;
         tc_fence_after();
@@ -845,10 +881,11 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
     else if (p.state_out && last)
       to = p.state_out + ((int64_t)slot * p.heads + head) * state_size;
     if (to && live) {
+      const float E = chunks > 0 ? decays[(chunks - 1) & 3].behind : 1.0f;
 #pragma unroll
       for (int j = 0; j < kMine; ++j) {
         const int e = quarter * kMine + j;
-        if (e < p.dk) to[(int64_t)e * p.dv + col] = S[j];
+        if (e < p.dk) to[(int64_t)e * p.dv + col] = S[j] * E;
       }
     }
   }
@@ -858,35 +895,41 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   if (warp == 0) tmem_dealloc(tmem, L::kColumns);
 }
 
-// The starting state of every segment, in the place of what it adds: a thread has a number of a head's state and runs over the
-// segments of a sequence.
+// The starting state of every segment of a sequence that is cut, in the place of what it adds: a thread has four numbers of a head's
+// state (dk * dv is a multiple of 64) and runs over the segments.
 __global__ void __launch_bounds__(256) segment_states_kernel(const ChunkParams p, const float* pool, int32_t blocks) {
   const uint32_t rest = blockIdx.x / (uint32_t)blocks;
   const int head = (int)(rest % (uint32_t)p.heads), b = (int)(rest / (uint32_t)p.heads);
-  const int slot = slot_of(p.seqs, b);
-  const int64_t size = (int64_t)p.dk * p.dv, e = (int64_t)(blockIdx.x % (uint32_t)blocks) * 256 + threadIdx.x;
-  if (slot < 0 || e >= size) return;
   const SequenceRows rows = rows_of(p.seqs, b);
-  const int32_t len = rows.end - rows.begin, n = len > p.L ? (len + p.L - 1) / p.L : 1;
+  const int32_t len = rows.end - rows.begin;
+  const int slot = slot_of(p.seqs, b);
+  const int64_t size = (int64_t)p.dk * p.dv, e = ((int64_t)(blockIdx.x % (uint32_t)blocks) * 256 + threadIdx.x) * 4;
+  if (len <= p.L || slot < 0 || e >= size) return;
+  const int32_t n = (len + p.L - 1) / p.L;
   // (as find_piece numbers them)
   const int64_t id0 = p.seqs.cu ? (int64_t)(rows.begin / p.L) + b : (int64_t)b * n;
-  float s = pool && resumes(p.seqs, b) ? pool[((int64_t)slot * p.heads + head) * size + e] : 0.0f;
-  constexpr int kAhead = 8;
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (pool && resumes(p.seqs, b)) s = *reinterpret_cast<const float4*>(pool + ((int64_t)slot * p.heads + head) * size + e);
+  constexpr int kAhead = 4;
   for (int i0 = 0; i0 < n; i0 += kAhead) {
-    float added[kAhead];
+    float4 added[kAhead];
     float2 total[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
+      if (i0 + i + 1 >= n) break;                              // (the last one's sum is not made)
       const int64_t at = (id0 + i0 + i) * p.heads + head;
-      const bool there = i0 + i + 1 < n;                       // (the last one's sum is not made)
-      added[i] = there ? p.added[at * size + e] : 0.0f;
-      total[i] = there ? p.totals[at] : make_float2(1.0f, 0.0f);
+      added[i] = *reinterpret_cast<const float4*>(p.added + at * size + e);
+      total[i] = p.totals[at];
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (i0 + i >= n) break;
-      p.added[((id0 + i0 + i) * p.heads + head) * size + e] = s;
-      s = carry(s, total[i], added[i]);
+      *reinterpret_cast<float4*>(p.added + ((id0 + i0 + i) * p.heads + head) * size + e) = s;
+      if (i0 + i + 1 >= n) break;
+      s.x = carry(s.x, total[i], added[i].x);
+      s.y = carry(s.y, total[i], added[i].y);
+      s.z = carry(s.z, total[i], added[i].z);
+      s.w = carry(s.w, total[i], added[i].w);
     }
   }
 }
@@ -898,8 +941,8 @@ struct ChunkPlan {
   size_t totals_off, added_off, bytes;
 };
 
-// Segments by an estimate, in chunks' times: rounds of 148 blocks over the chunks of a segment, and where sequences are cut, as many for
-// what the segments but the last add, which takes 0.6 of the time, and the time of two more launches.
+// Segments by an estimate, in chunks' times: rounds of 148 blocks over the chunks of a segment and two for a block's start, and where
+// sequences are cut, as many for what the segments but the last add, which takes 0.6 of the time, and the time of two more launches.
 ChunkPlan plan_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool has_cu) {
   ChunkPlan c = {};
   const int64_t longest = has_cu ? (s.max_len > 0 ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens) : s.tokens / s.sequences;
@@ -916,8 +959,8 @@ ChunkPlan plan_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool 
   int64_t best_n = 1;
   for (int64_t n = 1; n <= chunks && n <= 64; ++n) {
     const int64_t per = (chunks + n - 1) / n;
-    double cost = (double)((like * blocks * n + 147) / 148) * (double)per;
-    if (n > 1) cost += (double)((like * blocks * (n - 1) + 147) / 148) * (double)per * 0.6 + 8.0;
+    double cost = (double)((like * blocks * n + 147) / 148) * (double)(per + 2);
+    if (n > 1) cost += (double)((like * blocks * (n - 1) + 147) / 148) * (double)(per + 2) * 0.6 + 5.0;
     if (n == 1 || cost < best) { best = cost; best_n = n; }
   }
   if (const char* v = debug_getenv("IM2WIN_SEGMENTS")) best_n = std::min<int64_t>(std::max(atoi(v), 1), chunks);    // testing aid
@@ -980,13 +1023,12 @@ cudaError_t launch_all(const ChunkMaps& maps, ChunkParams& p, const ChunkPlan& p
     pieces = plan.segments;
     cudaError_t e = launch<T, DK, false>(maps, p, pieces, stream);
     if (e != cudaSuccess) return e;
-    const int32_t blocks = (int32_t)(((int64_t)p.dk * p.dv + 255) / 256);
+    const int32_t blocks = (int32_t)(((int64_t)p.dk * p.dv + 1023) / 1024);
     const int64_t grid = (int64_t)blocks * p.heads * a.shape.sequences;
     if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
     segment_states_kernel<<<(unsigned)grid, 256, 0, stream>>>(p, a.state_in, blocks);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    p.state_in = p.added;
     p.segmented = 1;
   }
   return launch<T, DK, true>(maps, p, pieces, stream);
