@@ -519,9 +519,9 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         load_decay(0, g0, g1);
         all_decay = chunk_decays(g0, g1, p.scale, E, decays[0]);
         load_decay(1, g0, g1);
-        if (chunks > 1) all_decay += chunk_decays(g0, g1, p.scale, E, decays[1]);
       }
       sync_all();
+      if (chunks > 1) all_decay += chunk_decays(g0, g1, p.scale, E, decays[1]);
       for (int c = 0; c < chunks; ++c) {
         if (c + 2 < chunks) load_decay(c + 2, g0, g1);
         if (c == whole) sync_all();
@@ -941,8 +941,11 @@ struct ChunkPlan {
   size_t totals_off, added_off, bytes;
 };
 
-// Segments by an estimate, in chunks' times: rounds of 148 blocks over the chunks of a segment and two for a block's start, and where
-// sequences are cut, as many for what the segments but the last add, which takes 0.6 of the time, and the time of two more launches.
+// Segments by an estimate, in chunks' times (2.6 us): a launch takes as long as its rounds of the longest pieces, or as all of its
+// work spread over 148 SMs if that is longer, four for the start and end of a block; where sequences are cut, what the segments but the
+// last add comes before, at 0.65 of the time, and two more launches.  (One sequence of 16384 tokens, 32 heads of 128 x 128: 256 chunks in
+// one piece 636 us, in 2, 4, 9, 18 segments 543, 303, 312, 378; 13 sequences of up to 2488, 24 heads of 64 x 128: 1, 2, 3 segments 140,
+// 196, 173.)
 ChunkPlan plan_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool has_cu) {
   ChunkPlan c = {};
   const int64_t longest = has_cu ? (s.max_len > 0 ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens) : s.tokens / s.sequences;
@@ -957,10 +960,16 @@ ChunkPlan plan_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool 
   if (like < 1) like = 1;
   double best = 0;
   int64_t best_n = 1;
+  constexpr double kEnds = 4.0, kAdds = 0.65, kLaunches = 7.0;
+  const double work = (double)((s.tokens / kChunk + s.sequences) * blocks);
   for (int64_t n = 1; n <= chunks && n <= 64; ++n) {
     const int64_t per = (chunks + n - 1) / n;
-    double cost = (double)((like * blocks * n + 147) / 148) * (double)(per + 2);
-    if (n > 1) cost += (double)((like * blocks * (n - 1) + 147) / 148) * (double)(per + 2) * 0.6 + 5.0;
+    auto launch_time = [&](int64_t longest_pieces, double all_chunks, double pieces) {
+      return std::max((double)((longest_pieces + 147) / 148) * ((double)per + kEnds), (all_chunks + pieces * kEnds) / 148.0);
+    };
+    const double pieces = (double)(number_of_pieces(s.tokens, s.sequences, n == 1 ? (int64_t)1 << 40 : per * kChunk, has_cu) * blocks);
+    double cost = launch_time(like * blocks * n, work, pieces);
+    if (n > 1) cost += kAdds * launch_time(like * blocks * (n - 1), (double)(like * blocks * (n - 1) * per), (double)(like * blocks * (n - 1))) + kLaunches;
     if (n == 1 || cost < best) { best = cost; best_n = n; }
   }
   if (const char* v = debug_getenv("IM2WIN_SEGMENTS")) best_n = std::min<int64_t>(std::max(atoi(v), 1), chunks);    // testing aid
