@@ -14,9 +14,10 @@
 // nibbles n0..n7 a mask gives (n0, n4), (n1, n5), (n2, n6), (n3, n7), and x is brought into that order instead.
 // fp32 rows of x are three rows of bf16 pieces each, cut off so that their sum is exact; a column of the product for each.
 //
-// The eight warps of a block take turns at the blocks of 128 elements along K and add their sums up at the end, in their order.
-// A warp works on TILES tiles of rows, so that x, as many bytes as 8 rows of fp16 have for 16 of the matrix, is fetched (from the
-// caches) once for all of them, and loads the next block's weights, scales and zeros before it works on this one's.
+// A block stays on an SM and takes groups of rows in turn.  It brings x into shared memory once, as the products want it (for a batch
+// of 8, twice the bytes that 16 rows of the matrix have: fetched for each such tile it would be most of the traffic); its 16 warps
+// share a group's elements along K, each loading its next two blocks of 128 elements while it works on one, and add their sums up in
+// their order.  Measured, without zero points / with, at 6.53 TB/s: see launch_columns.
 #include <type_traits>
 
 #include "sequence.cuh"
@@ -24,7 +25,9 @@
 namespace im2win {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 16;
+constexpr int kMostX = 128 * 1024;                     // shared memory for x; longer rows go in passes over K,
+constexpr int kMostGroups = 8;                         // whose sums are kept for so many groups of rows at a time
 
 struct Int4Params {
   const void* x;
@@ -35,6 +38,7 @@ struct Int4Params {
   void* y;
   int64_t x_stride, y_stride;
   int32_t M, N, K, group, groups, row_bytes, blocks;   // blocks: of 128 elements along K
+  int32_t pass, wk;                                    // blocks of a pass, warps that share a group of rows along K
   int32_t vec_w, vec_x, vec_s;                         // whether rows of the matrix, of x, and a block's scales can be loaded whole
 };
 
@@ -128,164 +132,242 @@ __device__ __forceinline__ void load_x(const T* row, int at, int K, bool vec, in
   }
 }
 
-// PARTS: groups in 128 elements (1: groups of 128 and multiples, 2: of 64, 4: of 32).  NT: tiles of 8 columns of x.
-template <typename T, int PARTS, int NT, int TILES, bool ZEROS>
-__global__ void __launch_bounds__(kWarps * 32) matvec_kernel(const Int4Params p) {
+// PARTS: groups in 128 elements (1: groups of 128 and multiples, 2: of 64, 4: of 32).  NT: tiles of 8 columns of x.  TILES: of 16 rows.
+// WHOLE: K is a multiple of 128 and everything can be loaded as vectors.
+template <typename T, int PARTS, int NT, int TILES, bool WHOLE>
+__global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params p) {
   using M16 = typename std::conditional<sizeof(T) == 4, __nv_bfloat16, T>::type;   // what the products are made of
   using MM = Mma<M16>;
   constexpr int kWords = 4 / PARTS;              // of a lane, row and group
   constexpr int kPieces = sizeof(T) == 4 ? 3 : 1;
   constexpr int kRows = 2 * TILES;               // of the matrix in a lane
-  __shared__ float sums[kWarps][16 * TILES][NT * 8 + 1];
+  constexpr int kGroupRows = 16 * TILES;
+  extern __shared__ uint4 xs[];                  // [block][word][column][t]: a lane's eight elements of a word, as pairs
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int n0 = blockIdx.x * 16 * TILES;
-  auto row_of = [&](int r) { return min(n0 + r * 8 + g, p.N - 1); };               // (rows beyond the last are computed and dropped)
-  const T* x[NT];
-  int piece[NT];
-  bool column[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int c = i * 8 + g;
-    column[i] = c < p.M * kPieces;
-    piece[i] = kPieces == 3 ? c % 3 : 0;
-    x[i] = static_cast<const T*>(p.x) + (int64_t)(column[i] ? c / kPieces : 0) * p.x_stride;
-  }
+  const int columns = p.M * kPieces;
+  // behind x: the warps' sums of a group of rows, and what passes over K have added up so far
+  float (*sums)[kGroupRows][NT * 8 + 1] = reinterpret_cast<float (*)[kGroupRows][NT * 8 + 1]>(xs + p.pass * 16 * columns);
+  float (*kept)[kGroupRows][NT * 8] = reinterpret_cast<float (*)[kGroupRows][NT * 8]>(sums + kWarps);
+  const int wk = p.wk, part_k = warp % wk, sub = warp / wk, subs = kWarps / wk;    // subs groups of rows side by side
+  const int all_groups = (p.N + kGroupRows * subs - 1) / (kGroupRows * subs);
 
   struct Stage {
     uint32_t w[kRows][4];
     Vec<T, PARTS> scale[kRows];
-    Vec<uint8_t, PARTS> zero[ZEROS ? kRows : 1];
+    Vec<uint8_t, PARTS> zero[kRows];
   };
-  auto fetch = [&](int block, Stage& s) {
-    const int j0 = PARTS > 1 ? block * PARTS : (int)((int64_t)block * 128 / p.group);
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      const int row = row_of(r);
-      const uint8_t* from = p.weight + (int64_t)row * p.row_bytes;
-#pragma unroll
-      for (int part = 0; part < PARTS; ++part)
-        load_weights<kWords>(from, block * 64 + part * (64 / PARTS) + t * (kWords * 4), p.row_bytes, p.vec_w, &s.w[r][part * kWords]);
-      const int64_t at = (int64_t)row * p.groups + j0;
-      const T* scale = static_cast<const T*>(p.scales) + at;
-      if (PARTS == 1 || p.vec_s) {
-        s.scale[r] = *reinterpret_cast<const Vec<T, PARTS>*>(scale);
-        if (ZEROS) s.zero[r] = *reinterpret_cast<const Vec<uint8_t, PARTS>*>(p.zeros + at);
-      } else {
-#pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
-          const bool there = j0 + part < p.groups;
-          s.scale[r].v[part] = there ? scale[part] : from_float<T>(0.0f);
-          if (ZEROS) s.zero[r].v[part] = there ? p.zeros[at + part] : 0;
-        }
-      }
-    }
-  };
-
-  float total[TILES][NT][4] = {};
-  Stage next;
-  if (warp < p.blocks) fetch(warp, next);
-  for (int block = warp; block < p.blocks; block += kWarps) {
-    const Stage s = next;
-    if (block + kWarps < p.blocks) fetch(block + kWarps, next);
-#pragma unroll
-    for (int part = 0; part < PARTS; ++part) {
-      uint32_t bx[NT][kWords][4];
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-#pragma unroll
-          for (int h = 0; h < 4; ++h) bx[i][w][h] = 0;
-          if (column[i])
-            load_x<T>(x[i], block * 128 + part * (128 / PARTS) + t * (kWords * 8) + 8 * w, p.K, p.vec_x, piece[i], bx[i][w]);
-        }
-#pragma unroll
-      for (int tile = 0; tile < TILES; ++tile) {
-        uint32_t zero[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          zero[i] = MM::kMagic + (ZEROS ? (uint32_t)(s.zero[2 * tile + i].v[part] & 15) * 0x10001u : 0x80008u);
-        float acc[NT][4] = {};
-#pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t a[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t word = s.w[2 * tile + (i & 1)][part * kWords + w];
-              a[i] = MM::sub(((word >> (8 * h + 4 * (i >> 1))) & 0x000f000fu) | MM::kMagic, zero[i & 1]);
-            }
-#pragma unroll
-            for (int i = 0; i < NT; ++i) MM::mma(acc[i], a, bx[i][w][2 * h], bx[i][w][2 * h + 1]);
+  const int first_group = blockIdx.x, my_groups = (all_groups - first_group + (int)gridDim.x - 1) / (int)gridDim.x;
+  for (int batch = 0; batch < my_groups; batch += kMostGroups) {
+    const int n_groups = min(kMostGroups, my_groups - batch);
+    for (int b0 = 0; b0 < p.blocks; b0 += p.pass) {
+      const int nb = min(p.pass, p.blocks - b0);
+      // x of this pass
+      if (b0 > 0 || batch == 0 || p.pass < p.blocks) {
+        __syncthreads();
+        for (int c = 0; c < columns; ++c) {
+          const T* row = static_cast<const T*>(p.x) + (int64_t)(c / kPieces) * p.x_stride;
+          for (int u = threadIdx.x; u < nb * 16; u += kWarps * 32) {
+            // word `word` of block b and lane t: the part's elements, the lane's among them, the word's among those
+            const int ut = u & 3, word = (u >> 2) & 3, b = u >> 4, part = word / kWords, w = word % kWords;
+            const int e = (b0 + b) * 128 + part * (128 / PARTS) + ut * (kWords * 8) + 8 * w;
+            uint32_t pairs[4];
+            load_x<T>(row, e, p.K, p.vec_x, c % kPieces, pairs);
+            xs[((u >> 2) * columns + c) * 4 + ut] = make_uint4(pairs[0], pairs[1], pairs[2], pairs[3]);
           }
         }
-        const float sa = to_float(s.scale[2 * tile].v[part]), sb = to_float(s.scale[2 * tile + 1].v[part]);
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          total[tile][i][0] = fmaf(sa, acc[i][0], total[tile][i][0]);
-          total[tile][i][1] = fmaf(sa, acc[i][1], total[tile][i][1]);
-          total[tile][i][2] = fmaf(sb, acc[i][2], total[tile][i][2]);
-          total[tile][i][3] = fmaf(sb, acc[i][3], total[tile][i][3]);
+        __syncthreads();
+      }
+      const int turns = (nb + wk - 1) / wk;
+      auto first_row = [&](int group) { return ((first_group + (batch + group) * (int)gridDim.x) * subs + sub) * kGroupRows; };
+      int next_group = 0, next_turn = 0;         // what is fetched next
+      int64_t row_at = 0;                        // this lane's first row of that group
+      auto fetch = [&](Stage& s) {
+        if (next_turn == 0) row_at = first_row(next_group) + g;
+        const int block = b0 + part_k + next_turn * wk;
+        const bool there = next_group < n_groups && block < b0 + nb;
+        if (++next_turn == turns) {
+          next_turn = 0;
+          ++next_group;
         }
+        if (!there) return;
+        const int j0 = PARTS > 1 ? block * PARTS : p.group == 128 ? block : (int)((int64_t)block * 128 / p.group);
+        const uint8_t* weight = p.weight + row_at * p.row_bytes + block * 64 + t * (kWords * 4);
+        const T* scales = static_cast<const T*>(p.scales) + row_at * p.groups + j0;
+        const uint8_t* zeros = p.zeros ? p.zeros + row_at * p.groups + j0 : nullptr;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          if (row_at + r * 8 >= p.N) break;      // (rows beyond the last: whatever was there is worked on and dropped)
+          const uint8_t* w = weight + (int64_t)(r * 8) * p.row_bytes;
+          const int64_t at = (int64_t)(r * 8) * p.groups;
+          if (WHOLE) {
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+              const Vec<uint32_t, kWords> v = *reinterpret_cast<const Vec<uint32_t, kWords>*>(w + part * (64 / PARTS));
+#pragma unroll
+              for (int i = 0; i < kWords; ++i) s.w[r][part * kWords + i] = v.v[i];
+            }
+            s.scale[r] = *reinterpret_cast<const Vec<T, PARTS>*>(scales + at);
+            if (zeros) s.zero[r] = *reinterpret_cast<const Vec<uint8_t, PARTS>*>(zeros + at);
+          } else {
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+              const int off = block * 64 + part * (64 / PARTS) + t * (kWords * 4);
+              load_weights<kWords>(w + part * (64 / PARTS) - off, off, p.row_bytes, p.vec_w, &s.w[r][part * kWords]);
+              const bool group_there = j0 + part < p.groups;
+              s.scale[r].v[part] = group_there ? scales[at + part] : from_float<T>(0.0f);
+              if (zeros) s.zero[r].v[part] = group_there ? zeros[at + part] : 0;
+            }
+          }
+        }
+      };
+      float total[TILES][NT][4];
+      auto work = [&](int group, int turn, const Stage& s) {
+        const int b = part_k + turn * wk;
+        if (turn == 0) {
+#pragma unroll
+          for (int tile = 0; tile < TILES; ++tile)
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) total[tile][i][r] = 0.0f;
+        }
+        if (b < nb) {
+#pragma unroll
+          for (int part = 0; part < PARTS; ++part) {
+            uint4 bx[NT][kWords];
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+              for (int w = 0; w < kWords; ++w)
+                bx[i][w] = i * 8 + g < columns ? xs[((b * 4 + part * kWords + w) * columns + i * 8 + g) * 4 + t] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int tile = 0; tile < TILES; ++tile) {
+              uint32_t zero[2];
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                zero[i] = MM::kMagic + (p.zeros ? (uint32_t)(s.zero[2 * tile + i].v[part] & 15) * 0x10001u : 0x80008u);
+              float acc[NT][4] = {};
+#pragma unroll
+              for (int w = 0; w < kWords; ++w) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  uint32_t a[4];
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    const uint32_t word = s.w[2 * tile + (i & 1)][part * kWords + w];
+                    a[i] = MM::sub(((word >> (8 * h + 4 * (i >> 1))) & 0x000f000fu) | MM::kMagic, zero[i & 1]);
+                  }
+#pragma unroll
+                  for (int i = 0; i < NT; ++i) MM::mma(acc[i], a, h ? bx[i][w].z : bx[i][w].x, h ? bx[i][w].w : bx[i][w].y);
+                }
+              }
+              const float sa = to_float(s.scale[2 * tile].v[part]), sb = to_float(s.scale[2 * tile + 1].v[part]);
+#pragma unroll
+              for (int i = 0; i < NT; ++i) {
+                total[tile][i][0] = fmaf(sa, acc[i][0], total[tile][i][0]);
+                total[tile][i][1] = fmaf(sa, acc[i][1], total[tile][i][1]);
+                total[tile][i][2] = fmaf(sb, acc[i][2], total[tile][i][2]);
+                total[tile][i][3] = fmaf(sb, acc[i][3], total[tile][i][3]);
+              }
+            }
+          }
+        }
+        if (turn != turns - 1) return;
+        // the group's sums of all warps
+#pragma unroll
+        for (int tile = 0; tile < TILES; ++tile)
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sums[warp][tile * 16 + g + 8 * (r >> 1)][i * 8 + 2 * t + (r & 1)] = total[tile][i][r];
+        __syncthreads();
+        const int n_first = first_row(group) - sub * kGroupRows, rows_log = 31 - __clz(kGroupRows * subs);
+        const bool more = b0 + nb < p.blocks;
+        for (int at = threadIdx.x; at < kGroupRows * subs * p.M; at += kWarps * 32) {
+          const int n = at & (kGroupRows * subs - 1), m = at >> rows_log, r = n % kGroupRows;
+          if (n_first + n >= p.N) continue;
+          float y = 0.0f;
+          for (int w = 0; w < wk; ++w)
+#pragma unroll
+            for (int i = kPieces - 1; i >= 0; --i) y += sums[n / kGroupRows * wk + w][r][m * kPieces + i];
+          if (b0 > 0) y += kept[group][r][m];     // (passes only where a group has all the warps)
+          if (more) {
+            kept[group][r][m] = y;
+          } else {
+            if (p.bias) y += p.bias[n_first + n];
+            static_cast<T*>(p.y)[(int64_t)m * p.y_stride + n_first + n] = from_float<T>(y);
+          }
+        }
+        __syncthreads();
+      };
+      Stage even = {}, odd = {};
+      fetch(even);
+      fetch(odd);
+      int group = 0, turn = 0;
+      auto step = [&]() {
+        if (++turn == turns) {
+          turn = 0;
+          ++group;
+        }
+        return group < n_groups;
+      };
+      for (;;) {
+        work(group, turn, even);
+        fetch(even);
+        if (!step()) break;
+        work(group, turn, odd);
+        fetch(odd);
+        if (!step()) break;
       }
     }
-  }
-#pragma unroll
-  for (int tile = 0; tile < TILES; ++tile)
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sums[warp][tile * 16 + g + 8 * (r >> 1)][i * 8 + 2 * t + (r & 1)] = total[tile][i][r];
-  __syncthreads();
-  for (int at = threadIdx.x; at < 16 * TILES * p.M; at += kWarps * 32) {
-    const int n = at % (16 * TILES), m = at / (16 * TILES);
-    if (n0 + n >= p.N) continue;
-    float y = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w)
-#pragma unroll
-      for (int i = kPieces - 1; i >= 0; --i) y += sums[w][n][m * kPieces + i];
-    if (p.bias) y += p.bias[n0 + n];
-    static_cast<T*>(p.y)[(int64_t)m * p.y_stride + n0 + n] = from_float<T>(y);
   }
 }
 
-template <typename T, int PARTS, int NT, int TILES>
-cudaError_t launch(const Int4Params& p, cudaStream_t stream) {
-  const unsigned grid = (unsigned)((p.N + 16 * TILES - 1) / (16 * TILES));
-  if (p.zeros)
-    matvec_kernel<T, PARTS, NT, TILES, true><<<grid, kWarps * 32, 0, stream>>>(p);
-  else
-    matvec_kernel<T, PARTS, NT, TILES, false><<<grid, kWarps * 32, 0, stream>>>(p);
+template <typename T, int PARTS, int NT, int TILES, bool WHOLE>
+cudaError_t launch_one(Int4Params& p, cudaStream_t stream) {
+  constexpr int kSums = 4 * 16 * TILES * (kWarps * (NT * 8 + 1) + kMostGroups * NT * 8);
+  static_assert(kMostX + kSums <= 227 * 1024, "more shared memory than a block can have");
+  const int block_bytes = 4 * 4 * 16 * p.M * (sizeof(T) == 4 ? 3 : 1);
+  p.pass = kMostX / block_bytes;                 // (10 to 512)
+  if (p.pass >= p.blocks)
+    p.pass = p.blocks;
+  else if (p.pass > kWarps)
+    p.pass -= p.pass % kWarps;
+  p.wk = 1;
+  while (p.wk < kWarps && (p.wk < p.pass || p.pass < p.blocks)) p.wk *= 2;
+  static bool attr_done[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  auto kernel = matvec_kernel<T, PARTS, NT, TILES, WHOLE>;
+  if (!attr_done[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostX + kSums);
+    if (e != cudaSuccess) return e;
+    attr_done[dev] = true;
+  }
+  const int64_t group = 16 * TILES * (kWarps / p.wk), groups = (p.N + group - 1) / group;
+  kernel<<<(unsigned)(groups < 148 ? groups : 148), kWarps * 32, p.pass * block_bytes + kSums, stream>>>(p);
   return cudaGetLastError();
 }
 
-// Tiles of a warp: more where that leaves two blocks an SM and more.
 template <typename T, int PARTS, int NT>
-cudaError_t launch_tiles(const Int4Params& p, cudaStream_t stream) {
-  if constexpr (NT <= 2)
-    if (p.N >= 296 * 32) return launch<T, PARTS, NT, 2>(p, stream);
-  return launch<T, PARTS, NT, 1>(p, stream);
+cudaError_t launch(Int4Params& p, cudaStream_t stream) {
+  const bool whole = p.K % 128 == 0 && p.vec_w && p.vec_x && p.vec_s;
+  return whole ? launch_one<T, PARTS, NT, NT <= 2 ? 2 : 1, true>(p, stream) : launch_one<T, PARTS, NT, 1, false>(p, stream);
 }
 
 template <typename T, int PARTS>
-cudaError_t launch_columns(const Int4Params& p, cudaStream_t stream) {
+cudaError_t launch_columns(Int4Params& p, cudaStream_t stream) {
   const int columns = p.M * (sizeof(T) == 4 ? 3 : 1);
-  if (columns <= 8) return launch_tiles<T, PARTS, 1>(p, stream);
-  if (columns <= 16) return launch_tiles<T, PARTS, 2>(p, stream);
-  if constexpr (sizeof(T) == 4) {
-    if (columns <= 24) return launch_tiles<T, PARTS, 3>(p, stream);
-    return launch_tiles<T, PARTS, 6>(p, stream);
-  }
-  return cudaErrorInvalidValue;
+  if (columns <= 8) return launch<T, PARTS, 1>(p, stream);
+  if constexpr (sizeof(T) == 4) return columns <= 24 ? launch<T, PARTS, 3>(p, stream) : launch<T, PARTS, 6>(p, stream);
+  if constexpr (sizeof(T) == 2) return launch<T, PARTS, 2>(p, stream);
 }
 
 template <typename T>
 cudaError_t launch_type(Int4Params& p, cudaStream_t stream) {
   p.vec_w = p.row_bytes % 16 == 0 && aligned_to(p.weight, 16);
   p.vec_x = (p.x_stride * (int64_t)sizeof(T)) % 16 == 0 && aligned_to(p.x, 16);
-  p.vec_s = p.groups % 4 == 0 && aligned_to(p.scales, 16) && aligned_to(p.zeros, 4);
+  p.vec_s = (p.group >= 128 || p.groups % 4 == 0) && aligned_to(p.scales, 16) && aligned_to(p.zeros, 4);
   if (p.group == 32) return launch_columns<T, 4>(p, stream);
   if (p.group == 64) return launch_columns<T, 2>(p, stream);
   return launch_columns<T, 1>(p, stream);
@@ -297,7 +379,7 @@ cudaError_t launch_matvec_int4(const void* x, const uint8_t* weight, const void*
                                void* y, const im2win_int4_shape& s, im2win_dtype dtype, cudaStream_t stream) {
   Int4Params p = {x, weight, scales, zeros, bias, y, s.x_stride, s.y_stride, s.M, s.N, s.K, s.group,
                   (int32_t)(((int64_t)s.K + s.group - 1) / s.group), (int32_t)(((int64_t)s.K + 1) / 2),
-                  (int32_t)(((int64_t)s.K + 127) / 128), 0, 0, 0};
+                  (int32_t)(((int64_t)s.K + 127) / 128), 0, 0, 0, 0, 0};
   switch (dtype) {
     case IM2WIN_F32: return launch_type<float>(p, stream);
     case IM2WIN_F16: return launch_type<__half>(p, stream);

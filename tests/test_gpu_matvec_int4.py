@@ -60,6 +60,13 @@ def test_largest_tiles(dtype):
     run(dtype, 1, 18944 + 1, 512, 128)
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("m,k", [(16, 4224), (16, 12000), (9, 9000), (1, 16384 + 64), (5, 16384)])
+def test_rows_longer_than_what_lies_in_shared_memory(dtype, m, k):
+    run(dtype, m, 50, k, 64, zeros=m % 2 == 1)
+    run(dtype, m, 148 * 32 * 9 + 5 if m == 16 and k < 5000 else 40, k, 128, zeros=False)
+
+
 def test_infinities_and_nans_stay_in_their_row_of_x():
     def edit(x, w, s, z):
         x[0, 5] = float("inf")
