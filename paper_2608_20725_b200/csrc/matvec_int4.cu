@@ -14,12 +14,16 @@
 // nibbles n0..n7 a mask gives (n0, n4), (n1, n5), (n2, n6), (n3, n7), and x is brought into that order instead.
 // fp32 rows of x are three rows of bf16 pieces each, cut off so that their sum is exact; a column of the product for each.
 //
-// A block stays on an SM and takes groups of rows in turn.  It brings x into shared memory once, as the products want it (for a batch
-// of 8, twice the bytes that 16 rows of the matrix have: fetched for each such tile it would be most of the traffic); its 16 warps
-// share a group's elements along K, each loading its next two blocks of 128 elements while it works on one, and add their sums up in
-// their order.  Measured, without zero points / with, at 6.53 TB/s: see launch_columns.
+// A block stays on an SM and takes tiles of 32 rows in turn; its 16 warps share a tile's elements along K, 128 each of 2048 at a time,
+// keep x for theirs in registers from one tile to the next, and add their sums up at the end of a tile, in their order.  The matrix
+// comes through a ring of kSlots such chunks in shared memory, row by row (bulk copies: loads to registers two blocks ahead, which share
+// the few scoreboards of a warp, reached 1.9 TB/s).  Rows of more than a pass of K (8192 elements for 8 columns of x, 2048 for more) go
+// in passes, whose sums are kept for kMostGroups tiles at a time.  Rows that do not start on 16-byte boundaries, and a K that is no
+// multiple of 128, go through registers (matvec_any_kernel).
 #include <type_traits>
 
+#include "common.cuh"
+#include "ptx_sm100.cuh"
 #include "sequence.cuh"
 
 namespace im2win {
@@ -50,7 +54,7 @@ template <> struct Mma<__half> {
     return *reinterpret_cast<const uint32_t*>(&r);
   }
   static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
@@ -62,7 +66,7 @@ template <> struct Mma<__nv_bfloat16> {
     return *reinterpret_cast<const uint32_t*>(&r);
   }
   static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
@@ -133,11 +137,12 @@ __device__ __forceinline__ void load_x(const T* row, int at, int K, bool vec, in
 }
 
 // PARTS: groups in 128 elements (1: groups of 128 and multiples, 2: of 64, 4: of 32).  NT: tiles of 8 columns of x.  TILES: of 16 rows.
-// WHOLE: K is a multiple of 128 and everything can be loaded as vectors.
-template <typename T, int PARTS, int NT, int TILES, bool WHOLE>
-__global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params p) {
+// Everything may be ragged and unaligned.
+template <typename T, int PARTS, int NT>
+__global__ void __launch_bounds__(kWarps * 32, 1) matvec_any_kernel(const Int4Params p) {
   using M16 = typename std::conditional<sizeof(T) == 4, __nv_bfloat16, T>::type;   // what the products are made of
   using MM = Mma<M16>;
+  constexpr int TILES = 1;                       // of 16 rows in a warp
   constexpr int kWords = 4 / PARTS;              // of a lane, row and group
   constexpr int kPieces = sizeof(T) == 4 ? 3 : 1;
   constexpr int kRows = 2 * TILES;               // of the matrix in a lane
@@ -199,16 +204,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
           if (row_at + r * 8 >= p.N) break;      // (rows beyond the last: whatever was there is worked on and dropped)
           const uint8_t* w = weight + (int64_t)(r * 8) * p.row_bytes;
           const int64_t at = (int64_t)(r * 8) * p.groups;
-          if (WHOLE) {
-#pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-              const Vec<uint32_t, kWords> v = *reinterpret_cast<const Vec<uint32_t, kWords>*>(w + part * (64 / PARTS));
-#pragma unroll
-              for (int i = 0; i < kWords; ++i) s.w[r][part * kWords + i] = v.v[i];
-            }
-            s.scale[r] = *reinterpret_cast<const Vec<T, PARTS>*>(scales + at);
-            if (zeros) s.zero[r] = *reinterpret_cast<const Vec<uint8_t, PARTS>*>(zeros + at);
-          } else {
 #pragma unroll
             for (int part = 0; part < PARTS; ++part) {
               const int off = block * 64 + part * (64 / PARTS) + t * (kWords * 4);
@@ -217,7 +212,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
               s.scale[r].v[part] = group_there ? scales[at + part] : from_float<T>(0.0f);
               if (zeros) s.zero[r].v[part] = group_there ? zeros[at + part] : 0;
             }
-          }
         }
       };
       float total[TILES][NT][4];
@@ -323,12 +317,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
   }
 }
 
-template <typename T, int PARTS, int NT, int TILES, bool WHOLE>
-cudaError_t launch_one(Int4Params& p, cudaStream_t stream) {
-  constexpr int kSums = 4 * 16 * TILES * (kWarps * (NT * 8 + 1) + kMostGroups * NT * 8);
+template <typename T, int PARTS, int NT>
+cudaError_t launch_any(Int4Params& p, cudaStream_t stream) {
+  constexpr int kSums = 4 * 16 * (kWarps * (NT * 8 + 1) + kMostGroups * NT * 8);
   static_assert(kMostX + kSums <= 227 * 1024, "more shared memory than a block can have");
   const int block_bytes = 4 * 4 * 16 * p.M * (sizeof(T) == 4 ? 3 : 1);
-  p.pass = kMostX / block_bytes;                 // (10 to 512)
+  p.pass = kMostX / block_bytes;                 // (20 to 512)
   if (p.pass >= p.blocks)
     p.pass = p.blocks;
   else if (p.pass > kWarps)
@@ -338,28 +332,283 @@ cudaError_t launch_one(Int4Params& p, cudaStream_t stream) {
   static bool attr_done[64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  auto kernel = matvec_kernel<T, PARTS, NT, TILES, WHOLE>;
+  auto kernel = matvec_any_kernel<T, PARTS, NT>;
   if (!attr_done[dev]) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostX + kSums);
     if (e != cudaSuccess) return e;
     attr_done[dev] = true;
   }
-  const int64_t group = 16 * TILES * (kWarps / p.wk), groups = (p.N + group - 1) / group;
+  const int64_t group = 16 * (kWarps / p.wk), groups = (p.N + group - 1) / group;
   kernel<<<(unsigned)(groups < 148 ? groups : 148), kWarps * 32, p.pass * block_bytes + kSums, stream>>>(p);
   return cudaGetLastError();
 }
 
+constexpr int kSlots = 4;
+constexpr int kTileRows = 32;                    // rows of a tile: two products high, so that what a warp does but products counts half
+constexpr int kChunkBlocks = kWarps;             // blocks of 128 elements of a chunk: one for each warp
+
+// A row of a chunk takes 1024 bytes and 64 / PARTS: the words that a warp reads at once then lie in different banks.
+template <int PARTS>
+constexpr int kRowPitch = kChunkBlocks * 64 + 64 / PARTS;
+
+template <typename T, int PARTS, int NT, int TURNS>
+__global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params p) {
+  using M16 = typename std::conditional<sizeof(T) == 4, __nv_bfloat16, T>::type;   // what the products are made of
+  using MM = Mma<M16>;
+  constexpr int kWords = 4 / PARTS;              // of a lane, row and group
+  constexpr int kPieces = sizeof(T) == 4 ? 3 : 1;
+  constexpr int kRows = kTileRows / 8;           // of a lane
+  constexpr uint32_t kSlot = kTileRows * kRowPitch<PARTS>;
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ __align__(8) uint64_t bars[2 * kSlots];           // full, empty
+  float (*sums)[kTileRows][NT * 8 + 1] = reinterpret_cast<float (*)[kTileRows][NT * 8 + 1]>(ring + kSlots * kSlot);
+  float (*kept)[kTileRows][NT * 8] = reinterpret_cast<float (*)[kTileRows][NT * 8]>(sums + kWarps);
+  const int lane = threadIdx.x & 31, warp = ptx::warp_index(), g = lane >> 2, t = lane & 3;
+  const int columns = p.M * kPieces;
+  const uint32_t ring_at = ptx::smem_u32(ring), full = ptx::smem_u32(bars), empty = ptx::smem_u32(bars + kSlots);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kSlots; ++i) {
+      ptx::mbar_init(full + i * 8, kWarps);      // a warp copies two rows each
+      ptx::mbar_init(empty + i * 8, kWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    ptx::fence_proxy_async_smem();
+  }
+  __syncthreads();
+  const int tiles = (p.N + kTileRows - 1) / kTileRows, first = blockIdx.x, mine = (tiles - first + (int)gridDim.x - 1) / (int)gridDim.x;
+  bool failed = false;
+  // Waits are for copies and warps of this block, which end by themselves.  Should one not, they give up.
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < (1u << 22) && !failed; ++i)
+      if (ptx::mbar_try_wait(bar, parity)) return;
+    failed = true;
+  };
+  uint32_t fill_slot = 0, fill_parity = 1, use_slot = 0, use_parity = 0;       // (the first wait for an empty slot passes)
+  const uint32_t words_at = g * kRowPitch<PARTS> + warp * 64 + t * (kWords * 4);
+  for (int batch = 0; batch < mine; batch += kMostGroups) {
+    const int n_tiles = min(kMostGroups, mine - batch);
+    for (int b0 = 0; b0 < p.blocks; b0 += TURNS * kChunkBlocks) {
+      const int nb = min(TURNS * kChunkBlocks, p.blocks - b0), turns = (nb + kChunkBlocks - 1) / kChunkBlocks;
+      auto first_row = [&](int tile) { return (first + (batch + tile) * (int)gridDim.x) * kTileRows; };
+      uint4 bx[TURNS][NT][4];
+#pragma unroll
+      for (int turn = 0; turn < TURNS; ++turn)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int word = 0; word < 4; ++word) {
+            const int c = i * 8 + g, b = turn * kChunkBlocks + warp;
+            uint32_t pairs[4] = {0, 0, 0, 0};
+            if (c < columns && b < nb)
+              load_x<T>(static_cast<const T*>(p.x) + (int64_t)(c / kPieces) * p.x_stride,
+                        (b0 + b) * 128 + word / kWords * (128 / PARTS) + t * (kWords * 8) + 8 * (word % kWords), p.K, true, c % kPieces, pairs);
+            bx[turn][i][word] = make_uint4(pairs[0], pairs[1], pairs[2], pairs[3]);
+          }
+      // this warp's two rows of the next chunk to be filled
+      int fill_tile = 0, fill_turn = 0;
+      const uint8_t* from = nullptr;
+      int64_t second = 0;                        // from the first of the two rows to the other
+      auto fill = [&]() {
+        if (fill_tile >= n_tiles) return;
+        if (fill_turn == 0) {
+          const int row = min(first_row(fill_tile) + 2 * warp, p.N - 1);
+          from = p.weight + (int64_t)row * p.row_bytes + (int64_t)b0 * 64;
+          second = row + 1 < p.N ? p.row_bytes : 0;
+        }
+        wait(empty + fill_slot * 8, fill_parity);
+        if (ptx::elect_one()) {
+          const uint32_t bytes = (uint32_t)min(kChunkBlocks, nb - fill_turn * kChunkBlocks) * 64;
+          const uint32_t to = ring_at + fill_slot * kSlot + 2 * warp * kRowPitch<PARTS>, bar = full + fill_slot * 8;
+          ptx::mbar_arrive_expect_tx(bar, 2 * bytes);
+          ptx::bulk_load(to, from, bytes, bar);
+          ptx::bulk_load(to + kRowPitch<PARTS>, from + second, bytes, bar);
+        }
+        __syncwarp();
+        from += kChunkBlocks * 64;
+        if (++fill_slot == kSlots) {
+          fill_slot = 0;
+          fill_parity ^= 1;
+        }
+        if (++fill_turn == turns) {
+          fill_turn = 0;
+          ++fill_tile;
+        }
+      };
+      Vec<T, PARTS> scale[kRows];
+      Vec<uint8_t, PARTS> zero[kRows];
+      const T* scales = nullptr;                 // of this lane's first row, for the next block that the warp works on
+      const uint8_t* zeros = nullptr;
+      uint32_t row_off[kRows];
+      auto fetch_scales = [&](int tile, int turn) {
+        const int b = b0 + turn * kChunkBlocks + warp;
+        if (tile >= n_tiles || turn * kChunkBlocks + warp >= nb) return;
+        const uint32_t j0 = PARTS > 1 ? b * PARTS : p.group == 128 ? b : (uint32_t)((int64_t)b * 128 / p.group);
+        if (turn == 0) {
+          const int row = min(first_row(tile) + g, p.N - 1);
+          const int64_t at = (int64_t)row * p.groups;
+          scales = static_cast<const T*>(p.scales) + at;
+          if (p.zeros) zeros = p.zeros + at;
+#pragma unroll
+          for (int r = 0; r < kRows; ++r) row_off[r] = (uint32_t)min(8 * r, p.N - 1 - row) * (uint32_t)p.groups;
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          scale[r] = *reinterpret_cast<const Vec<T, PARTS>*>(scales + (row_off[r] + j0));
+          if (p.zeros) zero[r] = *reinterpret_cast<const Vec<uint8_t, PARTS>*>(zeros + (row_off[r] + j0));
+        }
+      };
+      fetch_scales(0, 0);
+      for (int i = 0; i < kSlots - 1; ++i) fill();
+      float total[kRows / 2][NT][4];
+      for (int tile = 0; tile < n_tiles; ++tile) {
+#pragma unroll
+        for (int h = 0; h < kRows / 2; ++h)
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) total[h][i][r] = 0.0f;
+#pragma unroll
+        for (int turn = 0; turn < TURNS; ++turn) {
+          if (turn >= turns) break;
+          fill();                                // (into the slot of the chunk before)
+          wait(full + use_slot * 8, use_parity);
+          if (turn * kChunkBlocks + warp < nb) {
+            uint32_t words[kRows][4];
+            const uint8_t* at = ring + use_slot * kSlot + words_at;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+#pragma unroll
+              for (int part = 0; part < PARTS; ++part) {
+                const Vec<uint32_t, kWords> v = *reinterpret_cast<const Vec<uint32_t, kWords>*>(at + 8 * r * kRowPitch<PARTS> + part * (64 / PARTS));
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) words[r][part * kWords + w] = v.v[w];
+              }
+            float s[kRows][PARTS];
+            uint32_t z[kRows][PARTS];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+#pragma unroll
+              for (int part = 0; part < PARTS; ++part) {
+                s[r][part] = to_float(scale[r].v[part]);
+                z[r][part] = MM::kMagic + (p.zeros ? (uint32_t)(zero[r].v[part] & 15) * 0x10001u : 0x80008u);
+              }
+            if (turn + 1 < turns)
+              fetch_scales(tile, turn + 1);
+            else
+              fetch_scales(tile + 1, 0);
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+              float acc[kRows / 2][NT][4] = {};  // (products of different rows in turn: one that adds to the last waits 40 cycles for it)
+#pragma unroll
+              for (int w = 0; w < kWords; ++w)
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                  for (int h = 0; h < kRows / 2; ++h) {
+                    uint32_t a[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                      a[i] = MM::sub(((words[2 * h + (i & 1)][part * kWords + w] >> (8 * half + 4 * (i >> 1))) & 0x000f000fu) | MM::kMagic,
+                                     z[2 * h + (i & 1)][part]);
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                      const uint4 x = bx[turn][i][part * kWords + w];
+                      MM::mma(acc[h][i], a, half ? x.z : x.x, half ? x.w : x.y);
+                    }
+                  }
+#pragma unroll
+              for (int h = 0; h < kRows / 2; ++h)
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                  for (int r = 0; r < 4; ++r) total[h][i][r] = fmaf(s[2 * h + (r >> 1)][part], acc[h][i][r], total[h][i][r]);
+            }
+          } else if (turn + 1 == turns) {
+            fetch_scales(tile + 1, 0);
+          }
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(empty + use_slot * 8);
+          if (++use_slot == kSlots) {
+            use_slot = 0;
+            use_parity ^= 1;
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < kRows / 2; ++h)
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sums[warp][h * 16 + g + 8 * (r >> 1)][i * 8 + 2 * t + (r & 1)] = total[h][i][r];
+        __syncthreads();
+        const int n0 = first_row(tile);
+        const bool more = b0 + nb < p.blocks;
+        for (int at = threadIdx.x; at < kTileRows * p.M; at += kWarps * 32) {
+          const int n = at % kTileRows, m = at / kTileRows;
+          if (n0 + n >= p.N) continue;
+          float y = 0.0f;
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w)
+#pragma unroll
+            for (int i = kPieces - 1; i >= 0; --i) y += sums[w][n][m * kPieces + i];
+          if (b0 > 0) y += kept[tile][n][m];     // (this thread's own)
+          if (more) {
+            kept[tile][n][m] = y;
+          } else {
+            if (p.bias) y += p.bias[n0 + n];
+            static_cast<T*>(p.y)[(int64_t)m * p.y_stride + n0 + n] = from_float<T>(y);
+          }
+        }
+        __syncthreads();
+      }
+    }
+  }
+}
+
+template <typename T, int PARTS, int NT, int TURNS>
+cudaError_t launch_ring(const Int4Params& p, cudaStream_t stream) {
+  constexpr int kBytes = kSlots * kTileRows * kRowPitch<PARTS> + 4 * kTileRows * (kWarps * (NT * 8 + 1) + kMostGroups * NT * 8);
+  static_assert(kBytes + 1024 <= 227 * 1024, "more shared memory than a block can have");
+  static bool attr_done[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  auto kernel = matvec_kernel<T, PARTS, NT, TURNS>;
+  if (!attr_done[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e != cudaSuccess) return e;
+    attr_done[dev] = true;
+  }
+  const int64_t tiles = ((int64_t)p.N + kTileRows - 1) / kTileRows;
+  kernel<<<(unsigned)(tiles < 148 ? tiles : 148), kWarps * 32, kBytes, stream>>>(p);
+  return cudaGetLastError();
+}
+
+// Chunks of a pass by what registers hold: 64 of them x, or 32 or 48 with more columns and their sums.
 template <typename T, int PARTS, int NT>
 cudaError_t launch(Int4Params& p, cudaStream_t stream) {
-  const bool whole = p.K % 128 == 0 && p.vec_w && p.vec_x && p.vec_s;
-  return whole ? launch_one<T, PARTS, NT, NT <= 2 ? 2 : 1, true>(p, stream) : launch_one<T, PARTS, NT, 1, false>(p, stream);
+  if (!(p.K % 128 == 0 && p.vec_w && p.vec_x && p.vec_s)) return launch_any<T, PARTS, NT>(p, stream);
+  if constexpr (NT == 1) {
+    if (p.blocks <= 2 * kChunkBlocks) return launch_ring<T, PARTS, NT, 2>(p, stream);
+    return launch_ring<T, PARTS, NT, 4>(p, stream);
+  } else {
+    return launch_ring<T, PARTS, NT, 1>(p, stream);
+  }
 }
 
 template <typename T, int PARTS>
 cudaError_t launch_columns(Int4Params& p, cudaStream_t stream) {
   const int columns = p.M * (sizeof(T) == 4 ? 3 : 1);
   if (columns <= 8) return launch<T, PARTS, 1>(p, stream);
-  if constexpr (sizeof(T) == 4) return columns <= 24 ? launch<T, PARTS, 3>(p, stream) : launch<T, PARTS, 6>(p, stream);
+  if constexpr (sizeof(T) == 4) {
+    if (columns <= 24) return launch<T, PARTS, 3>(p, stream);
+    // more than eight rows of fp32: eight at a time, which reads the matrix twice
+    Int4Params rest = p;
+    p.M = 8;
+    rest.M -= 8;
+    rest.x = static_cast<const T*>(p.x) + 8 * p.x_stride;
+    rest.y = static_cast<T*>(p.y) + 8 * p.y_stride;
+    const cudaError_t e = launch<T, PARTS, 3>(p, stream);
+    return e != cudaSuccess ? e : launch_columns<T, PARTS>(rest, stream);
+  }
   if constexpr (sizeof(T) == 2) return launch<T, PARTS, 2>(p, stream);
 }
 
