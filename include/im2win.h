@@ -430,13 +430,13 @@ typedef struct {
  * `workspace`.  A max_len below the longest sequence's rows leaves results
  * undefined, but nothing outside the buffers is read or written.
  *
- * fp32 rows, single tokens and the shortest prompts run the recurrence as it
- * stands, in fp32, and so do rows of q, k or v that do not start on 16-byte
- * boundaries, dk above 128 and sizes that are no multiples of 8.  Others go by
- * chunks of 64 tokens on the tensor cores: there the weights of a chunk's
- * tokens for one another and the copy of the state that meets q are rounded
- * once to `dtype` (sums are fp32, in fp16 everything is scaled to the type's
- * range), which puts o off by about as much as its own rounding does.  The
+ * fp32 rows, dk above 128, single tokens and the shortest prompts run the
+ * recurrence as it stands, in fp32.  Others go by chunks of 64 tokens on the
+ * tensor cores: there the weights of a chunk's tokens for one another and the
+ * copy of the state that meets q are rounded once to `dtype` (sums are fp32, in
+ * fp16 everything is scaled to the type's range), which puts o off by about as
+ * much as its own rounding does; rows of q, k and v that start on 16-byte
+ * boundaries, and dk and dv of multiples of 8, are the fast ones.  The
  * states are fp32 throughout, to within a few units of their last place.  Sums
  * are in a fixed order: the same call gives the same bits.  An infinity or NaN
  * of a row reaches no row before it; where infinities of both signs meet,
@@ -453,7 +453,7 @@ im2win_status im2win_linear_attention(const void* q, const void* k, const void* 
                                       void* workspace, size_t workspace_bytes, const im2win_attention_shape* shape,
                                       im2win_dtype dtype, void* cuda_stream);
 /*
- * How a call with cu_seqlens runs such a shape with aligned rows (host-only, static storage; for reports and tests): "tokens" (the
+ * How a call with cu_seqlens runs such a shape (host-only, static storage; for reports and tests): "tokens" (the
  * recurrence), "chunks", "chunks+segments" (long sequences are cut, so that all of the GPU has work); "none" for an invalid shape.
  */
 const char* im2win_linear_attention_kernel_name(const im2win_attention_shape* shape, im2win_dtype dtype);

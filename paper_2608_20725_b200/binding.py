@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -111,10 +112,10 @@ def lib() -> ctypes.CDLL:
     L.im2win_conv_f16_nhwc.argtypes = [vp, vp, vp, P(Epilogue), vp, sz, P(Shape), vp]
     L.im2win_pack_filter_nhwc.argtypes = [vp, vp, sz, P(Shape), vp]
     L.im2win_conv_packed_nhwc.argtypes = [vp, vp, P(Epilogue), vp, sz, P(Shape), vp]
-    L.im2win_causal_conv1d.argtypes = [vp, vp, vp, vp, vp, vp, P(Sequences), P(Conv1dShape), ctypes.c_int, vp]
-    L.im2win_linear_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, P(Sequences), vp, sz, P(AttentionShape), ctypes.c_int, vp]
+    L.im2win_causal_conv1d.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp]
+    L.im2win_linear_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, ctypes.c_int, vp]
     L.im2win_linear_attention_workspace_size.argtypes = [P(AttentionShape), ctypes.c_int, P(sz)]
-    L.im2win_matvec_int4.argtypes = [vp, vp, vp, vp, vp, vp, P(Int4Shape), ctypes.c_int, vp]
+    L.im2win_matvec_int4.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp]
     for name in EXPORTS[1:]:
         getattr(L, name).restype = ctypes.c_int
     L.im2win_conv_kernel_name.restype = ctypes.c_char_p
@@ -392,6 +393,13 @@ def alloc_nhwc_buffers(shape, out_dtype: torch.dtype = torch.float32, out_layout
 # `cu_seqlens` is one token of each of `tokens` sequences (the next token of a generation).  See include/im2win.h.
 _SEQUENCE_DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
+# The structures above, as bytes: a call of one token is over in the time that a few ctypes structures take to fill (a whole call 13 us with
+# them, 10 without).
+_pack_sequences = struct.Struct("@3P").pack
+_pack_conv1d = struct.Struct("@6i2q").pack
+_pack_attention = struct.Struct("@8if5q").pack
+_pack_int4 = struct.Struct("@4i2q").pack
+
 
 def _sequence_dtype(dtype: torch.dtype) -> int:
     code = _SEQUENCE_DTYPES.get(dtype)
@@ -402,21 +410,23 @@ def _sequence_dtype(dtype: torch.dtype) -> int:
 
 def _on_current_device(*tensors) -> None:
     """The kernels are launched on the current device: tensors of another one, or of the host, are refused."""
-    device = None
+    device = -2
     for t in tensors:
-        if t is not None:
+        if t is not None and t.get_device() != device:
             at = t.get_device()
-            if at != device:
-                if at < 0:
-                    raise ValueError("tensors have to be on a CUDA device")
-                if device is not None or at != _device():
-                    raise ValueError("tensors have to be on the current device (see torch.cuda.device)")
-                device = at
+            if at < 0:
+                raise ValueError("tensors have to be on a CUDA device")
+            if device != -2 or at != _device():
+                raise ValueError("tensors have to be on the current device (see torch.cuda.device)")
+            device = at
 
 
 def _row_stride(t: torch.Tensor, inner: int, name: str) -> int:
     """Elements from a row of t to the next one: its last `inner` (1 or 2) dimensions are a row, dense; those before them count rows."""
-    shape, stride = t.shape, t.stride()
+    shape = t.shape
+    if t.is_contiguous():
+        return shape[-1] if inner == 1 else shape[-1] * shape[-2]
+    stride = t.stride()
     width = shape[-1]
     if stride[-1] != 1 and width != 1:
         raise ValueError(f"{name}: the elements of a row have to lie one behind the other")
@@ -435,7 +445,7 @@ def _row_stride(t: torch.Tensor, inner: int, name: str) -> int:
 
 
 def _take_sequences(rows, cu_seqlens, slots, resume, state, state_out):
-    """(tokens, sequences, states in a pool, pointer to im2win_sequences or None) for tensors with the leading dimensions `rows`."""
+    """(tokens, sequences, states in a pool, im2win_sequences as bytes or None) for tensors with the leading dimensions `rows`."""
     pool = 0
     if cu_seqlens is not None:
         if len(rows) != 1:
@@ -450,13 +460,15 @@ def _take_sequences(rows, cu_seqlens, slots, resume, state, state_out):
             raise ValueError("there has to be a sequence")
     if tokens >= 1 << 31:
         raise ValueError("fewer than 2^31 tokens")
-    for p in (state, state_out):
-        if p is not None:
-            if not p.is_contiguous():
-                raise ValueError("state and state_out have to be contiguous")
-            if p.shape[0] < 1 or (pool and p.shape[0] != pool):
-                raise ValueError("state and state_out have to hold as many states")
-            pool = p.shape[0]
+    if state is not None:
+        pool = state.shape[0]
+        if pool < 1 or not state.is_contiguous():
+            raise ValueError("state has to be contiguous, and to hold a state")
+    if state_out is not None and state_out is not state:
+        held = state_out.shape[0]
+        if held < 1 or not state_out.is_contiguous() or (pool and held != pool):
+            raise ValueError("state_out has to be contiguous, and to hold as many states as state")
+        pool = held
     if slots is not None:
         if slots.dtype != torch.int32 or slots.dim() != 1 or slots.numel() != sequences or not slots.is_contiguous():
             raise ValueError("slots: an int32 value for each sequence")
@@ -468,7 +480,7 @@ def _take_sequences(rows, cu_seqlens, slots, resume, state, state_out):
         raise ValueError("resume: a flag for each sequence")
     if cu_seqlens is None and slots is None and resume is None:
         return tokens, sequences, pool, None
-    return tokens, sequences, pool, ctypes.byref(Sequences(_ptr(cu_seqlens), _ptr(slots), _ptr(resume)))
+    return tokens, sequences, pool, _pack_sequences(_ptr(cu_seqlens) or 0, _ptr(slots) or 0, _ptr(resume) or 0)
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -494,14 +506,14 @@ def im2win_causal_conv1d(x, weight, y, bias=None, silu: bool = False, state=None
     if bias is not None and (bias.dtype != torch.float32 or bias.shape != (channels,) or not bias.is_contiguous()):
         raise ValueError("bias: [channels] of float32")
     for p in (state, state_out):
-        if p is not None and (p.dtype != dtype or p.shape[1:] != (taps - 1, channels)):
+        if p is not None and (p.dtype != dtype or p.dim() != 3 or p.shape[1] != taps - 1 or p.shape[2] != channels):
             raise ValueError("state and state_out: [slots, taps - 1, channels] of x's dtype")
     tokens, sequences, pool, seqs = _take_sequences(shape[:-1], cu_seqlens, slots, resume, state, state_out)
-    sizes = Conv1dShape(tokens, sequences, pool, channels, taps, 1 if silu else 0, _row_stride(x, 1, "x"), _row_stride(y, 1, "y"))
+    sizes = _pack_conv1d(tokens, sequences, pool, channels, taps, 1 if silu else 0, _row_stride(x, 1, "x"), _row_stride(y, 1, "y"))
     if taps == 1:                                            # nothing is carried
         state = state_out = None
-    code = lib().im2win_causal_conv1d(x.data_ptr(), weight.data_ptr(), _ptr(bias), y.data_ptr(), _ptr(state), _ptr(state_out), seqs,
-                                      ctypes.byref(sizes), code, _stream(stream))
+    code = (_lib or lib()).im2win_causal_conv1d(x.data_ptr(), weight.data_ptr(), _ptr(bias), y.data_ptr(), _ptr(state), _ptr(state_out), seqs,
+                                                sizes, code, _stream(stream))
     if code:
         _check(code, "im2win_causal_conv1d")
 
@@ -547,23 +559,24 @@ def im2win_linear_attention(q, k, v, log_decay, o, workspace, scale: float = 1.0
     if log_decay.dtype != torch.float32 or (gs != vs[:-1] and gs != (heads,)):
         raise ValueError("log_decay: [..., tokens, heads] or [heads] of float32")
     for p in (state, state_out):
-        if p is not None and (p.dtype != torch.float32 or p.shape[1:] != (heads, dk, dv)):
+        if p is not None and (p.dtype != torch.float32 or p.dim() != 4 or p.shape[1] != heads or p.shape[2] != dk or p.shape[3] != dv):
             raise ValueError("state and state_out: [slots, heads, dk, dv] of float32")
     if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace: contiguous, of uint8")
     tokens, sequences, pool, seqs = _take_sequences(qs[:-2], cu_seqlens, slots, resume, state, state_out)
-    strides = log_decay.stride()
-    if len(gs) == 1 or (tokens > 1 and all(n == 1 or step == 0 for n, step in zip(gs[:-1], strides))):
+    if tokens > 0 and len(gs) > 1 and log_decay.is_contiguous():
+        decay_stride = heads
+    elif len(gs) == 1 or (tokens > 1 and all(n == 1 or step == 0 for n, step in zip(gs[:-1], log_decay.stride()))):
         decay_stride = 0                                     # one decay for each head (it may be an expanded view)
-        if heads > 1 and strides[-1] != 1:
+        if heads > 1 and log_decay.stride(-1) != 1:
             raise ValueError("log_decay: the heads have to lie one behind the other")
     else:
         decay_stride = _row_stride(log_decay, 1, "log_decay")
-    sizes = AttentionShape(tokens, sequences, pool, max_len, heads, qk_heads, dk, dv, scale, _row_stride(q, 2, "q"), _row_stride(k, 2, "k"),
-                           _row_stride(v, 2, "v"), _row_stride(o, 2, "o"), decay_stride)
-    code = lib().im2win_linear_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), o.data_ptr(), _ptr(state),
-                                         _ptr(state_out), seqs, workspace.data_ptr(), workspace.nbytes, ctypes.byref(sizes),
-                                         code, _stream(stream))
+    sizes = _pack_attention(tokens, sequences, pool, max_len, heads, qk_heads, dk, dv, scale, _row_stride(q, 2, "q"), _row_stride(k, 2, "k"),
+                            _row_stride(v, 2, "v"), _row_stride(o, 2, "o"), decay_stride)
+    code = (_lib or lib()).im2win_linear_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), o.data_ptr(), _ptr(state),
+                                                   _ptr(state_out), seqs, workspace.data_ptr(), workspace.numel(), sizes, code,
+                                                   _stream(stream))
     if code:
         _check(code, "im2win_linear_attention")
 
@@ -588,9 +601,9 @@ def im2win_matvec_int4(x, weight, scales, y, group: int, zeros=None, bias=None, 
         raise ValueError("zeros: [N, ceil(K / group)] of uint8")
     if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,) or not bias.is_contiguous()):
         raise ValueError("bias: [N] of float32")
-    sizes = Int4Shape(m, n, k, group, _row_stride(x, 1, "x"), _row_stride(y, 1, "y"))
-    code = lib().im2win_matvec_int4(x.data_ptr(), weight.data_ptr(), scales.data_ptr(), _ptr(zeros), _ptr(bias), y.data_ptr(),
-                                    ctypes.byref(sizes), code, _stream(stream))
+    sizes = _pack_int4(m, n, k, group, _row_stride(x, 1, "x"), _row_stride(y, 1, "y"))
+    code = (_lib or lib()).im2win_matvec_int4(x.data_ptr(), weight.data_ptr(), scales.data_ptr(), _ptr(zeros), _ptr(bias), y.data_ptr(), sizes,
+                                              code, _stream(stream))
     if code:
         _check(code, "im2win_matvec_int4")
 

@@ -68,7 +68,7 @@ struct ChunkParams {
   Sequences seqs;
   int64_t q_stride, k_stride, v_stride, o_stride, decay_stride;
   int32_t heads, share, dk, dv, tiles, L;
-  int32_t segmented, o_by_map;           // o_by_map: rows of o start on 16-byte boundaries
+  int32_t segmented, by_map, o_by_map;   // by_map: rows of q, k and v start on 16-byte boundaries; o_by_map: those of o too
   float scale;
 };
 
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   const bool last = end == piece.rows.end;
   if (!OUT && last) return;                                    // (nothing starts behind it)
 
-  const int chunks = (end - first + kChunk - 1) / kChunk, whole = (end - first) / kChunk;
+  const int chunks = (end - first + kChunk - 1) / kChunk, whole = p.by_map ? (end - first) / kChunk : 0;
 
   const uint32_t loaded = smem_u32(bars), done = smem_u32(bars + kStages), intra_done = smem_u32(bars + kStages + 1),
                  dots_done = smem_u32(bars + kStages + 2), stored = smem_u32(bars + kStages + 3);
@@ -395,31 +395,38 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
 #pragma unroll
     for (int i = 0; i < 2; ++i) tma_load_3d(base + L::kQK + i * kPanel, &maps.v, (int)tile * kTile + i * 64, head, t0, bar);
   };
-  // The last chunk of a sequence: the workers; the rows of the next sequence, and those behind the last, as 0.
+  // The last chunk of a sequence: the workers; the rows of the next sequence, and those behind the last, as 0.  Rows that do not start
+  // on 16-byte boundaries: every chunk, an element at a time.
+  auto load_rows = [&](uint32_t to, const T* from, int64_t stride, int columns, int t0, int units) {
+    const int shift = units == 16 ? 4 : 3;
+#pragma unroll 1
+    for (int u = tid; u < kChunk * units; u += kThreads) {
+      const int r = u >> shift, cc = u & (units - 1);
+      const uint32_t at = to + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4);
+      const bool row_there = t0 + r < end;
+      if (p.by_map) {
+        const bool there = row_there && cc * 8 < columns;
+        copy16(at, from + (there ? (t0 + r) * stride + cc * 8 : 0), there);
+      } else {
+        const unsigned short* row = reinterpret_cast<const unsigned short*>(from) + (row_there ? (t0 + r) * stride : 0);
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t lo = row_there && cc * 8 + 2 * i < columns ? row[cc * 8 + 2 * i] : 0;
+          const uint32_t hi = row_there && cc * 8 + 2 * i + 1 < columns ? row[cc * 8 + 2 * i + 1] : 0;
+          w[i] = lo | hi << 16;
+        }
+        st_shared16(at, w[0], w[1], w[2], w[3]);
+      }
+    }
+  };
   auto load_part = [&](int c) {
-    const T* q = static_cast<const T*>(p.q) + (int64_t)(head / p.share) * p.dk;
-    const T* k = static_cast<const T*>(p.k) + (int64_t)(head / p.share) * p.dk;
-    const T* v = static_cast<const T*>(p.v) + (int64_t)head * p.dv + tile * kTile;
     const uint32_t base = smem + (c % kStages) * L::kStage;
     const int t0 = first + c * kChunk;
-    constexpr int kUnits = DK / 8;
-#pragma unroll 1
-    for (int u = tid; u < kChunk * kUnits; u += kThreads) {
-      const int r = u / kUnits, cc = u % kUnits;
-      const bool there = t0 + r < end && cc * 8 < p.dk;
-      const uint32_t at = (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4);
-      const int64_t t = there ? t0 + r : 0;
-      const int off = there ? cc * 8 : 0;
-      copy16(base + at, k + t * p.k_stride + off, there);
-      if (OUT) copy16(base + L::kQK + L::kV + at, q + t * p.q_stride + off, there);
-    }
-#pragma unroll 1
-    for (int u = tid; u < kChunk * 16; u += kThreads) {
-      const int r = u / 16, cc = u % 16;
-      const bool there = t0 + r < end && (int)tile * kTile + cc * 8 < p.dv;
-      const uint32_t at = (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4);
-      copy16(base + L::kQK + at, v + (there ? (t0 + r) * p.v_stride + cc * 8 : 0), there);
-    }
+    const int64_t qk_at = (int64_t)(head / p.share) * p.dk;
+    load_rows(base, static_cast<const T*>(p.k) + qk_at, p.k_stride, p.dk, t0, DK / 8);
+    if (OUT) load_rows(base + L::kQK + L::kV, static_cast<const T*>(p.q) + qk_at, p.q_stride, p.dk, t0, DK / 8);
+    load_rows(base + L::kQK, static_cast<const T*>(p.v) + (int64_t)head * p.dv + tile * kTile, p.v_stride, p.dv - (int)tile * kTile, t0, 16);
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   auto load_decay = [&](int c, float& g0, float& g1) {
@@ -463,7 +470,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       for (; c < chunks; ++c) {
         const uint32_t kt = smem + (c % kStages) * L::kStage, vt = kt + L::kQK, qt = vt + L::kV;
         const uint32_t pieces = smem + L::kPiecesAt + (OUT ? 0 : (c & 1) * L::kPieces);
-        if (c == whole) {
+        if (c >= whole) {
           sync_all();
           tc_fence_after();
           if (OUT && elect_one()) issue_dots(c);
@@ -524,7 +531,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       if (chunks > 1) all_decay += chunk_decays(g0, g1, p.scale, E, decays[1]);
       for (int c = 0; c < chunks; ++c) {
         if (c + 2 < chunks) load_decay(c + 2, g0, g1);
-        if (c == whole) sync_all();
+        if (c >= whole) sync_all();
         if (K::kScaled) sync_all();
         if (sync_or(false)) break;
         const bool odd_0 = *(volatile uint32_t*)&odd_values[c & 3] != 0;
@@ -713,7 +720,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
     for (int c = 0; c < chunks; ++c) {
       const uint32_t kt = smem + (c % kStages) * L::kStage, vt = kt + L::kQK;
       const uint32_t pieces = smem + L::kPiecesAt + (OUT ? 0 : (c & 1) * L::kPieces);
-      if (c == whole) {                                        // the last one, in part
+      if (c >= whole) {                                        // the last one, in part
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         fence_proxy_async_smem();
         sync_all();
@@ -728,7 +735,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
 
       constexpr int kUnits = DK / 8, kVectors = kChunk * kUnits / kThreads;
       uint4 kk[kVectors];
-      if (c == whole || !OUT) look_at_v(c);
+      if (c >= whole || !OUT) look_at_v(c);
 #pragma unroll
       for (int m = 0; m < kVectors; ++m) {
         const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
@@ -815,7 +822,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       if (failed) break;
       tc_fence_after();
       const bool odd_0 = *(volatile uint32_t*)&odd_values[c & 3] != 0;     // (set before the barrier: every thread sees the same)
-      if (c + 1 == whole && whole < chunks) load_part(whole);
+      if (c + 1 >= whole && c + 1 < chunks) load_part(c + 1);
       if (OUT) {
         if (c > 0 && !odd_1) {                                 // (an odd chunk's has been stored)
           uint32_t y[kTokens / 2];
@@ -895,41 +902,41 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   if (warp == 0) tmem_dealloc(tmem, L::kColumns);
 }
 
-// The starting state of every segment of a sequence that is cut, in the place of what it adds: a thread has four numbers of a head's
-// state (dk * dv is a multiple of 64) and runs over the segments.
+// The starting state of every segment of a sequence that is cut, in the place of what it adds: a thread has W numbers of a head's
+// state and runs over the segments.
+template <int W>
 __global__ void __launch_bounds__(256) segment_states_kernel(const ChunkParams p, const float* pool, int32_t blocks) {
   const uint32_t rest = blockIdx.x / (uint32_t)blocks;
   const int head = (int)(rest % (uint32_t)p.heads), b = (int)(rest / (uint32_t)p.heads);
   const SequenceRows rows = rows_of(p.seqs, b);
   const int32_t len = rows.end - rows.begin;
   const int slot = slot_of(p.seqs, b);
-  const int64_t size = (int64_t)p.dk * p.dv, e = ((int64_t)(blockIdx.x % (uint32_t)blocks) * 256 + threadIdx.x) * 4;
+  using V = Vec<float, W>;
+  const int64_t size = (int64_t)p.dk * p.dv, e = ((int64_t)(blockIdx.x % (uint32_t)blocks) * 256 + threadIdx.x) * W;
   if (len <= p.L || slot < 0 || e >= size) return;
   const int32_t n = (len + p.L - 1) / p.L;
   // (as find_piece numbers them)
   const int64_t id0 = p.seqs.cu ? (int64_t)(rows.begin / p.L) + b : (int64_t)b * n;
-  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  if (pool && resumes(p.seqs, b)) s = *reinterpret_cast<const float4*>(pool + ((int64_t)slot * p.heads + head) * size + e);
+  V s = {};
+  if (pool && resumes(p.seqs, b)) s = *reinterpret_cast<const V*>(pool + ((int64_t)slot * p.heads + head) * size + e);
   constexpr int kAhead = 4;
   for (int i0 = 0; i0 < n; i0 += kAhead) {
-    float4 added[kAhead];
+    V added[kAhead];
     float2 total[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (i0 + i + 1 >= n) break;                              // (the last one's sum is not made)
       const int64_t at = (id0 + i0 + i) * p.heads + head;
-      added[i] = *reinterpret_cast<const float4*>(p.added + at * size + e);
+      added[i] = *reinterpret_cast<const V*>(p.added + at * size + e);
       total[i] = p.totals[at];
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (i0 + i >= n) break;
-      *reinterpret_cast<float4*>(p.added + ((id0 + i0 + i) * p.heads + head) * size + e) = s;
+      *reinterpret_cast<V*>(p.added + ((id0 + i0 + i) * p.heads + head) * size + e) = s;
       if (i0 + i + 1 >= n) break;
-      s.x = carry(s.x, total[i], added[i].x);
-      s.y = carry(s.y, total[i], added[i].y);
-      s.z = carry(s.z, total[i], added[i].z);
-      s.w = carry(s.w, total[i], added[i].w);
+#pragma unroll
+      for (int u = 0; u < W; ++u) s.v[u] = carry(s.v[u], total[i], added[i].v[u]);
     }
   }
 }
@@ -949,8 +956,9 @@ struct ChunkPlan {
 ChunkPlan plan_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool has_cu) {
   ChunkPlan c = {};
   const int64_t longest = has_cu ? (s.max_len > 0 ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens) : s.tokens / s.sequences;
-  // Not the shortest prompts: up to 16 tokens the recurrence, which waits for nothing but its loads, is as fast.
-  c.eligible = dtype != IM2WIN_F32 && s.dk <= 128 && s.dk % 8 == 0 && s.dv % 8 == 0 && longest > 16;
+  // Not the shortest prompts: up to 16 tokens the recurrence, which waits for nothing but its loads, is as fast.  (Rows that start anywhere
+  // come an element at a time: 13 prompts of 9001 tokens, 24 heads of 61 x 123, 253 us, where 64 x 128 takes 120 and its recurrence 2600.)
+  c.eligible = dtype != IM2WIN_F32 && s.dk <= 128 && longest > 16;
   if (!c.eligible) return c;
   c.tiles = (s.dv + kTile - 1) / kTile;
   const int64_t blocks = (int64_t)s.heads * c.tiles;
@@ -1032,10 +1040,14 @@ cudaError_t launch_all(const ChunkMaps& maps, ChunkParams& p, const ChunkPlan& p
     pieces = plan.segments;
     cudaError_t e = launch<T, DK, false>(maps, p, pieces, stream);
     if (e != cudaSuccess) return e;
-    const int32_t blocks = (int32_t)(((int64_t)p.dk * p.dv + 1023) / 1024);
+    const int32_t width = p.dk * p.dv % 4 == 0 ? 4 : 1;
+    const int32_t blocks = (int32_t)(((int64_t)p.dk * p.dv + 256 * width - 1) / (256 * width));
     const int64_t grid = (int64_t)blocks * p.heads * a.shape.sequences;
     if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
-    segment_states_kernel<<<(unsigned)grid, 256, 0, stream>>>(p, a.state_in, blocks);
+    if (width == 4)
+      segment_states_kernel<4><<<(unsigned)grid, 256, 0, stream>>>(p, a.state_in, blocks);
+    else
+      segment_states_kernel<1><<<(unsigned)grid, 256, 0, stream>>>(p, a.state_in, blocks);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     p.segmented = 1;
@@ -1058,16 +1070,18 @@ cudaError_t launch_attention_chunks(const AttentionArgs& a, cudaStream_t stream)
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   ChunkParams p = {a.q, a.k, a.v, a.decay, a.o, a.state_in, a.state_out, reinterpret_cast<float*>(ws + plan.added_off),
                    reinterpret_cast<float2*>(ws + plan.totals_off), reinterpret_cast<uint32_t*>(ws), a.seqs, s.q_stride, s.k_stride,
-                   s.v_stride, s.o_stride, s.decay_stride, s.heads, s.heads / s.qk_heads, s.dk, s.dv, plan.tiles, plan.L, 0, 0, s.scale};
+                   s.v_stride, s.o_stride, s.decay_stride, s.heads, s.heads / s.qk_heads, s.dk, s.dv, plan.tiles, plan.L, 0, 0, 0, s.scale};
   const EncodeTiledFn fn = get_encode_fn();
   if (!fn) return cudaErrorNotSupported;
-  p.o_by_map = s.o_stride % 8 == 0 && aligned_to(a.o, 16);
+  p.by_map = s.dk % 8 == 0 && s.dv % 8 == 0 && s.q_stride % 8 == 0 && s.k_stride % 8 == 0 && s.v_stride % 8 == 0 && aligned_to(a.q, 16) &&
+             aligned_to(a.k, 16) && aligned_to(a.v, 16);
+  p.o_by_map = p.by_map && s.o_stride % 8 == 0 && aligned_to(a.o, 16);
   ChunkMaps maps = {};
   const CUtensorMapSwizzle rows = CU_TENSOR_MAP_SWIZZLE_128B;
-  if (!encode(fn, &maps.q, a.dtype, a.q, s.tokens, s.qk_heads, s.dk, s.q_stride, 64, rows) ||
+  if (p.by_map && (!encode(fn, &maps.q, a.dtype, a.q, s.tokens, s.qk_heads, s.dk, s.q_stride, 64, rows) ||
       !encode(fn, &maps.k, a.dtype, a.k, s.tokens, s.qk_heads, s.dk, s.k_stride, 64, rows) ||
       !encode(fn, &maps.v, a.dtype, a.v, s.tokens, s.heads, s.dv, s.v_stride, 64, rows) ||
-      (p.o_by_map && !encode(fn, &maps.o, a.dtype, a.o, s.tokens, s.heads, s.dv, s.o_stride, kTile, CU_TENSOR_MAP_SWIZZLE_NONE)))
+      (p.o_by_map && !encode(fn, &maps.o, a.dtype, a.o, s.tokens, s.heads, s.dv, s.o_stride, kTile, CU_TENSOR_MAP_SWIZZLE_NONE))))
     return cudaErrorInvalidValue;
   if (a.dtype == IM2WIN_F16)
     return s.dk <= 64 ? launch_all<__half, 64>(maps, p, plan, a, stream) : launch_all<__half, 128>(maps, p, plan, a, stream);

@@ -4,16 +4,17 @@
 //
 // Every row is read once and written once and meets 2K operations an element, so the memory bounds it.  A thread owns VEC
 // neighbouring channels (16 bytes) and walks down the rows of a piece of a sequence with the window's K-1 last rows in registers:
-// each element is loaded once, plus K-1 rows at the start of a piece.  Rows are loaded in batches of kBatch, so that as many loads
-// are under way.  The thread that has a sequence's first piece reads its old state and writes the new one, which is the old
+// each element is loaded once, plus K-1 rows at the start of a piece.  The next kBatch rows are loaded while kBatch are worked on.  The thread that has a sequence's first piece reads its old state and writes the new one, which is the old
 // state's rows and the last rows of x: no other thread touches either, so that both may lie in the same buffer.
+#include <type_traits>
+
 #include "sequence.cuh"
 
 namespace im2win {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kBatch = 8;                // rows whose loads are in flight together
+constexpr int kBatch = 4;                // rows that are loaded while the kBatch before them are worked on
 
 struct Conv1dParams {
   const void* x;
@@ -27,20 +28,77 @@ struct Conv1dParams {
   int32_t channels, blocks, L;           // blocks: of kThreads * VEC channels; L: rows of a piece
 };
 
+// Two floats whose sums and products go through the paired fp32 instructions: a row of 8 channels, 4 taps and the activation otherwise
+// takes 12 instructions an element, which the memory does not hide.
+struct Pair {
+  uint64_t v;
+};
+__device__ __forceinline__ Pair pair(float a, float b) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(a), "f"(b));
+  return p;
+}
+__device__ __forceinline__ void split(Pair p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
 // z / (1 + exp(-z)).  fp32: as it stands.  16-bit results: exp2 and the reciprocal of the special function units, whose errors of
-// 2^-22 (and 2^-24 |z| from the product) are far below the result's 2^-9 or 2^-12; the exact forms take 20 more instructions, which
-// the memory does not hide.
+// 2^-22 (and 2^-24 |z| from the product) are far below the result's 2^-9 or 2^-12.
 template <typename T>
-__device__ __forceinline__ float silu_of(float z) {
-  if constexpr (sizeof(T) == 4) return z / (1.0f + expf(-z));
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  return z * r;
+__device__ __forceinline__ Pair silu_of(Pair z) {
+  float a, b;
+  if constexpr (sizeof(T) == 4) {
+    split(z, a, b);
+    return pair(a / (1.0f + expf(-a)), b / (1.0f + expf(-b)));
+  } else {
+    constexpr float kScale = -1.4426950408889634f;
+    split(mul2(z, pair(kScale, kScale)), a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    split(add2(pair(a, b), pair(1.0f, 1.0f)), a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return mul2(z, pair(a, b));
+  }
+}
+
+// Two neighbouring elements as floats and back.
+template <typename T> __device__ __forceinline__ Pair load2(const T* at) { return pair(to_float(at[0]), to_float(at[1])); }
+template <> __device__ __forceinline__ Pair load2<__nv_bfloat16>(const __nv_bfloat16* at) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(at);
+  return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <typename T> __device__ __forceinline__ void store2(T* at, Pair p) {
+  float a, b;
+  split(p, a, b);
+  if constexpr (sizeof(T) == 4) {
+    at[0] = a;
+    at[1] = b;
+  } else if constexpr (sizeof(T) == 2) {
+    uint32_t w;
+    if constexpr (std::is_same<T, __half>::value)
+      asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
+    else
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
+    *reinterpret_cast<uint32_t*>(at) = w;
+  }
 }
 
 template <typename T, int VEC, int TAPS, bool SILU>
-__global__ void __launch_bounds__(kThreads) conv1d_kernel(const Conv1dParams p) {
+__global__ void __launch_bounds__(kThreads, 4) conv1d_kernel(const Conv1dParams p) {
   using V = Vec<T, VEC>;
   const uint32_t id = blockIdx.x / (uint32_t)p.blocks;
   const Piece piece = find_piece(p.seqs, id, p.L);
@@ -70,17 +128,25 @@ __global__ void __launch_bounds__(kThreads) conv1d_kernel(const Conv1dParams p) 
     weights[i] = *reinterpret_cast<const V*>(static_cast<const T*>(p.weight) + (int64_t)c * TAPS + i * VEC);
 #pragma unroll
   for (int i = 0; i < TAPS - 1; ++i) raw[i] = row(first - (TAPS - 1) + i);
-  float w[TAPS][VEC], b[VEC], win[TAPS][VEC];
+  constexpr int kPairs = (VEC + 1) / 2;          // (a single channel: a pair whose second is not used)
+  Pair w[TAPS][kPairs], b[kPairs], win[TAPS][kPairs];
+  auto elements = [&](const V& v, int j) {
+    if constexpr (VEC > 1) return load2<T>(v.v + 2 * j);
+    return pair(to_float(v.v[0]), 0.0f);
+  };
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) {
+  for (int j = 0; j < kPairs; ++j) {
 #pragma unroll
-    for (int i = 0; i < TAPS; ++i) w[i][j] = to_float(weights[(j * TAPS + i) / VEC].v[(j * TAPS + i) % VEC]);
-    b[j] = p.bias ? __ldg(p.bias + c + j) : 0.0f;
+    for (int i = 0; i < TAPS; ++i) {
+      auto weight = [&](int c) { return c < VEC ? to_float(weights[(c * TAPS + i) / VEC].v[(c * TAPS + i) % VEC]) : 0.0f; };
+      w[i][j] = pair(weight(2 * j), weight(2 * j + 1));
+    }
+    b[j] = pair(p.bias ? __ldg(p.bias + c + 2 * j) : 0.0f, p.bias && VEC > 1 ? __ldg(p.bias + c + 2 * j + 1) : 0.0f);
   }
 #pragma unroll
   for (int i = 0; i < TAPS - 1; ++i)
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) win[i][j] = to_float(raw[i].v[j]);
+    for (int j = 0; j < kPairs; ++j) win[i][j] = elements(raw[i], j);
 
   if (TAPS > 1 && p.state_out && leads) {
     T* out = static_cast<T*>(p.state_out) + state_at;
@@ -90,30 +156,50 @@ __global__ void __launch_bounds__(kThreads) conv1d_kernel(const Conv1dParams p) 
     for (int i = 0; i < TAPS - 1; ++i) *reinterpret_cast<V*>(out + (int64_t)i * p.channels) = raw[i];
   }
 
-  T* y = static_cast<T*>(p.y) + c;
-  for (int t0 = first; t0 < end; t0 += kBatch) {
-    V in[kBatch];
+  const T* x_next = x + (int64_t)first * p.x_stride;
+  T* y_next = static_cast<T*>(p.y) + c + (int64_t)first * p.y_stride;
+  auto work = [&](const V& in) {                 // a row: its sums, the window one further
+    V out;
 #pragma unroll
-    for (int r = 0; r < kBatch; ++r)
-      if (t0 + r < end) in[r] = *reinterpret_cast<const V*>(x + (int64_t)(t0 + r) * p.x_stride);
+    for (int j = 0; j < kPairs; ++j) {
+      win[TAPS - 1][j] = elements(in, j);
+      Pair z = b[j];
 #pragma unroll
-    for (int r = 0; r < kBatch; ++r) {
-      if (t0 + r >= end) break;
-      V out;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        win[TAPS - 1][j] = to_float(in[r].v[j]);
-        float z = b[j];
-#pragma unroll
-        for (int i = 0; i < TAPS; ++i) z = fmaf(w[i][j], win[i][j], z);
-        if (SILU) z = silu_of<T>(z);
-        out.v[j] = from_float<T>(z);
-#pragma unroll
-        for (int i = 0; i < TAPS - 1; ++i) win[i][j] = win[i + 1][j];
+      for (int i = 0; i < TAPS; ++i) z = fma2(w[i][j], win[i][j], z);
+      if (SILU) z = silu_of<T>(z);
+      if constexpr (VEC > 1) {
+        store2<T>(out.v + 2 * j, z);
+      } else {
+        float first_of, second_of;
+        split(z, first_of, second_of);
+        out.v[0] = from_float<T>(first_of);
       }
-      *reinterpret_cast<V*>(y + (int64_t)(t0 + r) * p.y_stride) = out;
+#pragma unroll
+      for (int i = 0; i < TAPS - 1; ++i) win[i][j] = win[i + 1][j];
     }
+    *reinterpret_cast<V*>(y_next) = out;
+    y_next += p.y_stride;
+  };
+  int left = end - first;
+  if (left >= kBatch) {
+    V next[kBatch];
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r, x_next += p.x_stride) next[r] = *reinterpret_cast<const V*>(x_next);
+    for (; left >= 2 * kBatch; left -= kBatch) {
+      V in[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) in[r] = next[r];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r, x_next += p.x_stride) next[r] = *reinterpret_cast<const V*>(x_next);
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) work(in[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) work(next[r]);
+    left -= kBatch;
   }
+#pragma unroll 1
+  for (; left > 0; --left, x_next += p.x_stride) work(*reinterpret_cast<const V*>(x_next));
 }
 
 template <typename T, int VEC, int TAPS>
@@ -128,8 +214,13 @@ cudaError_t launch(const Conv1dParams& p, int64_t grid, bool silu, cudaStream_t 
 template <typename T, int VEC>
 cudaError_t launch_taps(Conv1dParams& p, const im2win_conv1d_shape& s, cudaStream_t stream) {
   p.blocks = (s.channels + kThreads * VEC - 1) / (kThreads * VEC);
-  p.L = 32;
-  const int64_t grid = number_of_pieces(s.tokens, s.sequences, p.L, p.seqs.cu != nullptr) * p.blocks;
+  // Rows of a piece: 64, fewer where that leaves under seven blocks an SM (16384 tokens of 4096 channels, bf16, with the activation:
+  // 80, 71, 73, 84 us with 16, 32, 64, 128 at three blocks an SM, 63 and 61 with 32 and 64 at four).
+  int64_t grid = 0;
+  for (p.L = 64;; p.L /= 2) {
+    grid = number_of_pieces(s.tokens, s.sequences, p.L, p.seqs.cu != nullptr) * p.blocks;
+    if (grid >= 1000 || p.L == 16) break;
+  }
   if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
   const bool silu = s.silu != 0;
   switch (s.taps) {

@@ -124,7 +124,7 @@ struct AttentionArgs {
   im2win_dtype dtype;
 };
 cudaError_t launch_attention_tokens(const AttentionArgs& a, cudaStream_t stream);
-// Whether the sizes go by chunks (q, k and v have to start their rows on 16-byte boundaries too), and the workspace that takes.
+// Whether the sizes go by chunks, and the workspace that takes.
 bool attention_by_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool has_cu, size_t* workspace_bytes, bool* segmented);
 cudaError_t launch_attention_chunks(const AttentionArgs& a, cudaStream_t stream);
 cudaError_t launch_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros, const float* bias,

@@ -110,10 +110,8 @@ im2win_status im2win_linear_attention(const void* q, const void* k, const void* 
   bool segmented;
   const bool chunks = attention_by_chunks(*shape, dtype, a.seqs.cu != nullptr, &need, &segmented);
   if (workspace_bytes < need) return IM2WIN_ERR_WORKSPACE_TOO_SMALL;
-  const bool rows_aligned = shape->q_stride % 8 == 0 && shape->k_stride % 8 == 0 && shape->v_stride % 8 == 0 && aligned_to(q, 16) &&
-                            aligned_to(k, 16) && aligned_to(v, 16);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  return from_launch(chunks && rows_aligned ? launch_attention_chunks(a, stream) : launch_attention_tokens(a, stream));
+  return from_launch(chunks ? launch_attention_chunks(a, stream) : launch_attention_tokens(a, stream));
 }
 
 im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros,

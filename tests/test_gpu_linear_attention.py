@@ -116,6 +116,44 @@ def test_shared_heads_and_strides(dtype):
     run(dtype, [40, 90], 6, 2, 64, 128, pitch=5)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("segments", [1, 2, 3, 7])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 128), (37, 51), (128, 200)])
+def test_sequences_in_segments(dtype, segments, dk, dv, monkeypatch):
+    """Long sequences cut into any number of segments, beside short and empty ones, their states in place."""
+    monkeypatch.setenv("IM2WIN_SEGMENTS", str(segments))
+    run(dtype, [460, 3, 0, 200, 64, 129], 2, 1, dk, dv, tail=5, resume=[1, 1, 0, 0, 1, 1], in_place=True, slots=[3, 1, 0, 7, 2, 5], pool=8,
+        kernel="chunks" if segments == 1 else "chunks+segments")
+    run(dtype, [300, 300], 1, 1, dk, dv, mode="dense", decay="heads")
+
+
+def test_a_decay_that_empties_the_state_in_the_middle_of_segments(monkeypatch):
+    monkeypatch.setenv("IM2WIN_SEGMENTS", "4")
+    def edit(q, k, v, g, st):
+        g[100] = -math.inf
+        g[64 * 4 + 5] = -500.0
+        g[300:310] = -60.0
+    for dtype in ("f16", "bf16"):
+        run(dtype, [512], 2, 2, 64, 64, edit=edit)
+
+
+def test_large_and_small_values_in_fp16():
+    """States beyond the type's range and far below its smallest normal number."""
+    def large(q, k, v, g, st):
+        k.mul_(200)
+        v.mul_(300)
+        q.mul_(1e-2)
+        st.mul_(1e6)
+        g.mul_(0.1)
+    def small(q, k, v, g, st):
+        k.mul_(1e-3)
+        v.mul_(1e-3)
+        st.mul_(1e-7)
+        q.mul_(100)
+    run("f16", [150, 40], 2, 2, 64, 64, edit=large, scale=1e-6)
+    run("f16", [150, 40], 2, 2, 64, 64, edit=small, scale=1e3)
+
+
 def test_empty_calls_move_states():
     run("bf16", [0, 0, 0], 2, 2, 64, 64, resume=[1, 0, 1])
     run("f32", [0, 0], 1, 1, 64, 64, mode="dense")

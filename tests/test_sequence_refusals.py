@@ -147,3 +147,11 @@ def matvec(x=A, weight=A, scales=A, zeros=None, bias=None, y=A, dtype=binding.BF
 ], ids=str)
 def test_matvec_refuses(status, call):
     assert matvec(**call) == status
+
+
+def test_structures_and_their_bytes_agree():
+    for structure, pack, values in ((binding.Sequences, binding._pack_sequences, (A, 2 * A, 3 * A)),
+                                    (binding.Conv1dShape, binding._pack_conv1d, tuple(range(1, 9))),
+                                    (binding.AttentionShape, binding._pack_attention, (1, 2, 3, 4, 5, 6, 7, 8, 0.5, 9, 10, 11, 12, 13)),
+                                    (binding.Int4Shape, binding._pack_int4, tuple(range(1, 7)))):
+        assert bytes(structure(*values)) == pack(*values)
