@@ -90,6 +90,15 @@ def test_without_states(mode):
     run("f16", n, 40, 3, state=False, mode=mode, slots=[0, 5, -2, 1, 3])
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("taps", [1, 2, 4, 7, 8])
+@pytest.mark.parametrize("channels", [33, 2048])
+def test_single_tokens_of_many_sequences(dtype, taps, channels):
+    b = 301
+    slots = [(7 * i) % 320 if i % 5 else -1 for i in range(b)]
+    run(dtype, [1] * b, channels, taps, mode="step", slots=slots, pool=320, in_place=True, resume=[i % 3 != 1 for i in range(b)])
+
+
 def test_more_sequences_than_a_block_has_threads():
     run("f32", [i % 5 for i in range(700)], 8, 3, tail=1)
 
