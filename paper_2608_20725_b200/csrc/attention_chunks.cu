@@ -23,6 +23,12 @@
 // behind a strong decay.  A product of a masked 0, or of a piece that is 0 or has the other sign, with an infinity of v is a NaN: a
 // chunk whose k or v hold any has its intra part made again from the terms j <= i alone, and what it adds to the state from fp32 products.
 //
+// What bounds it: a chunk of 64 tokens (128 x 128, bf16) takes 2.5 us of an SM; its 64 KB take 1.5 us of an SM's part of the memory's
+// bandwidth and its products 0.7 us of the tensor cores.  The rest is the workers' instructions (pieces of k, S, P, o: half of the issue slots)
+// and what they wait for each other: pieces and S of the next chunk cannot start before this one's products are done.  One sequence of 16384
+// tokens, 32 heads of 128 x 128: 296 us (83 at 6.53 TB/s for rows read and written once), of which the segments' own sums are 100;
+// 13 sequences of 9001 tokens, 24 heads of 64 x 128, fp16: 117 (22).
+//
 // Long sequences are cut into segments of several chunks where there are too few heads and sequences for the GPU: one launch sums up
 // what each segment adds to a zero state, a second one runs over the segments of a sequence and leaves each one's starting state, and
 // the main one then has all segments at once.
@@ -1022,28 +1028,31 @@ cudaError_t launch(const ChunkMaps& maps, const ChunkParams& p, int64_t pieces, 
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!attr_done[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<T, DK, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
+    cudaError_t e = cudaFuncSetAttribute(chunk_kernel<T, DK, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
     if (e != cudaSuccess) return e;
+    // A build whose blocks start with fewer registers than the warpgroups ask for later would wait for them without end: not launched.
+    cudaFuncAttributes built;
+    e = cudaFuncGetAttributes(&built, chunk_kernel<T, DK, OUT>);
+    if (e != cudaSuccess) return e;
+    if (built.numRegs * kAllThreads < kThreads * kWorkerRegisters + (kAllThreads - kThreads) * kHelperRegisters) return cudaErrorNotSupported;
     attr_done[dev] = true;
   }
-  const int64_t grid = pieces * p.heads * p.tiles;
-  if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
+  const int64_t grid = pieces * p.heads * p.tiles;             // (launch_all has seen that it fits)
   chunk_kernel<T, DK, OUT><<<(unsigned)grid, kAllThreads, kBytes, stream>>>(maps, p);
   return cudaGetLastError();
 }
 
 template <typename T, int DK>
 cudaError_t launch_all(const ChunkMaps& maps, ChunkParams& p, const ChunkPlan& plan, const AttentionArgs& a, cudaStream_t stream) {
+  const int64_t pieces = plan.segments ? plan.segments : number_of_pieces(a.shape.tokens, a.shape.sequences, p.L, a.seqs.cu != nullptr);
+  const int32_t width = p.dk * p.dv % 4 == 0 ? 4 : 1;
+  const int32_t blocks = (int32_t)(((int64_t)p.dk * p.dv + 256 * width - 1) / (256 * width));
+  const int64_t grid = (int64_t)blocks * p.heads * a.shape.sequences, most = (int64_t)1 << 31;
+  if (pieces * p.heads * p.tiles >= most || (plan.segments && grid >= most)) return cudaErrorInvalidConfiguration;
   if (cudaMemsetAsync(p.status, 0, kStatusBytes, stream) != cudaSuccess) return cudaErrorUnknown;
-  int64_t pieces = number_of_pieces(a.shape.tokens, a.shape.sequences, p.L, a.seqs.cu != nullptr);
   if (plan.segments) {
-    pieces = plan.segments;
     cudaError_t e = launch<T, DK, false>(maps, p, pieces, stream);
     if (e != cudaSuccess) return e;
-    const int32_t width = p.dk * p.dv % 4 == 0 ? 4 : 1;
-    const int32_t blocks = (int32_t)(((int64_t)p.dk * p.dv + 256 * width - 1) / (256 * width));
-    const int64_t grid = (int64_t)blocks * p.heads * a.shape.sequences;
-    if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
     if (width == 4)
       segment_states_kernel<4><<<(unsigned)grid, 256, 0, stream>>>(p, a.state_in, blocks);
     else

@@ -6,6 +6,9 @@
 // w*R.. of S, a lane VEC neighbouring columns of each.  For one token the state, read and written, is all the traffic there is,
 // and every thread has its R loads under way at once.  o is the sum over the warps' rows, through shared memory, in their order.
 //
+// One token of each of 128 sequences, 32 heads of 128 x 128: 93 us, 5.7 TB/s of states (81 at the measured 6.53).  Prompts run here in
+// fp32 and with dk above 128: 0.4 us a token (412 tokens of heads of 48 x 80), 0.7 (128 x 128), the latency of a token's loads, sums and barrier.
+//
 // exp(g) as a float is off by up to 2^-25 of itself, the same way at every token of a head whose decay is constant: after n tokens n
 // times as much.  Decays near 1, which remember many tokens, are therefore applied as S + S (exp(g) - 1), whose error is that of the
 // sum, and over more than one token what each sum rounds off is kept and added to the next (against 64 bits, 412 tokens, decays of

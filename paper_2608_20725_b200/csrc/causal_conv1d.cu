@@ -6,6 +6,10 @@
 // neighbouring channels (16 bytes) and walks down the rows of a piece of a sequence with the window's K-1 last rows in registers:
 // each element is loaded once, plus K-1 rows at the start of a piece.  The next kBatch rows are loaded while kBatch are worked on.  The thread that has a sequence's first piece reads its old state and writes the new one, which is the old
 // state's rows and the last rows of x: no other thread touches either, so that both may lie in the same buffer.
+//
+// 16384 tokens of 4096 channels, bf16, 4 taps, activation: 60 us, 4.5 TB/s (41 us at the measured 6.53 TB/s; 54 without the
+// activation).  An element then takes 8 instructions and two of the special function units, which makes 28 and 31 us of the SMs'
+// time: what is over the memory's time is what of the three does not overlap.
 #include <type_traits>
 
 #include "sequence.cuh"

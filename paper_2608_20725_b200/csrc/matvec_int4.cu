@@ -2,12 +2,13 @@
 //
 //   y[m][n] = bias[n] + sum_groups s[n][j] * sum_{k in group j} (w[n][k] - z[n][j]) x[m][k].
 //
-// The matrix is read once, half a byte a weight, which bounds it for up to 16 rows.  At the memory's rate a lane of an SM has
-// under three instructions for each weight; one multiply-add a weight and row would take most of them already, so the products run
-// on mma.sync (16 rows of the matrix x 8 columns of x x 16 terms): what is left is 10 to 12 instructions for eight weights to make
-// them 16-bit numbers.  w - z lies in -15..15, which both 16-bit types hold exactly, and so are the products; a group's sum comes out
-// of the accumulators in fp32 and meets its scale there.  (tcgen05 wants its 128 rows of weights in shared or tensor memory: for
-// 8 columns that would be more work than the products.)
+// The matrix is read once, half a byte a weight, which should bound it for up to 16 rows.  The products run on mma.sync (16 rows of the
+// matrix x 8 columns of x x 16 terms): w - z lies in -15..15, which both 16-bit types hold exactly, and so are the products; a group's
+// sum comes out of the accumulators in fp32 and meets its scale there.  Making the 16-bit numbers takes 11 instructions for eight weights.
+// What bounds it now: a quarter of an SM makes one such product in some 64 cycles (its pipe then reads 50 % busy), 60 us for
+// 28672 x 8192, whose 117 MB the ring below alone brings in 26 (18 at the measured bandwidth): 62 us with groups of 128, 80 with 64, 97 with 32,
+// 84 with 64 and zero points, 8 rows or 1.  Products by paired fp32 multiply-adds were slower from one row on (80, 127, 224 us for 1,
+// 2, 4 rows).
 //
 // The order of the terms of a product is free as long as both operands agree.  Lane (g = lane/4, t = lane%4) holds rows g and g+8 of
 // a tile of the matrix and the t-th of four equal parts of a group's elements, so that it loads neighbouring bytes; of a word's eight
@@ -16,8 +17,8 @@
 //
 // A block stays on an SM and takes tiles of 32 rows in turn; its 16 warps share a tile's elements along K, 128 each of 2048 at a time,
 // keep x for theirs in registers from one tile to the next, and add their sums up at the end of a tile, in their order.  The matrix
-// comes through a ring of kSlots such chunks in shared memory, row by row (bulk copies: loads to registers two blocks ahead, which share
-// the few scoreboards of a warp, reached 1.9 TB/s).  Rows of more than a pass of K (8192 elements for 8 columns of x, 2048 for more) go
+// comes through a ring of kSlots such chunks in shared memory, row by row (bulk copies; loads to registers two blocks ahead took 100 us in
+// the place of 84).  Rows of more than a pass of K (8192 elements for 8 columns of x, 2048 for more) go
 // in passes, whose sums are kept for kMostGroups tiles at a time.  Rows that do not start on 16-byte boundaries, and a K that is no
 // multiple of 128, go through registers (matvec_any_kernel).
 #include <type_traits>
