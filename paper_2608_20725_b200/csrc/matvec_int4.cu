@@ -5,21 +5,23 @@
 // The matrix is read once, half a byte a weight, which should bound it for up to 16 rows.  The products run on mma.sync (16 rows of the
 // matrix x 8 columns of x x 16 terms): w - z lies in -15..15, which both 16-bit types hold exactly, and so are the products; a group's
 // sum comes out of the accumulators in fp32 and meets its scale there.  Making the 16-bit numbers takes 11 instructions for eight weights.
-// What bounds it now: a quarter of an SM makes one such product in some 64 cycles (its pipe then reads 50 % busy), 60 us for
-// 28672 x 8192, whose 117 MB the ring below alone brings in 26 (18 at the measured bandwidth): 62 us with groups of 128, 80 with 64, 97 with 32,
-// 84 with 64 and zero points, 8 rows or 1.  Products by paired fp32 multiply-adds were slower from one row on (80, 127, 224 us for 1,
-// 2, 4 rows).
+// What bounds it now: the instructions around the products (making the numbers, scales, sums), which take half of the issue slots, and
+// what they wait for.  28672 x 8192 (76 us by itself with groups of 64, zero points, 8 rows; all these between events around the call,
+// 6 more), whose 117 MB the ring below alone brings in 26 us (18 at the measured bandwidth): 59 us with groups
+// of 128, 96 with 32, 82 with 64 and zero points, 8 rows; 64 there with scales that are not loaded.  The products themselves are hidden: a
+// quarter of an SM makes one in 9 cycles, and without them the times are the same.  Paired fp32 multiply-adds in their place were slower
+// from one row on (80, 127, 224 us for 1, 2, 4 rows).
 //
 // The order of the terms of a product is free as long as both operands agree.  Lane (g = lane/4, t = lane%4) holds rows g and g+8 of
 // a tile of the matrix and the t-th of four equal parts of a group's elements, so that it loads neighbouring bytes; of a word's eight
 // nibbles n0..n7 a mask gives (n0, n4), (n1, n5), (n2, n6), (n3, n7), and x is brought into that order instead.
 // fp32 rows of x are three rows of bf16 pieces each, cut off so that their sum is exact; a column of the product for each.
 //
-// A block stays on an SM and takes tiles of 32 rows in turn; its 16 warps share a tile's elements along K, 128 each of 2048 at a time,
-// keep x for theirs in registers from one tile to the next, and add their sums up at the end of a tile, in their order.  The matrix
+// A block stays on an SM and takes its part of the rows, in tiles of 32; its 16 warps share a tile's elements along K, 128 each of 2048
+// at a time, keep x for theirs in registers from one tile to the next, and add their sums up at the end of a tile, in their order.  The matrix
 // comes through a ring of kSlots such chunks in shared memory, row by row (bulk copies; loads to registers two blocks ahead took 100 us in
-// the place of 84).  Rows of more than a pass of K (8192 elements for 8 columns of x, 2048 for more) go
-// in passes, whose sums are kept for kMostGroups tiles at a time.  Rows that do not start on 16-byte boundaries, and a K that is no
+// the place of 84).  Rows of more than a pass of K (4096 elements for 8 columns of x, 2048 for more columns or for groups of 32:
+// what registers hold; 8192 spilled, 90 us in the place of 82) go in passes, whose sums are kept for kMostGroups tiles at a time.  Rows that do not start on 16-byte boundaries, and a K that is no
 // multiple of 128, go through registers (matvec_any_kernel).
 #include <type_traits>
 
@@ -31,8 +33,8 @@ namespace im2win {
 namespace {
 
 constexpr int kWarps = 16;
-constexpr int kMostX = 128 * 1024;                     // shared memory for x; longer rows go in passes over K,
-constexpr int kMostGroups = 8;                         // whose sums are kept for so many groups of rows at a time
+constexpr int kMostX = 128 * 1024;                     // shared memory for x of matvec_any_kernel; longer rows go in passes over K,
+constexpr int kMostGroups = 8;                         // whose sums are kept for so many tiles or groups of rows at a time
 
 struct Int4Params {
   const void* x;
@@ -137,7 +139,7 @@ __device__ __forceinline__ void load_x(const T* row, int at, int K, bool vec, in
   }
 }
 
-// PARTS: groups in 128 elements (1: groups of 128 and multiples, 2: of 64, 4: of 32).  NT: tiles of 8 columns of x.  TILES: of 16 rows.
+// PARTS: groups in 128 elements (1: groups of 128 and multiples, 2: of 64, 4: of 32).  NT: tiles of 8 columns of x.
 // Everything may be ragged and unaligned.
 template <typename T, int PARTS, int NT>
 __global__ void __launch_bounds__(kWarps * 32, 1) matvec_any_kernel(const Int4Params p) {
@@ -376,7 +378,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
     ptx::fence_proxy_async_smem();
   }
   __syncthreads();
-  const int tiles = (p.N + kTileRows - 1) / kTileRows, first = blockIdx.x, mine = (tiles - first + (int)gridDim.x - 1) / (int)gridDim.x;
+  // the block's rows: 16 at a time, of which every block has as many as the others or one more
+  const int units = (p.N + 15) / 16, unit = (int)((int64_t)units * blockIdx.x / gridDim.x);
+  const int first = unit * 16, last = min((int)((int64_t)units * (blockIdx.x + 1) / gridDim.x) * 16, p.N);
+  const int mine = (last - first + kTileRows - 1) / kTileRows;
   bool failed = false;
   // Waits are for copies and warps of this block, which end by themselves.  Should one not, they give up.
   auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -390,7 +395,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
     const int n_tiles = min(kMostGroups, mine - batch);
     for (int b0 = 0; b0 < p.blocks; b0 += TURNS * kChunkBlocks) {
       const int nb = min(TURNS * kChunkBlocks, p.blocks - b0), turns = (nb + kChunkBlocks - 1) / kChunkBlocks;
-      auto first_row = [&](int tile) { return (first + (batch + tile) * (int)gridDim.x) * kTileRows; };
+      auto first_row = [&](int tile) { return first + (batch + tile) * kTileRows; };
       uint4 bx[TURNS][NT][4];
 #pragma unroll
       for (int turn = 0; turn < TURNS; ++turn)
@@ -435,9 +440,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
           ++fill_tile;
         }
       };
-      Vec<T, PARTS> scale[kRows];
-      Vec<uint8_t, PARTS> zero[kRows];
-      const T* scales = nullptr;                 // of this lane's first row, for the next block that the warp works on
+      Vec<T, PARTS> scale[TURNS][kRows];         // fetched a tile ahead
+      Vec<uint8_t, PARTS> zero[TURNS][kRows];
+      const T* scales = nullptr;                 // of this lane's first row of the tile that is fetched
       const uint8_t* zeros = nullptr;
       uint32_t row_off[kRows];
       auto fetch_scales = [&](int tile, int turn) {
@@ -454,12 +459,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
         }
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-          scale[r] = *reinterpret_cast<const Vec<T, PARTS>*>(scales + (row_off[r] + j0));
-          if (p.zeros) zero[r] = *reinterpret_cast<const Vec<uint8_t, PARTS>*>(zeros + (row_off[r] + j0));
+          scale[turn][r] = *reinterpret_cast<const Vec<T, PARTS>*>(scales + (row_off[r] + j0));
+          if (p.zeros) zero[turn][r] = *reinterpret_cast<const Vec<uint8_t, PARTS>*>(zeros + (row_off[r] + j0));
         }
       };
-      fetch_scales(0, 0);
-      for (int i = 0; i < kSlots - 1; ++i) fill();
+#pragma unroll
+      for (int turn = 0; turn < TURNS; ++turn) fetch_scales(0, turn);
+      // A slot is filled again a chunk after the one it held is done with, so that no warp waits for the slowest at every chunk; short
+      // runs need no slot twice and start with all they have.
+      const int ahead = n_tiles * turns < kSlots ? kSlots - 1 : kSlots - 2;
+      for (int i = 0; i < ahead; ++i) fill();
       float total[kRows / 2][NT][4];
       for (int tile = 0; tile < n_tiles; ++tile) {
 #pragma unroll
@@ -471,7 +480,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
 #pragma unroll
         for (int turn = 0; turn < TURNS; ++turn) {
           if (turn >= turns) break;
-          fill();                                // (into the slot of the chunk before)
+          fill();
           wait(full + use_slot * 8, use_parity);
           if (turn * kChunkBlocks + warp < nb) {
             uint32_t words[kRows][4];
@@ -490,42 +499,44 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
             for (int r = 0; r < kRows; ++r)
 #pragma unroll
               for (int part = 0; part < PARTS; ++part) {
-                s[r][part] = to_float(scale[r].v[part]);
-                z[r][part] = MM::kMagic + (p.zeros ? (uint32_t)(zero[r].v[part] & 15) * 0x10001u : 0x80008u);
+                s[r][part] = to_float(scale[turn][r].v[part]);
+                z[r][part] = MM::kMagic + (p.zeros ? (uint32_t)(zero[turn][r].v[part] & 15) * 0x10001u : 0x80008u);
               }
-            if (turn + 1 < turns)
-              fetch_scales(tile, turn + 1);
-            else
-              fetch_scales(tile + 1, 0);
+            fetch_scales(tile + 1, turn);
+            auto products = [&](auto high) {     // of 16 or 32 rows
+              constexpr int H = decltype(high)::value;
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-              float acc[kRows / 2][NT][4] = {};  // (products of different rows in turn: one that adds to the last waits 40 cycles for it)
+              for (int part = 0; part < PARTS; ++part) {
+                float acc[H][NT][4] = {};  // (products of different rows in turn: one that adds to the last waits 40 cycles for it)
 #pragma unroll
-              for (int w = 0; w < kWords; ++w)
+                for (int w = 0; w < kWords; ++w)
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
+                  for (int half = 0; half < 2; ++half)
 #pragma unroll
-                  for (int h = 0; h < kRows / 2; ++h) {
-                    uint32_t a[4];
+                    for (int h = 0; h < H; ++h) {
+                      uint32_t a[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                      a[i] = MM::sub(((words[2 * h + (i & 1)][part * kWords + w] >> (8 * half + 4 * (i >> 1))) & 0x000f000fu) | MM::kMagic,
-                                     z[2 * h + (i & 1)][part]);
+                      for (int i = 0; i < 4; ++i)
+                        a[i] = MM::sub(((words[2 * h + (i & 1)][part * kWords + w] >> (8 * half + 4 * (i >> 1))) & 0x000f000fu) | MM::kMagic,
+                                       z[2 * h + (i & 1)][part]);
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-                      const uint4 x = bx[turn][i][part * kWords + w];
-                      MM::mma(acc[h][i], a, half ? x.z : x.x, half ? x.w : x.y);
+                      for (int i = 0; i < NT; ++i) {
+                        const uint4 x = bx[turn][i][part * kWords + w];
+                        MM::mma(acc[h][i], a, half ? x.z : x.x, half ? x.w : x.y);
+                      }
                     }
-                  }
 #pragma unroll
-              for (int h = 0; h < kRows / 2; ++h)
+                for (int h = 0; h < H; ++h)
 #pragma unroll
-                for (int i = 0; i < NT; ++i)
+                  for (int i = 0; i < NT; ++i)
 #pragma unroll
-                  for (int r = 0; r < 4; ++r) total[h][i][r] = fmaf(s[2 * h + (r >> 1)][part], acc[h][i][r], total[h][i][r]);
-            }
-          } else if (turn + 1 == turns) {
-            fetch_scales(tile + 1, 0);
+                    for (int r = 0; r < 4; ++r) total[h][i][r] = fmaf(s[2 * h + (r >> 1)][part], acc[h][i][r], total[h][i][r]);
+              }
+            };
+            if (last - first_row(tile) > 16)
+              products(std::integral_constant<int, 2>());
+            else
+              products(std::integral_constant<int, 1>());
           }
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(empty + use_slot * 8);
@@ -545,7 +556,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
         const bool more = b0 + nb < p.blocks;
         for (int at = threadIdx.x; at < kTileRows * p.M; at += kWarps * 32) {
           const int n = at % kTileRows, m = at / kTileRows;
-          if (n0 + n >= p.N) continue;
+          if (n0 + n >= last) continue;
           float y = 0.0f;
 #pragma unroll
           for (int w = 0; w < kWarps; ++w)
@@ -578,21 +589,16 @@ cudaError_t launch_ring(const Int4Params& p, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     attr_done[dev] = true;
   }
-  const int64_t tiles = ((int64_t)p.N + kTileRows - 1) / kTileRows;
-  kernel<<<(unsigned)(tiles < 148 ? tiles : 148), kWarps * 32, kBytes, stream>>>(p);
+  const int64_t units = ((int64_t)p.N + 15) / 16;
+  kernel<<<(unsigned)(units < 148 ? units : 148), kWarps * 32, kBytes, stream>>>(p);
   return cudaGetLastError();
 }
 
-// Chunks of a pass by what registers hold: 64 of them x, or 32 or 48 with more columns and their sums.
+// Chunks of a pass by what registers hold: 32 of them x, or 16 to 48 with smaller groups or more columns and their sums.
 template <typename T, int PARTS, int NT>
 cudaError_t launch(Int4Params& p, cudaStream_t stream) {
   if (!(p.K % 128 == 0 && p.vec_w && p.vec_x && p.vec_s)) return launch_any<T, PARTS, NT>(p, stream);
-  if constexpr (NT == 1) {
-    if (p.blocks <= 2 * kChunkBlocks) return launch_ring<T, PARTS, NT, 2>(p, stream);
-    return launch_ring<T, PARTS, NT, 4>(p, stream);
-  } else {
-    return launch_ring<T, PARTS, NT, 1>(p, stream);
-  }
+  return launch_ring<T, PARTS, NT, NT == 1 && PARTS < 4 ? 2 : 1>(p, stream);
 }
 
 template <typename T, int PARTS>

@@ -67,6 +67,13 @@ def test_rows_longer_than_what_lies_in_shared_memory(dtype, m, k):
     run(dtype, m, 148 * 32 * 9 + 5 if m == 16 and k < 5000 else 40, k, 128, zeros=False)
 
 
+@pytest.mark.parametrize("dtype,group", [("f16", 64), ("bf16", 32), ("bf16", 128), ("f32", 64)])
+def test_parts_of_the_rows_that_differ_over_several_passes(dtype, group):
+    # blocks of an SM with an odd and an even number of 16 rows, the last one cut off; passes of up to 4096 elements, the last one shorter
+    run(dtype, 2, 148 * 16 * 3 + 5 * 16 + 3, 4096 + 5 * 128, group, zeros=group != 32)
+    run(dtype, 1, 148 * 16 * 17 + 16 + 5, 4096 + 2 * 128, group, zeros=group == 32)
+
+
 def test_infinities_and_nans_stay_in_their_row_of_x():
     def edit(x, w, s, z):
         x[0, 5] = float("inf")
