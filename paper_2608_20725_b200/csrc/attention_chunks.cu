@@ -12,8 +12,8 @@
 //   intra^T [dv][64 tokens] = v^T x P,  P_ij = exp(G_i - G_j) (q_i . k_j)
 //
 // v^T and the weighted k are read as they lie, rows of tokens, as operands whose 64 elements of a row are innermost along M or N
-// (transposed by the descriptor); the 64 x 64 products q . k, of which half are needed, are made by the warps (mma.sync) and stay in
-// registers until they are weighted and masked.
+// (transposed by the descriptor); the 64 x 64 products q . k are one more (64 rows: by the warps
+// they would take issue slots, which are short) and come to registers to be weighted and masked.
 //
 // What is rounded to 16 bits: P and the copy of S that meets q, once each, as the result o is; their errors and o's own rounding are of
 // one size and independent.  The weighted k are not: the state is carried from call to call in fp32 and has to stay fp32, so they go

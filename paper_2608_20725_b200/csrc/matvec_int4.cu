@@ -6,10 +6,10 @@
 // matrix x 8 columns of x x 16 terms): w - z lies in -15..15, which both 16-bit types hold exactly, and so are the products; a group's
 // sum comes out of the accumulators in fp32 and meets its scale there.  Making the 16-bit numbers takes 11 instructions for eight weights.
 // What bounds it now: the instructions around the products (making the numbers, scales, sums), which take half of the issue slots, and
-// what they wait for.  28672 x 8192 (76 us by itself with groups of 64, zero points, 8 rows; all these between events around the call,
-// 6 more), whose 117 MB the ring below alone brings in 26 us (18 at the measured bandwidth): 59 us with groups
-// of 128, 96 with 32, 82 with 64 and zero points, 8 rows; 64 there with scales that are not loaded.  The products themselves are hidden: a
-// quarter of an SM makes one in 9 cycles, and without them the times are the same.  Paired fp32 multiply-adds in their place were slower
+// what they wait for.  28672 x 8192, whose 117 MB the ring below alone brings in 26 us (18 at the measured bandwidth): 76 us with groups
+// of 64, zero points, 8 rows.  Between events around the call, which counts some 6 us more: 59 us with groups of 128, 96 with 32, 82 with
+// 64 and zero points, 64 there with scales that are not loaded.  The products themselves are hidden: a quarter of an SM makes one in 9
+// cycles, and without them the times are the same.  Paired fp32 multiply-adds in their place were slower
 // from one row on (80, 127, 224 us for 1, 2, 4 rows).
 //
 // The order of the terms of a product is free as long as both operands agree.  Lane (g = lane/4, t = lane%4) holds rows g and g+8 of
