@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
   const int first = unit * 16, last = min((int)((int64_t)units * (blockIdx.x + 1) / gridDim.x) * 16, p.N);
   const int mine = (last - first + kTileRows - 1) / kTileRows;
   bool failed = false;
-  // Waits are for copies and warps of this block, which end by themselves.  Should one not, they give up.
+  // Waits are for copies and warps of this block, which end by themselves.  Should one not, they give up, and y is NaN.
   auto wait = [&](uint32_t bar, uint32_t parity) {
     for (uint32_t i = 0; i < (1u << 22) && !failed; ++i)
       if (ptx::mbar_try_wait(bar, parity)) return;
@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
 #pragma unroll
           for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sums[warp][h * 16 + g + 8 * (r >> 1)][i * 8 + 2 * t + (r & 1)] = total[h][i][r];
+            for (int r = 0; r < 4; ++r) sums[warp][h * 16 + g + 8 * (r >> 1)][i * 8 + 2 * t + (r & 1)] = failed ? __int_as_float(0x7fffffff) : total[h][i][r];
         __syncthreads();
         const int n0 = first_row(tile);
         const bool more = b0 + nb < p.blocks;
