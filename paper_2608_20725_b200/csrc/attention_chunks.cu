@@ -18,7 +18,7 @@
 // What is rounded to 16 bits: P and the copy of S that meets q, once each, as the result o is; their errors and o's own rounding are of
 // one size and independent.  The weighted k are not: the state is carried from call to call in fp32 and has to stay fp32, so they go
 // through the tensor cores as pieces whose sum is the fp32 product to 2^-22 (three of bf16, cut off exactly; two of fp16).  fp16 has no
-// room for large or small numbers: S, P and the weighted k are brought to 2^13 by a power of two for each chunk.
+// room for large or small numbers: S, P and the weighted k are brought to 2^13 by a power of two for each chunk, of their largest.
 // log_decay is summed in 64 bits, differences are split into whole and fractional powers of two, so that no cancellation is left
 // behind a strong decay.  A product of a masked 0, or of a piece that is 0 or has the other sign, with an infinity of v is a NaN: a
 // chunk whose k or v hold any has its intra part made again from the terms j <= i alone, and what it adds to the state from fp32 products.
@@ -747,24 +747,32 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         const int u = tid + m * kThreads, r = u / kUnits, cc = u % kUnits;
         kk[m] = ld_shared16(kt + (cc / 8) * kPanel + r * 128 + (((cc % 8) ^ (r & 7)) << 4));
       }
-      uint32_t top = 0;
+      uint32_t tops[kVectors], top = 0;
 #pragma unroll
-      for (int m = 0; m < kVectors; ++m) top = K::largest(K::largest(K::largest(K::largest(top, kk[m].x), kk[m].y), kk[m].z), kk[m].w);
+      for (int m = 0; m < kVectors; ++m) {
+        tops[m] = K::largest(K::largest(K::largest(K::largest(0, kk[m].x), kk[m].y), kk[m].z), kk[m].w);
+        top = K::largest(top, tops[m]);
+      }
       const bool odd_k = K::odd(top);
       if (odd_k) odd_values[c & 3] = 1;
       float scale_k = 1.0f, scale_s = 1.0f, scale_p = 1.0f;
       if (K::kScaled) {
-        if (odd_k) {                                           // the largest of the others
-          top = 0;
+        // The largest of the weighted k: the weights of tokens far from the chunk's end are far from 1, below it or, where decays grow, above.
+        uint32_t km = 0;
 #pragma unroll
-          for (int m = 0; m < kVectors; ++m)
+        for (int m = 0; m < kVectors; ++m) {
+          uint32_t t = tops[m];
+          if (odd_k) {                                         // (of the finite ones)
+            t = 0;
 #pragma unroll
             for (uint32_t w : {kk[m].x, kk[m].y, kk[m].z, kk[m].w}) {
-              if ((w & 0x7c00u) != 0x7c00u) top = __vmaxu2(top, w & 0x7fffu);
-              if ((w & 0x7c000000u) != 0x7c000000u) top = __vmaxu2(top, w & 0x7fff0000u);
+              if ((w & 0x7c00u) != 0x7c00u) t = __vmaxu2(t, w & 0x7fffu);
+              if ((w & 0x7c000000u) != 0x7c000000u) t = __vmaxu2(t, w & 0x7fff0000u);
             }
+          }
+          km = max(km, finite_bits(fmaxf(K::low(t), K::high(t)) * decays[c & 3].to_end[(tid + m * kThreads) / kUnits]));
         }
-        raise_max(&largest[c & 3][0], max(finite_bits(K::low(top)), finite_bits(K::high(top))));
+        raise_max(&largest[c & 3][0], km);
         if (OUT) {
           float sm = 0.0f;
 #pragma unroll
