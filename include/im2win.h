@@ -439,10 +439,14 @@ typedef struct {
  * fp16 everything is scaled to the type's range), which puts o off by about as
  * much as its own rounding does; rows of q, k and v that start on 16-byte
  * boundaries, and dk and dv of multiples of 8, are the fast ones.  The
- * states are fp32 throughout, to within a few units of their last place.  Sums
- * are in a fixed order: the same call gives the same bits.  An infinity or NaN
- * of a row reaches no row before it; where infinities of both signs meet,
- * whether that gives an infinity or a NaN depends on the order of sums.
+ * states are fp32 throughout, to within a few units of the last place of the
+ * magnitudes that add up to an element; in fp16 what 64 tokens add is off by up
+ * to 2^-62 of their largest element of k, decayed up to the last of them, for
+ * every v it meets besides (an element that only far weaker tokens feed shows
+ * it).  Sums are in a fixed order: the same call gives the same bits.  An
+ * infinity or NaN of a row reaches no row before it; where infinities of both
+ * signs meet, whether that gives an infinity or a NaN depends on the order of
+ * sums.
  *
  * `workspace` needs the bytes of im2win_linear_attention_workspace_size; it
  * starts with a status block as a convolution's scratch does (cleared by the

@@ -17,8 +17,9 @@
 //
 // What is rounded to 16 bits: P and the copy of S that meets q, once each, as the result o is; their errors and o's own rounding are of
 // one size and independent.  The weighted k are not: the state is carried from call to call in fp32 and has to stay fp32, so they go
-// through the tensor cores as pieces whose sum is the fp32 product to 2^-22 (three of bf16, cut off exactly; two of fp16).  fp16 has no
-// room for large or small numbers: S, P and the weighted k are brought to 2^13 by a power of two for each chunk, of their largest.
+// through the tensor cores as three pieces whose sum is the fp32 product (of bf16: cut off; of fp16: each 2^12 times what it stands for
+// beside the one before, which the sums of the products undo as they go; off by 2^-62 of a chunk's largest).  fp16 has no room for large or
+// small numbers: S, P and the weighted k are brought to 2^13 by a power of two for each chunk, of their largest.
 // log_decay is summed in 64 bits, differences are split into whole and fractional powers of two, so that no cancellation is left
 // behind a strong decay.  A product of a masked 0, or of a piece that is 0 or has the other sign, with an infinity of v is a NaN: a
 // chunk whose k or v hold any has its intra part made again from the terms j <= i alone, and what it adds to the state from fp32 products.
@@ -86,6 +87,7 @@ struct alignas(64) ChunkMaps {
 template <typename T> struct Kind;
 template <> struct Kind<__nv_bfloat16> {
   static constexpr int kPieces = 3;
+  static constexpr int kPieceBits = 0;
   static constexpr bool kScaled = false;
   static constexpr uint32_t kFormats = (1u << 7) | (1u << 10);
   // The larger magnitudes, two at once; a NaN is larger than anything.
@@ -112,7 +114,8 @@ template <> struct Kind<__nv_bfloat16> {
   }
 };
 template <> struct Kind<__half> {
-  static constexpr int kPieces = 2;
+  static constexpr int kPieces = 3;
+  static constexpr int kPieceBits = 12;                        // a piece is that many bits above what it stands for, beside the one before
   static constexpr bool kScaled = true;
   static constexpr uint32_t kFormats = 0;
   static __device__ __forceinline__ uint32_t largest(uint32_t a, uint32_t b) {
@@ -128,11 +131,14 @@ template <> struct Kind<__half> {
   }
   static __device__ __forceinline__ float low(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xffffu))); }
   static __device__ __forceinline__ float high(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
-  // Two numbers as pieces: rounded, and the rest rounded (22 bits).
-  static __device__ __forceinline__ void split(float a, float b, uint32_t (&piece)[2]) {
+  // Two numbers below 2^14 as pieces: rounded, 2^12 times the rest rounded (at most half of the 8 that are a last place there, times
+  // 2^12: 2^14 again), and that once more: exact down to 2^-25, off by at most 2^-49 below.
+  static __device__ __forceinline__ void split(float a, float b, uint32_t (&piece)[3]) {
+    constexpr float kUp = (float)(1 << kPieceBits);
     piece[0] = pack(a, b);
-    const float a1 = a - low(piece[0]), b1 = b - high(piece[0]);
+    const float a1 = (a - low(piece[0])) * kUp, b1 = (b - high(piece[0])) * kUp;
     piece[1] = pack(a1, b1);
+    piece[2] = pack((a1 - low(piece[1])) * kUp, (b1 - high(piece[1])) * kUp);
   }
 };
 
@@ -172,6 +178,19 @@ __device__ __forceinline__ void umma_f16_ta(uint32_t tmem_d, uint32_t tmem_a, ui
       "setp.ne.b32 p, %5, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
       ::"r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// The same from descriptors, added to D times 2^-DOWN.
+template <int DOWN>
+__device__ __forceinline__ void umma_f16_onto_scaled(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc) {
+  static_assert(DOWN >= 0 && DOWN <= 15, "");
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %2};\n\t"
+      "mov.b64 db, {%3, %4};\n\t"
+      "setp.eq.b32 p, 0, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p, %6;\n\t}"
+      ::"r"(tmem_d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "n"(DOWN)
       : "memory");
 }
 // Descriptor halves of an operand whose rows of 64 elements (128 bytes, 128-byte swizzle) run along M or N: panels of 64 of them
@@ -502,10 +521,15 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
 #pragma unroll
           for (int n = K::kPieces - 1; n >= 0; --n)            // the smallest pieces first
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-              umma_f16_ab(tmem + L::kAdded + (OUT ? 0 : (c & 1) * DK), desc_lo_mn(vt + ks * 2048), kDescHi,
-                          desc_lo_mn(pieces + n * L::kQK + ks * 2048), kDescHi, K::kFormats | kAlongM | kAlongN | instr_desc_f16(128, DK),
-                          n < K::kPieces - 1 || ks > 0);
+            for (int ks = 0; ks < 4; ++ks) {
+              const uint32_t to = tmem + L::kAdded + (OUT ? 0 : (c & 1) * DK), a = desc_lo_mn(vt + ks * 2048),
+                             b = desc_lo_mn(pieces + n * L::kQK + ks * 2048);
+              constexpr uint32_t kDesc = K::kFormats | kAlongM | kAlongN | instr_desc_f16(128, DK);
+              if (K::kPieceBits > 0 && ks == 0 && n < K::kPieces - 1)
+                umma_f16_onto_scaled<K::kPieceBits>(to, a, kDescHi, b, kDescHi, kDesc);
+              else
+                umma_f16_ab(to, a, kDescHi, b, kDescHi, kDesc, n < K::kPieces - 1 || ks > 0);
+            }
           umma_commit(done + (OUT ? 0 : (c & 1) * 8));
           if (OUT) {
 #pragma unroll
