@@ -19,7 +19,7 @@
 // one size and independent.  The weighted k are not: the state is carried from call to call in fp32 and has to stay fp32, so they go
 // through the tensor cores as three pieces whose sum is the fp32 product (of bf16: cut off; of fp16: each 2^12 times what it stands for
 // beside the one before, which the sums of the products undo as they go; off by 2^-62 of a chunk's largest).  fp16 has no room for large or
-// small numbers: S, P and the weighted k are brought to 2^13 by a power of two for each chunk, of their largest.
+// small numbers: S, the weighted k and each row of P are brought to 2^13 by a power of two for each chunk, of their largest.
 // log_decay is summed in 64 bits, differences are split into whole and fractional powers of two, so that no cancellation is left
 // behind a strong decay.  A product of a masked 0, or of a piece that is 0 or has the other sign, with an infinity of v is a NaN: a
 // chunk whose k or v hold any has its intra part made again from the terms j <= i alone, and what it adds to the state from fp32 products.
@@ -217,8 +217,9 @@ struct alignas(16) Decays {
 __device__ __forceinline__ float scale_for(uint32_t bits) {
   const int e = (int)(bits >> 23);
   if (e == 0) return 1.0f;
-  return __uint_as_float((uint32_t)min(max(127 + 13 - (e - 127), 1), 254) << 23);
+  return __uint_as_float((uint32_t)min(max(127 + 13 - (e - 127), 1), 253) << 23);
 }
+__device__ __forceinline__ float unscale_for(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }     // its reciprocal
 __device__ __forceinline__ uint32_t finite_bits(float x) {
   const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
   return b < 0x7f800000u ? b : 0u;
@@ -377,7 +378,10 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   extern __shared__ uint8_t dynamic_smem[];
   __shared__ Decays decays[4];
   __shared__ __align__(8) uint64_t bars[kStages + 4];          // stages loaded; added done (two), intra, q . k done, o stored
-  __shared__ uint32_t tmem_base_at, abort_flag, odd_values[4], largest[4][3];
+  __shared__ uint32_t tmem_base_at, abort_flag, odd_values[4], largest[4][2];    // largest: of the weighted k, of S
+  // fp16: the exponents of the largest of each row of P, a byte for each quarter of its columns, and what undoes the row's scale
+  __shared__ __align__(16) uint32_t row_exponents[K::kScaled ? 2 : 1][kChunk];
+  __shared__ __align__(16) float row_unscale[K::kScaled ? 2 : 1][kChunk];
   const uint32_t smem = (smem_u32(dynamic_smem) + 1023u) & ~1023u;
   const int warp = warp_index(), lane = threadIdx.x & 31, tid = threadIdx.x;
   const uint32_t tile = blockIdx.x % (uint32_t)p.tiles, rest = blockIdx.x / (uint32_t)p.tiles;
@@ -399,11 +403,12 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   if (tid == 0) {
     for (int i = 0; i < kStages + 4; ++i) mbar_init(smem_u32(bars + i), 1);
     abort_flag = 0;
-    for (int i = 0; i < 12; ++i) largest[i / 3][i % 3] = 0;
+    for (int i = 0; i < 8; ++i) largest[i / 2][i % 2] = 0;
     for (int i = 0; i < 4; ++i) odd_values[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async_smem();
   }
+  if (K::kScaled && tid < 2 * kChunk) row_exponents[tid / kChunk][tid % kChunk] = 0;     // (as the quarters above the diagonal stay)
   if (OUT && tid < kPanel / 16) st_shared16(smem + L::kPAt + tid * 16, 0, 0, 0, 0);      // (above the diagonal it stays 0)
   auto wait = [&](uint32_t bar, uint32_t phase) { return wait_for(bar, phase & 1, &abort_flag, p.status); };
 
@@ -578,8 +583,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         __syncwarp();
         if (lane == 0) {
           odd_values[(c + 2) & 3] = 0;
-          if (K::kScaled)
-            for (int i = 0; i < 3; ++i) largest[(c + 2) & 3][i] = 0;
+          if (K::kScaled) largest[(c + 2) & 3][0] = largest[(c + 2) & 3][1] = 0;
         }
         if (OUT ? odd_0 : odd_1) sync_all();
         odd_2 = odd_1;
@@ -640,25 +644,31 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         }
       }
       if (K::kScaled) {
-        float pm = 0.0f;
+        // (a row for itself: its q, and the decays behind it, may be far from another's)
+        float top[2];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int h = 0; h < 2; ++h)
+          top[h] = fmaxf(fmaxf(fabsf(P[0][2 * h]), fabsf(P[0][2 * h + 1])), fmaxf(fabsf(P[1][2 * h]), fabsf(P[1][2 * h + 1])));
+        if (fmaxf(top[0], top[1]) > FLT_MAX) {                 // (of the finite ones)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) pm = fmaxf(pm, fabsf(P[n][i]));
-        if (pm > FLT_MAX) {
-          pm = 0.0f;
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pm = fmaxf(pm, fabsf(P[n][i]) <= FLT_MAX ? fabsf(P[n][i]) : 0.0f);
+          for (int h = 0; h < 2; ++h)
+            top[h] = __uint_as_float(max(max(finite_bits(P[0][2 * h]), finite_bits(P[0][2 * h + 1])),
+                                         max(finite_bits(P[1][2 * h]), finite_bits(P[1][2 * h + 1]))));
         }
-        raise_max(&largest[c & 3][1], __float_as_uint(pm));
+        uint32_t both = __float_as_uint(top[0]) >> 23 | (__float_as_uint(top[1]) >> 23) << 16;
+        both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 1));
+        both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 2));
+        if ((lane & 3) == 0) {
+          uint8_t* to = reinterpret_cast<uint8_t*>(&row_exponents[c & 1][ti]) + quarter;
+          to[0] = (uint8_t)both;
+          to[32] = (uint8_t)(both >> 16);
+        }
       }
     };
     // o of chunk c, whose products are done, two rows a register
-    auto make_o = [&](int c, float scale_s, float scale_p, bool odd, uint32_t (&y)[kTokens / 2]) {
+    auto make_o = [&](int c, float scale_s, bool odd, uint32_t (&y)[kTokens / 2]) {
       const Decays& d = decays[c & 3];
-      const float is = 1.0f / scale_s, ip = 1.0f / scale_p;
+      const float is = unscale_for(scale_s);
       uint32_t inter[kTokens], intra[kTokens];
       tmem_ld(tmem + lanes + L::kInter + (c & 1) * 64 + quarter * kTokens, inter);
       tmem_ld(tmem + lanes + L::kIntra + (c & 1) * 64 + quarter * kTokens, intra);
@@ -680,11 +690,13 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
 #pragma unroll
       for (int i = 0; i < kTokens; i += 4) {
         const float4 from = *reinterpret_cast<const float4*>(&d.from_start[quarter * kTokens + i]);
-        const float f[4] = {from.x, from.y, from.z, from.w};
+        float4 unscale = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+        if constexpr (K::kScaled) unscale = *reinterpret_cast<const float4*>(&row_unscale[c & 1][quarter * kTokens + i]);
+        const float f[4] = {from.x, from.y, from.z, from.w}, ip[4] = {unscale.x, unscale.y, unscale.z, unscale.w};
 #pragma unroll
         for (int u = 0; u < 4; u += 2)
-          y[(i + u) / 2] = K::pack(fmaf(f[u] * is, __uint_as_float(inter[i + u]), __uint_as_float(intra[i + u]) * ip),
-                                   fmaf(f[u + 1] * is, __uint_as_float(inter[i + u + 1]), __uint_as_float(intra[i + u + 1]) * ip));
+          y[(i + u) / 2] = K::pack(fmaf(f[u] * is, __uint_as_float(inter[i + u]), __uint_as_float(intra[i + u]) * ip[u]),
+                                   fmaf(f[u + 1] * is, __uint_as_float(inter[i + u + 1]), __uint_as_float(intra[i + u + 1]) * ip[u + 1]));
       }
     };
     auto store_o = [&](int c, const uint32_t (&y)[kTokens / 2]) {
@@ -721,7 +733,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
             if (u == i) added[u] = __float_as_uint(sum * scale_k);
         }
       }
-      const float ik = 1.0f / scale_k;
+      const float ik = unscale_for(scale_k);
 #pragma unroll
       for (int j = 0; j < kMine; ++j) S[j] = fmaf(S[j], total, __uint_as_float(added[j]) * ik);
     };
@@ -737,7 +749,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       }
       if (K::odd(top)) odd_values[c & 3] = 1;
     };
-    float prev_k = 1.0f, prev_s = 1.0f, prev_p = 1.0f;         // the chunk before's scales,
+    float prev_k = 1.0f, prev_s = 1.0f;                        // the chunk before's scales,
     bool odd_1 = false;                                        // whether its k and v hold infinities or NaNs
     sync_all();                                                // (the first decays)
     if (OUT && 0 < whole) {
@@ -779,7 +791,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       }
       const bool odd_k = K::odd(top);
       if (odd_k) odd_values[c & 3] = 1;
-      float scale_k = 1.0f, scale_s = 1.0f, scale_p = 1.0f;
+      float scale_k = 1.0f, scale_s = 1.0f;
       if (K::kScaled) {
         // The largest of the weighted k: the weights of tokens far from the chunk's end are far from 1, below it or, where decays grow, above.
         uint32_t km = 0;
@@ -806,14 +818,11 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
 #pragma unroll
             for (int j = 0; j < kMine; ++j) sm = fmaxf(sm, fabsf(S[j]) <= FLT_MAX ? fabsf(S[j]) : 0.0f);
           }
-          raise_max(&largest[c & 3][2], __float_as_uint(sm));
+          raise_max(&largest[c & 3][1], __float_as_uint(sm));
         }
         sync_all();
         scale_k = scale_for(largest[c & 3][0]);
-        if (OUT) {
-          scale_p = scale_for(largest[c & 3][1]);
-          scale_s = scale_for(largest[c & 3][2]);
-        }
+        if (OUT) scale_s = scale_for(largest[c & 3][1]);
       }
       if (OUT) {
         uint32_t r[kMine / 2];
@@ -845,12 +854,19 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         if (c > 0) failed = !wait(intra_done, c - 1) || failed;      // (it read P)
         if (makes_p) {
 #pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int ti = rb * 16 + (lane >> 2) + 8 * i, cc = quarter * 2 + n;
-              st_shared4(smem + L::kPAt + ti * 128 + ((cc ^ (ti & 7)) << 4) + (lane & 3) * 4, K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
+          for (int i = 0; i < 2; ++i) {
+            const int ti = rb * 16 + (lane >> 2) + 8 * i;
+            float scale_p = 1.0f;
+            if constexpr (K::kScaled) {
+              const uint32_t e = row_exponents[c & 1][ti];
+              scale_p = scale_for(max(max(e & 255u, e >> 8 & 255u), max(e >> 16 & 255u, e >> 24)) << 23);
+              if (quarter == 0 && (lane & 3) == 0) row_unscale[c & 1][ti] = unscale_for(scale_p);
             }
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+              st_shared4(smem + L::kPAt + ti * 128 + (((quarter * 2 + n) ^ (ti & 7)) << 4) + (lane & 3) * 4,
+                         K::pack(P[n][2 * i] * scale_p, P[n][2 * i + 1] * scale_p));
+          }
         }
         tmem_st_wait();
       }
@@ -864,7 +880,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       if (OUT) {
         if (c > 0 && !odd_1) {                                 // (an odd chunk's has been stored)
           uint32_t y[kTokens / 2];
-          make_o(c - 1, prev_s, prev_p, false, y);
+          make_o(c - 1, prev_s, false, y);
           if (p.o_by_map && c + 1 < chunks) {
             failed = !wait(stored, c) || failed;
             stage_o(y);
@@ -886,12 +902,11 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
           failed = !wait(intra_done, c) || failed;
           tc_fence_after();
           uint32_t y[kTokens / 2];
-          make_o(c, scale_s, scale_p, true, y);
+          make_o(c, scale_s, true, y);
           store_o(c, y);
           sync_all();                                          // (P and v have been read)
         }
         prev_s = scale_s;
-        prev_p = scale_p;
       } else {
         if (c > 0) {
           failed = !wait(done + ((c - 1) & 1) * 8, (c - 1) >> 1) || failed;
@@ -910,7 +925,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
           wait(intra_done, z);
           tc_fence_after();
           uint32_t y[kTokens / 2];
-          make_o(z, prev_s, prev_p, false, y);
+          make_o(z, prev_s, false, y);
           store_o(z, y);
         }
       } else {

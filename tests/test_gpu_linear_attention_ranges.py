@@ -83,3 +83,16 @@ def test_states_whose_later_v_are_zero_behind_any_decay(decay):
     weights = torch.exp(decay * torch.arange(63, -1, -1, dtype=torch.float64))
     off = off + 2.0 ** -62 * (k.double().abs() * weights[:, None, None]).max() * v.double().abs().sum(0)[0]
     close(state, new, off, "state_out")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dk", [64, 128])
+def test_rows_whose_weights_differ_by_2_to_the_36(dtype, dk):
+    """Row 0 meets one v; behind a decay of +25 the same v and its negative meet weights 2^36 times as large, which cancel."""
+    def edit(q, k, v, g, st):
+        st.zero_()
+        k[1] = k[0]
+        v[1], v[2:32] = -v[0], 0.0
+        g.zero_()
+        g[32] = 25.0
+    run(dtype, [40], 2, 1, dk, 64, edit=edit)
