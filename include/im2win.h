@@ -436,8 +436,9 @@ typedef struct {
  * recurrence as it stands, in fp32.  Others go by chunks of 64 tokens on the
  * tensor cores: there the weights of a chunk's tokens for one another and the
  * copy of the state that meets q are rounded once to `dtype` (sums are fp32, in
- * fp16 everything is scaled to the type's range), which puts o off by about as
- * much as its own rounding does; rows of q, k and v that start on 16-byte
+ * fp16 a row's weights and a column of the state are scaled to the type's range
+ * and what is below 2^-27 of their largest loses bits), which puts o off by
+ * about as much as its own rounding does; rows of q, k and v that start on 16-byte
  * boundaries, and dk and dv of multiples of 8, are the fast ones.  The
  * states are fp32 throughout, to within a few units of the last place of the
  * magnitudes that add up to an element; in fp16 what 64 tokens add is off by up

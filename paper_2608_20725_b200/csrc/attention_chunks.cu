@@ -19,7 +19,7 @@
 // one size and independent.  The weighted k are not: the state is carried from call to call in fp32 and has to stay fp32, so they go
 // through the tensor cores as three pieces whose sum is the fp32 product (of bf16: cut off; of fp16: each 2^12 times what it stands for
 // beside the one before, which the sums of the products undo as they go; off by 2^-62 of a chunk's largest).  fp16 has no room for large or
-// small numbers: S, the weighted k and each row of P are brought to 2^13 by a power of two for each chunk, of their largest.
+// small numbers: the weighted k, each column of S and each row of P are brought to 2^13 by a power of two for each chunk, of their largest.
 // log_decay is summed in 64 bits, differences are split into whole and fractional powers of two, so that no cancellation is left
 // behind a strong decay.  A product of a masked 0, or of a piece that is 0 or has the other sign, with an infinity of v is a NaN: a
 // chunk whose k or v hold any has its intra part made again from the terms j <= i alone, and what it adds to the state from fp32 products.
@@ -378,8 +378,9 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   extern __shared__ uint8_t dynamic_smem[];
   __shared__ Decays decays[4];
   __shared__ __align__(8) uint64_t bars[kStages + 4];          // stages loaded; added done (two), intra, q . k done, o stored
-  __shared__ uint32_t tmem_base_at, abort_flag, odd_values[4], largest[4][2];    // largest: of the weighted k, of S
-  // fp16: the exponents of the largest of each row of P, a byte for each quarter of its columns, and what undoes the row's scale
+  __shared__ uint32_t tmem_base_at, abort_flag, odd_values[4], largest[4];       // largest: of the weighted k
+  __shared__ uint32_t column_largest[K::kScaled && OUT ? 4 : 1][kTile];          // fp16: of each column of S
+  // and the exponents of the largest of each row of P, a byte for each quarter of its columns, and what undoes the row's scale
   __shared__ __align__(16) uint32_t row_exponents[K::kScaled ? 2 : 1][kChunk];
   __shared__ __align__(16) float row_unscale[K::kScaled ? 2 : 1][kChunk];
   const uint32_t smem = (smem_u32(dynamic_smem) + 1023u) & ~1023u;
@@ -403,11 +404,11 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   if (tid == 0) {
     for (int i = 0; i < kStages + 4; ++i) mbar_init(smem_u32(bars + i), 1);
     abort_flag = 0;
-    for (int i = 0; i < 8; ++i) largest[i / 2][i % 2] = 0;
-    for (int i = 0; i < 4; ++i) odd_values[i] = 0;
+    for (int i = 0; i < 4; ++i) largest[i] = odd_values[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async_smem();
   }
+  if (K::kScaled && OUT && tid < 4 * kTile) column_largest[tid / kTile][tid % kTile] = 0;
   if (K::kScaled && tid < 2 * kChunk) row_exponents[tid / kChunk][tid % kChunk] = 0;     // (as the quarters above the diagonal stay)
   if (OUT && tid < kPanel / 16) st_shared16(smem + L::kPAt + tid * 16, 0, 0, 0, 0);      // (above the diagonal it stays 0)
   auto wait = [&](uint32_t bar, uint32_t phase) { return wait_for(bar, phase & 1, &abort_flag, p.status); };
@@ -583,7 +584,11 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         __syncwarp();
         if (lane == 0) {
           odd_values[(c + 2) & 3] = 0;
-          if (K::kScaled) largest[(c + 2) & 3][0] = largest[(c + 2) & 3][1] = 0;
+          if (K::kScaled) largest[(c + 2) & 3] = 0;
+        }
+        if (K::kScaled && OUT) {
+#pragma unroll
+          for (int i = 0; i < kTile; i += 32) column_largest[(c + 2) & 3][i + lane] = 0;
         }
         if (OUT ? odd_0 : odd_1) sync_all();
         odd_2 = odd_1;
@@ -808,7 +813,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
           }
           km = max(km, finite_bits(fmaxf(K::low(t), K::high(t)) * decays[c & 3].to_end[(tid + m * kThreads) / kUnits]));
         }
-        raise_max(&largest[c & 3][0], km);
+        raise_max(&largest[c & 3], km);
         if (OUT) {
           float sm = 0.0f;
 #pragma unroll
@@ -818,11 +823,11 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
 #pragma unroll
             for (int j = 0; j < kMine; ++j) sm = fmaxf(sm, fabsf(S[j]) <= FLT_MAX ? fabsf(S[j]) : 0.0f);
           }
-          raise_max(&largest[c & 3][1], __float_as_uint(sm));
+          atomicMax(&column_largest[c & 3][row], __float_as_uint(sm));
         }
         sync_all();
-        scale_k = scale_for(largest[c & 3][0]);
-        if (OUT) scale_s = scale_for(largest[c & 3][1]);
+        scale_k = scale_for(largest[c & 3]);
+        if (OUT) scale_s = scale_for(column_largest[c & 3][row]);
       }
       if (OUT) {
         uint32_t r[kMine / 2];

@@ -96,3 +96,14 @@ def test_rows_whose_weights_differ_by_2_to_the_36(dtype, dk):
         g.zero_()
         g[32] = 25.0
     run(dtype, [40], 2, 1, dk, 64, edit=edit)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 200)])
+def test_columns_of_a_state_that_differ_by_2_to_the_100(dtype, dk, dv):
+    """Element (0, 0) of each state is 1e30 and alone in its column; q does not meet it."""
+    def edit(q, k, v, g, st):
+        q[:, :, 0], v[:, :, 0] = 0.0, 0.0
+        st[:, :, :, 0] = 0.0
+        st[:, :, 0, 0] = 1e30
+    run(dtype, [100], 2, 2, dk, dv, edit=edit)
