@@ -451,7 +451,8 @@ typedef struct {
  *
  * `workspace` needs the bytes of im2win_linear_attention_workspace_size; it
  * starts with a status block as a convolution's scratch does (cleared by the
- * call; see im2win_check_status).  Nothing in it outlives the call, but calls
+ * call; see im2win_check_status).  Should a bounded wait give up, the rows of o
+ * and the states that hang on it are NaN.  Nothing in it outlives the call, but calls
  * that may overlap on the GPU need one each.
  */
 im2win_status im2win_linear_attention_workspace_size(const im2win_attention_shape* shape, im2win_dtype dtype, size_t* bytes);

@@ -76,6 +76,7 @@ struct ChunkParams {
   int64_t q_stride, k_stride, v_stride, o_stride, decay_stride;
   int32_t heads, share, dk, dv, tiles, L;
   int32_t segmented, by_map, o_by_map;   // by_map: rows of q, k and v start on 16-byte boundaries; o_by_map: those of o too
+  int32_t drop;                          // testing aid: head 0 does not say that the products of this chunk are done (-1: all do)
   float scale;
 };
 
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   constexpr int kTokens = kChunk / kQuarters;                  // rows of o of a thread
   extern __shared__ uint8_t dynamic_smem[];
   __shared__ Decays decays[4];
-  __shared__ __align__(8) uint64_t bars[kStages + 4];          // stages loaded; added done (two), intra, q . k done, o stored
+  __shared__ __align__(8) uint64_t bars[kStages + 5];          // stages loaded; added done (two), intra, q . k done, o stored; all products done
   __shared__ uint32_t tmem_base_at, abort_flag, odd_values[4], largest[4];       // largest: of the weighted k
   __shared__ uint32_t column_largest[K::kScaled && OUT ? 4 : 1][kTile];          // fp16: of each column of S
   // and the exponents of the largest of each row of P, a byte for each quarter of its columns, and what undoes the row's scale
@@ -399,10 +400,10 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   const int chunks = (end - first + kChunk - 1) / kChunk, whole = p.by_map ? (end - first) / kChunk : 0;
 
   const uint32_t loaded = smem_u32(bars), done = smem_u32(bars + kStages), intra_done = smem_u32(bars + kStages + 1),
-                 dots_done = smem_u32(bars + kStages + 2), stored = smem_u32(bars + kStages + 3);
+                 dots_done = smem_u32(bars + kStages + 2), stored = smem_u32(bars + kStages + 3), drained = smem_u32(bars + kStages + 4);
   if (warp == 0) tmem_alloc(smem_u32(&tmem_base_at), L::kColumns);
   if (tid == 0) {
-    for (int i = 0; i < kStages + 4; ++i) mbar_init(smem_u32(bars + i), 1);
+    for (int i = 0; i < kStages + 5; ++i) mbar_init(smem_u32(bars + i), 1);
     abort_flag = 0;
     for (int i = 0; i < 4; ++i) largest[i] = odd_values[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -536,7 +537,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
               else
                 umma_f16_ab(to, a, kDescHi, b, kDescHi, kDesc, n < K::kPieces - 1 || ks > 0);
             }
-          umma_commit(done + (OUT ? 0 : (c & 1) * 8));
+          if (c != p.drop || head != 0) umma_commit(done + (OUT ? 0 : (c & 1) * 8));
           if (OUT) {
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks)
@@ -553,8 +554,12 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         __syncwarp();
         odd_1 = odd_0;
       }
-      if (failed)                                              // (its loads under way end before the block does)
+      // Its loads and products under way end before the block does and gives its tensor memory back.
+      if (failed)
         for (int i = c; i < c + 2 && i < whole; ++i) wait(loaded + (i % kStages) * 8, i / kStages);
+      if (elect_one()) umma_commit(drained);
+      __syncwarp();
+      wait(drained, 0);
     } else if (warp == kDecayWarp) {
       double all_decay = 0.0, E = 1.0;
       float g0 = 0.0f, g1 = 0.0f;
@@ -569,7 +574,10 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         if (c + 2 < chunks) load_decay(c + 2, g0, g1);
         if (c >= whole) sync_all();
         if (K::kScaled) sync_all();
-        if (sync_or(false)) break;
+        if (sync_or(false)) {
+          all_decay = (double)__builtin_nanf("");
+          break;
+        }
         const bool odd_0 = *(volatile uint32_t*)&odd_values[c & 3] != 0;
         if (OUT && elect_one()) {
           if (p.o_by_map && c > 1 && !odd_2) {
@@ -595,6 +603,8 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         odd_1 = odd_0;
       }
       if (OUT) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+      __syncwarp();
+      asm volatile("bar.arrive 2, %0;" ::"n"(kThreads + 32) : "memory");
       if (!OUT && tile == 0) {
         const float2 total = two_parts(all_decay);
         if (lane == 0) p.totals[(int64_t)id * p.heads + head] = total;
@@ -945,8 +955,15 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       to = p.added + ((int64_t)id * p.heads + head) * state_size;
     else if (p.state_out && last)
       to = p.state_out + ((int64_t)slot * p.heads + head) * state_size;
+    // Should a wait have given up, what there is of o and S is not to be taken for results.  (The rows of o under way have arrived.)
+    asm volatile("bar.sync 2, %0;" ::"n"(kThreads + 32) : "memory");
+    const bool gave_up = *(volatile uint32_t*)&abort_flag != 0;
+    if (OUT && gave_up && live) {
+      unsigned short* at = static_cast<unsigned short*>(p.o) + (int64_t)head * p.dv + col;
+      for (int t = first + quarter; t < end; t += kQuarters) at[(int64_t)t * p.o_stride] = 0x7fff;         // (a NaN of either type)
+    }
     if (to && live) {
-      const float E = chunks > 0 ? decays[(chunks - 1) & 3].behind : 1.0f;
+      const float E = gave_up ? __builtin_nanf("") : chunks > 0 ? decays[(chunks - 1) & 3].behind : 1.0f;
 #pragma unroll
       for (int j = 0; j < kMine; ++j) {
         const int e = quarter * kMine + j;
@@ -1102,7 +1119,13 @@ cudaError_t launch_all(const ChunkMaps& maps, ChunkParams& p, const ChunkPlan& p
   const int64_t grid = (int64_t)blocks * p.heads * a.shape.sequences, most = (int64_t)1 << 31;
   if (pieces * p.heads * p.tiles >= most || (plan.segments && grid >= most)) return cudaErrorInvalidConfiguration;
   if (cudaMemsetAsync(p.status, 0, kStatusBytes, stream) != cudaSuccess) return cudaErrorUnknown;
+  // Testing aids: a chunk that head 0 drops (ChunkParams) of the launch that makes o, or of the one that sums up; waits then give up
+  // after 4096 polls (word 1 of the status block).
+  const char* drop = debug_getenv("IM2WIN_ATTENTION_DROP");
+  const char* drop_sums = debug_getenv("IM2WIN_ATTENTION_DROP_SUMS");
+  if ((drop || drop_sums) && cudaMemsetAsync(reinterpret_cast<uint8_t*>(p.status) + 5, 0x10, 1, stream) != cudaSuccess) return cudaErrorUnknown;
   if (plan.segments) {
+    p.drop = drop_sums ? atoi(drop_sums) : -1;
     cudaError_t e = launch<T, DK, false>(maps, p, pieces, stream);
     if (e != cudaSuccess) return e;
     if (width == 4)
@@ -1113,6 +1136,7 @@ cudaError_t launch_all(const ChunkMaps& maps, ChunkParams& p, const ChunkPlan& p
     if (e != cudaSuccess) return e;
     p.segmented = 1;
   }
+  p.drop = drop ? atoi(drop) : -1;
   return launch<T, DK, true>(maps, p, pieces, stream);
 }
 
@@ -1131,7 +1155,7 @@ cudaError_t launch_attention_chunks(const AttentionArgs& a, cudaStream_t stream)
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
   ChunkParams p = {a.q, a.k, a.v, a.decay, a.o, a.state_in, a.state_out, reinterpret_cast<float*>(ws + plan.added_off),
                    reinterpret_cast<float2*>(ws + plan.totals_off), reinterpret_cast<uint32_t*>(ws), a.seqs, s.q_stride, s.k_stride,
-                   s.v_stride, s.o_stride, s.decay_stride, s.heads, s.heads / s.qk_heads, s.dk, s.dv, plan.tiles, plan.L, 0, 0, 0, s.scale};
+                   s.v_stride, s.o_stride, s.decay_stride, s.heads, s.heads / s.qk_heads, s.dk, s.dv, plan.tiles, plan.L, 0, 0, 0, -1, s.scale};
   const EncodeTiledFn fn = get_encode_fn();
   if (!fn) return cudaErrorNotSupported;
   p.by_map = s.dk % 8 == 0 && s.dv % 8 == 0 && s.q_stride % 8 == 0 && s.k_stride % 8 == 0 && s.v_stride % 8 == 0 && aligned_to(a.q, 16) &&
