@@ -483,7 +483,8 @@ typedef struct {
  * and y [M][N] hold elements of `dtype` (any of the three); bias holds floats
  * or is NULL.  (w - z) and its products with x are exact, sums are fp32, a
  * group's sum is multiplied by its scale in fp32, y is rounded once; the order
- * of sums is fixed by the shape.  The pointers need the alignment of their
+ * of sums is fixed by the shape.  Without a workspace there is no status block:
+ * should a bounded wait give up, the y that hang on it are NaN.  The pointers need the alignment of their
  * elements only; rows of x and of the matrix that start on 16-byte boundaries
  * are the fast ones.
  */

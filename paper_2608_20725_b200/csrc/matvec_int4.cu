@@ -23,6 +23,8 @@
 // the place of 84).  Rows of more than a pass of K (4096 elements for 8 columns of x, 2048 for more columns or for groups of 32:
 // what registers hold; 8192 spilled, 90 us in the place of 82) go in passes, whose sums are kept for kMostGroups tiles at a time.  Rows that do not start on 16-byte boundaries, and a K that is no
 // multiple of 128, go through registers (matvec_any_kernel).
+#include <stdlib.h>
+
 #include <type_traits>
 
 #include "common.cuh"
@@ -47,6 +49,8 @@ struct Int4Params {
   int32_t M, N, K, group, groups, row_bytes, blocks;   // blocks: of 128 elements along K
   int32_t pass, wk;                                    // blocks of a pass, warps that share a group of rows along K
   int32_t vec_w, vec_x, vec_s;                         // whether rows of the matrix, of x, and a block's scales can be loaded whole
+  uint32_t polls;                                      // looks, of a microsecond at most, before a wait gives up
+  int32_t drop;                                        // testing aid: a warp of block 0 does not say that it is done with this tile (-1: all do)
 };
 
 template <typename T> struct Mma;
@@ -354,6 +358,19 @@ constexpr int kChunkBlocks = kWarps;             // blocks of 128 elements of a 
 template <int PARTS>
 constexpr int kRowPitch = kChunkBlocks * 64 + 64 / PARTS;
 
+// One look at a barrier, of a microsecond at most.
+__device__ __forceinline__ bool try_wait_1us(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 1000;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 template <typename T, int PARTS, int NT, int TURNS>
 __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params p) {
   using M16 = typename std::conditional<sizeof(T) == 4, __nv_bfloat16, T>::type;   // what the products are made of
@@ -364,6 +381,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
   constexpr uint32_t kSlot = kTileRows * kRowPitch<PARTS>;
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ __align__(8) uint64_t bars[2 * kSlots];           // full, empty
+  __shared__ uint32_t gave_up;
   float (*sums)[kTileRows][NT * 8 + 1] = reinterpret_cast<float (*)[kTileRows][NT * 8 + 1]>(ring + kSlots * kSlot);
   float (*kept)[kTileRows][NT * 8] = reinterpret_cast<float (*)[kTileRows][NT * 8]>(sums + kWarps);
   const int lane = threadIdx.x & 31, warp = ptx::warp_index(), g = lane >> 2, t = lane & 3;
@@ -374,6 +392,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
       ptx::mbar_init(full + i * 8, kWarps);      // a warp copies two rows each
       ptx::mbar_init(empty + i * 8, kWarps);
     }
+    gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     ptx::fence_proxy_async_smem();
   }
@@ -383,11 +402,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
   const int first = unit * 16, last = min((int)((int64_t)units * (blockIdx.x + 1) / gridDim.x) * 16, p.N);
   const int mine = (last - first + kTileRows - 1) / kTileRows;
   bool failed = false;
-  // Waits are for copies and warps of this block, which end by themselves.  Should one not, they give up, and y is NaN.
-  auto wait = [&](uint32_t bar, uint32_t parity) {
-    for (uint32_t i = 0; i < (1u << 22) && !failed; ++i)
-      if (ptx::mbar_try_wait(bar, parity)) return;
+  // Waits are for copies and warps of this block, which end by themselves.  Should one not within some four seconds, it gives up, the
+  // others with it, and y is NaN from that tile on.
+  auto wait = [&](uint32_t bar, uint32_t parity) {             // (the whole warp, of one mind)
+    uint32_t left = failed ? 0 : p.polls;
+    bool there = false;
+    while (left-- > 0) {
+      there = __all_sync(0xffffffffu, try_wait_1us(bar, parity));
+      if (there || ((left & 255u) == 0u && *(volatile uint32_t*)&gave_up)) break;
+    }
+    if (there) return;
     failed = true;
+    gave_up = 1;
   };
   uint32_t fill_slot = 0, fill_parity = 1, use_slot = 0, use_parity = 0;       // (the first wait for an empty slot passes)
   const uint32_t words_at = g * kRowPitch<PARTS> + warp * 64 + t * (kWords * 4);
@@ -415,13 +441,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
       const uint8_t* from = nullptr;
       int64_t second = 0;                        // from the first of the two rows to the other
       auto fill = [&]() {
-        if (fill_tile >= n_tiles) return;
+        if (fill_tile >= n_tiles || failed) return;
         if (fill_turn == 0) {
           const int row = min(first_row(fill_tile) + 2 * warp, p.N - 1);
           from = p.weight + (int64_t)row * p.row_bytes + (int64_t)b0 * 64;
           second = row + 1 < p.N ? p.row_bytes : 0;
         }
         wait(empty + fill_slot * 8, fill_parity);
+        if (failed) return;
         if (ptx::elect_one()) {
           const uint32_t bytes = (uint32_t)min(kChunkBlocks, nb - fill_turn * kChunkBlocks) * 64;
           const uint32_t to = ring_at + fill_slot * kSlot + 2 * warp * kRowPitch<PARTS>, bar = full + fill_slot * 8;
@@ -539,7 +566,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
               products(std::integral_constant<int, 1>());
           }
           __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(empty + use_slot * 8);
+          if (failed) continue;
+          if (lane == 0 && !(tile == p.drop && warp == 3 && blockIdx.x == 0)) ptx::mbar_arrive(empty + use_slot * 8);
           if (++use_slot == kSlots) {
             use_slot = 0;
             use_parity ^= 1;
@@ -571,6 +599,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) matvec_kernel(const Int4Params
           }
         }
         __syncthreads();
+      }
+    }
+  }
+  if (failed) {                                  // copies under way end before the block does
+    failed = false;
+    while (!failed && (use_slot != fill_slot || use_parity == fill_parity)) {
+      wait(full + use_slot * 8, use_parity);
+      if (++use_slot == kSlots) {
+        use_slot = 0;
+        use_parity ^= 1;
       }
     }
   }
@@ -635,7 +673,11 @@ cudaError_t launch_matvec_int4(const void* x, const uint8_t* weight, const void*
                                void* y, const im2win_int4_shape& s, im2win_dtype dtype, cudaStream_t stream) {
   Int4Params p = {x, weight, scales, zeros, bias, y, s.x_stride, s.y_stride, s.M, s.N, s.K, s.group,
                   (int32_t)(((int64_t)s.K + s.group - 1) / s.group), (int32_t)(((int64_t)s.K + 1) / 2),
-                  (int32_t)(((int64_t)s.K + 127) / 128), 0, 0, 0, 0, 0};
+                  (int32_t)(((int64_t)s.K + 127) / 128), 0, 0, 0, 0, 0, 1u << 22, -1};
+  if (const char* v = debug_getenv("IM2WIN_MATVEC_DROP")) {    // testing aid
+    p.drop = atoi(v);
+    p.polls = 4096;
+  }
   switch (dtype) {
     case IM2WIN_F32: return launch_type<float>(p, stream);
     case IM2WIN_F16: return launch_type<__half>(p, stream);

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2608_20725_b200 import binding
-from sequence_helpers import DTYPES, close, half_step, linear_64, rounding, sequence_list
+from sequence_helpers import DTYPES, close, half_step, linear_64, matvec_64, rounding, sequence_list
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +69,30 @@ def test_attention_gives_up_in_the_sums_of_segments(dtype, dk, dv, drop, monkeyp
     ws, o, new, want = attention(dtype, [576], dk, dv)
     binding.im2win_check_status(ws)
     compare(dtype, o, new, want, slice(0, 2))
+
+
+@pytest.mark.parametrize("dtype,m,group", [("f16", 1, 128), ("bf16", 8, 64), ("bf16", 16, 32), ("f32", 2, 64), ("f32", 7, 128)])
+@pytest.mark.parametrize("k", [2048, 4096])
+def test_products_give_up_and_say_so(dtype, m, group, k, monkeypatch):
+    """A warp of the first block does not free its slot after the first tile: the ring stops there.  The tiles that had come by then are
+    right, the block's others NaN; those of the other blocks are right."""
+    n, rows, tdt = 148 * 32 * 7, 32 * 7, DTYPES[dtype]
+    gen = torch.Generator().manual_seed(m)
+    x = torch.randn(m, k, generator=gen).to(tdt)
+    w = torch.randint(0, 256, (n, k // 2), generator=gen, dtype=torch.uint8)
+    s = ((torch.rand(n, k // group, generator=gen) + 0.5) * 0.1).to(tdt)
+    xd, wd, sd, y = x.cuda(), w.cuda(), s.cuda(), torch.zeros(m, n, dtype=tdt, device="cuda")
+    want, a = matvec_64(x, w[:2 * rows], s[:2 * rows], None, None, group)
+    tol = (k / 8 + 16 + k // group) * 2.0 ** -23 * a + rounding(want, tdt)
+    monkeypatch.setenv("IM2WIN_MATVEC_DROP", "0")
+    binding.im2win_matvec_int4(xd, wd, sd, y, group)
+    torch.cuda.synchronize()
+    monkeypatch.delenv("IM2WIN_MATVEC_DROP")
+    bad = y.isnan().cpu()
+    assert bool(bad[:, 4 * 32:rows].all()) and not bool(bad[:, rows:].any()) and torch.equal(bad, bad[:1].expand_as(bad))
+    right = ~bad[0, :2 * rows]
+    close(y[:, :2 * rows][:, right.cuda()], want[:, right], tol[:, right], "y")
+    again = torch.zeros_like(y)
+    binding.im2win_matvec_int4(xd, wd, sd, again, group)
+    close(again[:, :2 * rows], want, tol, "y")
+    assert torch.equal(again[:, rows:], y[:, rows:])
