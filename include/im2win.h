@@ -491,6 +491,11 @@ typedef struct {
 im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros,
                                  const float* bias, void* y, const im2win_int4_shape* shape, im2win_dtype dtype,
                                  void* cuda_stream);
+/*
+ * How a call whose pointers start on 16-byte boundaries runs such a shape (host-only, static storage; for reports and tests): "ring" (K a
+ * multiple of 128, rows of x on 16-byte boundaries: the matrix by bulk copies through shared memory), "registers"; "none" for an invalid shape.
+ */
+const char* im2win_matvec_int4_kernel_name(const im2win_int4_shape* shape, im2win_dtype dtype);
 
 #ifdef __cplusplus
 }

@@ -32,6 +32,7 @@ EXPORTS = (
     "im2win_nhwc_workspace_size", "im2win_transform_nhwc", "im2win_conv_f16_nhwc", "im2win_pack_filter_nhwc",
     "im2win_conv_packed_nhwc", "im2win_causal_conv1d", "im2win_linear_attention",
     "im2win_linear_attention_workspace_size", "im2win_linear_attention_kernel_name", "im2win_matvec_int4",
+    "im2win_matvec_int4_kernel_name",
 )
 
 STATIC_SCRATCH_BYTES = 4 << 20
@@ -123,6 +124,8 @@ def lib() -> ctypes.CDLL:
     L.im2win_nhwc_kernel_name.restype = ctypes.c_char_p
     L.im2win_linear_attention_kernel_name.argtypes = [P(AttentionShape), ctypes.c_int]
     L.im2win_linear_attention_kernel_name.restype = ctypes.c_char_p
+    L.im2win_matvec_int4_kernel_name.argtypes = [P(Int4Shape), ctypes.c_int]
+    L.im2win_matvec_int4_kernel_name.restype = ctypes.c_char_p
     # the library looks at IM2WIN_DEBUG in its first plan: here, so that both sides see the same
     _debug = bool(os.environ.get("IM2WIN_DEBUG"))
     L.im2win_conv_kernel_name(ctypes.byref(Shape(1, 64, 1, 1, 1, 1, 1, 1, 0)), F32)
@@ -606,6 +609,11 @@ def im2win_matvec_int4(x, weight, scales, y, group: int, zeros=None, bias=None, 
                                               code, _stream(stream))
     if code:
         _check(code, "im2win_matvec_int4")
+
+
+def im2win_matvec_int4_kernel_name(m: int, n: int, k: int, group: int, dtype: int, x_stride: int = 0) -> str:
+    """How im2win_matvec_int4 runs these sizes where tensors start on 16-byte boundaries (for reports and tests)."""
+    return lib().im2win_matvec_int4_kernel_name(ctypes.byref(Int4Shape(m, n, k, group, x_stride or k, n)), dtype).decode()
 
 
 # ---------------------------------------------------------------- conveniences

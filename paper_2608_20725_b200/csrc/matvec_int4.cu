@@ -48,7 +48,7 @@ struct Int4Params {
   int64_t x_stride, y_stride;
   int32_t M, N, K, group, groups, row_bytes, blocks;   // blocks: of 128 elements along K
   int32_t pass, wk;                                    // blocks of a pass, warps that share a group of rows along K
-  int32_t vec_w, vec_x, vec_s;                         // whether rows of the matrix, of x, and a block's scales can be loaded whole
+  int32_t vec_w, vec_x, ring;                          // whether rows of the matrix and of x can be loaded whole; matvec_kernel or the other
   uint32_t polls;                                      // looks, of a microsecond at most, before a wait gives up
   int32_t drop;                                        // testing aid: a warp of block 0 does not say that it is done with this tile (-1: all do)
 };
@@ -635,7 +635,7 @@ cudaError_t launch_ring(const Int4Params& p, cudaStream_t stream) {
 // Chunks of a pass by what registers hold: 32 of them x, or 16 to 48 with smaller groups or more columns and their sums.
 template <typename T, int PARTS, int NT>
 cudaError_t launch(Int4Params& p, cudaStream_t stream) {
-  if (!(p.K % 128 == 0 && p.vec_w && p.vec_x && p.vec_s)) return launch_any<T, PARTS, NT>(p, stream);
+  if (!p.ring) return launch_any<T, PARTS, NT>(p, stream);
   return launch_ring<T, PARTS, NT, NT == 1 && PARTS < 4 ? 2 : 1>(p, stream);
 }
 
@@ -661,13 +661,19 @@ template <typename T>
 cudaError_t launch_type(Int4Params& p, cudaStream_t stream) {
   p.vec_w = p.row_bytes % 16 == 0 && aligned_to(p.weight, 16);
   p.vec_x = (p.x_stride * (int64_t)sizeof(T)) % 16 == 0 && aligned_to(p.x, 16);
-  p.vec_s = (p.group >= 128 || p.groups % 4 == 0) && aligned_to(p.scales, 16) && aligned_to(p.zeros, 4);
+  // (a row then has whole blocks of 128 elements, and a block's scales and zero points are loaded at once)
+  const size_t parts = p.group == 32 ? 4 : p.group == 64 ? 2 : 1;
+  p.ring = p.K % 128 == 0 && p.vec_w && p.vec_x && aligned_to(p.scales, parts * sizeof(T)) && aligned_to(p.zeros, parts);
   if (p.group == 32) return launch_columns<T, 4>(p, stream);
   if (p.group == 64) return launch_columns<T, 2>(p, stream);
   return launch_columns<T, 1>(p, stream);
 }
 
 }  // namespace
+
+bool matvec_by_ring(const im2win_int4_shape& s, im2win_dtype dtype) {
+  return s.K % 128 == 0 && s.x_stride * (int64_t)element_bytes(dtype) % 16 == 0;
+}
 
 cudaError_t launch_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros, const float* bias,
                                void* y, const im2win_int4_shape& s, im2win_dtype dtype, cudaStream_t stream) {

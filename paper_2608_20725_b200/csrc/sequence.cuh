@@ -153,6 +153,8 @@ cudaError_t launch_attention_tokens(const AttentionArgs& a, cudaStream_t stream)
 // Whether the sizes go by chunks, and the workspace that takes.
 bool attention_by_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool has_cu, size_t* workspace_bytes, bool* segmented);
 cudaError_t launch_attention_chunks(const AttentionArgs& a, cudaStream_t stream);
+// Whether rows that start on 16-byte boundaries come through the ring of bulk copies.
+bool matvec_by_ring(const im2win_int4_shape& s, im2win_dtype dtype);
 cudaError_t launch_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros, const float* bias,
                                void* y, const im2win_int4_shape& shape, im2win_dtype dtype, cudaStream_t stream);
 

@@ -40,6 +40,15 @@ im2win_status check_attention(const im2win_attention_shape* s, im2win_dtype dtyp
   return IM2WIN_OK;
 }
 
+im2win_status check_int4(const im2win_int4_shape* s, im2win_dtype dtype) {
+  if (!s) return IM2WIN_ERR_NULL_POINTER;
+  if (!known_dtype(dtype) || s->M < 1 || s->N < 1 || s->K < 1 || s->x_stride < s->K || s->y_stride < s->N || s->group < 1)
+    return IM2WIN_ERR_INVALID_ARG;
+  if (s->M > 16 || (s->group != 32 && s->group != 64 && s->group % 128 != 0) || s->K > kMost - 4096 || s->N > kMost - 4096)
+    return IM2WIN_ERR_UNSUPPORTED;
+  return IM2WIN_OK;
+}
+
 }  // namespace
 }  // namespace im2win
 
@@ -114,16 +123,17 @@ im2win_status im2win_linear_attention(const void* q, const void* k, const void* 
   return from_launch(chunks ? launch_attention_chunks(a, stream) : launch_attention_tokens(a, stream));
 }
 
+const char* im2win_matvec_int4_kernel_name(const im2win_int4_shape* shape, im2win_dtype dtype) {
+  if (check_int4(shape, dtype) != IM2WIN_OK) return "none";
+  return matvec_by_ring(*shape, dtype) ? "ring" : "registers";
+}
+
 im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros,
                                  const float* bias, void* y, const im2win_int4_shape* shape, im2win_dtype dtype,
                                  void* cuda_stream) {
-  if (!x || !weight || !scales || !y || !shape) return IM2WIN_ERR_NULL_POINTER;
-  if (!known_dtype(dtype) || shape->M < 1 || shape->N < 1 || shape->K < 1 || shape->x_stride < shape->K ||
-      shape->y_stride < shape->N || shape->group < 1)
-    return IM2WIN_ERR_INVALID_ARG;
-  if (shape->M > 16 || (shape->group != 32 && shape->group != 64 && shape->group % 128 != 0) || shape->K > kMost - 4096 ||
-      shape->N > kMost - 4096)
-    return IM2WIN_ERR_UNSUPPORTED;
+  if (!x || !weight || !scales || !y) return IM2WIN_ERR_NULL_POINTER;
+  const im2win_status st = check_int4(shape, dtype);
+  if (st != IM2WIN_OK) return st;
   const size_t es = element_bytes(dtype);
   for (const void* at : {x, scales, (const void*)y})
     if (!aligned_to(at, es)) return IM2WIN_ERR_MISALIGNED;
