@@ -6,6 +6,7 @@ namespace im2win {
 namespace {
 
 constexpr int64_t kMost = (int64_t)1 << 31;
+constexpr int64_t kMostRows = kMost - 4096;          // tokens, sequences: the kernels count in 32 bits, up to some chunks beyond the last one
 
 bool known_dtype(im2win_dtype dtype) { return dtype == IM2WIN_F32 || dtype == IM2WIN_F16 || dtype == IM2WIN_BF16; }
 
@@ -21,6 +22,7 @@ im2win_status take_sequences(const im2win_sequences* given, int32_t tokens, int3
   if (tokens < 0 || sequences < 1 || slots < 0) return IM2WIN_ERR_INVALID_ARG;
   if (!s->cu && tokens % sequences != 0) return IM2WIN_ERR_INVALID_ARG;
   if ((pools || s->slots) && slots < 1) return IM2WIN_ERR_INVALID_ARG;
+  if (tokens > kMostRows || sequences > kMostRows) return IM2WIN_ERR_UNSUPPORTED;
   if (pools && !s->slots && slots < sequences) return IM2WIN_ERR_INVALID_ARG;
   if (!aligned_to(s->cu, 4) || !aligned_to(s->slots, 4)) return IM2WIN_ERR_MISALIGNED;
   return IM2WIN_OK;
@@ -36,7 +38,9 @@ im2win_status check_attention(const im2win_attention_shape* s, im2win_dtype dtyp
   if (!known_dtype(dtype) || s->tokens < 0 || s->sequences < 1 || s->slots < 0 || s->max_len < 0 || s->heads < 1 ||
       s->qk_heads < 1 || s->heads % s->qk_heads != 0 || s->dk < 1 || s->dv < 1)
     return IM2WIN_ERR_INVALID_ARG;
-  if (s->dk > 256 || (int64_t)s->heads * s->dv >= kMost || (int64_t)s->heads * s->dk >= kMost) return IM2WIN_ERR_UNSUPPORTED;
+  if (s->tokens > kMostRows || s->sequences > kMostRows || s->dk > 256 || (int64_t)s->heads * s->dv >= kMost ||
+      (int64_t)s->heads * s->dk >= kMost)
+    return IM2WIN_ERR_UNSUPPORTED;
   return IM2WIN_OK;
 }
 
