@@ -396,9 +396,10 @@ typedef struct {
  * zeros) and no row of another sequence is ever met.  x, weight [channels]
  * [taps], y and the states [slots][taps-1][channels] hold elements of `dtype`
  * (any of the three); bias holds floats or is NULL.  Sums are fp32, y is
- * rounded once, states are copied bit for bit.  `seqs` may be NULL.  The
- * pointers need the alignment of their elements only; rows that start on
- * 16-byte boundaries and hold whole 16-byte vectors are the fast ones.
+ * rounded once (with silu, y of less than 2^-119 may come out as 0), states are
+ * copied bit for bit.  `seqs` may be NULL.  The pointers need the alignment of
+ * their elements only; rows that start on 16-byte boundaries and hold whole
+ * 16-byte vectors are the fast ones.
  */
 im2win_status im2win_causal_conv1d(const void* x, const void* weight, const float* bias, void* y,
                                    const void* state_in, void* state_out, const im2win_sequences* seqs,
@@ -433,27 +434,33 @@ typedef struct {
  * undefined, but nothing outside the buffers is read or written.
  *
  * fp32 rows, dk above 128, single tokens and the shortest prompts run the
- * recurrence as it stands, in fp32.  Others go by chunks of 64 tokens on the
- * tensor cores: there the weights of a chunk's tokens for one another and the
- * copy of the state that meets q are rounded once to `dtype` (sums are fp32, in
- * fp16 a row's weights and a column of the state are scaled to the type's range
- * and what is below 2^-27 of their largest loses bits), which puts o off by
- * about as much as its own rounding does; rows of q, k and v that start on 16-byte
- * boundaries, and dk and dv of multiples of 8, are the fast ones.  The
- * states are fp32 throughout, to within a few units of the last place of the
- * magnitudes that add up to an element; in fp16 what 64 tokens add is off by up
- * to 2^-62 of their largest element of k, decayed up to the last of them, for
- * every v it meets besides (an element that only far weaker tokens feed shows
- * it).  Sums are in a fixed order: the same call gives the same bits.  An
- * infinity or NaN of a row reaches no row before it; where infinities of both
- * signs meet, whether that gives an infinity or a NaN depends on the order of
- * sums.
+ * recurrence as it stands, in fp32: a block for a head (and a part of dv) of a
+ * sequence, row after row.  Its time goes by the longest sequence, 0.4 to 2
+ * microseconds a row; for prompts of thousands of rows in these forms matrix
+ * products are faster, with few heads several times.  Others go by chunks of 64
+ * tokens on the tensor cores: there the weights of a chunk's tokens for one
+ * another and the copy of the state that meets q are rounded once to `dtype`
+ * (sums are fp32, in fp16 a row's weights and a column of the state are scaled
+ * to the type's range and what is below 2^-27 of their largest loses bits),
+ * which puts o off by about as much as its own rounding does; rows of q, k and
+ * v that start on 16-byte boundaries, and dk and dv of multiples of 8, are the
+ * fast ones.  The states are fp32 throughout, to within a few units of the last
+ * place of the magnitudes that add up to an element; in fp16 what 64 tokens add
+ * is off by up to 2^-62 of their largest element of k, decayed up to the last
+ * of them, for every v it meets besides (an element that only far weaker tokens
+ * feed shows it).  Sums are in a fixed order: the same call gives the same
+ * bits.  An infinity or NaN of a row reaches no row before it; where infinities
+ * of both signs meet, whether that gives an infinity or a NaN depends on the
+ * order of sums.
  *
- * `workspace` needs the bytes of im2win_linear_attention_workspace_size; it
- * starts with a status block as a convolution's scratch does (cleared by the
- * call; see im2win_check_status).  Should a bounded wait give up, the rows of o
- * and the states that hang on it are NaN.  Nothing in it outlives the call, but calls
- * that may overlap on the GPU need one each.
+ * `workspace` needs the bytes of im2win_linear_attention_workspace_size.  They
+ * go by how the call is run and do not grow with its rows: one long sequence
+ * that is cut into segments needs megabytes, more rows in many sequences 256
+ * bytes.  Ask for each call's sizes, or take the largest of those a program
+ * makes.  It starts with a status block as a convolution's scratch does
+ * (cleared by the call; see im2win_check_status).  Should a bounded wait give
+ * up, the rows of o and the states that hang on it are NaN.  Nothing in it
+ * outlives the call, but calls that may overlap on the GPU need one each.
  */
 im2win_status im2win_linear_attention_workspace_size(const im2win_attention_shape* shape, im2win_dtype dtype, size_t* bytes);
 im2win_status im2win_linear_attention(const void* q, const void* k, const void* v, const float* log_decay, void* o,
@@ -481,12 +488,13 @@ typedef struct {
  * of `weight` [N][(K+1)/2]; z from `zeros` [N][ceil(K/group)] (bytes, taken
  * modulo 16), or 8 where `zeros` is NULL.  x [M][K], scales [N][ceil(K/group)]
  * and y [M][N] hold elements of `dtype` (any of the three); bias holds floats
- * or is NULL.  (w - z) and its products with x are exact, sums are fp32, a
+ * or is NULL.  (w - z) and its products with x are exact (of fp32 rows x to
+ * within 2^-133: of less than 2^-110 the last bits go), sums are fp32, a
  * group's sum is multiplied by its scale in fp32, y is rounded once; the order
  * of sums is fixed by the shape.  Without a workspace there is no status block:
- * should a bounded wait give up, the y that hang on it are NaN.  The pointers need the alignment of their
- * elements only; rows of x and of the matrix that start on 16-byte boundaries
- * are the fast ones.
+ * should a bounded wait give up, the y that hang on it are NaN.  The pointers
+ * need the alignment of their elements only; rows of x and of the matrix that
+ * start on 16-byte boundaries are the fast ones.
  */
 im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros,
                                  const float* bias, void* y, const im2win_int4_shape* shape, im2win_dtype dtype,

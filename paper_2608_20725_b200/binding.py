@@ -522,7 +522,7 @@ def im2win_causal_conv1d(x, weight, y, bias=None, silu: bool = False, state=None
 
 
 def make_attention_shape(tokens, sequences, heads, qk_heads, dk, dv, max_len=0) -> AttentionShape:
-    """The sizes that im2win_linear_attention's workspace depends on."""
+    """The sizes that im2win_linear_attention's workspace depends on (all of them: fewer tokens may need more of it)."""
     return AttentionShape(int(tokens), int(sequences), 0, int(max_len), int(heads), int(qk_heads), int(dk), int(dv), 1.0, 0, 0, 0, 0, 0)
 
 

@@ -27,8 +27,9 @@
 // What bounds it: a chunk of 64 tokens (128 x 128, bf16) takes 2.5 us of an SM; its 64 KB take 1.5 us of an SM's part of the memory's
 // bandwidth and its products 0.7 us of the tensor cores.  The rest is the workers' instructions (pieces of k, S, P, o: half of the issue slots)
 // and what they wait for each other: pieces and S of the next chunk cannot start before this one's products are done.  One sequence of 16384
-// tokens, 32 heads of 128 x 128: 296 us (83 at 6.53 TB/s for rows read and written once), of which the segments' own sums are 100;
-// 13 sequences of 9001 tokens, 24 heads of 64 x 128, fp16: 117 (22).
+// tokens, 32 heads of 128 x 128: 298 us (83 at 6.53 TB/s for rows read and written once), of which the segments' own sums are 100;
+// 13 sequences of 9001 tokens, 24 heads of 64 x 128, fp16: 120 (22).  fp16 pays for its range: scales for k, for the rows of P and for the
+// columns of S, and a third piece of k (16384 tokens, 32 heads of 128 x 128: 385 us, 357 with two pieces).
 //
 // Long sequences are cut into segments of several chunks where there are too few heads and sequences for the GPU: one launch sums up
 // what each segment adds to a zero state, a second one runs over the segments of a sequence and leaves each one's starting state, and
@@ -52,7 +53,8 @@ constexpr int kChunk = 64;               // tokens
 constexpr int kThreads = 512;           // that have a part of S; two more warps
 constexpr int kAllThreads = kThreads + 128;
 // Registers: 640 threads are launched with 96 each; four warpgroups of workers take what the fifth gives back (512 x 104 + 128 x 64).
-// With 96 the workers spill, to the L2 cache: shared memory leaves none of the first level.
+// What the workers spill goes to the L2 cache, since shared memory leaves none of the first level: with dk 128 some 40 bytes a thread
+// even so, in bf16 and fp16.
 constexpr int kWorkerRegisters = 104, kHelperRegisters = 64;
 constexpr int kQuarters = kThreads / 128; // parts of dk, and of a chunk's tokens, of the threads that have a column of dv
 constexpr int kStages = 3;
@@ -1025,9 +1027,10 @@ struct ChunkPlan {
 
 // Segments by an estimate, in chunks' times (2.6 us): a launch takes as long as its rounds of the longest pieces, or as all of its
 // work spread over 148 SMs if that is longer, four for the start and end of a block; where sequences are cut, what the segments but the
-// last add comes before, at 0.65 of the time, and two more launches.  (One sequence of 16384 tokens, 32 heads of 128 x 128: 256 chunks in
-// one piece 636 us, in 2, 4, 9, 18 segments 543, 303, 312, 378; 13 sequences of up to 2488, 24 heads of 64 x 128: 1, 2, 3 segments 140,
-// 196, 173.)
+// last add comes before, at 0.65 of the time, and two more launches.  (One sequence of 16384 tokens, 32 heads of 128 x 128, bf16: 256
+// chunks in one piece 628 us, in 2, 4, 5, 8, 9, 12, 18 segments 547, 301, 377, 321, 298, 343, 338: the estimate takes 9.  Of 8192 tokens 1,
+// 2, 4, 5, 9: 322, 294, 173, 215, 186: it takes 4.  13 sequences of up to 2488, 24 heads of 64 x 128, fp16: 1, 2, 3 segments 121, 182, 158:
+// it takes 1.)
 ChunkPlan plan_chunks(const im2win_attention_shape& s, im2win_dtype dtype, bool has_cu) {
   ChunkPlan c = {};
   const int64_t longest = has_cu ? (s.max_len > 0 ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens) : s.tokens / s.sequences;

@@ -7,7 +7,10 @@
 // and every thread has its R loads under way at once.  o is the sum over the warps' rows, through shared memory, in their order.
 //
 // One token of each of 128 sequences, 32 heads of 128 x 128: 93 us, 5.7 TB/s of states (81 at the measured 6.53).  Prompts run here in
-// fp32 and with dk above 128: 0.4 us a token (412 tokens of heads of 48 x 80), 0.7 (128 x 128), the latency of a token's loads, sums and barrier.
+// fp32 and with dk above 128: 0.4 us a token (412 tokens of heads of 48 x 80), 0.7 (128 x 128), 1.9 (256 x 128), the latency of a token's
+// loads, sums and barrier.  A sequence is one block's, however long and however much of the GPU is idle: 16384 tokens of 128 x 128 in fp32 take
+// 10.8 ms with 8 heads as with 32, and 30.6 ms with 32 heads of 256 x 128 in bf16, where the formula by chunks in plain matrix products
+// takes 2.5, 8.2 and 14.3.
 //
 // exp(g) as a float is off by up to 2^-25 of itself, the same way at every token of a head whose decay is constant: after n tokens n
 // times as much.  Decays near 1, which remember many tokens, are therefore applied as S + S (exp(g) - 1), whose error is that of the
