@@ -6,11 +6,13 @@
 // matrix x 8 columns of x x 16 terms): w - z lies in -15..15, which both 16-bit types hold exactly, and so are the products; a group's
 // sum comes out of the accumulators in fp32 and meets its scale there.  Making the 16-bit numbers takes 11 instructions for eight weights.
 // What bounds it now: the instructions around the products (making the numbers, scales, sums), which take half of the issue slots, and
-// what they wait for.  28672 x 8192, whose 117 MB the ring below alone brings in 26 us (18 at the measured bandwidth): 76 us with groups
-// of 64, zero points, 8 rows.  Between events around the call, which counts some 6 us more: 59 us with groups of 128, 96 with 32, 82 with
-// 64 and zero points, 64 there with scales that are not loaded.  The products themselves are hidden: a quarter of an SM makes one in 9
-// cycles, and without them the times are the same.  Paired fp32 multiply-adds in their place were slower
-// from one row on (80, 127, 224 us for 1, 2, 4 rows).
+// what they wait for.  28672 x 8192, whose 117 MB the ring below alone brings in 26 us (18 at the measured bandwidth), 8 rows of bf16, calls
+// from a graph: 73 us with groups of 64 and zero points, 68 without these, 56 with groups of 128, 92 with 32; groups of 128 with 1, 2, 4, 16
+// rows 54, 55, 55, 85; 8 rows of fp32 127.  Between events around a single call, which counts some 6 us more, groups of 64 with zero points
+// took 82, and 64 with scales that were not loaded: they are single loads of 2 to 16 bytes, rows apart.  The products themselves are hidden: a
+// quarter of an SM makes one in 9 cycles, and without them the times are the same.  Paired fp32 multiply-adds in their place were slower from
+// one row on (80, 127, 224 us for 1, 2, 4 rows).  Registers are at their limit of 128: groups of 64 with up to 8 columns of x spill 44 bytes in
+// bf16 and 12 in fp16, the forms of 16 and 24 columns up to 40 and 96.
 //
 // The order of the terms of a product is free as long as both operands agree.  Lane (g = lane/4, t = lane%4) holds rows g and g+8 of
 // a tile of the matrix and the t-th of four equal parts of a group's elements, so that it loads neighbouring bytes; of a word's eight
@@ -22,7 +24,7 @@
 // comes through a ring of kSlots such chunks in shared memory, row by row (bulk copies; loads to registers two blocks ahead took 100 us in
 // the place of 84).  Rows of more than a pass of K (4096 elements for 8 columns of x, 2048 for more columns or for groups of 32:
 // what registers hold; 8192 spilled, 90 us in the place of 82) go in passes, whose sums are kept for kMostGroups tiles at a time.  Rows that do not start on 16-byte boundaries, and a K that is no
-// multiple of 128, go through registers (matvec_any_kernel).
+// multiple of 128, go through registers (matvec_any_kernel), and so do scales or zero points that cannot be loaded a block at once.
 #include <stdlib.h>
 
 #include <type_traits>
