@@ -427,11 +427,10 @@ typedef struct {
  * q and k are [tokens][qk_heads][dk], v and o [tokens][heads][dv], with
  * elements of `dtype` (any of the three) and the heads of a row one behind the
  * other; log_decay holds floats (normally <= 0; -infinity empties the state;
- * those above 0 may add up to 80 over 64 tokens in a row, beyond which weights
- * overflow);
- * the states [slots][heads][dk][dv] are fp32 and 16-byte aligned, and so is
- * `workspace`.  A max_len below the longest sequence's rows leaves results
- * undefined, but nothing outside the buffers is read or written.
+ * those above 0 may add up to 70 over 64 tokens in a row, beyond which weights
+ * overflow); the states [slots][heads][dk][dv] are fp32 and 16-byte aligned,
+ * and so is `workspace`.  A max_len below the longest sequence's rows leaves
+ * results undefined, but nothing outside the buffers is read or written.
  *
  * fp32 rows, dk above 128, single tokens and the shortest prompts run the
  * recurrence as it stands, in fp32: a block for a head (and a part of dv) of a

@@ -107,3 +107,16 @@ def test_columns_of_a_state_that_differ_by_2_to_the_100(dtype, dk, dv):
         st[:, :, :, 0] = 0.0
         st[:, :, 0, 0] = 1e30
     run(dtype, [100], 2, 2, dk, dv, edit=edit)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dk", [64, 128])
+def test_decays_that_grow_as_far_as_they_may(dtype, dk):
+    """e^69 in a chunk, met by the largest k of fp16: weighted ones of 2^115.  scale brings the last rows into the type's range."""
+    def edit(q, k, v, g, st):
+        g.fill_(1.08)
+        k[3] = 65504.0
+        k[20] = -65504.0
+        v.mul_(2.0 ** -10)
+        st.mul_(2.0 ** -10)
+    run(dtype, [64], 2, 1, dk, 64, edit=edit, scale=2.0 ** -118)
