@@ -504,6 +504,106 @@ im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const voi
  */
 const char* im2win_matvec_int4_kernel_name(const im2win_int4_shape* shape, im2win_dtype dtype);
 
+typedef struct {
+  int32_t tokens;             /* rows of q, k, v, log_decay, beta and o (>= 0)            */
+  int32_t sequences;          /* >= 1; divides tokens where there is no cu_seqlens        */
+  int32_t slots;              /* states in each pool; 0 without pools and without slots   */
+  int32_t max_len;            /* rows of the longest sequence, or 0: unknown              */
+  int32_t heads;              /* heads of v and o                                         */
+  int32_t qk_heads;           /* heads of q and k; divides heads                          */
+  int32_t dk, dv;             /* elements of a q or k row (1 to 256), of a v or o row     */
+  int32_t normalize;          /* 1: rows of q and k of each head are divided by their norm */
+  float scale;
+  int64_t q_stride, k_stride, v_stride, o_stride;     /* elements from a row to the next  */
+  int64_t decay_stride;       /* floats from a row of log_decay to the next; 0: one decay
+                                 for each head, the same for every token                  */
+  int64_t beta_stride;        /* the same of beta                                         */
+} im2win_delta_shape;
+
+/*
+ * The gated delta rule.  Head h of a row t of sequence b, with q and k of head
+ * h / (heads / qk_heads) and a = exp(log_decay[t][h]):
+ *     u_t = beta[t][h] * (v_t - k_t a S_{t-1}),
+ *     S_t = a S_{t-1} + k_t^T u_t,                       S [dk][dv],
+ *     o_t = scale * q_t S_t,
+ * where normalize divides each q_t and k_t by sqrt(its sum of squares + 1e-6).
+ * Layouts, types and states are those of im2win_linear_attention; beta holds
+ * floats, for each token and head or each head (normally 0 to 1).  There is no
+ * workspace.  log_decay is normally <= 0 (-infinity empties the state; those
+ * above 0 may add up to 70 over 64 tokens in a row).  A max_len below the
+ * longest sequence's rows changes which way the call is run, not its results.
+ *
+ * Sums and states are fp32.  An infinity or NaN in a column of v, or of a
+ * state, makes that column of o from its row on, and of the state, infinities
+ * or NaNs (which of them is not defined); one of k, beta or log_decay (but
+ * -infinity) all of the head's, one of q its row of o.  It reaches no row
+ * before it.  The order of sums is fixed by the shape.
+ */
+im2win_status im2win_gated_delta_rule(const void* q, const void* k, const void* v, const float* log_decay, const float* beta,
+                                      void* o, const float* state_in, float* state_out, const im2win_sequences* seqs,
+                                      const im2win_delta_shape* shape, im2win_dtype dtype, void* cuda_stream);
+/*
+ * How a call with cu_seqlens runs such a shape (host-only, static storage; for reports and tests): "tokens" (the recurrence);
+ * "none" for an invalid shape.
+ */
+const char* im2win_gated_delta_rule_kernel_name(const im2win_delta_shape* shape, im2win_dtype dtype);
+
+typedef struct {
+  int32_t rows;               /* >= 0                                                     */
+  int32_t channels;           /* elements of a row (>= 1)                                 */
+  float eps;                  /* >= 0                                                     */
+  int64_t x_stride, residual_stride, residual_out_stride, y_stride;  /* elements from a row to the next (>= channels) */
+} im2win_norm_shape;
+
+/*
+ * Root-mean-square norm of rows, behind the addition of a residual, into their
+ * type or into 8 bits:
+ *     h = x + residual,                        added in fp32 and rounded to `dtype`
+ *     y = h * weight / sqrt(mean(h^2) + eps),
+ * over the channels of a row.  x, residual, weight [channels], residual_out
+ * (receives h) and y hold elements of `dtype` (any of the three).  residual
+ * and, with it, residual_out may be NULL, weight too (ones).  With `scales`
+ * [rows] (floats), y holds bytes instead, two's complement:
+ *     y = the whole number nearest to 127 h weight / max |h weight|  (ties to the even one),
+ *     scales = max |h weight| / (127 sqrt(mean(h^2) + eps)),
+ * so that y * scales is the normed row; which number is nearest is decided
+ * exactly, whatever the order of sums.  Rows of zeros are zeros, with a scale
+ * of 0; rows that hold an infinity or NaN (or whose h * weight passes the range
+ * of floats) are zeros with a scale of NaN.  Sums are fp32, y is rounded once.
+ * residual_out may be x or residual, and y (without scales) may be x or
+ * residual where residual_out is not, each with the same stride; other overlaps
+ * are not allowed.  The pointers need the alignment of their elements only; rows that
+ * start on 16-byte boundaries and hold whole 16-byte vectors are the fast ones.
+ */
+im2win_status im2win_rms_norm(const void* x, const void* residual, const void* weight, void* residual_out, void* y, float* scales,
+                              const im2win_norm_shape* shape, im2win_dtype dtype, void* cuda_stream);
+
+typedef struct {
+  int32_t M, N, K;            /* x [M][K] (M >= 0), matrix [N][K], y [M][N]               */
+  int64_t x_stride;           /* bytes from a row of x to the next one (>= K)             */
+  int64_t y_stride;           /* elements from a row of y to the next one (>= N)          */
+} im2win_int8_shape;
+
+/*
+ * Rows times a matrix, both in 8-bit integers (-128 to 127), with a scale for
+ * each row and each row of the matrix (a 1x1 layer whose positions are the
+ * rows):
+ *     y[m][n] = bias[n] + x_scales[m] * scales[n] * sum_k x[m][k] * weight[n][k].
+ * weight [N][K] is dense; x_scales [M], scales [N] and bias [N] (or NULL) hold
+ * floats, y elements of `dtype` (any of the three).  The sum is exact (32 bits:
+ * K of at most 131071), its conversion to fp32, products with the scales and
+ * the bias's addition are fp32, y is rounded once.  The pointers need the
+ * alignment of their elements only; rows of x and of the matrix that start on
+ * 16-byte boundaries (K a multiple of 16) are the fast ones.
+ */
+im2win_status im2win_matmul_int8(const int8_t* x, const float* x_scales, const int8_t* weight, const float* scales, const float* bias,
+                                 void* y, const im2win_int8_shape* shape, im2win_dtype dtype, void* cuda_stream);
+/*
+ * How a call whose pointers start on 16-byte boundaries runs such a shape (host-only, static storage; for reports and tests):
+ * "registers"; "none" for an invalid shape.
+ */
+const char* im2win_matmul_int8_kernel_name(const im2win_int8_shape* shape, im2win_dtype dtype);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,7 +32,8 @@ EXPORTS = (
     "im2win_nhwc_workspace_size", "im2win_transform_nhwc", "im2win_conv_f16_nhwc", "im2win_pack_filter_nhwc",
     "im2win_conv_packed_nhwc", "im2win_causal_conv1d", "im2win_linear_attention",
     "im2win_linear_attention_workspace_size", "im2win_linear_attention_kernel_name", "im2win_matvec_int4",
-    "im2win_matvec_int4_kernel_name",
+    "im2win_matvec_int4_kernel_name", "im2win_gated_delta_rule", "im2win_gated_delta_rule_kernel_name", "im2win_rms_norm",
+    "im2win_matmul_int8", "im2win_matmul_int8_kernel_name",
 )
 
 STATIC_SCRATCH_BYTES = 4 << 20
@@ -72,6 +73,21 @@ class AttentionShape(ctypes.Structure):
 
 class Int4Shape(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int32) for k in ("M", "N", "K", "group")] + [(k, ctypes.c_int64) for k in ("x_stride", "y_stride")]
+
+
+class DeltaShape(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("tokens", "sequences", "slots", "max_len", "heads", "qk_heads", "dk", "dv", "normalize")] + \
+               [("scale", ctypes.c_float)] + \
+               [(k, ctypes.c_int64) for k in ("q_stride", "k_stride", "v_stride", "o_stride", "decay_stride", "beta_stride")]
+
+
+class NormShape(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("rows", "channels")] + [("eps", ctypes.c_float)] + \
+               [(k, ctypes.c_int64) for k in ("x_stride", "residual_stride", "residual_out_stride", "y_stride")]
+
+
+class Int8Shape(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("M", "N", "K")] + [(k, ctypes.c_int64) for k in ("x_stride", "y_stride")]
 
 
 class Im2winError(RuntimeError):
@@ -117,6 +133,9 @@ def lib() -> ctypes.CDLL:
     L.im2win_linear_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, ctypes.c_int, vp]
     L.im2win_linear_attention_workspace_size.argtypes = [P(AttentionShape), ctypes.c_int, P(sz)]
     L.im2win_matvec_int4.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp]
+    L.im2win_gated_delta_rule.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp]
+    L.im2win_rms_norm.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp]
+    L.im2win_matmul_int8.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp]
     for name in EXPORTS[1:]:
         getattr(L, name).restype = ctypes.c_int
     L.im2win_conv_kernel_name.restype = ctypes.c_char_p
@@ -126,6 +145,10 @@ def lib() -> ctypes.CDLL:
     L.im2win_linear_attention_kernel_name.restype = ctypes.c_char_p
     L.im2win_matvec_int4_kernel_name.argtypes = [P(Int4Shape), ctypes.c_int]
     L.im2win_matvec_int4_kernel_name.restype = ctypes.c_char_p
+    L.im2win_gated_delta_rule_kernel_name.argtypes = [P(DeltaShape), ctypes.c_int]
+    L.im2win_gated_delta_rule_kernel_name.restype = ctypes.c_char_p
+    L.im2win_matmul_int8_kernel_name.argtypes = [P(Int8Shape), ctypes.c_int]
+    L.im2win_matmul_int8_kernel_name.restype = ctypes.c_char_p
     # the library looks at IM2WIN_DEBUG in its first plan: here, so that both sides see the same
     _debug = bool(os.environ.get("IM2WIN_DEBUG"))
     L.im2win_conv_kernel_name(ctypes.byref(Shape(1, 64, 1, 1, 1, 1, 1, 1, 0)), F32)
@@ -402,6 +425,9 @@ _pack_sequences = struct.Struct("@3P").pack
 _pack_conv1d = struct.Struct("@6i2q").pack
 _pack_attention = struct.Struct("@8if5q").pack
 _pack_int4 = struct.Struct("@4i2q").pack
+_pack_delta = struct.Struct("@9if6q").pack
+_pack_norm = struct.Struct("@2if4x4q").pack
+_pack_int8 = struct.Struct("@3i4x2q").pack
 
 
 def _sequence_dtype(dtype: torch.dtype) -> int:
@@ -614,6 +640,114 @@ def im2win_matvec_int4(x, weight, scales, y, group: int, zeros=None, bias=None, 
 def im2win_matvec_int4_kernel_name(m: int, n: int, k: int, group: int, dtype: int, x_stride: int = 0) -> str:
     """How im2win_matvec_int4 runs these sizes where tensors start on 16-byte boundaries (for reports and tests)."""
     return lib().im2win_matvec_int4_kernel_name(ctypes.byref(Int4Shape(m, n, k, group, x_stride or k, n)), dtype).decode()
+
+
+def make_delta_shape(tokens, sequences, heads, qk_heads, dk, dv, max_len=0) -> DeltaShape:
+    """The sizes that im2win_gated_delta_rule_kernel_name looks at."""
+    return DeltaShape(int(tokens), int(sequences), 0, int(max_len), int(heads), int(qk_heads), int(dk), int(dv), 0, 1.0, 0, 0, 0, 0, 0, 0)
+
+
+def im2win_gated_delta_rule_kernel_name(shape: DeltaShape, dtype: int) -> str:
+    """How im2win_gated_delta_rule runs these sizes (for reports and tests)."""
+    return lib().im2win_gated_delta_rule_kernel_name(ctypes.byref(shape), dtype).decode()
+
+
+def _by_token_or_head(t, heads: int, rows, tokens: int, name: str) -> int:
+    """Floats from a row of t ([..., tokens, heads], or [heads]) to the next one; 0: one value for each head."""
+    shape = t.shape
+    if t.dtype != torch.float32 or (shape != rows and shape != (heads,)):
+        raise ValueError(f"{name}: [..., tokens, heads] or [heads] of float32")
+    if tokens > 0 and len(shape) > 1 and t.is_contiguous():
+        return heads
+    if len(shape) == 1 or (tokens > 1 and all(n == 1 or step == 0 for n, step in zip(shape[:-1], t.stride()))):
+        if heads > 1 and t.stride(-1) != 1:                  # (one value for each head may be an expanded view)
+            raise ValueError(f"{name}: the heads have to lie one behind the other")
+        return 0
+    return _row_stride(t, 1, name)
+
+
+def im2win_gated_delta_rule(q, k, v, log_decay, beta, o, scale: float = 1.0, normalize: bool = False, state=None, state_out=None,
+                            cu_seqlens=None, slots=None, resume=None, max_len: int = 0, stream=None) -> None:
+    """The gated delta rule into o: q and k [tokens, qk_heads, dk] or [sequences, tokens, qk_heads, dk], v and o the same with heads and dv,
+    log_decay and beta float32 [tokens, heads] (or [sequences, tokens, heads]) or [heads], state and state_out float32 [slots, heads, dk,
+    dv] (may be one tensor)."""
+    dtype = q.dtype
+    code = _sequence_dtype(dtype)
+    _on_current_device(q, k, v, log_decay, beta, o, state, state_out, cu_seqlens, slots, resume)
+    if k.dtype != dtype or v.dtype != dtype or o.dtype != dtype:
+        raise ValueError("q, k, v and o have to be of one dtype")
+    qs, vs = q.shape, v.shape
+    if not 3 <= len(qs) <= 4 or k.shape != qs or o.shape != vs or vs[:-2] != qs[:-2]:
+        raise ValueError("q and k: [..., tokens, qk_heads, dk], v and o: [..., tokens, heads, dv]")
+    qk_heads, dk = qs[-2:]
+    heads, dv = vs[-2:]
+    for p in (state, state_out):
+        if p is not None and (p.dtype != torch.float32 or p.dim() != 4 or p.shape[1] != heads or p.shape[2] != dk or p.shape[3] != dv):
+            raise ValueError("state and state_out: [slots, heads, dk, dv] of float32")
+    tokens, sequences, pool, seqs = _take_sequences(qs[:-2], cu_seqlens, slots, resume, state, state_out)
+    sizes = _pack_delta(tokens, sequences, pool, max_len, heads, qk_heads, dk, dv, 1 if normalize else 0, scale, _row_stride(q, 2, "q"),
+                        _row_stride(k, 2, "k"), _row_stride(v, 2, "v"), _row_stride(o, 2, "o"),
+                        _by_token_or_head(log_decay, heads, vs[:-1], tokens, "log_decay"), _by_token_or_head(beta, heads, vs[:-1], tokens, "beta"))
+    code = (_lib or lib()).im2win_gated_delta_rule(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), beta.data_ptr(), o.data_ptr(),
+                                                   _ptr(state), _ptr(state_out), seqs, sizes, code, _stream(stream))
+    if code:
+        _check(code, "im2win_gated_delta_rule")
+
+
+def im2win_rms_norm(x, weight, y, scales=None, residual=None, residual_out=None, eps: float = 1e-6, stream=None) -> None:
+    """Root-mean-square norm of x (+ residual, their sum into residual_out) into y: all [rows, channels] of one dtype, weight [channels] or
+    None.  With scales, float32 [rows], y is int8 and y * scales the normed rows."""
+    dtype = x.dtype
+    code = _sequence_dtype(dtype)
+    _on_current_device(x, weight, y, scales, residual, residual_out)
+    shape = x.shape
+    if len(shape) != 2 or y.shape != shape or shape[1] < 1:
+        raise ValueError("x and y: [rows, channels]")
+    rows, channels = shape
+    if y.dtype != (dtype if scales is None else torch.int8):
+        raise ValueError("y: of x's dtype, or with scales of int8")
+    if scales is not None and (scales.dtype != torch.float32 or scales.shape != (rows,) or not scales.is_contiguous()):
+        raise ValueError("scales: [rows] of float32")
+    if weight is not None and (weight.dtype != dtype or weight.shape != (channels,) or not weight.is_contiguous()):
+        raise ValueError("weight: [channels] of x's dtype")
+    if residual is None and residual_out is not None:
+        raise ValueError("residual_out goes with a residual")
+    for t in (residual, residual_out):
+        if t is not None and (t.dtype != dtype or t.shape != shape):
+            raise ValueError("residual and residual_out: like x")
+    sizes = _pack_norm(rows, channels, eps, _row_stride(x, 1, "x"), 0 if residual is None else _row_stride(residual, 1, "residual"),
+                       0 if residual_out is None else _row_stride(residual_out, 1, "residual_out"), _row_stride(y, 1, "y"))
+    code = (_lib or lib()).im2win_rms_norm(x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(residual_out), y.data_ptr(), _ptr(scales), sizes, code,
+                                           _stream(stream))
+    if code:
+        _check(code, "im2win_rms_norm")
+
+
+def im2win_matmul_int8(x, x_scales, weight, scales, y, bias=None, stream=None) -> None:
+    """Rows times a matrix in 8-bit integers into y: x int8 [M, K], x_scales float32 [M], weight int8 [N, K], scales float32 [N], bias float32
+    [N], y [M, N]."""
+    code = _sequence_dtype(y.dtype)
+    _on_current_device(x, x_scales, weight, scales, y, bias)
+    if x.dim() != 2 or y.dim() != 2 or x.shape[0] != y.shape[0] or x.dtype != torch.int8:
+        raise ValueError("x: int8 [M, K], y: [M, N]")
+    (m, k), n = x.shape, y.shape[1]
+    if n < 1 or k < 1:
+        raise ValueError("N and K have to be positive")
+    if weight.dtype != torch.int8 or weight.shape != (n, k) or not weight.is_contiguous():
+        raise ValueError("weight: [N, K] of int8, contiguous")
+    for t, size, name in ((x_scales, m, "x_scales: [M]"), (scales, n, "scales: [N]"), (bias, n, "bias: [N]")):
+        if (t is not None or name[0] != "b") and (t.dtype != torch.float32 or t.shape != (size,) or not t.is_contiguous()):
+            raise ValueError(name + " of float32")
+    sizes = _pack_int8(m, n, k, _row_stride(x, 1, "x"), _row_stride(y, 1, "y"))
+    code = (_lib or lib()).im2win_matmul_int8(x.data_ptr(), x_scales.data_ptr(), weight.data_ptr(), scales.data_ptr(), _ptr(bias), y.data_ptr(),
+                                              sizes, code, _stream(stream))
+    if code:
+        _check(code, "im2win_matmul_int8")
+
+
+def im2win_matmul_int8_kernel_name(m: int, n: int, k: int, dtype: int, x_stride: int = 0) -> str:
+    """How im2win_matmul_int8 runs these sizes where tensors start on 16-byte boundaries (for reports and tests)."""
+    return lib().im2win_matmul_int8_kernel_name(ctypes.byref(Int8Shape(m, n, k, x_stride or k, n)), dtype).decode()
 
 
 # ---------------------------------------------------------------- conveniences

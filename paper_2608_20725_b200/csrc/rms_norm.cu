@@ -1,0 +1,264 @@
+// Root-mean-square norm of rows behind the addition of a residual, into their type or into 8 bits (im2win_rms_norm):
+//
+//   h = x + residual (rounded),   y = h w / sqrt(mean(h^2) + eps),   or   y = nearest(127 h w / top), scale = top / (127 sqrt(..)),
+//
+// with top the largest |h w| of the row.  A row is read once: its threads keep h in registers from the sum of squares to y.  Rows that
+// no block's registers hold (above 32768 elements of 16 bits, 16384 of 32 or where rows do not lie on vectors) are read again.
+//
+// In 8 bits the root drops out of which number is nearest: h w of 16-bit elements is exact in fp32, of fp32 ones in 64 bits, and its
+// quotient by the row's largest is looked at in fp32 first; one that comes within 1e-3 of halfway between two numbers (of its 127 it is
+// off by up to 127 * 3 * 2^-24 = 2.3e-5) is divided again in 64 bits, where ties are seen as such.
+#include <float.h>
+
+#include <algorithm>
+
+#include "sequence.cuh"
+
+namespace im2win {
+namespace {
+
+struct NormParams {
+  const void* x;
+  const void* residual;
+  const void* weight;
+  void* residual_out;
+  void* y;
+  float* scales;
+  int64_t x_stride, residual_stride, residual_out_stride, y_stride;
+  int32_t rows, channels;
+  float eps;
+};
+
+// The larger one; a NaN is larger than anything.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// 127 a w / top, rounded to the nearest whole number.
+__device__ __forceinline__ int nearest(float product, float per_top, float h, float w, double top) {
+  const float t = product * per_top;
+  const float r = rintf(t);
+  if (fabsf(t - r) < 0.499f) return (int)r;
+  return (int)rint((double)h * (double)w * 127.0 / top);
+}
+
+// THREADS: of a row, 32 (a block has four rows) or all of the block's.  V: elements of a vector; N vectors a thread, or (N == 0) any
+// number, read twice.
+template <typename T, int V, int N, bool WARP>
+__global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormParams p) {
+  using VT = Vec<T, V>;
+  using VB = Vec<int8_t, V>;
+  __shared__ float shared_sum[32], shared_top[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t row = WARP ? (int64_t)blockIdx.x * 4 + warp : (int64_t)blockIdx.x;
+  if (row >= p.rows) return;                                   // (a whole warp, or nobody)
+  const int tid = WARP ? lane : (int)threadIdx.x, threads = WARP ? 32 : (int)blockDim.x;
+  const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
+  const T* residual = p.residual ? static_cast<const T*>(p.residual) + row * p.residual_stride : nullptr;
+  T* out = p.residual_out ? static_cast<T*>(p.residual_out) + row * p.residual_out_stride : nullptr;
+  const T* weight = static_cast<const T*>(p.weight);
+  const int vectors = p.channels / V;                          // (V divides the channels)
+  const bool bytes = p.scales != nullptr;
+
+  auto load = [&](int i) {
+    VT h = *reinterpret_cast<const VT*>(x + (int64_t)i * V);
+    if (residual) {
+      const VT r = *reinterpret_cast<const VT*>(residual + (int64_t)i * V);
+#pragma unroll
+      for (int j = 0; j < V; ++j) h.v[j] = from_float<T>(to_float(h.v[j]) + to_float(r.v[j]));
+    }
+    return h;
+  };
+  auto weights = [&](int i) {
+    VT w;
+    if (weight) {
+      w = *reinterpret_cast<const VT*>(weight + (int64_t)i * V);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) w.v[j] = from_float<T>(1.0f);
+    }
+    return w;
+  };
+  float sum = 0.0f, top = 0.0f;
+  auto look = [&](const VT& h, int i) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum = fmaf(to_float(h.v[j]), to_float(h.v[j]), sum);
+    if (bytes) {
+      const VT w = weights(i);
+#pragma unroll
+      for (int j = 0; j < V; ++j) top = max_nan(top, fabsf(to_float(h.v[j]) * to_float(w.v[j])));
+    }
+  };
+  VT kept[N > 0 ? N : 1];
+  if constexpr (N > 0) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (tid + n * threads < vectors) kept[n] = load(tid + n * threads);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = tid + n * threads;
+      if (i < vectors) {
+        if (out) *reinterpret_cast<VT*>(out + (int64_t)i * V) = kept[n];
+        look(kept[n], i);
+      }
+    }
+  } else {
+    for (int i = tid; i < vectors; i += threads) {
+      const VT h = load(i);
+      if (out) *reinterpret_cast<VT*>(out + (int64_t)i * V) = h;
+      look(h, i);
+    }
+  }
+#pragma unroll
+  for (int s = 16; s > 0; s /= 2) {
+    sum += __shfl_xor_sync(0xffffffffu, sum, s);
+    top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, s));
+  }
+  if constexpr (!WARP) {
+    if (lane == 0) {
+      shared_sum[warp] = sum;
+      shared_top[warp] = top;
+    }
+    __syncthreads();
+    const bool there = lane < threads / 32;
+    sum = there ? shared_sum[lane] : 0.0f;
+    top = there ? shared_top[lane] : 0.0f;
+#pragma unroll
+    for (int s = 16; s > 0; s /= 2) {
+      sum += __shfl_xor_sync(0xffffffffu, sum, s);
+      top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, s));
+    }
+  }
+  const float rate = rsqrtf(sum / (float)p.channels + p.eps);
+
+  if (!bytes) {
+    T* y = static_cast<T*>(p.y) + row * p.y_stride;
+    auto finish = [&](const VT& h, int i) {
+      const VT w = weights(i);
+      VT r;
+#pragma unroll
+      for (int j = 0; j < V; ++j) r.v[j] = from_float<T>(to_float(h.v[j]) * rate * to_float(w.v[j]));
+      *reinterpret_cast<VT*>(y + (int64_t)i * V) = r;
+    };
+    if constexpr (N > 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        if (tid + n * threads < vectors) finish(kept[n], tid + n * threads);
+    } else {
+      for (int i = tid; i < vectors; i += threads) finish(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
+    }
+    return;
+  }
+  const bool fine = top <= FLT_MAX;                            // (not of a NaN)
+  if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7fffffff) : top * rate / 127.0f;
+  // fp32: the largest product in 64 bits, and all below 2^-90: products that fp32 does not hold exactly
+  const bool in_64 = sizeof(T) == 4 || top < 8e-28f;
+  double exact_top = top;
+  if (fine && in_64) {                                         // (the same for all threads of the row)
+    double most = 0.0;
+    auto raise = [&](const VT& h, int i) {
+      const VT w = weights(i);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float a = to_float(h.v[j]), b = to_float(w.v[j]);
+        if (fabsf(a * b) == top) most = fmax(most, fabs((double)a * (double)b));
+      }
+    };
+    if constexpr (N > 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        if (tid + n * threads < vectors) raise(kept[n], tid + n * threads);
+    } else {
+      for (int i = tid; i < vectors; i += threads) raise(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
+    }
+#pragma unroll
+    for (int s = 16; s > 0; s /= 2) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, s));
+    if constexpr (!WARP) {
+      __shared__ double shared_most[32];
+      if (lane == 0) shared_most[warp] = most;
+      __syncthreads();
+      most = lane < threads / 32 ? shared_most[lane] : 0.0;
+#pragma unroll
+      for (int s = 16; s > 0; s /= 2) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, s));
+    }
+    exact_top = most;
+  }
+  int8_t* y = static_cast<int8_t*>(p.y) + row * p.y_stride;
+  const bool zero = !fine || exact_top == 0.0;
+  const bool tiny = top < 8e-28f;                              // (products lose bits, and 127 / top is out of range)
+  const float per_top = zero ? 0.0f : 127.0f / top;
+  auto finish = [&](const VT& h, int i) {
+    const VT w = weights(i);
+    VB r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float a = to_float(h.v[j]), b = to_float(w.v[j]);
+      r.v[j] = zero ? 0 : tiny ? (int8_t)rint((double)a * (double)b * 127.0 / exact_top) : (int8_t)nearest(a * b, per_top, a, b, exact_top);
+    }
+    *reinterpret_cast<VB*>(y + (int64_t)i * V) = r;
+  };
+  if constexpr (N > 0) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (tid + n * threads < vectors) finish(kept[n], tid + n * threads);
+  } else {
+    for (int i = tid; i < vectors; i += threads) finish(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
+  }
+}
+
+// Rows of up to 1024 elements (128 where they do not lie on vectors) are a warp's; others a block's of as many threads as make four
+// vectors each or fewer, and one each where there are few rows and a row's time is its latency.
+template <typename T, int V>
+cudaError_t launch(const NormParams& p, cudaStream_t stream) {
+  constexpr int kMost = V > 1 ? 4 : 16;
+  const int64_t vectors = p.channels / V;
+  if (vectors <= 128) {
+    const unsigned grid = (unsigned)(((int64_t)p.rows + 3) / 4);
+    if (vectors <= 32)
+      rms_norm_kernel<T, V, 1, true><<<grid, 128, 0, stream>>>(p);
+    else
+      rms_norm_kernel<T, V, 4, true><<<grid, 128, 0, stream>>>(p);
+    return cudaGetLastError();
+  }
+  const bool few = p.rows <= 592;
+  auto threads_for = [&](int each) { return (int)((vectors + each * 32 - 1) / (each * 32) * 32); };
+  if (few && vectors <= 1024)
+    rms_norm_kernel<T, V, 1, false><<<p.rows, threads_for(1), 0, stream>>>(p);
+  else if (vectors <= 512)
+    rms_norm_kernel<T, V, 2, false><<<p.rows, threads_for(2), 0, stream>>>(p);
+  else if (vectors <= 1024 * 4)
+    rms_norm_kernel<T, V, 4, false><<<p.rows, std::min(threads_for(4), 1024), 0, stream>>>(p);
+  else if (V == 1 && vectors <= 1024 * kMost)
+    rms_norm_kernel<T, V, kMost, false><<<p.rows, threads_for(kMost), 0, stream>>>(p);
+  else
+    rms_norm_kernel<T, V, 0, false><<<p.rows, 1024, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_type(const NormParams& p, cudaStream_t stream) {
+  constexpr int V = 16 / sizeof(T);
+  auto rows_on = [&](const void* at, int64_t stride, int64_t size) { return !at || (aligned_to(at, V * size) && stride % V == 0); };
+  if (p.channels % V == 0 && rows_on(p.x, p.x_stride, sizeof(T)) && rows_on(p.residual, p.residual_stride, sizeof(T)) &&
+      rows_on(p.residual_out, p.residual_out_stride, sizeof(T)) && rows_on(p.weight, 0, sizeof(T)) &&
+      rows_on(p.y, p.y_stride, p.scales ? 1 : sizeof(T)))
+    return launch<T, V>(p, stream);
+  return launch<T, 1>(p, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_rms_norm(const void* x, const void* residual, const void* weight, void* residual_out, void* y, float* scales,
+                            const im2win_norm_shape& s, im2win_dtype dtype, cudaStream_t stream) {
+  const NormParams p = {x, residual, weight, residual_out, y, scales, s.x_stride, s.residual_stride, s.residual_out_stride, s.y_stride,
+                        s.rows, s.channels, s.eps};
+  switch (dtype) {
+    case IM2WIN_F32: return launch_type<float>(p, stream);
+    case IM2WIN_F16: return launch_type<__half>(p, stream);
+    default: return launch_type<__nv_bfloat16>(p, stream);
+  }
+}
+
+}  // namespace im2win

@@ -158,4 +158,35 @@ bool matvec_by_ring(const im2win_int4_shape& s, im2win_dtype dtype);
 cudaError_t launch_matvec_int4(const void* x, const uint8_t* weight, const void* scales, const uint8_t* zeros, const float* bias,
                                void* y, const im2win_int4_shape& shape, im2win_dtype dtype, cudaStream_t stream);
 
+struct DeltaArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const float* decay;
+  const float* beta;
+  void* o;
+  const float* state_in;
+  float* state_out;
+  Sequences seqs;
+  im2win_delta_shape shape;
+  im2win_dtype dtype;
+};
+constexpr float kNormalizeEps = 1e-6f;     // added to the sum of squares of a row of q or k
+cudaError_t launch_delta_tokens(const DeltaArgs& a, cudaStream_t stream);
+
+cudaError_t launch_rms_norm(const void* x, const void* residual, const void* weight, void* residual_out, void* y, float* scales,
+                            const im2win_norm_shape& shape, im2win_dtype dtype, cudaStream_t stream);
+
+struct Int8Args {
+  const int8_t* x;
+  const float* x_scales;
+  const int8_t* weight;
+  const float* scales;
+  const float* bias;
+  void* y;
+  im2win_int8_shape shape;
+  im2win_dtype dtype;
+};
+cudaError_t launch_matmul_int8_registers(const Int8Args& a, cudaStream_t stream);
+
 }  // namespace im2win

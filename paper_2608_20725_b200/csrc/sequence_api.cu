@@ -53,6 +53,24 @@ im2win_status check_int4(const im2win_int4_shape* s, im2win_dtype dtype) {
   return IM2WIN_OK;
 }
 
+im2win_status check_delta(const im2win_delta_shape* s, im2win_dtype dtype) {
+  if (!s) return IM2WIN_ERR_NULL_POINTER;
+  if (!known_dtype(dtype) || s->tokens < 0 || s->sequences < 1 || s->slots < 0 || s->max_len < 0 || s->heads < 1 ||
+      s->qk_heads < 1 || s->heads % s->qk_heads != 0 || s->dk < 1 || s->dv < 1 || (s->normalize != 0 && s->normalize != 1))
+    return IM2WIN_ERR_INVALID_ARG;
+  if (s->tokens > kMostRows || s->sequences > kMostRows || s->dk > 256 || (int64_t)s->heads * s->dv >= kMost ||
+      (int64_t)s->heads * s->dk >= kMost)
+    return IM2WIN_ERR_UNSUPPORTED;
+  return IM2WIN_OK;
+}
+
+im2win_status check_int8(const im2win_int8_shape* s, im2win_dtype dtype) {
+  if (!s) return IM2WIN_ERR_NULL_POINTER;
+  if (!known_dtype(dtype) || s->M < 0 || s->N < 1 || s->K < 1 || s->x_stride < s->K || s->y_stride < s->N) return IM2WIN_ERR_INVALID_ARG;
+  if (s->K > 131071 || s->M > kMostRows || s->N > kMostRows) return IM2WIN_ERR_UNSUPPORTED;
+  return IM2WIN_OK;
+}
+
 }  // namespace
 }  // namespace im2win
 
@@ -143,6 +161,67 @@ im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const voi
     if (!aligned_to(at, es)) return IM2WIN_ERR_MISALIGNED;
   if (!aligned_to(bias, 4)) return IM2WIN_ERR_MISALIGNED;
   return from_launch(launch_matvec_int4(x, weight, scales, zeros, bias, y, *shape, dtype, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+const char* im2win_gated_delta_rule_kernel_name(const im2win_delta_shape* shape, im2win_dtype dtype) {
+  if (check_delta(shape, dtype) != IM2WIN_OK) return "none";
+  return "tokens";
+}
+
+im2win_status im2win_gated_delta_rule(const void* q, const void* k, const void* v, const float* log_decay, const float* beta,
+                                      void* o, const float* state_in, float* state_out, const im2win_sequences* seqs,
+                                      const im2win_delta_shape* shape, im2win_dtype dtype, void* cuda_stream) {
+  im2win_status st = check_delta(shape, dtype);
+  if (st != IM2WIN_OK) return st;
+  const int64_t qk_row = (int64_t)shape->qk_heads * shape->dk, v_row = (int64_t)shape->heads * shape->dv;
+  if (shape->q_stride < qk_row || shape->k_stride < qk_row || shape->v_stride < v_row || shape->o_stride < v_row ||
+      (shape->decay_stride != 0 && shape->decay_stride < shape->heads) || (shape->beta_stride != 0 && shape->beta_stride < shape->heads))
+    return IM2WIN_ERR_INVALID_ARG;
+  DeltaArgs a = {q, k, v, log_decay, beta, o, state_in, state_out, {}, *shape, dtype};
+  st = take_sequences(seqs, shape->tokens, shape->sequences, shape->slots, state_in || state_out, &a.seqs);
+  if (st != IM2WIN_OK) return st;
+  if (shape->tokens > 0 && (!q || !k || !v || !log_decay || !beta || !o)) return IM2WIN_ERR_NULL_POINTER;
+  const size_t es = element_bytes(dtype);
+  for (const void* at : {q, k, v, (const void*)o})
+    if (!aligned_to(at, es)) return IM2WIN_ERR_MISALIGNED;
+  if (!aligned_to(log_decay, 4) || !aligned_to(beta, 4) || !aligned_to(state_in, 16) || !aligned_to(state_out, 16))
+    return IM2WIN_ERR_MISALIGNED;
+  return from_launch(launch_delta_tokens(a, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+im2win_status im2win_rms_norm(const void* x, const void* residual, const void* weight, void* residual_out, void* y, float* scales,
+                              const im2win_norm_shape* shape, im2win_dtype dtype, void* cuda_stream) {
+  if (!shape) return IM2WIN_ERR_NULL_POINTER;
+  if (!known_dtype(dtype) || shape->rows < 0 || shape->channels < 1 || !(shape->eps >= 0.0f) || shape->x_stride < shape->channels ||
+      shape->y_stride < shape->channels || (residual && shape->residual_stride < shape->channels) ||
+      (residual_out && (!residual || shape->residual_out_stride < shape->channels)))
+    return IM2WIN_ERR_INVALID_ARG;
+  if (shape->rows > kMostRows || shape->channels > kMostRows) return IM2WIN_ERR_UNSUPPORTED;
+  const size_t es = element_bytes(dtype);
+  for (const void* at : {x, residual, weight, (const void*)residual_out})
+    if (!aligned_to(at, es)) return IM2WIN_ERR_MISALIGNED;
+  if (!aligned_to(scales, 4) || (!scales && !aligned_to(y, es))) return IM2WIN_ERR_MISALIGNED;
+  if (shape->rows == 0) return IM2WIN_OK;
+  if (!x || !y) return IM2WIN_ERR_NULL_POINTER;
+  return from_launch(launch_rms_norm(x, residual, weight, residual_out, y, scales, *shape, dtype, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+const char* im2win_matmul_int8_kernel_name(const im2win_int8_shape* shape, im2win_dtype dtype) {
+  if (check_int8(shape, dtype) != IM2WIN_OK) return "none";
+  return "registers";
+}
+
+im2win_status im2win_matmul_int8(const int8_t* x, const float* x_scales, const int8_t* weight, const float* scales, const float* bias,
+                                 void* y, const im2win_int8_shape* shape, im2win_dtype dtype, void* cuda_stream) {
+  const im2win_status st = check_int8(shape, dtype);
+  if (st != IM2WIN_OK) return st;
+  if (!weight || !scales || (shape->M > 0 && (!x || !x_scales || !y))) return IM2WIN_ERR_NULL_POINTER;
+  if (!aligned_to(y, element_bytes(dtype))) return IM2WIN_ERR_MISALIGNED;
+  for (const float* at : {x_scales, scales, bias})
+    if (!aligned_to(at, 4)) return IM2WIN_ERR_MISALIGNED;
+  if (shape->M == 0) return IM2WIN_OK;
+  const Int8Args a = {x, x_scales, weight, scales, bias, y, *shape, dtype};
+  return from_launch(launch_matmul_int8_registers(a, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,106 @@
+"""im2win_matmul_int8 against sums of whole numbers: the sum is exact, its conversion, two products and the bias's sum round by 2^-24 each, y once."""
+import pytest
+import torch
+
+from paper_2608_20725_b200 import binding
+from sequence_helpers import DTYPES, Guarded, close, rounding
+
+pytestmark = pytest.mark.gpu
+
+
+def run(dtype, m, n, k, bias=False, pitch=0, y_pitch=0, shift=0, extremes=False, seed=1, kernel=None):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    tdt = DTYPES[dtype]
+    x, w = (torch.randint(-128, 128, (rows, k), generator=gen, device="cuda", dtype=torch.int8) for rows in (m, n))
+    if extremes:
+        x.fill_(-128)
+        w.fill_(-128)
+        w[::2] = 127
+    xs, ws = torch.rand(m, generator=gen, device="cuda") * 0.1, (torch.rand(n, generator=gen, device="cuda") + 0.5) * 0.01
+    b = torch.randn(n, generator=gen, device="cuda") if bias else None
+    xg, yg = Guarded((m, k), torch.int8, pitch, fill=99, shift=shift), Guarded((m, n), tdt, y_pitch)
+    xg.view.copy_(x)
+    if kernel:
+        assert binding.im2win_matmul_int8_kernel_name(m, n, k, binding._sequence_dtype(tdt), k + pitch) == kernel
+    binding.im2win_matmul_int8(xg.view, xs, w, ws, yg.view, bias=b)
+    torch.cuda.synchronize()
+    acc = x.double() @ w.double().T                  # (whole numbers below 2^53: exact)
+    want = acc * xs.double()[:, None] * ws.double()
+    off = 3 * 2.0 ** -24 * want.abs()
+    if bias:
+        want = want + b.double()
+        off = off + 2.0 ** -24 * (want.abs() + off)
+    want, off = want.cpu(), off.cpu()
+    close(yg.view, want, off + rounding(want, tdt), "y")
+    yg.assert_untouched_outside()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 64, 64), (1, 4096, 4096), (3, 100, 33), (8, 128, 128), (16, 1001, 2080), (17, 512, 1024),
+                                   (64, 256, 4096), (65, 129, 144), (128, 128, 16), (200, 300, 257), (701, 1001, 2080), (300, 72, 15)])
+def test_sizes(dtype, m, n, k):
+    run(dtype, m, n, k, bias=m % 2 == 1)
+
+
+@pytest.mark.parametrize("m", [1, 2, 5, 15, 16, 31, 33, 64, 100, 128, 129, 255, 256, 257, 511, 1000])
+def test_rows(m):
+    run("bf16", m, 384, 512)
+    run("f32", m, 200, 208, bias=True)
+
+
+@pytest.mark.parametrize("n", [8, 16, 63, 127, 128, 129, 255, 256, 257, 640, 1500])
+def test_columns(n):
+    for m in (4, 200):
+        run("f16", m, n, 384)
+
+
+@pytest.mark.parametrize("k", [16, 32, 48, 112, 128, 144, 240, 1040, 16384])
+def test_reductions(k):
+    for m in (4, 40, 200):
+        run("f32", m, 264, k)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_strides_and_rows_that_start_anywhere(dtype):
+    for m in (5, 300):
+        run(dtype, m, 200, 256, pitch=16, y_pitch=8)
+        run(dtype, m, 200, 256, pitch=3, y_pitch=1)
+        run(dtype, m, 200, 256, shift=1)
+        run(dtype, m, 201, 253, shift=2, pitch=5)
+        run(dtype, m, 200, 256, shift=4, y_pitch=56)
+
+
+@pytest.mark.parametrize("k", [4096, 131071, 131056])
+def test_the_largest_sums(k):
+    """2^31 - 2^14 and the like: as far as 32 bits go."""
+    for m in (2, 130):
+        run("f32", m, 130, k, extremes=True)
+
+
+def test_many_tiles():
+    run("bf16", 3000, 2100, 512, kernel=None)
+    run("bf16", 40, 30000, 256)
+
+
+def test_no_rows():
+    y = torch.zeros(0, 8, device="cuda")
+    binding.im2win_matmul_int8(torch.zeros(0, 16, dtype=torch.int8, device="cuda"), torch.zeros(0, device="cuda"),
+                               torch.zeros(8, 16, dtype=torch.int8, device="cuda"), torch.zeros(8, device="cuda"), y)
+
+
+@pytest.mark.parametrize("m", [4, 300])
+def test_captured_and_on_another_stream(m):
+    make = lambda rows: torch.randint(-127, 128, (rows, 512), device="cuda", dtype=torch.int8)
+    x, w, xs, ws = make(m), make(640), torch.rand(m, device="cuda"), torch.rand(640, device="cuda")
+    y, other = torch.zeros(m, 640, device="cuda"), torch.zeros(m, 640, device="cuda")
+    binding.im2win_matmul_int8(x, xs, w, ws, y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.im2win_matmul_int8(x, xs, w, ws, y)
+    x.copy_(make(m))
+    graph.replay()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    binding.im2win_matmul_int8(x, xs, w, ws, other, stream=side)
+    side.synchronize()
+    assert torch.equal(y, other) and bool(y.any())
