@@ -543,8 +543,8 @@ im2win_status im2win_gated_delta_rule(const void* q, const void* k, const void* 
                                       void* o, const float* state_in, float* state_out, const im2win_sequences* seqs,
                                       const im2win_delta_shape* shape, im2win_dtype dtype, void* cuda_stream);
 /*
- * How a call with cu_seqlens runs such a shape (host-only, static storage; for reports and tests): "tokens" (the recurrence);
- * "none" for an invalid shape.
+ * How a call with cu_seqlens runs such a shape (host-only, static storage; for reports and tests): "tokens" (the recurrence),
+ * "chunks" (64 tokens at a time); "none" for an invalid shape.
  */
 const char* im2win_gated_delta_rule_kernel_name(const im2win_delta_shape* shape, im2win_dtype dtype);
 

@@ -173,6 +173,8 @@ struct DeltaArgs {
 };
 constexpr float kNormalizeEps = 1e-6f;     // added to the sum of squares of a row of q or k
 cudaError_t launch_delta_tokens(const DeltaArgs& a, cudaStream_t stream);
+bool delta_by_chunks(const im2win_delta_shape& s, bool has_cu);
+cudaError_t launch_delta_chunks(const DeltaArgs& a, cudaStream_t stream);
 
 cudaError_t launch_rms_norm(const void* x, const void* residual, const void* weight, void* residual_out, void* y, float* scales,
                             const im2win_norm_shape& shape, im2win_dtype dtype, cudaStream_t stream);

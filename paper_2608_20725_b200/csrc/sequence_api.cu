@@ -165,7 +165,7 @@ im2win_status im2win_matvec_int4(const void* x, const uint8_t* weight, const voi
 
 const char* im2win_gated_delta_rule_kernel_name(const im2win_delta_shape* shape, im2win_dtype dtype) {
   if (check_delta(shape, dtype) != IM2WIN_OK) return "none";
-  return "tokens";
+  return delta_by_chunks(*shape, true) ? "chunks" : "tokens";
 }
 
 im2win_status im2win_gated_delta_rule(const void* q, const void* k, const void* v, const float* log_decay, const float* beta,
@@ -186,7 +186,8 @@ im2win_status im2win_gated_delta_rule(const void* q, const void* k, const void* 
     if (!aligned_to(at, es)) return IM2WIN_ERR_MISALIGNED;
   if (!aligned_to(log_decay, 4) || !aligned_to(beta, 4) || !aligned_to(state_in, 16) || !aligned_to(state_out, 16))
     return IM2WIN_ERR_MISALIGNED;
-  return from_launch(launch_delta_tokens(a, static_cast<cudaStream_t>(cuda_stream)));
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  return from_launch(delta_by_chunks(*shape, a.seqs.cu != nullptr) ? launch_delta_chunks(a, stream) : launch_delta_tokens(a, stream));
 }
 
 im2win_status im2win_rms_norm(const void* x, const void* residual, const void* weight, void* residual_out, void* y, float* scales,
