@@ -36,8 +36,6 @@ namespace {
 using ptx::smem_u32;
 
 constexpr int kChunk = 64;
-constexpr int kHelpers = 4;              // warps that prepare chunks
-constexpr int kAPitch = 68;              // floats
 
 struct ChunkParams {
   const void* q;
@@ -59,20 +57,25 @@ struct ChunkParams {
 struct alignas(16) Weights {
   float of_x[kChunk];                    // beta exp(G_i) of k S, without the scale of k
   float of_v[kChunk];                    // beta
-  float of_t[kChunk];                    // undoes T's scale of a row
   float to_end[kChunk];                  // exp(G_n - G_j), without the scale of k
   float of_q[kChunk];                    // scale exp(G_i) of q S, without the scale of q
   float of_p[kChunk];                    // undoes P's scale of a row
   float total, total_rest;               // exp(G_n) in two parts
-  float pad[2];
+  float of_t;                            // undoes T's scale
+  float pad;
 };
 
 struct Scratch {
-  float A[kChunk][kAPitch];              // A, then T
+  uint8_t A[2][kChunk * kChunk * 2];     // in two pieces, rows scaled, as far as to the diagonal's 16 x 16 blocks
+  uint8_t blocks[2][kChunk * 32];        // the inverses of those, in two pieces
+  float diagonal[4][16][20];             // the blocks, then their inverses, in fp32
+  float of_blocks[4];                    // undo the scales of the inverses
+  float unscale_a[kChunk];               // and of A's rows
   float k_row[kChunk], q_row[kChunk];    // what k and q in pieces are multiplied by
-  float whole[kChunk], part[kChunk];     // G_i in powers of two: its floor and the rest
-  float beta[kChunk];
+  int whole[kChunk];                     // G_i in powers of two: its floor; the rest is in the factors of A's and P's rows and columns
+  float of_a[kChunk], of_p[kChunk], of_column[kChunk];
   uint32_t bad_k[kChunk / 32], bad_q[kChunk / 32];             // rows that are not finite
+  uint32_t top_t;                        // T's largest element
 };
 
 template <typename T, int DK>
@@ -84,9 +87,14 @@ struct Layout {
   static constexpr uint32_t kWeightsAt = kPAt + kPieces * kSquare;
   static constexpr uint32_t kStage = kWeightsAt + sizeof(Weights);
   static constexpr uint32_t kScratchAt = 2 * kStage;
-  static constexpr uint32_t kVAt = (kScratchAt + sizeof(Scratch) + 127) / 128 * 128;
-  static constexpr uint32_t kV = sizeof(T) == 2 ? kChunk * 32 : 0;         // a warp's columns of v, and of o on its way out
-  static constexpr uint32_t bytes(int warps) { return kVAt + 2 * kV * warps; }
+  static constexpr uint32_t kEnd = (kScratchAt + sizeof(Scratch) + 127) / 128 * 128;
+  static constexpr uint32_t kRawAt = sizeof(T) == 2 ? kEnd : 0;            // (16 bits) rows of k and q as they come
+  static constexpr uint32_t kColumnsAt = kEnd + (sizeof(T) == 2 ? 2 * kRows : 0);
+  // of a warp with columns: two chunks of v (16 bits), then, where another warp makes o, what it needs: S and U in fp16 as operands, three pairs
+  // a lane, o on its way out
+  static constexpr uint32_t kV = sizeof(T) == 2 ? kChunk * 32 : 0;
+  static constexpr uint32_t kSAt = 2 * kV, kUAt = kSAt + DK / 16 * 512, kPairsAt = kUAt + 4 * 512, kOAt = kPairsAt + 3 * 256;
+  template <bool SPLIT> static constexpr uint32_t kColumns = SPLIT ? kOAt + kV : 2 * kV;
 };
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -132,7 +140,6 @@ __device__ __forceinline__ void stmatrix_trans(uint32_t addr, const uint32_t (&r
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void sync_helpers() { asm volatile("bar.sync 1, %0;" ::"n"(kHelpers * 32) : "memory"); }
 
 // Byte of a 16-byte unit of row r of rows of N elements of 16 bits (units swizzled by the row, so that the matrix loads have no conflicts).
 template <int N>
@@ -144,344 +151,492 @@ __device__ __forceinline__ uint32_t unit_at(int r, int unit) {
 
 // Eight elements of a row as floats; 0 beyond `columns` and where the row is not there.
 template <typename T>
-__device__ __forceinline__ void load8(const T* row, int at, int columns, bool there, bool vectors, float (&x)[8]) {
-  if (vectors) {
-    if constexpr (sizeof(T) == 2) {
-      uint4 w = make_uint4(0, 0, 0, 0);
-      if (there && at < columns) w = __ldg(reinterpret_cast<const uint4*>(row + at));
-      const Vec<T, 8> e = *reinterpret_cast<const Vec<T, 8>*>(&w);
+__device__ __forceinline__ void load8(const T* row, int at, int columns, bool there, float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (there && at < columns) w = __ldg(reinterpret_cast<const uint4*>(row + at));
+    const Vec<T, 8> e = *reinterpret_cast<const Vec<T, 8>*>(&w);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = to_float(e.v[j]);
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (there && at + 4 * h < columns) w = __ldg(reinterpret_cast<const float4*>(row + at + 4 * h));
-        x[4 * h] = w.x, x[4 * h + 1] = w.y, x[4 * h + 2] = w.z, x[4 * h + 3] = w.w;
-      }
-    }
+    for (int j = 0; j < 8; ++j) x[j] = to_float(e.v[j]);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = there && at + j < columns ? to_float(row[at + j]) : 0.0f;
+    for (int h = 0; h < 2; ++h) {
+      float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (there && at + 4 * h < columns) w = __ldg(reinterpret_cast<const float4*>(row + at + 4 * h));
+      x[4 * h] = w.x, x[4 * h + 1] = w.y, x[4 * h + 2] = w.z, x[4 * h + 3] = w.w;
+    }
   }
 }
 
-// Rows of q or k of a chunk to shared memory, scaled, in pieces: two threads a row.  Leaves what a row is multiplied by (the norm's and the
-// scale's reciprocals) and says which rows are not finite (they come out as 0).
-template <typename T, int DK>
-__device__ __forceinline__ void prepare_rows(const ChunkParams& p, const T* from, int64_t stride, int first, int end, uint32_t to, float* factor,
-                                             uint32_t* bad) {
+// H warps that make chunks.
+template <typename T, int DK, int H>
+struct Helpers {
   using L = Layout<T, DK>;
-  const int t = threadIdx.x & (kHelpers * 32 - 1), r = t >> 1, half = t & 1, lane = threadIdx.x & 31;
-  const bool there = first + r < end;
-  const T* row = from + (there ? (int64_t)(first + r) * stride : 0);
-  constexpr int kUnits = DK / 16;                              // of a thread: every second one of its row
-  float x[kUnits][8];
-#pragma unroll
-  for (int i = 0; i < kUnits; ++i) load8<T>(row, (2 * i + half) * 8, p.dk, there, p.qk_vectors, x[i]);
-  float top = 0.0f, squares = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kUnits; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      top = max_nan(top, fabsf(x[i][j]));
-      squares = fmaf(x[i][j], x[i][j], squares);
-    }
-  top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  squares += __shfl_xor_sync(0xffffffffu, squares, 1);
-  const bool odd = !(top <= FLT_MAX);
-  const float scale = scale_for(top);
-  const uint32_t odd_rows = __ballot_sync(0xffffffffu, odd);   // (two bits a row)
-#pragma unroll
-  for (int i = 0; i < kUnits; ++i) {
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) split(odd ? 0.0f : x[i][2 * j] * scale, odd ? 0.0f : x[i][2 * j + 1] * scale, hi[j], lo[j]);
-    const uint32_t at = to + unit_at<DK>(r, 2 * i + half);
-    ptx::st_shared16(at, hi[0], hi[1], hi[2], hi[3]);
-    if (L::kPieces == 2) ptx::st_shared16(at + L::kRows, lo[0], lo[1], lo[2], lo[3]);
-  }
-  if (half == 0) factor[r] = odd ? 0.0f : (p.normalize ? rsqrtf(squares + kNormalizeEps) : 1.0f) * unscale_for(scale);
-  if (lane == 0) {
-    uint32_t rows = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) rows |= (odd_rows >> (2 * i) & 1u) << i;
-    reinterpret_cast<uint16_t*>(bad)[(t >> 5)] = (uint16_t)rows;
-  }
-}
+  static constexpr int kThreads = H * 32;
+  static constexpr int kShare = 2;                             // threads of a row
+  static constexpr int kWeigher = H == 8 ? 4 : 0;              // the warp that sums up decays
+  static constexpr int kUnits = DK / 8 / kShare;               // 16-byte units (of 16-bit elements) of a thread: every kShare-th one
+  static constexpr bool kStaged = L::kRawAt != 0;
 
-// One warp: lane l has tokens 2l and 2l+1.  Sums of log_decay are of whole numbers of 2^-44 powers of two: exact.
-__device__ __forceinline__ void prepare_weights(const ChunkParams& p, const float (&g)[2], const float (&b)[2], int tokens, Scratch& s, Weights& w) {
-  constexpr float kNaN = __builtin_nanf("");
-  const int lane = threadIdx.x & 31;
-  auto powers = [](float x) -> int64_t {                       // (beyond 2^+-1000 nothing changes in fp32)
-    return __double2ll_rn((double)fminf(fmaxf(x, -700.0f), 700.0f) * (1.4426950408889634074 * 17592186044416.0));
-  };
-  int64_t a[2];
-  uint32_t odd[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    a[i] = powers(g[i]);
-    const bool row = (s.bad_k[lane >> 4] >> ((2 * lane + i) & 31) & 1u) != 0;
-    odd[i] = __ballot_sync(0xffffffffu, row || !(g[i] < __int_as_float(0x7f800000)) || !(fabsf(b[i]) <= FLT_MAX));
-  }
-  // the first token from which nothing is finite any more
-  const int first0 = odd[0] ? 2 * (__ffs(odd[0]) - 1) : kChunk, first1 = odd[1] ? 2 * (__ffs(odd[1]) - 1) + 1 : kChunk;
-  const int broken = min(first0, first1);
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    if (2 * lane + i >= broken) a[i] = 0;                      // (so that nothing that is finite meets what is not)
-  int64_t sum = a[0] + a[1];
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    const int64_t other = __shfl_up_sync(0xffffffffu, sum, d);
-    if (lane >= d) sum += other;
-  }
-  const int64_t all = __shfl_sync(0xffffffffu, sum, 31);
-  auto fraction = [](int64_t x) { return (float)((uint32_t)(x >> 20) & 0xffffffu) * 5.9604644775390625e-8f; };
-  auto power = [&](int64_t x) {
-    return exp2f(fraction(x)) * __uint_as_float((uint32_t)(min(max((int)(x >> 44), -127), 127) + 127) << 23);
-  };
-  const int64_t G[2] = {sum - a[1], sum};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int t = 2 * lane + i;
-    const bool gone = t >= broken;
-    const float beta = gone ? 0.0f : b[i], from_start = power(G[i]);
-    const bool bad_q = (s.bad_q[lane >> 4] >> (t & 31) & 1u) != 0;
-    s.whole[t] = (float)(int)(G[i] >> 44);
-    s.part[t] = fraction(G[i]);
-    s.beta[t] = beta;
-    w.of_x[t] = beta * from_start * s.k_row[t];
-    w.of_v[t] = beta;
-    w.to_end[t] = power(all - G[i]) * s.k_row[t];
-    w.of_q[t] = gone || bad_q ? kNaN : p.scale * from_start * s.q_row[t];
-  }
-  if (lane == 0) {
-    const double exact = exp2((double)all * (1.0 / 17592186044416.0));
-    const float total = (float)exact;
-    w.total = broken < tokens ? kNaN : total;
-    w.total_rest = (float)(exact - (double)total);
-  }
-}
+  const ChunkParams& p;
+  uint32_t smem;
+  uint8_t* generic;
+  Scratch& s;
+  int head, t, warp, lane;
+  float g[2], b[2];                                            // (the weigher) of the next chunk
 
-// T in the place of A.
-__device__ __forceinline__ void invert(Scratch& s) {
-  const int t = threadIdx.x & (kHelpers * 32 - 1), warp = t >> 5, lane = t & 31;
-  {
-    const int b0 = warp * 16, j = lane & 15;                   // (both halves of the warp do the same)
-    float x[16];
+  __device__ __forceinline__ Helpers(const ChunkParams& p_, uint32_t smem_, uint8_t* generic_, int head_, int t_)
+      : p(p_), smem(smem_), generic(generic_), s(*reinterpret_cast<Scratch*>(generic_ + L::kScratchAt)), head(head_), t(t_), warp(t_ >> 5), lane(t_ & 31) {}
+
+  static __device__ __forceinline__ void sync() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
+
+  // The next chunk's rows on their way: of 16 bits and in whole vectors to shared memory, where each thread finds what it has copied itself.
+  __device__ __forceinline__ void fetch(int first, int end) {
+    g[0] = g[1] = b[0] = b[1] = 0.0f;
+    if (warp == kWeigher) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i == j ? 1.0f : 0.0f;
-#pragma unroll
-    for (int k = 0; k < 15; ++k)
-#pragma unroll
-      for (int i = k + 1; i < 16; ++i) x[i] = fmaf(-s.A[b0 + i][b0 + k], x[k], x[i]);
-    __syncwarp();
-    if (lane < 16) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s.A[b0 + i][b0 + j] = x[i];
-    }
-  }
-  sync_helpers();
-  {
-    const int c0 = (t >> 6) * 32, r0 = c0 + 16, r = r0 + ((t & 63) >> 2), c = c0 + (t & 3) * 4;
-    float4 m = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    auto add = [&](float a, const float4& b) {
-      m.x = fmaf(a, b.x, m.x), m.y = fmaf(a, b.y, m.y), m.z = fmaf(a, b.z, m.z), m.w = fmaf(a, b.w, m.w);
-    };
-#pragma unroll
-    for (int k = 0; k < 16; ++k) add(s.A[r][c0 + k], *reinterpret_cast<const float4*>(&s.A[c0 + k][c]));
-    sync_helpers();
-    *reinterpret_cast<float4*>(&s.A[r][c]) = m;
-    sync_helpers();
-    m = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-    for (int k = 0; k < 16; ++k) add(-s.A[r][r0 + k], *reinterpret_cast<const float4*>(&s.A[r0 + k][c]));
-    sync_helpers();
-    *reinterpret_cast<float4*>(&s.A[r][c]) = m;
-  }
-  sync_helpers();
-  {
-    const int r = 32 + (t >> 3) * 2, c = (t & 7) * 4;
-    float4 m[2];
-    auto product = [&](int rows_at, int from) {                // rows r, r + 1 of A[..][rows_at ..] times rows `from`.. of columns c
-      m[0] = m[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-      for (int k = 0; k < 32; k += 4) {
-        const float4 a0 = *reinterpret_cast<const float4*>(&s.A[r][rows_at + k]), a1 = *reinterpret_cast<const float4*>(&s.A[r + 1][rows_at + k]);
-        const float f0[4] = {a0.x, a0.y, a0.z, a0.w}, f1[4] = {a1.x, a1.y, a1.z, a1.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 b = *reinterpret_cast<const float4*>(&s.A[from + k + i][c]);
-          m[0].x = fmaf(f0[i], b.x, m[0].x), m[0].y = fmaf(f0[i], b.y, m[0].y), m[0].z = fmaf(f0[i], b.z, m[0].z), m[0].w = fmaf(f0[i], b.w, m[0].w);
-          m[1].x = fmaf(f1[i], b.x, m[1].x), m[1].y = fmaf(f1[i], b.y, m[1].y), m[1].z = fmaf(f1[i], b.z, m[1].z), m[1].w = fmaf(f1[i], b.w, m[1].w);
+      for (int i = 0; i < 2; ++i) {
+        const int64_t at = first + 2 * lane + i;
+        if (at < end) {
+          g[i] = p.decay[at * p.decay_stride + head];
+          b[i] = p.beta[at * p.beta_stride + head];
         }
       }
-    };
-    product(0, 0);
-    sync_helpers();
-    *reinterpret_cast<float4*>(&s.A[r][c]) = m[0];
-    *reinterpret_cast<float4*>(&s.A[r + 1][c]) = m[1];
-    sync_helpers();
-    product(32, 32);
-    sync_helpers();
+    }
+    if constexpr (kStaged) {
+      if (p.qk_vectors) {
+        const int r = (t & 127) / kShare, part = t % kShare;
+        const bool row = first + r < end;
+        const T* k = static_cast<const T*>(p.k) + (int64_t)(head / p.share) * p.dk;
+        const T* q = static_cast<const T*>(p.q) + (int64_t)(head / p.share) * p.dk;
+        const T* kr = k + (row ? (int64_t)(first + r) * p.k_stride : 0);
+        const T* qr = q + (row ? (int64_t)(first + r) * p.q_stride : 0);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(&s.A[r + i][c]) = make_float4(-m[i].x, -m[i].y, -m[i].z, -m[i].w);
-  }
-  sync_helpers();
-}
-
-// Chunk of rows [first, end) into `stage`.
-template <typename T, int DK>
-__device__ __forceinline__ void prepare(const ChunkParams& p, int head, int first, int end, uint32_t smem, uint8_t* generic, uint32_t stage,
-                                        Scratch& s) {
-  using L = Layout<T, DK>;
-  const int warp = (threadIdx.x >> 5) & (kHelpers - 1), lane = threadIdx.x & 31;
-  Weights& w = *reinterpret_cast<Weights*>(generic + stage + L::kWeightsAt);
-  float g[2] = {0.0f, 0.0f}, b[2] = {0.0f, 0.0f};
-  if (warp == 0) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t t = first + 2 * lane + i;
-      if (t < end) {
-        g[i] = p.decay[t * p.decay_stride + head];
-        b[i] = p.beta[t * p.beta_stride + head];
+        for (int i = 0; i < kUnits; ++i) {
+          const int unit = i * kShare + part;
+          const bool there = row && unit * 8 < p.dk;
+          if (H == 4 || warp < 4) copy16(smem + L::kRawAt + unit_at<DK>(r, unit), there ? kr + unit * 8 : k, there);
+          if (H == 4 || warp >= 4) copy16(smem + L::kRawAt + L::kRows + unit_at<DK>(r, unit), there ? qr + unit * 8 : q, there);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
     }
   }
-  const int64_t at = (int64_t)(head / p.share) * p.dk;
-  const uint32_t kt = smem + stage, qt = kt + L::kQAt;
-  prepare_rows<T, DK>(p, static_cast<const T*>(p.k) + at, p.k_stride, first, end, kt, s.k_row, s.bad_k);
-  prepare_rows<T, DK>(p, static_cast<const T*>(p.q) + at, p.q_stride, first, end, qt, s.q_row, s.bad_q);
-  sync_helpers();
-  if (warp == 0) prepare_weights(p, g, b, end - first, s, w);
-  sync_helpers();
 
-  // 16 rows of k k^T and 16 of q k^T a warp, up to the diagonal
-  const int mi = lane >> 3, r8 = lane & 7, group = lane >> 2, pair = (lane & 3) * 2;
-  auto square = [&](uint32_t rows, int m, float (&acc)[8][4]) {
+  // Rows of q or k of a chunk to shared memory, scaled, in pieces.  Leaves what a row is multiplied by (the norm's and the scale's
+  // reciprocals) and says which rows are not finite (they come out as 0).
+  __device__ __forceinline__ void rows(const T* from, int64_t stride, int first, int end, uint32_t raw, uint32_t to, float* factor, uint32_t* bad) {
+    const int r = (t & 127) / kShare, part = t % kShare;
+    const bool there = first + r < end;
+    const T* row = from + (there ? (int64_t)(first + r) * stride : 0);
+    float x[kUnits][8];
+    if (kStaged && p.qk_vectors) {
+      if constexpr (kStaged) {
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
+        for (int i = 0; i < kUnits; ++i) {
+          const uint4 w = *reinterpret_cast<const uint4*>(generic + raw + unit_at<DK>(r, i * kShare + part));
+          const Vec<T, 8> e = *reinterpret_cast<const Vec<T, 8>*>(&w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[i][j] = to_float(e.v[j]);
+        }
+      }
+    } else if (p.qk_vectors) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) load8<T>(row, (i * kShare + part) * 8, p.dk, there, x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int at = (i * kShare + part) * 8 + j;
+          x[i][j] = there && at < p.dk ? to_float(row[at]) : 0.0f;
+        }
+    }
+    float top[4] = {}, squares[4] = {};
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        top[j & 3] = max_nan(top[j & 3], fabsf(x[i][j]));
+        squares[j & 3] = fmaf(x[i][j], x[i][j], squares[j & 3]);
+      }
+    top[0] = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3]));
+    squares[0] = (squares[0] + squares[1]) + (squares[2] + squares[3]);
+#pragma unroll
+    for (int d = 1; d < kShare; d *= 2) {
+      top[0] = max_nan(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
+      squares[0] += __shfl_xor_sync(0xffffffffu, squares[0], d);
+    }
+    const bool odd = !(top[0] <= FLT_MAX);
+    const float scale = scale_for(top[0]);
+    const uint32_t odd_rows = __ballot_sync(0xffffffffu, odd); // (kShare bits a row)
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) split(odd ? 0.0f : x[i][2 * j] * scale, odd ? 0.0f : x[i][2 * j + 1] * scale, hi[j], lo[j]);
+      const uint32_t at = to + unit_at<DK>(r, i * kShare + part);
+      ptx::st_shared16(at, hi[0], hi[1], hi[2], hi[3]);
+      if (L::kPieces == 2) ptx::st_shared16(at + L::kRows, lo[0], lo[1], lo[2], lo[3]);
+    }
+    if (part == 0) factor[r] = odd ? 0.0f : (p.normalize ? rsqrtf(squares[0] + kNormalizeEps) : 1.0f) * unscale_for(scale);
+    if (lane == 0) {
+      uint32_t bits = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bits |= (odd_rows >> (kShare * i) & 1u) << i;
+      reinterpret_cast<uint16_t*>(bad)[warp & 3] = (uint16_t)bits;
+    }
+  }
+
+  // One warp: lane l has tokens 2l and 2l+1.  Sums of log_decay are of whole numbers of 2^-44 powers of two: exact.
+  __device__ __forceinline__ void weights(Weights& w, int& broken, int64_t& all) const {
+    constexpr float kNaN = __builtin_nanf("");
+    auto powers = [](float x) -> int64_t {                     // (beyond 2^+-1000 nothing changes in fp32)
+      return __double2ll_rn((double)fminf(fmaxf(x, -700.0f), 700.0f) * (1.4426950408889634074 * 17592186044416.0));
+    };
+    int64_t a[2];
+    uint32_t odd[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      a[i] = powers(g[i]);
+      const bool row = (s.bad_k[lane >> 4] >> ((2 * lane + i) & 31) & 1u) != 0;
+      odd[i] = __ballot_sync(0xffffffffu, row || !(g[i] < __int_as_float(0x7f800000)) || !(fabsf(b[i]) <= FLT_MAX));
+    }
+    // the first token from which nothing is finite any more
+    const int first0 = odd[0] ? 2 * (__ffs(odd[0]) - 1) : kChunk, first1 = odd[1] ? 2 * (__ffs(odd[1]) - 1) + 1 : kChunk;
+    broken = min(first0, first1);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (2 * lane + i >= broken) a[i] = 0;                    // (so that nothing that is finite meets what is not)
+    int64_t sum = a[0] + a[1];
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int64_t other = __shfl_up_sync(0xffffffffu, sum, d);
+      if (lane >= d) sum += other;
+    }
+    all = __shfl_sync(0xffffffffu, sum, 31);
+    auto fraction = [](int64_t x) { return (float)((uint32_t)(x >> 20) & 0xffffffu) * 5.9604644775390625e-8f; };
+    auto power = [&](int64_t x) {
+      return exp2f(fraction(x)) * __uint_as_float((uint32_t)(min(max((int)(x >> 44), -127), 127) + 127) << 23);
+    };
+    const int64_t G[2] = {sum - a[1], sum};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = 2 * lane + i;
+      const bool gone = at >= broken;
+      const float beta = gone ? 0.0f : b[i], from_start = power(G[i]), part = exp2f(fraction(G[i]));
+      const float k_row = s.k_row[at], q_row = s.q_row[at];
+      const bool bad_q = (s.bad_q[lane >> 4] >> (at & 31) & 1u) != 0;
+      s.whole[at] = (int)(G[i] >> 44);
+      s.of_a[at] = beta * k_row * part;
+      s.of_p[at] = p.scale * q_row * part;
+      s.of_column[at] = k_row * exp2f(-fraction(G[i]));
+      w.of_x[at] = beta * from_start * k_row;
+      w.of_v[at] = beta;
+      w.to_end[at] = power(all - G[i]) * k_row;
+      w.of_q[at] = gone || bad_q ? kNaN : p.scale * from_start * q_row;
+    }
+    if (lane == 0) s.top_t = 0;
+  }
+  // (behind the barrier that the others wait at: 64-bit powers take their time)
+  __device__ __forceinline__ void total(Weights& w, int broken, int64_t all, int tokens) const {
+    if (lane == 0) {
+      const double exact = exp2((double)all * (1.0 / 17592186044416.0));
+      const float rounded = (float)exact;
+      w.total = broken < tokens ? __builtin_nanf("") : rounded;
+      w.total_rest = (float)(exact - (double)rounded);
+    }
+  }
+
+  // 16 rows (M) of products with k, up to the diagonal
+  template <int M>
+  __device__ __forceinline__ void square(uint32_t rows_at, uint32_t kt, float (&acc)[2 * M + 2][4]) const {
+    const int mi = lane >> 3, r8 = lane & 7;
+#pragma unroll
+    for (int n = 0; n < 2 * M + 2; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
-#pragma unroll 2
+#pragma unroll
     for (int ks = 0; ks < DK / 16; ++ks) {
       uint32_t a[L::kPieces][4];
 #pragma unroll
-      for (int i = 0; i < L::kPieces; ++i) ldmatrix(rows + i * L::kRows + unit_at<DK>(m * 16 + (mi & 1) * 8 + r8, 2 * ks + (mi >> 1)), a[i]);
+      for (int i = 0; i < L::kPieces; ++i) ldmatrix(rows_at + i * L::kRows + unit_at<DK>(M * 16 + (mi & 1) * 8 + r8, 2 * ks + (mi >> 1)), a[i]);
 #pragma unroll
-      for (int np = 0; np < 4; ++np) {
-        if (np > m) break;
+      for (int np = 0; np <= M; ++np) {
         uint32_t k0[4];
         ldmatrix(kt + unit_at<DK>(np * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1)), k0);
         if (L::kPieces == 2) {
           uint32_t k1[4];
           ldmatrix(kt + L::kRows + unit_at<DK>(np * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1)), k1);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            mma(acc[2 * np + h], a[0], k1[2 * h], k1[2 * h + 1]);
-            mma(acc[2 * np + h], a[L::kPieces - 1], k0[2 * h], k0[2 * h + 1]);
-          }
+          for (int h = 0; h < 2; ++h) mma(acc[2 * np + h], a[0], k1[2 * h], k1[2 * h + 1]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) mma(acc[2 * np + h], a[L::kPieces - 1], k0[2 * h], k0[2 * h + 1]);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) mma(acc[2 * np + h], a[0], k0[2 * h], k0[2 * h + 1]);
       }
     }
-  };
-  auto weigh = [&](int m, float (&acc)[8][4], float f0, float f1, bool with_diagonal) {
-    const int i0 = m * 16 + group;
-    const float w0 = s.whole[i0], w1 = s.whole[i0 + 8], p0 = s.part[i0], p1 = s.part[i0 + 8];
+  }
+  // times exp(G_i - G_j) and the factors of row and column; 0 above the diagonal.  Then the rows' scales, and in pieces to `to` (the second one
+  // only if it is wanted).
+  template <int M>
+  __device__ __forceinline__ void weigh(float (&acc)[2 * M + 2][4], const float* of_row, bool with_diagonal) const {
+    const int i0 = M * 16 + (lane >> 2), pair = (lane & 3) * 2;
+    const int w0 = s.whole[i0], w1 = s.whole[i0 + 8];
+    const float f0 = of_row[i0], f1 = of_row[i0 + 8];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      if (n > 2 * m + 1) break;
+    for (int n = 0; n < 2 * M + 2; ++n) {
       const int j = n * 8 + pair;
-      const float2 wj = *reinterpret_cast<const float2*>(&s.whole[j]), pj = *reinterpret_cast<const float2*>(&s.part[j]);
-      const float2 kj = *reinterpret_cast<const float2*>(&s.k_row[j]);
+      const int2 wj = *reinterpret_cast<const int2*>(&s.whole[j]);
+      const float2 kj = *reinterpret_cast<const float2*>(&s.of_column[j]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = i0 + (e >> 1) * 8, jj = j + (e & 1);
-        const float power = ((e >> 1 ? w1 : w0) - (e & 1 ? wj.y : wj.x)) + ((e >> 1 ? p1 : p0) - (e & 1 ? pj.y : pj.x));
-        const float x = acc[n][e] * (e >> 1 ? f1 : f0) * (e & 1 ? kj.y : kj.x) * exp2f(power);
-        acc[n][e] = jj < i || (with_diagonal && jj == i) ? x : 0.0f;
+        const int power = min(max((e >> 1 ? w1 : w0) - (e & 1 ? wj.y : wj.x), -127), 127);
+        const float x = acc[n][e] * ((e >> 1 ? f1 : f0) * (e & 1 ? kj.y : kj.x)) * __uint_as_float((uint32_t)(power + 127) << 23);
+        acc[n][e] = n < 2 * M || jj < i || (with_diagonal && jj == i) ? x : 0.0f;
       }
     }
-  };
-  {
-    float acc[8][4];
-    const int m = warp, i0 = m * 16 + group;
-    square(kt, m, acc);
-    weigh(m, acc, s.beta[i0] * s.k_row[i0], s.beta[i0 + 8] * s.k_row[i0 + 8], false);
-#pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      if (n > 2 * m + 1) break;
-      *reinterpret_cast<float2*>(&s.A[i0][n * 8 + pair]) = make_float2(acc[n][0], acc[n][1]);
-      *reinterpret_cast<float2*>(&s.A[i0 + 8][n * 8 + pair]) = make_float2(acc[n][2], acc[n][3]);
-    }
   }
-  {
-    float acc[8][4];
-    const int m = kHelpers - 1 - warp, i0 = m * 16 + group;
-    square(qt, m, acc);
-    weigh(m, acc, p.scale * s.q_row[i0], p.scale * s.q_row[i0 + 8], true);
+  template <int M>
+  __device__ __forceinline__ void store_scaled(const float (&acc)[2 * M + 2][4], uint8_t* to, uint32_t second, bool two, float* unscale) const {
+    const int i0 = M * 16 + (lane >> 2), pair = (lane & 3) * 2;
     float top[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      if (n > 2 * m + 1) break;
+    for (int n = 0; n < 2 * M + 2; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) top[e >> 1] = fmaxf(top[e >> 1], fabsf(acc[n][e]));
-    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
       top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
       const float scale = scale_for(top[h]);
       const int i = i0 + 8 * h;
-      if ((lane & 3) == 0) w.of_p[i] = unscale_for(scale);
+      if ((lane & 3) == 0) unscale[i] = unscale_for(scale);
 #pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        if (n > 2 * m + 1) break;
+      for (int n = 0; n < 2 * M + 2; ++n) {
         uint32_t hi, lo;
         split(acc[n][2 * h] * scale, acc[n][2 * h + 1] * scale, hi, lo);
-        uint8_t* to = generic + stage + L::kPAt + unit_at<kChunk>(i, n) + pair * 2;
-        *reinterpret_cast<uint32_t*>(to) = hi;
-        if (L::kPieces == 2) *reinterpret_cast<uint32_t*>(to + L::kSquare) = lo;
+        uint8_t* at = to + unit_at<kChunk>(i, n) + pair * 2;
+        *reinterpret_cast<uint32_t*>(at) = hi;
+        if (two) *reinterpret_cast<uint32_t*>(at + second) = lo;
       }
     }
   }
-  sync_helpers();
-  invert(s);
-  {
-    const int t = threadIdx.x & (kHelpers * 32 - 1), r = t >> 1, half = t & 1;
-    const int blocks = (r >> 4) + 1;                           // of 16 columns, up to the diagonal's
+
+  // Rows M of A, and the inverse of their diagonal block (left in fp32, and in pieces).
+  template <int M>
+  __device__ __forceinline__ void rows_of_a(uint32_t kt, bool& waited) const {
+    float acc[2 * M + 2][4];
+    square<M>(kt, kt, acc);
+    if (!waited) sync();                                       // (the weights)
+    waited = true;
+    weigh<M>(acc, s.of_a, false);
+    store_scaled<M>(acc, s.A[0], sizeof(s.A[0]), true, s.unscale_a);
+    const int g = lane >> 2, pair = (lane & 3) * 2;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<float2*>(&s.diagonal[M][g + 8 * h][n * 8 + pair]) = make_float2(acc[2 * M + n][2 * h], acc[2 * M + n][2 * h + 1]);
+    __syncwarp();
+  }
+  __device__ __forceinline__ void invert_block(int m) const {
+    float(&d)[16][20] = s.diagonal[m];
+    const int j = lane & 15;                                   // (a column; both halves of the warp do the same)
+    float x[16], top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = i == j ? 1.0f : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 15; ++k)
+#pragma unroll
+      for (int i = k + 1; i < 16; ++i) x[i] = fmaf(-d[i][k], x[k], x[i]);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      d[i][j] = x[i];
+      top = fmaxf(top, fabsf(x[i]));
+    }
+#pragma unroll
+    for (int e = 1; e < 16; e *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, e));
+    const float scale = scale_for(top);
+    if (lane == 0) s.of_blocks[m] = unscale_for(scale);
+    __syncwarp();
+    const int r = lane >> 1, half = lane & 1;                  // half a row
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 y = *reinterpret_cast<const float2*>(&d[r][half * 8 + 2 * i]);
+      split(y.x * scale, y.y * scale, hi[i], lo[i]);
+    }
+    const uint32_t at = smem_u32(s.blocks[0]) + block_unit(m * 16 + r, half);
+    ptx::st_shared16(at, hi[0], hi[1], hi[2], hi[3]);
+    ptx::st_shared16(at + sizeof(s.blocks[0]), lo[0], lo[1], lo[2], lo[3]);
+  }
+  static __device__ __forceinline__ uint32_t block_unit(int r, int half) { return (uint32_t)(r * 32 + ((half ^ (r >> 2 & 1)) << 4)); }
+
+  // 16 columns J of T below the diagonal block: T_iJ = -T_ii sum_k A_ik T_kJ, i downward, transposed, so that what one product gives is the next one's
+  // left operand.  Then all of the columns, scaled, to `to`.
+  template <int J>
+  __device__ __forceinline__ void columns_of_t(uint32_t to, Weights& w) const {
+    const int mi = lane >> 3, r8 = lane & 7, g = lane >> 2, pair = (lane & 3) * 2;
+    const uint32_t blocks = smem_u32(s.blocks[0]), a_at = smem_u32(s.A[0]);
+    float t[4 - J][2][4], unscale[4 - J][2];                   // T_iJ transposed: rows are columns of T
+    uint32_t hi[4 - J][4], lo[4 - J][4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[0][n][e] = s.diagonal[J][n * 8 + pair + (e & 1)][g + 8 * (e >> 1)];
+    {
+      const uint32_t at = blocks + block_unit(J * 16 + (mi >> 1) * 8 + r8, mi & 1);
+      ptx::ldmatrix_x4_trans(at, hi[0]);
+      ptx::ldmatrix_x4_trans(at + sizeof(s.blocks[0]), lo[0]);
+      unscale[0][0] = unscale[0][1] = s.of_blocks[J];
+    }
+    auto times = [&](float (&d)[2][4], const uint32_t (&ah)[4], const uint32_t (&al)[4], uint32_t at, uint32_t second) {
+      uint32_t b[4], bl[4];
+      ldmatrix(at, b);
+      ldmatrix(at + second, bl);
+      float small[2][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[n][e] = small[n][e] = 0.0f;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) mma(d[n], ah, b[2 * n], b[2 * n + 1]);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) mma(small[n], al, b[2 * n], b[2 * n + 1]);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) mma(small[n], ah, bl[2 * n], bl[2 * n + 1]);
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[n][e] += small[n][e];
+    };
+    auto in_pieces = [&](const float (&x)[2][4], uint32_t (&h)[4], uint32_t (&l)[4], float (&un)[2]) {
+      float top[2], scale[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        top[r] = fmaxf(fmaxf(fabsf(x[0][2 * r]), fabsf(x[0][2 * r + 1])), fmaxf(fabsf(x[1][2 * r]), fabsf(x[1][2 * r + 1])));
+        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+        scale[r] = scale_for(top[r]);
+        un[r] = unscale_for(scale[r]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) split(x[i >> 1][2 * (i & 1)] * scale[i & 1], x[i >> 1][2 * (i & 1) + 1] * scale[i & 1], h[i], l[i]);
+    };
+#pragma unroll
+    for (int i = J + 1; i < 4; ++i) {
+      float m[2][4];
+#pragma unroll
+      for (int k = J; k < i; ++k) {
+        float part[2][4];
+        times(part, hi[k - J], lo[k - J], a_at + unit_at<kChunk>(i * 16 + (mi >> 1) * 8 + r8, 2 * k + (mi & 1)), sizeof(s.A[0]));
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) m[n][e] = k == J ? part[n][e] * unscale[k - J][e >> 1] : fmaf(part[n][e], unscale[k - J][e >> 1], m[n][e]);
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const float2 f = *reinterpret_cast<const float2*>(&s.unscale_a[i * 16 + n * 8 + pair]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[n][e] *= e & 1 ? f.y : f.x;
+      }
+      uint32_t mh[4], ml[4];
+      float un[2];
+      in_pieces(m, mh, ml, un);
+      times(t[i - J], mh, ml, blocks + block_unit(i * 16 + (mi >> 1) * 8 + r8, mi & 1), sizeof(s.blocks[0]));
+      const float f = -s.of_blocks[i];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[i - J][n][e] *= f * un[e >> 1];
+      if (i < 3) in_pieces(t[i - J], hi[i - J], lo[i - J], unscale[i - J]);
+    }
     float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i >= blocks) break;
+    for (int i = 0; i < 4 - J; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; j += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(&s.A[r][i * 16 + half * 8 + j]);
-        top = fmaxf(fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y))), fmaxf(fabsf(x.z), fabsf(x.w)));
-      }
-    }
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const float scale = scale_for(top);
-    if (half == 0) w.of_t[r] = unscale_for(scale);
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i >= blocks) break;
-      uint32_t hi[4], lo[4];
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(t[i][n][e]));
+    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+    if (lane == 0) atomicMax(&s.top_t, most);
+    sync_four();
+    const float scale = scale_for(__uint_as_float(*(volatile uint32_t*)&s.top_t));
+    if (J == 0 && lane == 0) w.of_t = unscale_for(scale);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 x = *reinterpret_cast<const float2*>(&s.A[r][i * 16 + half * 8 + 2 * j]);
-        split(x.x * scale, x.y * scale, hi[j], lo[j]);
-      }
-      const uint32_t to = kt + L::kTAt + unit_at<kChunk>(r, 2 * i + half);
-      ptx::st_shared16(to, hi[0], hi[1], hi[2], hi[3]);
-      ptx::st_shared16(to + L::kSquare, lo[0], lo[1], lo[2], lo[3]);
+    for (int i = 0; i < 4 - J; ++i) {
+      uint32_t h[4], l[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) split(t[i][u >> 1][2 * (u & 1)] * scale, t[i][u >> 1][2 * (u & 1) + 1] * scale, h[u], l[u]);
+      const uint32_t at = to + unit_at<kChunk>((i + J) * 16 + (mi >> 1) * 8 + r8, 2 * J + (mi & 1));
+      stmatrix_trans(at, h);
+      stmatrix_trans(at + L::kSquare, l);
     }
   }
-}
+  static __device__ __forceinline__ void sync_four() { asm volatile("bar.sync 15, 128;" ::: "memory"); }
+
+  template <int M>
+  __device__ __forceinline__ void rows_of_p(uint32_t qt, uint32_t kt, uint32_t stage, Weights& w, bool& waited) const {
+    float acc[2 * M + 2][4];
+    square<M>(qt, kt, acc);
+    if (!waited) sync();
+    waited = true;
+    weigh<M>(acc, s.of_p, true);
+    store_scaled<M>(acc, generic + stage + L::kPAt, L::kSquare, L::kPieces == 2, w.of_p);
+  }
+
+  // Chunk of rows first up to first + 64 (or end), which were fetched, into `stage`; the next one is fetched.  Of eight warps four have k, A and
+  // T, the others q, the weights and P; of four all have both.
+  __device__ __forceinline__ void prepare(int first, int end, uint32_t stage) {
+    Weights& w = *reinterpret_cast<Weights*>(generic + stage + L::kWeightsAt);
+    const int64_t at = (int64_t)(head / p.share) * p.dk;
+    const uint32_t kt = smem + stage, qt = kt + L::kQAt;
+    if (kStaged) asm volatile("cp.async.wait_all;" ::: "memory");
+    if (H == 4 || warp < 4) rows(static_cast<const T*>(p.k) + at, p.k_stride, first, end, L::kRawAt, kt, s.k_row, s.bad_k);
+    if (H == 4 || warp >= 4) rows(static_cast<const T*>(p.q) + at, p.q_stride, first, end, L::kRawAt + L::kRows, qt, s.q_row, s.bad_q);
+    sync();
+    int broken = 0;
+    int64_t all = 0;
+    if (warp == kWeigher) weights(w, broken, all);
+    const int m = warp & 3;
+    bool waited = false;
+    if (H == 4 || warp < 4) {
+      switch (m) {
+        case 0: rows_of_a<0>(kt, waited); break;
+        case 1: rows_of_a<1>(kt, waited); break;
+        case 2: rows_of_a<2>(kt, waited); break;
+        default: rows_of_a<3>(kt, waited); break;
+      }
+      invert_block(m);
+      sync_four();
+      fetch(first + kChunk, end);
+      switch (m) {
+        case 0: columns_of_t<0>(kt + L::kTAt, w); break;
+        case 1: columns_of_t<1>(kt + L::kTAt, w); break;
+        case 2: columns_of_t<2>(kt + L::kTAt, w); break;
+        default: columns_of_t<3>(kt + L::kTAt, w); break;
+      }
+    }
+    if (H == 4 || warp >= 4) {
+      switch (H == 4 ? 3 - m : m) {
+        case 0: rows_of_p<0>(qt, kt, stage, w, waited); break;
+        case 1: rows_of_p<1>(qt, kt, stage, w, waited); break;
+        case 2: rows_of_p<2>(qt, kt, stage, w, waited); break;
+        default: rows_of_p<3>(qt, kt, stage, w, waited); break;
+      }
+      if (warp == kWeigher) total(w, broken, all, min(end - first, kChunk));
+      if (H == 8) fetch(first + kChunk, end);
+    }
+  }
+};
 
 // ------------------------------------------------------------------------------------------------ the columns of a warp
 
@@ -526,13 +681,17 @@ __device__ __forceinline__ void clean(float (&x)[8][4], int (&from)[2]) {
 // The largest magnitude of rows g and g + 8, in all four lanes that share them; a NaN where there is one.
 template <int N>
 __device__ __forceinline__ void largest(const float (&x)[N][4], float (&top)[2]) {
-  top[0] = top[1] = 0.0f;
+  float m[4][2];
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) top[e >> 1] = max_nan(top[e >> 1], fabsf(x[n][e]));
+    for (int h = 0; h < 2; ++h) {
+      const float two = max_nan(fabsf(x[n][2 * h]), fabsf(x[n][2 * h + 1]));
+      m[n & 3][h] = n < 4 ? two : max_nan(m[n & 3][h], two);
+    }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
+    top[h] = max_nan(max_nan(m[0][h], m[1][h]), max_nan(m[2][h], m[3][h]));
     top[h] = max_nan(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
     top[h] = max_nan(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
   }
@@ -548,23 +707,25 @@ __device__ __forceinline__ void operand(const float (&x)[N][4], int ks, const fl
   }
 }
 
-template <typename T, int DK>
+// 16 columns of a head.  SPLIT: one warp has the chain from S to S, another one makes o from S and U in fp16, which the first leaves in shared memory; it says
+// so at two barriers of the pair.  Otherwise one warp does both.
+template <typename T, int DK, bool SPLIT>
 struct Columns {
   using L = Layout<T, DK>;
   static constexpr bool kFull = L::kPieces == 2;               // fp32: o too from two pieces
+  static_assert(!(kFull && SPLIT), "");
 
   const ChunkParams& p;
-  uint32_t smem, v_at;
+  uint32_t smem, at0;
   uint8_t* generic;
-  int head, col0, lane, mi, r8, group, pair;
-  float S[DK / 8][4];
+  int head, col0, index, lane, mi, r8, group, pair;
 
-  __device__ __forceinline__ Columns(const ChunkParams& p_, uint32_t smem_, uint8_t* generic_, int head_, int col0_, int warp)
-      : p(p_), smem(smem_), v_at(smem_ + L::kVAt + 2 * L::kV * warp), generic(generic_), head(head_), col0(col0_) {
+  __device__ __forceinline__ Columns(const ChunkParams& p_, uint32_t smem_, uint8_t* generic_, int head_, int col0_, int index_)
+      : p(p_), smem(smem_), at0(L::kColumnsAt + L::template kColumns<SPLIT> * index_), generic(generic_), head(head_), col0(col0_), index(index_) {
     lane = threadIdx.x & 31;
     mi = lane >> 3, r8 = lane & 7, group = lane >> 2, pair = (lane & 3) * 2;
   }
-  __device__ __forceinline__ void states(const float* from) {
+  __device__ __forceinline__ void states(const float* from, float (&S)[DK / 8][4]) const {
 #pragma unroll
     for (int n = 0; n < DK / 8; ++n)
 #pragma unroll
@@ -573,7 +734,7 @@ struct Columns {
         S[n][e] = from && d < p.dk && c < p.dv ? from[(int64_t)d * p.dv + c] : 0.0f;
       }
   }
-  __device__ __forceinline__ void store_states(float* to) const {
+  __device__ __forceinline__ void store_states(float* to, const float (&S)[DK / 8][4]) const {
 #pragma unroll
     for (int n = 0; n < DK / 8; ++n)
 #pragma unroll
@@ -587,17 +748,20 @@ struct Columns {
   __device__ __forceinline__ void load_v(int buffer, int first, int end) const {
     if constexpr (sizeof(T) == 2) {
       const T* v = static_cast<const T*>(p.v) + (int64_t)head * p.dv + col0;
-      const uint32_t to = v_at + buffer * L::kV;
+      const uint32_t to = smem + at0 + buffer * L::kV;
+      if (p.v_vectors) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = i * 16 + (lane >> 1), half = lane & 1;
+          const bool there = first + t < end && col0 + half * 8 < p.dv;
+          copy16(to + v_unit(t, half), there ? v + (int64_t)(first + t) * p.v_stride + half * 8 : v, there);
+        }
+      } else {
 #pragma unroll 1
-      for (int i = 0; i < 4; ++i) {
-        const int t = i * 16 + (lane >> 1), half = lane & 1;
-        const bool row = first + t < end;
-        const T* from = v + (row ? (int64_t)(first + t) * p.v_stride + half * 8 : 0);
-        if (p.v_vectors) {
-          const bool there = row && col0 + half * 8 < p.dv;
-          copy16(to + v_unit(t, half), there ? from : v, there);
-        } else {
-          const uint16_t* e = reinterpret_cast<const uint16_t*>(from);
+        for (int i = 0; i < 4; ++i) {
+          const int t = i * 16 + (lane >> 1), half = lane & 1;
+          const bool row = first + t < end;
+          const uint16_t* e = reinterpret_cast<const uint16_t*>(v + (row ? (int64_t)(first + t) * p.v_stride + half * 8 : 0));
           uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
           for (int j = 0; j < 8; ++j)
@@ -609,9 +773,151 @@ struct Columns {
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
 
-  __device__ __forceinline__ void chunk(int c, int first, int end) {
-    const uint32_t kt = smem + (c & 1) * L::kStage, qt = kt + L::kQAt, tt = kt + L::kTAt, pt = kt + L::kPAt;
-    const Weights& w = *reinterpret_cast<const Weights*>(generic + (c & 1) * L::kStage + L::kWeightsAt);
+  // What the warp that makes o waits for: S of a chunk (which == 0), its U (1).
+  __device__ __forceinline__ void announce(int which) const { asm volatile("bar.arrive %0, 64;" ::"r"(2 + 2 * index + which) : "memory"); }
+  __device__ __forceinline__ void await(int which) const { asm volatile("bar.sync %0, 64;" ::"r"(2 + 2 * index + which) : "memory"); }
+  template <typename V>
+  __device__ __forceinline__ V& lane_pair(int which) const { return reinterpret_cast<V*>(generic + at0 + L::kPairsAt + which * 256)[lane]; }
+
+  __device__ __forceinline__ void multiply_q(uint32_t qt, int ks, const uint32_t (&hi)[4], const uint32_t (&lo)[4], float (&O)[8][4]) const {
+#pragma unroll
+    for (int np = 0; np < 4; ++np) {
+      const uint32_t at = qt + unit_at<DK>(np * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1));
+      uint32_t a[4];
+      ldmatrix(at, a);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (kFull) mma(O[2 * np + h], lo, a[2 * h], a[2 * h + 1]);
+        mma(O[2 * np + h], hi, a[2 * h], a[2 * h + 1]);
+      }
+      if (kFull) {
+        ldmatrix(at + L::kRows, a);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) mma(O[2 * np + h], hi, a[2 * h], a[2 * h + 1]);
+      }
+    }
+  }
+
+  // o = q S, which O holds, and P U, whose operand u(kk, hi, lo) gives
+  template <typename Operand>
+  __device__ __forceinline__ void finish_o(uint32_t pt, const Weights& w, float (&O)[8][4], const float (&per_s)[2], const float (&per_o)[2],
+                                           const Operand& u, bool odd, const int (&from)[2], uint32_t out_at, int first, int end) const {
+    float I[8][4];
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) I[n][e] = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      uint32_t hi[4], lo[4];
+      u(kk, hi, lo);
+#pragma unroll
+      for (int np = kk; np < 4; ++np) {
+        const uint32_t at = pt + unit_at<kChunk>(np * 16 + (mi >> 1) * 8 + r8, 2 * kk + (mi & 1));
+        uint32_t b[4];
+        ldmatrix(at, b);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (kFull) mma(I[2 * np + h], lo, b[2 * h], b[2 * h + 1]);
+          mma(I[2 * np + h], hi, b[2 * h], b[2 * h + 1]);
+        }
+        if (kFull) {
+          ldmatrix(at + L::kSquare, b);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) mma(I[2 * np + h], hi, b[2 * h], b[2 * h + 1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int np = 0; np < 4; ++np) {
+      uint32_t out[4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int n = 2 * np + h, t = n * 8 + pair;
+        const float2 fq = *reinterpret_cast<const float2*>(&w.of_q[t]), fp = *reinterpret_cast<const float2*>(&w.of_p[t]);
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = fmaf((e & 1 ? fq.y : fq.x) * per_s[e >> 1], O[n][e], (e & 1 ? fp.y : fp.x) * per_o[e >> 1] * I[n][e]);
+        if (odd) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (t + (e & 1) >= from[e >> 1]) y[e] = __builtin_nanf("");
+        }
+        if constexpr (kFull) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int row = first + t + (e & 1), at = col0 + group + 8 * (e >> 1);
+            if (row < end && at < p.dv) static_cast<float*>(p.o)[(int64_t)row * p.o_stride + (int64_t)head * p.dv + at] = y[e];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            Vec<T, 2> two;
+            two.v[0] = from_float<T>(y[2 * i]);
+            two.v[1] = from_float<T>(y[2 * i + 1]);
+            out[2 * h + i] = *reinterpret_cast<const uint32_t*>(&two);
+          }
+        }
+      }
+      if constexpr (!kFull) stmatrix_trans(smem + out_at + v_unit(np * 16 + (mi >> 1) * 8 + r8, mi & 1), out);
+    }
+    if constexpr (!kFull) {
+      __syncwarp();
+      T* o = static_cast<T*>(p.o) + (int64_t)head * p.dv + col0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = i * 16 + (lane >> 1), half = lane & 1;
+        if (first + t < end) {
+          const uint4 y = *reinterpret_cast<const uint4*>(generic + out_at + v_unit(t, half));
+          T* to = o + (int64_t)(first + t) * p.o_stride + half * 8;
+          if (p.o_vectors) {
+            if (col0 + half * 8 < p.dv) *reinterpret_cast<uint4*>(to) = y;
+          } else {
+            const Vec<T, 8> e = *reinterpret_cast<const Vec<T, 8>*>(&y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (col0 + half * 8 + j < p.dv) to[j] = e.v[j];
+          }
+        }
+      }
+      __syncwarp();
+    }
+  }
+
+  // o of chunk c, by the warp beside the chain's.
+  __device__ __forceinline__ void chunk_o(int c, int first, int end) const {
+    const uint32_t stage = (c & 1) * L::kStage;
+    const Weights& w = *reinterpret_cast<const Weights*>(generic + stage + L::kWeightsAt);
+    float O[8][4];
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) O[n][e] = 0.0f;
+    auto handed = [&](uint32_t at, int i, uint32_t (&hi)[4]) {
+      const uint4 x = reinterpret_cast<const uint4*>(generic + at0 + at)[i * 32 + lane];
+      hi[0] = x.x, hi[1] = x.y, hi[2] = x.z, hi[3] = x.w;
+    };
+    await(0);
+#pragma unroll
+    for (int ks = 0; ks < DK / 16; ++ks) {
+      uint32_t hi[4];
+      handed(L::kSAt, ks, hi);
+      multiply_q(smem + stage + L::kQAt, ks, hi, hi, O);
+    }
+    await(1);
+    const float2 ps = lane_pair<float2>(0), po = lane_pair<float2>(1);
+    const int2 f = lane_pair<int2>(2);
+    const float per_s[2] = {ps.x, ps.y}, per_o[2] = {po.x, po.y};
+    const int from[2] = {f.x, f.y};
+    const bool odd = __any_sync(0xffffffffu, min(f.x, f.y) < kChunk);
+    finish_o(smem + stage + L::kPAt, w, O, per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { handed(L::kUAt, kk, hi); }, odd, from,
+             at0 + L::kOAt, first, end);
+  }
+
+  // S of chunk c, and its o too where no other warp makes it.
+  __device__ __forceinline__ void chunk(int c, int first, int end, float (&S)[DK / 8][4]) const {
+    const uint32_t stage = (c & 1) * L::kStage, kt = smem + stage, qt = kt + L::kQAt, tt = kt + L::kTAt;
+    const Weights& w = *reinterpret_cast<const Weights*>(generic + stage + L::kWeightsAt);
     load_v((c + 1) & 1, first + kChunk, end);
     float v32[kFull ? 8 : 1][4];
     if constexpr (kFull) {
@@ -624,12 +930,15 @@ struct Columns {
         }
     }
 
-    // k S and q S
-    float X[8][4], O[8][4], top[2], scale[2], per_s[2];
+    // k S (and q S)
+    float X[8][4], O[SPLIT ? 1 : 8][4], top[2], scale[2], per_s[2];
 #pragma unroll
     for (int n = 0; n < 8; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) X[n][e] = O[n][e] = 0.0f;
+      for (int e = 0; e < 4; ++e) {
+        X[n][e] = 0.0f;
+        if constexpr (!SPLIT) O[n][e] = 0.0f;
+      }
     largest(S, top);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -640,29 +949,28 @@ struct Columns {
     for (int ks = 0; ks < DK / 16; ++ks) {
       uint32_t hi[4], lo[4];
       operand(S, ks, scale, hi, lo);
+      if constexpr (SPLIT) ptx::st_shared16(smem + at0 + L::kSAt + (ks * 32 + lane) * 16, hi[0], hi[1], hi[2], hi[3]);
 #pragma unroll
-      for (int np = 0; np < 4; ++np) {
-        const uint32_t at = unit_at<DK>(np * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1));
-        uint32_t b[4], a[4];
-        ldmatrix(kt + at, b);
-        ldmatrix(qt + at, a);
+      for (int half = 0; half < 2; ++half) {                   // (four accumulators, so that a product does not wait for the one before)
+        uint32_t b[2][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          mma(X[2 * np + h], lo, b[2 * h], b[2 * h + 1]);
-          if (kFull) mma(O[2 * np + h], lo, a[2 * h], a[2 * h + 1]);
-          mma(X[2 * np + h], hi, b[2 * h], b[2 * h + 1]);
-          mma(O[2 * np + h], hi, a[2 * h], a[2 * h + 1]);
-        }
+        for (int i = 0; i < 2; ++i) ldmatrix(kt + unit_at<DK>((2 * half + i) * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1)), b[i]);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) mma(X[4 * half + n], lo, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) mma(X[4 * half + n], hi, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
         if (kFull) {
-          ldmatrix(kt + L::kRows + at, b);
-          ldmatrix(qt + L::kRows + at, a);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            mma(X[2 * np + h], hi, b[2 * h], b[2 * h + 1]);
-            mma(O[2 * np + h], hi, a[2 * h], a[2 * h + 1]);
-          }
+          for (int i = 0; i < 2; ++i) ldmatrix(kt + L::kRows + unit_at<DK>((2 * half + i) * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1)), b[i]);
+#pragma unroll
+          for (int n = 0; n < 4; ++n) mma(X[4 * half + n], hi, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
         }
       }
+      if constexpr (!SPLIT) multiply_q(qt, ks, hi, lo, O);
+    }
+    if constexpr (SPLIT) {
+      lane_pair<float2>(0) = make_float2(per_s[0], per_s[1]);
+      announce(0);
     }
 
     // R, in the place of k S
@@ -671,7 +979,7 @@ struct Columns {
 #pragma unroll
     for (int np = 0; np < 4; ++np) {
       uint32_t vv[4] = {0, 0, 0, 0};
-      if constexpr (!kFull) ptx::ldmatrix_x4_trans(v_at + (c & 1) * L::kV + v_unit(np * 16 + (mi >> 1) * 8 + r8, mi & 1), vv);
+      if constexpr (!kFull) ptx::ldmatrix_x4_trans(smem + at0 + (c & 1) * L::kV + v_unit(np * 16 + (mi >> 1) * 8 + r8, mi & 1), vv);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int n = 2 * np + h;
@@ -703,39 +1011,38 @@ struct Columns {
       per_r[h] = unscale_for(scale[h]);
     }
 
-    // U (times R's scale)
+    // U (times R's and T's scales)
     float U[8][4];
-    {
-      uint32_t hi[4][4], lo[4][4];
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) operand(X, kk, scale, hi[kk], lo[kk]);
+    for (int n = 0; n < 8; ++n)
 #pragma unroll
-      for (int np = 0; np < 4; ++np) {
+      for (int e = 0; e < 4; ++e) U[n][e] = 0.0f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+    for (int kk = 0; kk < 4; ++kk) {
+      uint32_t hi[4], lo[4];
+      operand(X, kk, scale, hi, lo);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) U[2 * np + h][e] = 0.0f;
+      for (int np = kk; np < 4; np += 2) {                     // (two at a time, where there are)
+        uint32_t b[2][4], bl[2][4];
 #pragma unroll
-        for (int kk = 0; kk <= np; ++kk) {
-          const uint32_t at = tt + unit_at<kChunk>(np * 16 + (mi >> 1) * 8 + r8, 2 * kk + (mi & 1));
-          uint32_t b[4], bl[4];
-          ldmatrix(at, b);
-          ldmatrix(at + L::kSquare, bl);
+        for (int i = 0; i < 2; ++i) {
+          if (np + i > 3) break;
+          const uint32_t at = tt + unit_at<kChunk>((np + i) * 16 + (mi >> 1) * 8 + r8, 2 * kk + (mi & 1));
+          ldmatrix(at, b[i]);
+          ldmatrix(at + L::kSquare, bl[i]);
+        }
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            mma(U[2 * np + h], lo[kk], b[2 * h], b[2 * h + 1]);
-            mma(U[2 * np + h], hi[kk], bl[2 * h], bl[2 * h + 1]);
-            mma(U[2 * np + h], hi[kk], b[2 * h], b[2 * h + 1]);
+        for (int m = 0; m < 3; ++m)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            if (np + (n >> 1) > 3) break;
+            const uint32_t(&f)[4] = m == 1 ? bl[n >> 1] : b[n >> 1];
+            mma(U[2 * np + n], m == 0 ? lo : hi, f[2 * (n & 1)], f[2 * (n & 1) + 1]);
           }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float2 f = *reinterpret_cast<const float2*>(&w.of_t[(2 * np + h) * 8 + pair]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) U[2 * np + h][e] *= e & 1 ? f.y : f.x;
-        }
       }
     }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) per_r[h] *= w.of_t;
     largest(U, top);
     if (__any_sync(0xffffffffu, !(max_nan(top[0], top[1]) <= FLT_MAX))) {
       odd = true;
@@ -743,155 +1050,114 @@ struct Columns {
       largest(U, top);
     }
 
-    // o
+    // o, or what the other warp makes it from
     {
-      uint32_t hi[4][4], lo[4][4];
       float per_o[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         scale[h] = scale_for(top[h]);
         per_o[h] = unscale_for(scale[h]) * per_r[h];
       }
+      if constexpr (SPLIT) {
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) operand(U, kk, scale, hi[kk], lo[kk]);
+        for (int kk = 0; kk < 4; ++kk) {
+          uint32_t hi[4];
 #pragma unroll
-      for (int np = 0; np < 4; ++np) {
-        float I[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) I[h][e] = 0.0f;
-#pragma unroll
-        for (int kk = 0; kk <= np; ++kk) {
-          const uint32_t at = pt + unit_at<kChunk>(np * 16 + (mi >> 1) * 8 + r8, 2 * kk + (mi & 1));
-          uint32_t b[4];
-          ldmatrix(at, b);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (kFull) mma(I[h], lo[kk], b[2 * h], b[2 * h + 1]);
-            mma(I[h], hi[kk], b[2 * h], b[2 * h + 1]);
+          for (int i = 0; i < 4; ++i) {
+            const float f = scale[i & 1];
+            hi[i] = pack_half(U[2 * kk + (i >> 1)][2 * (i & 1)] * f, U[2 * kk + (i >> 1)][2 * (i & 1) + 1] * f);
           }
-          if (kFull) {
-            ldmatrix(at + L::kSquare, b);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) mma(I[h], hi[kk], b[2 * h], b[2 * h + 1]);
-          }
+          ptx::st_shared16(smem + at0 + L::kUAt + (kk * 32 + lane) * 16, hi[0], hi[1], hi[2], hi[3]);
         }
-        uint32_t out[4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int n = 2 * np + h, t = n * 8 + pair;
-          const float2 fq = *reinterpret_cast<const float2*>(&w.of_q[t]), fp = *reinterpret_cast<const float2*>(&w.of_p[t]);
-          float y[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            y[e] = fmaf((e & 1 ? fq.y : fq.x) * per_s[e >> 1], O[n][e], (e & 1 ? fp.y : fp.x) * per_o[e >> 1] * I[h][e]);
-            if (odd && t + (e & 1) >= from[e >> 1]) y[e] = __builtin_nanf("");
-          }
-          if constexpr (kFull) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int row = first + t + (e & 1), at = col0 + group + 8 * (e >> 1);
-              if (row < end && at < p.dv) static_cast<float*>(p.o)[(int64_t)row * p.o_stride + (int64_t)head * p.dv + at] = y[e];
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              Vec<T, 2> two;
-              two.v[0] = from_float<T>(y[2 * i]);
-              two.v[1] = from_float<T>(y[2 * i + 1]);
-              out[2 * h + i] = *reinterpret_cast<const uint32_t*>(&two);
-            }
-          }
-        }
-        if constexpr (!kFull) stmatrix_trans(v_at + (c & 1) * L::kV + v_unit(np * 16 + (mi >> 1) * 8 + r8, mi & 1), out);
+        lane_pair<float2>(1) = make_float2(per_o[0], per_o[1]);
+        lane_pair<int2>(2) = make_int2(from[0], from[1]);
+        announce(1);
+      } else {
+        finish_o(kt + L::kPAt, w, O, per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { operand(U, kk, scale, hi, lo); }, odd, from,
+                 at0 + (c & 1) * L::kV, first, end);
       }
     }
 
     // S
-    {
-      uint32_t hi[4][4], lo[4][4];
-      float per_u[2];
+    float per_u[2];
 #pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        const float2 f = *reinterpret_cast<const float2*>(&w.to_end[n * 8 + pair]);
+    for (int n = 0; n < 8; ++n) {
+      const float2 f = *reinterpret_cast<const float2*>(&w.to_end[n * 8 + pair]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) U[n][e] *= e & 1 ? f.y : f.x;
-      }
-      largest(U, top);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        scale[h] = scale_for(top[h]);
-        per_u[h] = unscale_for(scale[h]) * per_r[h];
-      }
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) operand(U, kk, scale, hi[kk], lo[kk]);
-      const float total = w.total, rest = w.total_rest;
-#pragma unroll
-      for (int np = 0; np < DK / 16; ++np) {
-        float added[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) added[h][e] = 0.0f;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const uint32_t at = kt + unit_at<DK>(kk * 16 + (mi & 1) * 8 + r8, 2 * np + (mi >> 1));
-          uint32_t b[4];
-          ptx::ldmatrix_x4_trans(at, b);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            mma(added[h], lo[kk], b[2 * h], b[2 * h + 1]);
-            mma(added[h], hi[kk], b[2 * h], b[2 * h + 1]);
-          }
-          if (kFull) {
-            ptx::ldmatrix_x4_trans(at + L::kRows, b);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) mma(added[h], hi[kk], b[2 * h], b[2 * h + 1]);
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float& s = S[2 * np + h][e];
-            s = fmaf(s, total, fmaf(s, rest, added[h][e] * per_u[e >> 1]));
-            if (odd && from[e >> 1] < kChunk) s = __builtin_nanf("");
-          }
-      }
+      for (int e = 0; e < 4; ++e) U[n][e] *= e & 1 ? f.y : f.x;
     }
-
-    if constexpr (!kFull) {
-      __syncwarp();
-      T* o = static_cast<T*>(p.o) + (int64_t)head * p.dv + col0;
+    largest(U, top);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = i * 16 + (lane >> 1), half = lane & 1;
-        if (first + t < end) {
-          const uint4 y = *reinterpret_cast<const uint4*>(generic + (v_at - smem) + (c & 1) * L::kV + v_unit(t, half));
-          T* to = o + (int64_t)(first + t) * p.o_stride + half * 8;
-          if (p.o_vectors) {
-            if (col0 + half * 8 < p.dv) *reinterpret_cast<uint4*>(to) = y;
-          } else {
-            const Vec<T, 8> e = *reinterpret_cast<const Vec<T, 8>*>(&y);
+    for (int h = 0; h < 2; ++h) {
+      scale[h] = scale_for(top[h]);
+      per_u[h] = unscale_for(scale[h]) * per_r[h];
+    }
+    uint32_t hi[4][4], lo[4][4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (col0 + half * 8 + j < p.dv) to[j] = e.v[j];
-          }
+    for (int kk = 0; kk < 4; ++kk) operand(U, kk, scale, hi[kk], lo[kk]);
+    const float total = w.total, rest = w.total_rest;
+#pragma unroll
+    for (int np = 0; np < DK / 16; np += 2) {
+      float added[4][4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) added[n][e] = 0.0f;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        uint32_t b[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) ptx::ldmatrix_x4_trans(kt + unit_at<DK>(kk * 16 + (mi & 1) * 8 + r8, 2 * (np + i) + (mi >> 1)), b[i]);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) mma(added[n], lo[kk], b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) mma(added[n], hi[kk], b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
+        if (kFull) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            ptx::ldmatrix_x4_trans(kt + L::kRows + unit_at<DK>(kk * 16 + (mi & 1) * 8 + r8, 2 * (np + i) + (mi >> 1)), b[i]);
+#pragma unroll
+          for (int n = 0; n < 4; ++n) mma(added[n], hi[kk], b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
         }
       }
-      __syncwarp();
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float& s = S[2 * np + n][e];
+          s = fmaf(s, total, fmaf(s, rest, added[n][e] * per_u[e >> 1]));
+        }
+    }
+    if (odd) {
+#pragma unroll
+      for (int n = 0; n < DK / 8; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (from[e >> 1] < kChunk) S[n][e] = __builtin_nanf("");
     }
   }
 };
 
-// W warps of 16 columns each, then the helpers.
-template <typename T, int DK, int W>
-__global__ void __launch_bounds__((W + kHelpers) * 32, 1) delta_chunks_kernel(const ChunkParams p) {
+// How a block's warps share the work: W with the chains of 16 columns each, with SPLIT as many that make o, then H helpers.  Registers: of the
+// warps with columns (with SPLIT and four of them: of those with the chains and of those that make o), of the helpers; what the warpgroups ask for
+// is no more than the block is launched with.
+template <int W_, bool SPLIT_, int H_, int CHAIN, int O, int HELP>
+struct Shape {
+  static constexpr int W = W_, H = H_, kWarps = SPLIT_ ? 2 * W_ : W_, kThreads = (kWarps + H_) * 32;
+  static constexpr bool SPLIT = SPLIT_;
+  static constexpr int kChain = CHAIN, kO = O, kHelp = HELP;
+  static constexpr int kLaunched = 65536 / kThreads / 8 * 8 > 255 ? 255 : 65536 / kThreads / 8 * 8;
+  static constexpr int kAsked = (O > 0 ? W_ * 32 * (CHAIN + O) : kWarps * 32 * CHAIN) + H_ * 32 * HELP;
+  static_assert(CHAIN == 0 || (O > 0 ? W_ : kWarps) % 4 == 0, "");
+  static_assert(CHAIN == 0 || kAsked <= kLaunched * kThreads, "");
+};
+
+template <typename T, int DK, typename F>
+__global__ void __launch_bounds__(F::kThreads, 1) delta_chunks_kernel(const ChunkParams p) {
   using L = Layout<T, DK>;
+  constexpr int W = F::W;
   extern __shared__ __align__(128) uint8_t dynamic_smem[];
   const uint32_t smem = smem_u32(dynamic_smem);
-  Scratch& scratch = *reinterpret_cast<Scratch*>(dynamic_smem + L::kScratchAt);
   const int warp = ptx::warp_index();
   const uint32_t tile = blockIdx.x % (uint32_t)p.tiles, rest = blockIdx.x / (uint32_t)p.tiles;
   const int head = (int)(rest % (uint32_t)p.heads), b = (int)(rest / (uint32_t)p.heads);
@@ -900,52 +1166,67 @@ __global__ void __launch_bounds__((W + kHelpers) * 32, 1) delta_chunks_kernel(co
   const SequenceRows rows = rows_of(p.seqs, b);
   const int chunks = (rows.end - rows.begin + kChunk - 1) / kChunk;
   const int64_t state_at = ((int64_t)slot * p.heads + head) * p.dk * p.dv;
-  if (warp >= W) {
-    if constexpr (W == 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    // (above the diagonal blocks nothing is written, and the products of T's halves meet it)
-    for (int i = threadIdx.x - W * 32; i < kChunk * kAPitch; i += kHelpers * 32) (&scratch.A[0][0])[i] = 0.0f;
+  if (warp >= F::kWarps) {
+    if constexpr (F::kChain > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kHelp));
+    const int t = (int)threadIdx.x - F::kWarps * 32;
+    Helpers<T, DK, F::H> helpers(p, smem, dynamic_smem, head, t);
+    helpers.fetch(rows.begin, rows.end);
     for (int c = 0; c < chunks; ++c) {
-      const int first = rows.begin + c * kChunk;
-      prepare<T, DK>(p, head, first, min(first + kChunk, rows.end), smem, dynamic_smem, (c & 1) * L::kStage, scratch);
+      helpers.prepare(rows.begin + c * kChunk, rows.end, (c & 1) * L::kStage);
       __syncthreads();
-    }
-  } else {
-    if constexpr (W == 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    const int col0 = ((int)tile * W + warp) * 16;
-    Columns<T, DK> mine(p, smem, dynamic_smem, head, col0, warp);
-    const bool live = col0 < p.dv;
-    mine.states(live && p.state_in && resumes(p.seqs, b) ? p.state_in + state_at : nullptr);
-    if (live) mine.load_v(0, rows.begin, rows.end);
-    for (int c = 0; c < chunks; ++c) {
-      __syncthreads();
-      if (live) mine.chunk(c, rows.begin + c * kChunk, rows.end);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-    if (live && p.state_out) mine.store_states(p.state_out + state_at);
+  } else {
+    // (a warpgroup as a whole: with four chains theirs and the one that makes o, otherwise all that have columns)
+    if constexpr (F::kChain > 0 && F::kO == 0) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kChain));
+    } else if constexpr (F::kChain > 0) {
+      if (warp < W) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kChain));
+      else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kO));
+    }
+    const int index = F::SPLIT && warp >= W ? warp - W : warp, col0 = ((int)tile * W + index) * 16;
+    const Columns<T, DK, F::SPLIT> mine(p, smem, dynamic_smem, head, col0, index);
+    const bool live = col0 < p.dv;
+    if (!F::SPLIT || warp < W) {
+      float S[DK / 8][4];
+      mine.states(live && p.state_in && resumes(p.seqs, b) ? p.state_in + state_at : nullptr, S);
+      if (live) mine.load_v(0, rows.begin, rows.end);
+      for (int c = 0; c < chunks; ++c) {
+        __syncthreads();
+        if (live) mine.chunk(c, rows.begin + c * kChunk, rows.end, S);
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      if (live && p.state_out) mine.store_states(p.state_out + state_at, S);
+    } else if constexpr (F::SPLIT) {
+      for (int c = 0; c < chunks; ++c) {
+        __syncthreads();
+        if (live) mine.chunk_o(c, rows.begin + c * kChunk, rows.end);
+      }
+    }
   }
 }
 
-template <typename T, int DK, int W>
+template <typename T, int DK, typename F>
 cudaError_t launch(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
-  constexpr uint32_t kBytes = Layout<T, DK>::bytes(W);
+  constexpr uint32_t kBytes = Layout<T, DK>::kColumnsAt + F::W * Layout<T, DK>::template kColumns<F::SPLIT>;
   static_assert(kBytes <= 227 * 1024, "");
   static bool attr_done[64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!attr_done[dev]) {
-    cudaError_t e = cudaFuncSetAttribute(delta_chunks_kernel<T, DK, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
+    cudaError_t e = cudaFuncSetAttribute(delta_chunks_kernel<T, DK, F>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
     if (e != cudaSuccess) return e;
     // A build whose blocks start with fewer registers than the warpgroups ask for later would wait for them without end: not launched.
     cudaFuncAttributes built;
-    e = cudaFuncGetAttributes(&built, delta_chunks_kernel<T, DK, W>);
+    e = cudaFuncGetAttributes(&built, delta_chunks_kernel<T, DK, F>);
     if (e != cudaSuccess) return e;
-    if (W == 8 && built.numRegs * (W + kHelpers) * 32 < W * 32 * 208 + kHelpers * 32 * 88) return cudaErrorNotSupported;
+    if (F::kChain > 0 && built.numRegs * F::kThreads < F::kAsked) return cudaErrorNotSupported;
     attr_done[dev] = true;
   }
-  p.tiles = (p.dv + 16 * W - 1) / (16 * W);
+  p.tiles = (p.dv + 16 * F::W - 1) / (16 * F::W);
   const int64_t grid = (int64_t)sequences * p.heads * p.tiles;
   if (grid >= ((int64_t)1 << 31)) return cudaErrorInvalidConfiguration;
-  delta_chunks_kernel<T, DK, W><<<(unsigned)grid, (W + kHelpers) * 32, kBytes, stream>>>(p);
+  delta_chunks_kernel<T, DK, F><<<(unsigned)grid, F::kThreads, kBytes, stream>>>(p);
   return cudaGetLastError();
 }
 
@@ -953,10 +1234,13 @@ template <typename T, int DK>
 cudaError_t launch_width(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
   const int64_t columns = (int64_t)sequences * p.heads * ((p.dv + 15) / 16);
   if constexpr (sizeof(T) == 2) {
-    if (p.dv > 64 && columns >= 148 * 8) return launch<T, DK, 8>(p, sequences, stream);
+    if (p.dv > 64 && columns >= 148 * 8) return launch<T, DK, Shape<8, false, 4, 208, 0, 88>>(p, sequences, stream);
+    if (p.dv > 32 && columns >= 148 * 4) return launch<T, DK, Shape<4, true, 8, 224, 112, 88>>(p, sequences, stream);
+    return launch<T, DK, Shape<2, true, 8, 208, 0, 144>>(p, sequences, stream);
+  } else {
+    if (p.dv > 32 && columns >= 148 * 4) return launch<T, DK, Shape<4, false, 4, 0, 0, 0>>(p, sequences, stream);
+    return launch<T, DK, Shape<2, false, 4, 0, 0, 0>>(p, sequences, stream);
   }
-  if (p.dv > 32 && columns >= 148 * 4) return launch<T, DK, 4>(p, sequences, stream);
-  return launch<T, DK, 2>(p, sequences, stream);
 }
 
 template <typename T>
