@@ -65,12 +65,9 @@ struct alignas(16) Weights {
   float pad;
 };
 
+constexpr int kAPitch = 72;              // floats: 8 rows of 4 pairs lie on all banks
 struct Scratch {
-  uint8_t A[2][kChunk * kChunk * 2];     // in two pieces, rows scaled, as far as to the diagonal's 16 x 16 blocks
-  uint8_t blocks[2][kChunk * 32];        // the inverses of those, in two pieces
-  float diagonal[4][16][20];             // the blocks, then their inverses, in fp32
-  float of_blocks[4];                    // undo the scales of the inverses
-  float unscale_a[kChunk];               // and of A's rows
+  float A[kChunk][kAPitch];              // as far as to the diagonal's 16 x 16 blocks, and those inverted
   float k_row[kChunk], q_row[kChunk];    // what k and q in pieces are multiplied by
   int whole[kChunk];                     // G_i in powers of two: its floor; the rest is in the factors of A's and P's rows and columns
   float of_a[kChunk], of_p[kChunk], of_column[kChunk];
@@ -123,9 +120,20 @@ __device__ __forceinline__ void split(float a, float b, uint32_t& hi, uint32_t& 
 }
 
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Left: lane l has rows l / 4 and that + 8 of columns l % 4 (0, 1) and that + 4 (2, 3); right: rows l % 4 and that + 4 of column l / 4.
+__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// x rounded to 11 bits, and the rest (of which the instruction takes 11).
+__device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
+  lo = __float_as_uint(x - __uint_as_float(hi));
 }
 __device__ __forceinline__ void ldmatrix(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -149,24 +157,36 @@ __device__ __forceinline__ uint32_t unit_at(int r, int unit) {
 
 // ------------------------------------------------------------------------------------------------ the helpers
 
-// Eight elements of a row as floats; 0 beyond `columns` and where the row is not there.
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int at, int columns, bool there, float (&x)[8]) {
-  if constexpr (sizeof(T) == 2) {
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (there && at < columns) w = __ldg(reinterpret_cast<const uint4*>(row + at));
-    const Vec<T, 8> e = *reinterpret_cast<const Vec<T, 8>*>(&w);
+// Eight elements of a row; 0 beyond `columns` and where the row is not there.
+__device__ __forceinline__ void load8(const float* row, int at, int columns, bool there, float (&x)[8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = to_float(e.v[j]);
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (there && at + 4 * h < columns) w = __ldg(reinterpret_cast<const float4*>(row + at + 4 * h));
-      x[4 * h] = w.x, x[4 * h + 1] = w.y, x[4 * h + 2] = w.z, x[4 * h + 3] = w.w;
-    }
+  for (int h = 0; h < 2; ++h) {
+    float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (there && at + 4 * h < columns) w = __ldg(reinterpret_cast<const float4*>(row + at + 4 * h));
+    x[4 * h] = w.x, x[4 * h + 1] = w.y, x[4 * h + 2] = w.z, x[4 * h + 3] = w.w;
   }
 }
+
+// Two elements of 16 bits: whether they are fp16 as they come, the larger magnitudes (a NaN is larger than anything), and both as floats.
+template <typename T> struct Half;
+template <> struct Half<__half> {
+  static constexpr bool kExact = true;
+  static __device__ __forceinline__ uint32_t largest(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("{\n\t.reg .b32 m;\n\tabs.f16x2 m, %2;\n\tmax.NaN.f16x2 %0, %1, m;\n\t}" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) { return unpack_half(w); }
+};
+template <> struct Half<__nv_bfloat16> {
+  static constexpr bool kExact = false;
+  static __device__ __forceinline__ uint32_t largest(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("{\n\t.reg .b32 m;\n\tabs.bf16x2 m, %2;\n\tmax.NaN.bf16x2 %0, %1, m;\n\t}" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+};
 
 // H warps that make chunks.
 template <typename T, int DK, int H>
@@ -211,7 +231,7 @@ struct Helpers {
         const T* q = static_cast<const T*>(p.q) + (int64_t)(head / p.share) * p.dk;
         const T* kr = k + (row ? (int64_t)(first + r) * p.k_stride : 0);
         const T* qr = q + (row ? (int64_t)(first + r) * p.q_stride : 0);
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < kUnits; ++i) {
           const int unit = i * kShare + part;
           const bool there = row && unit * 8 < p.dk;
@@ -223,67 +243,106 @@ struct Helpers {
     }
   }
 
-  // Rows of q or k of a chunk to shared memory, scaled, in pieces.  Leaves what a row is multiplied by (the norm's and the scale's
-  // reciprocals) and says which rows are not finite (they come out as 0).
+  // Rows of q or k of a chunk to shared memory, in pieces, scaled where they are not fp16 already.  Leaves what a row is multiplied by (the
+  // norm's and the scale's reciprocals) and says which rows are not finite (they come out as 0).
   __device__ __forceinline__ void rows(const T* from, int64_t stride, int first, int end, uint32_t raw, uint32_t to, float* factor, uint32_t* bad) {
     const int r = (t & 127) / kShare, part = t % kShare;
     const bool there = first + r < end;
     const T* row = from + (there ? (int64_t)(first + r) * stride : 0);
-    float x[kUnits][8];
-    if (kStaged && p.qk_vectors) {
-      if constexpr (kStaged) {
-#pragma unroll
+    float top = 0.0f, squares[2] = {0.0f, 0.0f}, scale = 1.0f;
+    if constexpr (sizeof(T) == 2) {
+      if (!p.qk_vectors) {
+        raw = to - smem;
+        const uint16_t* e = reinterpret_cast<const uint16_t*>(row);
+#pragma unroll 1
         for (int i = 0; i < kUnits; ++i) {
-          const uint4 w = *reinterpret_cast<const uint4*>(generic + raw + unit_at<DK>(r, i * kShare + part));
-          const Vec<T, 8> e = *reinterpret_cast<const Vec<T, 8>*>(&w);
+          const int at = (i * kShare + part) * 8;
+          uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[i][j] = to_float(e.v[j]);
+          for (int j = 0; j < 8; ++j)
+            if (there && at + j < p.dk) w[j / 2] |= (uint32_t)e[at + j] << (16 * (j & 1));
+          ptx::st_shared16(to + unit_at<DK>(r, i * kShare + part), w[0], w[1], w[2], w[3]);
         }
       }
-    } else if (p.qk_vectors) {
+      uint32_t most = 0;
+#pragma unroll 2
+      for (int i = 0; i < kUnits; ++i) {
+        const uint4 x = *reinterpret_cast<const uint4*>(generic + raw + unit_at<DK>(r, i * kShare + part));
 #pragma unroll
-      for (int i = 0; i < kUnits; ++i) load8<T>(row, (i * kShare + part) * 8, p.dk, there, x[i]);
+        for (uint32_t w : {x.x, x.y, x.z, x.w}) {
+          most = Half<T>::largest(most, w);
+          const float2 f = Half<T>::unpack(w);
+          squares[0] = fmaf(f.x, f.x, squares[0]);
+          squares[1] = fmaf(f.y, f.y, squares[1]);
+        }
+      }
+      const float2 f = Half<T>::unpack(most);
+      top = max_nan(f.x, f.y);
+      top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      const bool odd = !(top <= FLT_MAX);
+      if (!Half<T>::kExact) scale = scale_for(top);
+#pragma unroll 2
+      for (int i = 0; i < kUnits; ++i) {
+        const uint4 x = *reinterpret_cast<const uint4*>(generic + raw + unit_at<DK>(r, i * kShare + part));
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (!Half<T>::kExact) {
+            const float2 g = Half<T>::unpack(w[j]);
+            w[j] = pack_half(g.x * scale, g.y * scale);
+          }
+          if (odd) w[j] = 0;
+        }
+        ptx::st_shared16(to + unit_at<DK>(r, i * kShare + part), w[0], w[1], w[2], w[3]);
+      }
     } else {
+      float x[kUnits][8];
+      if (p.qk_vectors) {
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) load8(row, (i * kShare + part) * 8, p.dk, there, x[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int at = (i * kShare + part) * 8 + j;
+            x[i][j] = there && at < p.dk ? row[at] : 0.0f;
+          }
+      }
 #pragma unroll
       for (int i = 0; i < kUnits; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int at = (i * kShare + part) * 8 + j;
-          x[i][j] = there && at < p.dk ? to_float(row[at]) : 0.0f;
+          top = max_nan(top, fabsf(x[i][j]));
+          squares[j & 1] = fmaf(x[i][j], x[i][j], squares[j & 1]);
         }
-    }
-    float top[4] = {}, squares[4] = {};
+      top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      const bool odd = !(top <= FLT_MAX);
+      scale = scale_for(top);
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i)
+      for (int i = 0; i < kUnits; ++i) {
+        uint32_t hi[4], lo[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        top[j & 3] = max_nan(top[j & 3], fabsf(x[i][j]));
-        squares[j & 3] = fmaf(x[i][j], x[i][j], squares[j & 3]);
+        for (int j = 0; j < 4; ++j) {
+          split(x[i][2 * j] * scale, x[i][2 * j + 1] * scale, hi[j], lo[j]);
+          if (odd) hi[j] = lo[j] = 0;
+        }
+        const uint32_t at = to + unit_at<DK>(r, i * kShare + part);
+        ptx::st_shared16(at, hi[0], hi[1], hi[2], hi[3]);
+        ptx::st_shared16(at + L::kRows, lo[0], lo[1], lo[2], lo[3]);
       }
-    top[0] = max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3]));
-    squares[0] = (squares[0] + squares[1]) + (squares[2] + squares[3]);
-#pragma unroll
-    for (int d = 1; d < kShare; d *= 2) {
-      top[0] = max_nan(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
-      squares[0] += __shfl_xor_sync(0xffffffffu, squares[0], d);
     }
-    const bool odd = !(top[0] <= FLT_MAX);
-    const float scale = scale_for(top[0]);
-    const uint32_t odd_rows = __ballot_sync(0xffffffffu, odd); // (kShare bits a row)
-#pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-      uint32_t hi[4], lo[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) split(odd ? 0.0f : x[i][2 * j] * scale, odd ? 0.0f : x[i][2 * j + 1] * scale, hi[j], lo[j]);
-      const uint32_t at = to + unit_at<DK>(r, i * kShare + part);
-      ptx::st_shared16(at, hi[0], hi[1], hi[2], hi[3]);
-      if (L::kPieces == 2) ptx::st_shared16(at + L::kRows, lo[0], lo[1], lo[2], lo[3]);
-    }
+    squares[0] += squares[1];
+    squares[0] += __shfl_xor_sync(0xffffffffu, squares[0], 1);
+    const bool odd = !(top <= FLT_MAX);
+    const uint32_t odd_rows = __ballot_sync(0xffffffffu, odd); // (two bits a row)
     if (part == 0) factor[r] = odd ? 0.0f : (p.normalize ? rsqrtf(squares[0] + kNormalizeEps) : 1.0f) * unscale_for(scale);
     if (lane == 0) {
       uint32_t bits = 0;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) bits |= (odd_rows >> (kShare * i) & 1u) << i;
+      if (odd_rows) {
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i) bits |= (odd_rows >> (2 * i) & 1u) << i;
+      }
       reinterpret_cast<uint16_t*>(bad)[warp & 3] = (uint16_t)bits;
     }
   }
@@ -348,334 +407,313 @@ struct Helpers {
     }
   }
 
-  // 16 rows (M) of products with k, up to the diagonal
-  template <int M>
-  __device__ __forceinline__ void square(uint32_t rows_at, uint32_t kt, float (&acc)[2 * M + 2][4]) const {
+  // 16 rows (m) of products with k: the blocks left of the diagonal's, and that one.  (One piece of code for all warps and both k and q, loops rolled:
+  // the code that a block's warps run for a chunk, each its own part, has to fit the instruction cache.  With a variant for each m, 140 KB in all,
+  // a chunk of 32 columns of 128 x 128 took 14.4 us.)
+  struct Square {
+    float left[6][4], diagonal[2][4];
+  };
+  __device__ __forceinline__ void square(uint32_t rows_at, uint32_t kt, int m, Square& acc) const {
     const int mi = lane >> 3, r8 = lane & 7;
 #pragma unroll
-    for (int n = 0; n < 2 * M + 2; ++n)
+    for (int n = 0; n < 6; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
+      for (int i = 0; i < 4; ++i) acc.left[n][i] = 0.0f;
 #pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc.diagonal[n][i] = 0.0f;
+    const int a_row = m * 16 + (mi & 1) * 8 + r8, b_row = (mi >> 1) * 8 + r8;
+#pragma unroll 1
     for (int ks = 0; ks < DK / 16; ++ks) {
-      uint32_t a[L::kPieces][4];
+      uint32_t a[L::kPieces][4], b[4][L::kPieces][4];
 #pragma unroll
-      for (int i = 0; i < L::kPieces; ++i) ldmatrix(rows_at + i * L::kRows + unit_at<DK>(M * 16 + (mi & 1) * 8 + r8, 2 * ks + (mi >> 1)), a[i]);
+      for (int i = 0; i < L::kPieces; ++i) ldmatrix(rows_at + i * L::kRows + unit_at<DK>(a_row, 2 * ks + (mi >> 1)), a[i]);
 #pragma unroll
-      for (int np = 0; np <= M; ++np) {
-        uint32_t k0[4];
-        ldmatrix(kt + unit_at<DK>(np * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1)), k0);
-        if (L::kPieces == 2) {
-          uint32_t k1[4];
-          ldmatrix(kt + L::kRows + unit_at<DK>(np * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1)), k1);
+      for (int np = 0; np < 4; ++np)
+        if (np < m || np == 3) {                               // (the last one: the diagonal's)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) mma(acc[2 * np + h], a[0], k1[2 * h], k1[2 * h + 1]);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) mma(acc[2 * np + h], a[L::kPieces - 1], k0[2 * h], k0[2 * h + 1]);
+          for (int i = 0; i < L::kPieces; ++i)
+            ldmatrix(kt + i * L::kRows + unit_at<DK>((np == 3 ? m : np) * 16 + b_row, 2 * ks + (mi & 1)), b[np][i]);
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) mma(acc[2 * np + h], a[0], k0[2 * h], k0[2 * h + 1]);
-      }
+      for (int np = 0; np < 4; ++np)
+        if (np < m || np == 3) {
+#pragma unroll
+          for (int u = L::kPieces == 2 ? 0 : 2; u < 3; ++u)    // (the small products first)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t(&f)[4] = b[np][u == 0 ? L::kPieces - 1 : 0];
+              mma(np == 3 ? acc.diagonal[h] : acc.left[(np == 3 ? 0 : 2 * np) + h], a[u == 1 ? L::kPieces - 1 : 0], f[2 * h], f[2 * h + 1]);
+            }
+        }
     }
   }
-  // times exp(G_i - G_j) and the factors of row and column; 0 above the diagonal.  Then the rows' scales, and in pieces to `to` (the second one
-  // only if it is wanted).
-  template <int M>
-  __device__ __forceinline__ void weigh(float (&acc)[2 * M + 2][4], const float* of_row, bool with_diagonal) const {
-    const int i0 = M * 16 + (lane >> 2), pair = (lane & 3) * 2;
-    const int w0 = s.whole[i0], w1 = s.whole[i0 + 8];
-    const float f0 = of_row[i0], f1 = of_row[i0 + 8];
+  static __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(min(max(e, -127), 127) + 127) << 23); }
+  // times exp(G_i - G_j) and the factors of row and column; 0 above the diagonal, and on it for A.  Left of the diagonal's block
+  // exp(G_i - G_j) is taken apart at the block's first token: what has i is the row's, what has j the column's.
+  __device__ __forceinline__ void weigh(int m, Square& acc, const float* of_row, int diagonal) const {
+    const int i0 = m * 16 + (lane >> 2), pair = (lane & 3) * 2;
+    const int w[2] = {s.whole[i0], s.whole[i0 + 8]}, middle = s.whole[m * 16];
+    const float f[2] = {of_row[i0], of_row[i0 + 8]}, near[2] = {f[0] * power_of_two(w[0] - middle), f[1] * power_of_two(w[1] - middle)};
 #pragma unroll
-    for (int n = 0; n < 2 * M + 2; ++n) {
-      const int j = n * 8 + pair;
+    for (int n = 0; n < 6; ++n) {
+      if (n >= 2 * m) break;
+      const int2 wj = *reinterpret_cast<const int2*>(&s.whole[n * 8 + pair]);
+      const float2 kj = *reinterpret_cast<const float2*>(&s.of_column[n * 8 + pair]);
+      const float far[2] = {kj.x * power_of_two(middle - wj.x), kj.y * power_of_two(middle - wj.y)};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc.left[n][e] *= near[e >> 1] * far[e & 1];
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int j = m * 16 + n * 8 + pair;
       const int2 wj = *reinterpret_cast<const int2*>(&s.whole[j]);
       const float2 kj = *reinterpret_cast<const float2*>(&s.of_column[j]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = i0 + (e >> 1) * 8, jj = j + (e & 1);
-        const int power = min(max((e >> 1 ? w1 : w0) - (e & 1 ? wj.y : wj.x), -127), 127);
-        const float x = acc[n][e] * ((e >> 1 ? f1 : f0) * (e & 1 ? kj.y : kj.x)) * __uint_as_float((uint32_t)(power + 127) << 23);
-        acc[n][e] = n < 2 * M || jj < i || (with_diagonal && jj == i) ? x : 0.0f;
+        const float x = acc.diagonal[n][e] * (f[e >> 1] * (e & 1 ? kj.y : kj.x)) * power_of_two(w[e >> 1] - (e & 1 ? wj.y : wj.x));
+        acc.diagonal[n][e] = j + (e & 1) < i0 + (e >> 1) * 8 + diagonal ? x : 0.0f;
       }
     }
   }
-  template <int M>
-  __device__ __forceinline__ void store_scaled(const float (&acc)[2 * M + 2][4], uint8_t* to, uint32_t second, bool two, float* unscale) const {
-    const int i0 = M * 16 + (lane >> 2), pair = (lane & 3) * 2;
-    float top[2] = {0.0f, 0.0f};
+  // in pieces, rows scaled
+  __device__ __forceinline__ void store_p(int m, const Square& acc, uint8_t* to, float* unscale) const {
+    const int i0 = m * 16 + (lane >> 2), pair = (lane & 3) * 2;
+    float top[2], scale[2];
 #pragma unroll
-    for (int n = 0; n < 2 * M + 2; ++n)
+    for (int h = 0; h < 2; ++h) {
+      top[h] = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) top[e >> 1] = fmaxf(top[e >> 1], fabsf(acc[n][e]));
+      for (int n = 0; n < 2; ++n) top[h] = fmaxf(top[h], fmaxf(fabsf(acc.diagonal[n][2 * h]), fabsf(acc.diagonal[n][2 * h + 1])));
+    }
+#pragma unroll
+    for (int n = 0; n < 6; ++n) {
+      if (n >= 2 * m) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) top[h] = fmaxf(top[h], fmaxf(fabsf(acc.left[n][2 * h]), fabsf(acc.left[n][2 * h + 1])));
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
       top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
+      scale[h] = scale_for(top[h]);
+      if ((lane & 3) == 0) unscale[i0 + 8 * h] = unscale_for(scale[h]);
     }
+    auto store = [&](const float (&x)[4], int n) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float scale = scale_for(top[h]);
-      const int i = i0 + 8 * h;
-      if ((lane & 3) == 0) unscale[i] = unscale_for(scale);
-#pragma unroll
-      for (int n = 0; n < 2 * M + 2; ++n) {
+      for (int h = 0; h < 2; ++h) {
         uint32_t hi, lo;
-        split(acc[n][2 * h] * scale, acc[n][2 * h + 1] * scale, hi, lo);
-        uint8_t* at = to + unit_at<kChunk>(i, n) + pair * 2;
+        split(x[2 * h] * scale[h], x[2 * h + 1] * scale[h], hi, lo);
+        uint8_t* at = to + unit_at<kChunk>(i0 + 8 * h, n) + pair * 2;
         *reinterpret_cast<uint32_t*>(at) = hi;
-        if (two) *reinterpret_cast<uint32_t*>(at + second) = lo;
+        if (L::kPieces == 2) *reinterpret_cast<uint32_t*>(at + L::kSquare) = lo;
       }
+    };
+#pragma unroll
+    for (int n = 0; n < 2; ++n) store(acc.diagonal[n], 2 * m + n);
+#pragma unroll
+    for (int n = 0; n < 6; ++n) {
+      if (n >= 2 * m) break;
+      store(acc.left[n], n);
     }
   }
-
-  // Rows M of A, and the inverse of their diagonal block (left in fp32, and in pieces).
-  template <int M>
-  __device__ __forceinline__ void rows_of_a(uint32_t kt, bool& waited) const {
-    float acc[2 * M + 2][4];
-    square<M>(kt, kt, acc);
-    if (!waited) sync();                                       // (the weights)
-    waited = true;
-    weigh<M>(acc, s.of_a, false);
-    store_scaled<M>(acc, s.A[0], sizeof(s.A[0]), true, s.unscale_a);
-    const int g = lane >> 2, pair = (lane & 3) * 2;
+  __device__ __forceinline__ void store_a(int m, const Square& acc) const {
+    float* to = &s.A[m * 16 + (lane >> 2)][(lane & 3) * 2];
+    auto store = [&](const float (&x)[4], int n) {
+      *reinterpret_cast<float2*>(to + n * 8) = make_float2(x[0], x[1]);
+      *reinterpret_cast<float2*>(to + 8 * kAPitch + n * 8) = make_float2(x[2], x[3]);
+    };
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < 2; ++n) store(acc.diagonal[n], 2 * m + n);
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        *reinterpret_cast<float2*>(&s.diagonal[M][g + 8 * h][n * 8 + pair]) = make_float2(acc[2 * M + n][2 * h], acc[2 * M + n][2 * h + 1]);
+    for (int n = 0; n < 6; ++n) {
+      if (n >= 2 * m) break;
+      store(acc.left[n], n);
+    }
     __syncwarp();
   }
+  // The inverse of A's diagonal block m and 1, in its place: by substitution, a column a lane.
   __device__ __forceinline__ void invert_block(int m) const {
-    float(&d)[16][20] = s.diagonal[m];
-    const int j = lane & 15;                                   // (a column; both halves of the warp do the same)
-    float x[16], top = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i == j ? 1.0f : 0.0f;
-#pragma unroll
-    for (int k = 0; k < 15; ++k)
-#pragma unroll
-      for (int i = k + 1; i < 16; ++i) x[i] = fmaf(-d[i][k], x[k], x[i]);
-    __syncwarp();
+    float* d = &s.A[m * 16][m * 16];
+    const int j = lane & 15;                                   // (both halves of the warp do the same)
+    float x[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      d[i][j] = x[i];
-      top = fmaxf(top, fabsf(x[i]));
-    }
+      float sum[2] = {i == j ? 1.0f : 0.0f, 0.0f};
 #pragma unroll
-    for (int e = 1; e < 16; e *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, e));
-    const float scale = scale_for(top);
-    if (lane == 0) s.of_blocks[m] = unscale_for(scale);
+      for (int k = 0; k < i; k += 4) {
+        const float4 a = *reinterpret_cast<const float4*>(d + i * kAPitch + k);
+        sum[0] = fmaf(-a.x, x[k], sum[0]);
+        if (k + 1 < i) sum[1] = fmaf(-a.y, x[k + 1], sum[1]);
+        if (k + 2 < i) sum[0] = fmaf(-a.z, x[k + 2], sum[0]);
+        if (k + 3 < i) sum[1] = fmaf(-a.w, x[k + 3], sum[1]);
+      }
+      x[i] = sum[0] + sum[1];
+    }
     __syncwarp();
-    const int r = lane >> 1, half = lane & 1;                  // half a row
-    uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 y = *reinterpret_cast<const float2*>(&d[r][half * 8 + 2 * i]);
-      split(y.x * scale, y.y * scale, hi[i], lo[i]);
-    }
-    const uint32_t at = smem_u32(s.blocks[0]) + block_unit(m * 16 + r, half);
-    ptx::st_shared16(at, hi[0], hi[1], hi[2], hi[3]);
-    ptx::st_shared16(at + sizeof(s.blocks[0]), lo[0], lo[1], lo[2], lo[3]);
+    for (int i = 0; i < 16; ++i) d[i * kAPitch + j] = x[i];
   }
-  static __device__ __forceinline__ uint32_t block_unit(int r, int half) { return (uint32_t)(r * 32 + ((half ^ (r >> 2 & 1)) << 4)); }
 
-  // 16 columns J of T below the diagonal block: T_iJ = -T_ii sum_k A_ik T_kJ, i downward, transposed, so that what one product gives is the next one's
-  // left operand.  Then all of the columns, scaled, to `to`.
-  template <int J>
-  __device__ __forceinline__ void columns_of_t(uint32_t to, Weights& w) const {
+  // 16 columns J of T below the diagonal block: T_iJ = -T_ii sum_k A_ik T_kJ, i downward; kept in s.A above the diagonal, transposed.  All are transposed, so
+  // that what one product gives is the next one's left operand.  By TF32 instructions, whose exponents need no scales: operands in two pieces,
+  // three products a term; of eight columns of the left operand the even ones are taken for the first four.  Then all of the columns, scaled, to `to`.
+  __device__ __forceinline__ void columns_of_t(int J, uint32_t to, Weights& w) const {
     const int mi = lane >> 3, r8 = lane & 7, g = lane >> 2, pair = (lane & 3) * 2;
-    const uint32_t blocks = smem_u32(s.blocks[0]), a_at = smem_u32(s.A[0]);
-    float t[4 - J][2][4], unscale[4 - J][2];                   // T_iJ transposed: rows are columns of T
-    uint32_t hi[4 - J][4], lo[4 - J][4];
+    // d += x times (block (i, k) of s.A) transposed
+    auto times = [&](float (&d)[2][4], float (&small)[2][4], const float (&x)[2][4], int i, int k) {
+      const float* from = &s.A[i * 16 + g][k * 16 + pair];
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+      for (int ks = 0; ks < 2; ++ks) {
+        uint32_t ah[4], al[4], bh[2][2], bl[2][2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) t[0][n][e] = s.diagonal[J][n * 8 + pair + (e & 1)][g + 8 * (e >> 1)];
-    {
-      const uint32_t at = blocks + block_unit(J * 16 + (mi >> 1) * 8 + r8, mi & 1);
-      ptx::ldmatrix_x4_trans(at, hi[0]);
-      ptx::ldmatrix_x4_trans(at + sizeof(s.blocks[0]), lo[0]);
-      unscale[0][0] = unscale[0][1] = s.of_blocks[J];
-    }
-    auto times = [&](float (&d)[2][4], const uint32_t (&ah)[4], const uint32_t (&al)[4], uint32_t at, uint32_t second) {
-      uint32_t b[4], bl[4];
-      ldmatrix(at, b);
-      ldmatrix(at + second, bl);
-      float small[2][4];
+        for (int e = 0; e < 4; ++e) split_tf32(x[ks][e], ah[(e & 1) * 2 + (e >> 1)], al[(e & 1) * 2 + (e >> 1)]);
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < 2; ++n) {
+          const float2 b = *reinterpret_cast<const float2*>(from + n * 8 * kAPitch + ks * 8);
+          split_tf32(b.x, bh[n][0], bl[n][0]);
+          split_tf32(b.y, bh[n][1], bl[n][1]);
+        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) d[n][e] = small[n][e] = 0.0f;
+        for (int n = 0; n < 2; ++n) mma_tf32(d[n], ah, bh[n][0], bh[n][1]);
 #pragma unroll
-      for (int n = 0; n < 2; ++n) mma(d[n], ah, b[2 * n], b[2 * n + 1]);
+        for (int n = 0; n < 2; ++n) mma_tf32(small[n], al, bh[n][0], bh[n][1]);
 #pragma unroll
-      for (int n = 0; n < 2; ++n) mma(small[n], al, b[2 * n], b[2 * n + 1]);
-#pragma unroll
-      for (int n = 0; n < 2; ++n) mma(small[n], ah, bl[2 * n], bl[2 * n + 1]);
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) d[n][e] += small[n][e];
+        for (int n = 0; n < 2; ++n) mma_tf32(small[n], ah, bl[n][0], bl[n][1]);
+      }
     };
-    auto in_pieces = [&](const float (&x)[2][4], uint32_t (&h)[4], uint32_t (&l)[4], float (&un)[2]) {
-      float top[2], scale[2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        top[r] = fmaxf(fmaxf(fabsf(x[0][2 * r]), fabsf(x[0][2 * r + 1])), fmaxf(fabsf(x[1][2 * r]), fabsf(x[1][2 * r + 1])));
-        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-        scale[r] = scale_for(top[r]);
-        un[r] = unscale_for(scale[r]);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) split(x[i >> 1][2 * (i & 1)] * scale[i & 1], x[i >> 1][2 * (i & 1) + 1] * scale[i & 1], h[i], l[i]);
-    };
-#pragma unroll
-    for (int i = J + 1; i < 4; ++i) {
-      float m[2][4];
-#pragma unroll
-      for (int k = J; k < i; ++k) {
-        float part[2][4];
-        times(part, hi[k - J], lo[k - J], a_at + unit_at<kChunk>(i * 16 + (mi >> 1) * 8 + r8, 2 * k + (mi & 1)), sizeof(s.A[0]));
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) m[n][e] = k == J ? part[n][e] * unscale[k - J][e >> 1] : fmaf(part[n][e], unscale[k - J][e >> 1], m[n][e]);
-      }
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const float2 f = *reinterpret_cast<const float2*>(&s.unscale_a[i * 16 + n * 8 + pair]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) m[n][e] *= e & 1 ? f.y : f.x;
-      }
-      uint32_t mh[4], ml[4];
-      float un[2];
-      in_pieces(m, mh, ml, un);
-      times(t[i - J], mh, ml, blocks + block_unit(i * 16 + (mi >> 1) * 8 + r8, mi & 1), sizeof(s.blocks[0]));
-      const float f = -s.of_blocks[i];
+    // block (i, J), transposed: rows are columns of T
+    auto block = [&](int i, float (&x)[2][4]) {
+      const float* at = i == J ? &s.A[J * 16 + pair][J * 16 + g] : &s.A[J * 16 + g][i * 16 + pair];
+      const int along = i == J ? kAPitch : 1, across = i == J ? 1 : kAPitch;
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) t[i - J][n][e] *= f * un[e >> 1];
-      if (i < 3) in_pieces(t[i - J], hi[i - J], lo[i - J], unscale[i - J]);
-    }
+        for (int e = 0; e < 4; ++e) x[n][e] = at[(n * 8 + (e & 1)) * along + (e >> 1) * 8 * across];
+    };
+    auto clear = [&](float (&x)[2][4]) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[n][e] = 0.0f;
+    };
     float top = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4 - J; ++i)
+    auto raise = [&](const float (&x)[2][4]) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(t[i][n][e]));
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[n][e]));
+    };
+    float x[2][4];
+    block(J, x);
+    raise(x);
+#pragma unroll 1
+    for (int i = J + 1; i < 4; ++i) {
+      float m[2][4], small[2][4];
+      clear(m);
+      clear(small);
+#pragma unroll 1
+      for (int k = J; k < i; ++k) {
+        block(k, x);
+        times(m, small, x, i, k);
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[n][e] = -(m[n][e] + small[n][e]);
+      clear(x);
+      clear(small);
+      times(x, small, m, i, i);
+      __syncwarp();
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[n][e] += small[n][e];
+          s.A[J * 16 + g + 8 * (e >> 1)][i * 16 + n * 8 + pair + (e & 1)] = x[n][e];
+        }
+      raise(x);
+      __syncwarp();
+    }
     const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
     if (lane == 0) atomicMax(&s.top_t, most);
     sync_four();
     const float scale = scale_for(__uint_as_float(*(volatile uint32_t*)&s.top_t));
     if (J == 0 && lane == 0) w.of_t = unscale_for(scale);
-#pragma unroll
-    for (int i = 0; i < 4 - J; ++i) {
+#pragma unroll 1
+    for (int i = J; i < 4; ++i) {
       uint32_t h[4], l[4];
+      block(i, x);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) split(t[i][u >> 1][2 * (u & 1)] * scale, t[i][u >> 1][2 * (u & 1) + 1] * scale, h[u], l[u]);
-      const uint32_t at = to + unit_at<kChunk>((i + J) * 16 + (mi >> 1) * 8 + r8, 2 * J + (mi & 1));
+      for (int u = 0; u < 4; ++u) split(x[u >> 1][2 * (u & 1)] * scale, x[u >> 1][2 * (u & 1) + 1] * scale, h[u], l[u]);
+      const uint32_t at = to + unit_at<kChunk>(i * 16 + (mi >> 1) * 8 + r8, 2 * J + (mi & 1));
       stmatrix_trans(at, h);
       stmatrix_trans(at + L::kSquare, l);
     }
   }
   static __device__ __forceinline__ void sync_four() { asm volatile("bar.sync 15, 128;" ::: "memory"); }
 
-  template <int M>
-  __device__ __forceinline__ void rows_of_p(uint32_t qt, uint32_t kt, uint32_t stage, Weights& w, bool& waited) const {
-    float acc[2 * M + 2][4];
-    square<M>(qt, kt, acc);
-    if (!waited) sync();
-    waited = true;
-    weigh<M>(acc, s.of_p, true);
-    store_scaled<M>(acc, generic + stage + L::kPAt, L::kSquare, L::kPieces == 2, w.of_p);
-  }
-
   // Chunk of rows first up to first + 64 (or end), which were fetched, into `stage`; the next one is fetched.  Of eight warps four have k, A and
-  // T, the others q, the weights and P; of four all have both.
+  // T, the others q, the weights and P; of four all have both, one after the other.
   __device__ __forceinline__ void prepare(int first, int end, uint32_t stage) {
     Weights& w = *reinterpret_cast<Weights*>(generic + stage + L::kWeightsAt);
     const int64_t at = (int64_t)(head / p.share) * p.dk;
-    const uint32_t kt = smem + stage, qt = kt + L::kQAt;
+    const uint32_t kt = smem + stage;
+    const int from = H == 8 ? warp >> 2 : 0, to = H == 8 ? from + 1 : 2;       // 0: k, 1: q
     if (kStaged) asm volatile("cp.async.wait_all;" ::: "memory");
-    if (H == 4 || warp < 4) rows(static_cast<const T*>(p.k) + at, p.k_stride, first, end, L::kRawAt, kt, s.k_row, s.bad_k);
-    if (H == 4 || warp >= 4) rows(static_cast<const T*>(p.q) + at, p.q_stride, first, end, L::kRawAt + L::kRows, qt, s.q_row, s.bad_q);
+#pragma unroll 1
+    for (int q = from; q < to; ++q)
+      rows(static_cast<const T*>(q ? p.q : p.k) + at, q ? p.q_stride : p.k_stride, first, end, L::kRawAt + q * L::kRows, kt + q * L::kQAt,
+           q ? s.q_row : s.k_row, q ? s.bad_q : s.bad_k);
     sync();
     int broken = 0;
     int64_t all = 0;
     if (warp == kWeigher) weights(w, broken, all);
-    const int m = warp & 3;
-    bool waited = false;
+#pragma unroll 1
+    for (int q = from; q < to; ++q) {
+      const int m = H == 4 && q ? 3 - warp : warp & 3;
+      Square acc;
+      square(kt + q * L::kQAt, kt, m, acc);
+      if (q == from) sync();
+      weigh(m, acc, q ? s.of_p : s.of_a, q);
+      if (q) {
+        store_p(m, acc, generic + stage + L::kPAt, w.of_p);
+      } else {
+        store_a(m, acc);
+        invert_block(m);
+      }
+    }
+    fetch(first + kChunk, end);
     if (H == 4 || warp < 4) {
-      switch (m) {
-        case 0: rows_of_a<0>(kt, waited); break;
-        case 1: rows_of_a<1>(kt, waited); break;
-        case 2: rows_of_a<2>(kt, waited); break;
-        default: rows_of_a<3>(kt, waited); break;
-      }
-      invert_block(m);
       sync_four();
-      fetch(first + kChunk, end);
-      switch (m) {
-        case 0: columns_of_t<0>(kt + L::kTAt, w); break;
-        case 1: columns_of_t<1>(kt + L::kTAt, w); break;
-        case 2: columns_of_t<2>(kt + L::kTAt, w); break;
-        default: columns_of_t<3>(kt + L::kTAt, w); break;
-      }
+      columns_of_t(warp, kt + L::kTAt, w);
     }
-    if (H == 4 || warp >= 4) {
-      switch (H == 4 ? 3 - m : m) {
-        case 0: rows_of_p<0>(qt, kt, stage, w, waited); break;
-        case 1: rows_of_p<1>(qt, kt, stage, w, waited); break;
-        case 2: rows_of_p<2>(qt, kt, stage, w, waited); break;
-        default: rows_of_p<3>(qt, kt, stage, w, waited); break;
-      }
-      if (warp == kWeigher) total(w, broken, all, min(end - first, kChunk));
-      if (H == 8) fetch(first + kChunk, end);
-    }
+    if (warp == kWeigher) total(w, broken, all, min(end - first, kChunk));
   }
 };
 
 // ------------------------------------------------------------------------------------------------ the columns of a warp
 
 // Rows g and g + 8 of accumulators over tokens: from the first token on whose number is not finite all become 0; `from` says which.
-__device__ __noinline__ void clean_copy(float (&x)[8][4], int (&from)[2]) {
+// (In line: register counts set by warpgroup leave no room for calls.)
+__device__ __forceinline__ void clean(float (&x)[8][4], int (&from)[2]) {
   const int pair = (threadIdx.x & 3) * 2;
-  int first[2] = {from[0], from[1]};
 #pragma unroll
   for (int n = 0; n < 8; ++n)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (!(fabsf(x[n][e]) <= FLT_MAX)) first[e >> 1] = min(first[e >> 1], n * 8 + pair + (e & 1));
+      if (!(fabsf(x[n][e]) <= FLT_MAX)) from[e >> 1] = min(from[e >> 1], n * 8 + pair + (e & 1));
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    first[h] = min(first[h], __shfl_xor_sync(0xffffffffu, first[h], 1));
-    first[h] = min(first[h], __shfl_xor_sync(0xffffffffu, first[h], 2));
-    from[h] = first[h];
+    from[h] = min(from[h], __shfl_xor_sync(0xffffffffu, from[h], 1));
+    from[h] = min(from[h], __shfl_xor_sync(0xffffffffu, from[h], 2));
   }
 #pragma unroll
   for (int n = 0; n < 8; ++n)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (n * 8 + pair + (e & 1) >= from[e >> 1]) x[n][e] = 0.0f;
-}
-// (The copy keeps x itself in registers where this is not called.)
-__device__ __forceinline__ void clean(float (&x)[8][4], int (&from)[2]) {
-  float copy[8][4];
-  int first[2] = {from[0], from[1]};
-#pragma unroll
-  for (int n = 0; n < 8; ++n)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) copy[n][e] = x[n][e];
-  clean_copy(copy, first);
-#pragma unroll
-  for (int n = 0; n < 8; ++n)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[n][e] = copy[n][e];
-  from[0] = first[0];
-  from[1] = first[1];
 }
 
 // The largest magnitude of rows g and g + 8, in all four lanes that share them; a NaN where there is one.
