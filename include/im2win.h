@@ -592,15 +592,16 @@ typedef struct {
  * weight [N][K] is dense; x_scales [M], scales [N] and bias [N] (or NULL) hold
  * floats, y elements of `dtype` (any of the three).  The sum is exact (32 bits:
  * K of at most 131071), its conversion to fp32, products with the scales and
- * the bias's addition are fp32, y is rounded once.  The pointers need the
- * alignment of their elements only; rows of x and of the matrix that start on
+ * the bias's addition are fp32, y is rounded once.  Without a workspace there
+ * is no status block: should a bounded wait give up, the y that hang on it are
+ * NaN.  The pointers need the alignment of their elements only; rows of x and of the matrix that start on
  * 16-byte boundaries (K a multiple of 16) are the fast ones.
  */
 im2win_status im2win_matmul_int8(const int8_t* x, const float* x_scales, const int8_t* weight, const float* scales, const float* bias,
                                  void* y, const im2win_int8_shape* shape, im2win_dtype dtype, void* cuda_stream);
 /*
  * How a call whose pointers start on 16-byte boundaries runs such a shape (host-only, static storage; for reports and tests):
- * "registers"; "none" for an invalid shape.
+ * "tiles" (K a multiple of 16, rows of x on 16-byte boundaries: by TMA and tcgen05), "registers"; "none" for an invalid shape.
  */
 const char* im2win_matmul_int8_kernel_name(const im2win_int8_shape* shape, im2win_dtype dtype);
 

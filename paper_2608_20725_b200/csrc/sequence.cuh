@@ -189,6 +189,9 @@ struct Int8Args {
   im2win_int8_shape shape;
   im2win_dtype dtype;
 };
+// Whether rows that start on 16-byte boundaries come by TMA.
+bool matmul_int8_by_tiles(const im2win_int8_shape& s);
+cudaError_t launch_matmul_int8_tiles(const Int8Args& a, cudaStream_t stream);
 cudaError_t launch_matmul_int8_registers(const Int8Args& a, cudaStream_t stream);
 
 }  // namespace im2win

@@ -209,7 +209,7 @@ im2win_status im2win_rms_norm(const void* x, const void* residual, const void* w
 
 const char* im2win_matmul_int8_kernel_name(const im2win_int8_shape* shape, im2win_dtype dtype) {
   if (check_int8(shape, dtype) != IM2WIN_OK) return "none";
-  return "registers";
+  return matmul_int8_by_tiles(*shape) ? "tiles" : "registers";
 }
 
 im2win_status im2win_matmul_int8(const int8_t* x, const float* x_scales, const int8_t* weight, const float* scales, const float* bias,
@@ -222,7 +222,9 @@ im2win_status im2win_matmul_int8(const int8_t* x, const float* x_scales, const i
     if (!aligned_to(at, 4)) return IM2WIN_ERR_MISALIGNED;
   if (shape->M == 0) return IM2WIN_OK;
   const Int8Args a = {x, x_scales, weight, scales, bias, y, *shape, dtype};
-  return from_launch(launch_matmul_int8_registers(a, static_cast<cudaStream_t>(cuda_stream)));
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const bool tiles = matmul_int8_by_tiles(*shape) && aligned_to(x, 16) && aligned_to(weight, 16);
+  return from_launch(tiles ? launch_matmul_int8_tiles(a, stream) : launch_matmul_int8_registers(a, stream));
 }
 
 }  // extern "C"
