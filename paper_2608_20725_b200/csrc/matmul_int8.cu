@@ -17,12 +17,11 @@ namespace {
 using namespace ptx;
 
 constexpr int kRows = 128;               // of x, of a CTA's tile
-constexpr int kBlock = 128;              // elements (bytes) along K of a stage
+constexpr int kBlock = 128;              // elements (bytes) along K of a copy
 constexpr int kMaxStages = 12;
 constexpr int kFinishers = 8;            // warps that make y
 constexpr int kFirstFinisher = 4;
 constexpr int kThreads = (kFirstFinisher + kFinishers) * 32;
-constexpr uint32_t kRingBytes = 200 * 1024;
 constexpr int kGroup = 8;                // row tiles that are worked on together, so that what is read of x and the matrix stays in the L2 cache
 
 struct MatmulParams {
@@ -31,9 +30,10 @@ struct MatmulParams {
   const float* bias;
   void* y;
   int64_t y_stride;
-  int32_t M, N, blocks;                  // blocks: of K
+  int32_t M, N, blocks;                  // blocks: of K, of as many bytes as a stage has
   int32_t tiles_m, tiles_n;              // tiles_m: of the CTA or the pair
-  int32_t stages, vectors;               // vectors: rows of y start on 16-byte boundaries
+  int32_t x_rows, parts, stages;         // rows of x of a copy; 128-byte parts of a stage; stages
+  int32_t vectors;                       // whether rows of y start on 16-byte boundaries
   uint32_t polls;                        // looks, of a microsecond at most, before a wait gives up
   int32_t drop;                          // testing aid: the first CTA (pair) does not say that the sums of this tile of its are done (-1: it does)
 };
@@ -77,12 +77,12 @@ __host__ __device__ constexpr uint32_t instr_desc_i8(int M, int N) {
   return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-template <int BN, bool PAIR>
+template <typename T, int BN, bool PAIR>
 struct Tile {
+  static constexpr uint32_t kRingBytes = (sizeof(T) == 4 ? 184 : 200) * 1024;          // (beside what turns y)
   static constexpr int kMatrixRows = PAIR ? BN / 2 : BN;       // that a CTA stages
-  static constexpr uint32_t kA = kRows * kBlock, kB = kMatrixRows * kBlock, kStage = kA + kB;
-  static constexpr int kStages = kRingBytes / kStage < kMaxStages ? kRingBytes / kStage : kMaxStages;
-  static constexpr uint32_t kColumns = 2 * BN;                 // of tensor memory (BN >= 16)
+  static constexpr uint32_t kB = kMatrixRows * kBlock;
+  static constexpr uint32_t kColumns = 2 * BN;                 // of tensor memory
 };
 
 // Tile number w as (tile of rows, tile of columns): row tiles by groups, within a group the columns outermost.
@@ -96,11 +96,12 @@ __device__ __forceinline__ void place(const MatmulParams& p, int64_t w, int& tm,
 
 template <typename T, int BN, bool PAIR>
 __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUtensorMap& matrix_map, const MatmulParams& p) {
-  using L = Tile<BN, PAIR>;
+  using L = Tile<T, BN, PAIR>;
   extern __shared__ uint8_t dynamic_smem[];
   __shared__ __align__(8) uint64_t bars[2 * kMaxStages + 4];   // stages full, empty; sums done, taken (two)
   __shared__ uint32_t tmem_base_at, gave_up;
   __shared__ __align__(16) float factors[kFinishers][2][32];   // scales and bias of a warp's columns
+  __shared__ T turned[kFinishers][32][sizeof(T) == 4 ? 33 : 34];           // 32 x 32 of y on their way to rows that start anywhere
   const uint32_t ring = (smem_u32(dynamic_smem) + 1023u) & ~1023u;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
@@ -121,8 +122,8 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    if (PAIR) tmem_alloc_pair(smem_u32(&tmem_base_at), L::kColumns < 32 ? 32 : L::kColumns);
-    else tmem_alloc(smem_u32(&tmem_base_at), L::kColumns < 32 ? 32 : L::kColumns);
+    if (PAIR) tmem_alloc_pair(smem_u32(&tmem_base_at), L::kColumns);
+    else tmem_alloc(smem_u32(&tmem_base_at), L::kColumns);
   }
   tc_fence_before();
   __syncthreads();
@@ -145,6 +146,8 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
     return false;
   };
 
+  const uint32_t x_bytes = (uint32_t)p.x_rows * kBlock, part_bytes = x_bytes + L::kB, stage_bytes = p.parts * part_bytes;
+
   if (warp == 0) {
     const bool elected = elect_one();
     const uint32_t to_full = PAIR ? mapa_shared(full, 0) : full;             // the leader's
@@ -157,19 +160,24 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
       for (int b = 0; b < p.blocks; ++b) {
         if (!wait(empty + 8 * stage, phase)) break;
         if (elected) {
-          const uint32_t to = ring + stage * L::kStage, bar = to_full + 8 * stage;
-          // (what lies beyond a matrix reads as 0 and counts; in a pair the leader announces the bytes of both)
-          if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, (PAIR ? 2u : 1u) * L::kStage);
-          if (PAIR) {
-            tma_load_2d_pair(to, &x_map, b * kBlock, m0, bar);
-            tma_load_2d_pair(to + L::kA, &matrix_map, b * kBlock, n0, bar);
-          } else {
-            tma_load_2d(to, &x_map, b * kBlock, m0, bar);
-            tma_load_2d(to + L::kA, &matrix_map, b * kBlock, n0, bar);
+          const uint32_t bar = to_full + 8 * stage;
+          uint32_t to = ring + stage * stage_bytes;
+          // (What lies beyond a matrix reads as 0 and counts; in a pair the leader announces the bytes of both.  Of few rows no more than those, eight at a
+          // time, are copied; what the products find in the others' place makes sums that are not looked at.)
+          if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, (PAIR ? 2u : 1u) * stage_bytes);
+          for (int i = 0; i < p.parts; ++i, to += part_bytes) {
+            const int k = (b * p.parts + i) * kBlock;
+            if (PAIR) {
+              tma_load_2d_pair(to, &x_map, k, m0, bar);
+              tma_load_2d_pair(to + x_bytes, &matrix_map, k, n0, bar);
+            } else {
+              tma_load_2d(to, &x_map, k, m0, bar);
+              tma_load_2d(to + x_bytes, &matrix_map, k, n0, bar);
+            }
           }
         }
         __syncwarp();
-        if (++stage == L::kStages) stage = 0, phase ^= 1;
+        if (++stage == p.stages) stage = 0, phase ^= 1;
       }
     }
   } else if (warp == 1 && rank == 0) {
@@ -185,14 +193,17 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
       for (int b = 0; b < p.blocks; ++b) {
         if (!wait(full + 8 * stage, phase)) break;
         if (elected) {
-          const uint32_t a = smem_desc_lo(ring + stage * L::kStage), m = smem_desc_lo(ring + stage * L::kStage + L::kA);
+          uint32_t a = smem_desc_lo(ring + stage * stage_bytes);
+          for (int i = 0; i < p.parts; ++i, a += part_bytes >> 4) {
+            const uint32_t m = a + (x_bytes >> 4);
 #pragma unroll
-          for (int j = 0; j < kBlock / 32; ++j) umma_i8<PAIR>(to, a + 2 * j, m + 2 * j, kDesc, b > 0 || j > 0);
+            for (int j = 0; j < kBlock / 32; ++j) umma_i8<PAIR>(to, a + 2 * j, m + 2 * j, kDesc, b > 0 || i > 0 || j > 0);
+          }
           if (PAIR) umma_commit_pair(empty + 8 * stage);
           else umma_commit(empty + 8 * stage);
         }
         __syncwarp();
-        if (++stage == L::kStages) stage = 0, phase ^= 1;
+        if (++stage == p.stages) stage = 0, phase ^= 1;
       }
       if (!failed && elected && !(first == 0 && (int)it == p.drop)) {
         if (PAIR) umma_commit_pair(done + 8 * buffer);
@@ -203,7 +214,6 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
   } else if (warp >= kFirstFinisher) {
     const int index = warp - kFirstFinisher;
     constexpr int kParts = BN >= 64 ? 2 : 1;                   // of the columns; otherwise the upper four warps have nothing to do
-    constexpr int kWidth = BN < 32 ? BN : 32;
     const int row = (warp & 3) * 32 + lane, part = index >> 2;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;
     const uint32_t to_taken = PAIR ? mapa_shared(taken, 0) : taken;
@@ -218,7 +228,7 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
       tc_fence_after();
       if (part < kParts) {
 #pragma unroll 1
-        for (int c = part * (BN / kParts); c < (part + 1) * (BN / kParts); c += kWidth) {
+        for (int c = part * (BN / kParts); c < (part + 1) * (BN / kParts); c += 32) {
           const int n0 = tn * BN + c;
           if (n0 >= p.N) break;
           uint32_t sum[32];
@@ -230,9 +240,9 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
           __syncwarp();
           if (!failed) tmem_ld_wait_for(sum);
           if (m < p.M) {
-            float v[kWidth];
+            float v[32];
 #pragma unroll
-            for (int j = 0; j < kWidth; j += 4) {
+            for (int j = 0; j < 32; j += 4) {
               const float4 f = *reinterpret_cast<const float4*>(&factors[index][0][j]), a = *reinterpret_cast<const float4*>(&factors[index][1][j]);
               const float fs[4] = {f.x, f.y, f.z, f.w}, as[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -243,10 +253,10 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
               }
             }
             T* to = static_cast<T*>(p.y) + (int64_t)m * p.y_stride + n0;
-            if (p.vectors && n0 + kWidth <= p.N) {
+            if (p.vectors && n0 + 32 <= p.N) {
               constexpr int V = 16 / sizeof(T);
 #pragma unroll
-              for (int j = 0; j < kWidth; j += V) {
+              for (int j = 0; j < 32; j += V) {
                 Vec<T, V> out;
 #pragma unroll
                 for (int e = 0; e < V; ++e) out.v[e] = from_float<T>(v[j + e]);
@@ -254,9 +264,15 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
               }
             } else {
 #pragma unroll
-              for (int j = 0; j < kWidth; ++j)
-                if (n0 + j < p.N) to[j] = from_float<T>(v[j]);
+              for (int j = 0; j < 32; ++j) turned[index][lane][j] = from_float<T>(v[j]);
             }
+          }
+          if (!(p.vectors && n0 + 32 <= p.N)) {                // a row at a time
+            __syncwarp();
+            const int rows = min(32, p.M - (m - lane));
+            T* to = static_cast<T*>(p.y) + (int64_t)(m - lane) * p.y_stride + n0 + lane;
+            if (there)
+              for (int r = 0; r < rows; ++r) to[(int64_t)r * p.y_stride] = turned[index][r][lane];
           }
           __syncwarp();
         }
@@ -279,8 +295,8 @@ __device__ __forceinline__ void matmul_body(const CUtensorMap& x_map, const CUte
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
-    if (PAIR) tmem_dealloc_pair(tmem, L::kColumns < 32 ? 32 : L::kColumns);
-    else tmem_dealloc(tmem, L::kColumns < 32 ? 32 : L::kColumns);
+    if (PAIR) tmem_dealloc_pair(tmem, L::kColumns);
+    else tmem_dealloc(tmem, L::kColumns);
   }
 }
 
@@ -318,8 +334,8 @@ bool encode(EncodeTiledFn fn, CUtensorMap* map, const int8_t* at, int64_t rows, 
 
 template <typename T, int BN, bool PAIR>
 cudaError_t launch(const Int8Args& a, cudaStream_t stream) {
-  using L = Tile<BN, PAIR>;
-  constexpr uint32_t kBytes = L::kStages * L::kStage + 1024;
+  using L = Tile<T, BN, PAIR>;
+  constexpr uint32_t kBytes = L::kRingBytes + 1024;
   const im2win_int8_shape& s = a.shape;
   static bool attr_done[64] = {};
   int dev = 0;
@@ -335,11 +351,18 @@ cudaError_t launch(const Int8Args& a, cudaStream_t stream) {
   const EncodeTiledFn fn = get_encode_fn();
   if (!fn) return cudaErrorNotSupported;
   CUtensorMap x_map, matrix_map;
-  if (!encode(fn, &x_map, a.x, s.M, s.K, s.x_stride, kRows) || !encode(fn, &matrix_map, a.weight, s.N, s.K, s.K, L::kMatrixRows))
+  const int x_rows = s.M >= kRows ? kRows : (s.M + 7) / 8 * 8;
+  if (!encode(fn, &x_map, a.x, s.M, s.K, s.x_stride, x_rows) || !encode(fn, &matrix_map, a.weight, s.N, s.K, s.K, L::kMatrixRows))
     return cudaErrorInvalidValue;
   const int rows = PAIR ? 2 * kRows : kRows;
-  MatmulParams p = {a.x_scales, a.scales, a.bias, a.y, s.y_stride, s.M, s.N, (s.K + kBlock - 1) / kBlock, (int32_t)(((int64_t)s.M + rows - 1) / rows),
-                    (int32_t)(((int64_t)s.N + BN - 1) / BN), L::kStages, 0, 4000000u, -1};
+  MatmulParams p = {a.x_scales, a.scales, a.bias, a.y, s.y_stride, s.M, s.N, 0, (int32_t)(((int64_t)s.M + rows - 1) / rows),
+                    (int32_t)(((int64_t)s.N + BN - 1) / BN), x_rows, 1, 0, 0, 4000000u, -1};
+  // A stage takes some 0.2 us whatever it holds (8 rows x 4096 x 4096: 10.4 us with 32 stages' worth, 7.8 with 8), so that small ones are put together, and the ring is to
+  // hold four of them.  (Of few rows of x the products read on behind them: the last stage ends 16 KB before the ring does.)
+  const uint32_t part = x_rows * kBlock + L::kB, most = L::kRingBytes - (kRows - x_rows) * kBlock;
+  while (p.parts < 4 && 2 * p.parts * part <= most / 4 && p.parts * kBlock < s.K) p.parts *= 2;
+  p.stages = std::min<int>(kMaxStages, most / (p.parts * part));
+  p.blocks = (s.K + p.parts * kBlock - 1) / (p.parts * kBlock);
   p.vectors = aligned_to(a.y, 16) && s.y_stride * sizeof(T) % 16 == 0;
   if (const char* v = debug_getenv("IM2WIN_MATMUL_DROP")) {    // testing aid
     p.drop = atoi(v);

@@ -44,9 +44,10 @@ __device__ __forceinline__ int nearest(float product, float per_top, float h, fl
   return (int)rint((double)h * (double)w * 127.0 / top);
 }
 
-// THREADS: of a row, 32 (a block has four rows) or all of the block's.  V: elements of a vector; N vectors a thread, or (N == 0) any
-// number, read twice.
-template <typename T, int V, int N, bool WARP>
+// WARP: a row is a warp's (a block has four), otherwise all of the block's.  V: elements of a vector; N vectors a thread, or (N == 0) any
+// number, read twice.  BYTES: y in 8 bits, a kernel of its own for its registers.  (16384 rows of 4096 bf16 with a residual, 84 us at 6.4 TB/s, took 127 with
+// both in one kernel and the residual's loads behind a question each.)
+template <typename T, int V, int N, bool WARP, bool BYTES>
 __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormParams p) {
   using VT = Vec<T, V>;
   using VB = Vec<int8_t, V>;
@@ -60,15 +61,15 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
   T* out = p.residual_out ? static_cast<T*>(p.residual_out) + row * p.residual_out_stride : nullptr;
   const T* weight = static_cast<const T*>(p.weight);
   const int vectors = p.channels / V;                          // (V divides the channels)
-  const bool bytes = p.scales != nullptr;
 
-  auto load = [&](int i) {
-    VT h = *reinterpret_cast<const VT*>(x + (int64_t)i * V);
-    if (residual) {
-      const VT r = *reinterpret_cast<const VT*>(residual + (int64_t)i * V);
+  auto at = [&](const T* from, int i) { return *reinterpret_cast<const VT*>(from + (int64_t)i * V); };
+  auto add = [&](VT& h, const VT& r) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) h.v[j] = from_float<T>(to_float(h.v[j]) + to_float(r.v[j]));
-    }
+    for (int j = 0; j < V; ++j) h.v[j] = from_float<T>(to_float(h.v[j]) + to_float(r.v[j]));
+  };
+  auto load = [&](int i) {
+    VT h = at(x, i);
+    if (residual) add(h, at(residual, i));
     return h;
   };
   auto weights = [&](int i) {
@@ -85,7 +86,7 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
   auto look = [&](const VT& h, int i) {
 #pragma unroll
     for (int j = 0; j < V; ++j) sum = fmaf(to_float(h.v[j]), to_float(h.v[j]), sum);
-    if (bytes) {
+    if (BYTES) {
       const VT w = weights(i);
 #pragma unroll
       for (int j = 0; j < V; ++j) top = max_nan(top, fabsf(to_float(h.v[j]) * to_float(w.v[j])));
@@ -95,15 +96,22 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
   if constexpr (N > 0) {
 #pragma unroll
     for (int n = 0; n < N; ++n)
-      if (tid + n * threads < vectors) kept[n] = load(tid + n * threads);
+      if (tid + n * threads < vectors) kept[n] = at(x, tid + n * threads);
+    if (residual) {
+      VT more[N];                                              // (all loads under way before the first sum)
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int i = tid + n * threads;
-      if (i < vectors) {
-        if (out) *reinterpret_cast<VT*>(out + (int64_t)i * V) = kept[n];
-        look(kept[n], i);
-      }
+      for (int n = 0; n < N; ++n)
+        if (tid + n * threads < vectors) more[n] = at(residual, tid + n * threads);
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        if (tid + n * threads < vectors) {
+          add(kept[n], more[n]);
+          if (out) *reinterpret_cast<VT*>(out + (int64_t)(tid + n * threads) * V) = kept[n];
+        }
     }
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (tid + n * threads < vectors) look(kept[n], tid + n * threads);
   } else {
     for (int i = tid; i < vectors; i += threads) {
       const VT h = load(i);
@@ -133,7 +141,7 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
   }
   const float rate = rsqrtf(sum / (float)p.channels + p.eps);
 
-  if (!bytes) {
+  if constexpr (!BYTES) {
     T* y = static_cast<T*>(p.y) + row * p.y_stride;
     auto finish = [&](const VT& h, int i) {
       const VT w = weights(i);
@@ -150,90 +158,91 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
       for (int i = tid; i < vectors; i += threads) finish(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
     }
     return;
-  }
-  const bool fine = top <= FLT_MAX;                            // (not of a NaN)
-  if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7fffffff) : top * rate / 127.0f;
-  // fp32: the largest product in 64 bits, and all below 2^-90: products that fp32 does not hold exactly
-  const bool in_64 = sizeof(T) == 4 || top < 8e-28f;
-  double exact_top = top;
-  if (fine && in_64) {                                         // (the same for all threads of the row)
-    double most = 0.0;
-    auto raise = [&](const VT& h, int i) {
+  } else {
+    const bool fine = top <= FLT_MAX;                            // (not of a NaN)
+    if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7fffffff) : top * rate / 127.0f;
+    // fp32: the largest product in 64 bits, and all below 2^-90: products that fp32 does not hold exactly
+    const bool in_64 = sizeof(T) == 4 || top < 8e-28f;
+    double exact_top = top;
+    if (fine && in_64) {                                         // (the same for all threads of the row)
+      double most = 0.0;
+      auto raise = [&](const VT& h, int i) {
+        const VT w = weights(i);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float a = to_float(h.v[j]), b = to_float(w.v[j]);
+          if (fabsf(a * b) == top) most = fmax(most, fabs((double)a * (double)b));
+        }
+      };
+      if constexpr (N > 0) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if (tid + n * threads < vectors) raise(kept[n], tid + n * threads);
+      } else {
+        for (int i = tid; i < vectors; i += threads) raise(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
+      }
+#pragma unroll
+      for (int s = 16; s > 0; s /= 2) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, s));
+      if constexpr (!WARP) {
+        __shared__ double shared_most[32];
+        if (lane == 0) shared_most[warp] = most;
+        __syncthreads();
+        most = lane < threads / 32 ? shared_most[lane] : 0.0;
+#pragma unroll
+        for (int s = 16; s > 0; s /= 2) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, s));
+      }
+      exact_top = most;
+    }
+    int8_t* y = static_cast<int8_t*>(p.y) + row * p.y_stride;
+    const bool zero = !fine || exact_top == 0.0;
+    const bool tiny = top < 8e-28f;                              // (products lose bits, and 127 / top is out of range)
+    const float per_top = zero ? 0.0f : 127.0f / top;
+    auto finish = [&](const VT& h, int i) {
       const VT w = weights(i);
+      VB r;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float a = to_float(h.v[j]), b = to_float(w.v[j]);
-        if (fabsf(a * b) == top) most = fmax(most, fabs((double)a * (double)b));
+        r.v[j] = zero ? 0 : tiny ? (int8_t)rint((double)a * (double)b * 127.0 / exact_top) : (int8_t)nearest(a * b, per_top, a, b, exact_top);
       }
+      *reinterpret_cast<VB*>(y + (int64_t)i * V) = r;
     };
     if constexpr (N > 0) {
 #pragma unroll
       for (int n = 0; n < N; ++n)
-        if (tid + n * threads < vectors) raise(kept[n], tid + n * threads);
+        if (tid + n * threads < vectors) finish(kept[n], tid + n * threads);
     } else {
-      for (int i = tid; i < vectors; i += threads) raise(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
+      for (int i = tid; i < vectors; i += threads) finish(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
     }
-#pragma unroll
-    for (int s = 16; s > 0; s /= 2) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, s));
-    if constexpr (!WARP) {
-      __shared__ double shared_most[32];
-      if (lane == 0) shared_most[warp] = most;
-      __syncthreads();
-      most = lane < threads / 32 ? shared_most[lane] : 0.0;
-#pragma unroll
-      for (int s = 16; s > 0; s /= 2) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, s));
-    }
-    exact_top = most;
-  }
-  int8_t* y = static_cast<int8_t*>(p.y) + row * p.y_stride;
-  const bool zero = !fine || exact_top == 0.0;
-  const bool tiny = top < 8e-28f;                              // (products lose bits, and 127 / top is out of range)
-  const float per_top = zero ? 0.0f : 127.0f / top;
-  auto finish = [&](const VT& h, int i) {
-    const VT w = weights(i);
-    VB r;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float a = to_float(h.v[j]), b = to_float(w.v[j]);
-      r.v[j] = zero ? 0 : tiny ? (int8_t)rint((double)a * (double)b * 127.0 / exact_top) : (int8_t)nearest(a * b, per_top, a, b, exact_top);
-    }
-    *reinterpret_cast<VB*>(y + (int64_t)i * V) = r;
-  };
-  if constexpr (N > 0) {
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-      if (tid + n * threads < vectors) finish(kept[n], tid + n * threads);
-  } else {
-    for (int i = tid; i < vectors; i += threads) finish(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
   }
 }
 
 // Rows of up to 1024 elements (128 where they do not lie on vectors) are a warp's; others a block's of as many threads as make four
 // vectors each or fewer, and one each where there are few rows and a row's time is its latency.
-template <typename T, int V>
+template <typename T, int V, bool BYTES>
 cudaError_t launch(const NormParams& p, cudaStream_t stream) {
   constexpr int kMost = V > 1 ? 4 : 16;
   const int64_t vectors = p.channels / V;
   if (vectors <= 128) {
     const unsigned grid = (unsigned)(((int64_t)p.rows + 3) / 4);
     if (vectors <= 32)
-      rms_norm_kernel<T, V, 1, true><<<grid, 128, 0, stream>>>(p);
+      rms_norm_kernel<T, V, 1, true, BYTES><<<grid, 128, 0, stream>>>(p);
     else
-      rms_norm_kernel<T, V, 4, true><<<grid, 128, 0, stream>>>(p);
+      rms_norm_kernel<T, V, 4, true, BYTES><<<grid, 128, 0, stream>>>(p);
     return cudaGetLastError();
   }
   const bool few = p.rows <= 592;
   auto threads_for = [&](int each) { return (int)((vectors + each * 32 - 1) / (each * 32) * 32); };
   if (few && vectors <= 1024)
-    rms_norm_kernel<T, V, 1, false><<<p.rows, threads_for(1), 0, stream>>>(p);
+    rms_norm_kernel<T, V, 1, false, BYTES><<<p.rows, threads_for(1), 0, stream>>>(p);
   else if (vectors <= 512)
-    rms_norm_kernel<T, V, 2, false><<<p.rows, threads_for(2), 0, stream>>>(p);
+    rms_norm_kernel<T, V, 2, false, BYTES><<<p.rows, threads_for(2), 0, stream>>>(p);
   else if (vectors <= 1024 * 4)
-    rms_norm_kernel<T, V, 4, false><<<p.rows, std::min(threads_for(4), 1024), 0, stream>>>(p);
+    rms_norm_kernel<T, V, 4, false, BYTES><<<p.rows, std::min(threads_for(4), 1024), 0, stream>>>(p);
   else if (V == 1 && vectors <= 1024 * kMost)
-    rms_norm_kernel<T, V, kMost, false><<<p.rows, threads_for(kMost), 0, stream>>>(p);
+    rms_norm_kernel<T, V, kMost, false, BYTES><<<p.rows, threads_for(kMost), 0, stream>>>(p);
   else
-    rms_norm_kernel<T, V, 0, false><<<p.rows, 1024, 0, stream>>>(p);
+    rms_norm_kernel<T, V, 0, false, BYTES><<<p.rows, 1024, 0, stream>>>(p);
   return cudaGetLastError();
 }
 
@@ -244,8 +253,8 @@ cudaError_t launch_type(const NormParams& p, cudaStream_t stream) {
   if (p.channels % V == 0 && rows_on(p.x, p.x_stride, sizeof(T)) && rows_on(p.residual, p.residual_stride, sizeof(T)) &&
       rows_on(p.residual_out, p.residual_out_stride, sizeof(T)) && rows_on(p.weight, 0, sizeof(T)) &&
       rows_on(p.y, p.y_stride, p.scales ? 1 : sizeof(T)))
-    return launch<T, V>(p, stream);
-  return launch<T, 1>(p, stream);
+    return p.scales ? launch<T, V, true>(p, stream) : launch<T, V, false>(p, stream);
+  return p.scales ? launch<T, 1, true>(p, stream) : launch<T, 1, false>(p, stream);
 }
 
 }  // namespace
