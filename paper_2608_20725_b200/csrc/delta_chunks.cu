@@ -193,9 +193,7 @@ template <typename T, int DK, int H>
 struct Helpers {
   using L = Layout<T, DK>;
   static constexpr int kThreads = H * 32;
-  static constexpr int kShare = 2;                             // threads of a row
   static constexpr int kWeigher = H == 8 ? 4 : 0;              // the warp that sums up decays
-  static constexpr int kUnits = DK / 8 / kShare;               // 16-byte units (of 16-bit elements) of a thread: every kShare-th one
   static constexpr bool kStaged = L::kRawAt != 0;
 
   const ChunkParams& p;
@@ -210,43 +208,44 @@ struct Helpers {
 
   static __device__ __forceinline__ void sync() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
 
-  // The next chunk's rows on their way: of 16 bits and in whole vectors to shared memory, where each thread finds what it has copied itself.
-  __device__ __forceinline__ void fetch(int first, int end) {
+  // The next chunk on its way: its decays and betas, and its rows, of 16 bits and in whole vectors to shared memory, by four warps.
+  __device__ __forceinline__ void fetch_gates(int first, int end) {
     g[0] = g[1] = b[0] = b[1] = 0.0f;
-    if (warp == kWeigher) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int64_t at = first + 2 * lane + i;
-        if (at < end) {
-          g[i] = p.decay[at * p.decay_stride + head];
-          b[i] = p.beta[at * p.beta_stride + head];
-        }
+    for (int i = 0; i < 2; ++i) {
+      const int64_t at = first + 2 * lane + i;
+      if (at < end) {
+        g[i] = p.decay[at * p.decay_stride + head];
+        b[i] = p.beta[at * p.beta_stride + head];
       }
     }
-    if constexpr (kStaged) {
-      if (p.qk_vectors) {
-        const int r = (t & 127) / kShare, part = t % kShare;
-        const bool row = first + r < end;
-        const T* k = static_cast<const T*>(p.k) + (int64_t)(head / p.share) * p.dk;
-        const T* q = static_cast<const T*>(p.q) + (int64_t)(head / p.share) * p.dk;
-        const T* kr = k + (row ? (int64_t)(first + r) * p.k_stride : 0);
-        const T* qr = q + (row ? (int64_t)(first + r) * p.q_stride : 0);
+  }
+  __device__ __forceinline__ void fetch_rows(int first, int end) const {
+    if (kStaged && p.qk_vectors) {
+      const int r = (t & 127) >> 1, part = t & 1;
+      const bool row = first + r < end;
+      const int64_t at = (int64_t)(head / p.share) * p.dk;
+      const T* k = static_cast<const T*>(p.k) + at;
+      const T* q = static_cast<const T*>(p.q) + at;
+      const T* kr = k + (row ? (int64_t)(first + r) * p.k_stride : 0);
+      const T* qr = q + (row ? (int64_t)(first + r) * p.q_stride : 0);
 #pragma unroll 1
-        for (int i = 0; i < kUnits; ++i) {
-          const int unit = i * kShare + part;
-          const bool there = row && unit * 8 < p.dk;
-          if (H == 4 || warp < 4) copy16(smem + L::kRawAt + unit_at<DK>(r, unit), there ? kr + unit * 8 : k, there);
-          if (H == 4 || warp >= 4) copy16(smem + L::kRawAt + L::kRows + unit_at<DK>(r, unit), there ? qr + unit * 8 : q, there);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+      for (int unit = part; unit < DK / 8; unit += 2) {
+        const bool there = row && unit * 8 < p.dk;
+        copy16(smem + L::kRawAt + unit_at<DK>(r, unit), there ? kr + unit * 8 : k, there);
+        copy16(smem + L::kRawAt + L::kRows + unit_at<DK>(r, unit), there ? qr + unit * 8 : q, there);
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
   }
 
   // Rows of q or k of a chunk to shared memory, in pieces, scaled where they are not fp16 already.  Leaves what a row is multiplied by (the
   // norm's and the scale's reciprocals) and says which rows are not finite (they come out as 0).
-  __device__ __forceinline__ void rows(const T* from, int64_t stride, int first, int end, uint32_t raw, uint32_t to, float* factor, uint32_t* bad) {
-    const int r = (t & 127) / kShare, part = t % kShare;
+  // SHARE threads of u = 0, 1, .. have a row.
+  template <int SHARE>
+  __device__ __forceinline__ void rows(int u, const T* from, int64_t stride, int first, int end, uint32_t raw, uint32_t to, float* factor, uint32_t* bad) const {
+    constexpr int kShare = SHARE, kUnits = DK / 8 / SHARE;     // 16-byte units (of 16-bit elements) of a thread: every SHARE-th one
+    const int r = u / kShare, part = u % kShare;
     const bool there = first + r < end;
     const T* row = from + (there ? (int64_t)(first + r) * stride : 0);
     float top = 0.0f, squares[2] = {0.0f, 0.0f}, scale = 1.0f;
@@ -278,7 +277,8 @@ struct Helpers {
       }
       const float2 f = Half<T>::unpack(most);
       top = max_nan(f.x, f.y);
-      top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+#pragma unroll
+      for (int d = 1; d < kShare; d *= 2) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
       const bool odd = !(top <= FLT_MAX);
       if (!Half<T>::kExact) scale = scale_for(top);
 #pragma unroll 2
@@ -316,7 +316,8 @@ struct Helpers {
           top = max_nan(top, fabsf(x[i][j]));
           squares[j & 1] = fmaf(x[i][j], x[i][j], squares[j & 1]);
         }
-      top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+#pragma unroll
+      for (int d = 1; d < kShare; d *= 2) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
       const bool odd = !(top <= FLT_MAX);
       scale = scale_for(top);
 #pragma unroll
@@ -333,23 +334,30 @@ struct Helpers {
       }
     }
     squares[0] += squares[1];
-    squares[0] += __shfl_xor_sync(0xffffffffu, squares[0], 1);
+#pragma unroll
+    for (int d = 1; d < kShare; d *= 2) squares[0] += __shfl_xor_sync(0xffffffffu, squares[0], d);
     const bool odd = !(top <= FLT_MAX);
-    const uint32_t odd_rows = __ballot_sync(0xffffffffu, odd); // (two bits a row)
+    const uint32_t odd_rows = __ballot_sync(0xffffffffu, odd); // (SHARE bits a row)
     if (part == 0) factor[r] = odd ? 0.0f : (p.normalize ? rsqrtf(squares[0] + kNormalizeEps) : 1.0f) * unscale_for(scale);
     if (lane == 0) {
       uint32_t bits = 0;
       if (odd_rows) {
 #pragma unroll 1
-        for (int i = 0; i < 16; ++i) bits |= (odd_rows >> (2 * i) & 1u) << i;
+        for (int i = 0; i < 32 / kShare; ++i) bits |= (odd_rows >> (kShare * i) & 1u) << i;
       }
-      reinterpret_cast<uint16_t*>(bad)[warp & 3] = (uint16_t)bits;
+      if constexpr (kShare == 2) reinterpret_cast<uint16_t*>(bad)[u >> 5] = (uint16_t)bits;
+      else reinterpret_cast<uint8_t*>(bad)[u >> 5] = (uint8_t)bits;
     }
   }
 
+  // What the weigher keeps of its tokens, 2l and 2l+1, from k's weights to q's.
+  struct Sums {
+    int broken;                          // the first token from which nothing is finite any more
+    int64_t all;                         // G_n
+    float from_start[2], part[2];        // exp(G_i), and its part of a power of two
+  };
   // One warp: lane l has tokens 2l and 2l+1.  Sums of log_decay are of whole numbers of 2^-44 powers of two: exact.
-  __device__ __forceinline__ void weights(Weights& w, int& broken, int64_t& all) const {
-    constexpr float kNaN = __builtin_nanf("");
+  __device__ __forceinline__ void weights_of_k(Weights& w, Sums& kept) const {
     auto powers = [](float x) -> int64_t {                     // (beyond 2^+-1000 nothing changes in fp32)
       return __double2ll_rn((double)fminf(fmaxf(x, -700.0f), 700.0f) * (1.4426950408889634074 * 17592186044416.0));
     };
@@ -361,9 +369,8 @@ struct Helpers {
       const bool row = (s.bad_k[lane >> 4] >> ((2 * lane + i) & 31) & 1u) != 0;
       odd[i] = __ballot_sync(0xffffffffu, row || !(g[i] < __int_as_float(0x7f800000)) || !(fabsf(b[i]) <= FLT_MAX));
     }
-    // the first token from which nothing is finite any more
     const int first0 = odd[0] ? 2 * (__ffs(odd[0]) - 1) : kChunk, first1 = odd[1] ? 2 * (__ffs(odd[1]) - 1) + 1 : kChunk;
-    broken = min(first0, first1);
+    const int broken = min(first0, first1);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (2 * lane + i >= broken) a[i] = 0;                    // (so that nothing that is finite meets what is not)
@@ -373,7 +380,9 @@ struct Helpers {
       const int64_t other = __shfl_up_sync(0xffffffffu, sum, d);
       if (lane >= d) sum += other;
     }
-    all = __shfl_sync(0xffffffffu, sum, 31);
+    const int64_t all = __shfl_sync(0xffffffffu, sum, 31);
+    kept.broken = broken;
+    kept.all = all;
     auto fraction = [](int64_t x) { return (float)((uint32_t)(x >> 20) & 0xffffffu) * 5.9604644775390625e-8f; };
     auto power = [&](int64_t x) {
       return exp2f(fraction(x)) * __uint_as_float((uint32_t)(min(max((int)(x >> 44), -127), 127) + 127) << 23);
@@ -382,27 +391,34 @@ struct Helpers {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int at = 2 * lane + i;
-      const bool gone = at >= broken;
-      const float beta = gone ? 0.0f : b[i], from_start = power(G[i]), part = exp2f(fraction(G[i]));
-      const float k_row = s.k_row[at], q_row = s.q_row[at];
-      const bool bad_q = (s.bad_q[lane >> 4] >> (at & 31) & 1u) != 0;
+      const float beta = at >= broken ? 0.0f : b[i], k_row = s.k_row[at];
+      kept.from_start[i] = power(G[i]);
+      kept.part[i] = exp2f(fraction(G[i]));
       s.whole[at] = (int)(G[i] >> 44);
-      s.of_a[at] = beta * k_row * part;
-      s.of_p[at] = p.scale * q_row * part;
+      s.of_a[at] = beta * k_row * kept.part[i];
       s.of_column[at] = k_row * exp2f(-fraction(G[i]));
-      w.of_x[at] = beta * from_start * k_row;
+      w.of_x[at] = beta * kept.from_start[i] * k_row;
       w.of_v[at] = beta;
       w.to_end[at] = power(all - G[i]) * k_row;
-      w.of_q[at] = gone || bad_q ? kNaN : p.scale * from_start * q_row;
     }
     if (lane == 0) s.top_t = 0;
   }
-  // (behind the barrier that the others wait at: 64-bit powers take their time)
-  __device__ __forceinline__ void total(Weights& w, int broken, int64_t all, int tokens) const {
+  __device__ __forceinline__ void weights_of_q(Weights& w, const Sums& kept) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = 2 * lane + i;
+      const float q_row = s.q_row[at];
+      const bool bad_q = (s.bad_q[lane >> 4] >> (at & 31) & 1u) != 0;
+      s.of_p[at] = p.scale * q_row * kept.part[i];
+      w.of_q[at] = at >= kept.broken || bad_q ? __builtin_nanf("") : p.scale * kept.from_start[i] * q_row;
+    }
+  }
+  // (last of all: 64-bit powers take their time)
+  __device__ __forceinline__ void total(Weights& w, const Sums& kept, int tokens) const {
     if (lane == 0) {
-      const double exact = exp2((double)all * (1.0 / 17592186044416.0));
+      const double exact = exp2((double)kept.all * (1.0 / 17592186044416.0));
       const float rounded = (float)exact;
-      w.total = broken < tokens ? __builtin_nanf("") : rounded;
+      w.total = kept.broken < tokens ? __builtin_nanf("") : rounded;
       w.total_rest = (float)(exact - (double)rounded);
     }
   }
@@ -557,18 +573,29 @@ struct Helpers {
   }
 
   // 16 columns J of T below the diagonal block: T_iJ = -T_ii sum_k A_ik T_kJ, i downward; kept in s.A above the diagonal, transposed.  All are transposed, so
-  // that what one product gives is the next one's left operand.  By TF32 instructions, whose exponents need no scales: operands in two pieces,
-  // three products a term; of eight columns of the left operand the even ones are taken for the first four.  Then all of the columns, scaled, to `to`.
+  // that what one product gives is the next one's left operand, and each T_kJ meets all A_ik below it at once.  By TF32 instructions, whose exponents need no scales:
+  // operands in two pieces, three products a term; of eight columns of the left operand the even ones are taken for the first four.  Then all of the
+  // columns, scaled, to `to`.
   __device__ __forceinline__ void columns_of_t(int J, uint32_t to, Weights& w) const {
     const int mi = lane >> 3, r8 = lane & 7, g = lane >> 2, pair = (lane & 3) * 2;
-    // d += x times (block (i, k) of s.A) transposed
-    auto times = [&](float (&d)[2][4], float (&small)[2][4], const float (&x)[2][4], int i, int k) {
+    auto clear = [&](float (&x)[2][4]) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[n][e] = 0.0f;
+    };
+    auto in_pieces = [&](const float (&x)[2][4], uint32_t (&h)[2][4], uint32_t (&l)[2][4]) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split_tf32(x[n][e], h[n][(e & 1) * 2 + (e >> 1)], l[n][(e & 1) * 2 + (e >> 1)]);
+    };
+    // d, small += a times (block (i, k) of s.A) transposed
+    auto times = [&](float (&d)[2][4], float (&small)[2][4], const uint32_t (&ah)[2][4], const uint32_t (&al)[2][4], int i, int k) {
       const float* from = &s.A[i * 16 + g][k * 16 + pair];
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
-        uint32_t ah[4], al[4], bh[2][2], bl[2][2];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) split_tf32(x[ks][e], ah[(e & 1) * 2 + (e >> 1)], al[(e & 1) * 2 + (e >> 1)]);
+        uint32_t bh[2][2], bl[2][2];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           const float2 b = *reinterpret_cast<const float2*>(from + n * 8 * kAPitch + ks * 8);
@@ -576,65 +603,57 @@ struct Helpers {
           split_tf32(b.y, bh[n][1], bl[n][1]);
         }
 #pragma unroll
-        for (int n = 0; n < 2; ++n) mma_tf32(d[n], ah, bh[n][0], bh[n][1]);
+        for (int n = 0; n < 2; ++n) mma_tf32(d[n], ah[ks], bh[n][0], bh[n][1]);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) mma_tf32(small[n], al, bh[n][0], bh[n][1]);
+        for (int n = 0; n < 2; ++n) mma_tf32(small[n], al[ks], bh[n][0], bh[n][1]);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) mma_tf32(small[n], ah, bl[n][0], bl[n][1]);
+        for (int n = 0; n < 2; ++n) mma_tf32(small[n], ah[ks], bl[n][0], bl[n][1]);
       }
     };
-    // block (i, J), transposed: rows are columns of T
-    auto block = [&](int i, float (&x)[2][4]) {
-      const float* at = i == J ? &s.A[J * 16 + pair][J * 16 + g] : &s.A[J * 16 + g][i * 16 + pair];
-      const int along = i == J ? kAPitch : 1, across = i == J ? 1 : kAPitch;
+    float x[2][4], sums[3][2][4], smalls[3][2][4], top = 0.0f;
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = at[(n * 8 + (e & 1)) * along + (e >> 1) * 8 * across];
-    };
-    auto clear = [&](float (&x)[2][4]) {
+      for (int e = 0; e < 4; ++e) x[n][e] = s.A[J * 16 + n * 8 + pair + (e & 1)][J * 16 + g + 8 * (e >> 1)];
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+    for (int d = 0; d < 3; ++d) clear(sums[d]), clear(smalls[d]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = 0.0f;
-    };
-    float top = 0.0f;
-    auto raise = [&](const float (&x)[2][4]) {
+    for (int c = 0; c < 4; ++c) {                              // x: T_kJ, k = J + c
+      if (J + c > 3) break;
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[n][e]));
-    };
-    float x[2][4];
-    block(J, x);
-    raise(x);
-#pragma unroll 1
-    for (int i = J + 1; i < 4; ++i) {
-      float m[2][4], small[2][4];
-      clear(m);
-      clear(small);
-#pragma unroll 1
-      for (int k = J; k < i; ++k) {
-        block(k, x);
-        times(m, small, x, i, k);
+      if (c > 0) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            *reinterpret_cast<float2*>(&s.A[J * 16 + g + 8 * h][(J + c) * 16 + n * 8 + pair]) = make_float2(x[n][2 * h], x[n][2 * h + 1]);
       }
+      if (J + c == 3) break;
+      uint32_t hi[2][4], lo[2][4];
+      in_pieces(x, hi, lo);
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int d = c; d < 3; ++d) {                            // i = J + d + 1
+        if (J + d > 2) break;
+        times(sums[d], smalls[d], hi, lo, J + d + 1, J + c);
+      }
+      if (c < 3) {
+        float m[2][4], small[2][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) m[n][e] = -(m[n][e] + small[n][e]);
-      clear(x);
-      clear(small);
-      times(x, small, m, i, i);
-      __syncwarp();
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+          for (int e = 0; e < 4; ++e) m[n][e] = -(sums[c][n][e] + smalls[c][n][e]);
+        in_pieces(m, hi, lo);
+        clear(x);
+        clear(small);
+        times(x, small, hi, lo, J + c + 1, J + c + 1);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[n][e] += small[n][e];
-          s.A[J * 16 + g + 8 * (e >> 1)][i * 16 + n * 8 + pair + (e & 1)] = x[n][e];
-        }
-      raise(x);
-      __syncwarp();
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[n][e] += small[n][e];
+      }
     }
     const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
     if (lane == 0) atomicMax(&s.top_t, most);
@@ -643,53 +662,97 @@ struct Helpers {
     if (J == 0 && lane == 0) w.of_t = unscale_for(scale);
 #pragma unroll 1
     for (int i = J; i < 4; ++i) {
+      const float* at = i == J ? &s.A[J * 16 + pair][J * 16 + g] : &s.A[J * 16 + g][i * 16 + pair];
+      const int along = i == J ? kAPitch : 1, across = i == J ? 1 : kAPitch;
       uint32_t h[4], l[4];
-      block(i, x);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) split(x[u >> 1][2 * (u & 1)] * scale, x[u >> 1][2 * (u & 1) + 1] * scale, h[u], l[u]);
-      const uint32_t at = to + unit_at<kChunk>(i * 16 + (mi >> 1) * 8 + r8, 2 * J + (mi & 1));
-      stmatrix_trans(at, h);
-      stmatrix_trans(at + L::kSquare, l);
+      for (int u = 0; u < 4; ++u) {
+        const float* from = at + (u >> 1) * 8 * along + (u & 1) * 8 * across;
+        split(from[0] * scale, from[along] * scale, h[u], l[u]);
+      }
+      const uint32_t there = to + unit_at<kChunk>(i * 16 + (mi >> 1) * 8 + r8, 2 * J + (mi & 1));
+      stmatrix_trans(there, h);
+      stmatrix_trans(there + L::kSquare, l);
     }
   }
   static __device__ __forceinline__ void sync_four() { asm volatile("bar.sync 15, 128;" ::: "memory"); }
 
-  // Chunk of rows first up to first + 64 (or end), which were fetched, into `stage`; the next one is fetched.  Of eight warps four have k, A and
-  // T, the others q, the weights and P; of four all have both, one after the other.
+  static __device__ __forceinline__ void sync_q() { asm volatile("bar.sync 14, 128;" ::: "memory"); }
+
+  // The first chunk's rows on their way (of eight warps the latter four fetch).
+  __device__ __forceinline__ void begin(int first, int end) {
+    if (warp == kWeigher) fetch_gates(first, end);
+    if (H == 4 || warp >= 4) fetch_rows(first, end);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    sync();
+  }
+  // Chunk of rows first up to first + 64 (or end), which were fetched, into `stage`; the next one's are fetched.  Of eight warps four have A and T, whose
+  // way through a chunk is the longest, the others q, the weights and P; k's rows are everybody's.  Of four warps all have both, one after the other.
   __device__ __forceinline__ void prepare(int first, int end, uint32_t stage) {
     Weights& w = *reinterpret_cast<Weights*>(generic + stage + L::kWeightsAt);
     const int64_t at = (int64_t)(head / p.share) * p.dk;
-    const uint32_t kt = smem + stage;
-    const int from = H == 8 ? warp >> 2 : 0, to = H == 8 ? from + 1 : 2;       // 0: k, 1: q
-    if (kStaged) asm volatile("cp.async.wait_all;" ::: "memory");
-#pragma unroll 1
-    for (int q = from; q < to; ++q)
-      rows(static_cast<const T*>(q ? p.q : p.k) + at, q ? p.q_stride : p.k_stride, first, end, L::kRawAt + q * L::kRows, kt + q * L::kQAt,
-           q ? s.q_row : s.k_row, q ? s.bad_q : s.bad_k);
-    sync();
-    int broken = 0;
-    int64_t all = 0;
-    if (warp == kWeigher) weights(w, broken, all);
-#pragma unroll 1
-    for (int q = from; q < to; ++q) {
-      const int m = H == 4 && q ? 3 - warp : warp & 3;
-      Square acc;
-      square(kt + q * L::kQAt, kt, m, acc);
-      if (q == from) sync();
-      weigh(m, acc, q ? s.of_p : s.of_a, q);
-      if (q) {
-        store_p(m, acc, generic + stage + L::kPAt, w.of_p);
-      } else {
+    const uint32_t kt = smem + stage, qt = kt + L::kQAt;
+    const T* k = static_cast<const T*>(p.k) + at;
+    const T* q = static_cast<const T*>(p.q) + at;
+    const int tokens = min(end - first, kChunk), m = warp & 3;
+    Square acc;
+    Sums kept;
+    if constexpr (H == 8) {
+      rows<4>(t, k, p.k_stride, first, end, L::kRawAt, kt, s.k_row, s.bad_k);
+      sync();
+      if (warp < 4) {
+        square(kt, kt, m, acc);
+        sync();                                                // (k's weights)
+        weigh(m, acc, s.of_a, 0);
         store_a(m, acc);
         invert_block(m);
+        sync_four();
+        columns_of_t(m, kt + L::kTAt, w);
+      } else {
+        if (warp == kWeigher) {
+          weights_of_k(w, kept);
+          fetch_gates(first + kChunk, end);
+        }
+        asm volatile("bar.arrive 1, %0;" ::"n"(kThreads) : "memory");
+        rows<2>(t - 128, q, p.q_stride, first, end, L::kRawAt + L::kRows, qt, s.q_row, s.bad_q);
+        sync_q();
+        fetch_rows(first + kChunk, end);
+        if (warp == kWeigher) weights_of_q(w, kept);
+        square(qt, kt, m, acc);
+        sync_q();                                              // (q's weights)
+        weigh(m, acc, s.of_p, 1);
+        store_p(m, acc, generic + stage + L::kPAt, w.of_p);
+        if (warp == kWeigher) total(w, kept, tokens);
+        asm volatile("cp.async.wait_all;" ::: "memory");       // (the others find the rows behind the chunk's barrier)
       }
-    }
-    fetch(first + kChunk, end);
-    if (H == 4 || warp < 4) {
+    } else {
+      rows<2>(t, k, p.k_stride, first, end, L::kRawAt, kt, s.k_row, s.bad_k);
+      rows<2>(t, q, p.q_stride, first, end, L::kRawAt + L::kRows, qt, s.q_row, s.bad_q);
+      sync();
+      fetch_rows(first + kChunk, end);
+      if (warp == kWeigher) {
+        weights_of_k(w, kept);
+        weights_of_q(w, kept);
+        fetch_gates(first + kChunk, end);
+      }
+#pragma unroll 1
+      for (int which = 0; which < 2; ++which) {
+        const int mm = which ? 3 - m : m;
+        square(which ? qt : kt, kt, mm, acc);
+        if (!which) sync();
+        weigh(mm, acc, which ? s.of_p : s.of_a, which);
+        if (which) {
+          store_p(mm, acc, generic + stage + L::kPAt, w.of_p);
+        } else {
+          store_a(mm, acc);
+          invert_block(mm);
+        }
+      }
       sync_four();
-      columns_of_t(warp, kt + L::kTAt, w);
+      columns_of_t(m, kt + L::kTAt, w);
+      if (warp == kWeigher) total(w, kept, tokens);
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
-    if (warp == kWeigher) total(w, broken, all, min(end - first, kChunk));
   }
 };
 
@@ -817,65 +880,70 @@ struct Columns {
   template <typename V>
   __device__ __forceinline__ V& lane_pair(int which) const { return reinterpret_cast<V*>(generic + at0 + L::kPairsAt + which * 256)[lane]; }
 
-  __device__ __forceinline__ void multiply_q(uint32_t qt, int ks, const uint32_t (&hi)[4], const uint32_t (&lo)[4], float (&O)[8][4]) const {
+  // O += S q of 32 tokens (half), one step of dk
+  __device__ __forceinline__ void multiply_q(uint32_t qt, int half, int ks, const uint32_t (&hi)[4], const uint32_t (&lo)[4], float (&O)[4][4]) const {
 #pragma unroll
-    for (int np = 0; np < 4; ++np) {
-      const uint32_t at = qt + unit_at<DK>(np * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1));
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t at = qt + unit_at<DK>((2 * half + i) * 16 + (mi >> 1) * 8 + r8, 2 * ks + (mi & 1));
       uint32_t a[4];
       ldmatrix(at, a);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (kFull) mma(O[2 * np + h], lo, a[2 * h], a[2 * h + 1]);
-        mma(O[2 * np + h], hi, a[2 * h], a[2 * h + 1]);
+        if (kFull) mma(O[2 * i + h], lo, a[2 * h], a[2 * h + 1]);
+        mma(O[2 * i + h], hi, a[2 * h], a[2 * h + 1]);
       }
       if (kFull) {
         ldmatrix(at + L::kRows, a);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) mma(O[2 * np + h], hi, a[2 * h], a[2 * h + 1]);
+        for (int h = 0; h < 2; ++h) mma(O[2 * i + h], hi, a[2 * h], a[2 * h + 1]);
       }
     }
   }
 
-  // o = q S, which O holds, and P U, whose operand u(kk, hi, lo) gives
+  // o of 32 tokens (half): q S, which O holds, and P U, whose operand u(kk, hi, lo) gives.  16 bits: to shared memory.
   template <typename Operand>
-  __device__ __forceinline__ void finish_o(uint32_t pt, const Weights& w, float (&O)[8][4], const float (&per_s)[2], const float (&per_o)[2],
-                                           const Operand& u, bool odd, const int (&from)[2], uint32_t out_at, int first, int end) const {
-    float I[8][4];
+  __device__ __forceinline__ void finish_o(uint32_t pt, const Weights& w, int half, const float (&O)[4][4], const float (&per_s)[2],
+                                           const float (&per_o)[2], const Operand& u, bool odd, const int (&from)[2], uint32_t out_at, int first,
+                                           int end) const {
+    float I[4][4];
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
+    for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) I[n][e] = 0.0f;
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
+      if (kk > 2 * half + 1) break;
       uint32_t hi[4], lo[4];
       u(kk, hi, lo);
 #pragma unroll
-      for (int np = kk; np < 4; ++np) {
-        const uint32_t at = pt + unit_at<kChunk>(np * 16 + (mi >> 1) * 8 + r8, 2 * kk + (mi & 1));
+      for (int i = 0; i < 2; ++i) {
+        if (kk > 2 * half + i) continue;
+        const uint32_t at = pt + unit_at<kChunk>((2 * half + i) * 16 + (mi >> 1) * 8 + r8, 2 * kk + (mi & 1));
         uint32_t b[4];
         ldmatrix(at, b);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          if (kFull) mma(I[2 * np + h], lo, b[2 * h], b[2 * h + 1]);
-          mma(I[2 * np + h], hi, b[2 * h], b[2 * h + 1]);
+          if (kFull) mma(I[2 * i + h], lo, b[2 * h], b[2 * h + 1]);
+          mma(I[2 * i + h], hi, b[2 * h], b[2 * h + 1]);
         }
         if (kFull) {
           ldmatrix(at + L::kSquare, b);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) mma(I[2 * np + h], hi, b[2 * h], b[2 * h + 1]);
+          for (int h = 0; h < 2; ++h) mma(I[2 * i + h], hi, b[2 * h], b[2 * h + 1]);
         }
       }
     }
 #pragma unroll
-    for (int np = 0; np < 4; ++np) {
+    for (int i = 0; i < 2; ++i) {
       uint32_t out[4];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int n = 2 * np + h, t = n * 8 + pair;
+        const int t = (4 * half + 2 * i + h) * 8 + pair;
         const float2 fq = *reinterpret_cast<const float2*>(&w.of_q[t]), fp = *reinterpret_cast<const float2*>(&w.of_p[t]);
         float y[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = fmaf((e & 1 ? fq.y : fq.x) * per_s[e >> 1], O[n][e], (e & 1 ? fp.y : fp.x) * per_o[e >> 1] * I[n][e]);
+        for (int e = 0; e < 4; ++e)
+          y[e] = fmaf((e & 1 ? fq.y : fq.x) * per_s[e >> 1], O[2 * i + h][e], (e & 1 ? fp.y : fp.x) * per_o[e >> 1] * I[2 * i + h][e]);
         if (odd) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -889,16 +957,19 @@ struct Columns {
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+          for (int j = 0; j < 2; ++j) {
             Vec<T, 2> two;
-            two.v[0] = from_float<T>(y[2 * i]);
-            two.v[1] = from_float<T>(y[2 * i + 1]);
-            out[2 * h + i] = *reinterpret_cast<const uint32_t*>(&two);
+            two.v[0] = from_float<T>(y[2 * j]);
+            two.v[1] = from_float<T>(y[2 * j + 1]);
+            out[2 * h + j] = *reinterpret_cast<const uint32_t*>(&two);
           }
         }
       }
-      if constexpr (!kFull) stmatrix_trans(smem + out_at + v_unit(np * 16 + (mi >> 1) * 8 + r8, mi & 1), out);
+      if constexpr (!kFull) stmatrix_trans(smem + out_at + v_unit((2 * half + i) * 16 + (mi >> 1) * 8 + r8, mi & 1), out);
     }
+  }
+  // (16 bits) o of the chunk from shared memory to where it belongs
+  __device__ __forceinline__ void store_o(uint32_t out_at, int first, int end) const {
     if constexpr (!kFull) {
       __syncwarp();
       T* o = static_cast<T*>(p.o) + (int64_t)head * p.dv + col0;
@@ -926,21 +997,22 @@ struct Columns {
   __device__ __forceinline__ void chunk_o(int c, int first, int end) const {
     const uint32_t stage = (c & 1) * L::kStage;
     const Weights& w = *reinterpret_cast<const Weights*>(generic + stage + L::kWeightsAt);
-    float O[8][4];
+    float O[2][4][4];
 #pragma unroll
     for (int n = 0; n < 8; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) O[n][e] = 0.0f;
+      for (int e = 0; e < 4; ++e) O[n >> 2][n & 3][e] = 0.0f;
     auto handed = [&](uint32_t at, int i, uint32_t (&hi)[4]) {
       const uint4 x = reinterpret_cast<const uint4*>(generic + at0 + at)[i * 32 + lane];
       hi[0] = x.x, hi[1] = x.y, hi[2] = x.z, hi[3] = x.w;
     };
     await(0);
-#pragma unroll
+#pragma unroll 2
     for (int ks = 0; ks < DK / 16; ++ks) {
       uint32_t hi[4];
       handed(L::kSAt, ks, hi);
-      multiply_q(smem + stage + L::kQAt, ks, hi, hi, O);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) multiply_q(smem + stage + L::kQAt, half, ks, hi, hi, O[half]);
     }
     await(1);
     const float2 ps = lane_pair<float2>(0), po = lane_pair<float2>(1);
@@ -948,8 +1020,11 @@ struct Columns {
     const float per_s[2] = {ps.x, ps.y}, per_o[2] = {po.x, po.y};
     const int from[2] = {f.x, f.y};
     const bool odd = __any_sync(0xffffffffu, min(f.x, f.y) < kChunk);
-    finish_o(smem + stage + L::kPAt, w, O, per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { handed(L::kUAt, kk, hi); }, odd, from,
-             at0 + L::kOAt, first, end);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+      finish_o(smem + stage + L::kPAt, w, half, O[half], per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { handed(L::kUAt, kk, hi); },
+               odd, from, at0 + L::kOAt, first, end);
+    store_o(at0 + L::kOAt, first, end);
   }
 
   // S of chunk c, and its o too where no other warp makes it.
@@ -968,25 +1043,22 @@ struct Columns {
         }
     }
 
-    // k S (and q S)
-    float X[8][4], O[SPLIT ? 1 : 8][4], top[2], scale[2], per_s[2];
+    // k S
+    float X[8][4], top[2], scale[2], scale_s[2], per_s[2];
 #pragma unroll
     for (int n = 0; n < 8; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        X[n][e] = 0.0f;
-        if constexpr (!SPLIT) O[n][e] = 0.0f;
-      }
+      for (int e = 0; e < 4; ++e) X[n][e] = 0.0f;
     largest(S, top);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      scale[h] = scale_for(top[h]);
-      per_s[h] = unscale_for(scale[h]);
+      scale_s[h] = scale_for(top[h]);
+      per_s[h] = unscale_for(scale_s[h]);
     }
 #pragma unroll
     for (int ks = 0; ks < DK / 16; ++ks) {
       uint32_t hi[4], lo[4];
-      operand(S, ks, scale, hi, lo);
+      operand(S, ks, scale_s, hi, lo);
       if constexpr (SPLIT) ptx::st_shared16(smem + at0 + L::kSAt + (ks * 32 + lane) * 16, hi[0], hi[1], hi[2], hi[3]);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {                   // (four accumulators, so that a product does not wait for the one before)
@@ -1004,7 +1076,6 @@ struct Columns {
           for (int n = 0; n < 4; ++n) mma(X[4 * half + n], hi, b[n >> 1][2 * (n & 1)], b[n >> 1][2 * (n & 1) + 1]);
         }
       }
-      if constexpr (!SPLIT) multiply_q(qt, ks, hi, lo, O);
     }
     if constexpr (SPLIT) {
       lane_pair<float2>(0) = make_float2(per_s[0], per_s[1]);
@@ -1111,8 +1182,24 @@ struct Columns {
         lane_pair<int2>(2) = make_int2(from[0], from[1]);
         announce(1);
       } else {
-        finish_o(kt + L::kPAt, w, O, per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { operand(U, kk, scale, hi, lo); }, odd, from,
-                 at0 + (c & 1) * L::kV, first, end);
+        // (S is taken apart again, 32 tokens at a time: with q S made beside k S there are not the registers)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float O[4][4];
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[n][e] = 0.0f;
+#pragma unroll
+          for (int ks = 0; ks < DK / 16; ++ks) {
+            uint32_t hi[4], lo[4];
+            operand(S, ks, scale_s, hi, lo);
+            multiply_q(qt, half, ks, hi, lo, O);
+          }
+          finish_o(kt + L::kPAt, w, half, O, per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { operand(U, kk, scale, hi, lo); }, odd,
+                   from, at0 + (c & 1) * L::kV, first, end);
+        }
+        store_o(at0 + (c & 1) * L::kV, first, end);
       }
     }
 
@@ -1208,7 +1295,7 @@ __global__ void __launch_bounds__(F::kThreads, 1) delta_chunks_kernel(const Chun
     if constexpr (F::kChain > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kHelp));
     const int t = (int)threadIdx.x - F::kWarps * 32;
     Helpers<T, DK, F::H> helpers(p, smem, dynamic_smem, head, t);
-    helpers.fetch(rows.begin, rows.end);
+    helpers.begin(rows.begin, rows.end);
     for (int c = 0; c < chunks; ++c) {
       helpers.prepare(rows.begin + c * kChunk, rows.end, (c & 1) * L::kStage);
       __syncthreads();
@@ -1272,8 +1359,8 @@ template <typename T, int DK>
 cudaError_t launch_width(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
   const int64_t columns = (int64_t)sequences * p.heads * ((p.dv + 15) / 16);
   if constexpr (sizeof(T) == 2) {
-    if (p.dv > 64 && columns >= 148 * 8) return launch<T, DK, Shape<8, false, 4, 208, 0, 88>>(p, sequences, stream);
-    if (p.dv > 32 && columns >= 148 * 4) return launch<T, DK, Shape<4, true, 8, 224, 112, 88>>(p, sequences, stream);
+    if (p.dv > 64 && columns >= 148 * 8) return launch<T, DK, Shape<8, false, 8, 168, 0, 88>>(p, sequences, stream);
+    if (p.dv > 32 && columns >= 148 * 4) return launch<T, DK, Shape<4, true, 8, 208, 104, 96>>(p, sequences, stream);
     return launch<T, DK, Shape<2, true, 8, 208, 0, 144>>(p, sequences, stream);
   } else {
     if (p.dv > 32 && columns >= 148 * 4) return launch<T, DK, Shape<4, false, 4, 0, 0, 0>>(p, sequences, stream);
