@@ -73,6 +73,8 @@ struct Scratch {
   float of_a[kChunk], of_p[kChunk], of_column[kChunk];
   uint32_t bad_k[kChunk / 32], bad_q[kChunk / 32];             // rows that are not finite
   uint32_t top_t;                        // T's largest element
+  int broken;                            // the first token from which nothing is finite any more
+  int64_t all;                           // G_n
 };
 
 template <typename T, int DK>
@@ -106,6 +108,12 @@ __device__ __forceinline__ float scale_for(float top) {
 }
 __device__ __forceinline__ float unscale_for(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }
 
+// 2^x of x in -1..1.
+__device__ __forceinline__ float exp2_fraction(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 __device__ __forceinline__ uint32_t pack_half(float a, float b) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
@@ -241,11 +249,10 @@ struct Helpers {
 
   // Rows of q or k of a chunk to shared memory, in pieces, scaled where they are not fp16 already.  Leaves what a row is multiplied by (the
   // norm's and the scale's reciprocals) and says which rows are not finite (they come out as 0).
-  // SHARE threads of u = 0, 1, .. have a row.
-  template <int SHARE>
-  __device__ __forceinline__ void rows(int u, const T* from, int64_t stride, int first, int end, uint32_t raw, uint32_t to, float* factor, uint32_t* bad) const {
-    constexpr int kShare = SHARE, kUnits = DK / 8 / SHARE;     // 16-byte units (of 16-bit elements) of a thread: every SHARE-th one
-    const int r = u / kShare, part = u % kShare;
+  // Four threads of four warps have a row: rows base up to base + 31.
+  __device__ __forceinline__ void rows(int base, const T* from, int64_t stride, int first, int end, uint32_t raw, uint32_t to, float* factor, uint32_t* bad) const {
+    constexpr int kShare = 4, kUnits = DK / 8 / kShare;        // 16-byte units (of 16-bit elements) of a thread: every fourth one
+    const int u = t & 127, r = base + u / kShare, part = u % kShare;
     const bool there = first + r < end;
     const T* row = from + (there ? (int64_t)(first + r) * stride : 0);
     float top = 0.0f, squares[2] = {0.0f, 0.0f}, scale = 1.0f;
@@ -263,28 +270,32 @@ struct Helpers {
           ptx::st_shared16(to + unit_at<DK>(r, i * kShare + part), w[0], w[1], w[2], w[3]);
         }
       }
+      uint4 x[kUnits];
       uint32_t most = 0;
-#pragma unroll 2
-      for (int i = 0; i < kUnits; ++i) {
-        const uint4 x = *reinterpret_cast<const uint4*>(generic + raw + unit_at<DK>(r, i * kShare + part));
 #pragma unroll
-        for (uint32_t w : {x.x, x.y, x.z, x.w}) {
-          most = Half<T>::largest(most, w);
+      for (int i = 0; i < kUnits; ++i) x[i] = *reinterpret_cast<const uint4*>(generic + raw + unit_at<DK>(r, i * kShare + part));
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+        for (uint32_t w : {x[i].x, x[i].y, x[i].z, x[i].w}) {
+          if (!Half<T>::kExact) most = Half<T>::largest(most, w);
           const float2 f = Half<T>::unpack(w);
           squares[0] = fmaf(f.x, f.x, squares[0]);
           squares[1] = fmaf(f.y, f.y, squares[1]);
         }
+      if (Half<T>::kExact) {
+        top = squares[0] + squares[1];                         // (of fp16 it is finite where the elements are)
+      } else {
+        const float2 f = Half<T>::unpack(most);
+        top = max_nan(f.x, f.y);
       }
-      const float2 f = Half<T>::unpack(most);
-      top = max_nan(f.x, f.y);
 #pragma unroll
       for (int d = 1; d < kShare; d *= 2) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
       const bool odd = !(top <= FLT_MAX);
       if (!Half<T>::kExact) scale = scale_for(top);
-#pragma unroll 2
+#pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const uint4 x = *reinterpret_cast<const uint4*>(generic + raw + unit_at<DK>(r, i * kShare + part));
-        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           if (!Half<T>::kExact) {
@@ -337,7 +348,7 @@ struct Helpers {
 #pragma unroll
     for (int d = 1; d < kShare; d *= 2) squares[0] += __shfl_xor_sync(0xffffffffu, squares[0], d);
     const bool odd = !(top <= FLT_MAX);
-    const uint32_t odd_rows = __ballot_sync(0xffffffffu, odd); // (SHARE bits a row)
+    const uint32_t odd_rows = __ballot_sync(0xffffffffu, odd); // (four bits a row)
     if (part == 0) factor[r] = odd ? 0.0f : (p.normalize ? rsqrtf(squares[0] + kNormalizeEps) : 1.0f) * unscale_for(scale);
     if (lane == 0) {
       uint32_t bits = 0;
@@ -345,15 +356,13 @@ struct Helpers {
 #pragma unroll 1
         for (int i = 0; i < 32 / kShare; ++i) bits |= (odd_rows >> (kShare * i) & 1u) << i;
       }
-      if constexpr (kShare == 2) reinterpret_cast<uint16_t*>(bad)[u >> 5] = (uint16_t)bits;
-      else reinterpret_cast<uint8_t*>(bad)[u >> 5] = (uint8_t)bits;
+      reinterpret_cast<uint8_t*>(bad)[(base + u / kShare) >> 3] = (uint8_t)bits;
     }
   }
 
   // What the weigher keeps of its tokens, 2l and 2l+1, from k's weights to q's.
   struct Sums {
     int broken;                          // the first token from which nothing is finite any more
-    int64_t all;                         // G_n
     float from_start[2], part[2];        // exp(G_i), and its part of a power of two
   };
   // One warp: lane l has tokens 2l and 2l+1.  Sums of log_decay are of whole numbers of 2^-44 powers of two: exact.
@@ -382,26 +391,27 @@ struct Helpers {
     }
     const int64_t all = __shfl_sync(0xffffffffu, sum, 31);
     kept.broken = broken;
-    kept.all = all;
     auto fraction = [](int64_t x) { return (float)((uint32_t)(x >> 20) & 0xffffffu) * 5.9604644775390625e-8f; };
-    auto power = [&](int64_t x) {
-      return exp2f(fraction(x)) * __uint_as_float((uint32_t)(min(max((int)(x >> 44), -127), 127) + 127) << 23);
-    };
+    auto power = [&](int64_t x) { return exp2_fraction(fraction(x)) * power_of_two((int)(x >> 44)); };
     const int64_t G[2] = {sum - a[1], sum};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int at = 2 * lane + i;
       const float beta = at >= broken ? 0.0f : b[i], k_row = s.k_row[at];
-      kept.from_start[i] = power(G[i]);
-      kept.part[i] = exp2f(fraction(G[i]));
+      kept.part[i] = exp2_fraction(fraction(G[i]));
+      kept.from_start[i] = kept.part[i] * power_of_two((int)(G[i] >> 44));
       s.whole[at] = (int)(G[i] >> 44);
       s.of_a[at] = beta * k_row * kept.part[i];
-      s.of_column[at] = k_row * exp2f(-fraction(G[i]));
+      s.of_column[at] = k_row * exp2_fraction(-fraction(G[i]));
       w.of_x[at] = beta * kept.from_start[i] * k_row;
       w.of_v[at] = beta;
       w.to_end[at] = power(all - G[i]) * k_row;
     }
-    if (lane == 0) s.top_t = 0;
+    if (lane == 0) {
+      s.top_t = 0;
+      s.broken = broken;
+      s.all = all;
+    }
   }
   __device__ __forceinline__ void weights_of_q(Weights& w, const Sums& kept) const {
 #pragma unroll
@@ -413,12 +423,12 @@ struct Helpers {
       w.of_q[at] = at >= kept.broken || bad_q ? __builtin_nanf("") : p.scale * kept.from_start[i] * q_row;
     }
   }
-  // (last of all: 64-bit powers take their time)
-  __device__ __forceinline__ void total(Weights& w, const Sums& kept, int tokens) const {
+  // (by a warp that has little else to do: 64-bit powers take their time)
+  __device__ __forceinline__ void total(Weights& w, int tokens) const {
     if (lane == 0) {
-      const double exact = exp2((double)kept.all * (1.0 / 17592186044416.0));
+      const double exact = exp2((double)s.all * (1.0 / 17592186044416.0));
       const float rounded = (float)exact;
-      w.total = kept.broken < tokens ? __builtin_nanf("") : rounded;
+      w.total = s.broken < tokens ? __builtin_nanf("") : rounded;
       w.total_rest = (float)(exact - (double)rounded);
     }
   }
@@ -439,21 +449,24 @@ struct Helpers {
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc.diagonal[n][i] = 0.0f;
-    const int a_row = m * 16 + (mi & 1) * 8 + r8, b_row = (mi >> 1) * 8 + r8;
-#pragma unroll 1
+    const uint32_t a_at = rows_at + (m * 16 + (mi & 1) * 8 + r8) * DK * 2, b_at = kt + ((mi >> 1) * 8 + r8) * DK * 2, d_at = b_at + m * 16 * DK * 2;
+#pragma unroll 2
     for (int ks = 0; ks < DK / 16; ++ks) {
+      const uint32_t ua = (2 * ks + (mi >> 1)) ^ r8, ub = (2 * ks + (mi & 1)) ^ r8;            // (as unit_at)
       uint32_t a[L::kPieces][4], b[4][L::kPieces][4];
 #pragma unroll
-      for (int i = 0; i < L::kPieces; ++i) ldmatrix(rows_at + i * L::kRows + unit_at<DK>(a_row, 2 * ks + (mi >> 1)), a[i]);
+      for (int i = 0; i < L::kPieces; ++i) {
+        ldmatrix(a_at + ua * 16 + i * L::kRows, a[i]);
+        ldmatrix(d_at + ub * 16 + i * L::kRows, b[3][i]);
+      }
 #pragma unroll
-      for (int np = 0; np < 4; ++np)
-        if (np < m || np == 3) {                               // (the last one: the diagonal's)
+      for (int np = 0; np < 3; ++np)
+        if (np < m) {
 #pragma unroll
-          for (int i = 0; i < L::kPieces; ++i)
-            ldmatrix(kt + i * L::kRows + unit_at<DK>((np == 3 ? m : np) * 16 + b_row, 2 * ks + (mi & 1)), b[np][i]);
+          for (int i = 0; i < L::kPieces; ++i) ldmatrix(b_at + ub * 16 + np * 16 * DK * 2 + i * L::kRows, b[np][i]);
         }
 #pragma unroll
-      for (int np = 0; np < 4; ++np)
+      for (int np = 3; np >= 0; --np)                          // (the last one: the diagonal's)
         if (np < m || np == 3) {
 #pragma unroll
           for (int u = L::kPieces == 2 ? 0 : 2; u < 3; ++u)    // (the small products first)
@@ -573,87 +586,77 @@ struct Helpers {
   }
 
   // 16 columns J of T below the diagonal block: T_iJ = -T_ii sum_k A_ik T_kJ, i downward; kept in s.A above the diagonal, transposed.  All are transposed, so
-  // that what one product gives is the next one's left operand, and each T_kJ meets all A_ik below it at once.  By TF32 instructions, whose exponents need no scales:
-  // operands in two pieces, three products a term; of eight columns of the left operand the even ones are taken for the first four.  Then all of the
-  // columns, scaled, to `to`.
+  // that what one product gives is the next one's left operand.  By TF32 instructions, whose exponents need no scales: operands in two pieces,
+  // three products a term; of eight columns of the left operand the even ones are taken for the first four.  Then all of the columns, scaled, to `to`.
   __device__ __forceinline__ void columns_of_t(int J, uint32_t to, Weights& w) const {
     const int mi = lane >> 3, r8 = lane & 7, g = lane >> 2, pair = (lane & 3) * 2;
-    auto clear = [&](float (&x)[2][4]) {
+    float x[2][4], top = 0.0f;
+    // block (i, J), transposed: rows are columns of T
+    auto block = [&](int i) {
+      const float* at = i == J ? &s.A[J * 16 + pair][J * 16 + g] : &s.A[J * 16 + g][i * 16 + pair];
+      const int along = i == J ? kAPitch : 1, across = i == J ? 1 : kAPitch;
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = 0.0f;
+        for (int e = 0; e < 4; ++e) x[n][e] = at[(n * 8 + (e & 1)) * along + (e >> 1) * 8 * across];
     };
-    auto in_pieces = [&](const float (&x)[2][4], uint32_t (&h)[2][4], uint32_t (&l)[2][4]) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) split_tf32(x[n][e], h[n][(e & 1) * 2 + (e >> 1)], l[n][(e & 1) * 2 + (e >> 1)]);
-    };
-    // d, small += a times (block (i, k) of s.A) transposed
-    auto times = [&](float (&d)[2][4], float (&small)[2][4], const uint32_t (&ah)[2][4], const uint32_t (&al)[2][4], int i, int k) {
-      const float* from = &s.A[i * 16 + g][k * 16 + pair];
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        uint32_t bh[2][2], bl[2][2];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const float2 b = *reinterpret_cast<const float2*>(from + n * 8 * kAPitch + ks * 8);
-          split_tf32(b.x, bh[n][0], bl[n][0]);
-          split_tf32(b.y, bh[n][1], bl[n][1]);
-        }
-#pragma unroll
-        for (int n = 0; n < 2; ++n) mma_tf32(d[n], ah[ks], bh[n][0], bh[n][1]);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) mma_tf32(small[n], al[ks], bh[n][0], bh[n][1]);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) mma_tf32(small[n], ah[ks], bl[n][0], bl[n][1]);
-      }
-    };
-    float x[2][4], sums[3][2][4], smalls[3][2][4], top = 0.0f;
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[n][e] = s.A[J * 16 + n * 8 + pair + (e & 1)][J * 16 + g + 8 * (e >> 1)];
-#pragma unroll
-    for (int d = 0; d < 3; ++d) clear(sums[d]), clear(smalls[d]);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {                              // x: T_kJ, k = J + c
-      if (J + c > 3) break;
+    auto raise = [&]() {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[n][e]));
-      if (c > 0) {
+    };
+    block(J);
+    raise();
+#pragma unroll 1
+    for (int i = J + 1; i < 4; ++i) {
+      float d[2][4], small[2][2][4];
+#pragma unroll 1
+      for (int k = J; k <= i; ++k) {                           // (the last step: T_ii times the sum of the others)
+        if (k < i) {
+          block(k);
+        } else {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+          for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            *reinterpret_cast<float2*>(&s.A[J * 16 + g + 8 * h][(J + c) * 16 + n * 8 + pair]) = make_float2(x[n][2 * h], x[n][2 * h + 1]);
+            for (int e = 0; e < 4; ++e) x[n][e] = -(d[n][e] + (small[0][n][e] + small[1][n][e]));
+        }
+        if (k == J || k == i) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[n][e] = small[0][n][e] = small[1][n][e] = 0.0f;
+        }
+        const float* from = &s.A[i * 16 + g][k * 16 + pair];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          uint32_t ah[4], al[4], bh[2][2], bl[2][2];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) split_tf32(x[ks][e], ah[(e & 1) * 2 + (e >> 1)], al[(e & 1) * 2 + (e >> 1)]);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const float2 b = *reinterpret_cast<const float2*>(from + n * 8 * kAPitch + ks * 8);
+            split_tf32(b.x, bh[n][0], bl[n][0]);
+            split_tf32(b.y, bh[n][1], bl[n][1]);
+          }
+#pragma unroll
+          for (int n = 0; n < 2; ++n) mma_tf32(d[n], ah, bh[n][0], bh[n][1]);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) mma_tf32(small[0][n], al, bh[n][0], bh[n][1]);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) mma_tf32(small[1][n], ah, bl[n][0], bl[n][1]);
+        }
       }
-      if (J + c == 3) break;
-      uint32_t hi[2][4], lo[2][4];
-      in_pieces(x, hi, lo);
+      __syncwarp();
 #pragma unroll
-      for (int d = c; d < 3; ++d) {                            // i = J + d + 1
-        if (J + d > 2) break;
-        times(sums[d], smalls[d], hi, lo, J + d + 1, J + c);
-      }
-      if (c < 3) {
-        float m[2][4], small[2][4];
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) m[n][e] = -(sums[c][n][e] + smalls[c][n][e]);
-        in_pieces(m, hi, lo);
-        clear(x);
-        clear(small);
-        times(x, small, hi, lo, J + c + 1, J + c + 1);
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[n][e] += small[n][e];
-      }
+        for (int e = 0; e < 4; ++e) {
+          x[n][e] = d[n][e] + (small[0][n][e] + small[1][n][e]);
+          s.A[J * 16 + g + 8 * (e >> 1)][i * 16 + n * 8 + pair + (e & 1)] = x[n][e];
+        }
+      raise();
+      __syncwarp();
     }
     const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
     if (lane == 0) atomicMax(&s.top_t, most);
@@ -662,17 +665,13 @@ struct Helpers {
     if (J == 0 && lane == 0) w.of_t = unscale_for(scale);
 #pragma unroll 1
     for (int i = J; i < 4; ++i) {
-      const float* at = i == J ? &s.A[J * 16 + pair][J * 16 + g] : &s.A[J * 16 + g][i * 16 + pair];
-      const int along = i == J ? kAPitch : 1, across = i == J ? 1 : kAPitch;
       uint32_t h[4], l[4];
+      block(i);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float* from = at + (u >> 1) * 8 * along + (u & 1) * 8 * across;
-        split(from[0] * scale, from[along] * scale, h[u], l[u]);
-      }
-      const uint32_t there = to + unit_at<kChunk>(i * 16 + (mi >> 1) * 8 + r8, 2 * J + (mi & 1));
-      stmatrix_trans(there, h);
-      stmatrix_trans(there + L::kSquare, l);
+      for (int u = 0; u < 4; ++u) split(x[u >> 1][2 * (u & 1)] * scale, x[u >> 1][2 * (u & 1) + 1] * scale, h[u], l[u]);
+      const uint32_t at = to + unit_at<kChunk>(i * 16 + (mi >> 1) * 8 + r8, 2 * J + (mi & 1));
+      stmatrix_trans(at, h);
+      stmatrix_trans(at + L::kSquare, l);
     }
   }
   static __device__ __forceinline__ void sync_four() { asm volatile("bar.sync 15, 128;" ::: "memory"); }
@@ -694,65 +693,59 @@ struct Helpers {
     const uint32_t kt = smem + stage, qt = kt + L::kQAt;
     const T* k = static_cast<const T*>(p.k) + at;
     const T* q = static_cast<const T*>(p.q) + at;
-    const int tokens = min(end - first, kChunk), m = warp & 3;
-    Square acc;
+    const int tokens = min(end - first, kChunk), group = H == 8 ? warp >> 2 : 0;        // 0: k's warps, 1: q's
     Sums kept;
-    if constexpr (H == 8) {
-      rows<4>(t, k, p.k_stride, first, end, L::kRawAt, kt, s.k_row, s.bad_k);
-      sync();
-      if (warp < 4) {
-        square(kt, kt, m, acc);
-        sync();                                                // (k's weights)
-        weigh(m, acc, s.of_a, 0);
-        store_a(m, acc);
-        invert_block(m);
-        sync_four();
-        columns_of_t(m, kt + L::kTAt, w);
-      } else {
+    // (each piece of code once, whoever runs it: see square)
+    const int passes = H == 8 ? 1 + 2 * group : 4;
+#pragma unroll 1
+    for (int i = 0; i < passes; ++i) {
+      const bool of_q = H == 8 ? i > 0 : i > 1;
+      const int base = H == 8 && i == 0 ? group * 32 : H == 8 ? (i - 1) * 32 : (i & 1) * 32;
+      rows(base, of_q ? q : k, of_q ? p.q_stride : p.k_stride, first, end, L::kRawAt + (of_q ? L::kRows : 0), of_q ? qt : kt, of_q ? s.q_row : s.k_row,
+           of_q ? s.bad_q : s.bad_k);
+      if (H == 8 && i == 0) {
+        sync();
         if (warp == kWeigher) {
           weights_of_k(w, kept);
           fetch_gates(first + kChunk, end);
         }
-        asm volatile("bar.arrive 1, %0;" ::"n"(kThreads) : "memory");
-        rows<2>(t - 128, q, p.q_stride, first, end, L::kRawAt + L::kRows, qt, s.q_row, s.bad_q);
-        sync_q();
-        fetch_rows(first + kChunk, end);
-        if (warp == kWeigher) weights_of_q(w, kept);
-        square(qt, kt, m, acc);
-        sync_q();                                              // (q's weights)
-        weigh(m, acc, s.of_p, 1);
-        store_p(m, acc, generic + stage + L::kPAt, w.of_p);
-        if (warp == kWeigher) total(w, kept, tokens);
-        asm volatile("cp.async.wait_all;" ::: "memory");       // (the others find the rows behind the chunk's barrier)
+        if (group == 1) asm volatile("bar.arrive 1, %0;" ::"n"(kThreads) : "memory");
       }
-    } else {
-      rows<2>(t, k, p.k_stride, first, end, L::kRawAt, kt, s.k_row, s.bad_k);
-      rows<2>(t, q, p.q_stride, first, end, L::kRawAt + L::kRows, qt, s.q_row, s.bad_q);
+    }
+    if (H == 4) {
       sync();
-      fetch_rows(first + kChunk, end);
       if (warp == kWeigher) {
         weights_of_k(w, kept);
-        weights_of_q(w, kept);
         fetch_gates(first + kChunk, end);
       }
-#pragma unroll 1
-      for (int which = 0; which < 2; ++which) {
-        const int mm = which ? 3 - m : m;
-        square(which ? qt : kt, kt, mm, acc);
-        if (!which) sync();
-        weigh(mm, acc, which ? s.of_p : s.of_a, which);
-        if (which) {
-          store_p(mm, acc, generic + stage + L::kPAt, w.of_p);
-        } else {
-          store_a(mm, acc);
-          invert_block(mm);
-        }
-      }
-      sync_four();
-      columns_of_t(m, kt + L::kTAt, w);
-      if (warp == kWeigher) total(w, kept, tokens);
-      asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (group == 1) {
+      sync_q();
     }
+    if (H == 4 || group == 1) {
+      fetch_rows(first + kChunk, end);
+      if (warp == kWeigher) weights_of_q(w, kept);
+    }
+#pragma unroll 1
+    for (int of_q = group; of_q < (H == 8 ? group + 1 : 2); ++of_q) {
+      const int m = H == 4 && of_q ? 3 - warp : warp & 3;
+      Square acc;
+      square(of_q ? qt : kt, kt, m, acc);
+      if (H == 8 && of_q) sync_q();                            // (q's weights)
+      else if (H == 8 || !of_q) sync();                        // (k's weights)
+      weigh(m, acc, of_q ? s.of_p : s.of_a, of_q);
+      if (of_q) {
+        store_p(m, acc, generic + stage + L::kPAt, w.of_p);
+      } else {
+        store_a(m, acc);
+        invert_block(m);
+      }
+    }
+    if (H == 4 || group == 0) {
+      sync_four();
+      columns_of_t(warp, kt + L::kTAt, w);
+    }
+    if (warp == 3) total(w, tokens);
+    asm volatile("cp.async.wait_all;" ::: "memory");           // (the others find the rows behind the chunk's barrier)
   }
 };
 
@@ -851,7 +844,7 @@ struct Columns {
       const T* v = static_cast<const T*>(p.v) + (int64_t)head * p.dv + col0;
       const uint32_t to = smem + at0 + buffer * L::kV;
       if (p.v_vectors) {
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < 4; ++i) {
           const int t = i * 16 + (lane >> 1), half = lane & 1;
           const bool there = first + t < end && col0 + half * 8 < p.dv;
