@@ -10,14 +10,21 @@
 // another.  Its time is that chain's, so it is kept within a warp: a warp has 16 columns, and S^T, R^T, U^T and o^T [16][..] are
 // accumulators of the warps' own matrix instructions (m16n8k16), whose layout is that of the next product's left operand.  Nothing
 // between the three dependent products leaves the warp's registers.  (On tcgen05 each of them goes through tensor memory and a barrier,
-// and the split below, which is made of S, R and U in every chunk, costs the same issue slots.)  Four more warps make
-// A, T and the weights of the next chunk meanwhile; the two sides meet at a barrier a chunk.
+// and the split below, which is made of S, R and U in every chunk, costs the same issue slots.)  Four more warps, a team, make k, q, T, P
+// and the weights of a chunk ahead; of 16-bit rows there are two teams, each with every second chunk.
 //
 // The state is fp32 and stays so: operands are split into two fp16 pieces, 22 bits.  Every row of an operand is brought to below 2^15 by
 // a power of two first, so that what a piece leaves off is below 2^-39 of its row's largest element, whatever the type's range.  k and q
-// of 16 bits are one piece, of fp32 two; S, R and U are two pieces (S k, U k: two products a term; T R: three); T is inverted in fp32: 16 x 16
-// blocks by substitution, then two levels of -T_22 A_21 T_11.  For o of 16 bits S, P and U are rounded to fp16 once, which is finer than
-// o's own rounding; of fp32 they are two pieces too.
+// of 16 bits are one piece, of fp32 two; S, R and U are two pieces (S k, U k: two products a term; T R: three); T is inverted in blocks of
+// 16 x 16, those on the diagonal by substitution in fp32, the others by TF32 products in two pieces (21 bits).  For o of 16 bits S, P and U are
+// rounded to fp16 once, which is finer than o's own rounding; of fp32 they are two pieces too.  Against 64 bits the states of 600 tokens are off
+// by 1.5e-7 of their norm.
+//
+// What bounds it (128 x 128, fp16): a chunk of 64 tokens takes a block of 32 columns 6.5 us, of 64 columns 7.7; its chains alone 3.4 and 5.1, a team alone
+// 10.3.  Both are some 4000 instructions a warp, one after the other at about five cycles each (what the products, 8 cycles of an SM's quarter each, take is
+// 2 us of the chain's).  The instruction cache is part of it: the code of a chunk, 80 KB of which each warp runs its own part, misses it 450 times a
+// chunk, which is why the helpers' code exists once and in loops.  One prompt of 16384 tokens, 32 heads of 128 x 128, bf16: 1643 us (62 at 6.56 TB/s); token
+// by token 22200.  13 prompts of 9001 tokens, 24 heads of 64 x 128, fp16: 344 (22), token by token 4090.
 //
 // Infinities and NaNs: a token whose k, beta or decay is not finite, and those behind it, get a beta of 0, a weight of NaN for o and a
 // decay of NaN for S.  A column whose R or U is not finite from some token on is cleaned from there on, before it meets the zeros of T and P, and its
@@ -77,18 +84,18 @@ struct Scratch {
   int64_t all;                           // G_n
 };
 
-template <typename T, int DK>
+// TEAMS of four helper warps, each with a chunk of its own.
+template <typename T, int DK, int TEAMS>
 struct Layout {
   static constexpr int kPieces = sizeof(T) == 4 ? 2 : 1;
+  static constexpr int kSlots = TEAMS + 1;                     // chunks that are ready or being made
   static constexpr uint32_t kRows = kChunk * DK * 2;           // a piece of k or q
-  static constexpr uint32_t kSquare = kChunk * kChunk * 2;     // a piece of T or P
-  static constexpr uint32_t kQAt = kPieces * kRows, kTAt = 2 * kPieces * kRows, kPAt = kTAt + 2 * kSquare;
-  static constexpr uint32_t kWeightsAt = kPAt + kPieces * kSquare;
-  static constexpr uint32_t kStage = kWeightsAt + sizeof(Weights);
-  static constexpr uint32_t kScratchAt = 2 * kStage;
-  static constexpr uint32_t kEnd = (kScratchAt + sizeof(Scratch) + 127) / 128 * 128;
-  static constexpr uint32_t kRawAt = sizeof(T) == 2 ? kEnd : 0;            // (16 bits) rows of k and q as they come
-  static constexpr uint32_t kColumnsAt = kEnd + (sizeof(T) == 2 ? 2 * kRows : 0);
+  static constexpr uint32_t kTriangle = 10 * 512;              // a piece of T or P: their 16 x 16 blocks up to the diagonal, by rows of blocks
+  static constexpr uint32_t kQAt = kPieces * kRows, kTAt = 2 * kPieces * kRows, kPAt = kTAt + 2 * kTriangle;
+  static constexpr uint32_t kWeightsAt = kPAt + kPieces * kTriangle;
+  static constexpr uint32_t kStage = (kWeightsAt + sizeof(Weights) + 127) / 128 * 128;
+  static constexpr uint32_t kScratchAt = kSlots * kStage, kScratch = (sizeof(Scratch) + 127) / 128 * 128;
+  static constexpr uint32_t kColumnsAt = kScratchAt + TEAMS * kScratch;
   // of a warp with columns: two chunks of v (16 bits), then, where another warp makes o, what it needs: S and U in fp16 as operands, three pairs
   // a lane, o on its way out
   static constexpr uint32_t kV = sizeof(T) == 2 ? kChunk * 32 : 0;
@@ -163,6 +170,11 @@ __device__ __forceinline__ uint32_t unit_at(int r, int unit) {
   return (uint32_t)(r * N * 2 + ((unit ^ (r & 7)) << 4));
 }
 
+// Byte of half a row (16 bytes) r of block (i, k) of a triangle, the halves of every second four rows swapped.
+__device__ __forceinline__ uint32_t triangle_at(int i, int k, int r, int half) {
+  return (uint32_t)((i * (i + 1) / 2 + k) * 512 + r * 32 + ((half ^ (r >> 2 & 1)) << 4));
+}
+
 // ------------------------------------------------------------------------------------------------ the helpers
 
 // Eight elements of a row; 0 beyond `columns` and where the row is not there.
@@ -196,69 +208,67 @@ template <> struct Half<__nv_bfloat16> {
   static __device__ __forceinline__ float2 unpack(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 };
 
-// H warps that make chunks.
-template <typename T, int DK, int H>
+// A team of four warps that makes chunks.
+template <typename T, int DK, int TEAMS>
 struct Helpers {
-  using L = Layout<T, DK>;
-  static constexpr int kThreads = H * 32;
-  static constexpr int kWeigher = H == 8 ? 4 : 0;              // the warp that sums up decays
-  static constexpr bool kStaged = L::kRawAt != 0;
+  using L = Layout<T, DK, TEAMS>;
 
   const ChunkParams& p;
   uint32_t smem;
   uint8_t* generic;
   Scratch& s;
-  int head, t, warp, lane;
-  float g[2], b[2];                                            // (the weigher) of the next chunk
+  int head, team, t, warp, lane;
+  float g[2], b[2];                                            // (the first warp) of the next chunk
 
-  __device__ __forceinline__ Helpers(const ChunkParams& p_, uint32_t smem_, uint8_t* generic_, int head_, int t_)
-      : p(p_), smem(smem_), generic(generic_), s(*reinterpret_cast<Scratch*>(generic_ + L::kScratchAt)), head(head_), t(t_), warp(t_ >> 5), lane(t_ & 31) {}
+  __device__ __forceinline__ Helpers(const ChunkParams& p_, uint32_t smem_, uint8_t* generic_, int head_, int team_, int t_)
+      : p(p_), smem(smem_), generic(generic_), s(*reinterpret_cast<Scratch*>(generic_ + L::kScratchAt + team_ * L::kScratch)), head(head_), team(team_),
+        t(t_), warp(t_ >> 5), lane(t_ & 31) {}
 
-  static __device__ __forceinline__ void sync() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
+  __device__ __forceinline__ void sync() const { asm volatile("bar.sync %0, 128;" ::"r"(14 + team) : "memory"); }
 
-  // The next chunk on its way: its decays and betas, and its rows, of 16 bits and in whole vectors to shared memory, by four warps.
-  __device__ __forceinline__ void fetch_gates(int first, int end) {
-    g[0] = g[1] = b[0] = b[1] = 0.0f;
+  // The team's next chunk: its decays and betas to registers, its rows to the L2 cache.
+  __device__ __forceinline__ void fetch(int first, int end) {
+    if (warp == 0) {
+      g[0] = g[1] = b[0] = b[1] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t at = first + 2 * lane + i;
-      if (at < end) {
-        g[i] = p.decay[at * p.decay_stride + head];
-        b[i] = p.beta[at * p.beta_stride + head];
+      for (int i = 0; i < 2; ++i) {
+        const int64_t at = (int64_t)first + 2 * lane + i;
+        if (at < end) {
+          g[i] = p.decay[at * p.decay_stride + head];
+          b[i] = p.beta[at * p.beta_stride + head];
+        }
       }
     }
-  }
-  __device__ __forceinline__ void fetch_rows(int first, int end) const {
-    if (kStaged && p.qk_vectors) {
-      const int r = (t & 127) >> 1, part = t & 1;
-      const bool row = first + r < end;
-      const int64_t at = (int64_t)(head / p.share) * p.dk;
-      const T* k = static_cast<const T*>(p.k) + at;
-      const T* q = static_cast<const T*>(p.q) + at;
-      const T* kr = k + (row ? (int64_t)(first + r) * p.k_stride : 0);
-      const T* qr = q + (row ? (int64_t)(first + r) * p.q_stride : 0);
-#pragma unroll 1
-      for (int unit = part; unit < DK / 8; unit += 2) {
-        const bool there = row && unit * 8 < p.dk;
-        copy16(smem + L::kRawAt + unit_at<DK>(r, unit), there ? kr + unit * 8 : k, there);
-        copy16(smem + L::kRawAt + L::kRows + unit_at<DK>(r, unit), there ? qr + unit * 8 : q, there);
+    const int64_t row = (int64_t)first + (t >> 1);
+    const int64_t at = (int64_t)(head / p.share) * p.dk;
+    constexpr int kLine = 128 / sizeof(T);
+    if (row < end)
+      for (int e = (t & 1) * kLine; e < p.dk; e += 2 * kLine) {
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const T*>(p.k) + at + row * p.k_stride + e));
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const T*>(p.q) + at + row * p.q_stride + e));
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
   }
 
   // Rows of q or k of a chunk to shared memory, in pieces, scaled where they are not fp16 already.  Leaves what a row is multiplied by (the
   // norm's and the scale's reciprocals) and says which rows are not finite (they come out as 0).
-  // Four threads of four warps have a row: rows base up to base + 31.
-  __device__ __forceinline__ void rows(int base, const T* from, int64_t stride, int first, int end, uint32_t raw, uint32_t to, float* factor, uint32_t* bad) const {
+  // Four threads have a row: rows base up to base + 31.
+  __device__ __forceinline__ void rows(int base, const T* from, int64_t stride, int first, int end, uint32_t to, float* factor, uint32_t* bad) const {
     constexpr int kShare = 4, kUnits = DK / 8 / kShare;        // 16-byte units (of 16-bit elements) of a thread: every fourth one
-    const int u = t & 127, r = base + u / kShare, part = u % kShare;
+    const int r = base + t / kShare, part = t % kShare;
     const bool there = first + r < end;
     const T* row = from + (there ? (int64_t)(first + r) * stride : 0);
     float top = 0.0f, squares[2] = {0.0f, 0.0f}, scale = 1.0f;
     if constexpr (sizeof(T) == 2) {
-      if (!p.qk_vectors) {
-        raw = to - smem;
+      uint4 x[kUnits];
+      uint32_t most = 0;
+      if (p.qk_vectors) {
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+          const int at = (i * kShare + part) * 8;
+          x[i] = make_uint4(0, 0, 0, 0);
+          if (there && at < p.dk) x[i] = __ldg(reinterpret_cast<const uint4*>(row + at));
+        }
+      } else {
         const uint16_t* e = reinterpret_cast<const uint16_t*>(row);
 #pragma unroll 1
         for (int i = 0; i < kUnits; ++i) {
@@ -269,11 +279,9 @@ struct Helpers {
             if (there && at + j < p.dk) w[j / 2] |= (uint32_t)e[at + j] << (16 * (j & 1));
           ptx::st_shared16(to + unit_at<DK>(r, i * kShare + part), w[0], w[1], w[2], w[3]);
         }
-      }
-      uint4 x[kUnits];
-      uint32_t most = 0;
 #pragma unroll
-      for (int i = 0; i < kUnits; ++i) x[i] = *reinterpret_cast<const uint4*>(generic + raw + unit_at<DK>(r, i * kShare + part));
+        for (int i = 0; i < kUnits; ++i) x[i] = *reinterpret_cast<const uint4*>(generic + (to - smem) + unit_at<DK>(r, i * kShare + part));
+      }
 #pragma unroll
       for (int i = 0; i < kUnits; ++i)
 #pragma unroll
@@ -356,7 +364,7 @@ struct Helpers {
 #pragma unroll 1
         for (int i = 0; i < 32 / kShare; ++i) bits |= (odd_rows >> (kShare * i) & 1u) << i;
       }
-      reinterpret_cast<uint8_t*>(bad)[(base + u / kShare) >> 3] = (uint8_t)bits;
+      reinterpret_cast<uint8_t*>(bad)[r >> 3] = (uint8_t)bits;
     }
   }
 
@@ -534,9 +542,9 @@ struct Helpers {
       for (int h = 0; h < 2; ++h) {
         uint32_t hi, lo;
         split(x[2 * h] * scale[h], x[2 * h + 1] * scale[h], hi, lo);
-        uint8_t* at = to + unit_at<kChunk>(i0 + 8 * h, n) + pair * 2;
+        uint8_t* at = to + triangle_at(m, n >> 1, (lane >> 2) + 8 * h, n & 1) + pair * 2;
         *reinterpret_cast<uint32_t*>(at) = hi;
-        if (L::kPieces == 2) *reinterpret_cast<uint32_t*>(at + L::kSquare) = lo;
+        if (L::kPieces == 2) *reinterpret_cast<uint32_t*>(at + L::kTriangle) = lo;
       }
     };
 #pragma unroll
@@ -660,7 +668,7 @@ struct Helpers {
     }
     const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
     if (lane == 0) atomicMax(&s.top_t, most);
-    sync_four();
+    sync();
     const float scale = scale_for(__uint_as_float(*(volatile uint32_t*)&s.top_t));
     if (J == 0 && lane == 0) w.of_t = unscale_for(scale);
 #pragma unroll 1
@@ -669,69 +677,38 @@ struct Helpers {
       block(i);
 #pragma unroll
       for (int u = 0; u < 4; ++u) split(x[u >> 1][2 * (u & 1)] * scale, x[u >> 1][2 * (u & 1) + 1] * scale, h[u], l[u]);
-      const uint32_t at = to + unit_at<kChunk>(i * 16 + (mi >> 1) * 8 + r8, 2 * J + (mi & 1));
+      const uint32_t at = to + triangle_at(i, J, (mi >> 1) * 8 + r8, mi & 1);
       stmatrix_trans(at, h);
-      stmatrix_trans(at + L::kSquare, l);
+      stmatrix_trans(at + L::kTriangle, l);
     }
   }
-  static __device__ __forceinline__ void sync_four() { asm volatile("bar.sync 15, 128;" ::: "memory"); }
 
-  static __device__ __forceinline__ void sync_q() { asm volatile("bar.sync 14, 128;" ::: "memory"); }
-
-  // The first chunk's rows on their way (of eight warps the latter four fetch).
-  __device__ __forceinline__ void begin(int first, int end) {
-    if (warp == kWeigher) fetch_gates(first, end);
-    if (H == 4 || warp >= 4) fetch_rows(first, end);
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    sync();
-  }
-  // Chunk of rows first up to first + 64 (or end), which were fetched, into `stage`; the next one's are fetched.  Of eight warps four have A and T, whose
-  // way through a chunk is the longest, the others q, the weights and P; k's rows are everybody's.  Of four warps all have both, one after the other.
+  // Chunk of rows first up to first + 64 (or end) into `stage`; the team's next one, two chunks on where there are two teams, is fetched.
   __device__ __forceinline__ void prepare(int first, int end, uint32_t stage) {
     Weights& w = *reinterpret_cast<Weights*>(generic + stage + L::kWeightsAt);
     const int64_t at = (int64_t)(head / p.share) * p.dk;
     const uint32_t kt = smem + stage, qt = kt + L::kQAt;
     const T* k = static_cast<const T*>(p.k) + at;
     const T* q = static_cast<const T*>(p.q) + at;
-    const int tokens = min(end - first, kChunk), group = H == 8 ? warp >> 2 : 0;        // 0: k's warps, 1: q's
-    Sums kept;
-    // (each piece of code once, whoever runs it: see square)
-    const int passes = H == 8 ? 1 + 2 * group : 4;
+    // (each piece of code once, loops rolled: see square)
 #pragma unroll 1
-    for (int i = 0; i < passes; ++i) {
-      const bool of_q = H == 8 ? i > 0 : i > 1;
-      const int base = H == 8 && i == 0 ? group * 32 : H == 8 ? (i - 1) * 32 : (i & 1) * 32;
-      rows(base, of_q ? q : k, of_q ? p.q_stride : p.k_stride, first, end, L::kRawAt + (of_q ? L::kRows : 0), of_q ? qt : kt, of_q ? s.q_row : s.k_row,
-           of_q ? s.bad_q : s.bad_k);
-      if (H == 8 && i == 0) {
-        sync();
-        if (warp == kWeigher) {
-          weights_of_k(w, kept);
-          fetch_gates(first + kChunk, end);
-        }
-        if (group == 1) asm volatile("bar.arrive 1, %0;" ::"n"(kThreads) : "memory");
-      }
+    for (int i = 0; i < 4; ++i) {
+      const bool of_q = i > 1;
+      rows((i & 1) * 32, of_q ? q : k, of_q ? p.q_stride : p.k_stride, first, end, of_q ? qt : kt, of_q ? s.q_row : s.k_row, of_q ? s.bad_q : s.bad_k);
     }
-    if (H == 4) {
-      sync();
-      if (warp == kWeigher) {
-        weights_of_k(w, kept);
-        fetch_gates(first + kChunk, end);
-      }
-    } else if (group == 1) {
-      sync_q();
+    sync();
+    if (warp == 0) {
+      Sums kept;
+      weights_of_k(w, kept);
+      weights_of_q(w, kept);
     }
-    if (H == 4 || group == 1) {
-      fetch_rows(first + kChunk, end);
-      if (warp == kWeigher) weights_of_q(w, kept);
-    }
+    fetch(first + TEAMS * kChunk, end);
 #pragma unroll 1
-    for (int of_q = group; of_q < (H == 8 ? group + 1 : 2); ++of_q) {
-      const int m = H == 4 && of_q ? 3 - warp : warp & 3;
+    for (int of_q = 0; of_q < 2; ++of_q) {
+      const int m = of_q ? 3 - warp : warp;
       Square acc;
       square(of_q ? qt : kt, kt, m, acc);
-      if (H == 8 && of_q) sync_q();                            // (q's weights)
-      else if (H == 8 || !of_q) sync();                        // (k's weights)
+      if (!of_q) sync();                                       // (the weights)
       weigh(m, acc, of_q ? s.of_p : s.of_a, of_q);
       if (of_q) {
         store_p(m, acc, generic + stage + L::kPAt, w.of_p);
@@ -740,19 +717,15 @@ struct Helpers {
         invert_block(m);
       }
     }
-    if (H == 4 || group == 0) {
-      sync_four();
-      columns_of_t(warp, kt + L::kTAt, w);
-    }
-    if (warp == 3) total(w, tokens);
-    asm volatile("cp.async.wait_all;" ::: "memory");           // (the others find the rows behind the chunk's barrier)
+    sync();
+    columns_of_t(warp, kt + L::kTAt, w);
+    if (warp == 3) total(w, min(end - first, kChunk));
   }
 };
 
 // ------------------------------------------------------------------------------------------------ the columns of a warp
 
 // Rows g and g + 8 of accumulators over tokens: from the first token on whose number is not finite all become 0; `from` says which.
-// (In line: register counts set by warpgroup leave no room for calls.)
 __device__ __forceinline__ void clean(float (&x)[8][4], int (&from)[2]) {
   const int pair = (threadIdx.x & 3) * 2;
 #pragma unroll
@@ -803,9 +776,9 @@ __device__ __forceinline__ void operand(const float (&x)[N][4], int ks, const fl
 
 // 16 columns of a head.  SPLIT: one warp has the chain from S to S, another one makes o from S and U in fp16, which the first leaves in shared memory; it says
 // so at two barriers of the pair.  Otherwise one warp does both.
-template <typename T, int DK, bool SPLIT>
+template <typename T, int DK, bool SPLIT, int TEAMS>
 struct Columns {
-  using L = Layout<T, DK>;
+  using L = Layout<T, DK, TEAMS>;
   static constexpr bool kFull = L::kPieces == 2;               // fp32: o too from two pieces
   static_assert(!(kFull && SPLIT), "");
 
@@ -911,7 +884,7 @@ struct Columns {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (kk > 2 * half + i) continue;
-        const uint32_t at = pt + unit_at<kChunk>((2 * half + i) * 16 + (mi >> 1) * 8 + r8, 2 * kk + (mi & 1));
+        const uint32_t at = pt + triangle_at(2 * half + i, kk, (mi >> 1) * 8 + r8, mi & 1);
         uint32_t b[4];
         ldmatrix(at, b);
 #pragma unroll
@@ -920,7 +893,7 @@ struct Columns {
           mma(I[2 * i + h], hi, b[2 * h], b[2 * h + 1]);
         }
         if (kFull) {
-          ldmatrix(at + L::kSquare, b);
+          ldmatrix(at + L::kTriangle, b);
 #pragma unroll
           for (int h = 0; h < 2; ++h) mma(I[2 * i + h], hi, b[2 * h], b[2 * h + 1]);
         }
@@ -987,8 +960,7 @@ struct Columns {
   }
 
   // o of chunk c, by the warp beside the chain's.
-  __device__ __forceinline__ void chunk_o(int c, int first, int end) const {
-    const uint32_t stage = (c & 1) * L::kStage;
+  __device__ __forceinline__ void chunk_o(uint32_t stage, int first, int end) const {
     const Weights& w = *reinterpret_cast<const Weights*>(generic + stage + L::kWeightsAt);
     float O[2][4][4];
 #pragma unroll
@@ -1021,8 +993,8 @@ struct Columns {
   }
 
   // S of chunk c, and its o too where no other warp makes it.
-  __device__ __forceinline__ void chunk(int c, int first, int end, float (&S)[DK / 8][4]) const {
-    const uint32_t stage = (c & 1) * L::kStage, kt = smem + stage, qt = kt + L::kQAt, tt = kt + L::kTAt;
+  __device__ __forceinline__ void chunk(int c, uint32_t stage, int first, int end, float (&S)[DK / 8][4]) const {
+    const uint32_t kt = smem + stage, qt = kt + L::kQAt, tt = kt + L::kTAt;
     const Weights& w = *reinterpret_cast<const Weights*>(generic + stage + L::kWeightsAt);
     load_v((c + 1) & 1, first + kChunk, end);
     float v32[kFull ? 8 : 1][4];
@@ -1129,9 +1101,9 @@ struct Columns {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           if (np + i > 3) break;
-          const uint32_t at = tt + unit_at<kChunk>((np + i) * 16 + (mi >> 1) * 8 + r8, 2 * kk + (mi & 1));
+          const uint32_t at = tt + triangle_at(np + i, kk, (mi >> 1) * 8 + r8, mi & 1);
           ldmatrix(at, b[i]);
-          ldmatrix(at + L::kSquare, bl[i]);
+          ldmatrix(at + L::kTriangle, bl[i]);
         }
 #pragma unroll
         for (int m = 0; m < 3; ++m)
@@ -1256,23 +1228,26 @@ struct Columns {
   }
 };
 
-// How a block's warps share the work: W with the chains of 16 columns each, with SPLIT as many that make o, then H helpers.  Registers: of the
-// warps with columns (with SPLIT and four of them: of those with the chains and of those that make o), of the helpers; what the warpgroups ask for
-// is no more than the block is launched with.
-template <int W_, bool SPLIT_, int H_, int CHAIN, int O, int HELP>
+// How a block's warps share the work: W with the chains of 16 columns each, with SPLIT as many that make o, then TEAMS of four helpers.  Registers: of
+// the warpgroups with columns and of the helpers' (0: as launched); they ask for no more than the block is launched with.
+template <int W_, bool SPLIT_, int TEAMS_, int CHAIN, int HELP>
 struct Shape {
-  static constexpr int W = W_, H = H_, kWarps = SPLIT_ ? 2 * W_ : W_, kThreads = (kWarps + H_) * 32;
+  static constexpr int W = W_, TEAMS = TEAMS_, kWarps = SPLIT_ ? 2 * W_ : W_, kThreads = (kWarps + 4 * TEAMS_) * 32;
   static constexpr bool SPLIT = SPLIT_;
-  static constexpr int kChain = CHAIN, kO = O, kHelp = HELP;
-  static constexpr int kLaunched = 65536 / kThreads / 8 * 8 > 255 ? 255 : 65536 / kThreads / 8 * 8;
-  static constexpr int kAsked = (O > 0 ? W_ * 32 * (CHAIN + O) : kWarps * 32 * CHAIN) + H_ * 32 * HELP;
-  static_assert(CHAIN == 0 || (O > 0 ? W_ : kWarps) % 4 == 0, "");
-  static_assert(CHAIN == 0 || kAsked <= kLaunched * kThreads, "");
+  static constexpr int kChain = CHAIN, kHelp = HELP, kAsked = kWarps * 32 * CHAIN + 4 * TEAMS_ * 32 * HELP;
+  static_assert(CHAIN == 0 || (kWarps % 4 == 0 && kAsked <= 65536 / kThreads / 8 * 8 * kThreads), "");
 };
+
+// Chunk c is ready, and chunk c - 1 done with: a barrier for even and one for odd chunks, at which a team does not wait for the other one's chunks.
+template <int THREADS>
+__device__ __forceinline__ void chunk_barrier(int c, bool wait) {
+  if (wait) asm volatile("bar.sync %0, %1;" ::"r"((c & 1) * 13), "n"(THREADS) : "memory");
+  else asm volatile("bar.arrive %0, %1;" ::"r"((c & 1) * 13), "n"(THREADS) : "memory");
+}
 
 template <typename T, int DK, typename F>
 __global__ void __launch_bounds__(F::kThreads, 1) delta_chunks_kernel(const ChunkParams p) {
-  using L = Layout<T, DK>;
+  using L = Layout<T, DK, F::TEAMS>;
   constexpr int W = F::W;
   extern __shared__ __align__(128) uint8_t dynamic_smem[];
   const uint32_t smem = smem_u32(dynamic_smem);
@@ -1284,41 +1259,39 @@ __global__ void __launch_bounds__(F::kThreads, 1) delta_chunks_kernel(const Chun
   const SequenceRows rows = rows_of(p.seqs, b);
   const int chunks = (rows.end - rows.begin + kChunk - 1) / kChunk;
   const int64_t state_at = ((int64_t)slot * p.heads + head) * p.dk * p.dv;
+  uint32_t stage = 0;
+  auto next = [&]() { stage = stage == (L::kSlots - 1) * L::kStage ? 0 : stage + L::kStage; };
   if (warp >= F::kWarps) {
     if constexpr (F::kChain > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kHelp));
-    const int t = (int)threadIdx.x - F::kWarps * 32;
-    Helpers<T, DK, F::H> helpers(p, smem, dynamic_smem, head, t);
-    helpers.begin(rows.begin, rows.end);
-    for (int c = 0; c < chunks; ++c) {
-      helpers.prepare(rows.begin + c * kChunk, rows.end, (c & 1) * L::kStage);
-      __syncthreads();
+    const int t = (int)threadIdx.x - F::kWarps * 32, team = (warp - F::kWarps) >> 2;
+    Helpers<T, DK, F::TEAMS> helpers(p, smem, dynamic_smem, head, team, t & 127);
+    helpers.fetch(rows.begin + team * kChunk, rows.end);
+    // (Chunk c goes where chunk c - slots was.  Of one team that is the chunk before the last: done with at the barrier behind it.  Of two, the team
+    // begins chunk c behind the barrier of chunk c - 2, where c - 3 is done with.)
+    for (int c = 0; c < chunks; ++c, next()) {
+      const bool mine = F::TEAMS == 1 || (c & 1) == team;
+      if (mine) helpers.prepare(rows.begin + c * kChunk, rows.end, stage);
+      chunk_barrier<F::kThreads>(c, mine);
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
-    // (a warpgroup as a whole: with four chains theirs and the one that makes o, otherwise all that have columns)
-    if constexpr (F::kChain > 0 && F::kO == 0) {
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kChain));
-    } else if constexpr (F::kChain > 0) {
-      if (warp < W) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kChain));
-      else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kO));
-    }
+    if constexpr (F::kChain > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kChain));
     const int index = F::SPLIT && warp >= W ? warp - W : warp, col0 = ((int)tile * W + index) * 16;
-    const Columns<T, DK, F::SPLIT> mine(p, smem, dynamic_smem, head, col0, index);
+    const Columns<T, DK, F::SPLIT, F::TEAMS> mine(p, smem, dynamic_smem, head, col0, index);
     const bool live = col0 < p.dv;
     if (!F::SPLIT || warp < W) {
       float S[DK / 8][4];
       mine.states(live && p.state_in && resumes(p.seqs, b) ? p.state_in + state_at : nullptr, S);
       if (live) mine.load_v(0, rows.begin, rows.end);
-      for (int c = 0; c < chunks; ++c) {
-        __syncthreads();
-        if (live) mine.chunk(c, rows.begin + c * kChunk, rows.end, S);
+      for (int c = 0; c < chunks; ++c, next()) {
+        chunk_barrier<F::kThreads>(c, true);
+        if (live) mine.chunk(c, stage, rows.begin + c * kChunk, rows.end, S);
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       if (live && p.state_out) mine.store_states(p.state_out + state_at, S);
     } else if constexpr (F::SPLIT) {
-      for (int c = 0; c < chunks; ++c) {
-        __syncthreads();
-        if (live) mine.chunk_o(c, rows.begin + c * kChunk, rows.end);
+      for (int c = 0; c < chunks; ++c, next()) {
+        chunk_barrier<F::kThreads>(c, true);
+        if (live) mine.chunk_o(stage, rows.begin + c * kChunk, rows.end);
       }
     }
   }
@@ -1326,18 +1299,19 @@ __global__ void __launch_bounds__(F::kThreads, 1) delta_chunks_kernel(const Chun
 
 template <typename T, int DK, typename F>
 cudaError_t launch(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
-  constexpr uint32_t kBytes = Layout<T, DK>::kColumnsAt + F::W * Layout<T, DK>::template kColumns<F::SPLIT>;
+  using L = Layout<T, DK, F::TEAMS>;
+  constexpr uint32_t kBytes = L::kColumnsAt + F::W * L::template kColumns<F::SPLIT>;
   static_assert(kBytes <= 227 * 1024, "");
   static bool attr_done[64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!attr_done[dev]) {
-    cudaError_t e = cudaFuncSetAttribute(delta_chunks_kernel<T, DK, F>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
+    const cudaError_t e = cudaFuncSetAttribute(delta_chunks_kernel<T, DK, F>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
     if (e != cudaSuccess) return e;
     // A build whose blocks start with fewer registers than the warpgroups ask for later would wait for them without end: not launched.
     cudaFuncAttributes built;
-    e = cudaFuncGetAttributes(&built, delta_chunks_kernel<T, DK, F>);
-    if (e != cudaSuccess) return e;
+    const cudaError_t asked = cudaFuncGetAttributes(&built, delta_chunks_kernel<T, DK, F>);
+    if (asked != cudaSuccess) return asked;
     if (F::kChain > 0 && built.numRegs * F::kThreads < F::kAsked) return cudaErrorNotSupported;
     attr_done[dev] = true;
   }
@@ -1348,16 +1322,18 @@ cudaError_t launch(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
+// The columns of a block: 32 while that gives no more blocks than there are SMs, 64 beyond.  (A chunk of 64 tokens, 128 x 128, takes a block of 32 columns
+// 6.5 us, of 64 columns 7.7.  One prompt of 16384 tokens, 32 heads, 1643 and 1960 us; four of 8192 tokens in all 849 and 583; 128 columns and one team
+// 1136.)  fp32: its pieces leave shared memory for one team, and registers for o beside the chain.
 template <typename T, int DK>
 cudaError_t launch_width(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
-  const int64_t columns = (int64_t)sequences * p.heads * ((p.dv + 15) / 16);
+  const bool wide = p.dv > 32 && (int64_t)sequences * p.heads * ((p.dv + 31) / 32) > 148;
   if constexpr (sizeof(T) == 2) {
-    if (p.dv > 64 && columns >= 148 * 8) return launch<T, DK, Shape<8, false, 8, 168, 0, 88>>(p, sequences, stream);
-    if (p.dv > 32 && columns >= 148 * 4) return launch<T, DK, Shape<4, true, 8, 208, 104, 96>>(p, sequences, stream);
-    return launch<T, DK, Shape<2, true, 8, 208, 0, 144>>(p, sequences, stream);
+    if (wide) return launch<T, DK, Shape<4, false, 2, 232, 136>>(p, sequences, stream);
+    return launch<T, DK, Shape<2, true, 2, 208, 144>>(p, sequences, stream);
   } else {
-    if (p.dv > 32 && columns >= 148 * 4) return launch<T, DK, Shape<4, false, 4, 0, 0, 0>>(p, sequences, stream);
-    return launch<T, DK, Shape<2, false, 4, 0, 0, 0>>(p, sequences, stream);
+    if (wide) return launch<T, DK, Shape<4, false, 1, 0, 0>>(p, sequences, stream);
+    return launch<T, DK, Shape<2, false, 1, 0, 0>>(p, sequences, stream);
   }
 }
 

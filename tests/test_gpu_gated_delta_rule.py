@@ -259,3 +259,38 @@ def test_on_another_stream():
     binding.im2win_gated_delta_rule(q, k, v, g, beta, other, normalize=True, stream=side)
     side.synchronize()
     assert torch.equal(o, other) and bool(o.any())
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("heads,dk,dv", [(40, 64, 128), (75, 128, 64), (40, 100, 100), (52, 33, 96)])
+def test_more_columns_than_blocks_of_32(dtype, heads, dk, dv):
+    """Heads and columns beyond one block of 32 columns for each SM."""
+    run(dtype, [65, 20], heads, heads // 5 if heads % 5 == 0 else heads, dk, dv, tail=1, resume=[1, 0])
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_columns_that_are_not_finite_in_wide_blocks(dtype):
+    def edit(q, k, v, g, beta, st):
+        v[30, 3, 100] = math.inf
+        v[70, 39, 7] = math.nan
+        st[0, 5, 3, 64] = math.nan
+        k[80, 1, 0] = math.inf
+    run(dtype, [100], 40, 8, 64, 128, edit=edit)
+
+
+def test_pools_beyond_32_bits():
+    """A state whose first element is number 2^31 and more of the pool."""
+    pool = torch.empty(4200, 32, 128, 128, device="cuda")
+    gen = torch.Generator().manual_seed(2)
+    for n in (1, 40):
+        q, k, v = (torch.randn(n, 32, 128, generator=gen).bfloat16() for _ in range(3))
+        g, beta, st = -torch.rand(n, 32, generator=gen), torch.rand(n, 32, generator=gen), torch.randn(1, 32, 128, 128, generator=gen)
+        pool[4199].copy_(st[0])
+        o = torch.zeros(n, 32, 128, dtype=torch.bfloat16, device="cuda")
+        binding.im2win_gated_delta_rule(*(x.cuda() for x in (q, k, v, g, beta)), o, normalize=True, state=pool, state_out=pool,
+                                        cu_seqlens=torch.tensor([0, n], dtype=torch.int32, device="cuda"),
+                                        slots=torch.tensor([4199], dtype=torch.int32, device="cuda"))
+        want, off, new, new_off = delta_64(q, k, v, g, beta, 1.0, True, torch.zeros(n, 32, 128), st, st, sequence_list([n]), 1,
+                                           2 * half_step(torch.float16))
+        close(o, want, off + rounding(want, torch.bfloat16), "o")
+        close_columns(pool[4199:], new, new_off, "pool")

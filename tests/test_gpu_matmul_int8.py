@@ -104,3 +104,39 @@ def test_captured_and_on_another_stream(m):
     binding.im2win_matmul_int8(x, xs, w, ws, other, stream=side)
     side.synchronize()
     assert torch.equal(y, other) and bool(y.any())
+
+
+@pytest.mark.parametrize("k", [16, 15])
+def test_outputs_beyond_32_bits(k):
+    """Elements of y whose number passes 2^31."""
+    m, n = 70001, 32768
+    x, w = (torch.randint(-127, 128, (rows, k), device="cuda", dtype=torch.int8) for rows in (m, n))
+    xs, ws = torch.rand(m, device="cuda"), torch.rand(n, device="cuda")
+    y = torch.zeros(m, n, dtype=torch.float16, device="cuda")
+    binding.im2win_matmul_int8(x, xs, w, ws, y)
+    for part in (slice(0, 3), slice(m - 3, m)):
+        want = (x[part].double() @ w.double().T * xs[part].double()[:, None] * ws.double()).cpu()
+        # (65520 and more lies nearer to 2^16, which fp16 does not have, than to its largest number, 65504: an infinity)
+        want = torch.where(want.abs() >= 65520, want.sign() * torch.inf, want)
+        close(y[part], want, 3 * 2.0 ** -24 * want.abs() + rounding(want, torch.float16), "y")
+
+
+@pytest.mark.parametrize("m,n", [(300, 30000), (40, 40000)])
+@pytest.mark.parametrize("drop", ["0", "1"])
+def test_gives_up_and_says_so(m, n, drop, monkeypatch):
+    """The first CTA (pair) does not say that a tile's sums are done: a testing aid, which also lowers the limit of looks; the kernel returns.  What comes of
+    other CTAs is right, of this one's that tile and those behind it are NaN (of a pair all of them where its last waits ran out)."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x, w = (torch.randint(-127, 128, (rows, 256), generator=gen, device="cuda", dtype=torch.int8) for rows in (m, n))
+    xs, ws = torch.rand(m, generator=gen, device="cuda"), torch.rand(n, generator=gen, device="cuda")
+    y = torch.zeros(m, n, device="cuda")
+    monkeypatch.setenv("IM2WIN_MATMUL_DROP", drop)
+    binding.im2win_matmul_int8(x, xs, w, ws, y)
+    torch.cuda.synchronize()
+    monkeypatch.delenv("IM2WIN_MATMUL_DROP")
+    want = (x.double() @ w.double().T) * xs.double()[:, None] * ws.double()
+    bad = ~((y.double() - want).abs() <= 4 * 2.0 ** -24 * want.abs() + 2.0 ** -140)
+    assert bool(bad.any()) and bool(y[bad].isnan().all()) and float(bad.float().mean()) < 0.05
+    again = torch.zeros_like(y)
+    binding.im2win_matmul_int8(x, xs, w, ws, again)
+    assert not bool(((again.double() - want).abs() > 4 * 2.0 ** -24 * want.abs()).any())

@@ -177,3 +177,17 @@ def test_captured_and_on_another_stream():
     binding.im2win_rms_norm(x, w, other, stream=side)
     side.synchronize()
     assert torch.equal(y, other) and bool(y.any())
+
+
+def test_rows_beyond_32_bits():
+    """Elements whose number passes 2^31."""
+    rows, channels = 33000, 65600
+    x = torch.zeros(rows, channels, dtype=torch.bfloat16, device="cuda")
+    x[-3:] = torch.randn(3, channels, device="cuda").bfloat16()
+    y, scales = torch.zeros(rows, channels, dtype=torch.int8, device="cuda"), torch.zeros(rows, device="cuda")
+    binding.im2win_rms_norm(x, None, y, scales=scales)
+    h, z, rate = norm_64(x[-3:].cpu(), None, None, 1e-6)
+    q, want = int8_64(z, rate)
+    assert torch.equal(y[-3:].cpu().double(), q)
+    close(scales[-3:], want, OFF * want, "scales")
+    assert not y[:-3].any() and not scales[:-3].any()
