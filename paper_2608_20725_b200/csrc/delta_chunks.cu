@@ -16,8 +16,8 @@
 // The state is fp32 and stays so: operands are split into two fp16 pieces, 22 bits.  Every row of an operand is brought to below 2^15 by
 // a power of two first, so that what a piece leaves off is below 2^-39 of its row's largest element, whatever the type's range.  k and q
 // of 16 bits are one piece, of fp32 two; S, R and U are two pieces (S k, U k: two products a term; T R: three); T is inverted in blocks of
-// 16 x 16, those on the diagonal by substitution in fp32, the others by TF32 products in two pieces (21 bits).  For o of 16 bits S, P and U are
-// rounded to fp16 once, which is finer than o's own rounding; of fp32 they are two pieces too.  Against 64 bits the states of 600 tokens are off
+// 16 x 16, those on the diagonal by substitution in fp32, the others by TF32 products in two pieces (21 bits).  For o of bf16 S, P and U are
+// rounded to fp16 once, which is finer than o's own rounding, of fp16 P alone; of fp32 they are all two pieces.  Against 64 bits the states of 600 tokens are off
 // by 1.5e-7 of their norm.
 //
 // What bounds it (128 x 128, fp16): a chunk of 64 tokens takes a block of 32 columns 6.5 us, of 64 columns 7.7; its chains alone 3.4 and 5.1, a team alone
@@ -32,6 +32,7 @@
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "ptx_sm100.cuh"
@@ -96,11 +97,13 @@ struct Layout {
   static constexpr uint32_t kStage = (kWeightsAt + sizeof(Weights) + 127) / 128 * 128;
   static constexpr uint32_t kScratchAt = kSlots * kStage, kScratch = (sizeof(Scratch) + 127) / 128 * 128;
   static constexpr uint32_t kColumnsAt = kScratchAt + TEAMS * kScratch;
-  // of a warp with columns: two chunks of v (16 bits), then, where another warp makes o, what it needs: S and U in fp16 as operands, three pairs
-  // a lane, o on its way out
+  // fp16: o from two pieces of S and of U, so that P alone is rounded for it (with all three rounded once o was off by 1.7 times its own rounding)
+  static constexpr bool kTwo = std::is_same<T, __half>::value;
+  // of a warp with columns: two chunks of v (16 bits), where o leaves through too; then, where another warp makes o, what it needs: S and U as operands,
+  // three pairs a lane
   static constexpr uint32_t kV = sizeof(T) == 2 ? kChunk * 32 : 0;
-  static constexpr uint32_t kSAt = 2 * kV, kUAt = kSAt + DK / 16 * 512, kPairsAt = kUAt + 4 * 512, kOAt = kPairsAt + 3 * 256;
-  template <bool SPLIT> static constexpr uint32_t kColumns = SPLIT ? kOAt + kV : 2 * kV;
+  static constexpr uint32_t kSAt = 2 * kV, kUAt = kSAt + DK / 16 * 512 * (1 + kTwo), kPairsAt = kUAt + 4 * 512 * (1 + kTwo);
+  template <bool SPLIT> static constexpr uint32_t kColumns = SPLIT ? kPairsAt + 3 * 256 : 2 * kV;
 };
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -780,6 +783,7 @@ template <typename T, int DK, bool SPLIT, int TEAMS>
 struct Columns {
   using L = Layout<T, DK, TEAMS>;
   static constexpr bool kFull = L::kPieces == 2;               // fp32: o too from two pieces
+  static constexpr bool kLow = kFull || L::kTwo;               // of S and U
   static_assert(!(kFull && SPLIT), "");
 
   const ChunkParams& p;
@@ -855,7 +859,7 @@ struct Columns {
       ldmatrix(at, a);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (kFull) mma(O[2 * i + h], lo, a[2 * h], a[2 * h + 1]);
+        if (kLow) mma(O[2 * i + h], lo, a[2 * h], a[2 * h + 1]);
         mma(O[2 * i + h], hi, a[2 * h], a[2 * h + 1]);
       }
       if (kFull) {
@@ -889,7 +893,7 @@ struct Columns {
         ldmatrix(at, b);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          if (kFull) mma(I[2 * i + h], lo, b[2 * h], b[2 * h + 1]);
+          if (kLow) mma(I[2 * i + h], lo, b[2 * h], b[2 * h + 1]);
           mma(I[2 * i + h], hi, b[2 * h], b[2 * h + 1]);
         }
         if (kFull) {
@@ -960,24 +964,29 @@ struct Columns {
   }
 
   // o of chunk c, by the warp beside the chain's.
-  __device__ __forceinline__ void chunk_o(uint32_t stage, int first, int end) const {
+  __device__ __forceinline__ void chunk_o(int c, uint32_t stage, int first, int end) const {
     const Weights& w = *reinterpret_cast<const Weights*>(generic + stage + L::kWeightsAt);
     float O[2][4][4];
 #pragma unroll
     for (int n = 0; n < 8; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) O[n >> 2][n & 3][e] = 0.0f;
-    auto handed = [&](uint32_t at, int i, uint32_t (&hi)[4]) {
-      const uint4 x = reinterpret_cast<const uint4*>(generic + at0 + at)[i * 32 + lane];
+    auto handed = [&](uint32_t at, int steps, int i, uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+      const uint4* from = reinterpret_cast<const uint4*>(generic + at0 + at) + i * 32 + lane;
+      const uint4 x = from[0];
       hi[0] = x.x, hi[1] = x.y, hi[2] = x.z, hi[3] = x.w;
+      if constexpr (L::kTwo) {
+        const uint4 y = from[steps * 32];
+        lo[0] = y.x, lo[1] = y.y, lo[2] = y.z, lo[3] = y.w;
+      }
     };
     await(0);
 #pragma unroll 2
     for (int ks = 0; ks < DK / 16; ++ks) {
-      uint32_t hi[4];
-      handed(L::kSAt, ks, hi);
+      uint32_t hi[4], lo[4];
+      handed(L::kSAt, DK / 16, ks, hi, lo);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) multiply_q(smem + stage + L::kQAt, half, ks, hi, hi, O[half]);
+      for (int half = 0; half < 2; ++half) multiply_q(smem + stage + L::kQAt, half, ks, hi, lo, O[half]);
     }
     await(1);
     const float2 ps = lane_pair<float2>(0), po = lane_pair<float2>(1);
@@ -987,9 +996,9 @@ struct Columns {
     const bool odd = __any_sync(0xffffffffu, min(f.x, f.y) < kChunk);
 #pragma unroll
     for (int half = 0; half < 2; ++half)
-      finish_o(smem + stage + L::kPAt, w, half, O[half], per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { handed(L::kUAt, kk, hi); },
-               odd, from, at0 + L::kOAt, first, end);
-    store_o(at0 + L::kOAt, first, end);
+      finish_o(smem + stage + L::kPAt, w, half, O[half], per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { handed(L::kUAt, 4, kk, hi, lo); },
+               odd, from, at0 + (c & 1) * L::kV, first, end);
+    store_o(at0 + (c & 1) * L::kV, first, end);        // (v of the chunk has been read: seen with U)
   }
 
   // S of chunk c, and its o too where no other warp makes it.
@@ -1024,7 +1033,11 @@ struct Columns {
     for (int ks = 0; ks < DK / 16; ++ks) {
       uint32_t hi[4], lo[4];
       operand(S, ks, scale_s, hi, lo);
-      if constexpr (SPLIT) ptx::st_shared16(smem + at0 + L::kSAt + (ks * 32 + lane) * 16, hi[0], hi[1], hi[2], hi[3]);
+      if constexpr (SPLIT) {
+        const uint32_t to = smem + at0 + L::kSAt + (ks * 32 + lane) * 16;
+        ptx::st_shared16(to, hi[0], hi[1], hi[2], hi[3]);
+        if (L::kTwo) ptx::st_shared16(to + DK / 16 * 512, lo[0], lo[1], lo[2], lo[3]);
+      }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {                   // (four accumulators, so that a product does not wait for the one before)
         uint32_t b[2][4];
@@ -1135,13 +1148,11 @@ struct Columns {
       if constexpr (SPLIT) {
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
-          uint32_t hi[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float f = scale[i & 1];
-            hi[i] = pack_half(U[2 * kk + (i >> 1)][2 * (i & 1)] * f, U[2 * kk + (i >> 1)][2 * (i & 1) + 1] * f);
-          }
-          ptx::st_shared16(smem + at0 + L::kUAt + (kk * 32 + lane) * 16, hi[0], hi[1], hi[2], hi[3]);
+          uint32_t hi[4], lo[4];
+          operand(U, kk, scale, hi, lo);
+          const uint32_t to = smem + at0 + L::kUAt + (kk * 32 + lane) * 16;
+          ptx::st_shared16(to, hi[0], hi[1], hi[2], hi[3]);
+          if (L::kTwo) ptx::st_shared16(to + 4 * 512, lo[0], lo[1], lo[2], lo[3]);
         }
         lane_pair<float2>(1) = make_float2(per_o[0], per_o[1]);
         lane_pair<int2>(2) = make_int2(from[0], from[1]);
@@ -1291,7 +1302,7 @@ __global__ void __launch_bounds__(F::kThreads, 1) delta_chunks_kernel(const Chun
     } else if constexpr (F::SPLIT) {
       for (int c = 0; c < chunks; ++c, next()) {
         chunk_barrier<F::kThreads>(c, true);
-        if (live) mine.chunk_o(stage, rows.begin + c * kChunk, rows.end);
+        if (live) mine.chunk_o(c, stage, rows.begin + c * kChunk, rows.end);
       }
     }
   }
