@@ -77,6 +77,13 @@ def test_the_largest_sums(k):
         run("f32", m, 130, k, extremes=True)
 
 
+@pytest.mark.parametrize("m", [1, 2, 4, 5, 8, 15, 16, 17])
+def test_few_rows_that_start_anywhere(m):
+    for n, k in ((1, 1), (30, 17), (17, 31), (40, 2047), (33, 2049), (100, 4095), (1001, 8191)):
+        run("f32", m, n, k, bias=n % 2 == 1)
+    run("bf16", m, 64, 512, shift=3, pitch=1)
+
+
 def test_many_tiles():
     run("bf16", 3000, 2100, 512, kernel=None)
     run("bf16", 40, 30000, 256)
