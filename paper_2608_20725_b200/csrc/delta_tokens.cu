@@ -38,9 +38,11 @@ struct TokensParams {
 };
 
 // R: rows of S of a warp (dk <= kWarps * R); VEC: columns of a lane, dv a multiple of it; BATCH: tokens loaded while the BATCH before
-// them are worked on
+// them are worked on.  Single tokens: registers for two blocks of 64 numbers a thread on an SM, four of fewer.  (One token of each of 128 sequences, 32 heads
+// of 128 x 128, states in one order: 64 numbers a thread, one, two, three blocks 143, 104, 120 us; 32 numbers, as the registers fell, two blocks, 110, three 102,
+// four 100, and 93 in any order of a pool: 5.7 TB/s; 80 at the measured 6.56.)
 template <typename T, int R, int VEC, int BATCH>
-__global__ void __launch_bounds__(kWarps * 32) delta_tokens_kernel(const TokensParams p) {
+__global__ void __launch_bounds__(kWarps * 32, BATCH > 1 ? 1 : R * VEC >= 64 ? 2 : 4) delta_tokens_kernel(const TokensParams p) {
   using VF = Vec<float, VEC>;
   __shared__ __align__(16) float sums[BATCH > 1 ? 2 : 1][2][kWarps][32 * VEC];       // of k S and q S
   __shared__ float products[BATCH > 1 ? 2 : 1][3][kWarps];                           // of q k, q q, k k
