@@ -569,7 +569,8 @@ typedef struct {
  * so that y * scales is the normed row; which number is nearest is decided
  * exactly, whatever the order of sums.  Rows of zeros are zeros, with a scale
  * of 0; rows that hold an infinity or NaN (or whose h * weight passes the range
- * of floats) are zeros with a scale of NaN.  Sums are fp32, y is rounded once.
+ * of floats) are zeros with a scale of NaN.  Sums are fp32 (where the squares
+ * pass its range, y and the scale are 0), y is rounded once.
  * residual_out may be x or residual, and y (without scales) may be x or
  * residual where residual_out is not, each with the same stride; other overlaps
  * are not allowed.  The pointers need the alignment of their elements only; rows that

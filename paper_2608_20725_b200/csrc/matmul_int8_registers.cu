@@ -9,6 +9,8 @@
 // Up to 8 rows of x would leave most of a tile without work: a warp then has two rows of the matrix, a lane every 32nd 16 bytes of them, which meet
 // all rows of x, staged in shared memory, by products of four bytes (dp4a); the lanes' sums are added at the end.  (5 rows x 4001 x 8001: 31 us; of
 // 16 rows, 48, it is slower than the tiles.)
+#include <algorithm>
+
 #include "common.cuh"
 #include "ptx_sm100.cuh"
 #include "sequence.cuh"
@@ -164,7 +166,6 @@ template <typename T>
 cudaError_t launch_tiles(const Int8Args& a, const Bytes& x, const Bytes& weight, cudaStream_t stream) {
   auto tiles = [&](int64_t size, int64_t tile) { return (size + tile - 1) / tile; };
   const im2win_int8_shape& s = a.shape;
-  if (tiles(s.M, 64) > 65535) return cudaErrorInvalidConfiguration;
   if (tiles(s.M, 128) * tiles(s.N, 128) >= 296) {
     matmul_int8_kernel<T, 128><<<dim3((unsigned)tiles(s.N, 128), (unsigned)tiles(s.M, 128)), 256, 0, stream>>>(a, x, weight, 1);
     return cudaGetLastError();
@@ -242,6 +243,19 @@ cudaError_t launch_few(const Int8Args& a, const Bytes& x, const Bytes& weight, c
 }  // namespace
 
 cudaError_t launch_matmul_int8_registers(const Int8Args& a, cudaStream_t stream) {
+  constexpr int32_t kMostRows = 65535 * 64;                    // of a grid
+  if (a.shape.M > kMostRows) {
+    for (int64_t m = 0; m < a.shape.M; m += kMostRows) {
+      Int8Args part = a;
+      part.x += m * a.shape.x_stride;
+      part.x_scales += m;
+      part.y = static_cast<uint8_t*>(a.y) + m * a.shape.y_stride * (int64_t)element_bytes(a.dtype);
+      part.shape.M = (int32_t)std::min<int64_t>(a.shape.M - m, kMostRows);
+      const cudaError_t e = launch_matmul_int8_registers(part, stream);
+      if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+  }
   const im2win_int8_shape& s = a.shape;
   const Bytes x = {a.x, s.x_stride, (int64_t)(s.M - 1) * s.x_stride + s.K, s.M, s.K};
   const Bytes weight = {a.weight, s.K, (int64_t)s.N * s.K, s.N, s.K};

@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
     return;
   } else {
     const bool fine = top <= FLT_MAX;                            // (not of a NaN)
-    if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7fffffff) : top * rate / 127.0f;
+    if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7fffffff) : top == 0.0f ? 0.0f : top * rate / 127.0f;    // (0 times infinity: eps of 0)
     // fp32: the largest product in 64 bits, and all below 2^-90: products that fp32 does not hold exactly
     const bool in_64 = sizeof(T) == 4 || top < 8e-28f;
     double exact_top = top;

@@ -147,3 +147,13 @@ def test_gives_up_and_says_so(m, n, drop, monkeypatch):
     again = torch.zeros_like(y)
     binding.im2win_matmul_int8(x, xs, w, ws, again)
     assert not bool(((again.double() - want).abs() > 4 * 2.0 ** -24 * want.abs()).any())
+
+
+def test_more_rows_than_a_grid_has():
+    """Rows that start anywhere, more than 65535 tiles of 64."""
+    m = 65535 * 64 + 100
+    x, w = torch.randint(-127, 128, (m, 3), device="cuda", dtype=torch.int8), torch.randint(-127, 128, (9, 3), device="cuda", dtype=torch.int8)
+    xs, ws, y = torch.rand(m, device="cuda"), torch.rand(9, device="cuda"), torch.zeros(m, 9, device="cuda")
+    binding.im2win_matmul_int8(x, xs, w, ws, y)
+    want = x.double() @ w.double().T * xs.double()[:, None] * ws.double()
+    assert not bool(((y.double() - want).abs() > 3 * 2.0 ** -24 * want.abs()).any())

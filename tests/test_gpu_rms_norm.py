@@ -191,3 +191,18 @@ def test_rows_beyond_32_bits():
     assert torch.equal(y[-3:].cpu().double(), q)
     close(scales[-3:], want, OFF * want, "scales")
     assert not y[:-3].any() and not scales[:-3].any()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_zeros_without_eps_and_squares_beyond_the_range(dtype):
+    """A row of zeros and eps of 0 has a scale of 0; rows whose squares pass fp32 come out as 0."""
+    x = torch.zeros(2, 100, dtype=DTYPES[dtype], device="cuda")
+    if dtype != "f16":
+        x[1] = 1e25
+    y, scales = torch.full((2, 100), 5, dtype=torch.int8, device="cuda"), torch.full((2,), 5.0, device="cuda")
+    binding.im2win_rms_norm(x, None, y, scales=scales, eps=0.0)
+    assert not y[0].any() and not scales.any()
+    if dtype != "f16":
+        out = torch.ones_like(x)
+        binding.im2win_rms_norm(x, None, out)
+        assert not out.any()
