@@ -17,14 +17,14 @@
 // a power of two first, so that what a piece leaves off is below 2^-39 of its row's largest element, whatever the type's range.  k and q
 // of 16 bits are one piece, of fp32 two; S, R and U are two pieces (S k, U k: two products a term; T R: three); T is inverted in blocks of
 // 16 x 16, those on the diagonal by substitution in fp32, the others by TF32 products in two pieces (21 bits).  For o of bf16 S, P and U are
-// rounded to fp16 once, which is finer than o's own rounding, of fp16 P alone; of fp32 they are all two pieces.  Against 64 bits the states of 600 tokens are off
+// rounded to fp16 once, which is finer than o's own rounding; of fp16 and fp32 they are two pieces.  Against 64 bits the states of 600 tokens are off
 // by 1.5e-7 of their norm.
 //
-// What bounds it (128 x 128, fp16): a chunk of 64 tokens takes a block of 32 columns 6.5 us, of 64 columns 7.7; its chains alone 3.4 and 5.1, a team alone
-// 10.3.  Both are some 4000 instructions a warp, one after the other at about five cycles each (what the products, 8 cycles of an SM's quarter each, take is
+// What bounds it (128 x 128, fp16): a chunk of 64 tokens takes a block of 32 columns 6.3 us (bf16), of 64 columns 7.4 (fp16); its chains alone 3.4 and
+// 5.1, a team alone, with every second chunk, about 10.  Both are some 4000 instructions a warp, one after the other at about five cycles each (what the products, 8 cycles of an SM's quarter each, take is
 // 2 us of the chain's).  The instruction cache is part of it: the code of a chunk, 80 KB of which each warp runs its own part, misses it 450 times a
-// chunk, which is why the helpers' code exists once and in loops.  One prompt of 16384 tokens, 32 heads of 128 x 128, bf16: 1643 us (62 at 6.56 TB/s); token
-// by token 22200.  13 prompts of 9001 tokens, 24 heads of 64 x 128, fp16: 344 (22), token by token 4090.
+// chunk, which is why the helpers' code exists once and in loops.  One prompt of 16384 tokens, 32 heads of 128 x 128, bf16: 1610 us (62 at 6.56 TB/s), fp16
+// 1887; token by token 22200.  13 prompts of 9001 tokens, 24 heads of 64 x 128, fp16: 353 (22), token by token 4090.
 //
 // Infinities and NaNs: a token whose k, beta or decay is not finite, and those behind it, get a beta of 0, a weight of NaN for o and a
 // decay of NaN for S.  A column whose R or U is not finite from some token on is cleaned from there on, before it meets the zeros of T and P, and its
@@ -93,12 +93,13 @@ struct Layout {
   static constexpr uint32_t kRows = kChunk * DK * 2;           // a piece of k or q
   static constexpr uint32_t kTriangle = 10 * 512;              // a piece of T or P: their 16 x 16 blocks up to the diagonal, by rows of blocks
   static constexpr uint32_t kQAt = kPieces * kRows, kTAt = 2 * kPieces * kRows, kPAt = kTAt + 2 * kTriangle;
-  static constexpr uint32_t kWeightsAt = kPAt + kPieces * kTriangle;
+  // fp16: S, P and U are two pieces for o too (with all three rounded once it was off by 1.7 times its own rounding, with P alone by up to 1.6)
+  static constexpr bool kTwo = std::is_same<T, __half>::value;
+  static constexpr int kOfP = kPieces == 2 || kTwo ? 2 : 1;    // pieces of P
+  static constexpr uint32_t kWeightsAt = kPAt + kOfP * kTriangle;
   static constexpr uint32_t kStage = (kWeightsAt + sizeof(Weights) + 127) / 128 * 128;
   static constexpr uint32_t kScratchAt = kSlots * kStage, kScratch = (sizeof(Scratch) + 127) / 128 * 128;
   static constexpr uint32_t kColumnsAt = kScratchAt + TEAMS * kScratch;
-  // fp16: o from two pieces of S and of U, so that P alone is rounded for it (with all three rounded once o was off by 1.7 times its own rounding)
-  static constexpr bool kTwo = std::is_same<T, __half>::value;
   // of a warp with columns: two chunks of v (16 bits), where o leaves through too; then, where another warp makes o, what it needs: S and U as operands,
   // three pairs a lane
   static constexpr uint32_t kV = sizeof(T) == 2 ? kChunk * 32 : 0;
@@ -547,7 +548,7 @@ struct Helpers {
         split(x[2 * h] * scale[h], x[2 * h + 1] * scale[h], hi, lo);
         uint8_t* at = to + triangle_at(m, n >> 1, (lane >> 2) + 8 * h, n & 1) + pair * 2;
         *reinterpret_cast<uint32_t*>(at) = hi;
-        if (L::kPieces == 2) *reinterpret_cast<uint32_t*>(at + L::kTriangle) = lo;
+        if (L::kOfP == 2) *reinterpret_cast<uint32_t*>(at + L::kTriangle) = lo;
       }
     };
 #pragma unroll
@@ -598,9 +599,9 @@ struct Helpers {
 
   // 16 columns J of T below the diagonal block: T_iJ = -T_ii sum_k A_ik T_kJ, i downward; kept in s.A above the diagonal, transposed.  All are transposed, so
   // that what one product gives is the next one's left operand.  By TF32 instructions, whose exponents need no scales: operands in two pieces,
-  // three products a term; of eight columns of the left operand the even ones are taken for the first four.  Then all of the columns, scaled, to `to`.
-  __device__ __forceinline__ void columns_of_t(int J, uint32_t to, Weights& w) const {
-    const int mi = lane >> 3, r8 = lane & 7, g = lane >> 2, pair = (lane & 3) * 2;
+  // three products a term; of eight columns of the left operand the even ones are taken for the first four.
+  __device__ __forceinline__ void columns_of_t(int J) const {
+    const int g = lane >> 2, pair = (lane & 3) * 2;
     float x[2][4], top = 0.0f;
     // block (i, J), transposed: rows are columns of T
     auto block = [&](int i) {
@@ -671,15 +672,22 @@ struct Helpers {
     }
     const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
     if (lane == 0) atomicMax(&s.top_t, most);
-    sync();
+  }
+  // These columns of T, scaled by its largest element, in pieces.
+  __device__ __forceinline__ void store_t(int J, uint32_t to, Weights& w) const {
+    const int mi = lane >> 3, r8 = lane & 7, g = lane >> 2, pair = (lane & 3) * 2;
     const float scale = scale_for(__uint_as_float(*(volatile uint32_t*)&s.top_t));
     if (J == 0 && lane == 0) w.of_t = unscale_for(scale);
 #pragma unroll 1
     for (int i = J; i < 4; ++i) {
+      const float* from = i == J ? &s.A[J * 16 + pair][J * 16 + g] : &s.A[J * 16 + g][i * 16 + pair];
+      const int along = i == J ? kAPitch : 1, across = i == J ? 1 : kAPitch;
       uint32_t h[4], l[4];
-      block(i);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) split(x[u >> 1][2 * (u & 1)] * scale, x[u >> 1][2 * (u & 1) + 1] * scale, h[u], l[u]);
+      for (int u = 0; u < 4; ++u) {
+        const float* two = from + (u >> 1) * 8 * along + (u & 1) * 8 * across;
+        split(two[0] * scale, two[along] * scale, h[u], l[u]);
+      }
       const uint32_t at = to + triangle_at(i, J, (mi >> 1) * 8 + r8, mi & 1);
       stmatrix_trans(at, h);
       stmatrix_trans(at + L::kTriangle, l);
@@ -706,22 +714,24 @@ struct Helpers {
       weights_of_q(w, kept);
     }
     fetch(first + TEAMS * kChunk, end);
+    // (A warp has row tile `warp` of A and of P, and column tile `warp` of T: what is long of the ones is short of the other.)
 #pragma unroll 1
     for (int of_q = 0; of_q < 2; ++of_q) {
-      const int m = of_q ? 3 - warp : warp;
       Square acc;
-      square(of_q ? qt : kt, kt, m, acc);
+      square(of_q ? qt : kt, kt, warp, acc);
       if (!of_q) sync();                                       // (the weights)
-      weigh(m, acc, of_q ? s.of_p : s.of_a, of_q);
+      weigh(warp, acc, of_q ? s.of_p : s.of_a, of_q);
       if (of_q) {
-        store_p(m, acc, generic + stage + L::kPAt, w.of_p);
+        store_p(warp, acc, generic + stage + L::kPAt, w.of_p);
       } else {
-        store_a(m, acc);
-        invert_block(m);
+        store_a(warp, acc);
+        invert_block(warp);
+        sync();
+        columns_of_t(warp);
       }
     }
     sync();
-    columns_of_t(warp, kt + L::kTAt, w);
+    store_t(warp, kt + L::kTAt, w);
     if (warp == 3) total(w, min(end - first, kChunk));
   }
 };
@@ -896,7 +906,7 @@ struct Columns {
           if (kLow) mma(I[2 * i + h], lo, b[2 * h], b[2 * h + 1]);
           mma(I[2 * i + h], hi, b[2 * h], b[2 * h + 1]);
         }
-        if (kFull) {
+        if (L::kOfP == 2) {
           ldmatrix(at + L::kTriangle, b);
 #pragma unroll
           for (int h = 0; h < 2; ++h) mma(I[2 * i + h], hi, b[2 * h], b[2 * h + 1]);
@@ -1334,17 +1344,21 @@ cudaError_t launch(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
 }
 
 // The columns of a block: 32 while that gives no more blocks than there are SMs, 64 beyond.  (A chunk of 64 tokens, 128 x 128, takes a block of 32 columns
-// 6.5 us, of 64 columns 7.7.  One prompt of 16384 tokens, 32 heads, 1643 and 1960 us; four of 8192 tokens in all 849 and 583; 128 columns and one team
-// 1136.)  fp32: its pieces leave shared memory for one team, and registers for o beside the chain.
+// 6.3 us, of 64 columns 7.4.  Before the helpers' last step, bf16: one prompt of 16384 tokens, 32 heads, 1643 and 1960 us; four of 8192 tokens in all 849
+// and 583; 128 columns and one team 1136.)  fp32: its pieces leave shared memory for one team, and registers for o beside the chain.
 template <typename T, int DK>
 cudaError_t launch_width(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
   const bool wide = p.dv > 32 && (int64_t)sequences * p.heads * ((p.dv + 31) / 32) > 148;
-  if constexpr (sizeof(T) == 2) {
-    if (wide) return launch<T, DK, Shape<4, false, 2, 232, 136>>(p, sequences, stream);
-    return launch<T, DK, Shape<2, true, 2, 208, 144>>(p, sequences, stream);
-  } else {
+  if constexpr (sizeof(T) == 4) {
     if (wide) return launch<T, DK, Shape<4, false, 1, 0, 0>>(p, sequences, stream);
     return launch<T, DK, Shape<2, false, 1, 0, 0>>(p, sequences, stream);
+  } else {
+    // (fp16, dk above 64: S in two pieces for the warps that make o does not fit beside P's two; registers do it, at 64 columns.  That prompt takes 1887 us;
+    // 32 columns with o made in the chain's warps, whose registers then spill, 1946 against 1932 before that step)
+    if constexpr (!(Layout<T, DK, 2>::kTwo && DK > 64)) {
+      if (!wide) return launch<T, DK, Shape<2, true, 2, 208, 144>>(p, sequences, stream);
+    }
+    return launch<T, DK, Shape<4, false, 2, 232, 136>>(p, sequences, stream);
   }
 }
 
