@@ -531,13 +531,21 @@ typedef struct {
  * floats, for each token and head or each head (normally 0 to 1).  There is no
  * workspace.  log_decay is normally <= 0 (-infinity empties the state; those
  * above 0 may add up to 70 over 64 tokens in a row).  A max_len below the
- * longest sequence's rows changes which way the call is run, not its results.
+ * longest sequence's rows changes which way the call is run, not its results
+ * beyond the rounding of sums.
  *
- * Sums and states are fp32.  An infinity or NaN in a column of v, or of a
- * state, makes that column of o from its row on, and of the state, infinities
- * or NaNs (which of them is not defined); one of k, beta or log_decay (but
- * -infinity) all of the head's, one of q its row of o.  It reaches no row
- * before it.  The order of sums is fixed by the shape.
+ * Sums and states are fp32, and what a token makes takes no bits from those
+ * before it, whatever its size.  Prompts (more than 16 rows, dk of at most 128)
+ * go by chunks of 64 tokens: there decays that add up to less than 2^-126 leave
+ * nothing, numbers below 2^-110 lose bits, and where a token's part in a later
+ * one of the chunk passes the range of floats (without normalize, beta |k|^2
+ * above 2 lets it grow), rows from up to 15 before that one on are NaN.
+ *
+ * An infinity or NaN in a column of v, or of a state, makes that column of o
+ * from its row on, and of the state, infinities or NaNs (which of them is not
+ * defined); one of k, beta or log_decay (but -infinity) all of the head's, one
+ * of q its row of o.  It reaches no row before it.  The order of sums is fixed
+ * by the shape.
  */
 im2win_status im2win_gated_delta_rule(const void* q, const void* k, const void* v, const float* log_decay, const float* beta,
                                       void* o, const float* state_in, float* state_out, const im2win_sequences* seqs,

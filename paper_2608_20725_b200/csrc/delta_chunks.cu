@@ -13,12 +13,14 @@
 // and the split below, which is made of S, R and U in every chunk, costs the same issue slots.)  Four more warps, a team, make k, q, T, P
 // and the weights of a chunk ahead; of 16-bit rows there are two teams, each with every second chunk.
 //
-// The state is fp32 and stays so: operands are split into two fp16 pieces, 22 bits.  Every row of an operand is brought to below 2^15 by
-// a power of two first, so that what a piece leaves off is below 2^-39 of its row's largest element, whatever the type's range.  k and q
-// of 16 bits are one piece, of fp32 two; S, R and U are two pieces (S k, U k: two products a term; T R: three); T is inverted in blocks of
-// 16 x 16, those on the diagonal by substitution in fp32, the others by TF32 products in two pieces (21 bits).  For o of bf16 S, P and U are
-// rounded to fp16 once, which is finer than o's own rounding; of fp16 and fp32 they are two pieces.  Against 64 bits the states of 600 tokens are off
-// by 1.5e-7 of their norm.
+// The state is fp32 and stays so.  The products with k and q, and the one that adds to S, are of two fp16 pieces, 22 bits: every row of an operand is
+// brought to below 2^15 by a power of two first, so that what a piece leaves off is below 2^-39 of its row's largest element, whatever the type's range.
+// That suits rows along dk, which are summed up anyway, and what all tokens of a chunk add to S.  R, U, T and P are another matter: tokens meet only
+// those before them, which may be smaller by any factor, so that a scale for all of them would take their bits.  T R and P U are products of TF32
+// pieces (11 and 11 bits), which have fp32's exponents.  k and q of 16 bits are one piece, of fp32 two; S, R and U are two pieces (S k, U k: two products a
+// term; T R: three); T is inverted in blocks of 16 x 16, those on the diagonal by substitution in fp32, the others by TF32 products too.  For o
+// of bf16 S, P and U are rounded to 11 bits once, which is finer than o's own rounding; of fp16 and fp32 they are two pieces.  Against 64 bits the states
+// of 600 tokens are off by 2.3e-7 of their norm (of fp32 rows by 3.3e-7, and o by 7e-7; token by token both are 2e-7).
 //
 // What bounds it (128 x 128, fp16): a chunk of 64 tokens takes a block of 32 columns 6.3 us (bf16), of 64 columns 7.4 (fp16); its chains alone 3.4 and
 // 5.1, a team alone, with every second chunk, about 10.  Both are some 4000 instructions a warp, one after the other at about five cycles each (what the products, 8 cycles of an SM's quarter each, take is
@@ -67,20 +69,17 @@ struct alignas(16) Weights {
   float of_v[kChunk];                    // beta
   float to_end[kChunk];                  // exp(G_n - G_j), without the scale of k
   float of_q[kChunk];                    // scale exp(G_i) of q S, without the scale of q
-  float of_p[kChunk];                    // undoes P's scale of a row
   float total, total_rest;               // exp(G_n) in two parts
-  float of_t;                            // undoes T's scale
-  float pad;
+  float pad[2];
 };
 
-constexpr int kAPitch = 72;              // floats: 8 rows of 4 pairs lie on all banks
+constexpr int kBlock = 256;              // floats of a 16 x 16 block
 struct Scratch {
-  float A[kChunk][kAPitch];              // as far as to the diagonal's 16 x 16 blocks, and those inverted
+  float A[6 * kBlock];                   // its blocks left of the diagonal, by rows of blocks
   float k_row[kChunk], q_row[kChunk];    // what k and q in pieces are multiplied by
   int whole[kChunk];                     // G_i in powers of two: its floor; the rest is in the factors of A's and P's rows and columns
   float of_a[kChunk], of_p[kChunk], of_column[kChunk];
   uint32_t bad_k[kChunk / 32], bad_q[kChunk / 32];             // rows that are not finite
-  uint32_t top_t;                        // T's largest element
   int broken;                            // the first token from which nothing is finite any more
   int64_t all;                           // G_n
 };
@@ -91,19 +90,18 @@ struct Layout {
   static constexpr int kPieces = sizeof(T) == 4 ? 2 : 1;
   static constexpr int kSlots = TEAMS + 1;                     // chunks that are ready or being made
   static constexpr uint32_t kRows = kChunk * DK * 2;           // a piece of k or q
-  static constexpr uint32_t kTriangle = 10 * 512;              // a piece of T or P: their 16 x 16 blocks up to the diagonal, by rows of blocks
-  static constexpr uint32_t kQAt = kPieces * kRows, kTAt = 2 * kPieces * kRows, kPAt = kTAt + 2 * kTriangle;
+  static constexpr uint32_t kTriangle = 10 * kBlock * 4;       // T or P: their 16 x 16 blocks up to the diagonal, by rows of blocks
+  static constexpr uint32_t kQAt = kPieces * kRows, kTAt = 2 * kPieces * kRows, kPAt = kTAt + kTriangle;
   // fp16: S, P and U are two pieces for o too (with all three rounded once it was off by 1.7 times its own rounding, with P alone by up to 1.6)
-  static constexpr bool kTwo = std::is_same<T, __half>::value;
-  static constexpr int kOfP = kPieces == 2 || kTwo ? 2 : 1;    // pieces of P
-  static constexpr uint32_t kWeightsAt = kPAt + kOfP * kTriangle;
+  static constexpr bool kTwo = std::is_same<T, __half>::value, kTwoOfP = kPieces == 2 || kTwo;
+  static constexpr uint32_t kWeightsAt = kPAt + kTriangle;
   static constexpr uint32_t kStage = (kWeightsAt + sizeof(Weights) + 127) / 128 * 128;
   static constexpr uint32_t kScratchAt = kSlots * kStage, kScratch = (sizeof(Scratch) + 127) / 128 * 128;
   static constexpr uint32_t kColumnsAt = kScratchAt + TEAMS * kScratch;
-  // of a warp with columns: two chunks of v (16 bits), where o leaves through too; then, where another warp makes o, what it needs: S and U as operands,
+  // of a warp with columns: two chunks of v (16 bits), where o leaves through too; then, where another warp makes o, what it needs: S as operands, U,
   // three pairs a lane
   static constexpr uint32_t kV = sizeof(T) == 2 ? kChunk * 32 : 0;
-  static constexpr uint32_t kSAt = 2 * kV, kUAt = kSAt + DK / 16 * 512 * (1 + kTwo), kPairsAt = kUAt + 4 * 512 * (1 + kTwo);
+  static constexpr uint32_t kSAt = 2 * kV, kUAt = kSAt + DK / 16 * 512 * (1 + kTwo), kPairsAt = kUAt + 8 * 512;
   template <bool SPLIT> static constexpr uint32_t kColumns = SPLIT ? kPairsAt + 3 * 256 : 2 * kV;
 };
 
@@ -118,6 +116,8 @@ __device__ __forceinline__ float scale_for(float top) {
   return __uint_as_float((uint32_t)min(max(268 - e, 1), 253) << 23);
 }
 __device__ __forceinline__ float unscale_for(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }
+// The same for an operand in TF32 pieces, which have fp32's exponents: only where the smaller piece would fall below fp32's range, or rounding pass it.
+__device__ __forceinline__ float scale_for_tf32(float top) { return top < 0x1p-40f ? scale_for(top) : top > 0x1p120f ? 0x1p-8f : 1.0f; }
 
 // 2^x of x in -1..1.
 __device__ __forceinline__ float exp2_fraction(float x) {
@@ -149,10 +149,30 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], 
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// x rounded to 11 bits, and the rest (of which the instruction takes 11).
-__device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
-  lo = __float_as_uint(x - __uint_as_float(hi));
+// x rounded to 24 - BITS bits, away from 0 in the middle (a NaN stays one: as a whole number it may not).
+template <int BITS>
+__device__ __forceinline__ float rounded(float x) {
+  return fmaf(x, 0.0f, __uint_as_float((__float_as_uint(x) + (1u << (BITS - 1))) & ~((1u << BITS) - 1u)));
+}
+// Left operand from a tile of accumulators (rows g and g + 8, columns along its tokens), scaled, in pieces: rounded to 11 bits, and the rest, of which
+// the instruction takes 11.  (By whole numbers: the conversion instruction takes its time, one prompt of 16384 tokens 1706 instead of 1634 us.)  Of its eight
+// columns the even ones are taken for the first four, and so are the rows of right_tf32.
+__device__ __forceinline__ void left_tf32(const float (&x)[4], const float (&scale)[2], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float y = x[e] * scale[e >> 1];
+    const int to = (e & 1) * 2 + (e >> 1);
+    hi[to] = (__float_as_uint(y) + 0x1000u) & 0xffffe000u;
+    lo[to] = __float_as_uint(y - __uint_as_float(hi[to]));
+  }
+}
+// Right operand, of two numbers that are rounded to 22 bits: the first 11 of them, and the others.
+__device__ __forceinline__ void right_tf32(const float* two, uint32_t (&hi)[2], uint32_t (&lo)[2]) {
+  const float2 b = *reinterpret_cast<const float2*>(two);
+  hi[0] = __float_as_uint(b.x) & 0xffffe000u;
+  hi[1] = __float_as_uint(b.y) & 0xffffe000u;
+  lo[0] = __float_as_uint(b.x - __uint_as_float(hi[0]));
+  lo[1] = __float_as_uint(b.y - __uint_as_float(hi[1]));
 }
 __device__ __forceinline__ void ldmatrix(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -174,10 +194,11 @@ __device__ __forceinline__ uint32_t unit_at(int r, int unit) {
   return (uint32_t)(r * N * 2 + ((unit ^ (r & 7)) << 4));
 }
 
-// Byte of half a row (16 bytes) r of block (i, k) of a triangle, the halves of every second four rows swapped.
-__device__ __forceinline__ uint32_t triangle_at(int i, int k, int r, int half) {
-  return (uint32_t)((i * (i + 1) / 2 + k) * 512 + r * 32 + ((half ^ (r >> 2 & 1)) << 4));
-}
+// Block (i, k) of a triangle of 16 x 16 blocks with its diagonal, and without it; in a block, float (r, c), the halves of every second two rows
+// swapped: eight rows of four pairs, as the matrix instructions take them, have no conflicts.
+__host__ __device__ constexpr int block_at(int i, int k) { return (i * (i + 1) / 2 + k) * kBlock; }
+__host__ __device__ constexpr int left_block_at(int i, int k) { return (i * (i - 1) / 2 + k) * kBlock; }
+__host__ __device__ constexpr int float_at(int r, int c) { return r * 16 + (c ^ ((r & 2) << 2)); }
 
 // ------------------------------------------------------------------------------------------------ the helpers
 
@@ -420,7 +441,6 @@ struct Helpers {
       w.to_end[at] = power(all - G[i]) * k_row;
     }
     if (lane == 0) {
-      s.top_t = 0;
       s.broken = broken;
       s.all = all;
     }
@@ -431,7 +451,7 @@ struct Helpers {
       const int at = 2 * lane + i;
       const float q_row = s.q_row[at];
       const bool bad_q = (s.bad_q[lane >> 4] >> (at & 31) & 1u) != 0;
-      s.of_p[at] = p.scale * q_row * kept.part[i];
+      s.of_p[at] = q_row * kept.part[i];
       w.of_q[at] = at >= kept.broken || bad_q ? __builtin_nanf("") : p.scale * kept.from_start[i] * q_row;
     }
   }
@@ -518,73 +538,38 @@ struct Helpers {
       }
     }
   }
-  // in pieces, rows scaled
-  __device__ __forceinline__ void store_p(int m, const Square& acc, uint8_t* to, float* unscale) const {
-    const int i0 = m * 16 + (lane >> 2), pair = (lane & 3) * 2;
-    float top[2], scale[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      top[h] = 0.0f;
-#pragma unroll
-      for (int n = 0; n < 2; ++n) top[h] = fmaxf(top[h], fmaxf(fabsf(acc.diagonal[n][2 * h]), fabsf(acc.diagonal[n][2 * h + 1])));
-    }
-#pragma unroll
-    for (int n = 0; n < 6; ++n) {
-      if (n >= 2 * m) break;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) top[h] = fmaxf(top[h], fmaxf(fabsf(acc.left[n][2 * h]), fabsf(acc.left[n][2 * h + 1])));
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
-      top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
-      scale[h] = scale_for(top[h]);
-      if ((lane & 3) == 0) unscale[i0 + 8 * h] = unscale_for(scale[h]);
-    }
-    auto store = [&](const float (&x)[4], int n) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t hi, lo;
-        split(x[2 * h] * scale[h], x[2 * h + 1] * scale[h], hi, lo);
-        uint8_t* at = to + triangle_at(m, n >> 1, (lane >> 2) + 8 * h, n & 1) + pair * 2;
-        *reinterpret_cast<uint32_t*>(at) = hi;
-        if (L::kOfP == 2) *reinterpret_cast<uint32_t*>(at + L::kTriangle) = lo;
-      }
+  // Rows of blocks m of A (the diagonal's block as it is, into T's place) and of P, rounded to what their products take.
+  template <int BITS, int OF_DIAGONAL>
+  __device__ __forceinline__ void store(int m, const Square& acc, float* left, float* diagonal) const {
+    const int at = float_at(lane >> 2, (lane & 3) * 2);
+    auto put = [&](float* to, float a, float b, float c, float d) {
+      *reinterpret_cast<float2*>(to) = make_float2(a, b);
+      *reinterpret_cast<float2*>(to + 8 * 16) = make_float2(c, d);
     };
 #pragma unroll
-    for (int n = 0; n < 2; ++n) store(acc.diagonal[n], 2 * m + n);
+    for (int n = 0; n < 2; ++n) {
+      const float(&x)[4] = acc.diagonal[n];
+      if constexpr (OF_DIAGONAL == 0) put(diagonal + (at ^ (n * 8)), x[0], x[1], x[2], x[3]);
+      else put(diagonal + (at ^ (n * 8)), rounded<BITS>(x[0]), rounded<BITS>(x[1]), rounded<BITS>(x[2]), rounded<BITS>(x[3]));
+    }
 #pragma unroll
     for (int n = 0; n < 6; ++n) {
       if (n >= 2 * m) break;
-      store(acc.left[n], n);
+      const float(&x)[4] = acc.left[n];
+      put(left + (n >> 1) * kBlock + (at ^ ((n & 1) * 8)), rounded<BITS>(x[0]), rounded<BITS>(x[1]), rounded<BITS>(x[2]), rounded<BITS>(x[3]));
     }
   }
-  __device__ __forceinline__ void store_a(int m, const Square& acc) const {
-    float* to = &s.A[m * 16 + (lane >> 2)][(lane & 3) * 2];
-    auto store = [&](const float (&x)[4], int n) {
-      *reinterpret_cast<float2*>(to + n * 8) = make_float2(x[0], x[1]);
-      *reinterpret_cast<float2*>(to + 8 * kAPitch + n * 8) = make_float2(x[2], x[3]);
-    };
-#pragma unroll
-    for (int n = 0; n < 2; ++n) store(acc.diagonal[n], 2 * m + n);
-#pragma unroll
-    for (int n = 0; n < 6; ++n) {
-      if (n >= 2 * m) break;
-      store(acc.left[n], n);
-    }
-    __syncwarp();
-  }
-  // The inverse of A's diagonal block m and 1, in its place: by substitution, a column a lane.
-  __device__ __forceinline__ void invert_block(int m) const {
-    float* d = &s.A[m * 16][m * 16];
+  // The inverse of 1 and a diagonal block of A, in its place: by substitution, a column a lane.
+  __device__ __forceinline__ void invert_block(float* d) const {
     const int j = lane & 15;                                   // (both halves of the warp do the same)
     float x[16];
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       float sum[2] = {i == j ? 1.0f : 0.0f, 0.0f};
 #pragma unroll
       for (int k = 0; k < i; k += 4) {
-        const float4 a = *reinterpret_cast<const float4*>(d + i * kAPitch + k);
+        const float4 a = *reinterpret_cast<const float4*>(d + float_at(i, k));
         sum[0] = fmaf(-a.x, x[k], sum[0]);
         if (k + 1 < i) sum[1] = fmaf(-a.y, x[k + 1], sum[1]);
         if (k + 2 < i) sum[0] = fmaf(-a.z, x[k + 2], sum[0]);
@@ -594,39 +579,26 @@ struct Helpers {
     }
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) d[i * kAPitch + j] = x[i];
+    for (int i = 0; i < 16; ++i) d[float_at(i, j)] = rounded<2>(x[i]);
   }
 
-  // 16 columns J of T below the diagonal block: T_iJ = -T_ii sum_k A_ik T_kJ, i downward; kept in s.A above the diagonal, transposed.  All are transposed, so
-  // that what one product gives is the next one's left operand.  By TF32 instructions, whose exponents need no scales: operands in two pieces,
-  // three products a term; of eight columns of the left operand the even ones are taken for the first four.
-  __device__ __forceinline__ void columns_of_t(int J) const {
-    const int g = lane >> 2, pair = (lane & 3) * 2;
-    float x[2][4], top = 0.0f;
-    // block (i, J), transposed: rows are columns of T
-    auto block = [&](int i) {
-      const float* at = i == J ? &s.A[J * 16 + pair][J * 16 + g] : &s.A[J * 16 + g][i * 16 + pair];
-      const int along = i == J ? kAPitch : 1, across = i == J ? 1 : kAPitch;
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = at[(n * 8 + (e & 1)) * along + (e >> 1) * 8 * across];
-    };
-    auto raise = [&]() {
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[n][e]));
-    };
-    block(J);
-    raise();
+  // 16 columns J of T below the diagonal block: T_iJ = -T_ii sum_k A_ik T_kJ, i downward.  They are worked on transposed, so that what one product
+  // gives is the next one's left operand.  By TF32 instructions, whose exponents need no scales: operands in two pieces, three products a term.
+  __device__ __forceinline__ void columns_of_t(int J, float* T_blocks) const {
+    const int g = lane >> 2, pair = (lane & 3) * 2, right = float_at(g, pair), turned = pair * 16 + (g ^ ((pair & 2) << 2));
+    const float one[2] = {1.0f, 1.0f};
+    float x[2][4];
 #pragma unroll 1
     for (int i = J + 1; i < 4; ++i) {
       float d[2][4], small[2][2][4];
 #pragma unroll 1
       for (int k = J; k <= i; ++k) {                           // (the last step: T_ii times the sum of the others)
         if (k < i) {
-          block(k);
+          const float* at = T_blocks + block_at(k, J);         // rows of x are columns of T
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[n][e] = at[(turned ^ ((e >> 1) * 8)) + (n * 8 + (e & 1)) * 16];
         } else {
 #pragma unroll
           for (int n = 0; n < 2; ++n)
@@ -639,18 +611,13 @@ struct Helpers {
 #pragma unroll
             for (int e = 0; e < 4; ++e) d[n][e] = small[0][n][e] = small[1][n][e] = 0.0f;
         }
-        const float* from = &s.A[i * 16 + g][k * 16 + pair];
+        const float* from = k < i ? s.A + left_block_at(i, k) : T_blocks + block_at(i, i);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
           uint32_t ah[4], al[4], bh[2][2], bl[2][2];
+          left_tf32(x[ks], one, ah, al);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) split_tf32(x[ks][e], ah[(e & 1) * 2 + (e >> 1)], al[(e & 1) * 2 + (e >> 1)]);
-#pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const float2 b = *reinterpret_cast<const float2*>(from + n * 8 * kAPitch + ks * 8);
-            split_tf32(b.x, bh[n][0], bl[n][0]);
-            split_tf32(b.y, bh[n][1], bl[n][1]);
-          }
+          for (int n = 0; n < 2; ++n) right_tf32(from + n * 8 * 16 + (right ^ (ks * 8)), bh[n], bl[n]);
 #pragma unroll
           for (int n = 0; n < 2; ++n) mma_tf32(d[n], ah, bh[n][0], bh[n][1]);
 #pragma unroll
@@ -659,38 +626,12 @@ struct Helpers {
           for (int n = 0; n < 2; ++n) mma_tf32(small[1][n], ah, bl[n][0], bl[n][1]);
         }
       }
-      __syncwarp();
+      float* to = T_blocks + block_at(i, J);
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[n][e] = d[n][e] + (small[0][n][e] + small[1][n][e]);
-          s.A[J * 16 + g + 8 * (e >> 1)][i * 16 + n * 8 + pair + (e & 1)] = x[n][e];
-        }
-      raise();
+        for (int e = 0; e < 4; ++e) to[(turned ^ ((e >> 1) * 8)) + (n * 8 + (e & 1)) * 16] = rounded<2>(d[n][e] + (small[0][n][e] + small[1][n][e]));
       __syncwarp();
-    }
-    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
-    if (lane == 0) atomicMax(&s.top_t, most);
-  }
-  // These columns of T, scaled by its largest element, in pieces.
-  __device__ __forceinline__ void store_t(int J, uint32_t to, Weights& w) const {
-    const int mi = lane >> 3, r8 = lane & 7, g = lane >> 2, pair = (lane & 3) * 2;
-    const float scale = scale_for(__uint_as_float(*(volatile uint32_t*)&s.top_t));
-    if (J == 0 && lane == 0) w.of_t = unscale_for(scale);
-#pragma unroll 1
-    for (int i = J; i < 4; ++i) {
-      const float* from = i == J ? &s.A[J * 16 + pair][J * 16 + g] : &s.A[J * 16 + g][i * 16 + pair];
-      const int along = i == J ? kAPitch : 1, across = i == J ? 1 : kAPitch;
-      uint32_t h[4], l[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float* two = from + (u >> 1) * 8 * along + (u & 1) * 8 * across;
-        split(two[0] * scale, two[along] * scale, h[u], l[u]);
-      }
-      const uint32_t at = to + triangle_at(i, J, (mi >> 1) * 8 + r8, mi & 1);
-      stmatrix_trans(at, h);
-      stmatrix_trans(at + L::kTriangle, l);
     }
   }
 
@@ -722,16 +663,16 @@ struct Helpers {
       if (!of_q) sync();                                       // (the weights)
       weigh(warp, acc, of_q ? s.of_p : s.of_a, of_q);
       if (of_q) {
-        store_p(warp, acc, generic + stage + L::kPAt, w.of_p);
+        float* P = reinterpret_cast<float*>(generic + stage + L::kPAt);
+        store<L::kTwoOfP ? 2 : 13, 1>(warp, acc, P + block_at(warp, 0), P + block_at(warp, warp));
       } else {
-        store_a(warp, acc);
-        invert_block(warp);
+        float* T_blocks = reinterpret_cast<float*>(generic + stage + L::kTAt);
+        store<2, 0>(warp, acc, s.A + left_block_at(warp, 0), T_blocks + block_at(warp, warp));
+        invert_block(T_blocks + block_at(warp, warp));
         sync();
-        columns_of_t(warp);
+        columns_of_t(warp, T_blocks);
       }
     }
-    sync();
-    store_t(warp, kt + L::kTAt, w);
     if (warp == 3) total(w, min(end - first, kChunk));
   }
 };
@@ -880,9 +821,9 @@ struct Columns {
     }
   }
 
-  // o of 32 tokens (half): q S, which O holds, and P U, whose operand u(kk, hi, lo) gives.  16 bits: to shared memory.
+  // o of 32 tokens (half): q S, which O holds, and P U; u(n, hi, lo) gives the operand of U's tokens 8 n up to 8 n + 7.  16 bits: to shared memory.
   template <typename Operand>
-  __device__ __forceinline__ void finish_o(uint32_t pt, const Weights& w, int half, const float (&O)[4][4], const float (&per_s)[2],
+  __device__ __forceinline__ void finish_o(const float* P, const Weights& w, int half, const float (&O)[4][4], const float (&per_s)[2],
                                            const float (&per_o)[2], const Operand& u, bool odd, const int (&from)[2], uint32_t out_at, int first,
                                            int end) const {
     float I[4][4];
@@ -891,27 +832,21 @@ struct Columns {
 #pragma unroll
       for (int e = 0; e < 4; ++e) I[n][e] = 0.0f;
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      if (kk > 2 * half + 1) break;
-      uint32_t hi[4], lo[4];
-      u(kk, hi, lo);
+    for (int n = 0; n < 8; ++n) {
+      if (n > 4 * half + 3) break;
+      uint32_t hi[4], lo[4], bh[4][2], bl[4][2];
+      u(n, hi, lo);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (kk > 2 * half + i) continue;
-        const uint32_t at = pt + triangle_at(2 * half + i, kk, (mi >> 1) * 8 + r8, mi & 1);
-        uint32_t b[4];
-        ldmatrix(at, b);
+      for (int t = 0; t < 4; ++t)                              // (P is 0 where its tokens come before U's)
+        if (n <= 4 * half + t) right_tf32(P + block_at(2 * half + (t >> 1), n >> 1) + (t & 1) * 8 * 16 + float_at(group, (n & 1) * 8 + pair), bh[t], bl[t]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (kLow) mma(I[2 * i + h], lo, b[2 * h], b[2 * h + 1]);
-          mma(I[2 * i + h], hi, b[2 * h], b[2 * h + 1]);
-        }
-        if (L::kOfP == 2) {
-          ldmatrix(at + L::kTriangle, b);
+      for (int m = kLow ? 0 : 2; m < 3; ++m)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) mma(I[2 * i + h], hi, b[2 * h], b[2 * h + 1]);
-        }
-      }
+        for (int t = 0; t < 4; ++t)
+          if (n <= 4 * half + t) {
+            const uint32_t(&f)[2] = m == 1 ? bl[t] : bh[t];
+            mma_tf32(I[t], m == 0 ? lo : hi, f[0], f[1]);
+          }
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -919,11 +854,11 @@ struct Columns {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int t = (4 * half + 2 * i + h) * 8 + pair;
-        const float2 fq = *reinterpret_cast<const float2*>(&w.of_q[t]), fp = *reinterpret_cast<const float2*>(&w.of_p[t]);
+        const float2 fq = *reinterpret_cast<const float2*>(&w.of_q[t]);
         float y[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          y[e] = fmaf((e & 1 ? fq.y : fq.x) * per_s[e >> 1], O[2 * i + h][e], (e & 1 ? fp.y : fp.x) * per_o[e >> 1] * I[2 * i + h][e]);
+          y[e] = fmaf((e & 1 ? fq.y : fq.x) * per_s[e >> 1], O[2 * i + h][e], p.scale * per_o[e >> 1] * I[2 * i + h][e]);
         if (odd) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -981,12 +916,12 @@ struct Columns {
     for (int n = 0; n < 8; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) O[n >> 2][n & 3][e] = 0.0f;
-    auto handed = [&](uint32_t at, int steps, int i, uint32_t (&hi)[4], uint32_t (&lo)[4]) {
-      const uint4* from = reinterpret_cast<const uint4*>(generic + at0 + at) + i * 32 + lane;
+    auto handed_s = [&](int i, uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+      const uint4* from = reinterpret_cast<const uint4*>(generic + at0 + L::kSAt) + i * 32 + lane;
       const uint4 x = from[0];
       hi[0] = x.x, hi[1] = x.y, hi[2] = x.z, hi[3] = x.w;
       if constexpr (L::kTwo) {
-        const uint4 y = from[steps * 32];
+        const uint4 y = from[DK / 16 * 32];
         lo[0] = y.x, lo[1] = y.y, lo[2] = y.z, lo[3] = y.w;
       }
     };
@@ -994,7 +929,7 @@ struct Columns {
 #pragma unroll 2
     for (int ks = 0; ks < DK / 16; ++ks) {
       uint32_t hi[4], lo[4];
-      handed(L::kSAt, DK / 16, ks, hi, lo);
+      handed_s(ks, hi, lo);
 #pragma unroll
       for (int half = 0; half < 2; ++half) multiply_q(smem + stage + L::kQAt, half, ks, hi, lo, O[half]);
     }
@@ -1004,16 +939,23 @@ struct Columns {
     const float per_s[2] = {ps.x, ps.y}, per_o[2] = {po.x, po.y};
     const int from[2] = {f.x, f.y};
     const bool odd = __any_sync(0xffffffffu, min(f.x, f.y) < kChunk);
+    const float one[2] = {1.0f, 1.0f};
 #pragma unroll
     for (int half = 0; half < 2; ++half)
-      finish_o(smem + stage + L::kPAt, w, half, O[half], per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { handed(L::kUAt, 4, kk, hi, lo); },
+      finish_o(reinterpret_cast<const float*>(generic + stage + L::kPAt), w, half, O[half], per_s, per_o,
+               [&](int n, uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+                 const float4 x = reinterpret_cast<const float4*>(generic + at0 + L::kUAt)[n * 32 + lane];
+                 const float tile[4] = {x.x, x.y, x.z, x.w};
+                 left_tf32(tile, one, hi, lo);
+               },
                odd, from, at0 + (c & 1) * L::kV, first, end);
     store_o(at0 + (c & 1) * L::kV, first, end);        // (v of the chunk has been read: seen with U)
   }
 
   // S of chunk c, and its o too where no other warp makes it.
   __device__ __forceinline__ void chunk(int c, uint32_t stage, int first, int end, float (&S)[DK / 8][4]) const {
-    const uint32_t kt = smem + stage, qt = kt + L::kQAt, tt = kt + L::kTAt;
+    const uint32_t kt = smem + stage, qt = kt + L::kQAt;
+    const float* T_blocks = reinterpret_cast<const float*>(generic + stage + L::kTAt);
     const Weights& w = *reinterpret_cast<const Weights*>(generic + stage + L::kWeightsAt);
     load_v((c + 1) & 1, first + kChunk, end);
     float v32[kFull ? 8 : 1][4];
@@ -1104,42 +1046,37 @@ struct Columns {
     float per_r[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      scale[h] = scale_for(top[h]);
+      scale[h] = scale_for_tf32(top[h]);
       per_r[h] = unscale_for(scale[h]);
     }
 
-    // U (times R's and T's scales)
+    // U (times R's scale): eight tokens of R at a time with four tiles of T's rows
     float U[8][4];
 #pragma unroll
     for (int n = 0; n < 8; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) U[n][e] = 0.0f;
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
+    for (int n = 0; n < 8; ++n) {
       uint32_t hi[4], lo[4];
-      operand(X, kk, scale, hi, lo);
+      left_tf32(X[n], scale, hi, lo);
 #pragma unroll
-      for (int np = kk; np < 4; np += 2) {                     // (two at a time, where there are)
-        uint32_t b[2][4], bl[2][4];
+      for (int t0 = n / 4 * 4; t0 < 8; t0 += 4) {
+        uint32_t bh[4][2], bl[4][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (np + i > 3) break;
-          const uint32_t at = tt + triangle_at(np + i, kk, (mi >> 1) * 8 + r8, mi & 1);
-          ldmatrix(at, b[i]);
-          ldmatrix(at + L::kTriangle, bl[i]);
-        }
+        for (int t = 0; t < 4; ++t)
+          if (n <= t0 + t)
+            right_tf32(T_blocks + block_at((t0 + t) >> 1, n >> 1) + (t & 1) * 8 * 16 + float_at(group, (n & 1) * 8 + pair), bh[t], bl[t]);
 #pragma unroll
-        for (int m = 0; m < 3; ++m)
+        for (int m = 0; m < 3; ++m)                            // (the small products first)
 #pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            if (np + (n >> 1) > 3) break;
-            const uint32_t(&f)[4] = m == 1 ? bl[n >> 1] : b[n >> 1];
-            mma(U[2 * np + n], m == 0 ? lo : hi, f[2 * (n & 1)], f[2 * (n & 1) + 1]);
-          }
+          for (int t = 0; t < 4; ++t)
+            if (n <= t0 + t) {
+              const uint32_t(&f)[2] = m == 1 ? bl[t] : bh[t];
+              mma_tf32(U[t0 + t], m == 0 ? lo : hi, f[0], f[1]);
+            }
       }
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) per_r[h] *= w.of_t;
     largest(U, top);
     if (__any_sync(0xffffffffu, !(max_nan(top[0], top[1]) <= FLT_MAX))) {
       odd = true;
@@ -1152,18 +1089,14 @@ struct Columns {
       float per_o[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        scale[h] = scale_for(top[h]);
+        scale[h] = scale_for_tf32(top[h]);
         per_o[h] = unscale_for(scale[h]) * per_r[h];
       }
       if constexpr (SPLIT) {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          uint32_t hi[4], lo[4];
-          operand(U, kk, scale, hi, lo);
-          const uint32_t to = smem + at0 + L::kUAt + (kk * 32 + lane) * 16;
-          ptx::st_shared16(to, hi[0], hi[1], hi[2], hi[3]);
-          if (L::kTwo) ptx::st_shared16(to + 4 * 512, lo[0], lo[1], lo[2], lo[3]);
-        }
+        for (int n = 0; n < 8; ++n)
+          reinterpret_cast<float4*>(generic + at0 + L::kUAt)[n * 32 + lane] =
+              make_float4(U[n][0] * scale[0], U[n][1] * scale[0], U[n][2] * scale[1], U[n][3] * scale[1]);
         lane_pair<float2>(1) = make_float2(per_o[0], per_o[1]);
         lane_pair<int2>(2) = make_int2(from[0], from[1]);
         announce(1);
@@ -1182,8 +1115,8 @@ struct Columns {
             operand(S, ks, scale_s, hi, lo);
             multiply_q(qt, half, ks, hi, lo, O);
           }
-          finish_o(kt + L::kPAt, w, half, O, per_s, per_o, [&](int kk, uint32_t (&hi)[4], uint32_t (&lo)[4]) { operand(U, kk, scale, hi, lo); }, odd,
-                   from, at0 + (c & 1) * L::kV, first, end);
+          finish_o(reinterpret_cast<const float*>(generic + stage + L::kPAt), w, half, O, per_s, per_o,
+                   [&](int n, uint32_t (&hi)[4], uint32_t (&lo)[4]) { left_tf32(U[n], scale, hi, lo); }, odd, from, at0 + (c & 1) * L::kV, first, end);
         }
         store_o(at0 + (c & 1) * L::kV, first, end);
       }
