@@ -17,10 +17,11 @@
 // brought to below 2^15 by a power of two first, so that what a piece leaves off is below 2^-39 of its row's largest element, whatever the type's range.
 // That suits rows along dk, which are summed up anyway, and what all tokens of a chunk add to S.  R, U, T and P are another matter: tokens meet only
 // those before them, which may be smaller by any factor, so that a scale for all of them would take their bits.  T R and P U are products of TF32
-// pieces (11 and 11 bits), which have fp32's exponents.  k and q of 16 bits are one piece, of fp32 two; S, R and U are two pieces (S k, U k: two products a
-// term; T R: three); T is inverted in blocks of 16 x 16, those on the diagonal by substitution in fp32, the others by TF32 products too.  For o
-// of bf16 S, P and U are rounded to 11 bits once, which is finer than o's own rounding; of fp16 and fp32 they are two pieces.  Against 64 bits the states
-// of 600 tokens are off by 2.3e-7 of their norm (of fp32 rows by 3.3e-7, and o by 7e-7; token by token both are 2e-7).
+// pieces (11 and 11 bits), which have fp32's exponents; P U for o of bf16 of bf16 pieces (8 and 8, off by at most 2^-16: o's own rounding is 2^-9; S, P and
+// U in one piece of 11 bits each put o off by 2% more, and 1e-3 of its norm away from what sums in fp32 give).  k and q of 16 bits are
+// one piece, of fp32 two; S, R and U are two pieces (S k, U k: two products a term; T R and P U: three); T is inverted in blocks of 16 x 16, those on the
+// diagonal by substitution in fp32, the others by TF32 products too.  Against 64 bits the states of 600 tokens are off by 2.3e-7 of their norm (of fp32
+// rows by 3.3e-7, and o by 7e-7; token by token both are 2e-7).
 //
 // What bounds it (128 x 128, fp16): a chunk of 64 tokens takes a block of 32 columns 6.3 us (bf16), of 64 columns 7.4 (fp16); its chains alone 3.4 and
 // 5.1, a team alone, with every second chunk, about 10.  Both are some 4000 instructions a warp, one after the other at about five cycles each (what the products, 8 cycles of an SM's quarter each, take is
@@ -92,8 +93,8 @@ struct Layout {
   static constexpr uint32_t kRows = kChunk * DK * 2;           // a piece of k or q
   static constexpr uint32_t kTriangle = 10 * kBlock * 4;       // T or P: their 16 x 16 blocks up to the diagonal, by rows of blocks
   static constexpr uint32_t kQAt = kPieces * kRows, kTAt = 2 * kPieces * kRows, kPAt = kTAt + kTriangle;
-  // fp16: S, P and U are two pieces for o too (with all three rounded once it was off by 1.7 times its own rounding, with P alone by up to 1.6)
-  static constexpr bool kTwo = std::is_same<T, __half>::value, kTwoOfP = kPieces == 2 || kTwo;
+  // P U of bf16 rows: of two bf16 pieces each
+  static constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   static constexpr uint32_t kWeightsAt = kPAt + kTriangle;
   static constexpr uint32_t kStage = (kWeightsAt + sizeof(Weights) + 127) / 128 * 128;
   static constexpr uint32_t kScratchAt = kSlots * kStage, kScratch = (sizeof(Scratch) + 127) / 128 * 128;
@@ -101,7 +102,7 @@ struct Layout {
   // of a warp with columns: two chunks of v (16 bits), where o leaves through too; then, where another warp makes o, what it needs: S as operands, U,
   // three pairs a lane
   static constexpr uint32_t kV = sizeof(T) == 2 ? kChunk * 32 : 0;
-  static constexpr uint32_t kSAt = 2 * kV, kUAt = kSAt + DK / 16 * 512 * (1 + kTwo), kPairsAt = kUAt + 8 * 512;
+  static constexpr uint32_t kSAt = 2 * kV, kUAt = kSAt + DK / 16 * 1024, kPairsAt = kUAt + 8 * 512;
   template <bool SPLIT> static constexpr uint32_t kColumns = SPLIT ? kPairsAt + 3 * 256 : 2 * kV;
 };
 
@@ -149,22 +150,37 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], 
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// x rounded to 24 - BITS bits, away from 0 in the middle (a NaN stays one: as a whole number it may not).
-template <int BITS>
-__device__ __forceinline__ float rounded(float x) {
-  return fmaf(x, 0.0f, __uint_as_float((__float_as_uint(x) + (1u << (BITS - 1))) & ~((1u << BITS) - 1u)));
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Left operand from a tile of accumulators (rows g and g + 8, columns along its tokens), scaled, in pieces: rounded to 11 bits, and the rest, of which
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t& hi, uint32_t& lo) {
+  hi = pack_bf16(a, b);
+  lo = pack_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
+}
+// x rounded to 22 bits, away from 0 in the middle (a NaN stays one: as a whole number it may not).
+__device__ __forceinline__ float rounded_22(float x) { return fmaf(x, 0.0f, __uint_as_float((__float_as_uint(x) + 2u) & ~3u)); }
+// Left operand from a tile of accumulators (rows g and g + 8, columns along its tokens) in pieces: rounded to 11 bits, and the rest, of which
 // the instruction takes 11.  (By whole numbers: the conversion instruction takes its time, one prompt of 16384 tokens 1706 instead of 1634 us.)  Of its eight
 // columns the even ones are taken for the first four, and so are the rows of right_tf32.
-__device__ __forceinline__ void left_tf32(const float (&x)[4], const float (&scale)[2], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+__device__ __forceinline__ void left_tf32(const float (&x)[4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float y = x[e] * scale[e >> 1];
     const int to = (e & 1) * 2 + (e >> 1);
-    hi[to] = (__float_as_uint(y) + 0x1000u) & 0xffffe000u;
-    lo[to] = __float_as_uint(y - __uint_as_float(hi[to]));
+    hi[to] = (__float_as_uint(x[e]) + 0x1000u) & 0xffffe000u;
+    lo[to] = __float_as_uint(x[e] - __uint_as_float(hi[to]));
   }
+}
+// A tile of R or U, rows scaled.
+__device__ __forceinline__ void scaled(const float (&x)[4], const float (&scale)[2], float (&y)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = x[e] * scale[e >> 1];
 }
 // Right operand, of two numbers that are rounded to 22 bits: the first 11 of them, and the others.
 __device__ __forceinline__ void right_tf32(const float* two, uint32_t (&hi)[2], uint32_t (&lo)[2]) {
@@ -199,6 +215,11 @@ __device__ __forceinline__ uint32_t unit_at(int r, int unit) {
 __host__ __device__ constexpr int block_at(int i, int k) { return (i * (i + 1) / 2 + k) * kBlock; }
 __host__ __device__ constexpr int left_block_at(int i, int k) { return (i * (i - 1) / 2 + k) * kBlock; }
 __host__ __device__ constexpr int float_at(int r, int c) { return r * 16 + (c ^ ((r & 2) << 2)); }
+// The same of 16 bits: byte of half a row (16 bytes) r of block (i, k), the halves of every second four rows swapped, and of a piece.
+__host__ __device__ constexpr int half_row_at(int i, int k, int r, int half) {
+  return (i * (i + 1) / 2 + k) * 512 + r * 32 + ((half ^ (r >> 2 & 1)) << 4);
+}
+constexpr int kPieceOfP = 10 * 512;
 
 // ------------------------------------------------------------------------------------------------ the helpers
 
@@ -538,25 +559,40 @@ struct Helpers {
       }
     }
   }
-  // Rows of blocks m of A (the diagonal's block as it is, into T's place) and of P, rounded to what their products take.
-  template <int BITS, int OF_DIAGONAL>
+  // Row m of the blocks of A (the diagonal's block as it is, into T's place) or of P, rounded to what their products take.
+  template <bool OF_P>
   __device__ __forceinline__ void store(int m, const Square& acc, float* left, float* diagonal) const {
     const int at = float_at(lane >> 2, (lane & 3) * 2);
-    auto put = [&](float* to, float a, float b, float c, float d) {
-      *reinterpret_cast<float2*>(to) = make_float2(a, b);
-      *reinterpret_cast<float2*>(to + 8 * 16) = make_float2(c, d);
+    auto put = [&](const float(&x)[4], float* to, bool exact) {
+      *reinterpret_cast<float2*>(to) = exact ? make_float2(x[0], x[1]) : make_float2(rounded_22(x[0]), rounded_22(x[1]));
+      *reinterpret_cast<float2*>(to + 8 * 16) = exact ? make_float2(x[2], x[3]) : make_float2(rounded_22(x[2]), rounded_22(x[3]));
     };
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const float(&x)[4] = acc.diagonal[n];
-      if constexpr (OF_DIAGONAL == 0) put(diagonal + (at ^ (n * 8)), x[0], x[1], x[2], x[3]);
-      else put(diagonal + (at ^ (n * 8)), rounded<BITS>(x[0]), rounded<BITS>(x[1]), rounded<BITS>(x[2]), rounded<BITS>(x[3]));
-    }
+    for (int n = 0; n < 2; ++n) put(acc.diagonal[n], diagonal + (at ^ (n * 8)), !OF_P);
 #pragma unroll
     for (int n = 0; n < 6; ++n) {
       if (n >= 2 * m) break;
-      const float(&x)[4] = acc.left[n];
-      put(left + (n >> 1) * kBlock + (at ^ ((n & 1) * 8)), rounded<BITS>(x[0]), rounded<BITS>(x[1]), rounded<BITS>(x[2]), rounded<BITS>(x[3]));
+      put(acc.left[n], left + (n >> 1) * kBlock + (at ^ ((n & 1) * 8)), false);
+    }
+  }
+  // The same of P in bf16 pieces.
+  __device__ __forceinline__ void store_bf16(int m, const Square& acc, uint8_t* to) const {
+    auto put = [&](const float(&x)[4], int n) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t hi, lo;
+        split_bf16(x[2 * h], x[2 * h + 1], hi, lo);
+        uint8_t* at = to + half_row_at(m, n >> 1, (lane >> 2) + 8 * h, n & 1) + (lane & 3) * 4;
+        *reinterpret_cast<uint32_t*>(at) = hi;
+        *reinterpret_cast<uint32_t*>(at + kPieceOfP) = lo;
+      }
+    };
+#pragma unroll
+    for (int n = 0; n < 2; ++n) put(acc.diagonal[n], 2 * m + n);
+#pragma unroll
+    for (int n = 0; n < 6; ++n) {
+      if (n >= 2 * m) break;
+      put(acc.left[n], n);
     }
   }
   // The inverse of 1 and a diagonal block of A, in its place: by substitution, a column a lane.
@@ -579,14 +615,13 @@ struct Helpers {
     }
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) d[float_at(i, j)] = rounded<2>(x[i]);
+    for (int i = 0; i < 16; ++i) d[float_at(i, j)] = rounded_22(x[i]);
   }
 
   // 16 columns J of T below the diagonal block: T_iJ = -T_ii sum_k A_ik T_kJ, i downward.  They are worked on transposed, so that what one product
   // gives is the next one's left operand.  By TF32 instructions, whose exponents need no scales: operands in two pieces, three products a term.
   __device__ __forceinline__ void columns_of_t(int J, float* T_blocks) const {
     const int g = lane >> 2, pair = (lane & 3) * 2, right = float_at(g, pair), turned = pair * 16 + (g ^ ((pair & 2) << 2));
-    const float one[2] = {1.0f, 1.0f};
     float x[2][4];
 #pragma unroll 1
     for (int i = J + 1; i < 4; ++i) {
@@ -615,7 +650,7 @@ struct Helpers {
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
           uint32_t ah[4], al[4], bh[2][2], bl[2][2];
-          left_tf32(x[ks], one, ah, al);
+          left_tf32(x[ks], ah, al);
 #pragma unroll
           for (int n = 0; n < 2; ++n) right_tf32(from + n * 8 * 16 + (right ^ (ks * 8)), bh[n], bl[n]);
 #pragma unroll
@@ -630,7 +665,7 @@ struct Helpers {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) to[(turned ^ ((e >> 1) * 8)) + (n * 8 + (e & 1)) * 16] = rounded<2>(d[n][e] + (small[0][n][e] + small[1][n][e]));
+        for (int e = 0; e < 4; ++e) to[(turned ^ ((e >> 1) * 8)) + (n * 8 + (e & 1)) * 16] = rounded_22(d[n][e] + (small[0][n][e] + small[1][n][e]));
       __syncwarp();
     }
   }
@@ -664,10 +699,11 @@ struct Helpers {
       weigh(warp, acc, of_q ? s.of_p : s.of_a, of_q);
       if (of_q) {
         float* P = reinterpret_cast<float*>(generic + stage + L::kPAt);
-        store<L::kTwoOfP ? 2 : 13, 1>(warp, acc, P + block_at(warp, 0), P + block_at(warp, warp));
+        if constexpr (L::kBf16) store_bf16(warp, acc, generic + stage + L::kPAt);
+        else store<true>(warp, acc, P + block_at(warp, 0), P + block_at(warp, warp));
       } else {
         float* T_blocks = reinterpret_cast<float*>(generic + stage + L::kTAt);
-        store<2, 0>(warp, acc, s.A + left_block_at(warp, 0), T_blocks + block_at(warp, warp));
+        store<false>(warp, acc, s.A + left_block_at(warp, 0), T_blocks + block_at(warp, warp));
         invert_block(T_blocks + block_at(warp, warp));
         sync();
         columns_of_t(warp, T_blocks);
@@ -733,8 +769,7 @@ __device__ __forceinline__ void operand(const float (&x)[N][4], int ks, const fl
 template <typename T, int DK, bool SPLIT, int TEAMS>
 struct Columns {
   using L = Layout<T, DK, TEAMS>;
-  static constexpr bool kFull = L::kPieces == 2;               // fp32: o too from two pieces
-  static constexpr bool kLow = kFull || L::kTwo;               // of S and U
+  static constexpr bool kFull = L::kPieces == 2;               // fp32 rows
   static_assert(!(kFull && SPLIT), "");
 
   const ChunkParams& p;
@@ -810,7 +845,7 @@ struct Columns {
       ldmatrix(at, a);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (kLow) mma(O[2 * i + h], lo, a[2 * h], a[2 * h + 1]);
+        mma(O[2 * i + h], lo, a[2 * h], a[2 * h + 1]);
         mma(O[2 * i + h], hi, a[2 * h], a[2 * h + 1]);
       }
       if (kFull) {
@@ -821,32 +856,68 @@ struct Columns {
     }
   }
 
-  // o of 32 tokens (half): q S, which O holds, and P U; u(n, hi, lo) gives the operand of U's tokens 8 n up to 8 n + 7.  16 bits: to shared memory.
-  template <typename Operand>
-  __device__ __forceinline__ void finish_o(const float* P, const Weights& w, int half, const float (&O)[4][4], const float (&per_s)[2],
-                                           const float (&per_o)[2], const Operand& u, bool odd, const int (&from)[2], uint32_t out_at, int first,
+  // o of 32 tokens (half): q S, which O holds, and P U; tile(n, x) gives U's tokens 8 n up to 8 n + 7.  16 bits: to shared memory.
+  template <typename Tile>
+  __device__ __forceinline__ void finish_o(uint32_t P_at, const Weights& w, int half, const float (&O)[4][4], const float (&per_s)[2],
+                                           const float (&per_o)[2], const Tile& tile, bool odd, const int (&from)[2], uint32_t out_at, int first,
                                            int end) const {
     float I[4][4];
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) I[n][e] = 0.0f;
+    auto block = [&](int kk) {                                 // of 16 tokens of U
+      if constexpr (L::kBf16) {
+        uint32_t hi[4], lo[4], b[2][4], bl[2][4];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      if (n > 4 * half + 3) break;
-      uint32_t hi[4], lo[4], bh[4][2], bl[4][2];
-      u(n, hi, lo);
+        for (int i = 0; i < 2; ++i) {
+          float x[4];
+          tile(2 * kk + i, x);
+          split_bf16(x[0], x[1], hi[2 * i], lo[2 * i]);
+          split_bf16(x[2], x[3], hi[2 * i + 1], lo[2 * i + 1]);
+          if (kk > 2 * half + i) continue;
+          const uint32_t at = smem + P_at + half_row_at(2 * half + i, kk, (mi >> 1) * 8 + r8, mi & 1);
+          ldmatrix(at, b[i]);
+          ldmatrix(at + kPieceOfP, bl[i]);
+        }
 #pragma unroll
-      for (int t = 0; t < 4; ++t)                              // (P is 0 where its tokens come before U's)
-        if (n <= 4 * half + t) right_tf32(P + block_at(2 * half + (t >> 1), n >> 1) + (t & 1) * 8 * 16 + float_at(group, (n & 1) * 8 + pair), bh[t], bl[t]);
+        for (int m = 0; m < 3; ++m)                            // (the small products first)
 #pragma unroll
-      for (int m = kLow ? 0 : 2; m < 3; ++m)
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (n <= 4 * half + t) {
-            const uint32_t(&f)[2] = m == 1 ? bl[t] : bh[t];
-            mma_tf32(I[t], m == 0 ? lo : hi, f[0], f[1]);
+          for (int t = 0; t < 4; ++t) {
+            if (kk > 2 * half + (t >> 1)) continue;
+            const uint32_t(&f)[4] = m == 1 ? bl[t >> 1] : b[t >> 1];
+            mma_bf16(I[t], m == 0 ? lo : hi, f[2 * (t & 1)], f[2 * (t & 1) + 1]);
           }
+      } else {
+        const float* P = reinterpret_cast<const float*>(generic + P_at);
+#pragma unroll
+        for (int n = 2 * kk; n < 2 * kk + 2; ++n) {
+          float x[4];
+          uint32_t hi[4], lo[4], bh[4][2], bl[4][2];
+          tile(n, x);
+          left_tf32(x, hi, lo);
+#pragma unroll
+          for (int t = 0; t < 4; ++t)                          // (P is 0 where its tokens come before U's)
+            if (n <= 4 * half + t)
+              right_tf32(P + block_at(2 * half + (t >> 1), kk) + (t & 1) * 8 * 16 + float_at(group, (n & 1) * 8 + pair), bh[t], bl[t]);
+#pragma unroll
+          for (int m = 0; m < 3; ++m)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+              if (n <= 4 * half + t) {
+                const uint32_t(&f)[2] = m == 1 ? bl[t] : bh[t];
+                mma_tf32(I[t], m == 0 ? lo : hi, f[0], f[1]);
+              }
+        }
+      }
+    };
+    if constexpr (SPLIT) {                                     // (less code for the instruction cache: the long prompt 1616 to 1559 us)
+#pragma unroll 1
+      for (int kk = 0; kk < 2 * half + 2; ++kk) block(kk);
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        if (kk < 2 * half + 2) block(kk);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -920,13 +991,11 @@ struct Columns {
       const uint4* from = reinterpret_cast<const uint4*>(generic + at0 + L::kSAt) + i * 32 + lane;
       const uint4 x = from[0];
       hi[0] = x.x, hi[1] = x.y, hi[2] = x.z, hi[3] = x.w;
-      if constexpr (L::kTwo) {
-        const uint4 y = from[DK / 16 * 32];
-        lo[0] = y.x, lo[1] = y.y, lo[2] = y.z, lo[3] = y.w;
-      }
+      const uint4 y = from[DK / 16 * 32];
+      lo[0] = y.x, lo[1] = y.y, lo[2] = y.z, lo[3] = y.w;
     };
     await(0);
-#pragma unroll 2
+#pragma unroll 1
     for (int ks = 0; ks < DK / 16; ++ks) {
       uint32_t hi[4], lo[4];
       handed_s(ks, hi, lo);
@@ -939,14 +1008,12 @@ struct Columns {
     const float per_s[2] = {ps.x, ps.y}, per_o[2] = {po.x, po.y};
     const int from[2] = {f.x, f.y};
     const bool odd = __any_sync(0xffffffffu, min(f.x, f.y) < kChunk);
-    const float one[2] = {1.0f, 1.0f};
 #pragma unroll
     for (int half = 0; half < 2; ++half)
-      finish_o(reinterpret_cast<const float*>(generic + stage + L::kPAt), w, half, O[half], per_s, per_o,
-               [&](int n, uint32_t (&hi)[4], uint32_t (&lo)[4]) {
-                 const float4 x = reinterpret_cast<const float4*>(generic + at0 + L::kUAt)[n * 32 + lane];
-                 const float tile[4] = {x.x, x.y, x.z, x.w};
-                 left_tf32(tile, one, hi, lo);
+      finish_o(stage + L::kPAt, w, half, O[half], per_s, per_o,
+               [&](int n, float(&x)[4]) {
+                 const float4 y = reinterpret_cast<const float4*>(generic + at0 + L::kUAt)[n * 32 + lane];
+                 x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
                },
                odd, from, at0 + (c & 1) * L::kV, first, end);
     store_o(at0 + (c & 1) * L::kV, first, end);        // (v of the chunk has been read: seen with U)
@@ -970,7 +1037,15 @@ struct Columns {
     }
 
     // k S
-    float X[8][4], top[2], scale[2], scale_s[2], per_s[2];
+    constexpr bool kBeside = !SPLIT && !kFull;                 // q S beside k S (of fp32 rows there are not the registers)
+    float X[8][4], O[kBeside ? 2 : 1][4][4], top[2], scale[2], scale_s[2], per_s[2];
+    auto clear = [](float (&x)[4][4]) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[n][e] = 0.0f;
+    };
+    if constexpr (kBeside) clear(O[0]), clear(O[1]);
 #pragma unroll
     for (int n = 0; n < 8; ++n)
 #pragma unroll
@@ -988,7 +1063,11 @@ struct Columns {
       if constexpr (SPLIT) {
         const uint32_t to = smem + at0 + L::kSAt + (ks * 32 + lane) * 16;
         ptx::st_shared16(to, hi[0], hi[1], hi[2], hi[3]);
-        if (L::kTwo) ptx::st_shared16(to + DK / 16 * 512, lo[0], lo[1], lo[2], lo[3]);
+        ptx::st_shared16(to + DK / 16 * 512, lo[0], lo[1], lo[2], lo[3]);
+      }
+      if constexpr (kBeside) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) multiply_q(qt, half, ks, hi, lo, O[half]);
       }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {                   // (four accumulators, so that a product does not wait for the one before)
@@ -1058,8 +1137,10 @@ struct Columns {
       for (int e = 0; e < 4; ++e) U[n][e] = 0.0f;
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
+      float x[4];
       uint32_t hi[4], lo[4];
-      left_tf32(X[n], scale, hi, lo);
+      scaled(X[n], scale, x);
+      left_tf32(x, hi, lo);
 #pragma unroll
       for (int t0 = n / 4 * 4; t0 < 8; t0 += 4) {
         uint32_t bh[4][2], bl[4][2];
@@ -1101,22 +1182,20 @@ struct Columns {
         lane_pair<int2>(2) = make_int2(from[0], from[1]);
         announce(1);
       } else {
-        // (S is taken apart again, 32 tokens at a time: with q S made beside k S there are not the registers)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          float O[4][4];
+          float(&q_s)[4][4] = O[kBeside ? half : 0];
+          if constexpr (!kBeside) {                            // (S is taken apart again, 32 tokens at a time)
+            clear(q_s);
 #pragma unroll
-          for (int n = 0; n < 4; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) O[n][e] = 0.0f;
-#pragma unroll
-          for (int ks = 0; ks < DK / 16; ++ks) {
-            uint32_t hi[4], lo[4];
-            operand(S, ks, scale_s, hi, lo);
-            multiply_q(qt, half, ks, hi, lo, O);
+            for (int ks = 0; ks < DK / 16; ++ks) {
+              uint32_t hi[4], lo[4];
+              operand(S, ks, scale_s, hi, lo);
+              multiply_q(qt, half, ks, hi, lo, q_s);
+            }
           }
-          finish_o(reinterpret_cast<const float*>(generic + stage + L::kPAt), w, half, O, per_s, per_o,
-                   [&](int n, uint32_t (&hi)[4], uint32_t (&lo)[4]) { left_tf32(U[n], scale, hi, lo); }, odd, from, at0 + (c & 1) * L::kV, first, end);
+          finish_o(stage + L::kPAt, w, half, q_s, per_s, per_o, [&](int n, float(&x)[4]) { scaled(U[n], scale, x); }, odd, from, at0 + (c & 1) * L::kV,
+                   first, end);
         }
         store_o(at0 + (c & 1) * L::kV, first, end);
       }
@@ -1286,11 +1365,7 @@ cudaError_t launch_width(ChunkParams& p, int32_t sequences, cudaStream_t stream)
     if (wide) return launch<T, DK, Shape<4, false, 1, 0, 0>>(p, sequences, stream);
     return launch<T, DK, Shape<2, false, 1, 0, 0>>(p, sequences, stream);
   } else {
-    // (fp16, dk above 64: S in two pieces for the warps that make o does not fit beside P's two; registers do it, at 64 columns.  That prompt takes 1887 us;
-    // 32 columns with o made in the chain's warps, whose registers then spill, 1946 against 1932 before that step)
-    if constexpr (!(Layout<T, DK, 2>::kTwo && DK > 64)) {
-      if (!wide) return launch<T, DK, Shape<2, true, 2, 208, 144>>(p, sequences, stream);
-    }
+    if (!wide) return launch<T, DK, Shape<2, true, 2, 224, 136>>(p, sequences, stream);
     return launch<T, DK, Shape<4, false, 2, 232, 136>>(p, sequences, stream);
   }
 }
