@@ -222,7 +222,9 @@ cudaError_t launch(TokensParams& p, int32_t sequences, bool step, cudaStream_t s
 template <typename T, int R>
 cudaError_t launch_rows(TokensParams& p, int32_t sequences, bool step, cudaStream_t stream) {
   const int64_t columns = (int64_t)sequences * p.heads * p.dv;
-  if (R <= (step ? 8 : 16) && p.dv % 4 == 0 && p.dv > 64 && columns >= 296 * 128) return launch<T, R, R <= 16 ? 4 : 2>(p, sequences, step, stream);
+  if constexpr (R <= 16) {
+    if ((R <= 8 || !step) && p.dv % 4 == 0 && p.dv > 64 && columns >= 296 * 128) return launch<T, R, 4>(p, sequences, step, stream);
+  }
   if (p.dv % 2 == 0 && p.dv > 32 && columns >= 296 * 64) return launch<T, R, 2>(p, sequences, step, stream);
   return launch<T, R, 1>(p, sequences, step, stream);
 }
