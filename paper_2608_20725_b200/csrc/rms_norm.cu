@@ -6,11 +6,12 @@
 // no block's registers hold (above 32768 elements of 16 bits, 16384 of 32 or where rows do not lie on vectors) are read again.
 //
 // In 8 bits the root drops out of which number is nearest: h w of 16-bit elements is exact in fp32, of fp32 ones in 64 bits, and its
-// quotient by the row's largest is looked at in fp32 first; one that comes within 1e-3 of halfway between two numbers (of its 127 it is
-// off by up to 127 * 3 * 2^-24 = 2.3e-5) is divided again in 64 bits, where ties are seen as such.
+// quotient by the row's largest is looked at in fp32 first; where that comes within 1e-4 of halfway between two numbers, n and n + 1 (of its 127 it is
+// off by up to 127 * 3 * 2^-24 = 2.3e-5), the sign of 254 h w - (2 n + 1) top decides, exactly.
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "sequence.cuh"
 
@@ -36,12 +37,27 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-// 127 a w / top, rounded to the nearest whole number.
+// 127 z / top, which lies within n .. n + 1 (but for what tells halves from one another), rounded to the nearest whole number, ties to the even one: by the
+// sign of 254 |z| - (2 n + 1) top.  z and top are products of two elements, exact in 64 bits; what they are multiplied by here brings fp32 ones to 56 bits.
+template <typename T>
+__device__ __forceinline__ int nearest_of(double z, double top, float n) {
+  const double size = fabs(z), odd = 2.0f * n + 1.0f, a = __dmul_rn(254.0, size), b = __dmul_rn(odd, top);
+  double d = a - b;
+  if constexpr (sizeof(T) == 4) d += fma(254.0, size, -a) - fma(odd, top, -b);           // (a and b all but agree: both differences are exact)
+  const float r = d > 0.0 ? n + 1.0f : d < 0.0 ? n : 2.0f * rintf(0.5f * (n + 0.5f));
+  return z < 0.0 ? -(int)r : (int)r;
+}
+template <typename T>
 __device__ __forceinline__ int nearest(float product, float per_top, float h, float w, double top) {
   const float t = product * per_top;
   const float r = rintf(t);
-  if (fabsf(t - r) < 0.499f) return (int)r;
-  return (int)rint((double)h * (double)w * 127.0 / top);
+  if (fabsf(t - r) < 0.4999f) return (int)r;
+  return nearest_of<T>((double)h * (double)w, top, floorf(fabsf(t)));
+}
+template <typename T>
+__device__ __forceinline__ int nearest_in_64(double z, double top) {
+  const double t = z * 127.0 / top, r = rint(t);
+  return fabs(t - r) < 0.4999 ? (int)r : nearest_of<T>(z, top, (float)floor(fabs(t)));
 }
 
 // WARP: a row is a warp's (a block has four), otherwise all of the block's.  V: elements of a vector; N vectors a thread, or (N == 0) any
@@ -195,25 +211,29 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
     }
     int8_t* y = static_cast<int8_t*>(p.y) + row * p.y_stride;
     const bool zero = !fine || exact_top == 0.0;
-    const bool tiny = top < 8e-28f;                              // (products lose bits, and 127 / top is out of range)
     const float per_top = zero ? 0.0f : 127.0f / top;
-    auto finish = [&](const VT& h, int i) {
+    auto finish = [&](const VT& h, int i, auto tiny) {
       const VT w = weights(i);
       VB r;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float a = to_float(h.v[j]), b = to_float(w.v[j]);
-        r.v[j] = zero ? 0 : tiny ? (int8_t)rint((double)a * (double)b * 127.0 / exact_top) : (int8_t)nearest(a * b, per_top, a, b, exact_top);
+        if constexpr (tiny.value) r.v[j] = zero ? 0 : (int8_t)nearest_in_64<T>((double)a * (double)b, exact_top);
+        else r.v[j] = (int8_t)nearest<T>(a * b, per_top, a, b, exact_top);
       }
       *reinterpret_cast<VB*>(y + (int64_t)i * V) = r;
     };
-    if constexpr (N > 0) {
+    auto finish_all = [&](auto tiny) {
+      if constexpr (N > 0) {
 #pragma unroll
-      for (int n = 0; n < N; ++n)
-        if (tid + n * threads < vectors) finish(kept[n], tid + n * threads);
-    } else {
-      for (int i = tid; i < vectors; i += threads) finish(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
-    }
+        for (int n = 0; n < N; ++n)
+          if (tid + n * threads < vectors) finish(kept[n], tid + n * threads, tiny);
+      } else {
+        for (int i = tid; i < vectors; i += threads) finish(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i, tiny);
+      }
+    };
+    if (zero || top < 8e-28f) finish_all(std::true_type{});      // (products lose bits, and 127 / top is out of range)
+    else finish_all(std::false_type{});
   }
 }
 
