@@ -575,10 +575,12 @@ typedef struct {
  *     y = the whole number nearest to 127 h weight / max |h weight|  (ties to the even one),
  *     scales = max |h weight| / (127 sqrt(mean(h^2) + eps)),
  * so that y * scales is the normed row; which number is nearest is decided
- * exactly, whatever the order of sums.  Rows of zeros are zeros, with a scale
- * of 0; rows that hold an infinity or NaN (or whose h * weight passes the range
- * of floats) are zeros with a scale of NaN.  Sums are fp32 (where the squares
- * pass its range, y and the scale are 0), y is rounded once.
+ * exactly, whatever the order of sums.  Rows of zeros are zeros (without eps
+ * too), with a scale of 0; rows that hold an infinity or NaN (or whose h *
+ * weight passes the range of floats) are zeros with a scale of NaN.  Sums are
+ * fp32, of rows so small that their squares leave its range of larger numbers;
+ * where the squares pass its range, y of `dtype` and the scale are 0 (y in 8
+ * bits is what it is otherwise).  y of `dtype` is rounded once.
  * residual_out may be x or residual, and y (without scales) may be x or
  * residual where residual_out is not, each with the same stride; other overlaps
  * are not allowed.  The pointers need the alignment of their elements only; rows that

@@ -18,6 +18,8 @@
 namespace im2win {
 namespace {
 
+constexpr float kSmall = 0x1p-100f;      // of eps, and of the mean of squares
+
 struct NormParams {
   const void* x;
   const void* residual;
@@ -62,8 +64,9 @@ __device__ __forceinline__ int nearest_in_64(double z, double top) {
 
 // WARP: a row is a warp's (a block has four), otherwise all of the block's.  V: elements of a vector; N vectors a thread, or (N == 0) any
 // number, read twice.  BYTES: y in 8 bits, a kernel of its own for its registers.  (16384 rows of 4096 bf16 with a residual, 84 us at 6.4 TB/s, took 127 with
-// both in one kernel and the residual's loads behind a question each.)
-template <typename T, int V, int N, bool WARP, bool BYTES>
+// both in one kernel and the residual's loads behind a question each.)  SMALL: eps is so small that rows may be too, which is looked at; asking costs
+// 131072 rows of 128 a tenth of their time, which is instructions.
+template <typename T, int V, int N, bool WARP, bool BYTES, bool SMALL>
 __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormParams p) {
   using VT = Vec<T, V>;
   using VB = Vec<int8_t, V>;
@@ -108,7 +111,10 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
       for (int j = 0; j < V; ++j) top = max_nan(top, fabsf(to_float(h.v[j]) * to_float(w.v[j])));
     }
   };
-  VT kept[N > 0 ? N : 1];
+  VT kept[N > 0 ? N : 1], first;
+  if constexpr (N == 1 && WARP && !BYTES) {                      // (short rows: their weights before the sums)
+    if (tid < vectors) first = weights(tid);
+  }
   if constexpr (N > 0) {
 #pragma unroll
     for (int n = 0; n < N; ++n)
@@ -155,48 +161,71 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
       top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, s));
     }
   }
-  const float rate = rsqrtf(sum / (float)p.channels + p.eps);
-
-  if constexpr (!BYTES) {
-    T* y = static_cast<T*>(p.y) + row * p.y_stride;
-    auto finish = [&](const VT& h, int i) {
-      const VT w = weights(i);
-      VT r;
-#pragma unroll
-      for (int j = 0; j < V; ++j) r.v[j] = from_float<T>(to_float(h.v[j]) * rate * to_float(w.v[j]));
-      *reinterpret_cast<VT*>(y + (int64_t)i * V) = r;
-    };
+  auto each = [&](auto&& work) {                                 // work(h, its number) of all of the thread's vectors
     if constexpr (N > 0) {
 #pragma unroll
       for (int n = 0; n < N; ++n)
-        if (tid + n * threads < vectors) finish(kept[n], tid + n * threads);
+        if (tid + n * threads < vectors) work(kept[n], tid + n * threads);
     } else {
-      for (int i = tid; i < vectors; i += threads) finish(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
+      for (int i = tid; i < vectors; i += threads) work(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
     }
+  };
+  // Squares that fp32 may not hold, in a mean that eps does not lift: those of h times 2^96 are summed instead, and the rate is that of h times 2^96.  (Down
+  // to 2^-100 what is lost of a square is below 2^-49 of the mean.)  Rows of zeros without eps have a rate of 0.
+  constexpr float kUp = 0x1p96f;
+  const float mean = sum / (float)p.channels + p.eps;
+  const bool small = SMALL && mean < kSmall;                     // (the same for all threads of the row)
+  auto raised_rate = [&]() {
+    float sum = 0.0f;
+    each([&](const VT& h, int) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float a = to_float(h.v[j]) * kUp;
+        sum = fmaf(a, a, sum);
+      }
+    });
+#pragma unroll
+    for (int s = 16; s > 0; s /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+    if constexpr (!WARP) {
+      __syncthreads();
+      if (lane == 0) shared_sum[warp] = sum;
+      __syncthreads();
+      sum = lane < threads / 32 ? shared_sum[lane] : 0.0f;
+#pragma unroll
+      for (int s = 16; s > 0; s /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+    }
+    const float raised = sum / (float)p.channels + p.eps * kUp * kUp;
+    return raised > 0.0f ? rsqrtf(raised) : 0.0f;
+  };
+
+  if constexpr (!BYTES) {
+    T* y = static_cast<T*>(p.y) + row * p.y_stride;
+    float up = 1.0f, rate;
+    if (small) up = kUp, rate = raised_rate();
+    else rate = rsqrtf(mean);
+    each([&](const VT& h, int i) {
+      const VT w = N == 1 && WARP ? first : weights(i);
+      VT r;
+#pragma unroll
+      for (int j = 0; j < V; ++j) r.v[j] = from_float<T>((SMALL ? to_float(h.v[j]) * up : to_float(h.v[j])) * rate * to_float(w.v[j]));
+      *reinterpret_cast<VT*>(y + (int64_t)i * V) = r;
+    });
     return;
   } else {
     const bool fine = top <= FLT_MAX;                            // (not of a NaN)
-    if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7fffffff) : top == 0.0f ? 0.0f : top * rate / 127.0f;    // (0 times infinity: eps of 0)
     // fp32: the largest product in 64 bits, and all below 2^-90: products that fp32 does not hold exactly
     const bool in_64 = sizeof(T) == 4 || top < 8e-28f;
     double exact_top = top;
     if (fine && in_64) {                                         // (the same for all threads of the row)
       double most = 0.0;
-      auto raise = [&](const VT& h, int i) {
+      each([&](const VT& h, int i) {
         const VT w = weights(i);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           const float a = to_float(h.v[j]), b = to_float(w.v[j]);
           if (fabsf(a * b) == top) most = fmax(most, fabs((double)a * (double)b));
         }
-      };
-      if constexpr (N > 0) {
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-          if (tid + n * threads < vectors) raise(kept[n], tid + n * threads);
-      } else {
-        for (int i = tid; i < vectors; i += threads) raise(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i);
-      }
+      });
 #pragma unroll
       for (int s = 16; s > 0; s /= 2) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, s));
       if constexpr (!WARP) {
@@ -209,6 +238,8 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
       }
       exact_top = most;
     }
+    const float raised = small ? raised_rate() : 0.0f;
+    if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7fffffff) : small ? (float)(exact_top * (double)kUp) * raised / 127.0f : top * rsqrtf(mean) / 127.0f;
     int8_t* y = static_cast<int8_t*>(p.y) + row * p.y_stride;
     const bool zero = !fine || exact_top == 0.0;
     const float per_top = zero ? 0.0f : 127.0f / top;
@@ -223,47 +254,44 @@ __global__ void __launch_bounds__(WARP ? 128 : 1024) rms_norm_kernel(const NormP
       }
       *reinterpret_cast<VB*>(y + (int64_t)i * V) = r;
     };
-    auto finish_all = [&](auto tiny) {
-      if constexpr (N > 0) {
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-          if (tid + n * threads < vectors) finish(kept[n], tid + n * threads, tiny);
-      } else {
-        for (int i = tid; i < vectors; i += threads) finish(out ? *reinterpret_cast<const VT*>(out + (int64_t)i * V) : load(i), i, tiny);
-      }
-    };
-    if (zero || top < 8e-28f) finish_all(std::true_type{});      // (products lose bits, and 127 / top is out of range)
-    else finish_all(std::false_type{});
+    if (zero || top < 8e-28f) each([&](const VT& h, int i) { finish(h, i, std::true_type{}); });         // (products lose bits, and 127 / top is out of range)
+    else each([&](const VT& h, int i) { finish(h, i, std::false_type{}); });
   }
 }
 
 // Rows of up to 1024 elements (128 where they do not lie on vectors) are a warp's; others a block's of as many threads as make four
 // vectors each or fewer, and one each where there are few rows and a row's time is its latency.
-template <typename T, int V, bool BYTES>
+template <typename T, int V, bool BYTES, bool SMALL>
 cudaError_t launch(const NormParams& p, cudaStream_t stream) {
   constexpr int kMost = V > 1 ? 4 : 16;
   const int64_t vectors = p.channels / V;
   if (vectors <= 128) {
     const unsigned grid = (unsigned)(((int64_t)p.rows + 3) / 4);
     if (vectors <= 32)
-      rms_norm_kernel<T, V, 1, true, BYTES><<<grid, 128, 0, stream>>>(p);
+      rms_norm_kernel<T, V, 1, true, BYTES, SMALL><<<grid, 128, 0, stream>>>(p);
     else
-      rms_norm_kernel<T, V, 4, true, BYTES><<<grid, 128, 0, stream>>>(p);
+      rms_norm_kernel<T, V, 4, true, BYTES, SMALL><<<grid, 128, 0, stream>>>(p);
     return cudaGetLastError();
   }
   const bool few = p.rows <= 592;
   auto threads_for = [&](int each) { return (int)((vectors + each * 32 - 1) / (each * 32) * 32); };
   if (few && vectors <= 1024)
-    rms_norm_kernel<T, V, 1, false, BYTES><<<p.rows, threads_for(1), 0, stream>>>(p);
+    rms_norm_kernel<T, V, 1, false, BYTES, SMALL><<<p.rows, threads_for(1), 0, stream>>>(p);
   else if (vectors <= 512)
-    rms_norm_kernel<T, V, 2, false, BYTES><<<p.rows, threads_for(2), 0, stream>>>(p);
+    rms_norm_kernel<T, V, 2, false, BYTES, SMALL><<<p.rows, threads_for(2), 0, stream>>>(p);
   else if (vectors <= 1024 * 4)
-    rms_norm_kernel<T, V, 4, false, BYTES><<<p.rows, std::min(threads_for(4), 1024), 0, stream>>>(p);
+    rms_norm_kernel<T, V, 4, false, BYTES, SMALL><<<p.rows, std::min(threads_for(4), 1024), 0, stream>>>(p);
   else if (V == 1 && vectors <= 1024 * kMost)
-    rms_norm_kernel<T, V, kMost, false, BYTES><<<p.rows, threads_for(kMost), 0, stream>>>(p);
+    rms_norm_kernel<T, V, kMost, false, BYTES, SMALL><<<p.rows, threads_for(kMost), 0, stream>>>(p);
   else
-    rms_norm_kernel<T, V, 0, false, BYTES><<<p.rows, 1024, 0, stream>>>(p);
+    rms_norm_kernel<T, V, 0, false, BYTES, SMALL><<<p.rows, 1024, 0, stream>>>(p);
   return cudaGetLastError();
+}
+
+template <typename T, int V>
+cudaError_t launch_kind(const NormParams& p, cudaStream_t stream) {
+  if (p.eps < kSmall) return p.scales ? launch<T, V, true, true>(p, stream) : launch<T, V, false, true>(p, stream);
+  return p.scales ? launch<T, V, true, false>(p, stream) : launch<T, V, false, false>(p, stream);
 }
 
 template <typename T>
@@ -273,8 +301,8 @@ cudaError_t launch_type(const NormParams& p, cudaStream_t stream) {
   if (p.channels % V == 0 && rows_on(p.x, p.x_stride, sizeof(T)) && rows_on(p.residual, p.residual_stride, sizeof(T)) &&
       rows_on(p.residual_out, p.residual_out_stride, sizeof(T)) && rows_on(p.weight, 0, sizeof(T)) &&
       rows_on(p.y, p.y_stride, p.scales ? 1 : sizeof(T)))
-    return p.scales ? launch<T, V, true>(p, stream) : launch<T, V, false>(p, stream);
-  return p.scales ? launch<T, 1, true>(p, stream) : launch<T, 1, false>(p, stream);
+    return launch_kind<T, V>(p, stream);
+  return launch_kind<T, 1>(p, stream);
 }
 
 }  // namespace
