@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(TILE * 2) matmul_int8_kernel(const Int8Args p,
   }
   T* y = static_cast<T*>(p.y);
   auto finish = [&](int64_t m, int64_t n, int32_t sum, float x_scale) {
-    const float v = (float)sum * x_scale * p.scales[n];
+    const float v = __fmul_rn((float)sum * x_scale, p.scales[n]);         // (rounded before the bias is added, as by tiles)
     y[m * p.shape.y_stride + n] = from_float<T>(p.bias ? v + p.bias[n] : v);
   };
   if constexpr (TILE == 64) {
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kThreads) matmul_int8_few_kernel(const Int8Arg
       if (m >= M) break;
       const int32_t sum = __reduce_add_sync(0xffffffffu, acc[n][m]);
       if (lane == m && n0 + n < p.shape.N) {
-        const float v = (float)sum * p.x_scales[m] * p.scales[n0 + n];
+        const float v = __fmul_rn((float)sum * p.x_scales[m], p.scales[n0 + n]);
         y[m * p.shape.y_stride + n0 + n] = from_float<T>(p.bias ? v + p.bias[n0 + n] : v);
       }
     }
