@@ -526,7 +526,8 @@ typedef struct {
  *     u_t = beta[t][h] * (v_t - k_t a S_{t-1}),
  *     S_t = a S_{t-1} + k_t^T u_t,                       S [dk][dv],
  *     o_t = scale * q_t S_t,
- * where normalize divides each q_t and k_t by sqrt(its sum of squares + 1e-6).
+ * where normalize divides each q_t and k_t by sqrt(its sum of squares + 1e-6),
+ * a sum that has to stay within the range of floats (elements below 2^60).
  * Layouts, types and states are those of im2win_linear_attention; beta holds
  * floats, for each token and head or each head (normally 0 to 1).  There is no
  * workspace.  log_decay is normally <= 0 (-infinity empties the state; those
