@@ -21,7 +21,7 @@
 // U in one piece of 11 bits each put o off by 2% more, and 1e-3 of its norm away from what sums in fp32 give).  k and q of 16 bits are
 // one piece, of fp32 two; S, R and U are two pieces (S k, U k: two products a term; T R and P U: three); T is inverted in blocks of 16 x 16, those on the
 // diagonal by substitution in fp32, the others by TF32 products too.  Against 64 bits the states of 600 tokens are off by 2.3e-7 of their norm (of fp32
-// rows by 3.3e-7, and o by 7e-7; token by token both are 2e-7).
+// rows by 3.3e-7, and o by 5.7e-7; token by token both are 2e-7).
 //
 // What bounds it (128 x 128, fp16): a chunk of 64 tokens takes a block of 32 columns 6.3 us (bf16), of 64 columns 7.4 (fp16); its chains alone 3.4 and
 // 5.1, a team alone, with every second chunk, about 10.  Both are some 4000 instructions a warp, one after the other at about five cycles each (what the products, 8 cycles of an SM's quarter each, take is
@@ -836,7 +836,9 @@ struct Columns {
   template <typename V>
   __device__ __forceinline__ V& lane_pair(int which) const { return reinterpret_cast<V*>(generic + at0 + L::kPairsAt + which * 256)[lane]; }
 
-  // O += S q of 32 tokens (half), one step of dk
+  // O += S q of 32 tokens (half), one step of dk: the products of the small pieces, of the large ones, or both.  (What an instruction adds to an
+  // accumulator is cut off, not rounded: small products that come first lose less.)
+  template <bool SMALL, bool LARGE>
   __device__ __forceinline__ void multiply_q(uint32_t qt, int half, int ks, const uint32_t (&hi)[4], const uint32_t (&lo)[4], float (&O)[4][4]) const {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -845,10 +847,10 @@ struct Columns {
       ldmatrix(at, a);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        mma(O[2 * i + h], lo, a[2 * h], a[2 * h + 1]);
-        mma(O[2 * i + h], hi, a[2 * h], a[2 * h + 1]);
+        if (SMALL) mma(O[2 * i + h], lo, a[2 * h], a[2 * h + 1]);
+        if (LARGE) mma(O[2 * i + h], hi, a[2 * h], a[2 * h + 1]);
       }
-      if (kFull) {
+      if (kFull && SMALL) {
         ldmatrix(at + L::kRows, a);
 #pragma unroll
         for (int h = 0; h < 2; ++h) mma(O[2 * i + h], hi, a[2 * h], a[2 * h + 1]);
@@ -861,11 +863,12 @@ struct Columns {
   __device__ __forceinline__ void finish_o(uint32_t P_at, const Weights& w, int half, const float (&O)[4][4], const float (&per_s)[2],
                                            const float (&per_o)[2], const Tile& tile, bool odd, const int (&from)[2], uint32_t out_at, int first,
                                            int end) const {
-    float I[4][4];
+    constexpr int kSmall = kFull ? 4 : 1;                      // fp32 rows: sums of the small products of their own (o off by 5.7e-7 instead of 7.4e-7)
+    float I[4][4], small[kSmall][4];
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) I[n][e] = 0.0f;
+      for (int e = 0; e < 4; ++e) I[n][e] = small[n < kSmall ? n : 0][e] = 0.0f;
     auto block = [&](int kk) {                                 // of 16 tokens of U
       if constexpr (L::kBf16) {
         uint32_t hi[4], lo[4], b[2][4], bl[2][4];
@@ -906,7 +909,7 @@ struct Columns {
             for (int t = 0; t < 4; ++t)
               if (n <= 4 * half + t) {
                 const uint32_t(&f)[2] = m == 1 ? bl[t] : bh[t];
-                mma_tf32(I[t], m == 0 ? lo : hi, f[0], f[1]);
+                mma_tf32(kFull && m < 2 ? small[t < kSmall ? t : 0] : I[t], m == 0 ? lo : hi, f[0], f[1]);
               }
         }
       }
@@ -918,6 +921,12 @@ struct Columns {
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
         if (kk < 2 * half + 2) block(kk);
+    }
+    if constexpr (kFull) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) I[n][e] += small[n][e];
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -1000,7 +1009,7 @@ struct Columns {
       uint32_t hi[4], lo[4];
       handed_s(ks, hi, lo);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) multiply_q(smem + stage + L::kQAt, half, ks, hi, lo, O[half]);
+      for (int half = 0; half < 2; ++half) multiply_q<true, true>(smem + stage + L::kQAt, half, ks, hi, lo, O[half]);
     }
     await(1);
     const float2 ps = lane_pair<float2>(0), po = lane_pair<float2>(1);
@@ -1067,7 +1076,7 @@ struct Columns {
       }
       if constexpr (kBeside) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) multiply_q(qt, half, ks, hi, lo, O[half]);
+        for (int half = 0; half < 2; ++half) multiply_q<true, true>(qt, half, ks, hi, lo, O[half]);
       }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {                   // (four accumulators, so that a product does not wait for the one before)
@@ -1191,7 +1200,13 @@ struct Columns {
             for (int ks = 0; ks < DK / 16; ++ks) {
               uint32_t hi[4], lo[4];
               operand(S, ks, scale_s, hi, lo);
-              multiply_q(qt, half, ks, hi, lo, q_s);
+              multiply_q<true, false>(qt, half, ks, hi, lo, q_s);
+            }
+#pragma unroll
+            for (int ks = 0; ks < DK / 16; ++ks) {
+              uint32_t hi[4], lo[4];
+              operand(S, ks, scale_s, hi, lo);
+              multiply_q<false, true>(qt, half, ks, hi, lo, q_s);
             }
           }
           finish_o(stage + L::kPAt, w, half, q_s, per_s, per_o, [&](int n, float(&x)[4]) { scaled(U[n], scale, x); }, odd, from, at0 + (c & 1) * L::kV,
