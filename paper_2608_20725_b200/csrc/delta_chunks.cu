@@ -23,11 +23,12 @@
 // diagonal by substitution in fp32, the others by TF32 products too.  Against 64 bits the states of 600 tokens are off by 2.3e-7 of their norm (of fp32
 // rows by 3.3e-7, and o by 5.7e-7; token by token both are 2e-7).
 //
-// What bounds it (128 x 128, fp16): a chunk of 64 tokens takes a block of 32 columns 6.3 us (bf16), of 64 columns 7.4 (fp16); its chains alone 3.4 and
-// 5.1, a team alone, with every second chunk, about 10.  Both are some 4000 instructions a warp, one after the other at about five cycles each (what the products, 8 cycles of an SM's quarter each, take is
-// 2 us of the chain's).  The instruction cache is part of it: the code of a chunk, 80 KB of which each warp runs its own part, misses it 450 times a
-// chunk, which is why the helpers' code exists once and in loops.  One prompt of 16384 tokens, 32 heads of 128 x 128, bf16: 1610 us (62 at 6.56 TB/s), fp16
-// 1887; token by token 22200.  13 prompts of 9001 tokens, 24 heads of 64 x 128, fp16: 353 (22), token by token 4090.
+// What bounds it (128 x 128, bf16): a chunk of 64 tokens takes a block of 32 columns 6.1 to 6.5 us by the box; its chains and o alone 4.4, a team alone,
+// with every second chunk, 9.8.  Both are some 4000 instructions a warp, one after the other at about five cycles each (what the products, 8 cycles of an
+// SM's quarter each, take is 2 us of the chain's).  The instruction cache is part of it: the code of a chunk, some 80 KB of which each warp runs its own part,
+// misses it 500 times a chunk, which is why the code of helpers and of the warps that make o exists once and in loops.  One prompt of 16384 tokens, 32 heads
+// of 128 x 128, bf16: 1560 to 1660 us (62 at 6.56 TB/s), fp16 1535 to 1630; token by token 22200.  13 prompts of 9001 tokens, 24 heads of 64 x 128, fp16:
+// 364 (22), token by token 4090.
 //
 // Infinities and NaNs: a token whose k, beta or decay is not finite, and those behind it, get a beta of 0, a weight of NaN for o and a
 // decay of NaN for S.  A column whose R or U is not finite from some token on is cleaned from there on, before it meets the zeros of T and P, and its
@@ -106,11 +107,6 @@ struct Layout {
   template <bool SPLIT> static constexpr uint32_t kColumns = SPLIT ? kPairsAt + 3 * 256 : 2 * kV;
 };
 
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
 // A power of two that brings numbers of at most `top` to below 2^15, and its reciprocal.
 __device__ __forceinline__ float scale_for(float top) {
   const int e = (int)(__float_as_uint(top) >> 23 & 255u);
@@ -1370,9 +1366,9 @@ cudaError_t launch(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
-// The columns of a block: 32 while that gives no more blocks than there are SMs, 64 beyond.  (A chunk of 64 tokens, 128 x 128, takes a block of 32 columns
-// 6.3 us, of 64 columns 7.4.  Before the helpers' last step, bf16: one prompt of 16384 tokens, 32 heads, 1643 and 1960 us; four of 8192 tokens in all 849
-// and 583; 128 columns and one team 1136.)  fp32: its pieces leave shared memory for one team, and registers for o beside the chain.
+// The columns of a block: 32 while that gives no more blocks than there are SMs, 64 beyond.  (A chunk of 64 tokens, 128 x 128 in bf16, takes a block of
+// 32 columns 6.1 to 6.5 us; of 64 columns, with all SMs at work, 9.7: four prompts of 8192 tokens in all 620.)  fp32: its pieces leave shared memory
+// for one team, and registers for o beside the chain.
 template <typename T, int DK>
 cudaError_t launch_width(ChunkParams& p, int32_t sequences, cudaStream_t stream) {
   const bool wide = p.dv > 32 && (int64_t)sequences * p.heads * ((p.dv + 31) / 32) > 148;

@@ -32,13 +32,6 @@ struct NormParams {
   float eps;
 };
 
-// The larger one; a NaN is larger than anything.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-
 // 127 z / top, which lies within n .. n + 1 (but for what tells halves from one another), rounded to the nearest whole number, ties to the even one: by the
 // sign of 254 |z| - (2 n + 1) top.  z and top are products of two elements, exact in 64 bits; what they are multiplied by here brings fp32 ones to 56 bits.
 template <typename T>
