@@ -5,8 +5,9 @@ import math
 import pytest
 import torch
 
-from delta_helpers import run
-from sequence_helpers import DTYPES
+from delta_helpers import delta_64, run
+from paper_2608_20725_b200 import binding
+from sequence_helpers import DTYPES, close, rounding, sequence_list
 
 pytestmark = pytest.mark.gpu
 
@@ -109,3 +110,20 @@ def test_everything_small_or_large(dtype, size):
         v.mul_(size)
         st.mul_(size)
     check(dtype, [100], edit=edit)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_growth_beyond_the_range(dtype):
+    """Alike keys of beta |k|^2 of 20: a token's part in a later one grows by 19 a token and passes the range of floats some 30 tokens on.  Rows up to 15
+    before that are right, of the others each is, or is not finite."""
+    gen, tdt = torch.Generator().manual_seed(3), DTYPES[dtype]
+    q, v = (torch.randn(40, 1, 64, generator=gen).to(tdt) for _ in range(2))
+    k = (torch.ones(40, 1, 64) / 8).to(tdt)
+    g, beta = torch.zeros(1), torch.full((1,), 20.0)
+    o = torch.zeros(40, 1, 64, dtype=tdt, device="cuda")
+    binding.im2win_gated_delta_rule(*(x.cuda() for x in (q, k, v, g, beta)), o, scale=0.125, cu_seqlens=torch.tensor([0, 40], dtype=torch.int32, device="cuda"))
+    want, off = delta_64(q, k, v, g, beta, 0.125, False, torch.zeros(40, 1, 64), None, None, sequence_list([40]), 1,
+                         0.0 if dtype == "f32" else 3 * 2.0 ** -18)[:2]
+    off, got = off + rounding(want, tdt), o.double().cpu()
+    close(got[:14], want[:14], off[:14], "o")
+    assert bool((((got - want).abs() <= off) | ~torch.isfinite(got)).all())
